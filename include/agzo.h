@@ -271,6 +271,56 @@ int agzo_glue_swiglu(agzo_ctx* ctx, const void* a, int64_t lda, const void* u, i
                      int64_t d);
 int agzo_glue_add(agzo_ctx* ctx, void* h, int64_t ldh, const void* delta, int64_t ldd, int64_t n, int64_t d);
 
+/* Packed batches: sequences of different lengths back to back, without padding (bf16 device tensors as above; head_dim 64 or 128).
+ * These calls need the device that is current to be the context's.  They use the context's workspace, which cannot grow while the
+ * stream is captured: a call that would have to make it larger then is refused with AGZO_ENOMEM and enqueues nothing (make the call once
+ * before the capture).  A workspace that a captured call uses stays allocated until agzo_destroy, also where the context's grows
+ * later; graphs captured from one context share it and must not run at the same time.
+ *
+ * qk_norm_rope: norms of queries and keys for each head with the rotation by the token's position in one pass.  For the head_dim = D
+ *   values x of a head, n = gain x / sqrt(mean(x^2) + eps) (gain: device fp32 [D], the same for all heads, NULL = 1), then the pair
+ *   (n_i, n_{i + D/2}) turned by the angle positions[t] rope_theta^(-2i/D), in fp32 with one rounding to bf16; angles are reduced
+ *   in fp64, so that far positions (any int32) keep their fractions.  q [n][n_heads D] -> q_out, k [n][n_kv_heads D] -> k_out; either side
+ *   may be left out with 0 heads.  An output may be its own input (same pointer and leading dimension) and may not overlap
+ *   any tensor otherwise.  positions: device int32 [n].
+ * qk_norm_rope_backward: from the gradients dq_out, dk_out with respect to its results, those with respect to q, k (dq, dk) and, where wanted
+ *   (not NULL), to the gains (fp32 [D], sums over tokens and heads in a fixed order, overwritten).  q and k are the inputs of the forward
+ *   call.  dq may be dq_out or q (and dk dk_out or k), and may not overlap any tensor otherwise. */
+int agzo_glue_qk_norm_rope(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out,
+                           int64_t ldqo, void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const float* q_gain, const float* k_gain, float eps, float rope_theta);
+int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions,
+                                    const void* dq_out, int64_t lddqo, const void* dk_out, int64_t lddko, void* dq, int64_t lddq,
+                                    void* dk, int64_t lddk, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                    const float* q_gain, const float* k_gain, float* dq_gain, float* dk_gain, float eps, float rope_theta);
+
+/* Attention over packed sequences with grouped heads.  Sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the keys and values cu_k[s] ..
+ * cu_k[s + 1] - 1 (device int32 [n_seq + 1], not decreasing, within 0 .. n_q and 0 .. n_k: offsets outside are taken as the nearest inside);
+ * its queries are its last positions: with causal != 0 query i of Lq sees the keys 0 .. i + Lk - Lq of Lk, else all Lk.  Lq = Lk is a prompt,
+ * Lq = 1 a new token behind the keys that are there.  out = softmax(scale q k^T) v for each head (head h reads key head h / (n_heads / n_kv_heads)); the
+ * probabilities are rounded to bf16 for the second product, sums are fp32.  A query that sees no key (Lk < Lq, or no keys at all) gets 0
+ * and takes part in no gradient.  Values of keys that a query does not see have no part in its result, whatever they are (NaN and
+ * infinities too).  Rows of no sequence are neither read nor written.
+ *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key
+ *   backward: out, lse of the forward call with the same arguments and the gradient dout -> dq, dk, dv (all three written, for all rows of
+ *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
+ * Inputs are only read; outputs may not overlap inputs or each other.
+ * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, counts of 2^31 and more, leading
+ * dimensions from 2^22 on), scale not positive and finite, overlapping outputs. */
+typedef struct {
+    const void *q, *k, *v;       /* [n_q][n_heads head_dim], [n_k][n_kv_heads head_dim] twice */
+    int64_t ldq, ldk, ldv;
+    const int32_t *cu_q, *cu_k;
+    int64_t n_q, n_k;            /* rows of the tensors */
+    int32_t n_seq, n_heads, n_kv_heads, head_dim;
+    int32_t causal;
+    float scale;
+} agzo_packed_attention;
+int agzo_glue_attention_packed(agzo_ctx* ctx, const agzo_packed_attention* a, void* out, int64_t ldo, float* lse);
+int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attention* a, const void* out, int64_t ldo, const float* lse,
+                                        const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
+                                        int64_t lddv);
+
 /* Alg. 2 for n independent single-layer problems in one call (a layer set whose projections each have their own loss
  * and their own scalar g): every layer's base forward, all bases together (as agzo_basis_many), all projections X B
  * in one launch, the perturbed forwards, every scalar, and all updates in one batched sweep (as agzo_update_many).

@@ -28,7 +28,8 @@ EXPORTS = ["agzo_create", "agzo_destroy", "agzo_last_error", "agzo_check", "agzo
            "agzo_profile_read", "agzo_profile_clock", "agzo_probe_mfma", "agzo_philox_words", "agzo_fill_normal",
            "agzo_layer_forward_sketch", "agzo_qr", "agzo_basis", "agzo_perturbed_forward", "agzo_two_point", "agzo_dense_perturb", "agzo_update", "agzo_update_noalloc",
            "agzo_update_many", "agzo_step", "agzo_step_no_update", "agzo_basis_many", "agzo_step_many",
-           "agzo_glue_rmsnorm", "agzo_glue_swiglu", "agzo_glue_add", "agzo_glue_attention"]
+           "agzo_glue_rmsnorm", "agzo_glue_swiglu", "agzo_glue_add", "agzo_glue_attention",
+           "agzo_glue_qk_norm_rope", "agzo_glue_qk_norm_rope_backward", "agzo_glue_attention_packed", "agzo_glue_attention_packed_backward"]
 
 
 class AgzoLayer(ctypes.Structure):
@@ -58,6 +59,14 @@ class AgzoBasisItem(ctypes.Structure):
 class AgzoStepItem(ctypes.Structure):
     _fields_ = [("layer", AgzoLayer), ("W", ctypes.c_void_p), ("X", ctypes.c_void_p), ("loss", AgzoLossSpec),
                 ("seed", ctypes.c_uint64), ("out_dev", ctypes.c_void_p), ("B_out", ctypes.c_void_p)]
+
+
+class AgzoPackedAttention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64),
+                ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p), ("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64),
+                ("n_seq", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class AgzoError(RuntimeError):
@@ -108,6 +117,11 @@ def load():
     lib.agzo_glue_swiglu.argtypes = [vp, vp, i64, vp, i64, vp, i64, i64, i64]
     lib.agzo_glue_add.argtypes = [vp, vp, i64, vp, i64, i64, i64]
     lib.agzo_glue_attention.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, f32]
+    pp = ctypes.POINTER(AgzoPackedAttention)
+    lib.agzo_glue_qk_norm_rope.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, f32, f32]
+    lib.agzo_glue_qk_norm_rope_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, f32, f32]
+    lib.agzo_glue_attention_packed.argtypes = [vp, pp, vp, i64, vp]
+    lib.agzo_glue_attention_packed_backward.argtypes = [vp, pp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64]
     lib.agzo_step.argtypes = [vp, lp, vp, vp, sp, i32, f32, f32, u64, i32, vp]
     lib.agzo_step_no_update.argtypes = [vp, lp, vp, vp, sp, i32, f32, u64, i32, vp, vp]
     for name in EXPORTS:
@@ -127,6 +141,34 @@ def _dt(t):
     if t.dtype == torch.bfloat16:
         return BF16
     raise TypeError("unsupported dtype %s" % t.dtype)
+
+
+def _rows(t, name):
+    """(pointer, leading dimension) of a bf16 matrix; of None, nothing."""
+    if t is None:
+        return None, 0
+    if t.dtype != torch.bfloat16:
+        raise TypeError("%s must be bfloat16, not %s" % (name, t.dtype))
+    if t.dim() != 2 or (t.numel() and t.stride(1) != 1 and t.shape[1] != 1):
+        raise ValueError("%s must be a matrix with unit stride along its last axis" % name)
+    # (the stride of a single row says nothing)
+    return _ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _flat(t, name, dtype, numel):
+    """Pointer of a contiguous tensor of so many values; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if t.numel() != numel or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous values" % (name, numel))
+    return _ptr(t)
+
+
+def _same_shape(name, t, like):
+    if t is not None and (like is None or t.shape != like.shape):
+        raise ValueError("%s must have the shape %s" % (name, None if like is None else tuple(like.shape)))
 
 
 def make_layer(W=None, X=None, r=1, Y=None, d_out=None):
@@ -314,6 +356,75 @@ class Context:
         n_heads, n_kv = q.shape[1] // 128, k.shape[1] // 128
         self._rc(self.lib.agzo_glue_attention(self.h, _ptr(q), q.stride(0), _ptr(k), k.stride(0), _ptr(v), v.stride(0),
                                               _ptr(out), out.stride(0), n_seq, seq_len, n_heads, n_kv, rope_theta))
+
+    def _same_device(self, *tensors):
+        for t in tensors:
+            if t is not None and t.device != self.stream.device:
+                raise ValueError("a tensor on %s, and the context is of %s" % (t.device, self.stream.device))
+
+    def glue_qk_norm_rope(self, q, k, positions, q_out, k_out, head_dim=128, q_gain=None, k_gain=None, eps=1e-6, rope_theta=1.0e6):
+        """q [n][heads * head_dim], k [n][key heads * head_dim] -> q_out, k_out; either side may be None with its result."""
+        n = (q if q is not None else k).shape[0]
+        self._same_device(q, k, positions, q_out, k_out, q_gain, k_gain)
+        heads, kv = self._heads(q, k, head_dim, n)
+        for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+            _same_shape(name, t, like)
+        self._rc(self.lib.agzo_glue_qk_norm_rope(self.h, *_rows(q, "q"), *_rows(k, "k"), _flat(positions, "positions", torch.int32, n), *_rows(q_out, "q_out"),
+                                                 *_rows(k_out, "k_out"), n, heads, kv, head_dim, _flat(q_gain, "q_gain", torch.float32, head_dim),
+                                                 _flat(k_gain, "k_gain", torch.float32, head_dim), eps, rope_theta))
+
+    def glue_qk_norm_rope_backward(self, q, k, positions, dq_out, dk_out, dq, dk, head_dim=128, q_gain=None, k_gain=None, dq_gain=None, dk_gain=None,
+                                   eps=1e-6, rope_theta=1.0e6):
+        n = (q if q is not None else k).shape[0]
+        self._same_device(q, k, positions, dq_out, dk_out, dq, dk, q_gain, k_gain, dq_gain, dk_gain)
+        heads, kv = self._heads(q, k, head_dim, n)
+        for name, t, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k), ("dq", dq, q), ("dk", dk, k)):
+            _same_shape(name, t, like)
+        f32 = torch.float32
+        self._rc(self.lib.agzo_glue_qk_norm_rope_backward(
+            self.h, *_rows(q, "q"), *_rows(k, "k"), _flat(positions, "positions", torch.int32, n), *_rows(dq_out, "dq_out"), *_rows(dk_out, "dk_out"),
+            *_rows(dq, "dq"), *_rows(dk, "dk"), n, heads, kv, head_dim, _flat(q_gain, "q_gain", f32, head_dim), _flat(k_gain, "k_gain", f32, head_dim),
+            _flat(dq_gain, "dq_gain", f32, head_dim), _flat(dk_gain, "dk_gain", f32, head_dim), eps, rope_theta))
+
+    @staticmethod
+    def _heads(q, k, head_dim, n):
+        out = []
+        for t in (q, k):
+            if t is not None and (t.shape[0] != n or t.shape[1] % head_dim):
+                raise ValueError("rows of %d values, %d of them: need %d of a multiple of %d" % (t.shape[1], t.shape[0], n, head_dim))
+            out.append(0 if t is None else t.shape[1] // head_dim)
+        return out
+
+    def _packed(self, q, k, v, cu_q, cu_k, head_dim, scale, causal):
+        _same_shape("v", v, k)
+        a = AgzoPackedAttention()
+        (a.q, a.ldq), (a.k, a.ldk), (a.v, a.ldv) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+        if q.shape[1] % head_dim or k.shape[1] % head_dim:
+            raise ValueError("rows of %d and %d values: need multiples of %d" % (q.shape[1], k.shape[1], head_dim))
+        a.n_q, a.n_k, a.n_seq = q.shape[0], k.shape[0], cu_q.numel() - 1
+        a.cu_q, a.cu_k = _flat(cu_q, "cu_q", torch.int32, a.n_seq + 1), _flat(cu_k, "cu_k", torch.int32, a.n_seq + 1)
+        a.n_heads, a.n_kv_heads, a.head_dim = q.shape[1] // head_dim, k.shape[1] // head_dim, head_dim
+        a.causal, a.scale = int(causal), head_dim ** -0.5 if scale is None else scale
+        return a
+
+    def glue_attention_packed(self, q, k, v, out, cu_q, cu_k, head_dim=128, scale=None, causal=True, lse=None):
+        """q [n_q][heads * head_dim], k, v [n_k][key heads * head_dim] -> out like q; cu_q, cu_k: int32 offsets of the sequences
+        (n_seq + 1 each); scale None: head_dim ** -0.5; lse: float32 [n_q][heads] or None."""
+        self._same_device(q, k, v, out, cu_q, cu_k, lse)
+        a = self._packed(q, k, v, cu_q, cu_k, head_dim, scale, causal)
+        _same_shape("out", out, q)
+        o, ldo = _rows(out, "out")
+        self._rc(self.lib.agzo_glue_attention_packed(self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, a.n_q * a.n_heads)))
+
+    def glue_attention_packed_backward(self, q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, head_dim=128, scale=None, causal=True):
+        """out, lse: of glue_attention_packed with the same arguments; dout: the gradient with respect to out -> dq, dk, dv."""
+        self._same_device(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k)
+        a = self._packed(q, k, v, cu_q, cu_k, head_dim, scale, causal)
+        for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+            _same_shape(name, t, like)
+        (o, ldo), (do, lddo) = _rows(out, "out"), _rows(dout, "dout")
+        self._rc(self.lib.agzo_glue_attention_packed_backward(
+            self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, a.n_q * a.n_heads), do, lddo, *_rows(dq, "dq"), *_rows(dk, "dk"), *_rows(dv, "dv")))
 
     def step_no_update(self, L, W, X, loss, K, eps, seed, flags, out_dev, B_out):
         self._rc(self.lib.agzo_step_no_update(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), K, eps,

@@ -34,6 +34,8 @@ struct agzo_ctx {
     char err[512];
     char* ws;
     size_t ws_bytes;
+    bool ws_captured;             // a captured graph uses it
+    std::vector<char*> retired;   // such workspaces that a growth has replaced
     int* flag;   // device int: deferred numeric failure
     uint32_t prof;      // mask of timed kernel classes (bit = AGZO_PROF_* value)
     ProfClass pc[AGZO_PROF_KINDS];
@@ -186,10 +188,25 @@ Plan make_forward_plan(const agzo_layer& L, const agzo_loss_spec* loss, bool fus
 
 // wish: what a growth is to cover as well where there is room (grow.h)
 int reserve(agzo_ctx* ctx, size_t bytes, size_t wish = 0) {
-    if (bytes <= ctx->ws_bytes) return 0;
+    if (bytes == 0) return 0;
+    // (the default stream cannot be captured)
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (ctx->stream && hipStreamIsCapturing(ctx->stream, &capture) != hipSuccess) (void)hipGetLastError();
+    const bool captured = capture != hipStreamCaptureStatusNone;
+    if (bytes <= ctx->ws_bytes) {
+        ctx->ws_captured = ctx->ws_captured || captured;
+        return 0;
+    }
+    if (captured) return fail(ctx, AGZO_ENOMEM, "a workspace of %zu bytes, and it cannot grow while the stream is captured: make the call once before", bytes);
     HIPCHK(hipStreamSynchronize(ctx->stream));
     if (ctx->side) HIPCHK(hipStreamSynchronize(ctx->side));      // (joined to the above, unless joining failed)
-    if (ctx->ws) HIPCHK(hipFree(ctx->ws));
+    if (ctx->ws_captured) {
+        try { ctx->retired.push_back(ctx->ws); }
+        catch (...) { return fail(ctx, AGZO_ENOMEM, "out of host memory"); }
+        ctx->ws_captured = false;
+    } else if (ctx->ws) {
+        HIPCHK(hipFree(ctx->ws));
+    }
     const size_t had = ctx->ws_bytes;
     ctx->ws = nullptr;
     ctx->ws_bytes = 0;
@@ -696,6 +713,7 @@ int agzo_create(agzo_ctx** out, void* hip_stream) {
     ctx->err[0] = 0;
     ctx->ws = nullptr;
     ctx->ws_bytes = 0;
+    ctx->ws_captured = false;
     ctx->flag = nullptr;
     ctx->prof = 0;
     ctx->clk = nullptr;
@@ -738,6 +756,7 @@ void agzo_destroy(agzo_ctx* ctx) {
     if (ctx->fork) (void)hipEventDestroy(ctx->fork);
     if (ctx->join) (void)hipEventDestroy(ctx->join);
     if (ctx->ws) (void)hipFree(ctx->ws);
+    for (char* ws : ctx->retired) (void)hipFree(ws);
     if (ctx->flag) (void)hipFree(ctx->flag);
     if (ctx->clk) (void)hipFree(ctx->clk);
     for (auto& pc : ctx->pc) {
@@ -1339,6 +1358,133 @@ int agzo_glue_attention(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k
     TRY(reserve(ctx, glue_attention_workspace_bytes(n_seq, seq_len, n_heads, n_kv_heads, copies), (size_t)n * (n_heads + 2 * n_kv_heads) * 256));
     HIPCHK(launch_glue_attention(static_cast<const bf16_t*>(q), ldq, static_cast<const bf16_t*>(k), ldk, static_cast<const bf16_t*>(v), ldv,
                                  static_cast<bf16_t*>(out), ldo, n_seq, seq_len, n_heads, n_kv_heads, rope_theta, ctx->ws, ctx->stream));
+    return AGZO_OK;
+}
+
+namespace {
+// the calls on packed batches: launches go to the current device
+int check_device(agzo_ctx* ctx) {
+    int dev = -1;
+    HIPCHK(hipGetDevice(&dev));
+    if (dev != ctx->device) return fail(ctx, AGZO_EINVAL, "device %d is current, the context is of device %d", dev, ctx->device);
+    return 0;
+}
+
+struct Named { const char* name; Rows rows; };
+Named named(const char* name, const void* at, int64_t ld, int64_t n, int64_t d) { return Named{name, Rows{reinterpret_cast<uintptr_t>(at), 2 * ld, at ? n : 0, 2 * d}}; }
+// outputs that overlap each other or an input; in_place: inputs that an output may be (NULL: none), as pairs of indices
+int check_apart(agzo_ctx* ctx, std::initializer_list<Named> outs, std::initializer_list<Named> ins, std::initializer_list<std::pair<int, int>> in_place = {}) {
+    int o = 0;
+    for (const Named& a : outs) {
+        for (const Named* b = outs.begin() + o + 1; b != outs.end(); ++b)
+            if (rows_overlap(a.rows, b->rows)) return fail(ctx, AGZO_EINVAL, "%s and %s overlap", a.name, b->name);
+        int i = 0;
+        for (const Named& b : ins) {
+            const bool same = a.rows.at == b.rows.at && a.rows.ld == b.rows.ld;
+            bool allowed = false;
+            for (const auto& p : in_place) allowed = allowed || (same && p.first == o && p.second == i);
+            if (!allowed && rows_overlap(a.rows, b.rows)) return fail(ctx, AGZO_EINVAL, "%s and %s overlap", a.name, b.name);
+            ++i;
+        }
+        ++o;
+    }
+    return 0;
+}
+
+int check_norm_rope(agzo_ctx* ctx, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions, float eps, float rope_theta) {
+    if (!ctx) return AGZO_EINVAL;
+    if (n_heads < 0 || n_kv_heads < 0 || n_heads > 65535 || n_kv_heads > 65535 || (head_dim != 64 && head_dim != 128))
+        return fail(ctx, AGZO_EINVAL, "%d heads, %d key heads of %d values", n_heads, n_kv_heads, head_dim);
+    if (n < 0 || n > 0x7FFFFFFFLL) return fail(ctx, AGZO_EINVAL, "%lld tokens", (long long)n);
+    if (n > 0 && !positions) return fail(ctx, AGZO_EINVAL, "positions is NULL");
+    if (reinterpret_cast<uintptr_t>(positions) & 3) return fail(ctx, AGZO_EINVAL, "positions is misaligned");
+    if (!(eps >= 0.f) || !(eps < INFINITY)) return fail(ctx, AGZO_EINVAL, "eps must be finite and not negative");
+    if (!(rope_theta > 1.f) || !(rope_theta < INFINITY)) return fail(ctx, AGZO_EINVAL, "rope_theta must be finite and exceed 1");
+    return check_device(ctx);
+}
+
+int packed_args(agzo_ctx* ctx, const agzo_packed_attention* a, PackedArgs& out) {
+    if (!ctx) return AGZO_EINVAL;
+    if (!a) return fail(ctx, AGZO_EINVAL, "the attention's descriptor is NULL");
+    if (a->n_heads < 1 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads || a->n_heads > 65535 || (a->head_dim != 64 && a->head_dim != 128) || a->n_seq < 0)
+        return fail(ctx, AGZO_EINVAL, "bad attention shape: %d sequences, %d heads of %d values on %d key heads", a->n_seq, a->n_heads, a->head_dim, a->n_kv_heads);
+    if (a->n_q < 0 || a->n_k < 0 || a->n_k > 0x7FFFFFFFLL || a->n_q * (a->n_heads / a->n_kv_heads) > 0x7FFFFFFFLL || a->n_q > 0x7FFFFFFFLL)
+        return fail(ctx, AGZO_EINVAL, "%lld queries, %lld keys: too many", (long long)a->n_q, (long long)a->n_k);
+    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return fail(ctx, AGZO_EINVAL, "scale must be positive and finite");
+    if (a->ldq >= (1LL << 22) || a->ldk >= (1LL << 22) || a->ldv >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "leading dimensions must be below 2^22");
+    if (a->n_seq > 0 && (!a->cu_q || !a->cu_k || ((reinterpret_cast<uintptr_t>(a->cu_q) | reinterpret_cast<uintptr_t>(a->cu_k)) & 3)))
+        return fail(ctx, AGZO_EINVAL, "cu_q or cu_k is NULL or misaligned");
+    const int64_t dq = (int64_t)a->n_heads * a->head_dim, dkv = (int64_t)a->n_kv_heads * a->head_dim;
+    TRY(check_glue(ctx, a->n_q, dq, {a->q}, {a->ldq}));
+    TRY(check_glue(ctx, a->n_k, dkv, {a->k, a->v}, {a->ldk, a->ldv}));
+    out = PackedArgs{static_cast<const bf16_t*>(a->q), static_cast<const bf16_t*>(a->k), static_cast<const bf16_t*>(a->v), a->ldq, a->ldk, a->ldv,
+                     a->cu_q, a->cu_k, a->n_q, a->n_k, a->n_seq, a->n_heads, a->n_kv_heads, a->causal != 0, a->scale};
+    return check_device(ctx);
+}
+}  // namespace
+
+int agzo_glue_qk_norm_rope(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out,
+                           int64_t ldqo, void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const float* q_gain, const float* k_gain, float eps, float rope_theta) {
+    TRY(check_norm_rope(ctx, n, n_heads, n_kv_heads, head_dim, positions, eps, rope_theta));
+    const int64_t dq = (int64_t)n_heads * head_dim, dk = (int64_t)n_kv_heads * head_dim;
+    TRY(check_glue(ctx, n, dq, {q, q_out}, {ldq, ldqo}));
+    TRY(check_glue(ctx, n, dk, {k, k_out}, {ldk, ldko}));
+    TRY(check_apart(ctx, {named("q_out", q_out, ldqo, n, dq), named("k_out", k_out, ldko, n, dk)}, {named("q", q, ldq, n, dq), named("k", k, ldk, n, dk)}, {{0, 0}, {1, 1}}));
+    HIPCHK(launch_norm_rope(NormRopeSide{static_cast<const bf16_t*>(q), ldq, static_cast<bf16_t*>(q_out), ldqo, q_gain, n_heads},
+                            NormRopeSide{static_cast<const bf16_t*>(k), ldk, static_cast<bf16_t*>(k_out), ldko, k_gain, n_kv_heads}, positions, n, head_dim, eps,
+                            rope_theta, ctx->stream));
+    return AGZO_OK;
+}
+
+int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions,
+                                    const void* dq_out, int64_t lddqo, const void* dk_out, int64_t lddko, void* dq, int64_t lddq,
+                                    void* dk, int64_t lddk, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                    const float* q_gain, const float* k_gain, float* dq_gain, float* dk_gain, float eps, float rope_theta) {
+    TRY(check_norm_rope(ctx, n, n_heads, n_kv_heads, head_dim, positions, eps, rope_theta));
+    const int64_t wq = (int64_t)n_heads * head_dim, wk = (int64_t)n_kv_heads * head_dim;
+    TRY(check_glue(ctx, n, wq, {q, dq_out, dq}, {ldq, lddqo, lddq}));
+    TRY(check_glue(ctx, n, wk, {k, dk_out, dk}, {ldk, lddko, lddk}));
+    TRY(check_apart(ctx, {named("dq", dq, lddq, n, wq), named("dk", dk, lddk, n, wk)},
+                    {named("q", q, ldq, n, wq), named("dq_out", dq_out, lddqo, n, wq), named("k", k, ldk, n, wk), named("dk_out", dk_out, lddko, n, wk)},
+                    {{0, 0}, {0, 1}, {1, 2}, {1, 3}}));
+    if (dq_gain && dq_gain == dk_gain) return fail(ctx, AGZO_EINVAL, "dq_gain and dk_gain overlap");
+    if (dq_gain || dk_gain) TRY(reserve(ctx, norm_rope_workspace_bytes(n, head_dim)));
+    HIPCHK(launch_norm_rope_grad(NormRopeSide{static_cast<const bf16_t*>(q), ldq, static_cast<bf16_t*>(dq), lddq, q_gain, n_heads, static_cast<const bf16_t*>(dq_out), lddqo},
+                                 NormRopeSide{static_cast<const bf16_t*>(k), ldk, static_cast<bf16_t*>(dk), lddk, k_gain, n_kv_heads, static_cast<const bf16_t*>(dk_out), lddko},
+                                 positions, n, head_dim, eps, rope_theta, dq_gain, dk_gain, ctx->ws, ctx->stream));
+    return AGZO_OK;
+}
+
+int agzo_glue_attention_packed(agzo_ctx* ctx, const agzo_packed_attention* a, void* out, int64_t ldo, float* lse) {
+    PackedArgs p;
+    TRY(packed_args(ctx, a, p));
+    const int64_t dq = (int64_t)a->n_heads * a->head_dim, dkv = (int64_t)a->n_kv_heads * a->head_dim;
+    TRY(check_glue(ctx, a->n_q, dq, {out}, {ldo}));
+    if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
+    TRY(check_apart(ctx, {named("out", out, ldo, a->n_q, dq)}, {named("q", a->q, a->ldq, a->n_q, dq), named("k", a->k, a->ldk, a->n_k, dkv), named("v", a->v, a->ldv, a->n_k, dkv)}));
+    TRY(reserve(ctx, packed_forward_workspace_bytes(p, a->head_dim)));
+    HIPCHK(launch_packed_forward(p, a->head_dim, static_cast<bf16_t*>(out), ldo, lse, ctx->ws, ctx->stream));
+    return AGZO_OK;
+}
+
+int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attention* a, const void* out, int64_t ldo, const float* lse,
+                                        const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
+                                        int64_t lddv) {
+    PackedArgs p;
+    TRY(packed_args(ctx, a, p));
+    const int64_t wq = (int64_t)a->n_heads * a->head_dim, wk = (int64_t)a->n_kv_heads * a->head_dim;
+    TRY(check_glue(ctx, a->n_q, wq, {out, dout, dq}, {ldo, lddo, lddq}));
+    TRY(check_glue(ctx, a->n_k, wk, {dk, dv}, {lddk, lddv}));
+    if (lddo >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "leading dimensions must be below 2^22");
+    if (a->n_q > 0 && (!lse || (reinterpret_cast<uintptr_t>(lse) & 3))) return fail(ctx, AGZO_EINVAL, "lse is NULL or misaligned");
+    TRY(check_apart(ctx, {named("dq", dq, lddq, a->n_q, wq), named("dk", dk, lddk, a->n_k, wk), named("dv", dv, lddv, a->n_k, wk)},
+                    {named("q", a->q, a->ldq, a->n_q, wq), named("k", a->k, a->ldk, a->n_k, wk), named("v", a->v, a->ldv, a->n_k, wk),
+                     named("out", out, ldo, a->n_q, wq), named("dout", dout, lddo, a->n_q, wq)}));
+    TRY(reserve(ctx, packed_backward_workspace_bytes(p)));
+    const PackedGrad g{static_cast<const bf16_t*>(out), static_cast<const bf16_t*>(dout), ldo, lddo, lse, static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk),
+                       static_cast<bf16_t*>(dv), lddq, lddk, lddv};
+    HIPCHK(launch_packed_backward(p, a->head_dim, g, ctx->ws, ctx->stream));
     return AGZO_OK;
 }
 

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "agzo.h"
 
 namespace agzo {
@@ -367,6 +369,36 @@ size_t glue_attention_workspace_bytes(int n_seq, int seq_len, int n_heads, int n
 hipError_t launch_glue_attention(const bf16_t* q, int64_t ldq, const bf16_t* k, int64_t ldk, const bf16_t* v, int64_t ldv,
                                  bf16_t* out, int64_t ldo, int n_seq, int seq_len, int n_heads, int n_kv, float rope_theta,
                                  void* workspace, hipStream_t st);
+
+// glue_norm_rope.hip : norms of queries and keys for each head (64 or 128 values, gain [head_dim] or NULL) with the rotation by positions [n], rows [n][heads head_dim] bf16
+struct NormRopeSide {
+    const bf16_t* x; int64_t ldx;
+    bf16_t* y; int64_t ldy;            // forward: the result; backward: dx
+    const float* gain; int heads;
+    const bf16_t* dy = nullptr; int64_t lddy = 0;
+};
+size_t norm_rope_workspace_bytes(int64_t n, int head_dim);      // of the backward pass, where a gain's gradient is wanted
+hipError_t launch_norm_rope(const NormRopeSide& q, const NormRopeSide& k, const int32_t* positions, int64_t n, int head_dim, float eps, float theta, hipStream_t st);
+hipError_t launch_norm_rope_grad(const NormRopeSide& q, const NormRopeSide& k, const int32_t* positions, int64_t n, int head_dim, float eps, float theta,
+                                 float* dq_gain, float* dk_gain, void* workspace, hipStream_t st);
+
+// glue_packed.hip : attention over packed sequences, q [total_q][n_heads head_dim], k, v [total_k][n_kv head_dim] bf16, head_dim 64 or 128
+struct PackedArgs {
+    const bf16_t *q, *k, *v;
+    int64_t ldq, ldk, ldv;
+    const int32_t *cu_q, *cu_k;        // [n_seq + 1]
+    int64_t total_q, total_k;          // below 2^31, as total_q n_heads / n_kv
+    int n_seq, n_heads, n_kv, causal;
+    float scale;
+};
+struct PackedGrad {
+    const bf16_t *out, *dout; int64_t ldo, lddo; const float* lse;
+    bf16_t *dq, *dk, *dv; int64_t lddq, lddk, lddv;
+};
+size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim);
+hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st);
+size_t packed_backward_workspace_bytes(const PackedArgs& a);
+hipError_t launch_packed_backward(const PackedArgs& a, int head_dim, const PackedGrad& g, void* workspace, hipStream_t st);
 
 // probe.hip : register-only MFMA loop for measuring the sustained matrix rate and shader clock of the device;
 // clk4: four 64-bit words for the counters plus 1 KiB that the kernel may (never does) write behind them

@@ -1,0 +1,792 @@
+// Attention over packed sequences of different lengths, with grouped heads: a sequence's queries are its last positions, its keys all of them,
+//     o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i k_j - lse_i),  lse_i = log sum_j exp(scale q_i k_j),  j <= i + (keys - queries) if causal,
+// and back, with delta_i = do_i o_i:
+//     dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
+// the sums over i going through all heads of j's group too.
+//
+// Rows.  The heads of a group see the same keys, so a row is a (query, head) pair, row r of a sequence and key head being head r mod G of query
+// r / G (G heads to a group).  A tile of rows is full whether it holds many queries or a single one with its group's heads, and no
+// sum of the gradients crosses workgroups.
+//
+// All products are v_mfma_f32_32x32x16_bf16 over tiles of 32 and are made transposed: a lane holds, for ONE row (forward, dq) or ONE key (dk, dv),
+// column lane % 32 of the instruction, the scores of positions 8 (e / 4) + 4 (lane / 32) + e % 4 of the other side.  So what belongs to a row is
+// a lane's scalar, and the eight values of each 16 positions that a lane holds go into the second product as they are, whose other
+// operand is read from LDS with a transposition in the same order of positions.
+//
+// What a masked place holds takes part in nothing: scores there are replaced, not added to.  Only the second products multiply a
+// masked place's values, by 0, of which a value that is not finite makes a NaN.  Where a workgroup's results are not finite it goes over
+// its tiles once more with care: masked tiles then have such values taken out, and what the visible ones amount to is found by a product of two
+// indicators.
+#include "agzo_internal.h"
+
+namespace agzo {
+
+namespace {
+
+typedef __bf16 pk_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float pk_floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t pk_u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void* pk_lptr;
+typedef const __attribute__((address_space(1))) void* pk_gptr;
+union PkFrag { uint4 u; uint32_t w[4]; pk_bf16x8 v; };
+
+constexpr int PK_T = 64;                    // positions of a tile in LDS
+constexpr float PK_LOG2E = 1.44269504088896341f, PK_LN2 = 0.693147180559945309f;
+
+__device__ __forceinline__ pk_floatx16 pk_mfma(const PkFrag& a, const PkFrag& b, const pk_floatx16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ float pk_max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pk_sum_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A tile of 64 positions of HD values, 16-byte chunk c of row r at place c ^ swz(r).  Reads of 16 rows' same chunk, and reads with
+// transposition of 4 rows' four neighbouring chunks, then meet each bank once
+template <int HD>
+__device__ __forceinline__ int pk_swz(int r) { return HD == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3); }
+
+// Byte offsets, in a tile, of what a lane reads.  rows: chunk (lane / 32) of row lane % 32 (chunk 2 ks + lane / 32: ^ ks << 5; rows 32 further on: + 32
+// rows' bytes).  trans: for 16 positions, those 4 (lane / 32) .. + 4 of the first eight and of the second eight, dims 0 .. 32 (32 db ..: ^ db << 6;
+// 16 positions further on: + 16 rows' bytes)
+template <int HD>
+struct PkOffsets {
+    int rows, trans[2];
+    __device__ __forceinline__ PkOffsets() {
+        const int lane = threadIdx.x & 63, r = lane & 31, hi = lane >> 5, n16 = lane & 15, dg = (lane >> 4) & 1;
+        rows = r * (HD * 2) + ((hi ^ pk_swz<HD>(r)) << 4);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int tr = 8 * s + 4 * hi + (n16 >> 2);
+            trans[s] = tr * (HD * 2) + (((2 * dg + ((n16 & 3) >> 1)) ^ pk_swz<HD>(tr)) << 4) + (n16 & 1) * 8;
+        }
+    }
+};
+
+// four fragments with transposition (positions x dims): for HD = 128 the four groups of 32 dims of 16 positions, for HD = 64 the two of each of
+// two times 16 positions.  One statement with its wait: behind the builtin's the compiler waits for every direct load in flight
+template <int HD>
+__device__ __forceinline__ void pk_read_trans(uint32_t base, const PkOffsets<HD>& o, PkFrag (&f)[4]) {
+    pk_u32x2 lo[4], hi[4];
+    uint32_t at[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) at[i][s] = base + (HD == 128 ? (uint32_t)(o.trans[s] ^ (i << 6)) : (uint32_t)((o.trans[s] ^ ((i & 1) << 6)) + (i >> 1) * 16 * HD * 2));
+    asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\t"
+                 "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11\n\t"
+                 "ds_read_b64_tr_b16 %4, %12\n\tds_read_b64_tr_b16 %5, %13\n\t"
+                 "ds_read_b64_tr_b16 %6, %14\n\tds_read_b64_tr_b16 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3])
+                 : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "v"(at[3][0]), "v"(at[3][1])
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i].u = make_uint4(lo[i][0], lo[i][1], hi[i][0], hi[i][1]);
+}
+
+// acc[db] += (positions x dims of a tile)^T times four fragments of 16 positions each, for the 64 (HALF < 0) or 32 positions of the tile
+template <int HD, int FROM, int TO>
+__device__ __forceinline__ void pk_second(uint32_t tile, const PkOffsets<HD>& o, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
+    PkFrag f[4];
+    if constexpr (HD == 128) {
+#pragma unroll
+        for (int s = FROM; s < TO; ++s) {
+            pk_read_trans<HD>(tile + s * 16 * HD * 2, o, f);
+#pragma unroll
+            for (int db = 0; db < 4; ++db) acc[db] = pk_mfma(f[db], p[s], acc[db]);
+        }
+    } else {
+#pragma unroll
+        for (int s = FROM; s < TO; s += 2) {
+            pk_read_trans<HD>(tile + s * 16 * HD * 2, o, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i & 1] = pk_mfma(f[i], p[s + (i >> 1)], acc[i & 1]);
+        }
+    }
+}
+
+// The same with care: values that are not finite are taken out, and with INF, where `seen` (fragments of ones and zeros) has a one for them, the
+// sum becomes what they make of it: a product of seen with 1 for inf, 2^12 for -inf and 2^23 for NaN has at most 64 of each
+template <int HD, bool INF>
+__device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag (&p)[4], const PkFrag (&seen)[4], pk_floatx16 (&acc)[HD / 32]) {
+    const int lane = threadIdx.x & 63, hi = lane >> 5;
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db) {
+        const int dim = 32 * db + (lane & 31);
+        pk_floatx16 c = {};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            PkFrag f, k;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t fw = 0, kw = 0;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int i = 2 * w + b, r = 16 * s + (i >> 2) * 8 + 4 * hi + (i & 3);
+                    const uint32_t x = *reinterpret_cast<const bf16_t*>(tile + r * (HD * 2) + (((dim >> 3) ^ pk_swz<HD>(r)) << 4) + (dim & 7) * 2);
+                    const bool bad = (x & 0x7F80u) == 0x7F80u;
+                    fw |= (bad ? 0u : x) << (16 * b);
+                    // 2^23, 2^12 and 1 in bf16
+                    kw |= (!bad ? 0u : (x & 0x7Fu) ? 0x4B00u : (x & 0x8000u) ? 0x4580u : 0x3F80u) << (16 * b);
+                }
+                f.w[w] = fw;
+                k.w[w] = kw;
+            }
+            acc[db] = pk_mfma(f, p[s], acc[db]);       // (in the order of pk_second: the same bits)
+            if (INF) c = pk_mfma(k, seen[s], c);
+        }
+        if (INF) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const bool nan = c[e] >= 8388608.f, neg = c[e] >= 4096.f, pos = c[e] - 4096.f * floorf(c[e] * (1.f / 4096.f)) > 0.f;
+                acc[db][e] += c[e] == 0.f ? 0.f : nan || (neg && pos) ? NAN : neg ? -INFINITY : INFINITY;
+            }
+        }
+    }
+}
+
+// whether any of a lane's sums is not finite
+template <int N>
+__device__ __forceinline__ bool pk_not_finite(const pk_floatx16 (&acc)[N], float z = 0.f) {
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z = fmaf(acc[d][e], 0.f, z);
+    return !(z == 0.f);
+}
+
+// a lane's sums of its column (rows of the instruction: dims) times f, as bf16, to `row` (its row's first value): the halves of a wave
+// exchange what makes 16 bytes
+template <int HD>
+__device__ __forceinline__ void pk_store(const pk_floatx16 (&acc)[HD / 32], float f, bf16_t* row, bool store) {
+    const int hi = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+            const uint32_t a0 = pack_bf16x2(acc[db][4 * g] * f, acc[db][4 * g + 1] * f), a1 = pack_bf16x2(acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f);
+            const uint32_t b0 = pack_bf16x2(acc[db][4 * g + 4] * f, acc[db][4 * g + 5] * f), b1 = pack_bf16x2(acc[db][4 * g + 6] * f, acc[db][4 * g + 7] * f);
+            const auto r0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), r1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+            if (store) *reinterpret_cast<uint4*>(row + 32 * db + 8 * (g + hi)) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
+        }
+}
+
+// One sequence's places in the packed tensors, and a tile of it
+struct PkTile { int tile; int64_t q0, k0; int nq, nk; };
+
+// Tile number t of all sequences' tiles, UNIT rows (BY_KEYS: keys) each.  Offsets are taken as far as they lie inside the tensors and grow
+template <int UNIT, bool BY_KEYS>
+__device__ __forceinline__ bool pk_find(const PackedArgs& a, int64_t t, PkTile& out) {
+    const int lane = threadIdx.x & 63, G = a.n_heads / a.n_kv;
+    int64_t before = 0;
+    for (int b = 0; b < a.n_seq; b += 64) {
+        const int s = b + lane;
+        int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
+        if (s < a.n_seq) {
+            q0 = min(max(a.cu_q[s], 0), (int)a.total_q);   q1 = min(max(a.cu_q[s + 1], q0), (int)a.total_q);
+            k0 = min(max(a.cu_k[s], 0), (int)a.total_k);   k1 = min(max(a.cu_k[s + 1], k0), (int)a.total_k);
+        }
+        const int count = BY_KEYS ? (k1 - k0 + UNIT - 1) / UNIT : (int)(((int64_t)(q1 - q0) * G + UNIT - 1) / UNIT);
+        int sum = count;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(sum, off);
+            sum += lane >= off ? o : 0;
+        }
+        const int total = __builtin_amdgcn_readlane(sum, 63);
+        if (t < before + total) {
+            const uint64_t m = __builtin_amdgcn_ballot_w64(before + sum > t);
+            const int src = __builtin_ctzll(m);
+            out.tile = (int)(t - before) - __builtin_amdgcn_readlane(sum - count, src);
+            out.q0 = __builtin_amdgcn_readlane(q0, src);
+            out.k0 = __builtin_amdgcn_readlane(k0, src);
+            out.nq = __builtin_amdgcn_readlane(q1, src) - (int)out.q0;
+            out.nk = __builtin_amdgcn_readlane(k1, src) - (int)out.k0;
+            return true;
+        }
+        before += total;
+    }
+    return false;
+}
+
+// Direct loads of 64 rows to a tile in LDS by the four waves of a workgroup: the rows from `base` on, `ld` values apart; rows past `left` repeat
+// the last one
+template <int HD>
+struct PkLoader {
+    static constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);      // loads of a wave, rows of a load
+    int voff[N];
+    __device__ __forceinline__ PkLoader(int64_t ld) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = ROWS * (N * wave + i) + lane / (HD / 8);
+            voff[i] = (int)(r * ld * 2) + (((lane % (HD / 8)) ^ pk_swz<HD>(r)) << 4);
+        }
+    }
+    __device__ __forceinline__ void load(const bf16_t* base, int64_t ld, int left, char* tile) const {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, (int)0xFFFFFFFFu, 0x00020000);
+        char* to = tile + wave * (N * 1024);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            int off = voff[i];
+            if (left < PK_T) {
+                const int r = ROWS * (N * wave + i) + lane / (HD / 8);
+                off -= max(r - (left - 1), 0) * (int)(ld * 2);
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (pk_lptr)(to + i * 1024), 16, off, 0, 0, 0);
+        }
+    }
+};
+
+// loads of this wave have landed, then everybody's
+__device__ __forceinline__ void pk_arrive() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0x0070);              // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ void pk_zero(pk_floatx16& x) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = 0.f;
+}
+
+// e's position in a block of 32
+__device__ __forceinline__ int pk_pos(int e) { return 8 * (e >> 2) + (e & 3); }      // + 4 (lane / 32)
+
+// ones where positions kb + .. <= limit, as the fragments of 64 positions
+__device__ __forceinline__ void pk_seen(int kb, int limit, PkFrag (&f)[4]) {
+    const int rel = limit - kb - 4 * (int)((threadIdx.x >> 5) & 1);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int at = 16 * s + (w >> 1) * 8 + (w & 1) * 2;
+            f[s].w[w] = (at <= rel ? 0x3F80u : 0u) | (at + 1 <= rel ? 0x3F800000u : 0u);
+        }
+}
+
+constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
+
+// ---- forward ---------------------------------------------------------------------------------------------------
+// Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
+// waits.  A tile is 64 matrix instructions a wave (HD = 128, 2048 cycles) beside some 1500 cycles of exponentials and 32 KB of LDS reads.
+// part != NULL: workgroup y takes its share of the row tile's keys and leaves sums, maximum and sum of exponentials for pk_join_kernel
+template <int HD>
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_forward_kernel(
+        PackedArgs a, bf16_t* __restrict__ out, int64_t ldo, float* __restrict__ lse, float* __restrict__ part, float2* __restrict__ part_ml) {
+    extern __shared__ __align__(1024) char pk_smem[];
+    constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hi = lane >> 5;
+    // the last tiles first, for they have most keys; the key heads side by side: an XCD (workgroup number mod 8) then has few of them
+    const int64_t unit = (int64_t)gridDim.x - 1 - blockIdx.x;
+    const int kvh = (int)(unit % a.n_kv), G = a.n_heads / a.n_kv;
+    PkTile t;
+    if (!pk_find<PK_ROWS, false>(a, unit / a.n_kv, t)) return;
+    const int64_t R = (int64_t)t.nq * G;
+    const int64_t row0 = (int64_t)t.tile * PK_ROWS + wave * 32;
+    const int shift = t.nk - t.nq;
+    const int64_t row = min(row0 + (lane & 31), R - 1);
+    const bool mine = row0 + (lane & 31) < R;
+    const int tq = (int)(row / G), head = kvh * G + (int)(row - (int64_t)tq * G);
+    const int limit = a.causal ? tq + shift : t.nk - 1;                       // the last key that the lane's row sees
+    // the first and last of the wave's rows, and the last of the workgroup's
+    const int wfirst = a.causal ? (int)(min(row0, R - 1) / G) + shift : t.nk - 1;
+    const int wlast = row0 >= R ? -1 : a.causal ? (int)(min(row0 + 31, R - 1) / G) + shift : t.nk - 1;
+    const int last = a.causal ? (int)(min((int64_t)(t.tile + 1) * PK_ROWS - 1, R - 1) / G) + shift : t.nk - 1;
+    const int tiles = last < 0 ? 0 : last / PK_T + 1;
+    const int j0 = (int)((int64_t)tiles * blockIdx.y / gridDim.y), j1 = (int)((int64_t)tiles * (blockIdx.y + 1) / gridDim.y);
+    const bf16_t* Kh = a.k + t.k0 * a.ldk + kvh * HD;
+    const bf16_t* Vh = a.v + t.k0 * a.ldv + kvh * HD;
+    const PkLoader<HD> lk(a.ldk), lv(a.ldv);
+    auto request = [&](int j) __attribute__((always_inline)) {
+        char* stage = pk_smem + (j & 1) * (2 * TILE);
+        lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T, stage);
+        lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T, stage + TILE);
+    };
+    const PkOffsets<HD> off;
+    PkFrag qf[KS];
+    if (j0 < j1) {
+        request(j0);
+        const bf16_t* src = a.q + (t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(src + 16 * ks);
+    }
+    const float sc = a.scale * PK_LOG2E;
+    // sums are rescaled when a maximum has grown by more than 2^8 times: what they and the probabilities are relative to need not be the maximum itself
+    const float slack = 8.f / sc;
+    pk_floatx16 acc[DB];
+    float top, topsc, l;
+    for (bool careful = false;;) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+        top = -INFINITY; topsc = 0.f; l = 0.f;
+        for (int j = j0; j < j1; ++j) {
+            pk_arrive();
+            if (j + 1 < j1) request(j + 1);
+            const int kb = j * PK_T;
+            if (kb > wlast) continue;                                        // (wave-uniform)
+            const char* kt = pk_smem + (j & 1) * (2 * TILE);
+            pk_floatx16 s[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                pk_zero(s[h]);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    PkFrag kf;
+                    kf.v = *reinterpret_cast<const pk_bf16x8*>(kt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                    s[h] = pk_mfma(kf, qf[ks], s[h]);
+                }
+            }
+            const bool mask = kb + PK_T - 1 > wfirst;                        // (wave-uniform)
+            if (mask) {
+                const int rel = limit - kb - 4 * hi;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[h][e] = 32 * h + pk_pos(e) <= rel ? s[h][e] : -INFINITY;
+            }
+            float mx = s[0][0];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
+            mx = pk_max_halves(mx);
+            if (__any(mx > top + slack)) {
+                const float grown = fmaxf(top, mx), to = grown == -INFINITY ? 0.f : grown * sc;
+                const float alpha = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(topsc - to);
+                l *= alpha;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+                top = grown;
+                topsc = to;
+            }
+            PkFrag pf[4];
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][e], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[h][e + 1], sc, -topsc));
+                    sum[h] += p0 + p1;
+                    // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that)
+                    pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
+                }
+            l += sum[0] + sum[1];
+            if (careful && mask) {
+                PkFrag seen[4];
+                pk_seen(kb, limit, seen);
+                pk_second_careful<HD, true>(kt + TILE, pf, seen, acc);
+                continue;
+            }
+            const uint32_t vt = (uint32_t)(uintptr_t)(pk_lptr)const_cast<char*>(kt + TILE);
+            pk_second<HD, 0, 2>(vt, off, pf, acc);
+            if (kb + 32 <= wlast) pk_second<HD, 2, 4>(vt, off, pf, acc);
+        }
+        if (careful || !__syncthreads_or(mine && pk_not_finite(acc))) break;
+        careful = true;
+        if (j0 < j1) request(j0);
+    }
+    l = pk_sum_halves(l);
+    if (part) {
+        if (!mine) return;
+        const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + (t.q0 + tq) * a.n_heads + head;
+        float* to = part + at * HD + 4 * hi;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4*>(to + 32 * db + 8 * g) = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
+        if (hi == 0) part_ml[at] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
+        return;
+    }
+    const bool empty = limit < 0;
+    pk_store<HD>(acc, empty ? 0.f : 1.f / l, out + (t.q0 + tq) * ldo + (int64_t)head * HD, mine);
+    if (lse && mine && hi == 0) lse[(t.q0 + tq) * a.n_heads + head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
+}
+
+// Shares of the keys joined: HD / 4 lanes a row.  Rows of no sequence are left alone: their partial sums are what the workspace held
+template <int HD>
+__global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int shares,
+                                                      bf16_t* __restrict__ out, int64_t ldo, float* __restrict__ lse) {
+    constexpr int LANES = HD / 4;
+    const int64_t rows = a.total_q * a.n_heads, row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    if (row >= rows) return;
+    const int j = threadIdx.x % LANES;
+    const int64_t tok = row / a.n_heads;
+    // which sequence the token is of, by halves: the last one that starts at or before it
+    int lo = 0, hi = a.n_seq;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.cu_q[mid] <= tok) lo = mid;
+        else hi = mid;
+    }
+    const int q0 = min(max(a.cu_q[lo], 0), (int)a.total_q), q1 = min(max(a.cu_q[lo + 1], q0), (int)a.total_q);
+    if (tok < q0 || tok >= q1) return;
+    const int k0 = min(max(a.cu_k[lo], 0), (int)a.total_k), nk = min(max(a.cu_k[lo + 1], k0), (int)a.total_k) - k0;
+    const bool empty = (a.causal ? (int)(tok - q0) + nk - (q1 - q0) : nk - 1) < 0;
+    float top = -INFINITY;
+    for (int s = 0; s < shares; ++s) top = fmaxf(top, ml[s * rows + row].x);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    for (int s = 0; s < shares; ++s) {
+        const float2 m = ml[s * rows + row];
+        if (m.x == -INFINITY) continue;                       // a share that the row sees nothing of
+        const float f = __builtin_amdgcn_exp2f(m.x - top);
+        const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + row) * HD + 4 * j);
+        l = fmaf(f, m.y, l);
+        o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+    }
+    const float inv = empty ? 0.f : 1.f / l;
+    const int head = (int)(row - tok * a.n_heads);
+    *reinterpret_cast<uint2*>(out + tok * ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (lse && j == 0) lse[row] = empty ? -INFINITY : (top + log2f(l)) * PK_LN2;
+}
+
+// ---- backward --------------------------------------------------------------------------------------------------
+// {lse log2 e, do . o} of every row
+template <int HD>
+__global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_t* __restrict__ o, int64_t ldo, const bf16_t* __restrict__ d, int64_t ldd,
+                                                       const float* __restrict__ lse, float2* __restrict__ rowinfo) {
+    constexpr int LANES = HD / 8;
+    const int64_t rows = a.total_q * a.n_heads, row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    if (row >= rows) return;
+    const int j = threadIdx.x % LANES;
+    const int64_t tok = row / a.n_heads, col = (row - tok * a.n_heads) * HD + 8 * j;
+    const uint4 x = *reinterpret_cast<const uint4*>(o + tok * ldo + col), y = *reinterpret_cast<const uint4*>(d + tok * ldd + col);
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), s);
+        s = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), s);
+    }
+#pragma unroll
+    for (int w = LANES / 2; w > 0; w >>= 1) s += __shfl_xor(s, w);
+    if (j == 0) rowinfo[row] = make_float2(lse[row] * PK_LOG2E, s);
+}
+
+// dq: the forward's shape, with do beside q in registers, and K read with and without transposition
+template <int HD>
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_dq_kernel(
+        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const float2* __restrict__ rowinfo, bf16_t* __restrict__ dq, int64_t lddq) {
+    extern __shared__ __align__(1024) char pk_smem[];
+    constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hi = lane >> 5;
+    const int64_t unit = (int64_t)gridDim.x - 1 - blockIdx.x;
+    const int kvh = (int)(unit % a.n_kv), G = a.n_heads / a.n_kv;
+    PkTile t;
+    if (!pk_find<PK_ROWS, false>(a, unit / a.n_kv, t)) return;
+    const int64_t R = (int64_t)t.nq * G;
+    const int64_t row0 = (int64_t)t.tile * PK_ROWS + wave * 32;
+    const int shift = t.nk - t.nq;
+    const int64_t row = min(row0 + (lane & 31), R - 1);
+    const bool mine = row0 + (lane & 31) < R;
+    const int tq = (int)(row / G), head = kvh * G + (int)(row - (int64_t)tq * G);
+    const int limit = a.causal ? tq + shift : t.nk - 1;
+    const int wfirst = a.causal ? (int)(min(row0, R - 1) / G) + shift : t.nk - 1;
+    const int wlast = row0 >= R ? -1 : a.causal ? (int)(min(row0 + 31, R - 1) / G) + shift : t.nk - 1;
+    const int last = a.causal ? (int)(min((int64_t)(t.tile + 1) * PK_ROWS - 1, R - 1) / G) + shift : t.nk - 1;
+    const int tiles = last < 0 ? 0 : last / PK_T + 1;
+    const bf16_t* Kh = a.k + t.k0 * a.ldk + kvh * HD;
+    const bf16_t* Vh = a.v + t.k0 * a.ldv + kvh * HD;
+    const PkLoader<HD> lk(a.ldk), lv(a.ldv);
+    auto request = [&](int j) __attribute__((always_inline)) {
+        char* stage = pk_smem + (j & 1) * (2 * TILE);
+        lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T, stage);
+        lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T, stage + TILE);
+    };
+    const PkOffsets<HD> off;
+    PkFrag qf[KS], df[KS];
+    if (tiles > 0) request(0);
+    const bf16_t* qsrc = a.q + (t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
+    const bf16_t* dsrc = dout + (t.q0 + tq) * lddo + (int64_t)head * HD + 8 * hi;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
+        df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
+    }
+    const float2 info = rowinfo[(t.q0 + tq) * a.n_heads + head];
+    const float sc = a.scale * PK_LOG2E;
+    pk_floatx16 acc[DB];
+    for (bool careful = false;;) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+        for (int j = 0; j < tiles; ++j) {
+            pk_arrive();
+            if (j + 1 < tiles) request(j + 1);
+            const int kb = j * PK_T;
+            if (kb > wlast) continue;
+            const char* kt = pk_smem + (j & 1) * (2 * TILE);
+            const bool mask = kb + PK_T - 1 > wfirst;
+            PkFrag pf[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                pk_floatx16 s, dp;
+                pk_zero(s);
+                pk_zero(dp);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    PkFrag kf, vf;
+                    kf.v = *reinterpret_cast<const pk_bf16x8*>(kt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                    vf.v = *reinterpret_cast<const pk_bf16x8*>(kt + TILE + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                    s = pk_mfma(kf, qf[ks], s);
+                    dp = pk_mfma(vf, df[ks], dp);
+                }
+                float ds[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, -info.x)) * (dp[e] - info.y);
+                if (mask) {
+                    // (the only key that a row sees has the probability 1 whatever its score)
+                    const int rel = limit == 0 ? -1 : limit - kb - 4 * hi;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) ds[e] = 32 * h + pk_pos(e) <= rel ? ds[e] : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(ds[e], ds[e + 1]);
+            }
+            if (careful && mask) {
+                pk_second_careful<HD, false>(kt, pf, pf, acc);
+                continue;
+            }
+            const uint32_t ktr = (uint32_t)(uintptr_t)(pk_lptr)const_cast<char*>(kt);
+            pk_second<HD, 0, 2>(ktr, off, pf, acc);
+            if (kb + 32 <= wlast) pk_second<HD, 2, 4>(ktr, off, pf, acc);
+        }
+        if (careful || !__syncthreads_or(mine && pk_not_finite(acc))) break;
+        careful = true;
+        if (tiles > 0) request(0);
+    }
+    pk_store<HD>(acc, a.scale, dq + (t.q0 + tq) * lddq + (int64_t)head * HD, mine);
+}
+
+// dk, dv: four waves of 32 keys, K and V in registers, against tiles of 64 rows of q and do that they share
+template <int HD>
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_dkv_kernel(
+        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const float2* __restrict__ rowinfo,
+        bf16_t* __restrict__ dk, int64_t lddk, bf16_t* __restrict__ dv, int64_t lddv) {
+    extern __shared__ __align__(1024) char pk_smem[];
+    constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
+    float4* infos = reinterpret_cast<float4*>(pk_smem + 4 * TILE);            // two stages of {lse log2 e, delta, last key seen}
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hi = lane >> 5;
+    const int kvh = (int)(blockIdx.x % a.n_kv), G = a.n_heads / a.n_kv;
+    PkTile t;
+    if (!pk_find<PK_ROWS, true>(a, blockIdx.x / a.n_kv, t)) return;
+    const int R = t.nq * G, shift = t.nk - t.nq;
+    const int key0 = t.tile * PK_ROWS, wkey = key0 + wave * 32;
+    const int key = min(wkey + (lane & 31), t.nk - 1);
+    const bool mine = wkey + (lane & 31) < t.nk;
+    const int row0 = a.causal ? max(key0 - shift, 0) * G : 0;                  // (below R: key0 < nk)
+    const int tiles = (R - row0 + PK_T - 1) / PK_T;
+    const uint32_t magic = (uint32_t)(0x100000000ull / (uint32_t)G - (G == 1));
+    auto query_of = [&](int row) __attribute__((always_inline)) {             // row / G
+        int q = (int)__umulhi((uint32_t)row, magic);
+        q += row - q * G >= G;
+        return q;
+    };
+    // direct loads of a tile's rows; rows past the end repeat the last one
+    constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);
+    const bf16_t* Qh = a.q + t.q0 * a.ldq + (int64_t)kvh * G * HD;
+    const bf16_t* Dh = dout + t.q0 * lddo + (int64_t)kvh * G * HD;
+    auto request = [&](int j) __attribute__((always_inline)) {
+        char* stage = pk_smem + (j & 1) * (2 * TILE) + wave * (N * 1024);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = ROWS * (N * wave + i) + lane / (HD / 8), row = min(row0 + j * PK_T + r, R - 1);
+            const int q = query_of(row), chunk = (lane % (HD / 8)) ^ pk_swz<HD>(r);
+            const int col = (row - q * G) * HD + chunk * 8;
+            __builtin_amdgcn_global_load_lds((pk_gptr)(Qh + q * a.ldq + col), (pk_lptr)(stage + i * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((pk_gptr)(Dh + q * lddo + col), (pk_lptr)(stage + TILE + i * 1024), 16, 0, 0);
+        }
+    };
+    auto info_of = [&](int j) __attribute__((always_inline)) {                // of row lane of tile j
+        const int row = row0 + j * PK_T + lane, r = min(row, R - 1), q = query_of(r);
+        const float2 v = rowinfo[(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
+        const int limit = row >= R ? -1 : a.causal ? q + shift : t.nk - 1;
+        return make_float4(v.x, v.y, __int_as_float(limit), 0.f);
+    };
+    const PkOffsets<HD> off;
+    PkFrag kf[KS], vf[KS];
+    {
+        const bf16_t* ksrc = a.k + (t.k0 + key) * a.ldk + kvh * HD + 8 * hi;
+        const bf16_t* vsrc = a.v + (t.k0 + key) * a.ldv + kvh * HD + 8 * hi;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks].u = *reinterpret_cast<const uint4*>(ksrc + 16 * ks);
+            vf[ks].u = *reinterpret_cast<const uint4*>(vsrc + 16 * ks);
+        }
+    }
+    const float sc = a.scale * PK_LOG2E;
+    pk_floatx16 ak[DB], av[DB];
+    for (bool careful = false;;) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) { pk_zero(ak[d]); pk_zero(av[d]); }
+        if (tiles > 0) {
+            request(0);
+            if (wave == 0) infos[lane] = info_of(0);
+        }
+        for (int j = 0; j < tiles; ++j) {
+            pk_arrive();
+            float4 next;
+            const bool more = j + 1 < tiles;
+            if (more) {
+                if (wave == 0) next = info_of(j + 1);
+                request(j + 1);
+            }
+            const float4* info = infos + (j & 1) * PK_T;
+            const int first = query_of(min(row0 + j * PK_T, R - 1)), lastq = query_of(min(row0 + j * PK_T + PK_T - 1, R - 1));
+            const int low = a.causal ? first + shift : t.nk - 1, high = a.causal ? lastq + shift : t.nk - 1;     // the rows' first and last limit
+            if (high >= wkey) {                                              // (wave-uniform)
+                const bool mask = low < wkey + 31 || row0 + j * PK_T + PK_T > R;
+                const char* qt = pk_smem + (j & 1) * (2 * TILE);
+                PkFrag pf[4], df[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    pk_floatx16 s, dp;
+                    pk_zero(s);
+                    pk_zero(dp);
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        PkFrag qa, da;
+                        qa.v = *reinterpret_cast<const pk_bf16x8*>(qt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                        da.v = *reinterpret_cast<const pk_bf16x8*>(qt + TILE + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                        s = pk_mfma(qa, kf[ks], s);
+                        dp = pk_mfma(da, vf[ks], dp);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        float p[2], ds[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const float4 in = info[32 * h + pk_pos(e + u) + 4 * hi];
+                            p[u] = __builtin_amdgcn_exp2f(fmaf(s[e + u], sc, -in.x));
+                            ds[u] = p[u] * (dp[e + u] - in.y);
+                            if (mask) {
+                                const int limit = __float_as_int(in.z);
+                                const bool seen = wkey + (lane & 31) <= limit;
+                                p[u] = seen ? p[u] : 0.f;
+                                ds[u] = seen && limit > 0 ? ds[u] : 0.f;
+                            }
+                        }
+                        pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p[0], p[1]);
+                        df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(ds[0], ds[1]);
+                    }
+                }
+                if (careful && mask) {
+                    PkFrag seen[4];
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int at = 16 * s + (w >> 1) * 8 + (w & 1) * 2 + 4 * hi;
+                            seen[s].w[w] = (wkey + (lane & 31) <= __float_as_int(info[at].z) ? 0x3F80u : 0u) |
+                                           (wkey + (lane & 31) <= __float_as_int(info[at + 1].z) ? 0x3F800000u : 0u);
+                        }
+                    pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
+                    pk_second_careful<HD, false>(qt, df, df, ak);
+                } else {
+                    const uint32_t qtr = (uint32_t)(uintptr_t)(pk_lptr)const_cast<char*>(qt);
+                    pk_second<HD, 0, 4>(qtr + TILE, off, pf, av);
+                    pk_second<HD, 0, 4>(qtr, off, df, ak);
+                }
+            }
+            if (more && wave == 0) infos[((j + 1) & 1) * PK_T + lane] = next;
+        }
+        if (careful || !__syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) break;
+        careful = true;
+    }
+    pk_store<HD>(av, 1.f, dv + (t.k0 + key) * lddv + (int64_t)kvh * HD, mine);
+    pk_store<HD>(ak, a.scale, dk + (t.k0 + key) * lddk + (int64_t)kvh * HD, mine);
+}
+
+// an upper bound of the row (key) tiles of all sequences, whatever their lengths
+int64_t pk_units(int64_t total, int n_seq, int n_kv) { return (total / PK_ROWS + std::min<int64_t>(n_seq, total)) * n_kv; }
+
+// Few row tiles are dealt to several workgroups by keys, for about two to a compute unit, four tiles of keys each at least, as far as lengths can be told from
+// their mean
+int pk_shares(const PackedArgs& a) {
+    const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv);
+    if (units < 1) return 1;
+    const int64_t keys = a.total_k / std::max(1, a.n_seq), most = std::max<int64_t>(1, keys / (4 * PK_T));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / units, most, 64}));
+}
+
+template <typename F>
+hipError_t pk_lds(F* f, int bytes) {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <int HD>
+hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
+    constexpr int SMEM = 4 * PK_T * HD * 2;
+    static const hipError_t attr = pk_lds(pk_forward_kernel<HD>, SMEM);
+    if (attr != hipSuccess) return attr;
+    const int G = a.n_heads / a.n_kv, shares = pk_shares(a);
+    const int64_t units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
+    if (units > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    float* part = shares > 1 ? static_cast<float*>(workspace) : nullptr;
+    float2* ml = shares > 1 ? reinterpret_cast<float2*>(part + (int64_t)shares * rows * HD) : nullptr;
+    hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units, (unsigned)shares), dim3(64 * PK_WAVES), SMEM, st, a, out, ldo, lse, part, ml);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || shares == 1) return e;
+    const int64_t blocks = (rows * (HD / 4) + 255) / 256;
+    hipLaunchKernelGGL(pk_join_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, part, ml, shares, out, ldo, lse);
+    return hipGetLastError();
+}
+
+template <int HD>
+hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* workspace, hipStream_t st) {
+    constexpr int SMEM = 4 * PK_T * HD * 2, SMEM_KV = SMEM + 2 * PK_T * 16;
+    static const hipError_t attr_q = pk_lds(pk_dq_kernel<HD>, SMEM), attr_kv = pk_lds(pk_dkv_kernel<HD>, SMEM_KV);
+    if (attr_q != hipSuccess) return attr_q;
+    if (attr_kv != hipSuccess) return attr_kv;
+    const int64_t rows = a.total_q * a.n_heads, G = a.n_heads / a.n_kv;
+    const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv), blocks = (rows * (HD / 8) + 255) / 256;
+    if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    float2* info = static_cast<float2*>(workspace);
+    hipError_t e = hipSuccess;
+    if (rows > 0) {
+        hipLaunchKernelGGL(pk_delta_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, g.out, g.ldo, g.dout, g.lddo, g.lse, info);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(pk_dq_kernel<HD>, dim3((unsigned)dq_units), dim3(64 * PK_WAVES), SMEM, st, a, g.dout, g.lddo, info, g.dq, g.lddq);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.total_k > 0) {
+        hipLaunchKernelGGL(pk_dkv_kernel<HD>, dim3((unsigned)kv_units), dim3(64 * PK_WAVES), SMEM_KV, st, a, g.dout, g.lddo, info, g.dk, g.lddk, g.dv, g.lddv);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim) {
+    const int shares = pk_shares(a);
+    return shares == 1 ? 0 : (size_t)shares * a.total_q * a.n_heads * (head_dim * sizeof(float) + sizeof(float2));
+}
+size_t packed_backward_workspace_bytes(const PackedArgs& a) { return (size_t)a.total_q * a.n_heads * sizeof(float2); }
+
+hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
+    if (a.total_q == 0 || a.n_seq == 0) return hipSuccess;
+    return head_dim == 128 ? pk_launch_forward<128>(a, out, ldo, lse, workspace, st) : pk_launch_forward<64>(a, out, ldo, lse, workspace, st);
+}
+
+hipError_t launch_packed_backward(const PackedArgs& a, int head_dim, const PackedGrad& g, void* workspace, hipStream_t st) {
+    if (a.n_seq == 0) return hipSuccess;
+    return head_dim == 128 ? pk_launch_backward<128>(a, g, workspace, st) : pk_launch_backward<64>(a, g, workspace, st);
+}
+
+}  // namespace agzo
