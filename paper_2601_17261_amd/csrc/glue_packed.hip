@@ -17,6 +17,8 @@
 // masked place's values, by 0, of which a value that is not finite makes a NaN.  Where a workgroup's results are not finite it goes over
 // its tiles once more with care: masked tiles then have such values taken out, and what the visible ones amount to is found by a product of two
 // indicators.
+#include <type_traits>
+
 #include "agzo_internal.h"
 
 namespace agzo {
@@ -45,6 +47,11 @@ __device__ __forceinline__ float pk_sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+__device__ __forceinline__ uint4 pk_load16(__amdgpu_buffer_rsrc_t rsrc, int off) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 // A tile of 64 positions of HD values, 16-byte chunk c of row r at place c ^ swz(r).  Reads of 16 rows' same chunk, and reads with
 // transposition of 4 rows' four neighbouring chunks, then meet each bank once
 template <int HD>
@@ -67,46 +74,28 @@ struct PkOffsets {
     }
 };
 
-// four fragments with transposition (positions x dims): for HD = 128 the four groups of 32 dims of 16 positions, for HD = 64 the two of each of
-// two times 16 positions.  One statement with its wait: behind the builtin's the compiler waits for every direct load in flight
+// a fragment with transposition: 16 positions (from place `at` of a tile on) x 32 dims
+typedef __bf16 pk_bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) pk_bf16x4* pk_trptr;
 template <int HD>
-__device__ __forceinline__ void pk_read_trans(uint32_t base, const PkOffsets<HD>& o, PkFrag (&f)[4]) {
-    pk_u32x2 lo[4], hi[4];
-    uint32_t at[4][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) at[i][s] = base + (HD == 128 ? (uint32_t)(o.trans[s] ^ (i << 6)) : (uint32_t)((o.trans[s] ^ ((i & 1) << 6)) + (i >> 1) * 16 * HD * 2));
-    asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\t"
-                 "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11\n\t"
-                 "ds_read_b64_tr_b16 %4, %12\n\tds_read_b64_tr_b16 %5, %13\n\t"
-                 "ds_read_b64_tr_b16 %6, %14\n\tds_read_b64_tr_b16 %7, %15\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3])
-                 : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "v"(at[3][0]), "v"(at[3][1])
-                 : "memory");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i].u = make_uint4(lo[i][0], lo[i][1], hi[i][0], hi[i][1]);
+__device__ __forceinline__ void pk_read_trans(const char* at, const PkOffsets<HD>& o, int db, PkFrag& f) {
+    union { pk_bf16x4 v; uint2 u; } lo, hi;
+    lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(at + (o.trans[0] ^ (db << 6))));
+    hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(at + (o.trans[1] ^ (db << 6))));
+    f.u = make_uint4(lo.u.x, lo.u.y, hi.u.x, hi.u.y);
 }
 
-// acc[db] += (positions x dims of a tile)^T times four fragments of 16 positions each, for the 64 (HALF < 0) or 32 positions of the tile
+// acc[db] += (positions x dims of a tile)^T times fragments FROM .. TO of 16 positions each
 template <int HD, int FROM, int TO>
-__device__ __forceinline__ void pk_second(uint32_t tile, const PkOffsets<HD>& o, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
-    PkFrag f[4];
-    if constexpr (HD == 128) {
+__device__ __forceinline__ void pk_second(const char* tile, const PkOffsets<HD>& o, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
 #pragma unroll
-        for (int s = FROM; s < TO; ++s) {
-            pk_read_trans<HD>(tile + s * 16 * HD * 2, o, f);
+    for (int s = FROM; s < TO; ++s)
 #pragma unroll
-            for (int db = 0; db < 4; ++db) acc[db] = pk_mfma(f[db], p[s], acc[db]);
+        for (int db = 0; db < HD / 32; ++db) {
+            PkFrag f;
+            pk_read_trans<HD>(tile + s * 16 * HD * 2, o, db, f);
+            acc[db] = pk_mfma(f, p[s], acc[db]);
         }
-    } else {
-#pragma unroll
-        for (int s = FROM; s < TO; s += 2) {
-            pk_read_trans<HD>(tile + s * 16 * HD * 2, o, f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i & 1] = pk_mfma(f[i], p[s + (i >> 1)], acc[i & 1]);
-        }
-    }
 }
 
 // The same with care: values that are not finite are taken out, and with INF, where `seen` (fragments of ones and zeros) has a one for them, the
@@ -213,12 +202,13 @@ __device__ __forceinline__ bool pk_find(const PackedArgs& a, int64_t t, PkTile& 
     return false;
 }
 
-// Direct loads of 64 rows to a tile in LDS by the four waves of a workgroup: the rows from `base` on, `ld` values apart; rows past `left` repeat
-// the last one
+// 64 rows on their way to a tile in LDS, by the four waves of a workgroup: the rows from `base` on, `ld` values apart; rows past `left` repeat the
+// last one.  (Through registers: behind direct loads to LDS the compiler lets every read with transposition wait for all that are in flight)
 template <int HD>
 struct PkLoader {
     static constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);      // loads of a wave, rows of a load
     int voff[N];
+    uint4 data[N];
     __device__ __forceinline__ PkLoader(int64_t ld) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
@@ -227,30 +217,24 @@ struct PkLoader {
             voff[i] = (int)(r * ld * 2) + (((lane % (HD / 8)) ^ pk_swz<HD>(r)) << 4);
         }
     }
-    __device__ __forceinline__ void load(const bf16_t* base, int64_t ld, int left, char* tile) const {
+    __device__ __forceinline__ void load(const bf16_t* base, int64_t ld, int left) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, (int)0xFFFFFFFFu, 0x00020000);
-        char* to = tile + wave * (N * 1024);
+        if (left >= PK_T) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            int off = voff[i];
-            if (left < PK_T) {
-                const int r = ROWS * (N * wave + i) + lane / (HD / 8);
-                off -= max(r - (left - 1), 0) * (int)(ld * 2);
-            }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (pk_lptr)(to + i * 1024), 16, off, 0, 0, 0);
+            for (int i = 0; i < N; ++i) data[i] = pk_load16(rsrc, voff[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                data[i] = pk_load16(rsrc, voff[i] - max(ROWS * (N * wave + i) + lane / (HD / 8) - (left - 1), 0) * (int)(ld * 2));
         }
     }
+    __device__ __forceinline__ void store(char* tile) const {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(tile + (wave * N + i) * 1024 + lane * 16) = data[i];
+    }
 };
-
-// loads of this wave have landed, then everybody's
-__device__ __forceinline__ void pk_arrive() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-    __builtin_amdgcn_s_waitcnt(0x0070);              // vmcnt(0) lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-    __builtin_amdgcn_sched_barrier(0);
-}
 
 __device__ __forceinline__ void pk_zero(pk_floatx16& x) {
 #pragma unroll
@@ -305,11 +289,14 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const int j0 = (int)((int64_t)tiles * blockIdx.y / gridDim.y), j1 = (int)((int64_t)tiles * (blockIdx.y + 1) / gridDim.y);
     const bf16_t* Kh = a.k + t.k0 * a.ldk + kvh * HD;
     const bf16_t* Vh = a.v + t.k0 * a.ldv + kvh * HD;
-    const PkLoader<HD> lk(a.ldk), lv(a.ldv);
+    PkLoader<HD> lk(a.ldk), lv(a.ldv);
     auto request = [&](int j) __attribute__((always_inline)) {
-        char* stage = pk_smem + (j & 1) * (2 * TILE);
-        lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T, stage);
-        lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T, stage + TILE);
+        lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T);
+        lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T);
+    };
+    auto arrive = [&](int j) __attribute__((always_inline)) {
+        lk.store(pk_smem + (j & 1) * (2 * TILE));
+        lv.store(pk_smem + (j & 1) * (2 * TILE) + TILE);
     };
     const PkOffsets<HD> off;
     PkFrag qf[KS];
@@ -324,15 +311,10 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const float slack = 8.f / sc;
     pk_floatx16 acc[DB];
     float top, topsc, l;
-    for (bool careful = false;;) {
-#pragma unroll
-        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
-        top = -INFINITY; topsc = 0.f; l = 0.f;
-        for (int j = j0; j < j1; ++j) {
-            pk_arrive();
-            if (j + 1 < j1) request(j + 1);
+    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
+            constexpr bool careful = decltype(CAREFUL)::value;
             const int kb = j * PK_T;
-            if (kb > wlast) continue;                                        // (wave-uniform)
+            if (kb > wlast) return;                                          // (wave-uniform)
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
             pk_floatx16 s[2];
 #pragma unroll
@@ -386,15 +368,26 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
                 PkFrag seen[4];
                 pk_seen(kb, limit, seen);
                 pk_second_careful<HD, true>(kt + TILE, pf, seen, acc);
-                continue;
+                return;
             }
-            const uint32_t vt = (uint32_t)(uintptr_t)(pk_lptr)const_cast<char*>(kt + TILE);
-            pk_second<HD, 0, 2>(vt, off, pf, acc);
-            if (kb + 32 <= wlast) pk_second<HD, 2, 4>(vt, off, pf, acc);
+            pk_second<HD, 0, 4>(kt + TILE, off, pf, acc);
+    };
+    auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+        top = -INFINITY; topsc = 0.f; l = 0.f;
+        if (j0 < j1) arrive(j0);
+        for (int j = j0; j < j1; ++j) {
+            __syncthreads();
+            if (j + 1 < j1) request(j + 1);
+            one_tile(CAREFUL, j);
+            if (j + 1 < j1) arrive(j + 1);
         }
-        if (careful || !__syncthreads_or(mine && pk_not_finite(acc))) break;
-        careful = true;
+    };
+    all_tiles(std::false_type());
+    if (__syncthreads_or(mine && pk_not_finite(acc))) {
         if (j0 < j1) request(j0);
+        all_tiles(std::true_type());
     }
     l = pk_sum_halves(l);
     if (part) {
@@ -453,10 +446,19 @@ __global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float*
 }
 
 // ---- backward --------------------------------------------------------------------------------------------------
-// {lse log2 e, do . o} of every row
+// Per row -lse / scale and -delta, delta = do . o, each as three bf16 (24 bits): what the scores and do v^T are to be corrected by, as further values
+// of the rows of q and do that are multiplied by ones.  (0 for rows that see nothing)
+__device__ __forceinline__ uint2 pk_split3(float f) {
+    bf16_t h, m, l;
+    split3_bf16(f, h, m, l);
+    return make_uint2((uint32_t)h | (uint32_t)m << 16, l);
+}
+__device__ __forceinline__ float pk_join3(uint32_t a, uint32_t b) {
+    return (__uint_as_float(a << 16) + __uint_as_float(a & 0xFFFF0000u)) + __uint_as_float(b << 16);
+}
 template <int HD>
 __global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_t* __restrict__ o, int64_t ldo, const bf16_t* __restrict__ d, int64_t ldd,
-                                                       const float* __restrict__ lse, float2* __restrict__ rowinfo) {
+                                                       const float* __restrict__ lse, uint4* __restrict__ rowinfo) {
     constexpr int LANES = HD / 8;
     const int64_t rows = a.total_q * a.n_heads, row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
     if (row >= rows) return;
@@ -472,13 +474,16 @@ __global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_
     }
 #pragma unroll
     for (int w = LANES / 2; w > 0; w >>= 1) s += __shfl_xor(s, w);
-    if (j == 0) rowinfo[row] = make_float2(lse[row] * PK_LOG2E, s);
+    if (j != 0) return;
+    const float at = lse[row];
+    const uint2 u = pk_split3(at == -INFINITY ? 0.f : -at / a.scale), v = pk_split3(-s);
+    rowinfo[row] = make_uint4(u.x, u.y, v.x, v.y);
 }
 
 // dq: the forward's shape, with do beside q in registers, and K read with and without transposition
 template <int HD>
 __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_dq_kernel(
-        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const float2* __restrict__ rowinfo, bf16_t* __restrict__ dq, int64_t lddq) {
+        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const uint4* __restrict__ rowinfo, bf16_t* __restrict__ dq, int64_t lddq) {
     extern __shared__ __align__(1024) char pk_smem[];
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -500,11 +505,14 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const int tiles = last < 0 ? 0 : last / PK_T + 1;
     const bf16_t* Kh = a.k + t.k0 * a.ldk + kvh * HD;
     const bf16_t* Vh = a.v + t.k0 * a.ldv + kvh * HD;
-    const PkLoader<HD> lk(a.ldk), lv(a.ldv);
+    PkLoader<HD> lk(a.ldk), lv(a.ldv);
     auto request = [&](int j) __attribute__((always_inline)) {
-        char* stage = pk_smem + (j & 1) * (2 * TILE);
-        lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T, stage);
-        lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T, stage + TILE);
+        lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T);
+        lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T);
+    };
+    auto arrive = [&](int j) __attribute__((always_inline)) {
+        lk.store(pk_smem + (j & 1) * (2 * TILE));
+        lv.store(pk_smem + (j & 1) * (2 * TILE) + TILE);
     };
     const PkOffsets<HD> off;
     PkFrag qf[KS], df[KS];
@@ -516,17 +524,14 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
         df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
     }
-    const float2 info = rowinfo[(t.q0 + tq) * a.n_heads + head];
+    const uint4 parts = rowinfo[(t.q0 + tq) * a.n_heads + head];
     const float sc = a.scale * PK_LOG2E;
+    const float2 info = make_float2(-sc * pk_join3(parts.x, parts.y), -pk_join3(parts.z, parts.w));      // lse log2 e, delta
     pk_floatx16 acc[DB];
-    for (bool careful = false;;) {
-#pragma unroll
-        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
-        for (int j = 0; j < tiles; ++j) {
-            pk_arrive();
-            if (j + 1 < tiles) request(j + 1);
+    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
+            constexpr bool careful = decltype(CAREFUL)::value;
             const int kb = j * PK_T;
-            if (kb > wlast) continue;
+            if (kb > wlast) return;
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
             const bool mask = kb + PK_T - 1 > wfirst;
             PkFrag pf[4];
@@ -557,27 +562,40 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
             }
             if (careful && mask) {
                 pk_second_careful<HD, false>(kt, pf, pf, acc);
-                continue;
+                return;
             }
-            const uint32_t ktr = (uint32_t)(uintptr_t)(pk_lptr)const_cast<char*>(kt);
-            pk_second<HD, 0, 2>(ktr, off, pf, acc);
-            if (kb + 32 <= wlast) pk_second<HD, 2, 4>(ktr, off, pf, acc);
+            pk_second<HD, 0, 4>(kt, off, pf, acc);
+    };
+    auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+        if (tiles > 0) arrive(0);
+        for (int j = 0; j < tiles; ++j) {
+            __syncthreads();
+            if (j + 1 < tiles) request(j + 1);
+            one_tile(CAREFUL, j);
+            if (j + 1 < tiles) arrive(j + 1);
         }
-        if (careful || !__syncthreads_or(mine && pk_not_finite(acc))) break;
-        careful = true;
+    };
+    all_tiles(std::false_type());
+    if (__syncthreads_or(mine && pk_not_finite(acc))) {
         if (tiles > 0) request(0);
+        all_tiles(std::true_type());
     }
     pk_store<HD>(acc, a.scale, dq + (t.q0 + tq) * lddq + (int64_t)head * HD, mine);
 }
 
-// dk, dv: four waves of 32 keys, K and V in registers, against tiles of 64 rows of q and do that they share
+// dk, dv: four waves of 32 keys, K and V in registers, against tiles of 64 rows of q and do that they share.  Sums, operands and scores are some 300
+// registers: one wave to a SIMD.  What belongs to a row comes in through the products, as a further step of 16 dims of which three are used: read row by
+// row in the instruction's layout it was 24 KB of LDS reads a tile and wave beside 64 KB of operands
 template <int HD>
-__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_dkv_kernel(
-        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const float2* __restrict__ rowinfo,
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1, 1))) void pk_dkv_kernel(
+        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const uint4* __restrict__ rowinfo,
         bf16_t* __restrict__ dk, int64_t lddk, bf16_t* __restrict__ dv, int64_t lddv) {
     extern __shared__ __align__(1024) char pk_smem[];
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
-    float4* infos = reinterpret_cast<float4*>(pk_smem + 4 * TILE);            // two stages of {lse log2 e, delta, last key seen}
+    uint4* infos = reinterpret_cast<uint4*>(pk_smem + 4 * TILE);              // two stages of a tile's rows
+    int* limits = reinterpret_cast<int*>(infos + 2 * PK_T);                   // ... and the last key that they see
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
     const int kvh = (int)(blockIdx.x % a.n_kv), G = a.n_heads / a.n_kv;
@@ -595,30 +613,45 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         q += row - q * G >= G;
         return q;
     };
-    // direct loads of a tile's rows; rows past the end repeat the last one
+    // a tile's rows on their way; rows past the end repeat the last one
     constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);
     const bf16_t* Qh = a.q + t.q0 * a.ldq + (int64_t)kvh * G * HD;
     const bf16_t* Dh = dout + t.q0 * lddo + (int64_t)kvh * G * HD;
+    uint4 qd[N], dd[N], next = make_uint4(0, 0, 0, 0);
+    int next_limit = -1;
     auto request = [&](int j) __attribute__((always_inline)) {
-        char* stage = pk_smem + (j & 1) * (2 * TILE) + wave * (N * 1024);
+        const int base = row0 + j * PK_T, q0 = query_of(base);
+        const auto rq = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Qh + q0 * a.ldq), 0, (int)0xFFFFFFFFu, 0x00020000);
+        const auto rd = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Dh + q0 * lddo), 0, (int)0xFFFFFFFFu, 0x00020000);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r = ROWS * (N * wave + i) + lane / (HD / 8), row = min(row0 + j * PK_T + r, R - 1);
-            const int q = query_of(row), chunk = (lane % (HD / 8)) ^ pk_swz<HD>(r);
-            const int col = (row - q * G) * HD + chunk * 8;
-            __builtin_amdgcn_global_load_lds((pk_gptr)(Qh + q * a.ldq + col), (pk_lptr)(stage + i * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((pk_gptr)(Dh + q * lddo + col), (pk_lptr)(stage + TILE + i * 1024), 16, 0, 0);
+            const int r = ROWS * (N * wave + i) + lane / (HD / 8), row = min(base + r, R - 1);
+            const int q = query_of(row), col = ((row - q * G) * HD + ((lane % (HD / 8)) ^ pk_swz<HD>(r)) * 8) * 2;
+            qd[i] = pk_load16(rq, (q - q0) * (int)(2 * a.ldq) + col);
+            dd[i] = pk_load16(rd, (q - q0) * (int)(2 * lddo) + col);
+        }
+        if (wave == 0) {
+            const int r = min(base + lane, R - 1), q = query_of(r);
+            next = rowinfo[(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
+            next_limit = base + lane >= R ? -1 : a.causal ? q + shift : t.nk - 1;
         }
     };
-    auto info_of = [&](int j) __attribute__((always_inline)) {                // of row lane of tile j
-        const int row = row0 + j * PK_T + lane, r = min(row, R - 1), q = query_of(r);
-        const float2 v = rowinfo[(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
-        const int limit = row >= R ? -1 : a.causal ? q + shift : t.nk - 1;
-        return make_float4(v.x, v.y, __int_as_float(limit), 0.f);
+    auto arrive = [&](int j) __attribute__((always_inline)) {
+        char* stage = pk_smem + (j & 1) * (2 * TILE) + wave * (N * 1024) + lane * 16;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            *reinterpret_cast<uint4*>(stage + i * 1024) = qd[i];
+            *reinterpret_cast<uint4*>(stage + TILE + i * 1024) = dd[i];
+        }
+        if (wave == 0) {
+            infos[(j & 1) * PK_T + lane] = next;
+            limits[(j & 1) * PK_T + lane] = next_limit;
+        }
     };
     const PkOffsets<HD> off;
-    PkFrag kf[KS], vf[KS];
-    {
+    PkFrag kf[KS], vf[KS], ones;
+    if (tiles > 0) {
+        request(0);
         const bf16_t* ksrc = a.k + (t.k0 + key) * a.ldk + kvh * HD + 8 * hi;
         const bf16_t* vsrc = a.v + (t.k0 + key) * a.ldv + kvh * HD + 8 * hi;
 #pragma unroll
@@ -627,84 +660,90 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
             vf[ks].u = *reinterpret_cast<const uint4*>(vsrc + 16 * ks);
         }
     }
+    ones.u = hi ? make_uint4(0, 0, 0, 0) : make_uint4(0x3F803F80u, 0x3F80u, 0, 0);
     const float sc = a.scale * PK_LOG2E;
     pk_floatx16 ak[DB], av[DB];
-    for (bool careful = false;;) {
+    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
+        constexpr bool careful = decltype(CAREFUL)::value;
+        const int base = row0 + j * PK_T;
+        const int low = a.causal ? query_of(base) + shift : t.nk - 1, high = a.causal ? query_of(min(base + PK_T - 1, R - 1)) + shift : t.nk - 1;   // the rows' first and last limit
+        if (high < wkey) return;                                              // (wave-uniform)
+        const bool mask = low < wkey + 31 || base + PK_T > R;
+        const char* qt = pk_smem + (j & 1) * (2 * TILE);
+        const uint4* info = infos + (j & 1) * PK_T;
+        const int* limit = limits + (j & 1) * PK_T + 4 * hi;
+        PkFrag pf[4], df[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            pk_floatx16 s, dp;
+            pk_zero(s);
+            pk_zero(dp);
+            const uint4 in = info[32 * h + (lane & 31)];
+            PkFrag x;
+            x.u = make_uint4(in.x, in.y, 0, 0);
+            s = pk_mfma(x, ones, s);
+            x.u = make_uint4(in.z, in.w, 0, 0);
+            dp = pk_mfma(x, ones, dp);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                PkFrag qa, da;
+                qa.v = *reinterpret_cast<const pk_bf16x8*>(qt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                da.v = *reinterpret_cast<const pk_bf16x8*>(qt + TILE + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                s = pk_mfma(qa, kf[ks], s);
+                dp = pk_mfma(da, vf[ks], dp);
+            }
+            float p[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(s[e] * sc);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dp[e] *= p[e];
+            if (mask) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int last = limit[32 * h + pk_pos(e)];
+                    const bool seen = wkey + (lane & 31) <= last;
+                    p[e] = seen ? p[e] : 0.f;
+                    // (the only key that a row sees has the probability 1 whatever its score)
+                    dp[e] = seen && last > 0 ? dp[e] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p[e], p[e + 1]);
+                df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(dp[e], dp[e + 1]);
+            }
+        }
+        if (careful && mask) {
+            PkFrag seen[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int at = 16 * s + (w >> 1) * 8 + (w & 1) * 2;
+                    seen[s].w[w] = (wkey + (lane & 31) <= limit[at] ? 0x3F80u : 0u) | (wkey + (lane & 31) <= limit[at + 1] ? 0x3F800000u : 0u);
+                }
+            pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
+            pk_second_careful<HD, false>(qt, df, df, ak);
+        } else {
+            pk_second<HD, 0, 4>(qt + TILE, off, pf, av);
+            pk_second<HD, 0, 4>(qt, off, df, ak);
+        }
+    };
+    auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) { pk_zero(ak[d]); pk_zero(av[d]); }
-        if (tiles > 0) {
-            request(0);
-            if (wave == 0) infos[lane] = info_of(0);
-        }
+        if (tiles > 0) arrive(0);
         for (int j = 0; j < tiles; ++j) {
-            pk_arrive();
-            float4 next;
-            const bool more = j + 1 < tiles;
-            if (more) {
-                if (wave == 0) next = info_of(j + 1);
-                request(j + 1);
-            }
-            const float4* info = infos + (j & 1) * PK_T;
-            const int first = query_of(min(row0 + j * PK_T, R - 1)), lastq = query_of(min(row0 + j * PK_T + PK_T - 1, R - 1));
-            const int low = a.causal ? first + shift : t.nk - 1, high = a.causal ? lastq + shift : t.nk - 1;     // the rows' first and last limit
-            if (high >= wkey) {                                              // (wave-uniform)
-                const bool mask = low < wkey + 31 || row0 + j * PK_T + PK_T > R;
-                const char* qt = pk_smem + (j & 1) * (2 * TILE);
-                PkFrag pf[4], df[4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    pk_floatx16 s, dp;
-                    pk_zero(s);
-                    pk_zero(dp);
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        PkFrag qa, da;
-                        qa.v = *reinterpret_cast<const pk_bf16x8*>(qt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
-                        da.v = *reinterpret_cast<const pk_bf16x8*>(qt + TILE + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
-                        s = pk_mfma(qa, kf[ks], s);
-                        dp = pk_mfma(da, vf[ks], dp);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        float p[2], ds[2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const float4 in = info[32 * h + pk_pos(e + u) + 4 * hi];
-                            p[u] = __builtin_amdgcn_exp2f(fmaf(s[e + u], sc, -in.x));
-                            ds[u] = p[u] * (dp[e + u] - in.y);
-                            if (mask) {
-                                const int limit = __float_as_int(in.z);
-                                const bool seen = wkey + (lane & 31) <= limit;
-                                p[u] = seen ? p[u] : 0.f;
-                                ds[u] = seen && limit > 0 ? ds[u] : 0.f;
-                            }
-                        }
-                        pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p[0], p[1]);
-                        df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(ds[0], ds[1]);
-                    }
-                }
-                if (careful && mask) {
-                    PkFrag seen[4];
-#pragma unroll
-                    for (int s = 0; s < 4; ++s)
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const int at = 16 * s + (w >> 1) * 8 + (w & 1) * 2 + 4 * hi;
-                            seen[s].w[w] = (wkey + (lane & 31) <= __float_as_int(info[at].z) ? 0x3F80u : 0u) |
-                                           (wkey + (lane & 31) <= __float_as_int(info[at + 1].z) ? 0x3F800000u : 0u);
-                        }
-                    pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
-                    pk_second_careful<HD, false>(qt, df, df, ak);
-                } else {
-                    const uint32_t qtr = (uint32_t)(uintptr_t)(pk_lptr)const_cast<char*>(qt);
-                    pk_second<HD, 0, 4>(qtr + TILE, off, pf, av);
-                    pk_second<HD, 0, 4>(qtr, off, df, ak);
-                }
-            }
-            if (more && wave == 0) infos[((j + 1) & 1) * PK_T + lane] = next;
+            __syncthreads();
+            if (j + 1 < tiles) request(j + 1);
+            one_tile(CAREFUL, j);
+            if (j + 1 < tiles) arrive(j + 1);
         }
-        if (careful || !__syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) break;
-        careful = true;
+    };
+    all_tiles(std::false_type());
+    if (__syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) {
+        if (tiles > 0) request(0);
+        all_tiles(std::true_type());
     }
     pk_store<HD>(av, 1.f, dv + (t.k0 + key) * lddv + (int64_t)kvh * HD, mine);
     pk_store<HD>(ak, a.scale, dk + (t.k0 + key) * lddk + (int64_t)kvh * HD, mine);
@@ -747,14 +786,14 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
 
 template <int HD>
 hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* workspace, hipStream_t st) {
-    constexpr int SMEM = 4 * PK_T * HD * 2, SMEM_KV = SMEM + 2 * PK_T * 16;
+    constexpr int SMEM = 4 * PK_T * HD * 2, SMEM_KV = SMEM + 2 * PK_T * 20;
     static const hipError_t attr_q = pk_lds(pk_dq_kernel<HD>, SMEM), attr_kv = pk_lds(pk_dkv_kernel<HD>, SMEM_KV);
     if (attr_q != hipSuccess) return attr_q;
     if (attr_kv != hipSuccess) return attr_kv;
     const int64_t rows = a.total_q * a.n_heads, G = a.n_heads / a.n_kv;
     const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv), blocks = (rows * (HD / 8) + 255) / 256;
     if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    float2* info = static_cast<float2*>(workspace);
+    uint4* info = static_cast<uint4*>(workspace);
     hipError_t e = hipSuccess;
     if (rows > 0) {
         hipLaunchKernelGGL(pk_delta_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, g.out, g.ldo, g.dout, g.lddo, g.lse, info);
@@ -777,7 +816,7 @@ size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim) {
     const int shares = pk_shares(a);
     return shares == 1 ? 0 : (size_t)shares * a.total_q * a.n_heads * (head_dim * sizeof(float) + sizeof(float2));
 }
-size_t packed_backward_workspace_bytes(const PackedArgs& a) { return (size_t)a.total_q * a.n_heads * sizeof(float2); }
+size_t packed_backward_workspace_bytes(const PackedArgs& a) { return (size_t)a.total_q * a.n_heads * sizeof(uint4); }
 
 hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
     if (a.total_q == 0 || a.n_seq == 0) return hipSuccess;
