@@ -321,6 +321,21 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
                                         const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
                                         int64_t lddv);
 
+/* Token cross-entropy of a layer's outputs and its gradient (an LM head: d_out outputs; the layer's r, y_dtype and ldy are not used), without
+ * the logits ever being stored.  loss: kind AGZO_LOSS_CE, target ids [n_tokens]; rows whose id is not in [0, d_out) are not counted.
+ *   ce_forward: *loss_dev = mean over the counted rows of lse_t - y_t[id] (0 if there are none) and, where wanted, lse [n_tokens] device fp32,
+ *     lse_t = log sum exp of row t's logits, of every row.  bf16 and fp32 layers; the loss is agzo_layer_forward_sketch's, bit for bit.
+ *   ce_backward (bf16 layers): with D = (softmax(Y) - onehot(id)) g / count in the counted rows, 0 in the others, dX = D W [n_tokens][d_in]
+ *     and dW = D^T X [d_out][d_in], bf16, overwritten; either may be NULL.  lse: of ce_forward with the same arguments; g = *g_dev (1 if NULL).  The
+ *     logits are made again for a piece of the outputs at a time, D is rounded to bf16 for the products, sums are fp32, in an order that
+ *     depends on the shape alone.  Workspace: three to five buffers of a piece, of 2^27 values at most unless n_tokens or d_in pass 2^17.
+ * Device, workspace and captures as for the calls on packed batches.
+ * Errors: AGZO_EINVAL for a bad layer or loss, NULL or misaligned tensors, outputs that overlap an input or each other, more than 2^21
+ * tokens or inputs (backward). */
+int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, double* loss_dev, float* lse);
+int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, const float* lse,
+                     const double* g_dev, void* dX, int64_t lddx, void* dW, int64_t lddw);
+
 /* Alg. 2 for n independent single-layer problems in one call (a layer set whose projections each have their own loss
  * and their own scalar g): every layer's base forward, all bases together (as agzo_basis_many), all projections X B
  * in one launch, the perturbed forwards, every scalar, and all updates in one batched sweep (as agzo_update_many).

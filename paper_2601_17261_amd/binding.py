@@ -29,7 +29,8 @@ EXPORTS = ["agzo_create", "agzo_destroy", "agzo_last_error", "agzo_check", "agzo
            "agzo_layer_forward_sketch", "agzo_qr", "agzo_basis", "agzo_perturbed_forward", "agzo_two_point", "agzo_dense_perturb", "agzo_update", "agzo_update_noalloc",
            "agzo_update_many", "agzo_step", "agzo_step_no_update", "agzo_basis_many", "agzo_step_many",
            "agzo_glue_rmsnorm", "agzo_glue_swiglu", "agzo_glue_add", "agzo_glue_attention",
-           "agzo_glue_qk_norm_rope", "agzo_glue_qk_norm_rope_backward", "agzo_glue_attention_packed", "agzo_glue_attention_packed_backward"]
+           "agzo_glue_qk_norm_rope", "agzo_glue_qk_norm_rope_backward", "agzo_glue_attention_packed", "agzo_glue_attention_packed_backward",
+           "agzo_ce_forward", "agzo_ce_backward"]
 
 
 class AgzoLayer(ctypes.Structure):
@@ -122,6 +123,8 @@ def load():
     lib.agzo_glue_qk_norm_rope_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, f32, f32]
     lib.agzo_glue_attention_packed.argtypes = [vp, pp, vp, i64, vp]
     lib.agzo_glue_attention_packed_backward.argtypes = [vp, pp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64]
+    lib.agzo_ce_forward.argtypes = [vp, lp, vp, vp, sp, vp, vp]
+    lib.agzo_ce_backward.argtypes = [vp, lp, vp, vp, sp, vp, vp, vp, i64, vp, i64]
     lib.agzo_step.argtypes = [vp, lp, vp, vp, sp, i32, f32, f32, u64, i32, vp]
     lib.agzo_step_no_update.argtypes = [vp, lp, vp, vp, sp, i32, f32, u64, i32, vp, vp]
     for name in EXPORTS:
@@ -361,6 +364,20 @@ class Context:
         for t in tensors:
             if t is not None and t.device != self.stream.device:
                 raise ValueError("a tensor on %s, and the context is of %s" % (t.device, self.stream.device))
+
+    def ce_forward(self, L, W, X, loss, loss_dev, lse=None):
+        """loss: make_loss(ids, LOSS_CE); loss_dev: one float64 on the device; lse: float32 [n_tokens] or None."""
+        self._same_device(W, X, loss_dev, lse)
+        self._rc(self.lib.agzo_ce_forward(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), _flat(loss_dev, "loss_dev", torch.float64, 1),
+                                          _flat(lse, "lse", torch.float32, L.n_tokens)))
+
+    def ce_backward(self, L, W, X, loss, lse, dX, dW, g_dev=None):
+        """lse: of ce_forward; dX like X, dW like W (either may be None); g_dev: one float64 on the device or None (1)."""
+        self._same_device(W, X, lse, dX, dW, g_dev)
+        _same_shape("dX", dX, X)
+        _same_shape("dW", dW, W)
+        self._rc(self.lib.agzo_ce_backward(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), _flat(lse, "lse", torch.float32, L.n_tokens),
+                                           _flat(g_dev, "g_dev", torch.float64, 1), *_rows(dX, "dX"), *_rows(dW, "dW")))
 
     def glue_qk_norm_rope(self, q, k, positions, q_out, k_out, head_dim=128, q_gain=None, k_gain=None, eps=1e-6, rope_theta=1.0e6):
         """q [n][heads * head_dim], k [n][key heads * head_dim] -> q_out, k_out; either side may be None with its result."""

@@ -389,7 +389,7 @@ struct SideForward { hipStream_t stream; int slots; };
 int op_forward(agzo_ctx* ctx, const agzo_layer& L, const Plan& p, const void* W, const void* X, const float* P,
                float eps_signed, uint64_t seed, void* Y, const agzo_loss_spec* loss, double* loss_dev,
                bool shared = false, int part_slot = 0, bool defer_finish = false, bool fused_sketch = false, bool ext_ready = false, int ext_side = 0,
-               const SideForward* side = nullptr) {
+               const SideForward* side = nullptr, float* lse = nullptr) {
     hipStream_t st = side ? side->stream : ctx->stream;
     GemmLossArgs la;
     const bool has_loss = loss && loss->kind != AGZO_LOSS_NONE;
@@ -429,7 +429,7 @@ int op_forward(agzo_ctx* ctx, const agzo_layer& L, const Plan& p, const void* W,
         }
         if (ce)
             HIPCHK(launch_ce_combine(la.ce_ms, la.ce_tl, ids, L.n_tokens, L.d_out, gemm_bf16_ce_chunks(L.d_out), shared ? 3 : 1,
-                                     la.partials, loss_dev, st));
+                                     la.partials, loss_dev, st, lse));
     } else {
         F32FwdArgs a = forward_f32_args(L, W, X, P, eps_signed, seed, la, shared);
         if (!ce) {
@@ -441,7 +441,7 @@ int op_forward(agzo_ctx* ctx, const agzo_layer& L, const Plan& p, const void* W,
             a.ldy = Y ? L.ldy : L.d_out;
             if (shared) { a.P = nullptr; a.shared = 0; }
             HIPCHK(launch_forward_f32_many(&a, 1, st));
-            HIPCHK(launch_ce_rows_f32(a.Y, a.ldy, L.n_tokens, L.d_out, ids, la.partials, loss_dev, st));
+            HIPCHK(launch_ce_rows_f32(a.Y, a.ldy, L.n_tokens, L.d_out, ids, la.partials, loss_dev, st, lse));
             for (int ph = 1; shared && ph < 3; ++ph) {      // Y0 + eps D, then - 2 eps D
                 HIPCHK(launch_rank_term_f32(a.Y, a.ldy, L.n_tokens, L.d_out, P, L.r, ph == 1 ? eps_signed : -2.f * eps_signed, seed, st));
                 HIPCHK(launch_ce_rows_f32(a.Y, a.ldy, L.n_tokens, L.d_out, ids, la.partials, loss_dev + ph, st));
@@ -1422,6 +1422,51 @@ int packed_args(agzo_ctx* ctx, const agzo_packed_attention* a, PackedArgs& out) 
     return check_device(ctx);
 }
 }  // namespace
+
+namespace {
+// the checks of agzo_ce_forward and agzo_ce_backward; copy: the layer with a rank that no call on it uses
+int check_ce(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, agzo_layer& copy) {
+    if (!ctx) return AGZO_EINVAL;
+    if (!L) return fail(ctx, AGZO_EINVAL, "layer descriptor is NULL");
+    copy = *L;
+    copy.r = 1;
+    TRY(check_layer(ctx, &copy, true));
+    if (!W || !X) return fail(ctx, AGZO_EINVAL, "W or X is NULL");
+    TRY(check_operands(ctx, &copy, W, X));
+    if (!loss || loss->kind != AGZO_LOSS_CE || !loss->target) return fail(ctx, AGZO_EINVAL, "a cross-entropy with target ids is needed");
+    if (reinterpret_cast<uintptr_t>(loss->target) & 3) return fail(ctx, AGZO_EINVAL, "the target ids are misaligned");
+    return check_device(ctx);
+}
+}  // namespace
+
+int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, double* loss_dev, float* lse) {
+    agzo_layer c;
+    TRY(check_ce(ctx, L, W, X, loss, c));
+    if (!loss_dev) return fail(ctx, AGZO_EINVAL, "loss_dev is NULL");
+    if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
+    const Plan p = make_forward_plan(c, loss, false, W, X, nullptr);
+    TRY(reserve(ctx, p.total));
+    return op_forward(ctx, c, p, W, X, nullptr, 0.f, 0, nullptr, loss, loss_dev, false, 0, false, false, false, 0, nullptr, lse);
+}
+
+int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, const float* lse,
+                     const double* g_dev, void* dX, int64_t lddx, void* dW, int64_t lddw) {
+    agzo_layer c;
+    TRY(check_ce(ctx, L, W, X, loss, c));
+    if (c.dtype != AGZO_BF16) return fail(ctx, AGZO_EINVAL, "gradients are made for bf16 layers");
+    if (c.n_tokens > (1LL << 21) || c.d_in > (1LL << 21)) return fail(ctx, AGZO_EINVAL, "more than 2^21 tokens or inputs");
+    if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3)) return fail(ctx, AGZO_EINVAL, "lse is NULL or misaligned");
+    if (!dX && !dW) return fail(ctx, AGZO_EINVAL, "neither dX nor dW is wanted");
+    if (dX) TRY(check_glue(ctx, c.n_tokens, c.d_in, {dX}, {lddx}));
+    if (dW) TRY(check_glue(ctx, c.d_out, c.d_in, {dW}, {lddw}));
+    TRY(check_apart(ctx, {named("dX", dX, lddx, c.n_tokens, c.d_in), named("dW", dW, lddw, c.d_out, c.d_in)},
+                    {named("X", X, c.ldx, c.n_tokens, c.d_in), named("W", W, c.ldw, c.d_out, c.d_in)}));
+    TRY(reserve(ctx, ce_grad_workspace_bytes(c.n_tokens, c.d_out, c.d_in, dX != nullptr, dW != nullptr)));
+    const CeGradArgs a{static_cast<const bf16_t*>(X), c.ldx, static_cast<const bf16_t*>(W), c.ldw, c.n_tokens, c.d_out, c.d_in,
+                       static_cast<const int32_t*>(loss->target), lse, g_dev, static_cast<bf16_t*>(dX), lddx, static_cast<bf16_t*>(dW), lddw};
+    HIPCHK(launch_ce_grad(a, ctx->ws, ctx->stream));
+    return AGZO_OK;
+}
 
 int agzo_glue_qk_norm_rope(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out,
                            int64_t ldqo, void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,

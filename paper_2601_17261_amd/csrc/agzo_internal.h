@@ -333,15 +333,27 @@ hipError_t launch_update_many(const UpdateDesc* d, int n, int nk, void* workspac
 
 // loss.hip
 // cross-entropy from the GEMM's per-chunk softmax statistics: out[ph] = mean over rows with target >= 0 of
-// log(sum exp) - logit[target];  ms: float2 [nphase][nchunk][M], tl: float [nphase][M]
+// log(sum exp) - logit[target], lse (nullable): log(sum exp) of every row;  ms: float2 [nphase][nchunk][M], tl: float [nphase][M]
 int gemm_bf16_ce_chunks(int64_t N);
 // tokens per (sum, count) pair of the scratch, 2 doubles a pair and phase
 constexpr int kCeCombineTokens = 16;
 hipError_t launch_ce_combine(const void* ms, const float* tl, const int32_t* target, int64_t M, int64_t N, int nchunk,
-                             int nphase, double* scratch, double* out, hipStream_t st);
+                             int nphase, double* scratch, double* out, hipStream_t st, float* lse = nullptr);
 // cross-entropy of stored fp32 logits Y [M][N] (fp32-storage path): out[0] as above
 hipError_t launch_ce_rows_f32(const float* Y, int64_t ldy, int64_t M, int64_t N, const int32_t* target, double* scratch,
-                              double* out, hipStream_t st);
+                              double* out, hipStream_t st, float* lse = nullptr);
+
+// ce_grad.hip : gradient of that loss: dX [M][d], dW [V][d] bf16 (either may be NULL), g: device scalar (NULL: 1), lse: of every row
+struct CeGradArgs {
+    const bf16_t* X; int64_t ldx;
+    const bf16_t* W; int64_t ldw;
+    int64_t M, V, d;
+    const int32_t* ids; const float* lse; const double* g;
+    bf16_t* dX; int64_t lddx;
+    bf16_t* dW; int64_t lddw;
+};
+size_t ce_grad_workspace_bytes(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw);
+hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st);
 // out[b] = scale * sum(partials[b*n .. b*n+n)), b < nout
 hipError_t launch_finish_loss(const double* partials, int n, double scale, double* out, int nout, hipStream_t st);
 hipError_t launch_two_point(double* out4, float eps, int one_sided, hipStream_t st);

@@ -1,0 +1,193 @@
+// Gradient of the softmax cross-entropy of a layer's outputs Y = X W^T [M][V], whose mean over the counted rows is the loss of loss.hip:
+//     D_tv = (exp(y_tv - lse_t) - [v = id_t]) g / count   (0 in rows that are not counted),     dX = D W,     dW = D^T X.
+// The logits are made once more, for a piece of the outputs at a time, and only D of that piece is stored, as bf16, in both orders: the
+// products contract over outputs and over tokens, and the forward's kernels want the contracted dimension side by side.  So W's piece and X are
+// transposed too, which is 2 of the 2 M Vp d operations' bytes a value.
+// This file: everything between the products.
+#include "agzo_internal.h"
+
+namespace agzo {
+
+namespace {
+
+// g / max(count, 1) of the rows whose id is an output, as fp32; one workgroup
+__global__ __launch_bounds__(1024) void ce_scale_kernel(const int32_t* __restrict__ ids, int64_t M, int64_t V, const double* __restrict__ g, float* __restrict__ scale) {
+    __shared__ int red[16];
+    int n = 0;
+    for (int64_t t = threadIdx.x; t < M; t += 1024) n += ids[t] >= 0 && ids[t] < V;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 16; ++w) n += red[w];
+    *scale = (float)((g ? *g : 1.0) / (double)max(n, 1));
+}
+
+// y [C][ldy] = x^T of x [R][ldx] in 64 x 64 tiles; columns R .. ldy of y are zeros (rows C and on are not written), and with ids those of the rows
+// that are not counted: D is 0 there, and a value that is not finite would make NaNs of it
+__global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict__ x, int64_t ldx, int64_t R, int64_t C, bf16_t* __restrict__ y, int64_t ldy,
+                                                        const int32_t* __restrict__ ids, int64_t V) {
+    __shared__ bf16_t tile[64][66];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    const int t = threadIdx.x;
+    for (int i = t; i < 64 * 8; i += 256) {
+        const int r = i >> 3, c = (i & 7) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        const bool counted = !ids || (r0 + r < R && ids[r0 + r] >= 0 && ids[r0 + r] < V);
+        if (counted && r0 + r < R && c0 + c < C) v = *reinterpret_cast<const uint4*>(x + (r0 + r) * ldx + c0 + c);      // (C is a multiple of 8)
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<uint32_t*>(&tile[r][c + 2 * k]) = w[k];
+    }
+    __syncthreads();
+    for (int i = t; i < 64 * 8; i += 256) {
+        const int c = i >> 3, r = (i & 7) * 8;
+        if (c0 + c >= C || r0 + r >= ldy) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[r + 2 * k][c] | (uint32_t)tile[r + 2 * k + 1][c] << 16;
+        *reinterpret_cast<uint4*>(y + (c0 + c) * ldy + r0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// D and D^T of a piece, from its logits z [M][ldz]: outputs v0 .. v0 + n; D [M][ldd] zero from column n on, D^T [n][ldt] zero from column M on
+__global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __restrict__ z, int64_t ldz, int64_t M, int64_t v0, int64_t n, int64_t V,
+                                                              const int32_t* __restrict__ ids, const float* __restrict__ lse, const float* __restrict__ scale,
+                                                              bf16_t* __restrict__ d, int64_t ldd, bf16_t* __restrict__ dt, int64_t ldt) {
+    __shared__ bf16_t tile[64][66];
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    const int t = threadIdx.x;
+    const float f = *scale;
+    for (int i = t; i < 64 * 32; i += 256) {
+        const int r = i >> 5, c = (i & 31) * 2;
+        const int64_t row = r0 + r;
+        float v[2] = {0.f, 0.f};
+        if (row < M) {
+            const int id = ids[row];
+            if (id >= 0 && id < V) {
+                const float l = lse[row];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (c0 + c + u < n) {
+                        const float p = __builtin_amdgcn_exp2f((z[row * ldz + c0 + c + u] - l) * 1.44269504088896341f);
+                        v[u] = (v0 + c0 + c + u == id ? p - 1.f : p) * f;
+                    }
+            }
+        }
+        const uint32_t w = pack_bf16x2(v[0], v[1]);
+        *reinterpret_cast<uint32_t*>(&tile[r][c]) = w;
+        if (row < M && c0 + c < ldd) *reinterpret_cast<uint32_t*>(d + row * ldd + c0 + c) = w;
+    }
+    __syncthreads();
+    for (int i = t; i < 64 * 8; i += 256) {
+        const int c = i >> 3, r = (i & 7) * 8;
+        if (c0 + c >= n || r0 + r >= ldt) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[r + 2 * k][c] | (uint32_t)tile[r + 2 * k + 1][c] << 16;
+        *reinterpret_cast<uint4*>(dt + (c0 + c) * ldt + r0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// sum (+)= part, rows of d side by side; last: out <- the sum as bf16
+__global__ __launch_bounds__(256) void ce_add_kernel(const float* __restrict__ part, float* __restrict__ sum, int64_t M, int64_t d, bool first, bf16_t* __restrict__ out, int64_t ldo) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= M * d) return;
+    float4 s = *reinterpret_cast<const float4*>(part + i);
+    if (!first) {
+        const float4 o = *reinterpret_cast<const float4*>(sum + i);
+        s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+    }
+    if (out) {
+        const int64_t row = i / d;
+        *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+    } else {
+        *reinterpret_cast<float4*>(sum + i) = s;
+    }
+}
+
+inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
+
+// Outputs of a piece: some 2^27 values of D (and of W transposed), which is 256 MB each, and pieces of about the same size
+int64_t ce_piece(int64_t M, int64_t V, int64_t d) {
+    const int64_t most = std::max<int64_t>(1024, (1LL << 27) / std::max(M, d) / 256 * 256);
+    const int64_t pieces = (V + most - 1) / most;
+    return ((V + pieces - 1) / pieces + 255) / 256 * 256;
+}
+
+struct CeLayout {
+    int64_t piece, m64;
+    size_t scale, z, d, dt, wt, xt, part, sum, total;
+};
+CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) {
+    CeLayout l;
+    l.piece = std::min(ce_piece(M, V, d), up64(V));
+    l.m64 = up64(M);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
+    l.scale = take(256);
+    l.z = take((size_t)M * l.piece * 4);
+    l.d = take((size_t)M * l.piece * 2);
+    l.dt = take((size_t)l.piece * l.m64 * 2);
+    l.wt = take(want_dx ? (size_t)d * l.piece * 2 : 0);
+    l.part = take(want_dx ? (size_t)M * d * 4 : 0);
+    l.sum = take(want_dx ? (size_t)M * d * 4 : 0);
+    l.xt = take(want_dw ? (size_t)d * l.m64 * 2 : 0);
+    l.total = o;
+    return l;
+}
+
+hipError_t transpose(const bf16_t* x, int64_t ldx, int64_t R, int64_t C, bf16_t* y, int64_t ldy, const int32_t* ids, int64_t V, hipStream_t st) {
+    hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)((ldy + 63) / 64), (unsigned)((C + 63) / 64)), dim3(256), 0, st, x, ldx, R, C, y, ldy, ids, V);
+    return hipGetLastError();
+}
+
+hipError_t product(const bf16_t* x, int64_t ldx, const bf16_t* w, int64_t ldw, int64_t M, int64_t N, int64_t K, void* y, int y_dtype, int64_t ldy, hipStream_t st) {
+    GemmBf16Args a;
+    a.X = x; a.ldx = ldx; a.W = w; a.ldw = ldw; a.M = M; a.N = N; a.K = K; a.Y = y; a.y_dtype = y_dtype; a.ldy = ldy;
+    a.P = nullptr; a.r = 1; a.eps_signed = 0.f; a.seed = 0;
+    a.loss.kind = AGZO_LOSS_NONE; a.loss.target_dtype = 0; a.loss.target = nullptr; a.loss.ldt = 0; a.loss.partials = nullptr;
+    return launch_gemm_bf16(a, st);
+}
+
+}  // namespace
+
+size_t ce_grad_workspace_bytes(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) { return ce_layout(M, V, d, want_dx, want_dw).total; }
+
+hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) {
+    const CeLayout l = ce_layout(a.M, a.V, a.d, a.dX != nullptr, a.dW != nullptr);
+    char* ws = static_cast<char*>(workspace);
+    float* scale = reinterpret_cast<float*>(ws + l.scale);
+    float* z = reinterpret_cast<float*>(ws + l.z);
+    bf16_t *D = reinterpret_cast<bf16_t*>(ws + l.d), *Dt = reinterpret_cast<bf16_t*>(ws + l.dt), *Wt = reinterpret_cast<bf16_t*>(ws + l.wt), *Xt = reinterpret_cast<bf16_t*>(ws + l.xt);
+    float *part = reinterpret_cast<float*>(ws + l.part), *sum = reinterpret_cast<float*>(ws + l.sum);
+#define CE_TRY(expr)                            \
+    do {                                        \
+        const hipError_t e__ = (expr);          \
+        if (e__ != hipSuccess) return e__;      \
+    } while (0)
+    hipLaunchKernelGGL(ce_scale_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, scale);
+    CE_TRY(hipGetLastError());
+    if (a.dW) CE_TRY(transpose(a.X, a.ldx, a.M, a.d, Xt, l.m64, a.ids, a.V, st));
+    for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
+        const int64_t n = std::min(l.piece, a.V - v0), n64 = up64(n);
+        const bf16_t* W = a.W + v0 * a.ldw;
+        CE_TRY(product(a.X, a.ldx, W, a.ldw, a.M, n, a.d, z, AGZO_F32, n, st));
+        hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(n64 / 64), (unsigned)(l.m64 / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.V, a.ids, a.lse, scale, D, n64, Dt, l.m64);
+        CE_TRY(hipGetLastError());
+        if (a.dW) CE_TRY(product(Dt, l.m64, Xt, l.m64, n, a.d, l.m64, a.dW + v0 * a.lddw, AGZO_BF16, a.lddw, st));
+        if (a.dX) {
+            CE_TRY(transpose(W, a.ldw, n, a.d, Wt, n64, nullptr, 0, st));
+            CE_TRY(product(D, n64, Wt, n64, a.M, a.d, n64, part, AGZO_F32, a.d, st));
+            const bool last = v0 + n >= a.V;
+            hipLaunchKernelGGL(ce_add_kernel, dim3((unsigned)((a.M * a.d / 4 + 255) / 256)), dim3(256), 0, st, part, sum, a.M, a.d, v0 == 0, last ? a.dX : nullptr, a.lddx);
+            CE_TRY(hipGetLastError());
+        }
+    }
+#undef CE_TRY
+    return hipSuccess;
+}
+
+}  // namespace agzo

@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void finish_two_point_many_kernel(const Finish
 constexpr int CE_TOK = kCeCombineTokens, CE_LANES = 256 / CE_TOK, CE_FLIGHT = 8;
 __global__ __launch_bounds__(256) void ce_combine_kernel(const float2* __restrict__ ms, const float* __restrict__ tl,
                                                          const int32_t* __restrict__ target, int64_t M, int64_t N,
-                                                         int nchunk, double* __restrict__ scratch) {
+                                                         int nchunk, double* __restrict__ scratch, float* __restrict__ lse) {
     __shared__ double rm[CE_LANES][CE_TOK], rs[CE_LANES][CE_TOK];
     const int tid = threadIdx.x, tok = tid % CE_TOK, part = tid / CE_TOK;
     const int ph = blockIdx.y;
@@ -91,7 +91,8 @@ __global__ __launch_bounds__(256) void ce_combine_kernel(const float2* __restric
     const int tgt = t < M ? target[t] : -1;
     const bool counted = tgt >= 0 && tgt < N;
     double mx = -INFINITY, s = 0.0;
-    if (counted) {
+    const bool wanted = counted || (lse && t < M);             // (lse: of every row)
+    if (wanted) {
         const float2* m = ms + (int64_t)ph * nchunk * M + t;
         for (int c0 = part; c0 < nchunk; c0 += CE_LANES * CE_FLIGHT) {
             float2 v[CE_FLIGHT];
@@ -120,10 +121,13 @@ __global__ __launch_bounds__(256) void ce_combine_kernel(const float2* __restric
     __syncthreads();
     if (part != 0) return;
     double loss = 0.0, cnt = 0.0;
-    if (counted) {
+    if (wanted) {
         for (int l = 1; l < CE_LANES && l < nchunk; ++l) mx = fmax(mx, rm[l][tok]);
         s = 0.0;
         for (int l = 0; l < CE_LANES && l < nchunk; ++l) s += rs[l][tok] * exp(rm[l][tok] - mx);
+        if (lse) lse[(int64_t)ph * M + t] = (float)(log(s) + mx);
+    }
+    if (counted) {
         loss = log(s) + mx - (double)tl[(int64_t)ph * M + t];
         cnt = 1.0;
     }
@@ -157,22 +161,23 @@ __global__ __launch_bounds__(256) void ce_finish_kernel(const double* __restrict
 }
 
 hipError_t launch_ce_combine(const void* ms, const float* tl, const int32_t* target, int64_t M, int64_t N, int nchunk,
-                             int nphase, double* scratch, double* out, hipStream_t st) {
+                             int nphase, double* scratch, double* out, hipStream_t st, float* lse) {
     const int nblk = (int)((M + CE_TOK - 1) / CE_TOK);
     hipLaunchKernelGGL(ce_combine_kernel, dim3(nblk, nphase), dim3(256), 0, st, reinterpret_cast<const float2*>(ms), tl,
-                       target, M, N, nchunk, scratch);
+                       target, M, N, nchunk, scratch, lse);
     hipLaunchKernelGGL(ce_finish_kernel, dim3(nphase), dim3(256), 0, st, scratch, nblk, out);
     return hipGetLastError();
 }
 
 // fp32-storage path: one workgroup per token row of stored logits, fp64 statistics
 __global__ __launch_bounds__(256) void ce_rows_f32_kernel(const float* __restrict__ Y, int64_t ldy, int64_t M, int64_t N,
-                                                          const int32_t* __restrict__ target, double* __restrict__ scratch) {
+                                                          const int32_t* __restrict__ target, double* __restrict__ scratch, float* __restrict__ lse) {
     __shared__ double red[256];
     const int tid = threadIdx.x;
     const int64_t t = blockIdx.x;
     const int tgt = target[t];
-    if (tgt < 0 || tgt >= N) {   // ignored row; an id outside the layer's outputs has no logit and is skipped too
+    const bool counted = tgt >= 0 && tgt < N;
+    if (!counted && !lse) {   // ignored row; an id outside the layer's outputs has no logit and is skipped too
         if (tid == 0) { scratch[t * 2] = 0.0; scratch[t * 2 + 1] = 0.0; }
         return;
     }
@@ -196,14 +201,15 @@ __global__ __launch_bounds__(256) void ce_rows_f32_kernel(const float* __restric
         __syncthreads();
     }
     if (tid == 0) {
-        scratch[t * 2] = log(red[0]) + mx - (double)y[tgt];
-        scratch[t * 2 + 1] = 1.0;
+        scratch[t * 2] = counted ? log(red[0]) + mx - (double)y[tgt] : 0.0;
+        scratch[t * 2 + 1] = counted ? 1.0 : 0.0;
+        if (lse) lse[t] = (float)(log(red[0]) + mx);
     }
 }
 
 hipError_t launch_ce_rows_f32(const float* Y, int64_t ldy, int64_t M, int64_t N, const int32_t* target, double* scratch,
-                              double* out, hipStream_t st) {
-    hipLaunchKernelGGL(ce_rows_f32_kernel, dim3((unsigned)M), dim3(256), 0, st, Y, ldy, M, N, target, scratch);
+                              double* out, hipStream_t st, float* lse) {
+    hipLaunchKernelGGL(ce_rows_f32_kernel, dim3((unsigned)M), dim3(256), 0, st, Y, ldy, M, N, target, scratch, lse);
     hipLaunchKernelGGL(ce_finish_kernel, dim3(1), dim3(256), 0, st, scratch, (int)M, out);
     return hipGetLastError();
 }
