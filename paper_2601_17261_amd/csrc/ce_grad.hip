@@ -2,16 +2,17 @@
 //     D_tv = (exp(y_tv - lse_t) - [v = id_t]) g / count   (0 in rows that are not counted),     dX = D W,     dW = D^T X.
 // The logits are made once more, for a piece of the outputs at a time, and only D of that piece is stored, as bf16, in both orders: the
 // products contract over outputs and over tokens, and the forward's kernels want the contracted dimension side by side.  So W's piece and X are
-// transposed too, which is 2 of the 2 M Vp d operations' bytes a value.
-// This file: everything between the products.
-#include "agzo_internal.h"
+// transposed too.  The products are those of gemm_bf16_aligned.hip where a 256 x 256 tile fits: D leaves the logits' product in both orders, and dX is
+// summed over the pieces in fp32, in shares of a piece where its tiles alone would not fill the chip.  Other shapes go through fp32 logits and the forward's kernels.
+// This file: everything around the products.
+#include "gemm_bf16_common.h"
 
 namespace agzo {
 
 namespace {
 
-// g / max(count, 1) of the rows whose id is an output, as fp32; one workgroup
-__global__ __launch_bounds__(1024) void ce_scale_kernel(const int32_t* __restrict__ ids, int64_t M, int64_t V, const double* __restrict__ g, float* __restrict__ scale) {
+// g / max(count, 1), count of the rows whose id is an output, as each such row's factor, 0 for the others; one workgroup
+__global__ __launch_bounds__(1024) void ce_factor_kernel(const int32_t* __restrict__ ids, int64_t M, int64_t V, const double* __restrict__ g, float* __restrict__ rowf) {
     __shared__ int red[16];
     int n = 0;
     for (int64_t t = threadIdx.x; t < M; t += 1024) n += ids[t] >= 0 && ids[t] < V;
@@ -19,9 +20,18 @@ __global__ __launch_bounds__(1024) void ce_scale_kernel(const int32_t* __restric
     for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < 16; ++w) n += red[w];
-    *scale = (float)((g ? *g : 1.0) / (double)max(n, 1));
+    n = 0;
+    for (int w = 0; w < 16; ++w) n += red[w];
+    const float f = (float)((g ? *g : 1.0) / (double)max(n, 1));
+    for (int64_t t = threadIdx.x; t < M; t += 1024) rowf[t] = ids[t] >= 0 && ids[t] < V ? f : 0.f;
+}
+
+// columns from .. to of rows of ld values <- 0
+__global__ __launch_bounds__(256) void ce_zero_kernel(bf16_t* __restrict__ y, int64_t rows, int64_t ld, int64_t from, int64_t to) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, w = to - from;
+    if (i >= rows * w) return;
+    const int64_t row = i / w;
+    y[row * ld + from + (i - row * w)] = 0;
 }
 
 // y [C][ldy] = x^T of x [R][ldx] in 64 x 64 tiles; columns R .. ldy of y are zeros (rows C and on are not written), and with ids those of the rows
@@ -52,28 +62,26 @@ __global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict
 }
 
 // D and D^T of a piece, from its logits z [M][ldz]: outputs v0 .. v0 + n; D [M][ldd] zero from column n on, D^T [n][ldt] zero from column M on
-__global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __restrict__ z, int64_t ldz, int64_t M, int64_t v0, int64_t n, int64_t V,
-                                                              const int32_t* __restrict__ ids, const float* __restrict__ lse, const float* __restrict__ scale,
+__global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __restrict__ z, int64_t ldz, int64_t M, int64_t v0, int64_t n,
+                                                              const int32_t* __restrict__ ids, const float* __restrict__ lse, const float* __restrict__ rowf,
                                                               bf16_t* __restrict__ d, int64_t ldd, bf16_t* __restrict__ dt, int64_t ldt) {
     __shared__ bf16_t tile[64][66];
     const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
     const int t = threadIdx.x;
-    const float f = *scale;
     for (int i = t; i < 64 * 32; i += 256) {
         const int r = i >> 5, c = (i & 31) * 2;
         const int64_t row = r0 + r;
         float v[2] = {0.f, 0.f};
-        if (row < M) {
+        const float f = row < M ? rowf[row] : 0.f;
+        if (f != 0.f) {
+            const float l = lse[row];
             const int id = ids[row];
-            if (id >= 0 && id < V) {
-                const float l = lse[row];
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    if (c0 + c + u < n) {
-                        const float p = __builtin_amdgcn_exp2f((z[row * ldz + c0 + c + u] - l) * 1.44269504088896341f);
-                        v[u] = (v0 + c0 + c + u == id ? p - 1.f : p) * f;
-                    }
-            }
+            for (int u = 0; u < 2; ++u)
+                if (c0 + c + u < n) {
+                    const float p = __builtin_amdgcn_exp2f((z[row * ldz + c0 + c + u] - l) * 1.44269504088896341f);
+                    v[u] = (v0 + c0 + c + u == id ? p - 1.f : p) * f;
+                }
         }
         const uint32_t w = pack_bf16x2(v[0], v[1]);
         *reinterpret_cast<uint32_t*>(&tile[r][c]) = w;
@@ -90,21 +98,25 @@ __global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __res
     }
 }
 
-// sum (+)= part, rows of d side by side; last: out <- the sum as bf16
-__global__ __launch_bounds__(256) void ce_add_kernel(const float* __restrict__ part, float* __restrict__ sum, int64_t M, int64_t d, bool first, bf16_t* __restrict__ out, int64_t ldo) {
+// sum += part
+__global__ __launch_bounds__(256) void ce_add_kernel(const float* __restrict__ part, float* __restrict__ sum, int64_t n) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const float4 a = *reinterpret_cast<const float4*>(part + i), b = *reinterpret_cast<const float4*>(sum + i);
+    *reinterpret_cast<float4*>(sum + i) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
+
+// dX: the shares' sums [shares][M][d] added in order, as bf16
+__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, int shares, int64_t M, int64_t d, bf16_t* __restrict__ out, int64_t ldo) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= M * d) return;
-    float4 s = *reinterpret_cast<const float4*>(part + i);
-    if (!first) {
-        const float4 o = *reinterpret_cast<const float4*>(sum + i);
+    float4 s = *reinterpret_cast<const float4*>(sums + i);
+    for (int k = 1; k < shares; ++k) {
+        const float4 o = *reinterpret_cast<const float4*>(sums + k * M * d + i);
         s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
     }
-    if (out) {
-        const int64_t row = i / d;
-        *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
-    } else {
-        *reinterpret_cast<float4*>(sum + i) = s;
-    }
+    const int64_t row = i / d;
+    *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -118,22 +130,32 @@ int64_t ce_piece(int64_t M, int64_t V, int64_t d) {
 }
 
 struct CeLayout {
-    int64_t piece, m64;
-    size_t scale, z, d, dt, wt, xt, part, sum, total;
+    int64_t piece, m64, width;      // outputs of a piece, tokens and outputs as far as zeros go
+    bool tiles_z, tiles_x;          // 256 x 256 tiles fit the logits of a piece, the sums of dX
+    int shares;
+    size_t rowf, z, d, dt, wt, xt, part, sum, total;
 };
+// D's columns of a piece of n outputs: its shares' slices
+int64_t ce_width(int64_t n, int shares) { return shares == 1 ? std::max<int64_t>(up64(n), 2 * BK) : std::max<int64_t>((up64(n) / 64 + shares - 1) / shares, 2) * 64 * shares; }
+
 CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) {
     CeLayout l;
-    l.piece = std::min(ce_piece(M, V, d), up64(V));
+    l.piece = std::min(ce_piece(M, V, d), V);
     l.m64 = up64(M);
+    l.tiles_z = gemm_bf16_grad_fits(M, l.piece, d);
+    l.tiles_x = gemm_bf16_grad_fits(M, d, 2 * BK);
+    l.shares = want_dx && l.tiles_x ? gemm_bf16_sum_shares(M, d, up64(l.piece) / 64) : 1;
+    l.width = ce_width(l.piece, l.shares);
+    const int64_t last = V - (V - 1) / l.piece * l.piece, logits = !l.tiles_z ? l.piece : gemm_bf16_grad_fits(M, last, d) ? 0 : last;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
-    l.scale = take(256);
-    l.z = take((size_t)M * l.piece * 4);
-    l.d = take((size_t)M * l.piece * 2);
+    l.rowf = take((size_t)M * 4);
+    l.z = take((size_t)M * logits * 4);
+    l.d = take((size_t)M * l.width * 2);
     l.dt = take((size_t)l.piece * l.m64 * 2);
-    l.wt = take(want_dx ? (size_t)d * l.piece * 2 : 0);
-    l.part = take(want_dx ? (size_t)M * d * 4 : 0);
-    l.sum = take(want_dx ? (size_t)M * d * 4 : 0);
+    l.wt = take(want_dx ? (size_t)d * l.width * 2 : 0);
+    l.part = take(want_dx && !l.tiles_x && l.piece < V ? (size_t)M * d * 4 : 0);
+    l.sum = take(want_dx ? (size_t)l.shares * M * d * 4 : 0);
     l.xt = take(want_dw ? (size_t)d * l.m64 * 2 : 0);
     l.total = o;
     return l;
@@ -141,6 +163,12 @@ CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) 
 
 hipError_t transpose(const bf16_t* x, int64_t ldx, int64_t R, int64_t C, bf16_t* y, int64_t ldy, const int32_t* ids, int64_t V, hipStream_t st) {
     hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)((ldy + 63) / 64), (unsigned)((C + 63) / 64)), dim3(256), 0, st, x, ldx, R, C, y, ldy, ids, V);
+    return hipGetLastError();
+}
+
+hipError_t zero_columns(bf16_t* y, int64_t rows, int64_t ld, int64_t from, int64_t to, hipStream_t st) {
+    if (from >= to) return hipSuccess;
+    hipLaunchKernelGGL(ce_zero_kernel, dim3((unsigned)((rows * (to - from) + 255) / 256)), dim3(256), 0, st, y, rows, ld, from, to);
     return hipGetLastError();
 }
 
@@ -159,32 +187,46 @@ size_t ce_grad_workspace_bytes(int64_t M, int64_t V, int64_t d, bool want_dx, bo
 hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) {
     const CeLayout l = ce_layout(a.M, a.V, a.d, a.dX != nullptr, a.dW != nullptr);
     char* ws = static_cast<char*>(workspace);
-    float* scale = reinterpret_cast<float*>(ws + l.scale);
-    float* z = reinterpret_cast<float*>(ws + l.z);
+    float *rowf = reinterpret_cast<float*>(ws + l.rowf), *z = reinterpret_cast<float*>(ws + l.z);
     bf16_t *D = reinterpret_cast<bf16_t*>(ws + l.d), *Dt = reinterpret_cast<bf16_t*>(ws + l.dt), *Wt = reinterpret_cast<bf16_t*>(ws + l.wt), *Xt = reinterpret_cast<bf16_t*>(ws + l.xt);
     float *part = reinterpret_cast<float*>(ws + l.part), *sum = reinterpret_cast<float*>(ws + l.sum);
+    const unsigned sums = (unsigned)((a.M * a.d / 4 + 255) / 256);
 #define CE_TRY(expr)                            \
     do {                                        \
         const hipError_t e__ = (expr);          \
         if (e__ != hipSuccess) return e__;      \
     } while (0)
-    hipLaunchKernelGGL(ce_scale_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, scale);
+    hipLaunchKernelGGL(ce_factor_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, rowf);
     CE_TRY(hipGetLastError());
     if (a.dW) CE_TRY(transpose(a.X, a.ldx, a.M, a.d, Xt, l.m64, a.ids, a.V, st));
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
-        const int64_t n = std::min(l.piece, a.V - v0), n64 = up64(n);
+        const int64_t n = std::min(l.piece, a.V - v0), width = ce_width(n, l.shares);
         const bf16_t* W = a.W + v0 * a.ldw;
-        CE_TRY(product(a.X, a.ldx, W, a.ldw, a.M, n, a.d, z, AGZO_F32, n, st));
-        hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(n64 / 64), (unsigned)(l.m64 / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.V, a.ids, a.lse, scale, D, n64, Dt, l.m64);
-        CE_TRY(hipGetLastError());
-        if (a.dW) CE_TRY(product(Dt, l.m64, Xt, l.m64, n, a.d, l.m64, a.dW + v0 * a.lddw, AGZO_BF16, a.lddw, st));
-        if (a.dX) {
-            CE_TRY(transpose(W, a.ldw, n, a.d, Wt, n64, nullptr, 0, st));
-            CE_TRY(product(D, n64, Wt, n64, a.M, a.d, n64, part, AGZO_F32, a.d, st));
-            const bool last = v0 + n >= a.V;
-            hipLaunchKernelGGL(ce_add_kernel, dim3((unsigned)((a.M * a.d / 4 + 255) / 256)), dim3(256), 0, st, part, sum, a.M, a.d, v0 == 0, last ? a.dX : nullptr, a.lddx);
+        if (gemm_bf16_grad_fits(a.M, n, a.d)) {
+            CE_TRY(launch_gemm_bf16_softmax_grad(a.X, a.ldx, W, a.ldw, a.M, n, a.d, v0, a.ids, a.lse, rowf, D, width, Dt, l.m64, st));
+            if (a.dX) CE_TRY(zero_columns(D, a.M, width, n, width, st));
+            if (a.dW) CE_TRY(zero_columns(Dt, n, l.m64, a.M, l.m64, st));
+        } else {
+            CE_TRY(product(a.X, a.ldx, W, a.ldw, a.M, n, a.d, z, AGZO_F32, n, st));
+            hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(width / 64), (unsigned)(l.m64 / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.ids, a.lse, rowf, D, width, Dt, l.m64);
             CE_TRY(hipGetLastError());
         }
+        if (a.dW) CE_TRY(product(Dt, l.m64, Xt, l.m64, n, a.d, l.m64, a.dW + v0 * a.lddw, AGZO_BF16, a.lddw, st));
+        if (!a.dX) continue;
+        CE_TRY(transpose(W, a.ldw, n, a.d, Wt, width, nullptr, 0, st));
+        if (l.tiles_x) {
+            CE_TRY(launch_gemm_bf16_sum(D, width, Wt, width, a.M, a.d, width / l.shares, l.shares, sum, v0 > 0, st));
+            continue;
+        }
+        CE_TRY(product(D, width, Wt, width, a.M, a.d, width, v0 ? part : sum, AGZO_F32, a.d, st));
+        if (v0) {
+            hipLaunchKernelGGL(ce_add_kernel, dim3(sums), dim3(256), 0, st, part, sum, a.M * a.d);
+            CE_TRY(hipGetLastError());
+        }
+    }
+    if (a.dX) {
+        hipLaunchKernelGGL(ce_dx_kernel, dim3(sums), dim3(256), 0, st, sum, l.shares, a.M, a.d, a.dX, a.lddx);
+        CE_TRY(hipGetLastError());
     }
 #undef CE_TRY
     return hipSuccess;

@@ -3,6 +3,8 @@
 //     OUT = 1:  Y = X W^T (+ eps (X B) G^T) stored as bf16                     (a layer inside a model, Alg. 2)
 //     OUT = 2:  the same logits never stored: per token and 128-column chunk their maximum and the sum of exponentials
 //               around it, and the target's logit (token cross-entropy of a model's last layer; loss.hip combines them)
+//     OUT = 3:  Y (+)= X W^T in fp32, the sums over shares of d_in by themselves (products of the cross-entropy's gradient, ce_grad.hip)
+//     OUT = 4:  (exp(Y - lse) - onehot) f, f by token, stored as bf16 and once more transposed (that gradient with respect to the logits)
 // Same tile, tile layout in LDS and direct global -> LDS operand loads as gemm_bf16.hip (256 x 256 tile, four waves of
 // 128 x 128, 64-wide K slices), but a kernel of its own with one straight path and nothing else compiled in: M and N of
 // at least 256, d_in of at least 128, the rank-r extension as prepared operands.
@@ -118,6 +120,8 @@ struct AlignedItem {
     unsigned long long* clk;
     int ext_ld, tiles_m, tiles_n, group_m, vec_ok;
     int sub;                                       // partials are those of gemm_bf16_mid.hip: one per 128 x 128 outputs
+    // (OUT = 3: K is a share of d_in, there are ext_ld of them, and sub says whether sums are added to.  OUT = 4: ce_target, ce_tl and partials
+    // are ids, lse and f of the tokens, the latter as fp32; ce_ms is the transposed output, ldt its leading dimension, sub the first output's number)
 };
 
 // Tile lists over the tiles of several problems (one evaluation, squared error).  The tiles of a problem are dealt to the XCDs in runs
@@ -179,7 +183,14 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
     // moment share a few W tiles and a band of X tiles.
     // LISTS: the same over the runs of several problems; the lists are the launch's, which knows what a tile of each takes.
     int64_t tm = 0, tn = 0;
-    auto tile_of = [&](const AlignedItem& a, int lin, int64_t& tm_, int64_t& tn_) __attribute__((always_inline)) {
+    // (OUT = 3: share after share; the shares of the current and the next tile)
+    int share = 0, sharen = 0;
+    auto tile_of = [&](const AlignedItem& a, int lin, int64_t& tm_, int64_t& tn_, int* share_ = nullptr) __attribute__((always_inline)) {
+        if constexpr (OUT == 3) {
+            const int tiles = a.tiles_m * a.tiles_n, s = lin / tiles;
+            lin -= s * tiles;
+            *share_ = __builtin_amdgcn_readfirstlane(s);
+        }
         const int group = lin / (a.group_m * a.tiles_n);
         const int first_m = group * a.group_m;
         const int gsz = min(a.group_m, a.tiles_m - first_m);
@@ -190,15 +201,15 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
     // lists of one problem's tiles
     int G = 0;
     if constexpr (!LISTS) G = (int)tb.gx[CAP == 1 ? 0 : &only - tb.a];
-    const int nwg = LISTS ? 0 : item(cq).tiles_m * item(cq).tiles_n;
+    const int nwg = LISTS ? 0 : item(cq).tiles_m * item(cq).tiles_n * (OUT == 3 ? item(cq).ext_ld : 1);
     const bool by_xcd = (G % 8 == 0);
     const int S = by_xcd ? G / 8 : G;
     const int xcd = by_xcd ? (int)wgid % 8 : 0, slot = by_xcd ? (int)wgid / 8 : (int)wgid;
     const int per = by_xcd ? nwg / 8 : nwg;
     const int n_run = slot < per ? (per - slot + S - 1) / S : 0;
     const int n_tiles = __builtin_amdgcn_readfirstlane(n_run + ((by_xcd && slot == S - 1 && xcd < nwg - 8 * per) ? 1 : 0));
-    auto tile_at = [&](int i, int64_t& tm_, int64_t& tn_) __attribute__((always_inline)) {
-        tile_of(item(cq), (i < n_run) ? xcd * per + slot + i * S : 8 * per + xcd, tm_, tn_);
+    auto tile_at = [&](int i, int64_t& tm_, int64_t& tn_, int* share_) __attribute__((always_inline)) {
+        tile_of(item(cq), (i < n_run) ? xcd * per + slot + i * S : 8 * per + xcd, tm_, tn_, share_);
     };
     // lists over several problems: problem (l_rest: what is left of it) and round of this workgroup's next tile, the tiles of the run
     // taken in earlier rounds, and, lane by lane, how many tiles the slots of the XCD take of the problem
@@ -250,7 +261,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
         advance();
     } else {
         if (n_tiles == 0) return;
-        tile_at(0, tm, tn);
+        tile_at(0, tm, tn, &share);
     }
     // first row and column of a tile
     auto origin = [&](int64_t t, int64_t size) __attribute__((always_inline)) {
@@ -270,6 +281,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
         const bool has_ext = item(cq).Xext != nullptr;
         xb = item(cq).X + m0 * item(cq).ldx;
         wb_ = item(cq).W + n0 * item(cq).ldw;
+        if constexpr (OUT == 3) { xb += share * item(cq).K; wb_ += share * item(cq).K; }
         xb2 = has_ext ? item(cq).Xext + m0 * item(cq).ext_ld : xb;
         wb2 = has_ext ? item(cq).Wext + n0 * item(cq).ext_ld : wb_;
         wb3 = (has_ext && PHASES == 3) ? item(cq).Wext2 + n0 * item(cq).ext_ld : wb_;
@@ -281,10 +293,12 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
             if (!l_more) { nq = cq; tmn = tm; tnn = tn; }
         } else {
             nq = cq; tmn = tm; tnn = tn;
-            if (i < n_tiles) tile_at(i, tmn, tnn);
+            sharen = share;
+            if (i < n_tiles) tile_at(i, tmn, tnn, &sharen);
         }
         xbn = item(nq).X + origin(tmn, item(nq).M) * item(nq).ldx;
         wbn = item(nq).W + origin(tnn, item(nq).N) * item(nq).ldw;
+        if constexpr (OUT == 3) { xbn += sharen * item(nq).K; wbn += sharen * item(nq).K; }
         hmn = second_half(tmn, item(nq).M);
         hnn = second_half(tnn, item(nq).N);
         if (LISTS) { l_ldxn = (int)item(nq).ldx; l_ldwn = (int)item(nq).ldw; }
@@ -295,7 +309,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
             cq = nq; tm = tmn; tn = tnn;
             advance();
         } else {
-            tile_at(it + 1, tm, tn);
+            tile_at(it + 1, tm, tn, &share);
         }
         m0 = origin(tm, item(cq).M);   n0 = origin(tn, item(cq).N);
         hm = second_half(tm, item(cq).M);   hn = second_half(tn, item(cq).N);
@@ -748,6 +762,127 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
             }
             __syncthreads();                                 // the next W loads go into that stage
             if (!more) break;
+        } else if constexpr (OUT == 3) {
+            // As above with fp32 values: a token block of the wave, 16 tokens of 128 outputs, at a time, stored two whole rows to an instruction.
+            // What the tile before this one stores is left to it, for sums that are added to may be added to once
+            settle();
+            char* stg = smem + W_BASE + ((wst == 0) ? 2 : wst - 1) * TILE_BYTES + wave * 8192;
+            const int rs = RAGGED ? (int)(tm * BT - m0) - wb * 128 : 0, cs = RAGGED ? (int)(tn * BT - n0) - wa * 128 : 0;
+            const bool add = item(cq).sub != 0;
+            const int cc = lane & 31;
+            float* yw = reinterpret_cast<float*>(item(cq).Y) + ((int64_t)share * item(cq).M + m0 + wb * 128) * item(cq).ldy + n0 + wa * 128 + cc * 4;
+#pragma clang loop unroll(full)
+            for (int J = 0; J < 8; ++J) {
+                asm volatile("" ::: "memory");               // (or the compiler asks for more than a block's sums ahead and spills them)
+                float4 old[8];
+#pragma clang loop unroll(full)
+                for (int n = 0; n < 8; ++n) old[n] = add ? *reinterpret_cast<const float4*>(yw + (int64_t)(J * 16 + 2 * n + (lane >> 5)) * item(cq).ldy) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma clang loop unroll(full)
+                for (int i4 = 0; i4 < 2; ++i4)
+#pragma clang loop unroll(full)
+                    for (int t = 0; t < 4; ++t) {
+                        const floatx4 v = acc[i4 * 4 + t][J];
+                        const int c = i4 * 16 + lg * 4 + t;
+                        *reinterpret_cast<float4*>(stg + lc * 512 + ((c ^ lc) << 4)) = make_float4(from_acc(v[0]), from_acc(v[1]), from_acc(v[2]), from_acc(v[3]));
+                    }
+#pragma clang loop unroll(full)
+                for (int n = 0; n < 8; ++n) {
+                    const int t = 2 * n + (lane >> 5);
+                    float4 v = *reinterpret_cast<const float4*>(stg + t * 512 + ((cc ^ t) << 4));
+                    v.x += old[n].x; v.y += old[n].y; v.z += old[n].z; v.w += old[n].w;
+                    // (outputs are a multiple of 8, so four go together)
+                    if (!RAGGED || (J * 16 + t >= rs && cc * 4 >= cs)) *reinterpret_cast<float4*>(yw + (int64_t)(J * 16 + t) * item(cq).ldy) = v;
+                }
+            }
+            __syncthreads();                                 // the next W loads go into that stage
+            if (!more) break;
+        } else if constexpr (OUT == 4) {
+            // As OUT = 1; the block in LDS is read once more with transposition, eight tokens of an output to a lane
+            settle();
+            char* stg = smem + W_BASE + ((wst == 0) ? 2 : wst - 1) * TILE_BYTES + wave * 8192;
+            const uint32_t stg32 = (uint32_t)(uintptr_t)(lptr_t)stg;
+            constexpr float LOG2E = 1.44269504088896341f;
+            const float* lse = item(cq).ce_tl + m0 + wb * 128 + lc;
+            const float* rowf = reinterpret_cast<const float*>(item(cq).partials) + m0 + wb * 128 + lc;
+            const int32_t* ids = item(cq).ce_target + m0 + wb * 128 + lc;
+            float l2[8], f[8];
+            int at[8];                                       // the target's place among the lane's outputs, 16 and more: elsewhere
+#pragma clang loop unroll(full)
+            for (int J = 0; J < 8; ++J) {
+                l2[J] = lse[J * 16] * LOG2E;
+                f[J] = rowf[J * 16];
+                const int64_t rel = (int64_t)ids[J * 16] - item(cq).sub - (n0 + wa * 128);
+                at[J] = rel >= 0 && rel < 128 && (((int)rel >> 4) & 3) == lg ? ((int)rel >> 6) * 16 + ((int)rel & 15) : 64;
+            }
+#pragma clang loop unroll(full)
+            for (int r2 = 0; r2 < 4; ++r2) {
+#pragma clang loop unroll(full)
+                for (int jj = 0; jj < 2; ++jj) {
+                    const int J = 2 * r2 + jj, trow = jj * 16 + lc;
+                    float p[32];
+#pragma clang loop unroll(full)
+                    for (int I = 0; I < 8; ++I)
+#pragma clang loop unroll(full)
+                        for (int e = 0; e < 4; ++e) p[4 * I + e] = __builtin_amdgcn_exp2f(fmaf(from_acc(acc[I][J][e]), LOG2E, -l2[J]));
+                    // (as with the statistics: most waves have no target among their outputs)
+                    if (__builtin_amdgcn_ballot_w64(at[J] < 64) != 0) {
+#pragma clang loop unroll(full)
+                        for (int i = 0; i < 32; ++i) p[i] -= at[J] == i ? 1.f : 0.f;
+                    }
+#pragma clang loop unroll(full)
+                    for (int i4 = 0; i4 < 2; ++i4) {
+                        uint32_t w[8];
+#pragma clang loop unroll(full)
+                        for (int k = 0; k < 8; ++k) {
+                            const uint32_t two = pack_bf16x2(p[16 * i4 + 2 * k] * f[J], p[16 * i4 + 2 * k + 1] * f[J]);
+                            w[k] = f[J] == 0.f ? 0u : two;               // (a row that is not counted, whatever its logits are)
+                        }
+                        const int c0 = i4 * 8 + lg * 2;
+                        *reinterpret_cast<uint4*>(stg + trow * 256 + ((c0 ^ (trow & 15)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(stg + trow * 256 + (((c0 + 1) ^ (trow & 15)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
+                }
+                const int cc = lane & 15;
+#pragma clang loop unroll(full)
+                for (int n = 0; n < 8; ++n) {
+                    const int t = 4 * n + (lane >> 4);
+                    const uint4 v = *reinterpret_cast<const uint4*>(stg + t * 256 + ((cc ^ (t & 15)) << 4));
+                    bf16_t* dst = reinterpret_cast<bf16_t*>(item(cq).Y) + (m0 + wb * 128 + r2 * 32 + t) * item(cq).ldy + n0 + wa * 128 + cc * 8;
+                    if (RAGGED) store16_any(dst, v);
+                    else *reinterpret_cast<uint4*>(dst) = v;
+                }
+                // reads that transpose 4 tokens x 16 outputs in every 16 lanes: lane lc asks for 8 bytes of token lc / 4 and receives the four
+                // tokens' values of output lc
+                const int t0 = 8 * lg + (lc >> 2);
+                bf16_t* dt = reinterpret_cast<bf16_t*>(item(cq).ce_ms) + (n0 + wa * 128 + lc) * item(cq).ldt + m0 + wb * 128 + r2 * 32 + 8 * lg;
+#pragma clang loop unroll(full)
+                for (int half = 0; half < 2; ++half) {
+                    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                    u32x2 lo[4], hi[4];
+                    uint32_t a0[4], a1[4];
+#pragma clang loop unroll(full)
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = 2 * (4 * half + k) + ((lc & 3) >> 1), b = (lc & 1) * 8;
+                        a0[k] = stg32 + t0 * 256 + ((c ^ (t0 & 15)) << 4) + b;
+                        a1[k] = stg32 + (t0 + 4) * 256 + ((c ^ ((t0 + 4) & 15)) << 4) + b;
+                    }
+                    asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\t"
+                                 "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11\n\t"
+                                 "ds_read_b64_tr_b16 %4, %12\n\tds_read_b64_tr_b16 %5, %13\n\t"
+                                 "ds_read_b64_tr_b16 %6, %14\n\tds_read_b64_tr_b16 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+                                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3])
+                                 : "v"(a0[0]), "v"(a1[0]), "v"(a0[1]), "v"(a1[1]), "v"(a0[2]), "v"(a1[2]), "v"(a0[3]), "v"(a1[3]) : "memory");
+#pragma clang loop unroll(full)
+                    for (int k = 0; k < 4; ++k) {
+                        const uint4 v = make_uint4(lo[k][0], lo[k][1], hi[k][0], hi[k][1]);
+                        bf16_t* dst = dt + (int64_t)(4 * half + k) * 16 * item(cq).ldt;
+                        if (RAGGED) store16_any(dst, v);
+                        else *reinterpret_cast<uint4*>(dst) = v;
+                    }
+                }
+            }
+            __syncthreads();                                 // the next W loads go into that stage
+            if (!more) break;
         } else if constexpr (OUT == 2) {
             // a lane holds 32 of the 128 logits of the wave's columns for each of eight tokens; the lanes lane ^ 16, ^ 32, ^ 48
             // hold the others.  Online softmax over the wave's 128 columns, per token
@@ -1074,6 +1209,59 @@ hipError_t launch_gemm_bf16_aligned_lists(const GemmParams* const* a, const bool
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+// Lists of one problem's tiles for the two outputs of the cross-entropy's gradient
+template <int OUT>
+static hipError_t launch_grad(const AlignedItem& a, bool ragged, int64_t tiles, hipStream_t st) {
+    int slots = 0;
+    const hipError_t e = list_slots(&slots);
+    if (e != hipSuccess) return e;
+    if (slots < 1 || tiles > 0x7FFFFFFFLL / 8) return hipErrorInvalidValue;
+    const int64_t G = std::min<int64_t>((tiles + 7) / 8 * 8, 8 * slots);
+    const KBatch<AlignedItem, 1> tb{1, {0}, {(uint32_t)G}, {a}};
+    return ragged ? launch_aligned_grid<OUT, false, 1, true, 1>(tb, (unsigned)G, st) : launch_aligned_grid<OUT, false, 1, false, 1>(tb, (unsigned)G, st);
+}
+
+static AlignedItem grad_item(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K) {
+    AlignedItem a{};
+    a.X = X; a.ldx = ldx; a.W = W; a.ldw = ldw; a.M = M; a.N = N; a.K = K;
+    a.tiles_m = (int)((M + BT - 1) / BT); a.tiles_n = (int)((N + BT - 1) / BT);
+    a.group_m = K >= 8192 ? 4 : 8;
+    return a;
+}
+
+bool gemm_bf16_grad_fits(int64_t M, int64_t N, int64_t K) { return M >= BT && N >= BT && K >= 2 * BK; }
+
+// Shares of `slices` 64-wide slices that leave the fewest slices to the workgroup that has most, a tile's change counted as six of them; a share has eight at
+// least, and its sums are 4 bytes an output more to write and read
+int gemm_bf16_sum_shares(int64_t M, int64_t N, int64_t slices) {
+    int slots = 0;
+    if (list_slots(&slots) != hipSuccess || slots < 1) return 1;
+    const int64_t tiles = ((M + BT - 1) / BT) * ((N + BT - 1) / BT);
+    int best = 1;
+    double best_cost = -1.0;
+    for (int s = 1; s <= 16 && slices / s >= 8; ++s) {
+        const double cost = (double)((tiles * s + 8 * slots - 1) / (8 * slots)) * ((double)((slices + s - 1) / s) + 6.0) + (double)s * M * N * 2e-6;
+        if (best_cost < 0.0 || cost < 0.97 * best_cost) { best = s; best_cost = cost; }
+    }
+    return best;
+}
+
+hipError_t launch_gemm_bf16_sum(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int shares, float* Y, bool add, hipStream_t st) {
+    if (!gemm_bf16_grad_fits(M, N, K) || shares < 1 || K % BK || N % 8) return hipErrorInvalidValue;
+    AlignedItem a = grad_item(X, ldx, W, ldw, M, N, K);
+    a.Y = Y; a.ldy = N; a.ext_ld = shares; a.sub = add ? 1 : 0;
+    return launch_grad<3>(a, M % BT || N % BT, (int64_t)a.tiles_m * a.tiles_n * shares, st);
+}
+
+hipError_t launch_gemm_bf16_softmax_grad(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int64_t first, const int32_t* ids,
+                                         const float* lse, const float* rowf, bf16_t* D, int64_t ldd, bf16_t* Dt, int64_t ldt, hipStream_t st) {
+    if (!gemm_bf16_grad_fits(M, N, K) || ldd % 8 || ldt % 8) return hipErrorInvalidValue;
+    AlignedItem a = grad_item(X, ldx, W, ldw, M, N, K);
+    a.Y = D; a.ldy = ldd; a.ce_ms = reinterpret_cast<float2*>(Dt); a.ldt = ldt; a.ce_target = ids; a.ce_tl = const_cast<float*>(lse);
+    a.partials = reinterpret_cast<double*>(const_cast<float*>(rowf)); a.sub = (int)first;
+    return launch_grad<4>(a, M % BT || N % BT || K % BK, (int64_t)a.tiles_m * a.tiles_n, st);
 }
 
 template <bool RAGGED>

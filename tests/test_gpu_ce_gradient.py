@@ -54,7 +54,7 @@ def check(got, want):
 
 @pytest.mark.parametrize("n,d,v,pad", [
     (1, 8, 1, 0), (1, 64, 2, 0), (3, 40, 7, 8), (7, 2048, 999, 0), (63, 72, 64, 0), (64, 64, 65, 16), (65, 136, 257, 0), (200, 256, 1000, 0),
-    (256, 128, 256, 0), (257, 264, 4097, 8), (300, 512, 12345, 0), (1000, 1024, 5000, 0), (5, 16, 140000, 0), (70, 8, 300001, 0),
+    (256, 128, 256, 0), (257, 264, 4097, 8), (256, 256, 512, 0), (512, 128, 768, 0), (300, 512, 12345, 0), (1000, 1024, 5000, 0), (5, 16, 140000, 0), (70, 8, 300001, 0),
     # several pieces of the outputs
     (2049, 64, 70001, 0), (40, 8192, 33000, 0)])
 def test_loss_and_gradients(n, d, v, pad):
