@@ -164,40 +164,57 @@ __device__ __forceinline__ void pk_store(const pk_floatx16 (&acc)[HD / 32], floa
         }
 }
 
+// x / d for 0 <= x < 2^31, 1 <= d: the quotient by a multiplication is at most one short.  (A division is some 30 instructions, of 64 bits 100: three of them
+// and the scan below were half of what a workgroup did before its first load)
+struct PkDiv {
+    uint32_t d, m;
+    __device__ __forceinline__ explicit PkDiv(int by) : d((uint32_t)by), m((uint32_t)(0x100000000ull / (uint32_t)by - (by == 1))) {}
+    __device__ __forceinline__ int operator()(int x) const {
+        uint32_t q = __umulhi((uint32_t)x, m);
+        q += (uint32_t)x - q * d >= d;
+        return (int)q;
+    }
+};
+
+// sums over the lanes up to each, and the sum of all
+__device__ __forceinline__ int pk_scan(int x) {
+#pragma unroll
+    for (int shift = 1; shift < 16; shift <<= 1) {
+        // row_shr: within 16 lanes
+        const int o = shift == 1 ? __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true) : shift == 2 ? __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true)
+                    : shift == 4 ? __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true) : __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+        x += o;
+    }
+    const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31), c = b + __builtin_amdgcn_readlane(x, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return x + (row == 0 ? 0 : row == 1 ? a : row == 2 ? b : c);
+}
+
 // One sequence's places in the packed tensors, and a tile of it
-struct PkTile { int tile; int64_t q0, k0; int nq, nk; };
+struct PkTile { int tile, q0, k0, nq, nk; };
 
 // Tile number t of all sequences' tiles, UNIT rows (BY_KEYS: keys) each.  Offsets are taken as far as they lie inside the tensors and grow
 template <int UNIT, bool BY_KEYS>
-__device__ __forceinline__ bool pk_find(const PackedArgs& a, int64_t t, PkTile& out) {
-    const int lane = threadIdx.x & 63, G = a.n_heads / a.n_kv;
-    int64_t before = 0;
+__device__ __forceinline__ bool pk_find(const PackedArgs& a, int t, int G, PkTile& out) {
+    const int lane = threadIdx.x & 63, total_q = (int)a.total_q, total_k = (int)a.total_k;
     for (int b = 0; b < a.n_seq; b += 64) {
-        const int s = b + lane;
-        int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
-        if (s < a.n_seq) {
-            q0 = min(max(a.cu_q[s], 0), (int)a.total_q);   q1 = min(max(a.cu_q[s + 1], q0), (int)a.total_q);
-            k0 = min(max(a.cu_k[s], 0), (int)a.total_k);   k1 = min(max(a.cu_k[s + 1], k0), (int)a.total_k);
-        }
-        const int count = BY_KEYS ? (k1 - k0 + UNIT - 1) / UNIT : (int)(((int64_t)(q1 - q0) * G + UNIT - 1) / UNIT);
-        int sum = count;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int o = __shfl_up(sum, off);
-            sum += lane >= off ? o : 0;
-        }
+        const int s = min(b + lane, a.n_seq - 1);
+        int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
+        q0 = min(max(q0, 0), total_q);   q1 = min(max(q1, q0), total_q);
+        k0 = min(max(k0, 0), total_k);   k1 = min(max(k1, k0), total_k);
+        const int count = b + lane >= a.n_seq ? 0 : (int)(((BY_KEYS ? (uint32_t)(k1 - k0) : (uint32_t)(q1 - q0) * (uint32_t)G) + (UNIT - 1)) / UNIT);
+        const int sum = pk_scan(count);
         const int total = __builtin_amdgcn_readlane(sum, 63);
-        if (t < before + total) {
-            const uint64_t m = __builtin_amdgcn_ballot_w64(before + sum > t);
-            const int src = __builtin_ctzll(m);
-            out.tile = (int)(t - before) - __builtin_amdgcn_readlane(sum - count, src);
+        if (t < total) {
+            const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > t));
+            out.tile = t - __builtin_amdgcn_readlane(sum - count, src);
             out.q0 = __builtin_amdgcn_readlane(q0, src);
             out.k0 = __builtin_amdgcn_readlane(k0, src);
-            out.nq = __builtin_amdgcn_readlane(q1, src) - (int)out.q0;
-            out.nk = __builtin_amdgcn_readlane(k1, src) - (int)out.k0;
+            out.nq = __builtin_amdgcn_readlane(q1, src) - out.q0;
+            out.nk = __builtin_amdgcn_readlane(k1, src) - out.k0;
             return true;
         }
-        before += total;
+        t -= total;
     }
     return false;
 }
@@ -270,25 +287,23 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
     // the last tiles first, for they have most keys; the key heads side by side: an XCD (workgroup number mod 8) then has few of them
-    const int64_t unit = (int64_t)gridDim.x - 1 - blockIdx.x;
-    const int kvh = (int)(unit % a.n_kv), G = a.n_heads / a.n_kv;
+    const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)(gridDim.x - 1 - blockIdx.x), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, unit / a.n_kv, t)) return;
-    const int64_t R = (int64_t)t.nq * G;
-    const int64_t row0 = (int64_t)t.tile * PK_ROWS + wave * 32;
-    const int shift = t.nk - t.nq;
-    const int64_t row = min(row0 + (lane & 31), R - 1);
+    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return;
+    const PkDiv by_group(G);
+    const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
+    const int row = min(row0 + (lane & 31), R - 1);
     const bool mine = row0 + (lane & 31) < R;
-    const int tq = (int)(row / G), head = kvh * G + (int)(row - (int64_t)tq * G);
+    const int tq = by_group(row), head = kvh * G + row - tq * G;
     const int limit = a.causal ? tq + shift : t.nk - 1;                       // the last key that the lane's row sees
     // the first and last of the wave's rows, and the last of the workgroup's
-    const int wfirst = a.causal ? (int)(min(row0, R - 1) / G) + shift : t.nk - 1;
-    const int wlast = row0 >= R ? -1 : a.causal ? (int)(min(row0 + 31, R - 1) / G) + shift : t.nk - 1;
-    const int last = a.causal ? (int)(min((int64_t)(t.tile + 1) * PK_ROWS - 1, R - 1) / G) + shift : t.nk - 1;
+    const int wfirst = a.causal ? by_group(min(row0, R - 1)) + shift : t.nk - 1;
+    const int wlast = row0 >= R ? -1 : a.causal ? by_group(min(row0 + 31, R - 1)) + shift : t.nk - 1;
+    const int last = a.causal ? by_group(min((t.tile + 1) * PK_ROWS - 1, R - 1)) + shift : t.nk - 1;
     const int tiles = last < 0 ? 0 : last / PK_T + 1;
     const int j0 = (int)((int64_t)tiles * blockIdx.y / gridDim.y), j1 = (int)((int64_t)tiles * (blockIdx.y + 1) / gridDim.y);
-    const bf16_t* Kh = a.k + t.k0 * a.ldk + kvh * HD;
-    const bf16_t* Vh = a.v + t.k0 * a.ldv + kvh * HD;
+    const bf16_t* Kh = a.k + (int64_t)t.k0 * a.ldk + kvh * HD;
+    const bf16_t* Vh = a.v + (int64_t)t.k0 * a.ldv + kvh * HD;
     PkLoader<HD> lk(a.ldk), lv(a.ldv);
     auto request = [&](int j) __attribute__((always_inline)) {
         lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T);
@@ -302,7 +317,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     PkFrag qf[KS];
     if (j0 < j1) {
         request(j0);
-        const bf16_t* src = a.q + (t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
+        const bf16_t* src = a.q + (int64_t)(t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(src + 16 * ks);
     }
@@ -392,7 +407,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     l = pk_sum_halves(l);
     if (part) {
         if (!mine) return;
-        const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + (t.q0 + tq) * a.n_heads + head;
+        const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + (int64_t)(t.q0 + tq) * a.n_heads + head;
         float* to = part + at * HD + 4 * hi;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -403,8 +418,8 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         return;
     }
     const bool empty = limit < 0;
-    pk_store<HD>(acc, empty ? 0.f : 1.f / l, out + (t.q0 + tq) * ldo + (int64_t)head * HD, mine);
-    if (lse && mine && hi == 0) lse[(t.q0 + tq) * a.n_heads + head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
+    pk_store<HD>(acc, empty ? 0.f : 1.f / l, out + (int64_t)(t.q0 + tq) * ldo + (int64_t)head * HD, mine);
+    if (lse && mine && hi == 0) lse[(int64_t)(t.q0 + tq) * a.n_heads + head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
 }
 
 // Shares of the keys joined: HD / 4 lanes a row.  Rows of no sequence are left alone: their partial sums are what the workspace held
@@ -488,23 +503,22 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
-    const int64_t unit = (int64_t)gridDim.x - 1 - blockIdx.x;
-    const int kvh = (int)(unit % a.n_kv), G = a.n_heads / a.n_kv;
+    const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)(gridDim.x - 1 - blockIdx.x), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, unit / a.n_kv, t)) return;
-    const int64_t R = (int64_t)t.nq * G;
-    const int64_t row0 = (int64_t)t.tile * PK_ROWS + wave * 32;
-    const int shift = t.nk - t.nq;
-    const int64_t row = min(row0 + (lane & 31), R - 1);
+    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return;
+    const PkDiv by_group(G);
+    const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
+    const int row = min(row0 + (lane & 31), R - 1);
     const bool mine = row0 + (lane & 31) < R;
-    const int tq = (int)(row / G), head = kvh * G + (int)(row - (int64_t)tq * G);
-    const int limit = a.causal ? tq + shift : t.nk - 1;
-    const int wfirst = a.causal ? (int)(min(row0, R - 1) / G) + shift : t.nk - 1;
-    const int wlast = row0 >= R ? -1 : a.causal ? (int)(min(row0 + 31, R - 1) / G) + shift : t.nk - 1;
-    const int last = a.causal ? (int)(min((int64_t)(t.tile + 1) * PK_ROWS - 1, R - 1) / G) + shift : t.nk - 1;
+    const int tq = by_group(row), head = kvh * G + row - tq * G;
+    const int limit = a.causal ? tq + shift : t.nk - 1;                       // the last key that the lane's row sees
+    // the first and last of the wave's rows, and the last of the workgroup's
+    const int wfirst = a.causal ? by_group(min(row0, R - 1)) + shift : t.nk - 1;
+    const int wlast = row0 >= R ? -1 : a.causal ? by_group(min(row0 + 31, R - 1)) + shift : t.nk - 1;
+    const int last = a.causal ? by_group(min((t.tile + 1) * PK_ROWS - 1, R - 1)) + shift : t.nk - 1;
     const int tiles = last < 0 ? 0 : last / PK_T + 1;
-    const bf16_t* Kh = a.k + t.k0 * a.ldk + kvh * HD;
-    const bf16_t* Vh = a.v + t.k0 * a.ldv + kvh * HD;
+    const bf16_t* Kh = a.k + (int64_t)t.k0 * a.ldk + kvh * HD;
+    const bf16_t* Vh = a.v + (int64_t)t.k0 * a.ldv + kvh * HD;
     PkLoader<HD> lk(a.ldk), lv(a.ldv);
     auto request = [&](int j) __attribute__((always_inline)) {
         lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T);
@@ -517,14 +531,14 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const PkOffsets<HD> off;
     PkFrag qf[KS], df[KS];
     if (tiles > 0) request(0);
-    const bf16_t* qsrc = a.q + (t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
-    const bf16_t* dsrc = dout + (t.q0 + tq) * lddo + (int64_t)head * HD + 8 * hi;
+    const bf16_t* qsrc = a.q + (int64_t)(t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
+    const bf16_t* dsrc = dout + (int64_t)(t.q0 + tq) * lddo + (int64_t)head * HD + 8 * hi;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
         df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
     }
-    const uint4 parts = rowinfo[(t.q0 + tq) * a.n_heads + head];
+    const uint4 parts = rowinfo[(int64_t)(t.q0 + tq) * a.n_heads + head];
     const float sc = a.scale * PK_LOG2E;
     const float2 info = make_float2(-sc * pk_join3(parts.x, parts.y), -pk_join3(parts.z, parts.w));      // lse log2 e, delta
     pk_floatx16 acc[DB];
@@ -582,7 +596,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         if (tiles > 0) request(0);
         all_tiles(std::true_type());
     }
-    pk_store<HD>(acc, a.scale, dq + (t.q0 + tq) * lddq + (int64_t)head * HD, mine);
+    pk_store<HD>(acc, a.scale, dq + (int64_t)(t.q0 + tq) * lddq + (int64_t)head * HD, mine);
 }
 
 // dk, dv: four waves of 32 keys, K and V in registers, against tiles of 64 rows of q and do that they share.  Sums, operands and scores are some 300
@@ -598,25 +612,20 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     int* limits = reinterpret_cast<int*>(infos + 2 * PK_T);                   // ... and the last key that they see
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
-    const int kvh = (int)(blockIdx.x % a.n_kv), G = a.n_heads / a.n_kv;
+    const int G = PkDiv(a.n_kv)(a.n_heads), at = PkDiv(a.n_kv)((int)blockIdx.x), kvh = (int)blockIdx.x - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, true>(a, blockIdx.x / a.n_kv, t)) return;
+    if (!pk_find<PK_ROWS, true>(a, at, G, t)) return;
     const int R = t.nq * G, shift = t.nk - t.nq;
     const int key0 = t.tile * PK_ROWS, wkey = key0 + wave * 32;
     const int key = min(wkey + (lane & 31), t.nk - 1);
     const bool mine = wkey + (lane & 31) < t.nk;
     const int row0 = a.causal ? max(key0 - shift, 0) * G : 0;                  // (below R: key0 < nk)
     const int tiles = (R - row0 + PK_T - 1) / PK_T;
-    const uint32_t magic = (uint32_t)(0x100000000ull / (uint32_t)G - (G == 1));
-    auto query_of = [&](int row) __attribute__((always_inline)) {             // row / G
-        int q = (int)__umulhi((uint32_t)row, magic);
-        q += row - q * G >= G;
-        return q;
-    };
+    const PkDiv query_of(G);
     // a tile's rows on their way; rows past the end repeat the last one
     constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);
-    const bf16_t* Qh = a.q + t.q0 * a.ldq + (int64_t)kvh * G * HD;
-    const bf16_t* Dh = dout + t.q0 * lddo + (int64_t)kvh * G * HD;
+    const bf16_t* Qh = a.q + (int64_t)t.q0 * a.ldq + (int64_t)kvh * G * HD;
+    const bf16_t* Dh = dout + (int64_t)t.q0 * lddo + (int64_t)kvh * G * HD;
     uint4 qd[N], dd[N], next = make_uint4(0, 0, 0, 0);
     int next_limit = -1;
     auto request = [&](int j) __attribute__((always_inline)) {
@@ -632,7 +641,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
         }
         if (wave == 0) {
             const int r = min(base + lane, R - 1), q = query_of(r);
-            next = rowinfo[(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
+            next = rowinfo[(int64_t)(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
             next_limit = base + lane >= R ? -1 : a.causal ? q + shift : t.nk - 1;
         }
     };
@@ -652,8 +661,8 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     PkFrag kf[KS], vf[KS], ones;
     if (tiles > 0) {
         request(0);
-        const bf16_t* ksrc = a.k + (t.k0 + key) * a.ldk + kvh * HD + 8 * hi;
-        const bf16_t* vsrc = a.v + (t.k0 + key) * a.ldv + kvh * HD + 8 * hi;
+        const bf16_t* ksrc = a.k + (int64_t)(t.k0 + key) * a.ldk + kvh * HD + 8 * hi;
+        const bf16_t* vsrc = a.v + (int64_t)(t.k0 + key) * a.ldv + kvh * HD + 8 * hi;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             kf[ks].u = *reinterpret_cast<const uint4*>(ksrc + 16 * ks);
@@ -745,8 +754,8 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
         if (tiles > 0) request(0);
         all_tiles(std::true_type());
     }
-    pk_store<HD>(av, 1.f, dv + (t.k0 + key) * lddv + (int64_t)kvh * HD, mine);
-    pk_store<HD>(ak, a.scale, dk + (t.k0 + key) * lddk + (int64_t)kvh * HD, mine);
+    pk_store<HD>(av, 1.f, dv + (int64_t)(t.k0 + key) * lddv + (int64_t)kvh * HD, mine);
+    pk_store<HD>(ak, a.scale, dk + (int64_t)(t.k0 + key) * lddk + (int64_t)kvh * HD, mine);
 }
 
 // an upper bound of the row (key) tiles of all sequences, whatever their lengths
