@@ -47,8 +47,8 @@ __device__ __forceinline__ float pk_sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ uint4 pk_load16(__amdgpu_buffer_rsrc_t rsrc, int off) {
-    const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
+__device__ __forceinline__ uint4 pk_load16(__amdgpu_buffer_rsrc_t rsrc, int off, int uniform) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, uniform, 0);
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
@@ -72,28 +72,37 @@ struct PkOffsets {
             trans[s] = tr * (HD * 2) + (((2 * dg + ((n16 & 3) >> 1)) ^ pk_swz<HD>(tr)) << 4) + (n16 & 1) * 8;
         }
     }
+    // of a tile that starts `at` bytes into LDS, a multiple of 256.  (Values that the compiler does not know: it would work out every read's address ahead of
+    // the loop over tiles and spill them, and a wait for a reload is one for the next tile's loads too)
+    __device__ __forceinline__ PkOffsets(const PkOffsets& of, int at) : rows(of.rows + at), trans{of.trans[0] + at, of.trans[1] + at} {
+        asm volatile("" : "+v"(rows), "+v"(trans[0]), "+v"(trans[1]));
+    }
+    // chunk 2 ks + lane / 32 of row 32 h + lane % 32
+    __device__ __forceinline__ pk_bf16x8 row(const char* lds, int h, int ks, int more = 0) const {
+        return *reinterpret_cast<const pk_bf16x8*>(lds + ((rows ^ (ks << 5)) + h * 32 * HD * 2 + more));
+    }
 };
 
 // a fragment with transposition: 16 positions (from place `at` of a tile on) x 32 dims
 typedef __bf16 pk_bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pk_bf16x4* pk_trptr;
 template <int HD>
-__device__ __forceinline__ void pk_read_trans(const char* at, const PkOffsets<HD>& o, int db, PkFrag& f) {
+__device__ __forceinline__ void pk_read_trans(const char* lds, const PkOffsets<HD>& o, int at, int db, PkFrag& f) {
     union { pk_bf16x4 v; uint2 u; } lo, hi;
-    lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(at + (o.trans[0] ^ (db << 6))));
-    hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(at + (o.trans[1] ^ (db << 6))));
+    lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(lds + ((o.trans[0] ^ (db << 6)) + at)));
+    hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(lds + ((o.trans[1] ^ (db << 6)) + at)));
     f.u = make_uint4(lo.u.x, lo.u.y, hi.u.x, hi.u.y);
 }
 
 // acc[db] += (positions x dims of a tile)^T times fragments FROM .. TO of 16 positions each
 template <int HD, int FROM, int TO>
-__device__ __forceinline__ void pk_second(const char* tile, const PkOffsets<HD>& o, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
+__device__ __forceinline__ void pk_second(const char* lds, const PkOffsets<HD>& o, int at, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
 #pragma unroll
     for (int s = FROM; s < TO; ++s)
 #pragma unroll
         for (int db = 0; db < HD / 32; ++db) {
             PkFrag f;
-            pk_read_trans<HD>(tile + s * 16 * HD * 2, o, db, f);
+            pk_read_trans<HD>(lds, o, at + s * 16 * HD * 2, db, f);
             acc[db] = pk_mfma(f, p[s], acc[db]);
         }
 }
@@ -221,29 +230,27 @@ __device__ __forceinline__ bool pk_find(const PackedArgs& a, int t, int G, PkTil
 
 // 64 rows on their way to a tile in LDS, by the four waves of a workgroup: the rows from `base` on, `ld` values apart; rows past `left` repeat the
 // last one.  (Through registers: behind direct loads to LDS the compiler lets every read with transposition wait for all that are in flight)
+// (A wave's loads are 1024 bytes each, whose rows differ in the low bits of r / 4 alone, and with them the places of chunks)
 template <int HD>
 struct PkLoader {
     static constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);      // loads of a wave, rows of a load
-    int voff[N];
+    static_assert(ROWS * N == 16 && (HD == 128 || HD == 64), "swz() of the rows of load i");
+    int row, chunk;      // of the first load: byte offset of the lane's row, place of its chunk
     uint4 data[N];
-    __device__ __forceinline__ PkLoader(int64_t ld) {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = ROWS * (N * wave + i) + lane / (HD / 8);
-            voff[i] = (int)(r * ld * 2) + (((lane % (HD / 8)) ^ pk_swz<HD>(r)) << 4);
-        }
+    __device__ __forceinline__ explicit PkLoader(int64_t ld) {
+        const int lane = threadIdx.x & 63, r = 16 * (int)(threadIdx.x >> 6) + lane / (HD / 8);
+        row = r * (int)(ld * 2);
+        chunk = (lane % (HD / 8)) ^ pk_swz<HD>(r);
     }
     __device__ __forceinline__ void load(const bf16_t* base, int64_t ld, int left) {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, (int)0xFFFFFFFFu, 0x00020000);
         if (left >= PK_T) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) data[i] = pk_load16(rsrc, voff[i]);
+            for (int i = 0; i < N; ++i) data[i] = pk_load16(rsrc, row + ((chunk ^ pk_swz<HD>(ROWS * i)) << 4), ROWS * i * (int)(ld * 2));
         } else {
+            const int r = 16 * (int)(threadIdx.x >> 6) + (int)(threadIdx.x & 63) / (HD / 8);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                data[i] = pk_load16(rsrc, voff[i] - max(ROWS * (N * wave + i) + lane / (HD / 8) - (left - 1), 0) * (int)(ld * 2));
+            for (int i = 0; i < N; ++i) data[i] = pk_load16(rsrc, min(r + ROWS * i, left - 1) * (int)(ld * 2) + ((chunk ^ pk_swz<HD>(ROWS * i)) << 4), 0);
         }
     }
     __device__ __forceinline__ void store(char* tile) const {
@@ -292,10 +299,16 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     if (!pk_find<PK_ROWS, false>(a, at, G, t)) return;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
-    const int row = min(row0 + (lane & 31), R - 1);
-    const bool mine = row0 + (lane & 31) < R;
-    const int tq = by_group(row), head = kvh * G + row - tq * G;
-    const int limit = a.causal ? tq + shift : t.nk - 1;                       // the last key that the lane's row sees
+    // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
+    // again: kept through the loop they are spilled, and a wait for a reload is one for the next tile's loads too)
+    struct Row { int64_t tok; int head, limit; bool mine; };
+    auto row_of_lane = [&]() __attribute__((always_inline)) {
+        int lane_ = (int)threadIdx.x & 31;
+        asm volatile("" : "+v"(lane_));
+        const int row = min(row0 + lane_, R - 1), q = by_group(row);
+        return Row{t.q0 + q, kvh * G + row - q * G, a.causal ? q + shift : t.nk - 1, row0 + lane_ < R};
+    };
+    auto limit_of = [&]() __attribute__((always_inline)) { return row_of_lane().limit; };
     // the first and last of the wave's rows, and the last of the workgroup's
     const int wfirst = a.causal ? by_group(min(row0, R - 1)) + shift : t.nk - 1;
     const int wlast = row0 >= R ? -1 : a.causal ? by_group(min(row0 + 31, R - 1)) + shift : t.nk - 1;
@@ -315,12 +328,17 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     };
     const PkOffsets<HD> off;
     PkFrag qf[KS];
-    if (j0 < j1) {
+    // the first tile and the queries (once more for a pass with care: kept for it they would be spilled, and a wait for a reload in the loop is one for the next
+    // tile's loads too).  Waited for here: what is left to the loop to wait for, it waits for in every round, and with it for the next tile's loads
+    auto begin = [&]() __attribute__((always_inline)) {
+        if (j0 >= j1) return;
         request(j0);
-        const bf16_t* src = a.q + (int64_t)(t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
+        const Row r = row_of_lane();
+        const bf16_t* qsrc = a.q + r.tok * a.ldq + (int64_t)r.head * HD + 8 * hi;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(src + 16 * ks);
-    }
+        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+    };
     const float sc = a.scale * PK_LOG2E;
     // sums are rescaled when a maximum has grown by more than 2^8 times: what they and the probabilities are relative to need not be the maximum itself
     const float slack = 8.f / sc;
@@ -331,20 +349,27 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
             const int kb = j * PK_T;
             if (kb > wlast) return;                                          // (wave-uniform)
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
+            // (operands are read four instructions ahead, the exponentials of 16 keys run beside the second product of the 16 before them: left to
+            // itself the compiler reads right before each instruction)
+            const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+            PkFrag f[4];
+            auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = o.row(pk_smem, i & 1, i >> 1); };
+            auto read_v = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(pk_smem, o, TILE + (i / DB) * 16 * HD * 2, i % DB, f[i & 3]); };
+            const pk_floatx16 zero = {};
             pk_floatx16 s[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                pk_zero(s[h]);
+            for (int i = 0; i < 4; ++i) read_k(i);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    PkFrag kf;
-                    kf.v = *reinterpret_cast<const pk_bf16x8*>(kt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
-                    s[h] = pk_mfma(kf, qf[ks], s[h]);
-                }
+            for (int i = 0; i < 2 * KS; ++i) {
+                s[i & 1] = pk_mfma(f[i & 3], qf[i >> 1], i < 2 ? zero : s[i & 1]);
+                if (i + 4 < 2 * KS) read_k(i + 4);
+                else read_v(i + 4 - 2 * KS);
+                __builtin_amdgcn_sched_barrier(0);
             }
             const bool mask = kb + PK_T - 1 > wfirst;                        // (wave-uniform)
             if (mask) {
-                const int rel = limit - kb - 4 * hi;
+                const int rel = limit_of() - kb - 4 * hi;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -368,29 +393,39 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
                 topsc = to;
             }
             PkFrag pf[4];
-            float sum[2] = {0.f, 0.f};
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][e], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[h][e + 1], sc, -topsc));
-                    sum[h] += p0 + p1;
-                    // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that)
-                    pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
-                }
-            l += sum[0] + sum[1];
+            // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that)
+            auto two = [&](int e) __attribute__((always_inline)) {              // probabilities e and e + 1 of the lane's 32
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][(e & 15) + 1], sc, -topsc));
+                l += p0 + p1;
+                pf[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
+            };
             if (careful && mask) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) two(e);
                 PkFrag seen[4];
-                pk_seen(kb, limit, seen);
+                pk_seen(kb, limit_of(), seen);
                 pk_second_careful<HD, true>(kt + TILE, pf, seen, acc);
                 return;
             }
-            pk_second<HD, 0, 4>(kt + TILE, off, pf, acc);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) two(e);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4 * DB; ++i) {
+                acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
+                if (i + 4 < 4 * DB) read_v(i + 4);
+                if (i < 3 * DB) {
+#pragma unroll
+                    for (int e = 0; e < 8 / DB; e += 2) two(8 + i * (8 / DB) + e);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
     };
     auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
         top = -INFINITY; topsc = 0.f; l = 0.f;
+        begin();
         if (j0 < j1) arrive(j0);
         for (int j = j0; j < j1; ++j) {
             __syncthreads();
@@ -400,14 +435,12 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         }
     };
     all_tiles(std::false_type());
-    if (__syncthreads_or(mine && pk_not_finite(acc))) {
-        if (j0 < j1) request(j0);
-        all_tiles(std::true_type());
-    }
+    if (__syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) all_tiles(std::true_type());
     l = pk_sum_halves(l);
+    const Row r = row_of_lane();
     if (part) {
-        if (!mine) return;
-        const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + (int64_t)(t.q0 + tq) * a.n_heads + head;
+        if (!r.mine) return;
+        const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + r.tok * a.n_heads + r.head;
         float* to = part + at * HD + 4 * hi;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -417,9 +450,9 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         if (hi == 0) part_ml[at] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
         return;
     }
-    const bool empty = limit < 0;
-    pk_store<HD>(acc, empty ? 0.f : 1.f / l, out + (int64_t)(t.q0 + tq) * ldo + (int64_t)head * HD, mine);
-    if (lse && mine && hi == 0) lse[(int64_t)(t.q0 + tq) * a.n_heads + head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
+    const bool empty = r.limit < 0;
+    pk_store<HD>(acc, empty ? 0.f : 1.f / l, out + r.tok * ldo + (int64_t)r.head * HD, r.mine);
+    if (lse && r.mine && hi == 0) lse[r.tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
 }
 
 // Shares of the keys joined: HD / 4 lanes a row.  Rows of no sequence are left alone: their partial sums are what the workspace held
@@ -508,10 +541,16 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     if (!pk_find<PK_ROWS, false>(a, at, G, t)) return;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
-    const int row = min(row0 + (lane & 31), R - 1);
-    const bool mine = row0 + (lane & 31) < R;
-    const int tq = by_group(row), head = kvh * G + row - tq * G;
-    const int limit = a.causal ? tq + shift : t.nk - 1;                       // the last key that the lane's row sees
+    // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
+    // again: kept through the loop they are spilled, and a wait for a reload is one for the next tile's loads too)
+    struct Row { int64_t tok; int head, limit; bool mine; };
+    auto row_of_lane = [&]() __attribute__((always_inline)) {
+        int lane_ = (int)threadIdx.x & 31;
+        asm volatile("" : "+v"(lane_));
+        const int row = min(row0 + lane_, R - 1), q = by_group(row);
+        return Row{t.q0 + q, kvh * G + row - q * G, a.causal ? q + shift : t.nk - 1, row0 + lane_ < R};
+    };
+    auto limit_of = [&]() __attribute__((always_inline)) { return row_of_lane().limit; };
     // the first and last of the wave's rows, and the last of the workgroup's
     const int wfirst = a.causal ? by_group(min(row0, R - 1)) + shift : t.nk - 1;
     const int wlast = row0 >= R ? -1 : a.causal ? by_group(min(row0 + 31, R - 1)) + shift : t.nk - 1;
@@ -530,17 +569,22 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     };
     const PkOffsets<HD> off;
     PkFrag qf[KS], df[KS];
-    if (tiles > 0) request(0);
-    const bf16_t* qsrc = a.q + (int64_t)(t.q0 + tq) * a.ldq + (int64_t)head * HD + 8 * hi;
-    const bf16_t* dsrc = dout + (int64_t)(t.q0 + tq) * lddo + (int64_t)head * HD + 8 * hi;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-        qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
-        df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
-    }
-    const uint4 parts = rowinfo[(int64_t)(t.q0 + tq) * a.n_heads + head];
     const float sc = a.scale * PK_LOG2E;
-    const float2 info = make_float2(-sc * pk_join3(parts.x, parts.y), -pk_join3(parts.z, parts.w));      // lse log2 e, delta
+    float2 info;                                                              // lse log2 e, delta
+    auto begin = [&]() __attribute__((always_inline)) {                       // (as in the forward)
+        if (tiles > 0) request(0);
+        const Row r = row_of_lane();
+        const bf16_t* qsrc = a.q + r.tok * a.ldq + (int64_t)r.head * HD + 8 * hi;
+        const bf16_t* dsrc = dout + r.tok * lddo + (int64_t)r.head * HD + 8 * hi;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
+            df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
+        }
+        const uint4 parts = rowinfo[r.tok * a.n_heads + r.head];
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        info = make_float2(-sc * pk_join3(parts.x, parts.y), -pk_join3(parts.z, parts.w));
+    };
     pk_floatx16 acc[DB];
     auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
             constexpr bool careful = decltype(CAREFUL)::value;
@@ -548,41 +592,71 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
             if (kb > wlast) return;
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
             const bool mask = kb + PK_T - 1 > wfirst;
-            PkFrag pf[4];
+            // (operands two pairs of instructions ahead; see the forward)
+            PkFrag fk[2], fv[2], ft[2], pf[4];
+            const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+            auto read_rows = [&](int i) __attribute__((always_inline)) {
+                fk[i & 1].v = o.row(pk_smem, i / KS, i % KS);
+                fv[i & 1].v = o.row(pk_smem, i / KS, i % KS, TILE);
+            };
+            auto read_trans = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(pk_smem, o, (i / DB) * 16 * HD * 2, i % DB, ft[i & 1]); };
+            const pk_floatx16 zero = {};
+            read_rows(0);
+            read_rows(1);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 pk_floatx16 s, dp;
-                pk_zero(s);
-                pk_zero(dp);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    PkFrag kf, vf;
-                    kf.v = *reinterpret_cast<const pk_bf16x8*>(kt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
-                    vf.v = *reinterpret_cast<const pk_bf16x8*>(kt + TILE + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
-                    s = pk_mfma(kf, qf[ks], s);
-                    dp = pk_mfma(vf, df[ks], dp);
+                    const int i = h * KS + ks;
+                    s = pk_mfma(fk[i & 1], qf[ks], ks == 0 ? zero : s);
+                    dp = pk_mfma(fv[i & 1], df[ks], ks == 0 ? zero : dp);
+                    if (i + 2 < 2 * KS) read_rows(i + 2);
+                    // the second product of the 32 keys before
+                    if (h == 1 && !careful) {
+#pragma unroll
+                        for (int u = 0; u < 2 * DB / KS; ++u) {
+                            const int n = ks * (2 * DB / KS) + u;
+                            acc[n % DB] = pk_mfma(ft[n & 1], pf[n / DB], acc[n % DB]);
+                            read_trans(n + 2);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                if (h == 0 && !careful) { read_trans(0); read_trans(1); }
                 float ds[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, -info.x)) * (dp[e] - info.y);
                 if (mask) {
                     // (the only key that a row sees has the probability 1 whatever its score)
-                    const int rel = limit == 0 ? -1 : limit - kb - 4 * hi;
+                    const int limit = limit_of(), rel = limit == 0 ? -1 : limit - kb - 4 * hi;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) ds[e] = 32 * h + pk_pos(e) <= rel ? ds[e] : 0.f;
                 }
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(ds[e], ds[e + 1]);
             }
-            if (careful && mask) {
-                pk_second_careful<HD, false>(kt, pf, pf, acc);
-                return;
+            if constexpr (careful) {
+                if (mask) {
+                    pk_second_careful<HD, false>(kt, pf, pf, acc);
+                    return;
+                }
+                read_trans(0);
+                read_trans(1);
             }
-            pk_second<HD, 0, 4>(kt, off, pf, acc);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = careful ? 0 : 2 * DB; n < 4 * DB; ++n) {
+                acc[n % DB] = pk_mfma(ft[n & 1], pf[n / DB], acc[n % DB]);
+                if (n + 2 < 4 * DB) read_trans(n + 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     };
     auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+        begin();
         if (tiles > 0) arrive(0);
         for (int j = 0; j < tiles; ++j) {
             __syncthreads();
@@ -592,11 +666,9 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         }
     };
     all_tiles(std::false_type());
-    if (__syncthreads_or(mine && pk_not_finite(acc))) {
-        if (tiles > 0) request(0);
-        all_tiles(std::true_type());
-    }
-    pk_store<HD>(acc, a.scale, dq + (int64_t)(t.q0 + tq) * lddq + (int64_t)head * HD, mine);
+    if (__syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) all_tiles(std::true_type());
+    const Row r = row_of_lane();
+    pk_store<HD>(acc, a.scale, dq + r.tok * lddq + (int64_t)r.head * HD, r.mine);
 }
 
 // dk, dv: four waves of 32 keys, K and V in registers, against tiles of 64 rows of q and do that they share.  Sums, operands and scores are some 300
@@ -628,21 +700,58 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     const bf16_t* Dh = dout + (int64_t)t.q0 * lddo + (int64_t)kvh * G * HD;
     uint4 qd[N], dd[N], next = make_uint4(0, 0, 0, 0);
     int next_limit = -1;
-    auto request = [&](int j) __attribute__((always_inline)) {
-        const int base = row0 + j * PK_T, q0 = query_of(base);
-        const auto rq = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Qh + q0 * a.ldq), 0, (int)0xFFFFFFFFu, 0x00020000);
-        const auto rd = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Dh + q0 * lddo), 0, (int)0xFFFFFFFFu, 0x00020000);
+    // Where the next tile starts: its first row's query and head, and the lane's rows relative to that query: head and byte offsets.  A tile on, 64 rows are
+    // so many queries and heads, with a query more where the heads pass G
+    const int step_q = query_of(PK_T), step_h = PK_T - step_q * G, ldq2 = (int)(2 * a.ldq), ldd2 = (int)(2 * lddo);
+    int at_q, at_h, lane_h[N], lane_q[N], lane_d[N];
+    auto start_rows = [&]() __attribute__((always_inline)) {
+        at_q = query_of(row0);
+        at_h = row0 - at_q * G;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r = ROWS * (N * wave + i) + lane / (HD / 8), row = min(base + r, R - 1);
-            const int q = query_of(row), col = ((row - q * G) * HD + ((lane % (HD / 8)) ^ pk_swz<HD>(r)) * 8) * 2;
-            qd[i] = pk_load16(rq, (q - q0) * (int)(2 * a.ldq) + col);
-            dd[i] = pk_load16(rd, (q - q0) * (int)(2 * lddo) + col);
+            const int r = ROWS * (N * wave + i) + lane / (HD / 8), q = query_of(at_h + r), chunk = ((lane % (HD / 8)) ^ pk_swz<HD>(r)) << 4;
+            lane_h[i] = at_h + r - q * G;
+            lane_q[i] = q * ldq2 + lane_h[i] * (HD * 2) + chunk;
+            lane_d[i] = q * ldd2 + lane_h[i] * (HD * 2) + chunk;
+        }
+    };
+    auto request = [&](int j) __attribute__((always_inline)) {
+        const int base = row0 + j * PK_T;
+        const auto rq = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Qh + at_q * a.ldq), 0, (int)0xFFFFFFFFu, 0x00020000);
+        const auto rd = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Dh + at_q * lddo), 0, (int)0xFFFFFFFFu, 0x00020000);
+        if (base + PK_T <= R) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                qd[i] = pk_load16(rq, lane_q[i], 0);
+                dd[i] = pk_load16(rd, lane_d[i], 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = ROWS * (N * wave + i) + lane / (HD / 8), row = min(base + r, R - 1);
+                const int q = query_of(row), col = ((row - q * G) * HD + ((lane % (HD / 8)) ^ pk_swz<HD>(r)) * 8) * 2;
+                qd[i] = pk_load16(rq, (q - at_q) * ldq2 + col, 0);
+                dd[i] = pk_load16(rd, (q - at_q) * ldd2 + col, 0);
+            }
         }
         if (wave == 0) {
             const int r = min(base + lane, R - 1), q = query_of(r);
             next = rowinfo[(int64_t)(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
             next_limit = base + lane >= R ? -1 : a.causal ? q + shift : t.nk - 1;
+        }
+        // on to the tile behind
+        at_q += step_q;
+        at_h += step_h;
+        const bool over = at_h >= G;
+        at_q += over ? 1 : 0;
+        at_h -= over ? G : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int h = lane_h[i] + step_h, back = h >= G ? HD * 2 * G : 0, more = (h >= G ? 1 : 0) - (over ? 1 : 0);
+            lane_h[i] = h >= G ? h - G : h;
+            const int by = step_h * (HD * 2) - back;
+            lane_q[i] += by + (more > 0 ? ldq2 : more < 0 ? -ldq2 : 0);
+            lane_d[i] += by + (more > 0 ? ldd2 : more < 0 ? -ldd2 : 0);
         }
     };
     auto arrive = [&](int j) __attribute__((always_inline)) {
@@ -659,29 +768,27 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     };
     const PkOffsets<HD> off;
     PkFrag kf[KS], vf[KS], ones;
-    if (tiles > 0) {
+    const bf16_t* ksrc = a.k + (int64_t)(t.k0 + key) * a.ldk + kvh * HD + 8 * hi;
+    const bf16_t* vsrc = a.v + (int64_t)(t.k0 + key) * a.ldv + kvh * HD + 8 * hi;
+    auto begin = [&]() __attribute__((always_inline)) {                       // (as in the forward)
+        if (tiles <= 0) return;
+        start_rows();
         request(0);
-        const bf16_t* ksrc = a.k + (int64_t)(t.k0 + key) * a.ldk + kvh * HD + 8 * hi;
-        const bf16_t* vsrc = a.v + (int64_t)(t.k0 + key) * a.ldv + kvh * HD + 8 * hi;
+        asm volatile("" : "+v"(ksrc), "+v"(vsrc));
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             kf[ks].u = *reinterpret_cast<const uint4*>(ksrc + 16 * ks);
             vf[ks].u = *reinterpret_cast<const uint4*>(vsrc + 16 * ks);
         }
-    }
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+    };
     ones.u = hi ? make_uint4(0, 0, 0, 0) : make_uint4(0x3F803F80u, 0x3F80u, 0, 0);
     const float sc = a.scale * PK_LOG2E;
     pk_floatx16 ak[DB], av[DB];
-    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
-        constexpr bool careful = decltype(CAREFUL)::value;
-        const int base = row0 + j * PK_T;
-        const int low = a.causal ? query_of(base) + shift : t.nk - 1, high = a.causal ? query_of(min(base + PK_T - 1, R - 1)) + shift : t.nk - 1;   // the rows' first and last limit
-        if (high < wkey) return;                                              // (wave-uniform)
-        const bool mask = low < wkey + 31 || base + PK_T > R;
-        const char* qt = pk_smem + (j & 1) * (2 * TILE);
+    auto scores = [&](auto MASK, int j, PkFrag (&pf)[4], PkFrag (&df)[4]) __attribute__((always_inline)) {
+        const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
         const uint4* info = infos + (j & 1) * PK_T;
         const int* limit = limits + (j & 1) * PK_T + 4 * hi;
-        PkFrag pf[4], df[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             pk_floatx16 s, dp;
@@ -696,8 +803,8 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 PkFrag qa, da;
-                qa.v = *reinterpret_cast<const pk_bf16x8*>(qt + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
-                da.v = *reinterpret_cast<const pk_bf16x8*>(qt + TILE + h * 32 * HD * 2 + (off.rows ^ (ks << 5)));
+                qa.v = o.row(pk_smem, h, ks);
+                da.v = o.row(pk_smem, h, ks, TILE);
                 s = pk_mfma(qa, kf[ks], s);
                 dp = pk_mfma(da, vf[ks], dp);
             }
@@ -706,7 +813,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
             for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(s[e] * sc);
 #pragma unroll
             for (int e = 0; e < 16; ++e) dp[e] *= p[e];
-            if (mask) {
+            if constexpr (decltype(MASK)::value) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int last = limit[32 * h + pk_pos(e)];
@@ -722,7 +829,88 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
                 df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(dp[e], dp[e + 1]);
             }
         }
-        if (careful && mask) {
+    };
+    // A tile whose rows all see all keys of the wave, in an order of its own, which the compiler is kept to: with one wave to a SIMD nothing else fills the waits,
+    // and left to itself the compiler reads operands right before each instruction.  Operands are read four instructions ahead; the first 32 rows' scores; the
+    // others' beside the first ones' exponentials; the second products of the first beside the others' exponentials; the rest
+    auto all_seen = [&](int j) __attribute__((always_inline)) {
+        const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+        const uint4* info = infos + (j & 1) * PK_T;
+        PkFrag fq[4], fd[4], xl[2], xd[2], pf[4], df[4];
+        const pk_floatx16 zero = {};
+        pk_floatx16 s[2], dp[2];
+        float p_[2], d_[2];
+        auto read_rows = [&](int i) __attribute__((always_inline)) {
+            fq[i & 3].v = o.row(pk_smem, i / KS, i % KS);
+            fd[i & 3].v = o.row(pk_smem, i / KS, i % KS, TILE);
+        };
+        // second products: for each 16 rows the DB groups of dims of dv, then those of dk
+        auto read_trans = [&](int i) __attribute__((always_inline)) {
+            const int slab = i / (2 * DB), k = i % (2 * DB);
+            pk_read_trans<HD>(pk_smem, o, (k < DB ? TILE : 0) + slab * 16 * HD * 2, k % DB, fq[i & 3]);
+        };
+        auto element = [&](int h, int e) __attribute__((always_inline)) {
+            p_[e & 1] = __builtin_amdgcn_exp2f(s[h][e] * sc);
+            d_[e & 1] = dp[h][e] * p_[e & 1];
+            if (e & 1) {
+                pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p_[0], p_[1]);
+                df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(d_[0], d_[1]);
+            }
+        };
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 in = info[32 * h + (lane & 31)];
+            xl[h].u = make_uint4(in.x, in.y, 0, 0);
+            xd[h].u = make_uint4(in.z, in.w, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) read_rows(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+            const int h = i / KS, ks = i % KS;
+            if (ks == 0) {
+                s[h] = pk_mfma(xl[h], ones, zero);
+                dp[h] = pk_mfma(xd[h], ones, zero);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            s[h] = pk_mfma(fq[i & 3], kf[ks], s[h]);
+            dp[h] = pk_mfma(fd[i & 3], vf[ks], dp[h]);
+            if (i + 4 < 2 * KS) read_rows(i + 4);
+            else read_trans(i + 4 - 2 * KS);
+            if (h == 1) {
+#pragma unroll
+                for (int e = 0; e < 16 / KS; ++e) element(0, ks * (16 / KS) + e);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8 * DB; ++i) {
+            const int slab = i / (2 * DB), k = i % (2 * DB);
+            if (k < DB) av[k] = pk_mfma(fq[i & 3], pf[slab], av[k]);
+            else ak[k - DB] = pk_mfma(fq[i & 3], df[slab], ak[k - DB]);
+            if (i + 4 < 8 * DB) read_trans(i + 4);
+            if (i < 4 * DB) {
+#pragma unroll
+                for (int e = 0; e < 4 / DB; ++e) element(1, i * (4 / DB) + e);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
+        constexpr bool careful = decltype(CAREFUL)::value;
+        const int base = row0 + j * PK_T;
+        const int low = a.causal ? query_of(base) + shift : t.nk - 1, high = a.causal ? query_of(min(base + PK_T - 1, R - 1)) + shift : t.nk - 1;   // the rows' first and last limit
+        if (high < wkey) return;                                              // (wave-uniform)
+        const char* qt = pk_smem + (j & 1) * (2 * TILE);
+        PkFrag pf[4], df[4];
+        if (low >= wkey + 31 && base + PK_T <= R) {
+            all_seen(j);
+            return;
+        }
+        scores(std::true_type(), j, pf, df);
+        if constexpr (careful) {
+            const int* limit = limits + (j & 1) * PK_T + 4 * hi;
             PkFrag seen[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s)
@@ -734,24 +922,28 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
             pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
             pk_second_careful<HD, false>(qt, df, df, ak);
         } else {
-            pk_second<HD, 0, 4>(qt + TILE, off, pf, av);
-            pk_second<HD, 0, 4>(qt, off, df, ak);
+            const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+            pk_second<HD, 0, 4>(pk_smem, o, TILE, pf, av);
+            pk_second<HD, 0, 4>(pk_smem, o, 0, df, ak);
         }
     };
     auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) { pk_zero(ak[d]); pk_zero(av[d]); }
+        begin();
         if (tiles > 0) arrive(0);
         for (int j = 0; j < tiles; ++j) {
             __syncthreads();
             if (j + 1 < tiles) request(j + 1);
             one_tile(CAREFUL, j);
+            // (the sums stay in accumulation registers: where the ways through a tile meet, the compiler takes them to ordinary ones and back, 256 instructions)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) asm volatile("" : "+a"(ak[d]), "+a"(av[d]));
             if (j + 1 < tiles) arrive(j + 1);
         }
     };
     all_tiles(std::false_type());
     if (__syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) {
-        if (tiles > 0) request(0);
         all_tiles(std::true_type());
     }
     pk_store<HD>(av, 1.f, dv + (int64_t)(t.k0 + key) * lddv + (int64_t)kvh * HD, mine);
