@@ -29,6 +29,7 @@ typedef __bf16 pk_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float pk_floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t pk_u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* pk_lptr;
+typedef __attribute__((address_space(3))) char* pk_lchar;
 typedef const __attribute__((address_space(1))) void* pk_gptr;
 union PkFrag { uint4 u; uint32_t w[4]; pk_bf16x8 v; };
 
@@ -72,14 +73,15 @@ struct PkOffsets {
             trans[s] = tr * (HD * 2) + (((2 * dg + ((n16 & 3) >> 1)) ^ pk_swz<HD>(tr)) << 4) + (n16 & 1) * 8;
         }
     }
-    // of a tile that starts `at` bytes into LDS, a multiple of 256.  (Values that the compiler does not know: it would work out every read's address ahead of
+    // addresses in LDS of a tile that starts at `at`, a multiple of 256.  (Values that the compiler does not know: it would work out every read's address ahead of
     // the loop over tiles and spill them, and a wait for a reload is one for the next tile's loads too)
     __device__ __forceinline__ PkOffsets(const PkOffsets& of, int at) : rows(of.rows + at), trans{of.trans[0] + at, of.trans[1] + at} {
         asm volatile("" : "+v"(rows), "+v"(trans[0]), "+v"(trans[1]));
     }
     // chunk 2 ks + lane / 32 of row 32 h + lane % 32
-    __device__ __forceinline__ pk_bf16x8 row(const char* lds, int h, int ks, int more = 0) const {
-        return *reinterpret_cast<const pk_bf16x8*>(lds + ((rows ^ (ks << 5)) + h * 32 * HD * 2 + more));
+    __device__ __forceinline__ pk_bf16x8 row(int h, int ks, int more = 0) const {
+        typedef const __attribute__((address_space(3))) pk_bf16x8* ptr;
+        return *(ptr)(uintptr_t)(uint32_t)((rows ^ (ks << 5)) + h * 32 * HD * 2 + more);
     }
 };
 
@@ -87,22 +89,22 @@ struct PkOffsets {
 typedef __bf16 pk_bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pk_bf16x4* pk_trptr;
 template <int HD>
-__device__ __forceinline__ void pk_read_trans(const char* lds, const PkOffsets<HD>& o, int at, int db, PkFrag& f) {
+__device__ __forceinline__ void pk_read_trans(const PkOffsets<HD>& o, int at, int db, PkFrag& f) {
     union { pk_bf16x4 v; uint2 u; } lo, hi;
-    lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(lds + ((o.trans[0] ^ (db << 6)) + at)));
-    hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(pk_lptr)const_cast<char*>(lds + ((o.trans[1] ^ (db << 6)) + at)));
+    lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(uintptr_t)(uint32_t)((o.trans[0] ^ (db << 6)) + at));
+    hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(uintptr_t)(uint32_t)((o.trans[1] ^ (db << 6)) + at));
     f.u = make_uint4(lo.u.x, lo.u.y, hi.u.x, hi.u.y);
 }
 
 // acc[db] += (positions x dims of a tile)^T times fragments FROM .. TO of 16 positions each
 template <int HD, int FROM, int TO>
-__device__ __forceinline__ void pk_second(const char* lds, const PkOffsets<HD>& o, int at, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
+__device__ __forceinline__ void pk_second(const PkOffsets<HD>& o, int at, const PkFrag (&p)[4], pk_floatx16 (&acc)[HD / 32]) {
 #pragma unroll
     for (int s = FROM; s < TO; ++s)
 #pragma unroll
         for (int db = 0; db < HD / 32; ++db) {
             PkFrag f;
-            pk_read_trans<HD>(lds, o, at + s * 16 * HD * 2, db, f);
+            pk_read_trans<HD>(o, at + s * 16 * HD * 2, db, f);
             acc[db] = pk_mfma(f, p[s], acc[db]);
         }
 }
@@ -235,23 +237,16 @@ template <int HD>
 struct PkLoader {
     static constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);      // loads of a wave, rows of a load
     static_assert(ROWS * N == 16 && (HD == 128 || HD == 64), "swz() of the rows of load i");
-    int row, chunk;      // of the first load: byte offset of the lane's row, place of its chunk
     uint4 data[N];
-    __device__ __forceinline__ explicit PkLoader(int64_t ld) {
-        const int lane = threadIdx.x & 63, r = 16 * (int)(threadIdx.x >> 6) + lane / (HD / 8);
-        row = r * (int)(ld * 2);
-        chunk = (lane % (HD / 8)) ^ pk_swz<HD>(r);
-    }
     __device__ __forceinline__ void load(const bf16_t* base, int64_t ld, int left) {
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, (int)0xFFFFFFFFu, 0x00020000);
-        if (left >= PK_T) {
+        // (one way for tiles inside a sequence and at its end: loads on two ways are moved where these meet, and waited for.  Rows are below 2^6, their bytes 2^23)
+        int lane_ = (int)threadIdx.x;
+        asm volatile("" : "+v"(lane_));
+        const int lane = lane_ & 63, r = 16 * (lane_ >> 6) + lane / (HD / 8), chunk = ((lane % (HD / 8)) ^ pk_swz<HD>(r)) << 4;
 #pragma unroll
-            for (int i = 0; i < N; ++i) data[i] = pk_load16(rsrc, row + ((chunk ^ pk_swz<HD>(ROWS * i)) << 4), ROWS * i * (int)(ld * 2));
-        } else {
-            const int r = 16 * (int)(threadIdx.x >> 6) + (int)(threadIdx.x & 63) / (HD / 8);
-#pragma unroll
-            for (int i = 0; i < N; ++i) data[i] = pk_load16(rsrc, min(r + ROWS * i, left - 1) * (int)(ld * 2) + ((chunk ^ pk_swz<HD>(ROWS * i)) << 4), 0);
-        }
+        for (int i = 0; i < N; ++i)
+            data[i] = pk_load16(rsrc, (int)(__umul24((uint32_t)min(r + ROWS * i, left - 1), (uint32_t)(2 * ld)) + (uint32_t)(chunk ^ (pk_swz<HD>(ROWS * i) << 4))), 0);
     }
     __device__ __forceinline__ void store(char* tile) const {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -286,17 +281,20 @@ constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits.  A tile is 64 matrix instructions a wave (HD = 128, 2048 cycles) beside some 1500 cycles of exponentials and 32 KB of LDS reads.
 // part != NULL: workgroup y takes its share of the row tile's keys and leaves sums, maximum and sum of exponentials for pk_join_kernel
-template <int HD>
-__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_forward_kernel(
-        PackedArgs a, bf16_t* __restrict__ out, int64_t ldo, float* __restrict__ lse, float* __restrict__ part, float2* __restrict__ part_ml) {
-    extern __shared__ __align__(1024) char pk_smem[];
+//
+// Returns whether the workgroup has to go over its tiles once more, with care (and has stored nothing then)
+struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; };
+template <int HD, bool careful>
+__device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardOut& to_, pk_lchar lds) {
+    char* pk_smem = (char*)lds;
+    const int lds_at = (int)(uint32_t)(uintptr_t)lds;
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
     // the last tiles first, for they have most keys; the key heads side by side: an XCD (workgroup number mod 8) then has few of them
     const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)(gridDim.x - 1 - blockIdx.x), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return;
+    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return false;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
     // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
@@ -317,7 +315,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const int j0 = (int)((int64_t)tiles * blockIdx.y / gridDim.y), j1 = (int)((int64_t)tiles * (blockIdx.y + 1) / gridDim.y);
     const bf16_t* Kh = a.k + (int64_t)t.k0 * a.ldk + kvh * HD;
     const bf16_t* Vh = a.v + (int64_t)t.k0 * a.ldv + kvh * HD;
-    PkLoader<HD> lk(a.ldk), lv(a.ldv);
+    PkLoader<HD> lk, lv;
     auto request = [&](int j) __attribute__((always_inline)) {
         lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T);
         lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T);
@@ -344,17 +342,16 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const float slack = 8.f / sc;
     pk_floatx16 acc[DB];
     float top, topsc, l;
-    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
-            constexpr bool careful = decltype(CAREFUL)::value;
+    auto one_tile = [&](int j) __attribute__((always_inline)) {
             const int kb = j * PK_T;
             if (kb > wlast) return;                                          // (wave-uniform)
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
             // (operands are read four instructions ahead, the exponentials of 16 keys run beside the second product of the 16 before them: left to
             // itself the compiler reads right before each instruction)
-            const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+            const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
             PkFrag f[4];
-            auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = o.row(pk_smem, i & 1, i >> 1); };
-            auto read_v = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(pk_smem, o, TILE + (i / DB) * 16 * HD * 2, i % DB, f[i & 3]); };
+            auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = o.row(i & 1, i >> 1); };
+            auto read_v = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(o, TILE + (i / DB) * 16 * HD * 2, i % DB, f[i & 3]); };
             const pk_floatx16 zero = {};
             pk_floatx16 s[2];
 #pragma unroll
@@ -421,38 +418,44 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
-    auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
-        top = -INFINITY; topsc = 0.f; l = 0.f;
-        begin();
-        if (j0 < j1) arrive(j0);
-        for (int j = j0; j < j1; ++j) {
-            __syncthreads();
-            if (j + 1 < j1) request(j + 1);
-            one_tile(CAREFUL, j);
-            if (j + 1 < j1) arrive(j + 1);
-        }
-    };
-    all_tiles(std::false_type());
-    if (__syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) all_tiles(std::true_type());
+    for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+    top = -INFINITY; topsc = 0.f; l = 0.f;
+    begin();
+    if (j0 < j1) arrive(j0);
+    for (int j = j0; j < j1; ++j) {
+        __syncthreads();
+        if (j + 1 < j1) request(j + 1);
+        one_tile(j);
+        if (j + 1 < j1) arrive(j + 1);
+    }
+    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return true;
     l = pk_sum_halves(l);
     const Row r = row_of_lane();
-    if (part) {
-        if (!r.mine) return;
+    if (to_.part) {
+        if (!r.mine) return false;
         const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + r.tok * a.n_heads + r.head;
-        float* to = part + at * HD + 4 * hi;
+        float* to = to_.part + at * HD + 4 * hi;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<float4*>(to + 32 * db + 8 * g) = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
-        if (hi == 0) part_ml[at] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
-        return;
+        if (hi == 0) to_.part_ml[at] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
+        return false;
     }
     const bool empty = r.limit < 0;
-    pk_store<HD>(acc, empty ? 0.f : 1.f / l, out + r.tok * ldo + (int64_t)r.head * HD, r.mine);
-    if (lse && r.mine && hi == 0) lse[r.tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
+    pk_store<HD>(acc, empty ? 0.f : 1.f / l, to_.out + r.tok * to_.ldo + (int64_t)r.head * HD, r.mine);
+    if (to_.lse && r.mine && hi == 0) to_.lse[r.tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
+    return false;
+}
+// (a function that is called: its registers are not the kernel's)
+template <int HD>
+__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, pk_lchar lds) { (void)pk_forward<HD, true>(a, to, lds); }
+template <int HD>
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_forward_kernel(PackedArgs a, PkForwardOut to) {
+    extern __shared__ __align__(1024) char pk_dynamic[];
+    if (pk_forward<HD, false>(a, to, (pk_lchar)pk_dynamic)) pk_forward_again<HD>(a, to, (pk_lchar)pk_dynamic);
 }
 
 // Shares of the keys joined: HD / 4 lanes a row.  Rows of no sequence are left alone: their partial sums are what the workspace held
@@ -528,17 +531,19 @@ __global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_
     rowinfo[row] = make_uint4(u.x, u.y, v.x, v.y);
 }
 
+struct PkBackward { const bf16_t* dout; int64_t lddo; const uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; };
+
 // dq: the forward's shape, with do beside q in registers, and K read with and without transposition
-template <int HD>
-__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_dq_kernel(
-        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const uint4* __restrict__ rowinfo, bf16_t* __restrict__ dq, int64_t lddq) {
-    extern __shared__ __align__(1024) char pk_smem[];
+template <int HD, bool careful>
+__device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, pk_lchar lds) {
+    char* pk_smem = (char*)lds;
+    const int lds_at = (int)(uint32_t)(uintptr_t)lds;
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
     const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)(gridDim.x - 1 - blockIdx.x), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return;
+    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return false;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
     // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
@@ -558,7 +563,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
     const int tiles = last < 0 ? 0 : last / PK_T + 1;
     const bf16_t* Kh = a.k + (int64_t)t.k0 * a.ldk + kvh * HD;
     const bf16_t* Vh = a.v + (int64_t)t.k0 * a.ldv + kvh * HD;
-    PkLoader<HD> lk(a.ldk), lv(a.ldv);
+    PkLoader<HD> lk, lv;
     auto request = [&](int j) __attribute__((always_inline)) {
         lk.load(Kh + (int64_t)j * PK_T * a.ldk, a.ldk, t.nk - j * PK_T);
         lv.load(Vh + (int64_t)j * PK_T * a.ldv, a.ldv, t.nk - j * PK_T);
@@ -575,31 +580,30 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
         if (tiles > 0) request(0);
         const Row r = row_of_lane();
         const bf16_t* qsrc = a.q + r.tok * a.ldq + (int64_t)r.head * HD + 8 * hi;
-        const bf16_t* dsrc = dout + r.tok * lddo + (int64_t)r.head * HD + 8 * hi;
+        const bf16_t* dsrc = g.dout + r.tok * g.lddo + (int64_t)r.head * HD + 8 * hi;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
             df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
         }
-        const uint4 parts = rowinfo[r.tok * a.n_heads + r.head];
+        const uint4 parts = g.rowinfo[r.tok * a.n_heads + r.head];
         __builtin_amdgcn_s_waitcnt(0x0F70);
         info = make_float2(-sc * pk_join3(parts.x, parts.y), -pk_join3(parts.z, parts.w));
     };
     pk_floatx16 acc[DB];
-    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
-            constexpr bool careful = decltype(CAREFUL)::value;
+    auto one_tile = [&](int j) __attribute__((always_inline)) {
             const int kb = j * PK_T;
             if (kb > wlast) return;
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
             const bool mask = kb + PK_T - 1 > wfirst;
             // (operands two pairs of instructions ahead; see the forward)
             PkFrag fk[2], fv[2], ft[2], pf[4];
-            const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+            const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
             auto read_rows = [&](int i) __attribute__((always_inline)) {
-                fk[i & 1].v = o.row(pk_smem, i / KS, i % KS);
-                fv[i & 1].v = o.row(pk_smem, i / KS, i % KS, TILE);
+                fk[i & 1].v = o.row(i / KS, i % KS);
+                fv[i & 1].v = o.row(i / KS, i % KS, TILE);
             };
-            auto read_trans = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(pk_smem, o, (i / DB) * 16 * HD * 2, i % DB, ft[i & 1]); };
+            auto read_trans = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(o, (i / DB) * 16 * HD * 2, i % DB, ft[i & 1]); };
             const pk_floatx16 zero = {};
             read_rows(0);
             read_rows(1);
@@ -653,32 +657,38 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
-    auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
-        begin();
-        if (tiles > 0) arrive(0);
-        for (int j = 0; j < tiles; ++j) {
-            __syncthreads();
-            if (j + 1 < tiles) request(j + 1);
-            one_tile(CAREFUL, j);
-            if (j + 1 < tiles) arrive(j + 1);
-        }
-    };
-    all_tiles(std::false_type());
-    if (__syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) all_tiles(std::true_type());
+    for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+    begin();
+    if (tiles > 0) arrive(0);
+    for (int j = 0; j < tiles; ++j) {
+        __syncthreads();
+        if (j + 1 < tiles) request(j + 1);
+        one_tile(j);
+        if (j + 1 < tiles) arrive(j + 1);
+    }
+    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return true;
     const Row r = row_of_lane();
-    pk_store<HD>(acc, a.scale, dq + r.tok * lddq + (int64_t)r.head * HD, r.mine);
+    pk_store<HD>(acc, a.scale, g.dq + r.tok * g.lddq + (int64_t)r.head * HD, r.mine);
+    return false;
+}
+template <int HD>
+__device__ __noinline__ void pk_dq_again(PackedArgs a, PkBackward g, pk_lchar lds) { (void)pk_dq<HD, true>(a, g, lds); }
+template <int HD>
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_dq_kernel(PackedArgs a, PkBackward g) {
+    extern __shared__ __align__(1024) char pk_dynamic[];
+    if (pk_dq<HD, false>(a, g, (pk_lchar)pk_dynamic)) pk_dq_again<HD>(a, g, (pk_lchar)pk_dynamic);
 }
 
 // dk, dv: four waves of 32 keys, K and V in registers, against tiles of 64 rows of q and do that they share.  Sums, operands and scores are some 300
 // registers: one wave to a SIMD.  What belongs to a row comes in through the products, as a further step of 16 dims of which three are used: read row by
 // row in the instruction's layout it was 24 KB of LDS reads a tile and wave beside 64 KB of operands
-template <int HD>
-__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1, 1))) void pk_dkv_kernel(
-        PackedArgs a, const bf16_t* __restrict__ dout, int64_t lddo, const uint4* __restrict__ rowinfo,
-        bf16_t* __restrict__ dk, int64_t lddk, bf16_t* __restrict__ dv, int64_t lddv) {
-    extern __shared__ __align__(1024) char pk_smem[];
+template <int HD, bool careful>
+__device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g, pk_lchar lds) {
+    char* pk_smem = (char*)lds;
+    const int lds_at = (int)(uint32_t)(uintptr_t)lds;
+    const bf16_t* dout = g.dout;
+    const int64_t lddo = g.lddo;
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     uint4* infos = reinterpret_cast<uint4*>(pk_smem + 4 * TILE);              // two stages of a tile's rows
     int* limits = reinterpret_cast<int*>(infos + 2 * PK_T);                   // ... and the last key that they see
@@ -686,7 +696,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     const int hi = lane >> 5;
     const int G = PkDiv(a.n_kv)(a.n_heads), at = PkDiv(a.n_kv)((int)blockIdx.x), kvh = (int)blockIdx.x - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, true>(a, at, G, t)) return;
+    if (!pk_find<PK_ROWS, true>(a, at, G, t)) return false;
     const int R = t.nq * G, shift = t.nk - t.nq;
     const int key0 = t.tile * PK_ROWS, wkey = key0 + wave * 32;
     const int key = min(wkey + (lane & 31), t.nk - 1);
@@ -719,24 +729,18 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
         const int base = row0 + j * PK_T;
         const auto rq = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Qh + at_q * a.ldq), 0, (int)0xFFFFFFFFu, 0x00020000);
         const auto rd = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(Dh + at_q * lddo), 0, (int)0xFFFFFFFFu, 0x00020000);
-        if (base + PK_T <= R) {
+        // (one way for all tiles, as in PkLoader)
+        const int left = R - base, end_q = query_of(R - 1), end_h = R - 1 - end_q * G;
+        const int end_at_q = (end_q - at_q) * ldq2 + end_h * (HD * 2), end_at_d = (end_q - at_q) * ldd2 + end_h * (HD * 2);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                qd[i] = pk_load16(rq, lane_q[i], 0);
-                dd[i] = pk_load16(rd, lane_d[i], 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int r = ROWS * (N * wave + i) + lane / (HD / 8), row = min(base + r, R - 1);
-                const int q = query_of(row), col = ((row - q * G) * HD + ((lane % (HD / 8)) ^ pk_swz<HD>(r)) * 8) * 2;
-                qd[i] = pk_load16(rq, (q - at_q) * ldq2 + col, 0);
-                dd[i] = pk_load16(rd, (q - at_q) * ldd2 + col, 0);
-            }
+        for (int i = 0; i < N; ++i) {
+            const int r = ROWS * (N * wave + i) + lane / (HD / 8), chunk = ((lane % (HD / 8)) ^ pk_swz<HD>(r)) << 4;
+            qd[i] = pk_load16(rq, r < left ? lane_q[i] : end_at_q + chunk, 0);
+            dd[i] = pk_load16(rd, r < left ? lane_d[i] : end_at_d + chunk, 0);
         }
         if (wave == 0) {
             const int r = min(base + lane, R - 1), q = query_of(r);
-            next = rowinfo[(int64_t)(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
+            next = g.rowinfo[(int64_t)(t.q0 + q) * a.n_heads + kvh * G + (r - q * G)];
             next_limit = base + lane >= R ? -1 : a.causal ? q + shift : t.nk - 1;
         }
         // on to the tile behind
@@ -786,7 +790,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     const float sc = a.scale * PK_LOG2E;
     pk_floatx16 ak[DB], av[DB];
     auto scores = [&](auto MASK, int j, PkFrag (&pf)[4], PkFrag (&df)[4]) __attribute__((always_inline)) {
-        const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+        const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
         const uint4* info = infos + (j & 1) * PK_T;
         const int* limit = limits + (j & 1) * PK_T + 4 * hi;
 #pragma unroll
@@ -803,8 +807,8 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 PkFrag qa, da;
-                qa.v = o.row(pk_smem, h, ks);
-                da.v = o.row(pk_smem, h, ks, TILE);
+                qa.v = o.row(h, ks);
+                da.v = o.row(h, ks, TILE);
                 s = pk_mfma(qa, kf[ks], s);
                 dp = pk_mfma(da, vf[ks], dp);
             }
@@ -834,20 +838,20 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     // and left to itself the compiler reads operands right before each instruction.  Operands are read four instructions ahead; the first 32 rows' scores; the
     // others' beside the first ones' exponentials; the second products of the first beside the others' exponentials; the rest
     auto all_seen = [&](int j) __attribute__((always_inline)) {
-        const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
+        const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
         const uint4* info = infos + (j & 1) * PK_T;
         PkFrag fq[4], fd[4], xl[2], xd[2], pf[4], df[4];
         const pk_floatx16 zero = {};
         pk_floatx16 s[2], dp[2];
         float p_[2], d_[2];
         auto read_rows = [&](int i) __attribute__((always_inline)) {
-            fq[i & 3].v = o.row(pk_smem, i / KS, i % KS);
-            fd[i & 3].v = o.row(pk_smem, i / KS, i % KS, TILE);
+            fq[i & 3].v = o.row(i / KS, i % KS);
+            fd[i & 3].v = o.row(i / KS, i % KS, TILE);
         };
         // second products: for each 16 rows the DB groups of dims of dv, then those of dk
         auto read_trans = [&](int i) __attribute__((always_inline)) {
             const int slab = i / (2 * DB), k = i % (2 * DB);
-            pk_read_trans<HD>(pk_smem, o, (k < DB ? TILE : 0) + slab * 16 * HD * 2, k % DB, fq[i & 3]);
+            pk_read_trans<HD>(o, (k < DB ? TILE : 0) + slab * 16 * HD * 2, k % DB, fq[i & 3]);
         };
         auto element = [&](int h, int e) __attribute__((always_inline)) {
             p_[e & 1] = __builtin_amdgcn_exp2f(s[h][e] * sc);
@@ -897,8 +901,7 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto one_tile = [&](auto CAREFUL, int j) __attribute__((always_inline)) {
-        constexpr bool careful = decltype(CAREFUL)::value;
+    auto one_tile = [&](int j) __attribute__((always_inline)) {
         const int base = row0 + j * PK_T;
         const int low = a.causal ? query_of(base) + shift : t.nk - 1, high = a.causal ? query_of(min(base + PK_T - 1, R - 1)) + shift : t.nk - 1;   // the rows' first and last limit
         if (high < wkey) return;                                              // (wave-uniform)
@@ -922,32 +925,35 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
             pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
             pk_second_careful<HD, false>(qt, df, df, ak);
         } else {
-            const PkOffsets<HD> o(off, (j & 1) * (2 * TILE));
-            pk_second<HD, 0, 4>(pk_smem, o, TILE, pf, av);
-            pk_second<HD, 0, 4>(pk_smem, o, 0, df, ak);
+            const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
+            pk_second<HD, 0, 4>(o, TILE, pf, av);
+            pk_second<HD, 0, 4>(o, 0, df, ak);
         }
     };
-    auto all_tiles = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d) { pk_zero(ak[d]); pk_zero(av[d]); }
-        begin();
-        if (tiles > 0) arrive(0);
-        for (int j = 0; j < tiles; ++j) {
-            __syncthreads();
-            if (j + 1 < tiles) request(j + 1);
-            one_tile(CAREFUL, j);
-            // (the sums stay in accumulation registers: where the ways through a tile meet, the compiler takes them to ordinary ones and back, 256 instructions)
+    for (int d = 0; d < DB; ++d) { pk_zero(ak[d]); pk_zero(av[d]); }
+    begin();
+    if (tiles > 0) arrive(0);
+    for (int j = 0; j < tiles; ++j) {
+        __syncthreads();
+        if (j + 1 < tiles) request(j + 1);
+        one_tile(j);
+        // (the sums stay in accumulation registers: where the ways through a tile meet, the compiler takes them to ordinary ones and back, 256 instructions)
 #pragma unroll
-            for (int d = 0; d < DB; ++d) asm volatile("" : "+a"(ak[d]), "+a"(av[d]));
-            if (j + 1 < tiles) arrive(j + 1);
-        }
-    };
-    all_tiles(std::false_type());
-    if (__syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) {
-        all_tiles(std::true_type());
+        for (int d = 0; d < DB; ++d) asm volatile("" : "+a"(ak[d]), "+a"(av[d]));
+        if (j + 1 < tiles) arrive(j + 1);
     }
-    pk_store<HD>(av, 1.f, dv + (int64_t)(t.k0 + key) * lddv + (int64_t)kvh * HD, mine);
-    pk_store<HD>(ak, a.scale, dk + (int64_t)(t.k0 + key) * lddk + (int64_t)kvh * HD, mine);
+    if (!careful && __syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) return true;
+    pk_store<HD>(av, 1.f, g.dv + (int64_t)(t.k0 + key) * g.lddv + (int64_t)kvh * HD, mine);
+    pk_store<HD>(ak, a.scale, g.dk + (int64_t)(t.k0 + key) * g.lddk + (int64_t)kvh * HD, mine);
+    return false;
+}
+template <int HD>
+__device__ __noinline__ void pk_dkv_again(PackedArgs a, PkBackward g, pk_lchar lds) { (void)pk_dkv<HD, true>(a, g, lds); }
+template <int HD>
+__global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1, 1))) void pk_dkv_kernel(PackedArgs a, PkBackward g) {
+    extern __shared__ __align__(1024) char pk_dynamic[];
+    if (pk_dkv<HD, false>(a, g, (pk_lchar)pk_dynamic)) pk_dkv_again<HD>(a, g, (pk_lchar)pk_dynamic);
 }
 
 // an upper bound of the row (key) tiles of all sequences, whatever their lengths
@@ -977,7 +983,7 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
     if (units > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     float* part = shares > 1 ? static_cast<float*>(workspace) : nullptr;
     float2* ml = shares > 1 ? reinterpret_cast<float2*>(part + (int64_t)shares * rows * HD) : nullptr;
-    hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units, (unsigned)shares), dim3(64 * PK_WAVES), SMEM, st, a, out, ldo, lse, part, ml);
+    hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units, (unsigned)shares), dim3(64 * PK_WAVES), SMEM, st, a, PkForwardOut{out, ldo, lse, part, ml});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares == 1) return e;
     const int64_t blocks = (rows * (HD / 4) + 255) / 256;
@@ -995,17 +1001,18 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
     const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv), blocks = (rows * (HD / 8) + 255) / 256;
     if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     uint4* info = static_cast<uint4*>(workspace);
+    const PkBackward b{g.dout, g.lddo, info, g.dq, g.lddq, g.dk, g.lddk, g.dv, g.lddv};
     hipError_t e = hipSuccess;
     if (rows > 0) {
         hipLaunchKernelGGL(pk_delta_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, g.out, g.ldo, g.dout, g.lddo, g.lse, info);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(pk_dq_kernel<HD>, dim3((unsigned)dq_units), dim3(64 * PK_WAVES), SMEM, st, a, g.dout, g.lddo, info, g.dq, g.lddq);
+        hipLaunchKernelGGL(pk_dq_kernel<HD>, dim3((unsigned)dq_units), dim3(64 * PK_WAVES), SMEM, st, a, b);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (a.total_k > 0) {
-        hipLaunchKernelGGL(pk_dkv_kernel<HD>, dim3((unsigned)kv_units), dim3(64 * PK_WAVES), SMEM_KV, st, a, g.dout, g.lddo, info, g.dk, g.lddk, g.dv, g.lddv);
+        hipLaunchKernelGGL(pk_dkv_kernel<HD>, dim3((unsigned)kv_units), dim3(64 * PK_WAVES), SMEM_KV, st, a, b);
         e = hipGetLastError();
     }
     return e;
