@@ -789,55 +789,14 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
     ones.u = hi ? make_uint4(0, 0, 0, 0) : make_uint4(0x3F803F80u, 0x3F80u, 0, 0);
     const float sc = a.scale * PK_LOG2E;
     pk_floatx16 ak[DB], av[DB];
-    auto scores = [&](auto MASK, int j, PkFrag (&pf)[4], PkFrag (&df)[4]) __attribute__((always_inline)) {
-        const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
-        const uint4* info = infos + (j & 1) * PK_T;
+    // A tile in an order of its own, which the compiler is kept to: with one wave to a SIMD nothing else fills the waits, and left to itself the compiler reads
+    // operands right before each instruction.  Operands are read four instructions ahead; the first 32 rows' scores; the others' beside the first ones'
+    // exponentials; the second products of the first beside the others' exponentials; the rest.  MASK: not all of its rows see all keys of the wave
+    auto tile = [&](auto MASK, int j) __attribute__((always_inline)) {
+        constexpr bool mask = decltype(MASK)::value, apart = careful && mask;
         const int* limit = limits + (j & 1) * PK_T + 4 * hi;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            pk_floatx16 s, dp;
-            pk_zero(s);
-            pk_zero(dp);
-            const uint4 in = info[32 * h + (lane & 31)];
-            PkFrag x;
-            x.u = make_uint4(in.x, in.y, 0, 0);
-            s = pk_mfma(x, ones, s);
-            x.u = make_uint4(in.z, in.w, 0, 0);
-            dp = pk_mfma(x, ones, dp);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                PkFrag qa, da;
-                qa.v = o.row(h, ks);
-                da.v = o.row(h, ks, TILE);
-                s = pk_mfma(qa, kf[ks], s);
-                dp = pk_mfma(da, vf[ks], dp);
-            }
-            float p[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(s[e] * sc);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) dp[e] *= p[e];
-            if constexpr (decltype(MASK)::value) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int last = limit[32 * h + pk_pos(e)];
-                    const bool seen = wkey + (lane & 31) <= last;
-                    p[e] = seen ? p[e] : 0.f;
-                    // (the only key that a row sees has the probability 1 whatever its score)
-                    dp[e] = seen && last > 0 ? dp[e] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p[e], p[e + 1]);
-                df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(dp[e], dp[e + 1]);
-            }
-        }
-    };
-    // A tile whose rows all see all keys of the wave, in an order of its own, which the compiler is kept to: with one wave to a SIMD nothing else fills the waits,
-    // and left to itself the compiler reads operands right before each instruction.  Operands are read four instructions ahead; the first 32 rows' scores; the
-    // others' beside the first ones' exponentials; the second products of the first beside the others' exponentials; the rest
-    auto all_seen = [&](int j) __attribute__((always_inline)) {
+        int4 last[2];
+        auto read_last = [&](int h, int g4) __attribute__((always_inline)) { last[g4 & 1] = *reinterpret_cast<const int4*>(limit + 32 * h + 8 * g4); };
         const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
         const uint4* info = infos + (j & 1) * PK_T;
         PkFrag fq[4], fd[4], xl[2], xd[2], pf[4], df[4];
@@ -856,6 +815,15 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
         auto element = [&](int h, int e) __attribute__((always_inline)) {
             p_[e & 1] = __builtin_amdgcn_exp2f(s[h][e] * sc);
             d_[e & 1] = dp[h][e] * p_[e & 1];
+            if constexpr (mask) {
+                if (e % 4 == 0 && e < 12) read_last(h, e / 4 + 1);
+                const int4 l4 = last[(e >> 2) & 1];
+                const int l = (e & 3) == 0 ? l4.x : (e & 3) == 1 ? l4.y : (e & 3) == 2 ? l4.z : l4.w;
+                const bool seen = wkey + (lane & 31) <= l;
+                p_[e & 1] = seen ? p_[e & 1] : 0.f;
+                // (the only key that a row sees has the probability 1 whatever its score)
+                d_[e & 1] = seen && l > 0 ? d_[e & 1] : 0.f;
+            }
             if (e & 1) {
                 pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p_[0], p_[1]);
                 df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(d_[0], d_[1]);
@@ -874,6 +842,9 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
         for (int i = 0; i < 2 * KS; ++i) {
             const int h = i / KS, ks = i % KS;
             if (ks == 0) {
+                if constexpr (mask) {
+                    if (h == 1) read_last(0, 0);
+                }
                 s[h] = pk_mfma(xl[h], ones, zero);
                 dp[h] = pk_mfma(xd[h], ones, zero);
                 __builtin_amdgcn_sched_barrier(0);
@@ -881,12 +852,29 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
             s[h] = pk_mfma(fq[i & 3], kf[ks], s[h]);
             dp[h] = pk_mfma(fd[i & 3], vf[ks], dp[h]);
             if (i + 4 < 2 * KS) read_rows(i + 4);
-            else read_trans(i + 4 - 2 * KS);
+            else if (!apart) read_trans(i + 4 - 2 * KS);
             if (h == 1) {
 #pragma unroll
                 for (int e = 0; e < 16 / KS; ++e) element(0, ks * (16 / KS) + e);
             }
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (mask) read_last(1, 0);
+        if constexpr (apart) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) element(1, e);
+            const char* qt = pk_smem + (j & 1) * (2 * TILE);
+            PkFrag seen[4];
+#pragma unroll
+            for (int s4 = 0; s4 < 4; ++s4)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int at = 16 * s4 + (w >> 1) * 8 + (w & 1) * 2;
+                    seen[s4].w[w] = (wkey + (lane & 31) <= limit[at] ? 0x3F80u : 0u) | (wkey + (lane & 31) <= limit[at + 1] ? 0x3F800000u : 0u);
+                }
+            pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
+            pk_second_careful<HD, false>(qt, df, df, ak);
+            return;
         }
 #pragma unroll
         for (int i = 0; i < 8 * DB; ++i) {
@@ -905,30 +893,8 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
         const int base = row0 + j * PK_T;
         const int low = a.causal ? query_of(base) + shift : t.nk - 1, high = a.causal ? query_of(min(base + PK_T - 1, R - 1)) + shift : t.nk - 1;   // the rows' first and last limit
         if (high < wkey) return;                                              // (wave-uniform)
-        const char* qt = pk_smem + (j & 1) * (2 * TILE);
-        PkFrag pf[4], df[4];
-        if (low >= wkey + 31 && base + PK_T <= R) {
-            all_seen(j);
-            return;
-        }
-        scores(std::true_type(), j, pf, df);
-        if constexpr (careful) {
-            const int* limit = limits + (j & 1) * PK_T + 4 * hi;
-            PkFrag seen[4];
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int at = 16 * s + (w >> 1) * 8 + (w & 1) * 2;
-                    seen[s].w[w] = (wkey + (lane & 31) <= limit[at] ? 0x3F80u : 0u) | (wkey + (lane & 31) <= limit[at + 1] ? 0x3F800000u : 0u);
-                }
-            pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
-            pk_second_careful<HD, false>(qt, df, df, ak);
-        } else {
-            const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
-            pk_second<HD, 0, 4>(o, TILE, pf, av);
-            pk_second<HD, 0, 4>(o, 0, df, ak);
-        }
+        if (low >= wkey + 31 && base + PK_T <= R) tile(std::false_type(), j);
+        else tile(std::true_type(), j);
     };
 #pragma unroll
     for (int d = 0; d < DB; ++d) { pk_zero(ak[d]); pk_zero(av[d]); }
