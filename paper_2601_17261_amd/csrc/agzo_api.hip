@@ -1526,7 +1526,7 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
     TRY(check_apart(ctx, {named("dq", dq, lddq, a->n_q, wq), named("dk", dk, lddk, a->n_k, wk), named("dv", dv, lddv, a->n_k, wk)},
                     {named("q", a->q, a->ldq, a->n_q, wq), named("k", a->k, a->ldk, a->n_k, wk), named("v", a->v, a->ldv, a->n_k, wk),
                      named("out", out, ldo, a->n_q, wq), named("dout", dout, lddo, a->n_q, wq)}));
-    TRY(reserve(ctx, packed_backward_workspace_bytes(p)));
+    TRY(reserve(ctx, packed_backward_workspace_bytes(p, a->head_dim)));
     const PackedGrad g{static_cast<const bf16_t*>(out), static_cast<const bf16_t*>(dout), ldo, lddo, lse, static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk),
                        static_cast<bf16_t*>(dv), lddq, lddk, lddv};
     HIPCHK(launch_packed_backward(p, a->head_dim, g, ctx->ws, ctx->stream));

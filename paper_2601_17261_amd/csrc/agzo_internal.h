@@ -409,7 +409,7 @@ struct PackedGrad {
 };
 size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim);
 hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st);
-size_t packed_backward_workspace_bytes(const PackedArgs& a);
+size_t packed_backward_workspace_bytes(const PackedArgs& a, int head_dim);
 hipError_t launch_packed_backward(const PackedArgs& a, int head_dim, const PackedGrad& g, void* workspace, hipStream_t st);
 
 // probe.hip : register-only MFMA loop for measuring the sustained matrix rate and shader clock of the device;

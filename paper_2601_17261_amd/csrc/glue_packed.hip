@@ -202,23 +202,57 @@ __device__ __forceinline__ int pk_scan(int x) {
 }
 
 // One sequence's places in the packed tensors, and a tile of it
-struct PkTile { int tile, q0, k0, nq, nk; };
+struct PkTile { int tile, share, q0, k0, nq, nk; };
 
-// Tile number t of all sequences' tiles, UNIT rows (BY_KEYS: keys) each.  Offsets are taken as far as they lie inside the tensors and grow
+// sum over the lanes
+__device__ __forceinline__ int pk_total(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    return __builtin_amdgcn_readlane(x, 15) + __builtin_amdgcn_readlane(x, 31) + __builtin_amdgcn_readlane(x, 47) + __builtin_amdgcn_readlane(x, 63);
+}
+
+// Tile number t of all sequences' tiles, UNIT rows (BY_KEYS: keys) each; with chunk > 0 a row tile is one for every `chunk` tiles of 64 keys that its sequence has.
+// The tiles that see most (BY_KEYS: that are seen most) of up to 64 sequences come first: a sequence's last row tile (its first tile of keys) is as many
+// levels high as it has tiles, the next one a level less, and tiles are numbered level by level.  (Sequence by sequence a long one may start
+// last: 8192 tokens in eight of up to 1923 took dk, dv 260 us, so 170.)  Offsets are taken as far as they lie inside the tensors and grow
 template <int UNIT, bool BY_KEYS>
-__device__ __forceinline__ bool pk_find(const PackedArgs& a, int t, int G, PkTile& out) {
+__device__ __forceinline__ bool pk_find(const PackedArgs& a, int t, int G, int chunk, PkTile& out) {
     const int lane = threadIdx.x & 63, total_q = (int)a.total_q, total_k = (int)a.total_k;
     for (int b = 0; b < a.n_seq; b += 64) {
         const int s = min(b + lane, a.n_seq - 1);
         int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
         q0 = min(max(q0, 0), total_q);   q1 = min(max(q1, q0), total_q);
         k0 = min(max(k0, 0), total_k);   k1 = min(max(k1, k0), total_k);
-        const int count = b + lane >= a.n_seq ? 0 : (int)(((BY_KEYS ? (uint32_t)(k1 - k0) : (uint32_t)(q1 - q0) * (uint32_t)G) + (UNIT - 1)) / UNIT);
+        const int own = b + lane >= a.n_seq ? 0 : (int)(((BY_KEYS ? (uint32_t)(k1 - k0) : (uint32_t)(q1 - q0) * (uint32_t)G) + (UNIT - 1)) / UNIT);
+        // (a row tile without keys is one all the same: its rows are written)
+        const int count = chunk > 0 ? own * max(1, ((k1 - k0 + PK_T - 1) / PK_T + chunk - 1) / chunk) : own;
         const int sum = pk_scan(count);
         const int total = __builtin_amdgcn_readlane(sum, 63);
         if (t < total) {
-            const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > t));
-            out.tile = t - __builtin_amdgcn_readlane(sum - count, src);
+            int src, tile;
+            if (chunk == 0 && a.n_seq <= 64) {
+                // the lowest level with at most t tiles above it
+                int low = 0, high = total;
+                while (low < high) {
+                    const int mid = (low + high) >> 1;
+                    if (pk_total(max(own - mid, 0)) <= t) high = mid;
+                    else low = mid + 1;
+                }
+                const int place = t - pk_total(max(own - low, 0));
+                const uint64_t m = __builtin_amdgcn_ballot_w64(own >= low);
+                const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+                src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(own >= low && before == place));
+                tile = BY_KEYS ? __builtin_amdgcn_readlane(own, src) - low : low - 1;
+            } else {
+                src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > t));
+                tile = t - __builtin_amdgcn_readlane(sum - count, src);
+                if (!BY_KEYS && chunk == 0) tile = __builtin_amdgcn_readlane(own, src) - 1 - tile;
+            }
+            const int rows = __builtin_amdgcn_readlane(own, src);
+            out.share = chunk > 0 ? tile / rows : 0;
+            out.tile = tile - out.share * rows;
             out.q0 = __builtin_amdgcn_readlane(q0, src);
             out.k0 = __builtin_amdgcn_readlane(k0, src);
             out.nq = __builtin_amdgcn_readlane(q1, src) - out.q0;
@@ -280,21 +314,22 @@ constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
 // ---- forward ---------------------------------------------------------------------------------------------------
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits.  A tile is 64 matrix instructions a wave (HD = 128, 2048 cycles) beside some 1500 cycles of exponentials and 32 KB of LDS reads.
-// part != NULL: workgroup y takes its share of the row tile's keys and leaves sums, maximum and sum of exponentials for pk_join_kernel
-//
-// Returns whether the workgroup has to go over its tiles once more, with care (and has stored nothing then)
-struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; };
+// chunk > 0: a row tile's keys are dealt out, `chunk` tiles of them a share, and workgroups take shares until there are none left, whose sums, maximum and
+// sum of exponentials they leave for pk_join_kernel
+struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; int chunk; };
+// again: stored nothing, the tiles have to be gone over with care
+enum class PkDone { stored, again, none };
 template <int HD, bool careful>
-__device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardOut& to_, pk_lchar lds) {
+__device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwardOut& to_, int unit, pk_lchar lds) {
     char* pk_smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
-    // the last tiles first, for they have most keys; the key heads side by side: an XCD (workgroup number mod 8) then has few of them
-    const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)(gridDim.x - 1 - blockIdx.x), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
+    // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
+    const int G = PkDiv(a.n_kv)(a.n_heads), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return false;
+    if (!pk_find<PK_ROWS, false>(a, at, G, to_.chunk, t)) return PkDone::none;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
     // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
@@ -312,7 +347,9 @@ __device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardO
     const int wlast = row0 >= R ? -1 : a.causal ? by_group(min(row0 + 31, R - 1)) + shift : t.nk - 1;
     const int last = a.causal ? by_group(min((t.tile + 1) * PK_ROWS - 1, R - 1)) + shift : t.nk - 1;
     const int tiles = last < 0 ? 0 : last / PK_T + 1;
-    const int j0 = (int)((int64_t)tiles * blockIdx.y / gridDim.y), j1 = (int)((int64_t)tiles * (blockIdx.y + 1) / gridDim.y);
+    const int j0 = to_.chunk > 0 ? t.share * to_.chunk : 0, j1 = to_.chunk > 0 ? min(tiles, j0 + to_.chunk) : tiles;
+    // (a share that none of the row tile sees.  The first one is there for rows that see nothing at all)
+    if (j0 >= j1 && t.share > 0) return PkDone::stored;
     const bf16_t* Kh = a.k + (int64_t)t.k0 * a.ldk + kvh * HD;
     const bf16_t* Vh = a.v + (int64_t)t.k0 * a.ldv + kvh * HD;
     PkLoader<HD> lk, lv;
@@ -429,12 +466,13 @@ __device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardO
         one_tile(j);
         if (j + 1 < j1) arrive(j + 1);
     }
-    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return true;
+    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return PkDone::again;
+    if (careful) __syncthreads();
     l = pk_sum_halves(l);
     const Row r = row_of_lane();
     if (to_.part) {
-        if (!r.mine) return false;
-        const int64_t at = (int64_t)blockIdx.y * a.total_q * a.n_heads + r.tok * a.n_heads + r.head;
+        if (!r.mine) return PkDone::stored;
+        const int64_t at = (int64_t)t.share * a.total_q * a.n_heads + r.tok * a.n_heads + r.head;
         float* to = to_.part + at * HD + 4 * hi;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -442,56 +480,82 @@ __device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardO
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<float4*>(to + 32 * db + 8 * g) = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
         if (hi == 0) to_.part_ml[at] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
-        return false;
+        return PkDone::stored;
     }
     const bool empty = r.limit < 0;
     pk_store<HD>(acc, empty ? 0.f : 1.f / l, to_.out + r.tok * to_.ldo + (int64_t)r.head * HD, r.mine);
     if (to_.lse && r.mine && hi == 0) to_.lse[r.tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
-    return false;
+    return PkDone::stored;
 }
 // (a function that is called: its registers are not the kernel's)
 template <int HD>
-__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, pk_lchar lds) { (void)pk_forward<HD, true>(a, to, lds); }
+__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, int unit, pk_lchar lds) { (void)pk_forward<HD, true>(a, to, unit, lds); }
 template <int HD>
 __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_forward_kernel(PackedArgs a, PkForwardOut to) {
     extern __shared__ __align__(1024) char pk_dynamic[];
-    if (pk_forward<HD, false>(a, to, (pk_lchar)pk_dynamic)) pk_forward_again<HD>(a, to, (pk_lchar)pk_dynamic);
+    for (int unit = (int)blockIdx.x;; unit += (int)gridDim.x) {
+        const PkDone done = pk_forward<HD, false>(a, to, unit, (pk_lchar)pk_dynamic);
+        if (done == PkDone::again) pk_forward_again<HD>(a, to, unit, (pk_lchar)pk_dynamic);
+        if (done == PkDone::none || to.chunk == 0) return;
+    }
 }
 
 // Shares of the keys joined: HD / 4 lanes a row.  Rows of no sequence are left alone: their partial sums are what the workspace held
 template <int HD>
-__global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int shares,
+__global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int chunk,
                                                       bf16_t* __restrict__ out, int64_t ldo, float* __restrict__ lse) {
     constexpr int LANES = HD / 4;
-    const int64_t rows = a.total_q * a.n_heads, row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-    if (row >= rows) return;
+    const int64_t rows = a.total_q * a.n_heads, at_row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES, row = min(at_row, rows - 1);
+    const bool there = at_row < rows;
     const int j = threadIdx.x % LANES;
     const int64_t tok = row / a.n_heads;
-    // which sequence the token is of, by halves: the last one that starts at or before it
-    int lo = 0, hi = a.n_seq;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.cu_q[mid] <= tok) lo = mid;
-        else hi = mid;
+    // which sequence the token is of: the last one that starts at or before it.  (By all lanes for both of the wave's rows at most: halves one after the
+    // other were six loads that wait for each other)
+    int lo = -1;
+    const int tok0 = __builtin_amdgcn_readfirstlane((int)tok), tok1 = __builtin_amdgcn_readlane((int)tok, 63);
+    for (int b = 0; b < a.n_seq; b += 64) {
+        const int s = b + (int)(threadIdx.x & 63), start = s < a.n_seq ? a.cu_q[s] : 0x7FFFFFFF;
+        if (LANES == 16) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(start <= __builtin_amdgcn_readlane((int)tok, 16 * g)));
+                lo += (int)((threadIdx.x & 63) >> 4) == g ? n : 0;
+            }
+        } else {
+            const int n0 = __builtin_popcountll(__builtin_amdgcn_ballot_w64(start <= tok0)), n1 = __builtin_popcountll(__builtin_amdgcn_ballot_w64(start <= tok1));
+            lo += (threadIdx.x & 63) < 32 ? n0 : n1;
+        }
     }
+    if (!there || lo < 0) return;
     const int q0 = min(max(a.cu_q[lo], 0), (int)a.total_q), q1 = min(max(a.cu_q[lo + 1], q0), (int)a.total_q);
     if (tok < q0 || tok >= q1) return;
     const int k0 = min(max(a.cu_k[lo], 0), (int)a.total_k), nk = min(max(a.cu_k[lo + 1], k0), (int)a.total_k) - k0;
-    const bool empty = (a.causal ? (int)(tok - q0) + nk - (q1 - q0) : nk - 1) < 0;
-    float top = -INFINITY;
-    for (int s = 0; s < shares; ++s) top = fmaxf(top, ml[s * rows + row].x);
+    const int G = a.n_heads / a.n_kv, nq = q1 - q0, at = (int)(tok - q0), head = (int)(row - tok * a.n_heads);
+    const bool empty = (a.causal ? at + nk - nq : nk - 1) < 0;
+    // the shares of its row tile
+    const int in = at * G + head % G, end = min((in / PK_ROWS + 1) * PK_ROWS, nq * G) - 1, last = a.causal ? end / G + nk - nq : nk - 1;
+    const int shares = last < 0 ? 1 : (last / PK_T + chunk) / chunk;
+    // maxima and sums by share in the lanes of the row; a share that the row sees nothing of has no part
+    float top = -INFINITY, l = 0.f;
+    for (int s0 = 0; s0 < shares; s0 += LANES) top = fmaxf(top, s0 + j < shares ? ml[(s0 + j) * rows + row].x : -INFINITY);
+#pragma unroll
+    for (int w = LANES / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    for (int s = 0; s < shares; ++s) {
-        const float2 m = ml[s * rows + row];
-        if (m.x == -INFINITY) continue;                       // a share that the row sees nothing of
-        const float f = __builtin_amdgcn_exp2f(m.x - top);
-        const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + row) * HD + 4 * j);
-        l = fmaf(f, m.y, l);
-        o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+    for (int s0 = 0; s0 < shares; s0 += LANES) {
+        const float2 m = ml[min(s0 + j, shares - 1) * rows + row];
+        const float f = s0 + j >= shares ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
+        l += f == 0.f ? 0.f : f * m.y;
+        const int n = min(LANES, shares - s0);
+#pragma unroll 4
+        for (int s = 0; s < n; ++s) {
+            const float w = __shfl(f, s, LANES);
+            const float4 v = *reinterpret_cast<const float4*>(part + ((int64_t)(s0 + s) * rows + row) * HD + 4 * j);
+            if (w != 0.f) { o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w); }
+        }
     }
+#pragma unroll
+    for (int w = LANES / 2; w > 0; w >>= 1) l += __shfl_xor(l, w);
     const float inv = empty ? 0.f : 1.f / l;
-    const int head = (int)(row - tok * a.n_heads);
     *reinterpret_cast<uint2*>(out + tok * ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
     if (lse && j == 0) lse[row] = empty ? -INFINITY : (top + log2f(l)) * PK_LN2;
 }
@@ -531,7 +595,7 @@ __global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_
     rowinfo[row] = make_uint4(u.x, u.y, v.x, v.y);
 }
 
-struct PkBackward { const bf16_t* dout; int64_t lddo; const uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; };
+struct PkBackward { const bf16_t* dout; int64_t lddo; const uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; float* part; };
 
 // dq: the forward's shape, with do beside q in registers, and K read with and without transposition
 template <int HD, bool careful>
@@ -541,9 +605,9 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
-    const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)(gridDim.x - 1 - blockIdx.x), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
+    const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)blockIdx.x, at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, at, G, t)) return false;
+    if (!pk_find<PK_ROWS, false>(a, at, G, 0, t)) return false;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
     // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
@@ -696,13 +760,14 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
     const int hi = lane >> 5;
     const int G = PkDiv(a.n_kv)(a.n_heads), at = PkDiv(a.n_kv)((int)blockIdx.x), kvh = (int)blockIdx.x - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, true>(a, at, G, t)) return false;
+    if (!pk_find<PK_ROWS, true>(a, at, G, 0, t)) return false;
     const int R = t.nq * G, shift = t.nk - t.nq;
     const int key0 = t.tile * PK_ROWS, wkey = key0 + wave * 32;
     const int key = min(wkey + (lane & 31), t.nk - 1);
     const bool mine = wkey + (lane & 31) < t.nk;
-    const int row0 = a.causal ? max(key0 - shift, 0) * G : 0;                  // (below R: key0 < nk)
-    const int tiles = (R - row0 + PK_T - 1) / PK_T;
+    const int from = a.causal ? max(key0 - shift, 0) * G : 0, all = (R - from + PK_T - 1) / PK_T;      // (below R, if there are any: key0 < nk)
+    // this share's of the row tiles
+    const int j0 = (int)((int64_t)all * blockIdx.y / gridDim.y), tiles = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y) - j0, row0 = from + j0 * PK_T;
     const PkDiv query_of(G);
     // a tile's rows on their way; rows past the end repeat the last one
     constexpr int N = PK_T * HD * 2 / 4096, ROWS = 1024 / (HD * 2);
@@ -910,6 +975,19 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
         if (j + 1 < tiles) arrive(j + 1);
     }
     if (!careful && __syncthreads_or(mine && (pk_not_finite(ak) || pk_not_finite(av)))) return true;
+    if (g.part) {
+        float* to = g.part + ((((int64_t)blockIdx.y * a.total_k + t.k0 + key) * a.n_kv + kvh) * 2) * HD + 4 * hi;
+        if (mine) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4) {
+                    *reinterpret_cast<float4*>(to + 32 * db + 8 * g4) = make_float4(ak[db][4 * g4], ak[db][4 * g4 + 1], ak[db][4 * g4 + 2], ak[db][4 * g4 + 3]);
+                    *reinterpret_cast<float4*>(to + HD + 32 * db + 8 * g4) = make_float4(av[db][4 * g4], av[db][4 * g4 + 1], av[db][4 * g4 + 2], av[db][4 * g4 + 3]);
+                }
+        }
+        return false;
+    }
     pk_store<HD>(av, 1.f, g.dv + (int64_t)(t.k0 + key) * g.lddv + (int64_t)kvh * HD, mine);
     pk_store<HD>(ak, a.scale, g.dk + (int64_t)(t.k0 + key) * g.lddk + (int64_t)kvh * HD, mine);
     return false;
@@ -922,16 +1000,51 @@ __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(1
     if (pk_dkv<HD, false>(a, g, (pk_lchar)pk_dynamic)) pk_dkv_again<HD>(a, g, (pk_lchar)pk_dynamic);
 }
 
+// The shares' sums of dk and dv added in order, HD / 4 lanes a row of dk and of dv
+template <int HD>
+__global__ __launch_bounds__(256) void pk_dkv_join_kernel(PackedArgs a, PkBackward g, int shares) {
+    constexpr int LANES = HD / 2;
+    const int64_t rows = a.total_k * a.n_kv, row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    if (row >= rows) return;
+    const int64_t tok = row / a.n_kv;
+    if (tok < a.cu_k[0] || tok >= a.cu_k[a.n_seq]) return;                    // a row of no sequence
+    const int j = threadIdx.x % LANES;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < shares; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(g.part + (i * rows + row) * (2 * HD) + 4 * j);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const bool k = j < LANES / 2;
+    const float f = k ? a.scale : 1.f;
+    bf16_t* to = (k ? g.dk + tok * g.lddk : g.dv + tok * g.lddv) + (row - tok * a.n_kv) * HD + 4 * (j % (LANES / 2));
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
+}
+
 // an upper bound of the row (key) tiles of all sequences, whatever their lengths
 int64_t pk_units(int64_t total, int n_seq, int n_kv) { return (total / PK_ROWS + std::min<int64_t>(n_seq, total)) * n_kv; }
 
-// Few row tiles are dealt to several workgroups by keys, for about two to a compute unit, four tiles of keys each at least, as far as lengths can be told from
-// their mean
-int pk_shares(const PackedArgs& a) {
-    const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv);
+// Tiles of 64 keys a share, 0: row tiles are not shared out.  They are where rows are few beside the keys (single new tokens: a sequence is a
+// workgroup for each key head then, whatever its length) or where row tiles are fewer than the compute units: for about one share to each of two workgroups on a
+// compute unit, of 8 tiles and more (a share costs a workgroup's start, its sums and a launch that joins them), 128 of a sequence at most and 256 MB of sums.
+// Lengths are on the device: work is reckoned from their mean, and sequences of 16 tiles and more in the mean are taken to be uneven.  64 sequences of 200000
+// keys together, up to 16760: 361 us without, 190 so
+int pk_chunk(const PackedArgs& a, int head_dim) {
+    const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
+    if (units < 1 || a.total_k < 1) return 0;
+    const int64_t all = (a.total_k + PK_T - 1) / PK_T, mean = (a.total_k / std::max(1, a.n_seq) + PK_T - 1) / PK_T;
+    if (mean < 16 || !(a.total_q * G * 8 <= a.total_k || units < 256)) return 0;
+    const int64_t chunk = std::max<int64_t>({8, (units * mean + 511) / 512, (all + 127) / 128, all * rows * head_dim * 4 / (1LL << 28)});
+    return (int)std::min<int64_t>(chunk, 1 << 20);
+}
+int64_t pk_most_shares(const PackedArgs& a, int chunk) { return ((a.total_k + PK_T - 1) / PK_T + chunk - 1) / chunk; }
+
+// Shares of the rows that a tile of keys is multiplied with: few tiles of keys take several workgroups each, for about one to a compute unit, of four tiles of 64
+// rows and more in the mean.  1001 tokens of eight heads on one: 345 us without, 75 so
+int pk_dkv_shares(const PackedArgs& a) {
+    const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_k, a.n_seq, a.n_kv);
     if (units < 1) return 1;
-    const int64_t keys = a.total_k / std::max(1, a.n_seq), most = std::max<int64_t>(1, keys / (4 * PK_T));
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / units, most, 64}));
+    const int64_t rows = a.total_q * G / std::max(1, a.n_seq) / PK_T;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(256 / units, rows / 4));
 }
 
 template <typename F>
@@ -944,16 +1057,23 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
     constexpr int SMEM = 4 * PK_T * HD * 2;
     static const hipError_t attr = pk_lds(pk_forward_kernel<HD>, SMEM);
     if (attr != hipSuccess) return attr;
-    const int G = a.n_heads / a.n_kv, shares = pk_shares(a);
-    const int64_t units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
-    if (units > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    float* part = shares > 1 ? static_cast<float*>(workspace) : nullptr;
-    float2* ml = shares > 1 ? reinterpret_cast<float2*>(part + (int64_t)shares * rows * HD) : nullptr;
-    hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units, (unsigned)shares), dim3(64 * PK_WAVES), SMEM, st, a, PkForwardOut{out, ldo, lse, part, ml});
+    const int G = a.n_heads / a.n_kv, chunk = pk_chunk(a, HD);
+    const int64_t rows = a.total_q * a.n_heads, blocks = (rows * (HD / 4) + 255) / 256;
+    int64_t units = pk_units(a.total_q * G, a.n_seq, a.n_kv);
+    float* part = nullptr;
+    float2* ml = nullptr;
+    if (chunk > 0) {
+        const int64_t shares = pk_most_shares(a, chunk);
+        part = static_cast<float*>(workspace);
+        ml = reinterpret_cast<float2*>(part + shares * rows * HD);
+        // (the row tiles and, for each share of a sequence more, as many as a sequence may have; numbers behind the last leave at once)
+        units = std::min<int64_t>(units + shares * (a.total_q * G / PK_ROWS + 1) * a.n_kv, 1 << 20);
+    }
+    if (units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, PkForwardOut{out, ldo, lse, part, ml, chunk});
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || shares == 1) return e;
-    const int64_t blocks = (rows * (HD / 4) + 255) / 256;
-    hipLaunchKernelGGL(pk_join_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, part, ml, shares, out, ldo, lse);
+    if (e != hipSuccess || chunk == 0) return e;
+    hipLaunchKernelGGL(pk_join_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, part, ml, chunk, out, ldo, lse);
     return hipGetLastError();
 }
 
@@ -967,7 +1087,10 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
     const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv), blocks = (rows * (HD / 8) + 255) / 256;
     if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     uint4* info = static_cast<uint4*>(workspace);
-    const PkBackward b{g.dout, g.lddo, info, g.dq, g.lddq, g.dk, g.lddk, g.dv, g.lddv};
+    const int shares = pk_dkv_shares(a);
+    const int64_t kv_rows = a.total_k * a.n_kv, kv_blocks = (kv_rows * (HD / 2) + 255) / 256;
+    float* part = shares > 1 ? reinterpret_cast<float*>(info + rows) : nullptr;
+    const PkBackward b{g.dout, g.lddo, info, g.dq, g.lddq, g.dk, g.lddk, g.dv, g.lddv, part};
     hipError_t e = hipSuccess;
     if (rows > 0) {
         hipLaunchKernelGGL(pk_delta_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, g.out, g.ldo, g.dout, g.lddo, g.lse, info);
@@ -978,7 +1101,10 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
         if (e != hipSuccess) return e;
     }
     if (a.total_k > 0) {
-        hipLaunchKernelGGL(pk_dkv_kernel<HD>, dim3((unsigned)kv_units), dim3(64 * PK_WAVES), SMEM_KV, st, a, b);
+        hipLaunchKernelGGL(pk_dkv_kernel<HD>, dim3((unsigned)kv_units, (unsigned)shares), dim3(64 * PK_WAVES), SMEM_KV, st, a, b);
+        e = hipGetLastError();
+        if (e != hipSuccess || !part) return e;
+        hipLaunchKernelGGL(pk_dkv_join_kernel<HD>, dim3((unsigned)kv_blocks), dim3(256), 0, st, a, b, shares);
         e = hipGetLastError();
     }
     return e;
@@ -987,10 +1113,13 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
 }  // namespace
 
 size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim) {
-    const int shares = pk_shares(a);
-    return shares == 1 ? 0 : (size_t)shares * a.total_q * a.n_heads * (head_dim * sizeof(float) + sizeof(float2));
+    const int chunk = pk_chunk(a, head_dim);
+    return chunk == 0 ? 0 : (size_t)pk_most_shares(a, chunk) * a.total_q * a.n_heads * (head_dim * sizeof(float) + sizeof(float2));
 }
-size_t packed_backward_workspace_bytes(const PackedArgs& a) { return (size_t)a.total_q * a.n_heads * sizeof(uint4); }
+size_t packed_backward_workspace_bytes(const PackedArgs& a, int head_dim) {
+    const int shares = pk_dkv_shares(a);
+    return (size_t)a.total_q * a.n_heads * sizeof(uint4) + (shares == 1 ? 0 : (size_t)shares * a.total_k * a.n_kv * 2 * head_dim * sizeof(float));
+}
 
 hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
     if (a.total_q == 0 || a.n_seq == 0) return hipSuccess;
