@@ -595,7 +595,7 @@ __global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_
     rowinfo[row] = make_uint4(u.x, u.y, v.x, v.y);
 }
 
-struct PkBackward { const bf16_t* dout; int64_t lddo; const uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; float* part; };
+struct PkBackward { const bf16_t* dout; int64_t lddo; uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; float* part; };
 
 // dq: the forward's shape, with do beside q in registers, and K read with and without transposition
 template <int HD, bool careful>
@@ -725,6 +725,39 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
     for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
     begin();
     if (tiles > 0) arrive(0);
+    // Delta of rows that see one tile of keys at most, exactly: with out's and the probabilities' roundings in it the differences do - delta of few keys are off by
+    // 2^-8 of themselves (dq of sequences of some five tokens by 0.0045 of its norm, so by 0.0025), and here it is 32 instructions more.  For dk and dv too, and
+    // for a pass with care, which reads it
+    if (!careful && tiles == 1) {
+        __syncthreads();
+        if (wlast >= 0) {
+            const PkOffsets<HD> o(off, lds_at);
+            const int rel = limit_of() - 4 * hi;
+            float rest = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                pk_floatx16 s = {}, dp = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    PkFrag kf, vf;
+                    kf.v = o.row(h, ks);
+                    vf.v = o.row(h, ks, TILE);
+                    s = pk_mfma(kf, qf[ks], s);
+                    dp = pk_mfma(vf, df[ks], dp);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) rest += 32 * h + pk_pos(e) <= rel ? __builtin_amdgcn_exp2f(fmaf(s[e], sc, -info.x)) * (dp[e] - info.y) : 0.f;
+            }
+            rest = pk_sum_halves(rest);
+            info.y += rest;
+            const Row r = row_of_lane();
+            if (r.mine && hi == 0 && r.limit >= 0) {
+                const uint2 v = pk_split3(-info.y);
+                uint2* to = reinterpret_cast<uint2*>(g.rowinfo + r.tok * a.n_heads + r.head) + 1;
+                *to = v;
+            }
+        }
+    }
     for (int j = 0; j < tiles; ++j) {
         __syncthreads();
         if (j + 1 < tiles) request(j + 1);
