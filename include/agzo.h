@@ -324,7 +324,8 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
 /* Token cross-entropy of a layer's outputs and its gradient (an LM head: d_out outputs; the layer's r, y_dtype and ldy are not used), without
  * the logits ever being stored.  loss: kind AGZO_LOSS_CE, target ids [n_tokens]; rows whose id is not in [0, d_out) are not counted.
  *   ce_forward: *loss_dev = mean over the counted rows of lse_t - y_t[id] (0 if there are none) and, where wanted, lse [n_tokens] device fp32,
- *     lse_t = log sum exp of row t's logits, of every row.  bf16 and fp32 layers; the loss is agzo_layer_forward_sketch's, bit for bit.
+ *     lse_t = log sum exp of row t's logits, of every row.  bf16 and fp32 layers; the loss is agzo_layer_forward_sketch's, bit for
+ *     bit for fp32 layers and from 33 tokens on (fewer have sums of their own order).
  *   ce_backward (bf16 layers): with D = (softmax(Y) - onehot(id)) g / count in the counted rows, 0 in the others, dX = D W [n_tokens][d_in]
  *     and dW = D^T X [d_out][d_in], bf16, overwritten; either may be NULL.  lse: of ce_forward with the same arguments; g = *g_dev (1 if NULL).  The
  *     logits are made again for a piece of the outputs at a time, D is rounded to bf16 for the products, sums are fp32, in an order that

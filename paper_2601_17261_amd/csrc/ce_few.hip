@@ -1,0 +1,382 @@
+// Token cross-entropy of a layer's outputs, and its gradient, for few tokens (answers that are scored, a short sentence): what counts is that W is read, and dW
+// written, at the rate of memory.  Products are v_mfma_f32_32x32x16_bf16 with W's rows or dims as the instruction's rows and the tokens as its columns.
+//
+// Logits, up to 32 tokens: a workgroup has 32 outputs, its four waves every fourth 256 bytes of their rows, requested a round ahead straight into registers in the
+// layout of the instruction: whole lines, 8 KB a wave, and nothing that a wave waits for another with until the four sums meet in LDS.
+// 7 tokens, 2048 -> 32000 (131 MB): 30 us, and the 256 x 256 tiles of gemm_bf16_aligned.hip 54.  Two blocks of tokens leave room for one wave a SIMD:
+// 40 tokens, 1024 -> 50000: 52 us, the tiles 38; so more tokens go to the tiles.
+#include "gemm_bf16_common.h"
+
+namespace agzo {
+
+namespace {
+
+union FewFrag { uint4 u; uint2 h[2]; bf16x8 v; };
+constexpr int FEW_OUT = 32, FEW_K = 128;                 // outputs of a workgroup, values of a row that a wave reads at a time
+constexpr float FEW_LOG2E = 1.44269504088896341f;
+
+__device__ __forceinline__ uint4 few_load(__amdgpu_buffer_rsrc_t r, int off) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rsrc(const bf16_t* base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, (int)(uint32_t)kPastEnd, 0x00020000);
+}
+
+struct FewArgs {
+    const bf16_t* X; int64_t ldx;
+    const bf16_t* W; int64_t ldw;
+    int M; int64_t V, d;
+    const int32_t* ids;
+    // statistics of 32 outputs each, [token][outputs / 32], and the targets' logits
+    float2* ms; float* tl; int64_t nch;
+    // gradient: D [M][ldd], D^T [V][32]
+    const float* lse; const double* g; bf16_t* D; int64_t ldd; bf16_t* Dt;
+};
+
+template <bool GRAD>
+__global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
+    __shared__ float red[4][FEW_OUT][33];
+    __shared__ float2 part[8][32];
+    __shared__ __align__(16) bf16_t tile[GRAD ? FEW_OUT : 1][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
+    const int64_t out0 = (int64_t)blockIdx.x * FEW_OUT;
+    const int left = (int)min((int64_t)FEW_OUT, a.V - out0);
+    const auto rw = few_rsrc(a.W + out0 * a.ldw), rx = few_rsrc(a.X);
+    // (outputs and tokens past the end repeat the last ones, uncounted)
+    const int woff = min(r, left - 1) * (int)(2 * a.ldw) + 16 * hi, xoff = min(r, a.M - 1) * (int)(2 * a.ldx) + 16 * hi;
+    const int nchunk = (int)((a.d + FEW_K - 1) / FEW_K);
+    FewFrag w0[8], x0[8], w1[8], x1[8];
+    auto load = [&](int c, FewFrag (&w)[8], FewFrag (&x)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int at = c * (2 * FEW_K) + 32 * s;
+            const bool in = c * FEW_K + 16 * s + 8 * hi < (int)a.d;            // (past the row: zeros)
+            w[s].u = few_load(rw, in ? woff + at : kPastEnd);
+            x[s].u = few_load(rx, in ? xoff + at : kPastEnd);
+        }
+    };
+    floatx16 acc = {};
+    auto multiply = [&](const FewFrag (&w)[8], const FewFrag (&x)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[s].v, x[s].v, acc, 0, 0, 0);
+    };
+    if (wave < nchunk) load(wave, w0, x0);
+    for (int c = wave; c < nchunk; c += 8) {
+        if (c + 4 < nchunk) load(c + 4, w1, x1);
+        multiply(w0, x0);
+        if (c + 4 >= nchunk) break;
+        if (c + 8 < nchunk) load(c + 8, w0, x0);
+        multiply(w1, x1);
+    }
+    // a lane's sums: token r, outputs 8 (e / 4) + 4 hi + e % 4
+#pragma unroll
+    for (int e = 0; e < 16; ++e) red[wave][8 * (e >> 2) + 4 * hi + (e & 3)][r] = acc[e];
+    float f = 0.f;
+    if (GRAD) {
+        if (tid < FEW_OUT * 4) reinterpret_cast<uint4*>(&tile[0][0])[tid] = make_uint4(0, 0, 0, 0);
+        const int id = lane < a.M ? a.ids[lane] : -1;
+        const int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(id >= 0 && id < a.V));
+        f = (float)((a.g ? *a.g : 1.0) / (double)max(count, 1));
+    }
+    __syncthreads();
+    // four outputs of a token a thread
+    const int grp = tid >> 5, tok = tid & 31;
+    float y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) y[u] = (red[0][4 * grp + u][tok] + red[1][4 * grp + u][tok]) + (red[2][4 * grp + u][tok] + red[3][4 * grp + u][tok]);
+    const int64_t id = tok < a.M ? a.ids[tok] : -1;
+    if (!GRAD) {
+        float mx = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (4 * grp + u < left) {
+                mx = fmaxf(mx, y[u]);
+                if (out0 + 4 * grp + u == id) a.tl[tok] = y[u];
+            }
+        // (a NaN among them stays in the sum)
+        const float m0 = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (4 * grp + u < left) s += __builtin_amdgcn_exp2f((y[u] - m0) * FEW_LOG2E);
+        part[grp][tok] = make_float2(mx, s);
+    } else {
+        const bool counted = id >= 0 && id < a.V;
+        const float l = tok < a.M ? a.lse[tok] : 0.f;
+        float v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float p = __builtin_amdgcn_exp2f((y[u] - l) * FEW_LOG2E);
+            v[u] = counted && 4 * grp + u < left ? (out0 + 4 * grp + u == id ? p - 1.f : p) * f : 0.f;
+        }
+        const uint2 two = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        if (tok < a.M) {
+            *reinterpret_cast<uint2*>(a.D + tok * a.ldd + out0 + 4 * grp) = two;
+            tile[4 * grp][tok] = (bf16_t)two.x; tile[4 * grp + 1][tok] = (bf16_t)(two.x >> 16);
+            tile[4 * grp + 2][tok] = (bf16_t)two.y; tile[4 * grp + 3][tok] = (bf16_t)(two.y >> 16);
+        }
+    }
+    __syncthreads();
+    if (GRAD) {
+        if (a.Dt && tid < 4 * left) *reinterpret_cast<uint4*>(a.Dt + out0 * 32 + tid * 8) = reinterpret_cast<const uint4*>(&tile[0][0])[tid];
+        return;
+    }
+    if (tid >= a.M) return;
+    float mx = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int g8 = 0; g8 < 8; ++g8) mx = fmaxf(mx, part[g8][tid].x);
+#pragma unroll
+    for (int g8 = 0; g8 < 8; ++g8) {
+        const float2 p = part[g8][tid];
+        s += p.y == 0.f ? 0.f : p.y * __builtin_amdgcn_exp2f((p.x - (mx == -INFINITY ? 0.f : mx)) * FEW_LOG2E);
+    }
+    a.ms[tid * a.nch + blockIdx.x] = make_float2(mx, s);
+}
+
+// Loss and lse from the statistics, in one workgroup: a wave a token, sums in fp64
+__global__ __launch_bounds__(1024) void ce_few_finish_kernel(const float2* __restrict__ ms, const float* __restrict__ tl, const int32_t* __restrict__ ids, int M, int64_t V, int64_t nch,
+                                                             float* __restrict__ lse, double* __restrict__ out) {
+    __shared__ double sum[16], count[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double loss = 0.0, n = 0.0;
+    for (int t = wave; t < M; t += 16) {
+        const float2* m = ms + t * nch;
+        double mx = -INFINITY, s = 0.0;
+        for (int64_t c0 = lane; c0 < nch; c0 += 64 * 8) {
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = m[min(c0 + 64 * u, nch - 1)];
+            float top = v[0].x;
+#pragma unroll
+            for (int u = 1; u < 8; ++u) top = c0 + 64 * u < nch ? fmaxf(top, v[u].x) : top;
+            const double mn = fmax(mx, (double)top);
+            s = s > 0.0 ? s * exp(mx - mn) : s;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (c0 + 64 * u < nch && v[u].y != 0.f) s += (double)v[u].y * exp((double)v[u].x - mn);
+            mx = mn;
+        }
+        double top = mx;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) top = fmax(top, __shfl_xor(top, off));
+        s = s == 0.0 ? 0.0 : s * exp(mx - top);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+        const double l = log(s) + top;
+        const int id = ids[t];
+        if (lse && lane == 0) lse[t] = (float)l;
+        if (id >= 0 && id < V) {
+            loss += l - (double)tl[t];
+            n += 1.0;
+        }
+    }
+    if (lane == 0) { sum[wave] = loss; count[wave] = n; }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 16; ++w) { loss += sum[w]; n += count[w]; }
+    *out = n > 0.0 ? loss / n : 0.0;
+}
+
+// A tile of 32 rows of 128 values, for a wave or a workgroup, which is read transposed: a lane gets four rows' values of a column with each read
+typedef __bf16 few_bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) few_bf16x4* few_trptr;
+// 16 bytes c of row i lie at place c ^ few_swz(i): no two rows that a write or a read touches at once share banks
+__device__ __forceinline__ int few_swz(int i) { return ((i & 3) << 2) | ((i >> 2) & 3); }
+struct FewTrans {
+    int at[2];
+    __device__ __forceinline__ explicit FewTrans(int lane) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int n16 = lane & 15, tr = 8 * s + 4 * (lane >> 5) + (n16 >> 2), c = 2 * ((lane >> 4) & 1) + ((n16 & 3) >> 1);
+            at[s] = tr * 256 + ((c ^ few_swz(tr)) << 4) + (n16 & 1) * 8;
+        }
+    }
+    // columns 32 b .. 32 b + 31 as the instruction's rows; contracted rows 16 s + 4 hi .. + 3 and 16 s + 8 + 4 hi .. + 3
+    __device__ __forceinline__ FewFrag read(const char* tile, int s, int b) const {
+        union { few_bf16x4 v; uint2 u; } lo, up;
+        lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((few_trptr)(tile + s * 4096 + (at[0] ^ (b << 6))));
+        up.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((few_trptr)(tile + s * 4096 + (at[1] ^ (b << 6))));
+        FewFrag f;
+        f.h[0] = lo.u;
+        f.h[1] = up.u;
+        return f;
+    }
+};
+// the other operand, its columns' rows in that order
+__device__ __forceinline__ FewFrag few_order(const bf16_t* row, int s) {
+    FewFrag f;
+    f.h[0] = *reinterpret_cast<const uint2*>(row + 16 * s);
+    f.h[1] = *reinterpret_cast<const uint2*>(row + 16 * s + 8);
+    return f;
+}
+
+// dX = D W for up to 255 tokens, or for rows too short for a tile's 256: a workgroup has 128 dims, 32 TB tokens and a share of the outputs, its waves 32 outputs in
+// turn.  Rows of W go through LDS, a wave's own 8 KB, so that no wave waits for another and no transposed copy of W is made; D's values straight from memory.
+// sums [shares][M][d], added to if this is not the first piece of the outputs.  7 tokens, 2048 <- 32000: 22 us (5.9 TB/s: W lies in the last cache by then);
+// a transposed copy and a product of it 51 and 340.  200 tokens, four blocks that read W each: 102, and 51 and 347
+template <int TB>
+__global__ __launch_bounds__(256) void ce_few_dx_kernel(const bf16_t* __restrict__ D, int64_t ldd, const bf16_t* __restrict__ W, int64_t ldw, int64_t M, int64_t n, int64_t d, bool add,
+                                                        float* __restrict__ sums) {
+    __shared__ __align__(1024) char stage[4][32 * 256];
+    __shared__ float red[4][32][33];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
+    const int64_t d0 = (int64_t)blockIdx.x * 128, m0 = (int64_t)blockIdx.z * (32 * TB);
+    const int64_t blocks = (n + 31) / 32;
+    char* own = stage[wave];
+    const FewTrans trans(lane);
+    uint4 data[8];
+    auto load = [&](int64_t b) __attribute__((always_inline)) {
+        const auto rs = few_rsrc(W + b * 32 * ldw + d0);
+        const int left = (int)min((int64_t)32, n - b * 32);
+        // (rows past the end repeat the last one: their D is 0)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int row = 4 * q + (lane >> 4), chunk = (lane & 15) ^ few_swz(row);
+            data[q] = few_load(rs, d0 + 8 * chunk < d ? min(row, left - 1) * (int)(2 * ldw) + 16 * chunk : kPastEnd);
+        }
+    };
+    const bf16_t* drow[TB];
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb) drow[tb] = D + min(m0 + 32 * tb + r, M - 1) * ldd + 4 * hi;
+    floatx16 acc[TB][4] = {};
+    const int64_t first = (int64_t)blockIdx.y * 4 + wave, step = (int64_t)gridDim.y * 4;
+    if (first < blocks) load(first);
+    for (int64_t b = first; b < blocks; b += step) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(own + q * 1024 + lane * 16) = data[q];
+        FewFrag x[TB][2];
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) x[tb][s] = few_order(drow[tb] + b * 32, s);
+        if (b + step < blocks) load(b + step);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                const FewFrag w = trans.read(own, s, db);
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb) acc[tb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.v, x[tb][s].v, acc[tb][db], 0, 0, 0);
+            }
+    }
+    // the waves' sums, 32 dims of 32 tokens at a time
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) red[wave][8 * (e >> 2) + 4 * hi + (e & 3)][r] = acc[tb][db][e];
+            __syncthreads();
+            const int dim = tid & 31;
+            if (d0 + 32 * db + dim < d)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int c = (tid >> 5) + 8 * u;
+                    const int64_t tok = m0 + 32 * tb + c;
+                    if (tok >= M) continue;
+                    float* to = sums + (blockIdx.y * M + tok) * d + d0 + 32 * db + dim;
+                    const float s = (red[0][dim][c] + red[1][dim][c]) + (red[2][dim][c] + red[3][dim][c]);
+                    *to = add ? *to + s : s;
+                }
+        }
+}
+
+// dW = D^T X for up to 32 tokens: a workgroup has 128 dims, whose X lies in LDS (rows that are not counted as zeros: D is 0 there, and a value that is not finite
+// would make NaNs of it) and in registers from there, and its waves take 32 outputs in turn.  Bound by what it writes.  7 tokens, 2048 x 32000: 27 us (4.8 TB/s), a product of X transposed 72
+__global__ __launch_bounds__(256) void ce_few_dw_kernel(const bf16_t* __restrict__ Dt, const bf16_t* __restrict__ X, int64_t ldx, int M, int64_t V, int64_t d, const int32_t* __restrict__ ids,
+                                                        bf16_t* __restrict__ dW, int64_t lddw) {
+    __shared__ __align__(1024) char xs[32 * 256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
+    const int64_t d0 = (int64_t)blockIdx.x * 128, blocks = (V + 31) / 32;
+    for (int i = tid; i < 32 * 16; i += 256) {
+        const int row = i >> 4, c = i & 15, id = row < M ? ids[row] : -1;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (id >= 0 && id < V && d0 + 8 * c < d) v = *reinterpret_cast<const uint4*>(X + row * ldx + d0 + 8 * c);
+        *reinterpret_cast<uint4*>(xs + row * 256 + ((c ^ few_swz(row)) << 4)) = v;
+    }
+    __syncthreads();
+    const FewTrans trans(lane);
+    FewFrag x[2][4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) x[s][db] = trans.read(xs, s, db);
+    for (int64_t b = (int64_t)blockIdx.y * 4 + wave; b < blocks; b += (int64_t)gridDim.y * 4) {
+        const int64_t out = b * 32 + r;
+        const bf16_t* row = Dt + min(out, V - 1) * 32 + 4 * hi;
+        const FewFrag t0 = few_order(row, 0), t1 = few_order(row, 1);
+        bf16_t* to = dW + out * lddw + d0 + 8 * hi;
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+            floatx16 acc = {};
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0][db].v, t0.v, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1][db].v, t1.v, acc, 0, 0, 0);
+            // dims 16 h + 8 hi .. + 7 after the halves have changed places
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t a0 = pack_bf16x2(acc[8 * h], acc[8 * h + 1]), a1 = pack_bf16x2(acc[8 * h + 2], acc[8 * h + 3]);
+                const uint32_t b0 = pack_bf16x2(acc[8 * h + 4], acc[8 * h + 5]), b1 = pack_bf16x2(acc[8 * h + 6], acc[8 * h + 7]);
+                const auto p = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), q = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+                if (out < V && d0 + 32 * db + 16 * h + 8 * hi < d) *reinterpret_cast<uint4*>(to + 32 * db + 16 * h) = make_uint4(p[0], q[0], p[1], q[1]);
+            }
+        }
+    }
+}
+
+FewArgs few_args(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids) {
+    FewArgs a{};
+    a.X = X; a.ldx = ldx; a.W = W; a.ldw = ldw; a.M = (int)M; a.V = V; a.d = d; a.ids = ids;
+    return a;
+}
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+size_t ce_few_workspace_bytes(int64_t M, int64_t V) { return up256((size_t)((V + FEW_OUT - 1) / FEW_OUT) * M * sizeof(float2)) + up256((size_t)M * 4); }
+
+hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, float* lse, double* out, void* workspace, hipStream_t st) {
+    if (M < 1 || M > kCeFewTokens) return hipErrorInvalidValue;
+    FewArgs a = few_args(X, ldx, W, ldw, M, V, d, ids);
+    a.nch = (V + FEW_OUT - 1) / FEW_OUT;
+    char* ws = static_cast<char*>(workspace);
+    a.ms = reinterpret_cast<float2*>(ws);
+    a.tl = reinterpret_cast<float*>(ws + up256((size_t)a.nch * M * sizeof(float2)));
+    hipLaunchKernelGGL(ce_few_kernel<false>, dim3((unsigned)a.nch), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(ce_few_finish_kernel, dim3(1), dim3(1024), 0, st, a.ms, a.tl, ids, (int)M, V, a.nch, lse, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_ce_few_d(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, const float* lse, const double* g,
+                           bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st) {
+    if (M < 1 || M > kCeFewTokens || ldd < (V + 31) / 32 * 32 || ldd % 4) return hipErrorInvalidValue;
+    FewArgs a = few_args(X, ldx, W, ldw, M, V, d, ids);
+    a.lse = lse; a.g = g; a.D = D; a.ldd = ldd; a.Dt = Dt;
+    hipLaunchKernelGGL(ce_few_kernel<true>, dim3((unsigned)((V + FEW_OUT - 1) / FEW_OUT)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+// for two workgroups to a compute unit, of eight blocks of 32 outputs to a wave at least
+int ce_few_dx_shares(int64_t M, int64_t n, int64_t d) {
+    const int64_t tiles = (d + 127) / 128 * ((M + 63) / 64), blocks = (n + 31) / 32;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, blocks / 32, 64}));
+}
+
+hipError_t launch_ce_few_dx(const bf16_t* D, int64_t ldd, const bf16_t* W, int64_t ldw, int64_t M, int64_t n, int64_t d, int shares, bool add, float* sums, hipStream_t st) {
+    if (M < 1 || shares < 1 || ldd < (n + 31) / 32 * 32 || ldd % 4) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((d + 127) / 128), (unsigned)shares, (unsigned)((M + 63) / 64));
+    if (M <= 32) hipLaunchKernelGGL(ce_few_dx_kernel<1>, grid, dim3(256), 0, st, D, ldd, W, ldw, M, n, d, add, sums);
+    else hipLaunchKernelGGL(ce_few_dx_kernel<2>, grid, dim3(256), 0, st, D, ldd, W, ldw, M, n, d, add, sums);
+    return hipGetLastError();
+}
+
+hipError_t launch_ce_few_dw(const bf16_t* Dt, const bf16_t* X, int64_t ldx, int64_t M, int64_t V, int64_t d, const int32_t* ids, bf16_t* dW, int64_t lddw, hipStream_t st) {
+    if (M < 1 || M > kCeFewTokens) return hipErrorInvalidValue;
+    const int64_t slices = (d + 127) / 128, groups = (V + 127) / 128;
+    // eight workgroups to a compute unit, no more: each has to read X first
+    const dim3 grid((unsigned)slices, (unsigned)std::max<int64_t>(1, std::min(groups, 2048 / slices)));
+    hipLaunchKernelGGL(ce_few_dw_kernel, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, V, d, ids, dW, lddw);
+    return hipGetLastError();
+}
+
+}  // namespace agzo

@@ -3,7 +3,8 @@
 // The logits are made once more, for a piece of the outputs at a time, and only D of that piece is stored, as bf16, in both orders: the
 // products contract over outputs and over tokens, and the forward's kernels want the contracted dimension side by side.  So W's piece and X are
 // transposed too.  The products are those of gemm_bf16_aligned.hip where a 256 x 256 tile fits: D leaves the logits' product in both orders, and dX is
-// summed over the pieces in fp32, in shares of a piece where its tiles alone would not fill the chip.  Other shapes go through fp32 logits and the forward's kernels.
+// summed over the pieces in fp32, in shares of a piece where its tiles alone would not fill the chip.  Other shapes go through fp32 logits and
+// the forward's kernels, their dX and all of the gradient of few tokens through those of ce_few.hip, which copy nothing transposed.
 // This file: everything around the products.
 #include "gemm_bf16_common.h"
 
@@ -98,22 +99,18 @@ __global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __res
     }
 }
 
-// sum += part
-__global__ __launch_bounds__(256) void ce_add_kernel(const float* __restrict__ part, float* __restrict__ sum, int64_t n) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    const float4 a = *reinterpret_cast<const float4*>(part + i), b = *reinterpret_cast<const float4*>(sum + i);
-    *reinterpret_cast<float4*>(sum + i) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
-}
-
 // dX: the shares' sums [shares][M][d] added in order, as bf16
 __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, int shares, int64_t M, int64_t d, bf16_t* __restrict__ out, int64_t ldo) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
     if (i >= M * d) return;
     float4 s = *reinterpret_cast<const float4*>(sums + i);
-    for (int k = 1; k < shares; ++k) {
-        const float4 o = *reinterpret_cast<const float4*>(sums + k * M * d + i);
-        s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+    for (int k = 1; k < shares; k += 8) {
+        float4 o[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) o[u] = *reinterpret_cast<const float4*>(sums + min(k + u, shares - 1) * M * d + i);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (k + u < shares) { s.x += o[u].x; s.y += o[u].y; s.z += o[u].z; s.w += o[u].w; }
     }
     const int64_t row = i / d;
     *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
@@ -131,32 +128,33 @@ int64_t ce_piece(int64_t M, int64_t V, int64_t d) {
 
 struct CeLayout {
     int64_t piece, m64, width;      // outputs of a piece, tokens and outputs as far as zeros go
+    bool few;                       // the kernels of ce_few.hip, all outputs at once
     bool tiles_z, tiles_x;          // 256 x 256 tiles fit the logits of a piece, the sums of dX
     int shares;
-    size_t rowf, z, d, dt, wt, xt, part, sum, total;
+    size_t rowf, z, d, dt, wt, xt, sum, total;
 };
 // D's columns of a piece of n outputs: its shares' slices
 int64_t ce_width(int64_t n, int shares) { return shares == 1 ? std::max<int64_t>(up64(n), 2 * BK) : std::max<int64_t>((up64(n) / 64 + shares - 1) / shares, 2) * 64 * shares; }
 
 CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) {
     CeLayout l;
-    l.piece = std::min(ce_piece(M, V, d), V);
-    l.m64 = up64(M);
+    l.few = M <= kCeFewTokens;
+    l.piece = l.few ? V : std::min(ce_piece(M, V, d), V);
+    l.m64 = l.few ? 32 : up64(M);
     l.tiles_z = gemm_bf16_grad_fits(M, l.piece, d);
     l.tiles_x = gemm_bf16_grad_fits(M, d, 2 * BK);
-    l.shares = want_dx && l.tiles_x ? gemm_bf16_sum_shares(M, d, up64(l.piece) / 64) : 1;
-    l.width = ce_width(l.piece, l.shares);
-    const int64_t last = V - (V - 1) / l.piece * l.piece, logits = !l.tiles_z ? l.piece : gemm_bf16_grad_fits(M, last, d) ? 0 : last;
+    l.shares = !want_dx ? 1 : l.tiles_x ? gemm_bf16_sum_shares(M, d, up64(l.piece) / 64) : ce_few_dx_shares(M, l.piece, d);
+    l.width = ce_width(l.piece, l.tiles_x ? l.shares : 1);
+    const int64_t last = V - (V - 1) / l.piece * l.piece, logits = l.few ? 0 : !l.tiles_z ? l.piece : gemm_bf16_grad_fits(M, last, d) ? 0 : last;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
     l.rowf = take((size_t)M * 4);
     l.z = take((size_t)M * logits * 4);
     l.d = take((size_t)M * l.width * 2);
-    l.dt = take((size_t)l.piece * l.m64 * 2);
-    l.wt = take(want_dx ? (size_t)d * l.width * 2 : 0);
-    l.part = take(want_dx && !l.tiles_x && l.piece < V ? (size_t)M * d * 4 : 0);
+    l.dt = take(want_dw || !l.few ? (size_t)l.piece * l.m64 * 2 : 0);
+    l.wt = take(want_dx && l.tiles_x ? (size_t)d * l.width * 2 : 0);
     l.sum = take(want_dx ? (size_t)l.shares * M * d * 4 : 0);
-    l.xt = take(want_dw ? (size_t)d * l.m64 * 2 : 0);
+    l.xt = take(want_dw && !l.few ? (size_t)d * l.m64 * 2 : 0);
     l.total = o;
     return l;
 }
@@ -189,18 +187,28 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
     char* ws = static_cast<char*>(workspace);
     float *rowf = reinterpret_cast<float*>(ws + l.rowf), *z = reinterpret_cast<float*>(ws + l.z);
     bf16_t *D = reinterpret_cast<bf16_t*>(ws + l.d), *Dt = reinterpret_cast<bf16_t*>(ws + l.dt), *Wt = reinterpret_cast<bf16_t*>(ws + l.wt), *Xt = reinterpret_cast<bf16_t*>(ws + l.xt);
-    float *part = reinterpret_cast<float*>(ws + l.part), *sum = reinterpret_cast<float*>(ws + l.sum);
-    const unsigned sums = (unsigned)((a.M * a.d / 4 + 255) / 256);
+    float* sum = reinterpret_cast<float*>(ws + l.sum);
+    // (few values: a wave a workgroup, for the sake of their number)
+    const int wide = a.M * a.d <= 1 << 18 ? 64 : 256;
+    const unsigned sums = (unsigned)((a.M * a.d / 4 + wide - 1) / wide);
 #define CE_TRY(expr)                            \
     do {                                        \
         const hipError_t e__ = (expr);          \
         if (e__ != hipSuccess) return e__;      \
     } while (0)
+    if (l.few) {
+        CE_TRY(launch_ce_few_d(a.X, a.ldx, a.W, a.ldw, a.M, a.V, a.d, a.ids, a.lse, a.g, D, l.width, a.dW ? Dt : nullptr, st));
+        if (a.dW) CE_TRY(launch_ce_few_dw(Dt, a.X, a.ldx, a.M, a.V, a.d, a.ids, a.dW, a.lddw, st));
+        if (!a.dX) return hipSuccess;
+        CE_TRY(launch_ce_few_dx(D, l.width, a.W, a.ldw, a.M, a.V, a.d, l.shares, false, sum, st));
+        hipLaunchKernelGGL(ce_dx_kernel, dim3(sums), dim3(wide), 0, st, sum, l.shares, a.M, a.d, a.dX, a.lddx);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(ce_factor_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, rowf);
     CE_TRY(hipGetLastError());
     if (a.dW) CE_TRY(transpose(a.X, a.ldx, a.M, a.d, Xt, l.m64, a.ids, a.V, st));
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
-        const int64_t n = std::min(l.piece, a.V - v0), width = ce_width(n, l.shares);
+        const int64_t n = std::min(l.piece, a.V - v0), width = ce_width(n, l.tiles_x ? l.shares : 1);
         const bf16_t* W = a.W + v0 * a.ldw;
         if (gemm_bf16_grad_fits(a.M, n, a.d)) {
             CE_TRY(launch_gemm_bf16_softmax_grad(a.X, a.ldx, W, a.ldw, a.M, n, a.d, v0, a.ids, a.lse, rowf, D, width, Dt, l.m64, st));
@@ -213,19 +221,15 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
         }
         if (a.dW) CE_TRY(product(Dt, l.m64, Xt, l.m64, n, a.d, l.m64, a.dW + v0 * a.lddw, AGZO_BF16, a.lddw, st));
         if (!a.dX) continue;
-        CE_TRY(transpose(W, a.ldw, n, a.d, Wt, width, nullptr, 0, st));
-        if (l.tiles_x) {
-            CE_TRY(launch_gemm_bf16_sum(D, width, Wt, width, a.M, a.d, width / l.shares, l.shares, sum, v0 > 0, st));
+        if (!l.tiles_x) {
+            CE_TRY(launch_ce_few_dx(D, width, W, a.ldw, a.M, n, a.d, l.shares, v0 > 0, sum, st));
             continue;
         }
-        CE_TRY(product(D, width, Wt, width, a.M, a.d, width, v0 ? part : sum, AGZO_F32, a.d, st));
-        if (v0) {
-            hipLaunchKernelGGL(ce_add_kernel, dim3(sums), dim3(256), 0, st, part, sum, a.M * a.d);
-            CE_TRY(hipGetLastError());
-        }
+        CE_TRY(transpose(W, a.ldw, n, a.d, Wt, width, nullptr, 0, st));
+        CE_TRY(launch_gemm_bf16_sum(D, width, Wt, width, a.M, a.d, width / l.shares, l.shares, sum, v0 > 0, st));
     }
     if (a.dX) {
-        hipLaunchKernelGGL(ce_dx_kernel, dim3(sums), dim3(256), 0, st, sum, l.shares, a.M, a.d, a.dX, a.lddx);
+        hipLaunchKernelGGL(ce_dx_kernel, dim3(sums), dim3(wide), 0, st, sum, l.shares, a.M, a.d, a.dX, a.lddx);
         CE_TRY(hipGetLastError());
     }
 #undef CE_TRY
