@@ -150,7 +150,7 @@ __device__ __forceinline__ int own_problem(const KBatch<AlignedItem, CAP>& tb, u
 __device__ __forceinline__ int own_problem(const TileLists&, uint32_t&) { return 0; }
 
 template <int OUT, bool T_F32, int PHASES, bool RAGGED, int CAP>
-__global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArgs<PHASES, CAP> tb) {
+__device__ __forceinline__ void aligned_tiles(const AlignedArgs<PHASES, CAP>& tb) {
     static_assert(OUT == 0 || (PHASES == 1 && !T_F32), "the kernels without a squared-error target have one evaluation");
     constexpr bool LISTS = PHASES == 1 && CAP > 1;
     constexpr bool LATE_T = RAGGED && OUT == 0;    // the target is subtracted after the last slice
@@ -1026,16 +1026,33 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
 }
 
 template <int OUT, bool T_F32, int PHASES, bool RAGGED, int CAP>
+__global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArgs<PHASES, CAP> tb) {
+    aligned_tiles<OUT, T_F32, PHASES, RAGGED, CAP>(tb);
+}
+
+// the products of a loss's gradient (OUT = 3, 4)
+template <int OUT, bool RAGGED>
+__global__ __launch_bounds__(256) void gemm_bf16_gradient_kernel(const AlignedArgs<1, 1> tb) {
+    aligned_tiles<OUT, false, 1, RAGGED, 1>(tb);
+}
+
+template <int OUT, bool T_F32, int PHASES, bool RAGGED, int CAP>
+constexpr auto aligned_kernel() {
+    if constexpr (OUT >= 3) return &gemm_bf16_gradient_kernel<OUT, RAGGED>;
+    else return &gemm_bf16_aligned_kernel<OUT, T_F32, PHASES, RAGGED, CAP>;
+}
+
+template <int OUT, bool T_F32, int PHASES, bool RAGGED, int CAP>
 static hipError_t launch_aligned_grid(const AlignedArgs<PHASES, CAP>& tb, unsigned blocks, hipStream_t st) {
     static bool attr_set = false;
     const int smem = 5 * TILE_BYTES;           // three W stages and two X stages: all 160 KiB of a compute unit's LDS
     if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_bf16_aligned_kernel<OUT, T_F32, PHASES, RAGGED, CAP>),
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(aligned_kernel<OUT, T_F32, PHASES, RAGGED, CAP>()),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != hipSuccess) return e;
         attr_set = true;
     }
-    hipLaunchKernelGGL((gemm_bf16_aligned_kernel<OUT, T_F32, PHASES, RAGGED, CAP>), dim3(blocks), dim3(256), smem, st, tb);
+    hipLaunchKernelGGL((aligned_kernel<OUT, T_F32, PHASES, RAGGED, CAP>()), dim3(blocks), dim3(256), smem, st, tb);
     return hipGetLastError();
 }
 
