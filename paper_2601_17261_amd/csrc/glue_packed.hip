@@ -110,8 +110,9 @@ __device__ __forceinline__ void pk_second(const PkOffsets<HD>& o, int at, const 
 }
 
 // The same with care: values that are not finite are taken out, and with INF, where `seen` (fragments of ones and zeros) has a one for them, the
-// sum becomes what they make of it: a product of seen with 1 for inf, 2^12 for -inf and 2^23 for NaN has at most 64 of each
-template <int HD, bool INF>
+// sum becomes what they make of it: a product of seen with 1 for inf, 2^12 for -inf and 2^23 for NaN has at most 64 of each.  LOW: p's second part
+// in its place
+template <int HD, bool INF, bool LOW = false>
 __device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag (&p)[4], const PkFrag (&seen)[4], pk_floatx16 (&acc)[HD / 32]) {
     const int lane = threadIdx.x & 63, hi = lane >> 5;
 #pragma unroll
@@ -137,6 +138,7 @@ __device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag
                 k.w[w] = kw;
             }
             acc[db] = pk_mfma(f, p[s], acc[db]);       // (in the order of pk_second: the same bits)
+            if (LOW) acc[db] = pk_mfma(f, seen[s], acc[db]);
             if (INF) c = pk_mfma(k, seen[s], c);
         }
         if (INF) {
@@ -661,7 +663,9 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
             const bool mask = kb + PK_T - 1 > wfirst;
             // (operands two pairs of instructions ahead; see the forward)
-            PkFrag fk[2], fv[2], ft[2], pf[4];
+            // dS in two bf16 parts (16 bits): the keys of a head share directions, dS of a row sums to 0, so that its roundings are large beside what is left of
+            // the sum: in one part dq was off by 0.0028 of its norm, and is by 0.0020 (0.0017 is out's own rounding).  8192 tokens: 131 us for 105
+            PkFrag fk[2], fv[2], ft[2], pf[4], pl[4];
             const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
             auto read_rows = [&](int i) __attribute__((always_inline)) {
                 fk[i & 1].v = o.row(i / KS, i % KS);
@@ -687,6 +691,7 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
                         for (int u = 0; u < 2 * DB / KS; ++u) {
                             const int n = ks * (2 * DB / KS) + u;
                             acc[n % DB] = pk_mfma(ft[n & 1], pf[n / DB], acc[n % DB]);
+                            acc[n % DB] = pk_mfma(ft[n & 1], pl[n / DB], acc[n % DB]);
                             read_trans(n + 2);
                         }
                     }
@@ -703,11 +708,15 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
                     for (int e = 0; e < 16; ++e) ds[e] = 32 * h + pk_pos(e) <= rel ? ds[e] : 0.f;
                 }
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(ds[e], ds[e + 1]);
+                for (int e = 0; e < 16; e += 2) {
+                    const uint32_t w = pack_bf16x2(ds[e], ds[e + 1]);
+                    pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = w;
+                    pl[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(ds[e] - __uint_as_float(w << 16), ds[e + 1] - __uint_as_float(w & 0xFFFF0000u));
+                }
             }
             if constexpr (careful) {
                 if (mask) {
-                    pk_second_careful<HD, false>(kt, pf, pf, acc);
+                    pk_second_careful<HD, false, true>(kt, pf, pl, acc);
                     return;
                 }
                 read_trans(0);
@@ -717,6 +726,7 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
 #pragma unroll
             for (int n = careful ? 0 : 2 * DB; n < 4 * DB; ++n) {
                 acc[n % DB] = pk_mfma(ft[n & 1], pf[n / DB], acc[n % DB]);
+                acc[n % DB] = pk_mfma(ft[n & 1], pl[n / DB], acc[n % DB]);
                 if (n + 2 < 4 * DB) read_trans(n + 2);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -726,7 +736,7 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
     begin();
     if (tiles > 0) arrive(0);
     // Delta of rows that see one tile of keys at most, exactly: with out's and the probabilities' roundings in it the differences do - delta of few keys are off by
-    // 2^-8 of themselves (dq of sequences of some five tokens by 0.0045 of its norm, so by 0.0025), and here it is 32 instructions more.  For dk and dv too, and
+    // 2^-8 of themselves (dq of sequences of some five tokens by 0.0045 of its norm, so by 0.0017), and here it is 32 instructions more.  For dk and dv too, and
     // for a pass with care, which reads it
     if (!careful && tiles == 1) {
         __syncthreads();
