@@ -343,16 +343,18 @@ hipError_t launch_ce_combine(const void* ms, const float* tl, const int32_t* tar
 hipError_t launch_ce_rows_f32(const float* Y, int64_t ldy, int64_t M, int64_t N, const int32_t* target, double* scratch,
                               double* out, hipStream_t st, float* lse = nullptr);
 
-// ce_few.hip : the same loss and its gradient for few tokens, bf16.  D [M][ldd] (ldd: outputs rounded up to 32 at least) and, where wanted, D^T [V][32], zero from
-// column M on; dX's sums over shares of the outputs, [shares][M][d] fp32, for any number of tokens
+// ce_few.hip : the same loss and its gradient for few tokens, bf16.  D = exp(y - lse) - onehot, 0 in rows that are not counted, [M][ldd] (ldd: outputs rounded up to 32
+// at least), where wanted D^T [V][32], zero from column M on, and g / count as *scale; dX's sums without that factor, over shares of the outputs, [shares][M][d] fp32, for
+// any number of tokens; dW = *scale D^T X for up to ldt = 32, 64 or 128 of them
 constexpr int64_t kCeFewTokens = 32;
 size_t ce_few_workspace_bytes(int64_t M, int64_t V);
 hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, float* lse, double* out, void* workspace, hipStream_t st);
 hipError_t launch_ce_few_d(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, const float* lse, const double* g,
-                           bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st);
+                           float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st);
 int ce_few_dx_shares(int64_t M, int64_t n, int64_t d);
 hipError_t launch_ce_few_dx(const bf16_t* D, int64_t ldd, const bf16_t* W, int64_t ldw, int64_t M, int64_t n, int64_t d, int shares, bool add, float* sums, hipStream_t st);
-hipError_t launch_ce_few_dw(const bf16_t* Dt, const bf16_t* X, int64_t ldx, int64_t M, int64_t V, int64_t d, const int32_t* ids, bf16_t* dW, int64_t lddw, hipStream_t st);
+hipError_t launch_ce_few_dw(const bf16_t* Dt, int64_t ldt, const bf16_t* X, int64_t ldx, int64_t M, int64_t n, int64_t d, const int32_t* ids, int64_t V, const float* scale,
+                            bf16_t* dW, int64_t lddw, hipStream_t st);
 
 // ce_grad.hip : gradient of that loss: dX [M][d], dW [V][d] bf16 (either may be NULL), g: device scalar (NULL: 1), lse: of every row
 struct CeGradArgs {

@@ -31,7 +31,7 @@ struct FewArgs {
     // statistics of 32 outputs each, [token][outputs / 32], and the targets' logits
     float2* ms; float* tl; int64_t nch;
     // gradient: D [M][ldd], D^T [V][32]
-    const float* lse; const double* g; bf16_t* D; int64_t ldd; bf16_t* Dt;
+    const float* lse; const double* g; bf16_t* D; int64_t ldd; bf16_t* Dt; float* scale;
 };
 
 template <bool GRAD>
@@ -72,12 +72,11 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
     // a lane's sums: token r, outputs 8 (e / 4) + 4 hi + e % 4
 #pragma unroll
     for (int e = 0; e < 16; ++e) red[wave][8 * (e >> 2) + 4 * hi + (e & 3)][r] = acc[e];
-    float f = 0.f;
     if (GRAD) {
         if (tid < FEW_OUT * 4) reinterpret_cast<uint4*>(&tile[0][0])[tid] = make_uint4(0, 0, 0, 0);
         const int id = lane < a.M ? a.ids[lane] : -1;
         const int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(id >= 0 && id < a.V));
-        f = (float)((a.g ? *a.g : 1.0) / (double)max(count, 1));
+        if (blockIdx.x == 0 && tid == 0) *a.scale = (float)((a.g ? *a.g : 1.0) / (double)max(count, 1));
     }
     __syncthreads();
     // four outputs of a token a thread
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const float p = __builtin_amdgcn_exp2f((y[u] - l) * FEW_LOG2E);
-            v[u] = counted && 4 * grp + u < left ? (out0 + 4 * grp + u == id ? p - 1.f : p) * f : 0.f;
+            v[u] = counted && 4 * grp + u < left ? (out0 + 4 * grp + u == id ? p - 1.f : p) : 0.f;
         }
         const uint2 two = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
         if (tok < a.M) {
@@ -282,43 +281,48 @@ __global__ __launch_bounds__(256) void ce_few_dx_kernel(const bf16_t* __restrict
         }
 }
 
-// dW = D^T X for up to 32 tokens: a workgroup has 128 dims, whose X lies in LDS (rows that are not counted as zeros: D is 0 there, and a value that is not finite
-// would make NaNs of it) and in registers from there, and its waves take 32 outputs in turn.  Bound by what it writes.  7 tokens, 2048 x 32000: 27 us (4.8 TB/s), a product of X transposed 72
-__global__ __launch_bounds__(256) void ce_few_dw_kernel(const bf16_t* __restrict__ Dt, const bf16_t* __restrict__ X, int64_t ldx, int M, int64_t V, int64_t d, const int32_t* __restrict__ ids,
-                                                        bf16_t* __restrict__ dW, int64_t lddw) {
-    __shared__ __align__(1024) char xs[32 * 256];
+// dW = *scale D^T X for up to 32 KB tokens, as many as D^T [n][32 KB] has columns: a workgroup has 128 dims, whose X lies in LDS (rows that are not counted as
+// zeros: D is 0 there, and a value that is not finite would make NaNs of it) and in registers from there, and its waves take 32 outputs in turn.
+// Bound by what it writes.  7 tokens, 2048 x 32000: 27 us (4.8 TB/s), a product of X transposed 72
+template <int KB>
+__global__ __launch_bounds__(256) void ce_few_dw_kernel(const bf16_t* __restrict__ Dt, const bf16_t* __restrict__ X, int64_t ldx, int M, int64_t n, int64_t d, const int32_t* __restrict__ ids,
+                                                        int64_t V, const float* __restrict__ scale, bf16_t* __restrict__ dW, int64_t lddw) {
+    __shared__ __align__(1024) char xs[KB][32 * 256];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
-    const int64_t d0 = (int64_t)blockIdx.x * 128, blocks = (V + 31) / 32;
-    for (int i = tid; i < 32 * 16; i += 256) {
+    const int64_t d0 = (int64_t)blockIdx.x * 128, blocks = (n + 31) / 32;
+    const float f = *scale;
+    for (int i = tid; i < 32 * KB * 16; i += 256) {
         const int row = i >> 4, c = i & 15, id = row < M ? ids[row] : -1;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (id >= 0 && id < V && d0 + 8 * c < d) v = *reinterpret_cast<const uint4*>(X + row * ldx + d0 + 8 * c);
-        *reinterpret_cast<uint4*>(xs + row * 256 + ((c ^ few_swz(row)) << 4)) = v;
+        *reinterpret_cast<uint4*>(xs[row >> 5] + (row & 31) * 256 + ((c ^ few_swz(row & 31)) << 4)) = v;
     }
     __syncthreads();
     const FewTrans trans(lane);
-    FewFrag x[2][4];
+    FewFrag x[2 * KB][4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2 * KB; ++s)
 #pragma unroll
-        for (int db = 0; db < 4; ++db) x[s][db] = trans.read(xs, s, db);
+        for (int db = 0; db < 4; ++db) x[s][db] = trans.read(xs[s >> 1], s & 1, db);
     for (int64_t b = (int64_t)blockIdx.y * 4 + wave; b < blocks; b += (int64_t)gridDim.y * 4) {
         const int64_t out = b * 32 + r;
-        const bf16_t* row = Dt + min(out, V - 1) * 32 + 4 * hi;
-        const FewFrag t0 = few_order(row, 0), t1 = few_order(row, 1);
+        const bf16_t* row = Dt + min(out, n - 1) * (32 * KB) + 4 * hi;
+        FewFrag t[2 * KB];
+#pragma unroll
+        for (int s = 0; s < 2 * KB; ++s) t[s] = few_order(row, s);
         bf16_t* to = dW + out * lddw + d0 + 8 * hi;
 #pragma unroll
         for (int db = 0; db < 4; ++db) {
             floatx16 acc = {};
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0][db].v, t0.v, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1][db].v, t1.v, acc, 0, 0, 0);
+#pragma unroll
+            for (int s = 0; s < 2 * KB; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[s][db].v, t[s].v, acc, 0, 0, 0);
             // dims 16 h + 8 hi .. + 7 after the halves have changed places
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t a0 = pack_bf16x2(acc[8 * h], acc[8 * h + 1]), a1 = pack_bf16x2(acc[8 * h + 2], acc[8 * h + 3]);
-                const uint32_t b0 = pack_bf16x2(acc[8 * h + 4], acc[8 * h + 5]), b1 = pack_bf16x2(acc[8 * h + 6], acc[8 * h + 7]);
+                const uint32_t a0 = pack_bf16x2(acc[8 * h] * f, acc[8 * h + 1] * f), a1 = pack_bf16x2(acc[8 * h + 2] * f, acc[8 * h + 3] * f);
+                const uint32_t b0 = pack_bf16x2(acc[8 * h + 4] * f, acc[8 * h + 5] * f), b1 = pack_bf16x2(acc[8 * h + 6] * f, acc[8 * h + 7] * f);
                 const auto p = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), q = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-                if (out < V && d0 + 32 * db + 16 * h + 8 * hi < d) *reinterpret_cast<uint4*>(to + 32 * db + 16 * h) = make_uint4(p[0], q[0], p[1], q[1]);
+                if (out < n && d0 + 32 * db + 16 * h + 8 * hi < d) *reinterpret_cast<uint4*>(to + 32 * db + 16 * h) = make_uint4(p[0], q[0], p[1], q[1]);
             }
         }
     }
@@ -348,10 +352,10 @@ hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t 
 }
 
 hipError_t launch_ce_few_d(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, const float* lse, const double* g,
-                           bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st) {
+                           float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st) {
     if (M < 1 || M > kCeFewTokens || ldd < (V + 31) / 32 * 32 || ldd % 4) return hipErrorInvalidValue;
     FewArgs a = few_args(X, ldx, W, ldw, M, V, d, ids);
-    a.lse = lse; a.g = g; a.D = D; a.ldd = ldd; a.Dt = Dt;
+    a.lse = lse; a.g = g; a.scale = scale; a.D = D; a.ldd = ldd; a.Dt = Dt;
     hipLaunchKernelGGL(ce_few_kernel<true>, dim3((unsigned)((V + FEW_OUT - 1) / FEW_OUT)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
@@ -370,12 +374,15 @@ hipError_t launch_ce_few_dx(const bf16_t* D, int64_t ldd, const bf16_t* W, int64
     return hipGetLastError();
 }
 
-hipError_t launch_ce_few_dw(const bf16_t* Dt, const bf16_t* X, int64_t ldx, int64_t M, int64_t V, int64_t d, const int32_t* ids, bf16_t* dW, int64_t lddw, hipStream_t st) {
-    if (M < 1 || M > kCeFewTokens) return hipErrorInvalidValue;
-    const int64_t slices = (d + 127) / 128, groups = (V + 127) / 128;
+hipError_t launch_ce_few_dw(const bf16_t* Dt, int64_t ldt, const bf16_t* X, int64_t ldx, int64_t M, int64_t n, int64_t d, const int32_t* ids, int64_t V, const float* scale,
+                            bf16_t* dW, int64_t lddw, hipStream_t st) {
+    if (M < 1 || M > ldt || (ldt != 32 && ldt != 64 && ldt != 128)) return hipErrorInvalidValue;
+    const int64_t slices = (d + 127) / 128, groups = (n + 127) / 128;
     // eight workgroups to a compute unit, no more: each has to read X first
     const dim3 grid((unsigned)slices, (unsigned)std::max<int64_t>(1, std::min(groups, 2048 / slices)));
-    hipLaunchKernelGGL(ce_few_dw_kernel, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, V, d, ids, dW, lddw);
+    if (ldt == 32) hipLaunchKernelGGL(ce_few_dw_kernel<1>, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, n, d, ids, V, scale, dW, lddw);
+    else if (ldt == 64) hipLaunchKernelGGL(ce_few_dw_kernel<2>, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, n, d, ids, V, scale, dW, lddw);
+    else hipLaunchKernelGGL(ce_few_dw_kernel<4>, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, n, d, ids, V, scale, dW, lddw);
     return hipGetLastError();
 }
 

@@ -1,6 +1,7 @@
 // Gradient of the softmax cross-entropy of a layer's outputs Y = X W^T [M][V], whose mean over the counted rows is the loss of loss.hip:
-//     D_tv = (exp(y_tv - lse_t) - [v = id_t]) g / count   (0 in rows that are not counted),     dX = D W,     dW = D^T X.
-// The logits are made once more, for a piece of the outputs at a time, and only D of that piece is stored, as bf16, in both orders: the
+//     D_tv = exp(y_tv - lse_t) - [v = id_t]   (0 in rows that are not counted),     dX = f D W,     dW = f D^T X,     f = g / count.
+// The logits are made once more, for a piece of the outputs at a time, and only D of that piece is stored, as bf16, in both orders
+// (without f, whose rounding all of its values would share: with it in D the gradients of 8192 tokens of 131072 outputs were off by 0.0032 of their norm): the
 // products contract over outputs and over tokens, and the forward's kernels want the contracted dimension side by side.  So W's piece and X are
 // transposed too.  The products are those of gemm_bf16_aligned.hip where a 256 x 256 tile fits: D leaves the logits' product in both orders, and dX is
 // summed over the pieces in fp32, in shares of a piece where its tiles alone would not fill the chip.  Other shapes go through fp32 logits and
@@ -12,8 +13,8 @@ namespace agzo {
 
 namespace {
 
-// g / max(count, 1), count of the rows whose id is an output, as each such row's factor, 0 for the others; one workgroup
-__global__ __launch_bounds__(1024) void ce_factor_kernel(const int32_t* __restrict__ ids, int64_t M, int64_t V, const double* __restrict__ g, float* __restrict__ rowf) {
+// *scale = g / max(count, 1), count of the rows whose id is an output; rowf: 1 for these, 0 for the others; one workgroup
+__global__ __launch_bounds__(1024) void ce_factor_kernel(const int32_t* __restrict__ ids, int64_t M, int64_t V, const double* __restrict__ g, float* __restrict__ rowf, float* __restrict__ scale) {
     __shared__ int red[16];
     int n = 0;
     for (int64_t t = threadIdx.x; t < M; t += 1024) n += ids[t] >= 0 && ids[t] < V;
@@ -23,8 +24,8 @@ __global__ __launch_bounds__(1024) void ce_factor_kernel(const int32_t* __restri
     __syncthreads();
     n = 0;
     for (int w = 0; w < 16; ++w) n += red[w];
-    const float f = (float)((g ? *g : 1.0) / (double)max(n, 1));
-    for (int64_t t = threadIdx.x; t < M; t += 1024) rowf[t] = ids[t] >= 0 && ids[t] < V ? f : 0.f;
+    if (threadIdx.x == 0) *scale = (float)((g ? *g : 1.0) / (double)max(n, 1));
+    for (int64_t t = threadIdx.x; t < M; t += 1024) rowf[t] = ids[t] >= 0 && ids[t] < V ? 1.f : 0.f;
 }
 
 // columns from .. to of rows of ld values <- 0
@@ -73,15 +74,14 @@ __global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __res
         const int r = i >> 5, c = (i & 31) * 2;
         const int64_t row = r0 + r;
         float v[2] = {0.f, 0.f};
-        const float f = row < M ? rowf[row] : 0.f;
-        if (f != 0.f) {
+        if (row < M && rowf[row] != 0.f) {
             const float l = lse[row];
             const int id = ids[row];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 if (c0 + c + u < n) {
                     const float p = __builtin_amdgcn_exp2f((z[row * ldz + c0 + c + u] - l) * 1.44269504088896341f);
-                    v[u] = (v0 + c0 + c + u == id ? p - 1.f : p) * f;
+                    v[u] = v0 + c0 + c + u == id ? p - 1.f : p;
                 }
         }
         const uint32_t w = pack_bf16x2(v[0], v[1]);
@@ -99,8 +99,8 @@ __global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __res
     }
 }
 
-// dX: the shares' sums [shares][M][d] added in order, as bf16
-__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, int shares, int64_t M, int64_t d, bf16_t* __restrict__ out, int64_t ldo) {
+// dX or dW: the shares' sums [shares][M][d] added in order, times *scale, as bf16
+__global__ __launch_bounds__(256) void ce_join_kernel(const float* __restrict__ sums, int shares, int64_t M, int64_t d, const float* __restrict__ scale, bf16_t* __restrict__ out, int64_t ldo) {
     const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
     if (i >= M * d) return;
     float4 s = *reinterpret_cast<const float4*>(sums + i);
@@ -113,7 +113,13 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
             if (k + u < shares) { s.x += o[u].x; s.y += o[u].y; s.z += o[u].z; s.w += o[u].w; }
     }
     const int64_t row = i / d;
-    *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+    const float f = *scale;
+    *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
+}
+hipError_t join(const float* sums, int shares, int64_t M, int64_t d, const float* scale, bf16_t* out, int64_t ldo, hipStream_t st) {
+    const int wide = M * d <= 1 << 18 ? 64 : 256;      // (few values: a wave a workgroup, for the sake of their number)
+    hipLaunchKernelGGL(ce_join_kernel, dim3((unsigned)((M * d / 4 + wide - 1) / wide)), dim3(wide), 0, st, sums, shares, M, d, scale, out, ldo);
+    return hipGetLastError();
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -127,34 +133,43 @@ int64_t ce_piece(int64_t M, int64_t V, int64_t d) {
 }
 
 struct CeLayout {
-    int64_t piece, m64, width;      // outputs of a piece, tokens and outputs as far as zeros go
+    int64_t piece, width, kt;       // outputs of a piece; outputs and tokens as far as zeros go
     bool few;                       // the kernels of ce_few.hip, all outputs at once
+    bool few_w;                     // and for dW
     bool tiles_z, tiles_x;          // 256 x 256 tiles fit the logits of a piece, the sums of dX
-    int shares;
-    size_t rowf, z, d, dt, wt, xt, sum, total;
+    int shares, shares_w;           // of dX's outputs, of dW's tokens
+    size_t rowf, scale, z, d, dt, wt, xt, sum, wsum, total;
 };
-// D's columns of a piece of n outputs: its shares' slices
+// D's columns of n outputs (D^T's of n tokens): their shares' slices
 int64_t ce_width(int64_t n, int shares) { return shares == 1 ? std::max<int64_t>(up64(n), 2 * BK) : std::max<int64_t>((up64(n) / 64 + shares - 1) / shares, 2) * 64 * shares; }
+
+// whether the tiles store dW themselves, of n outputs; else it goes through fp32 sums, which shares of the tokens or a kernel for any shape leave
+bool ce_dw_stored(const CeLayout& l, int64_t n, int64_t d) { return gemm_bf16_grad_fits(n, d, l.kt) && l.shares_w == 1; }
 
 CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) {
     CeLayout l;
     l.few = M <= kCeFewTokens;
+    l.few_w = M <= 128;
     l.piece = l.few ? V : std::min(ce_piece(M, V, d), V);
-    l.m64 = l.few ? 32 : up64(M);
     l.tiles_z = gemm_bf16_grad_fits(M, l.piece, d);
     l.tiles_x = gemm_bf16_grad_fits(M, d, 2 * BK);
     l.shares = !want_dx ? 1 : l.tiles_x ? gemm_bf16_sum_shares(M, d, up64(l.piece) / 64) : ce_few_dx_shares(M, l.piece, d);
+    l.shares_w = l.few_w || !want_dw || !gemm_bf16_grad_fits(l.piece, d, M) ? 1 : gemm_bf16_sum_shares(l.piece, d, up64(M) / 64);
     l.width = ce_width(l.piece, l.tiles_x ? l.shares : 1);
+    l.kt = M <= 32 ? 32 : M <= 64 ? 64 : ce_width(M, l.shares_w);
     const int64_t last = V - (V - 1) / l.piece * l.piece, logits = l.few ? 0 : !l.tiles_z ? l.piece : gemm_bf16_grad_fits(M, last, d) ? 0 : last;
+    const int64_t sums_w = !want_dw || l.few_w ? 0 : !ce_dw_stored(l, l.piece, d) ? l.piece : !ce_dw_stored(l, last, d) ? last : 0;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
     l.rowf = take((size_t)M * 4);
+    l.scale = take(4);
     l.z = take((size_t)M * logits * 4);
     l.d = take((size_t)M * l.width * 2);
-    l.dt = take(want_dw || !l.few ? (size_t)l.piece * l.m64 * 2 : 0);
+    l.dt = take(want_dw || !l.few ? (size_t)l.piece * l.kt * 2 : 0);
     l.wt = take(want_dx && l.tiles_x ? (size_t)d * l.width * 2 : 0);
     l.sum = take(want_dx ? (size_t)l.shares * M * d * 4 : 0);
-    l.xt = take(want_dw && !l.few ? (size_t)d * l.m64 * 2 : 0);
+    l.wsum = take((size_t)l.shares_w * sums_w * d * 4);
+    l.xt = take(want_dw && !l.few_w ? (size_t)d * l.kt * 2 : 0);
     l.total = o;
     return l;
 }
@@ -170,9 +185,9 @@ hipError_t zero_columns(bf16_t* y, int64_t rows, int64_t ld, int64_t from, int64
     return hipGetLastError();
 }
 
-hipError_t product(const bf16_t* x, int64_t ldx, const bf16_t* w, int64_t ldw, int64_t M, int64_t N, int64_t K, void* y, int y_dtype, int64_t ldy, hipStream_t st) {
+hipError_t product(const bf16_t* x, int64_t ldx, const bf16_t* w, int64_t ldw, int64_t M, int64_t N, int64_t K, float* y, int64_t ldy, hipStream_t st) {
     GemmBf16Args a;
-    a.X = x; a.ldx = ldx; a.W = w; a.ldw = ldw; a.M = M; a.N = N; a.K = K; a.Y = y; a.y_dtype = y_dtype; a.ldy = ldy;
+    a.X = x; a.ldx = ldx; a.W = w; a.ldw = ldw; a.M = M; a.N = N; a.K = K; a.Y = y; a.y_dtype = AGZO_F32; a.ldy = ldy;
     a.P = nullptr; a.r = 1; a.eps_signed = 0.f; a.seed = 0;
     a.loss.kind = AGZO_LOSS_NONE; a.loss.target_dtype = 0; a.loss.target = nullptr; a.loss.ldt = 0; a.loss.partials = nullptr;
     return launch_gemm_bf16(a, st);
@@ -185,41 +200,48 @@ size_t ce_grad_workspace_bytes(int64_t M, int64_t V, int64_t d, bool want_dx, bo
 hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) {
     const CeLayout l = ce_layout(a.M, a.V, a.d, a.dX != nullptr, a.dW != nullptr);
     char* ws = static_cast<char*>(workspace);
-    float *rowf = reinterpret_cast<float*>(ws + l.rowf), *z = reinterpret_cast<float*>(ws + l.z);
+    float *rowf = reinterpret_cast<float*>(ws + l.rowf), *scale = reinterpret_cast<float*>(ws + l.scale), *z = reinterpret_cast<float*>(ws + l.z);
     bf16_t *D = reinterpret_cast<bf16_t*>(ws + l.d), *Dt = reinterpret_cast<bf16_t*>(ws + l.dt), *Wt = reinterpret_cast<bf16_t*>(ws + l.wt), *Xt = reinterpret_cast<bf16_t*>(ws + l.xt);
-    float* sum = reinterpret_cast<float*>(ws + l.sum);
-    // (few values: a wave a workgroup, for the sake of their number)
-    const int wide = a.M * a.d <= 1 << 18 ? 64 : 256;
-    const unsigned sums = (unsigned)((a.M * a.d / 4 + wide - 1) / wide);
+    float *sum = reinterpret_cast<float*>(ws + l.sum), *wsum = reinterpret_cast<float*>(ws + l.wsum);
 #define CE_TRY(expr)                            \
     do {                                        \
         const hipError_t e__ = (expr);          \
         if (e__ != hipSuccess) return e__;      \
     } while (0)
     if (l.few) {
-        CE_TRY(launch_ce_few_d(a.X, a.ldx, a.W, a.ldw, a.M, a.V, a.d, a.ids, a.lse, a.g, D, l.width, a.dW ? Dt : nullptr, st));
-        if (a.dW) CE_TRY(launch_ce_few_dw(Dt, a.X, a.ldx, a.M, a.V, a.d, a.ids, a.dW, a.lddw, st));
-        if (!a.dX) return hipSuccess;
-        CE_TRY(launch_ce_few_dx(D, l.width, a.W, a.ldw, a.M, a.V, a.d, l.shares, false, sum, st));
-        hipLaunchKernelGGL(ce_dx_kernel, dim3(sums), dim3(wide), 0, st, sum, l.shares, a.M, a.d, a.dX, a.lddx);
-        return hipGetLastError();
+        CE_TRY(launch_ce_few_d(a.X, a.ldx, a.W, a.ldw, a.M, a.V, a.d, a.ids, a.lse, a.g, scale, D, l.width, a.dW ? Dt : nullptr, st));
+    } else {
+        hipLaunchKernelGGL(ce_factor_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, rowf, scale);
+        CE_TRY(hipGetLastError());
+        if (a.dW && !l.few_w) CE_TRY(transpose(a.X, a.ldx, a.M, a.d, Xt, l.kt, a.ids, a.V, st));
     }
-    hipLaunchKernelGGL(ce_factor_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, rowf);
-    CE_TRY(hipGetLastError());
-    if (a.dW) CE_TRY(transpose(a.X, a.ldx, a.M, a.d, Xt, l.m64, a.ids, a.V, st));
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
         const int64_t n = std::min(l.piece, a.V - v0), width = ce_width(n, l.tiles_x ? l.shares : 1);
         const bf16_t* W = a.W + v0 * a.ldw;
-        if (gemm_bf16_grad_fits(a.M, n, a.d)) {
-            CE_TRY(launch_gemm_bf16_softmax_grad(a.X, a.ldx, W, a.ldw, a.M, n, a.d, v0, a.ids, a.lse, rowf, D, width, Dt, l.m64, st));
+        if (l.few) {
+            // (D is there)
+        } else if (gemm_bf16_grad_fits(a.M, n, a.d)) {
+            CE_TRY(launch_gemm_bf16_softmax_grad(a.X, a.ldx, W, a.ldw, a.M, n, a.d, v0, a.ids, a.lse, rowf, D, width, Dt, l.kt, st));
             if (a.dX) CE_TRY(zero_columns(D, a.M, width, n, width, st));
-            if (a.dW) CE_TRY(zero_columns(Dt, n, l.m64, a.M, l.m64, st));
+            if (a.dW) CE_TRY(zero_columns(Dt, n, l.kt, a.M, l.kt, st));
         } else {
-            CE_TRY(product(a.X, a.ldx, W, a.ldw, a.M, n, a.d, z, AGZO_F32, n, st));
-            hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(width / 64), (unsigned)(l.m64 / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.ids, a.lse, rowf, D, width, Dt, l.m64);
+            CE_TRY(product(a.X, a.ldx, W, a.ldw, a.M, n, a.d, z, n, st));
+            hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(width / 64), (unsigned)(l.kt / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.ids, a.lse, rowf, D, width, Dt, l.kt);
             CE_TRY(hipGetLastError());
         }
-        if (a.dW) CE_TRY(product(Dt, l.m64, Xt, l.m64, n, a.d, l.m64, a.dW + v0 * a.lddw, AGZO_BF16, a.lddw, st));
+        if (a.dW) {
+            bf16_t* dW = a.dW + v0 * a.lddw;
+            if (l.few_w) {
+                CE_TRY(launch_ce_few_dw(Dt, l.kt, a.X, a.ldx, a.M, n, a.d, a.ids, a.V, scale, dW, a.lddw, st));
+            } else if (ce_dw_stored(l, n, a.d)) {
+                CE_TRY(launch_gemm_bf16_scaled(Dt, l.kt, Xt, l.kt, n, a.d, l.kt, scale, dW, a.lddw, st));
+            } else {
+                const bool fits = gemm_bf16_grad_fits(n, a.d, l.kt / l.shares_w);
+                if (fits) CE_TRY(launch_gemm_bf16_sum(Dt, l.kt, Xt, l.kt, n, a.d, l.kt / l.shares_w, l.shares_w, wsum, false, st));
+                else CE_TRY(product(Dt, l.kt, Xt, l.kt, n, a.d, l.kt, wsum, a.d, st));
+                CE_TRY(join(wsum, fits ? l.shares_w : 1, n, a.d, scale, dW, a.lddw, st));
+            }
+        }
         if (!a.dX) continue;
         if (!l.tiles_x) {
             CE_TRY(launch_ce_few_dx(D, width, W, a.ldw, a.M, n, a.d, l.shares, v0 > 0, sum, st));
@@ -228,12 +250,8 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
         CE_TRY(transpose(W, a.ldw, n, a.d, Wt, width, nullptr, 0, st));
         CE_TRY(launch_gemm_bf16_sum(D, width, Wt, width, a.M, a.d, width / l.shares, l.shares, sum, v0 > 0, st));
     }
-    if (a.dX) {
-        hipLaunchKernelGGL(ce_dx_kernel, dim3(sums), dim3(wide), 0, st, sum, l.shares, a.M, a.d, a.dX, a.lddx);
-        CE_TRY(hipGetLastError());
-    }
 #undef CE_TRY
-    return hipSuccess;
+    return a.dX ? join(sum, l.shares, a.M, a.d, scale, a.dX, a.lddx, st) : hipSuccess;
 }
 
 }  // namespace agzo

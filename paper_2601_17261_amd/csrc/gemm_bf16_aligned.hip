@@ -4,7 +4,8 @@
 //     OUT = 2:  the same logits never stored: per token and 128-column chunk their maximum and the sum of exponentials
 //               around it, and the target's logit (token cross-entropy of a model's last layer; loss.hip combines them)
 //     OUT = 3:  Y (+)= X W^T in fp32, the sums over shares of d_in by themselves (products of the cross-entropy's gradient, ce_grad.hip)
-//     OUT = 4:  (exp(Y - lse) - onehot) f, f by token, stored as bf16 and once more transposed (that gradient with respect to the logits)
+//     OUT = 4:  exp(Y - lse) - onehot of the tokens that count, stored as bf16 and once more transposed (that gradient with respect to the logits)
+//     OUT = 5:  f X W^T stored as bf16, f one number
 // Same tile, tile layout in LDS and direct global -> LDS operand loads as gemm_bf16.hip (256 x 256 tile, four waves of
 // 128 x 128, 64-wide K slices), but a kernel of its own with one straight path and nothing else compiled in: M and N of
 // at least 256, d_in of at least 128, the rank-r extension as prepared operands.
@@ -121,7 +122,7 @@ struct AlignedItem {
     int ext_ld, tiles_m, tiles_n, group_m, vec_ok;
     int sub;                                       // partials are those of gemm_bf16_mid.hip: one per 128 x 128 outputs
     // (OUT = 3: K is a share of d_in, there are ext_ld of them, and sub says whether sums are added to.  OUT = 4: ce_target, ce_tl and partials
-    // are ids, lse and f of the tokens, the latter as fp32; ce_ms is the transposed output, ldt its leading dimension, sub the first output's number)
+    // are ids, lse and 1 or 0 (counted or not) of the tokens, the latter as fp32, OUT = 5: partials is f as fp32; ce_ms is the transposed output, ldt its leading dimension, sub the first output's number)
 };
 
 // Tile lists over the tiles of several problems (one evaluation, squared error).  The tiles of a problem are dealt to the XCDs in runs
@@ -723,13 +724,16 @@ __device__ __forceinline__ void aligned_tiles(const AlignedArgs<PHASES, CAP>& tb
         // the tile's last matrix instruction has issued; the stages of slice g hold the next tile's first slice, fragment
         // set 0 its sub-step 0, and its second slice is in flight; W stage wst - 1 is idle until the next W loads
         const bool more = LISTS ? l_more : it + 1 < n_tiles;
-        if constexpr (OUT == 1) {
+        if constexpr (OUT == 1 || OUT == 5) {
             // A lane holds 16 consecutive outputs of one token per group of four blocks, so stored from the registers every
             // store touches 16 rows.  Instead each wave passes its 128 x 128 block through LDS, 32 tokens at a time, in its
             // quarter of the W stage that is idle between two tiles: written as held (16-byte chunk c of row t at
             // c ^ (t mod 16): the lanes of one write spread over all banks), read back 16 lanes to a 256-byte row, and
             // stored four whole rows to an instruction.
             settle();
+            float f = 1.f;                                   // (OUT = 5)
+            if constexpr (OUT == 5) f = *reinterpret_cast<const float*>(item(cq).partials);
+            auto out = [&](float v) __attribute__((always_inline)) { return OUT == 5 ? from_acc(v) * f : from_acc(v); };
             char* stg = smem + W_BASE + ((wst == 0) ? 2 : wst - 1) * TILE_BYTES + wave * 8192;
 #pragma clang loop unroll(full)
             for (int r2 = 0; r2 < 4; ++r2) {
@@ -742,8 +746,8 @@ __device__ __forceinline__ void aligned_tiles(const AlignedArgs<PHASES, CAP>& tb
 #pragma clang loop unroll(full)
                         for (int t = 0; t < 4; ++t) {
                             const floatx4 v = acc[i4 * 4 + t][J];
-                            w[2 * t] = pack_bf16x2(from_acc(v[0]), from_acc(v[1]));
-                            w[2 * t + 1] = pack_bf16x2(from_acc(v[2]), from_acc(v[3]));
+                            w[2 * t] = pack_bf16x2(out(v[0]), out(v[1]));
+                            w[2 * t + 1] = pack_bf16x2(out(v[2]), out(v[3]));
                         }
                         const int c0 = i4 * 8 + lg * 2;
                         *reinterpret_cast<uint4*>(stg + trow * 256 + ((c0 ^ (trow & 15)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -834,7 +838,7 @@ __device__ __forceinline__ void aligned_tiles(const AlignedArgs<PHASES, CAP>& tb
                         uint32_t w[8];
 #pragma clang loop unroll(full)
                         for (int k = 0; k < 8; ++k) {
-                            const uint32_t two = pack_bf16x2(p[16 * i4 + 2 * k] * f[J], p[16 * i4 + 2 * k + 1] * f[J]);
+                            const uint32_t two = pack_bf16x2(p[16 * i4 + 2 * k], p[16 * i4 + 2 * k + 1]);
                             w[k] = f[J] == 0.f ? 0u : two;               // (a row that is not counted, whatever its logits are)
                         }
                         const int c0 = i4 * 8 + lg * 2;
@@ -1030,7 +1034,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_aligned_kernel(const AlignedArg
     aligned_tiles<OUT, T_F32, PHASES, RAGGED, CAP>(tb);
 }
 
-// the products of a loss's gradient (OUT = 3, 4)
+// the products of a loss's gradient (OUT = 3, 4, 5)
 template <int OUT, bool RAGGED>
 __global__ __launch_bounds__(256) void gemm_bf16_gradient_kernel(const AlignedArgs<1, 1> tb) {
     aligned_tiles<OUT, false, 1, RAGGED, 1>(tb);
@@ -1270,6 +1274,13 @@ hipError_t launch_gemm_bf16_sum(const bf16_t* X, int64_t ldx, const bf16_t* W, i
     AlignedItem a = grad_item(X, ldx, W, ldw, M, N, K);
     a.Y = Y; a.ldy = N; a.ext_ld = shares; a.sub = add ? 1 : 0;
     return launch_grad<3>(a, M % BT || N % BT, (int64_t)a.tiles_m * a.tiles_n * shares, st);
+}
+
+hipError_t launch_gemm_bf16_scaled(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, const float* scale, bf16_t* Y, int64_t ldy, hipStream_t st) {
+    if (!gemm_bf16_grad_fits(M, N, K) || N % 8 || ldy % 8 || (reinterpret_cast<uintptr_t>(Y) & 15)) return hipErrorInvalidValue;
+    AlignedItem a = grad_item(X, ldx, W, ldw, M, N, K);
+    a.Y = Y; a.ldy = ldy; a.partials = reinterpret_cast<double*>(const_cast<float*>(scale));
+    return launch_grad<5>(a, M % BT || N % BT || K % BK, (int64_t)a.tiles_m * a.tiles_n, st);
 }
 
 hipError_t launch_gemm_bf16_softmax_grad(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int64_t first, const int32_t* ids,

@@ -113,7 +113,9 @@ hipError_t launch_gemm_bf16_aligned_lists(const GemmParams* const* a, const bool
 bool gemm_bf16_grad_fits(int64_t M, int64_t N, int64_t K);
 int gemm_bf16_sum_shares(int64_t M, int64_t N, int64_t slices);
 hipError_t launch_gemm_bf16_sum(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int shares, float* Y, bool add, hipStream_t st);
-// D [M][ldd] = (exp(X W^T - lse) - onehot) rowf and D^T [N][ldt], both bf16; first: what the first output's id is; rows with rowf 0 are 0
+// Y [M][ldy] = *scale X W^T, bf16
+hipError_t launch_gemm_bf16_scaled(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, const float* scale, bf16_t* Y, int64_t ldy, hipStream_t st);
+// D [M][ldd] = exp(X W^T - lse) - onehot and D^T [N][ldt], both bf16; first: what the first output's id is; rows whose rowf is 0 are 0
 hipError_t launch_gemm_bf16_softmax_grad(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int64_t first, const int32_t* ids,
                                          const float* lse, const float* rowf, bf16_t* D, int64_t ldd, bf16_t* Dt, int64_t ldt, hipStream_t st);
 // squared error with p.shared (f0, f+, f- in one pass, needs Wext2, partials [3][tiles]): up to kBatchMax layers together
