@@ -301,16 +301,19 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  * probabilities are rounded to bf16 for the second product, sums are fp32.  A query that sees no key (Lk < Lq, or no keys at all) gets 0
  * and takes part in no gradient.  Values of keys that a query does not see have no part in its result, whatever they are (NaN and
  * infinities too).  Rows of no sequence are neither read nor written.
+ *   k_len (nullable; forward call only): how many of its keys sequence s has, the first k_len[s] (0 .. cu_k[s + 1] - cu_k[s]: a length outside is taken as
+ *     the nearest of these): a cache with room for each sequence, of which the rest is not read
  *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key
  *   backward: out, lse of the forward call with the same arguments and the gradient dout -> dq, dk, dv (all three written, for all rows of
  *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
  * Inputs are only read; outputs may not overlap inputs or each other.
  * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, counts of 2^31 and more, leading
- * dimensions from 2^22 on), scale not positive and finite, overlapping outputs. */
+ * dimensions from 2^22 on), scale not positive and finite, overlapping outputs, lengths in the backward call. */
 typedef struct {
     const void *q, *k, *v;       /* [n_q][n_heads head_dim], [n_k][n_kv_heads head_dim] twice */
     int64_t ldq, ldk, ldv;
     const int32_t *cu_q, *cu_k;
+    const int32_t* k_len;        /* nullable: device int32 [n_seq] */
     int64_t n_q, n_k;            /* rows of the tensors */
     int32_t n_seq, n_heads, n_kv_heads, head_dim;
     int32_t causal;

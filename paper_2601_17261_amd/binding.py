@@ -65,7 +65,7 @@ class AgzoStepItem(ctypes.Structure):
 class AgzoPackedAttention(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64),
-                ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p), ("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64),
+                ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p), ("k_len", ctypes.c_void_p), ("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64),
                 ("n_seq", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("causal", ctypes.c_int32), ("scale", ctypes.c_float)]
 
@@ -424,11 +424,13 @@ class Context:
         a.causal, a.scale = int(causal), head_dim ** -0.5 if scale is None else scale
         return a
 
-    def glue_attention_packed(self, q, k, v, out, cu_q, cu_k, head_dim=128, scale=None, causal=True, lse=None):
+    def glue_attention_packed(self, q, k, v, out, cu_q, cu_k, head_dim=128, scale=None, causal=True, lse=None, k_len=None):
         """q [n_q][heads * head_dim], k, v [n_k][key heads * head_dim] -> out like q; cu_q, cu_k: int32 offsets of the sequences
-        (n_seq + 1 each); scale None: head_dim ** -0.5; lse: float32 [n_q][heads] or None."""
-        self._same_device(q, k, v, out, cu_q, cu_k, lse)
+        (n_seq + 1 each); scale None: head_dim ** -0.5; lse: float32 [n_q][heads] or None; k_len: int32 [n_seq], how many keys each has
+        of its room (a cache), or None: all."""
+        self._same_device(q, k, v, out, cu_q, cu_k, lse, k_len)
         a = self._packed(q, k, v, cu_q, cu_k, head_dim, scale, causal)
+        a.k_len = _flat(k_len, "k_len", torch.int32, a.n_seq)
         _same_shape("out", out, q)
         o, ldo = _rows(out, "out")
         self._rc(self.lib.agzo_glue_attention_packed(self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, a.n_q * a.n_heads)))

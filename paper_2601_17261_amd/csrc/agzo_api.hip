@@ -1414,11 +1414,12 @@ int packed_args(agzo_ctx* ctx, const agzo_packed_attention* a, PackedArgs& out) 
     if (a->ldq >= (1LL << 22) || a->ldk >= (1LL << 22) || a->ldv >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "leading dimensions must be below 2^22");
     if (a->n_seq > 0 && (!a->cu_q || !a->cu_k || ((reinterpret_cast<uintptr_t>(a->cu_q) | reinterpret_cast<uintptr_t>(a->cu_k)) & 3)))
         return fail(ctx, AGZO_EINVAL, "cu_q or cu_k is NULL or misaligned");
+    if (reinterpret_cast<uintptr_t>(a->k_len) & 3) return fail(ctx, AGZO_EINVAL, "k_len is misaligned");
     const int64_t dq = (int64_t)a->n_heads * a->head_dim, dkv = (int64_t)a->n_kv_heads * a->head_dim;
     TRY(check_glue(ctx, a->n_q, dq, {a->q}, {a->ldq}));
     TRY(check_glue(ctx, a->n_k, dkv, {a->k, a->v}, {a->ldk, a->ldv}));
     out = PackedArgs{static_cast<const bf16_t*>(a->q), static_cast<const bf16_t*>(a->k), static_cast<const bf16_t*>(a->v), a->ldq, a->ldk, a->ldv,
-                     a->cu_q, a->cu_k, a->n_q, a->n_k, a->n_seq, a->n_heads, a->n_kv_heads, a->causal != 0, a->scale};
+                     a->cu_q, a->cu_k, a->n_seq ? a->k_len : nullptr, a->n_q, a->n_k, a->n_seq, a->n_heads, a->n_kv_heads, a->causal != 0, a->scale};
     return check_device(ctx);
 }
 }  // namespace
@@ -1524,6 +1525,7 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
                                         int64_t lddv) {
     PackedArgs p;
     TRY(packed_args(ctx, a, p));
+    if (a->k_len) return fail(ctx, AGZO_EINVAL, "k_len is for the forward call");
     const int64_t wq = (int64_t)a->n_heads * a->head_dim, wk = (int64_t)a->n_kv_heads * a->head_dim;
     TRY(check_glue(ctx, a->n_q, wq, {out, dout, dq}, {ldo, lddo, lddq}));
     TRY(check_glue(ctx, a->n_k, wk, {dk, dv}, {lddk, lddv}));

@@ -412,6 +412,7 @@ struct PackedArgs {
     const bf16_t *q, *k, *v;
     int64_t ldq, ldk, ldv;
     const int32_t *cu_q, *cu_k;        // [n_seq + 1]
+    const int32_t* k_len;              // [n_seq], nullable (forward): keys of its room that a sequence has
     int64_t total_q, total_k;          // below 2^31, as total_q n_heads / n_kv
     int n_seq, n_heads, n_kv, causal;
     float scale;

@@ -227,6 +227,7 @@ __device__ __forceinline__ bool pk_find(const PackedArgs& a, int t, int G, int c
         int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
         q0 = min(max(q0, 0), total_q);   q1 = min(max(q1, q0), total_q);
         k0 = min(max(k0, 0), total_k);   k1 = min(max(k1, k0), total_k);
+        if (!BY_KEYS && a.k_len) k1 = k0 + min(max(a.k_len[s], 0), k1 - k0);
         const int own = b + lane >= a.n_seq ? 0 : (int)(((BY_KEYS ? (uint32_t)(k1 - k0) : (uint32_t)(q1 - q0) * (uint32_t)G) + (UNIT - 1)) / UNIT);
         // (a row tile without keys is one all the same: its rows are written)
         const int count = chunk > 0 ? own * max(1, ((k1 - k0 + PK_T - 1) / PK_T + chunk - 1) / chunk) : own;
@@ -531,7 +532,8 @@ __global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float*
     if (!there || lo < 0) return;
     const int q0 = min(max(a.cu_q[lo], 0), (int)a.total_q), q1 = min(max(a.cu_q[lo + 1], q0), (int)a.total_q);
     if (tok < q0 || tok >= q1) return;
-    const int k0 = min(max(a.cu_k[lo], 0), (int)a.total_k), nk = min(max(a.cu_k[lo + 1], k0), (int)a.total_k) - k0;
+    const int k0 = min(max(a.cu_k[lo], 0), (int)a.total_k), room = min(max(a.cu_k[lo + 1], k0), (int)a.total_k) - k0;
+    const int nk = a.k_len ? min(max(a.k_len[lo], 0), room) : room;
     const int G = a.n_heads / a.n_kv, nq = q1 - q0, at = (int)(tok - q0), head = (int)(row - tok * a.n_heads);
     const bool empty = (a.causal ? at + nk - nq : nk - 1) < 0;
     // the shares of its row tile
