@@ -146,27 +146,39 @@ def _dt(t):
     raise TypeError("unsupported dtype %s" % t.dtype)
 
 
-def _rows(t, name):
-    """(pointer, leading dimension) of a bf16 matrix; of None, nothing."""
-    if t is None:
-        return None, 0
-    if t.dtype != torch.bfloat16:
+# (the calls below take some microseconds, so what is asked of each tensor on the way to them is asked once)
+def _matrix(t, name):
+    """(pointer, leading dimension, rows, values of a row) of a bf16 matrix."""
+    if t.dtype is not torch.bfloat16:
         raise TypeError("%s must be bfloat16, not %s" % (name, t.dtype))
-    if t.dim() != 2 or (t.numel() and t.stride(1) != 1 and t.shape[1] != 1):
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix with unit stride along its last axis" % name)
+    (n, d), (ld, unit) = t.shape, t.stride()
+    if unit != 1 and d > 1 and n:
         raise ValueError("%s must be a matrix with unit stride along its last axis" % name)
     # (the stride of a single row says nothing)
-    return _ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), ld if n > 1 else d, n, d
+
+
+def _rows(t, name, n=None, d=None):
+    """(pointer, leading dimension) of a bf16 matrix, of n x d if these are given; of None, nothing."""
+    if t is None:
+        return None, 0
+    p, ld, n_, d_ = _matrix(t, name)
+    if n is not None and (n_ != n or d_ != d):
+        raise ValueError("%s must have the shape %s" % (name, (n, d)))
+    return p, ld
 
 
 def _flat(t, name, dtype, numel):
     """Pointer of a contiguous tensor of so many values; None stays None."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
     if t.numel() != numel or not t.is_contiguous():
         raise ValueError("%s must be %d contiguous values" % (name, numel))
-    return _ptr(t)
+    return t.data_ptr()
 
 
 def _same_shape(name, t, like):
@@ -216,6 +228,7 @@ class Context:
         if rc != 0:
             raise AgzoError(rc, "agzo_create failed")
         self.h = h
+        self.device = self.stream.device.index
 
     def close(self):
         if getattr(self, "h", None):
@@ -361,8 +374,9 @@ class Context:
                                               _ptr(out), out.stride(0), n_seq, seq_len, n_heads, n_kv, rope_theta))
 
     def _same_device(self, *tensors):
+        device = self.device
         for t in tensors:
-            if t is not None and t.device != self.stream.device:
+            if t is not None and t.get_device() != device:
                 raise ValueError("a tensor on %s, and the context is of %s" % (t.device, self.stream.device))
 
     def ce_forward(self, L, W, X, loss, loss_dev, lse=None):
@@ -381,69 +395,63 @@ class Context:
 
     def glue_qk_norm_rope(self, q, k, positions, q_out, k_out, head_dim=128, q_gain=None, k_gain=None, eps=1e-6, rope_theta=1.0e6):
         """q [n][heads * head_dim], k [n][key heads * head_dim] -> q_out, k_out; either side may be None with its result."""
-        n = (q if q is not None else k).shape[0]
         self._same_device(q, k, positions, q_out, k_out, q_gain, k_gain)
-        heads, kv = self._heads(q, k, head_dim, n)
-        for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
-            _same_shape(name, t, like)
-        self._rc(self.lib.agzo_glue_qk_norm_rope(self.h, *_rows(q, "q"), *_rows(k, "k"), _flat(positions, "positions", torch.int32, n), *_rows(q_out, "q_out"),
-                                                 *_rows(k_out, "k_out"), n, heads, kv, head_dim, _flat(q_gain, "q_gain", torch.float32, head_dim),
-                                                 _flat(k_gain, "k_gain", torch.float32, head_dim), eps, rope_theta))
+        (pq, lq, _, wq), (pk, lk, n, wk) = self._heads(q, k, head_dim)
+        f32 = torch.float32
+        self._rc(self.lib.agzo_glue_qk_norm_rope(
+            self.h, pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n), *_rows(q_out, "q_out", n, wq), *_rows(k_out, "k_out", n, wk), n,
+            wq // head_dim, wk // head_dim, head_dim, _flat(q_gain, "q_gain", f32, head_dim), _flat(k_gain, "k_gain", f32, head_dim), eps, rope_theta))
 
     def glue_qk_norm_rope_backward(self, q, k, positions, dq_out, dk_out, dq, dk, head_dim=128, q_gain=None, k_gain=None, dq_gain=None, dk_gain=None,
                                    eps=1e-6, rope_theta=1.0e6):
-        n = (q if q is not None else k).shape[0]
+        """q, k: the inputs of glue_qk_norm_rope; dq_out, dk_out: the gradients with respect to its results -> dq, dk and, where given, dq_gain and
+        dk_gain (float32 [head_dim])."""
         self._same_device(q, k, positions, dq_out, dk_out, dq, dk, q_gain, k_gain, dq_gain, dk_gain)
-        heads, kv = self._heads(q, k, head_dim, n)
-        for name, t, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k), ("dq", dq, q), ("dk", dk, k)):
-            _same_shape(name, t, like)
+        (pq, lq, _, wq), (pk, lk, n, wk) = self._heads(q, k, head_dim)
         f32 = torch.float32
         self._rc(self.lib.agzo_glue_qk_norm_rope_backward(
-            self.h, *_rows(q, "q"), *_rows(k, "k"), _flat(positions, "positions", torch.int32, n), *_rows(dq_out, "dq_out"), *_rows(dk_out, "dk_out"),
-            *_rows(dq, "dq"), *_rows(dk, "dk"), n, heads, kv, head_dim, _flat(q_gain, "q_gain", f32, head_dim), _flat(k_gain, "k_gain", f32, head_dim),
-            _flat(dq_gain, "dq_gain", f32, head_dim), _flat(dk_gain, "dk_gain", f32, head_dim), eps, rope_theta))
+            self.h, pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n), *_rows(dq_out, "dq_out", n, wq), *_rows(dk_out, "dk_out", n, wk),
+            *_rows(dq, "dq", n, wq), *_rows(dk, "dk", n, wk), n, wq // head_dim, wk // head_dim, head_dim, _flat(q_gain, "q_gain", f32, head_dim),
+            _flat(k_gain, "k_gain", f32, head_dim), _flat(dq_gain, "dq_gain", f32, head_dim), _flat(dk_gain, "dk_gain", f32, head_dim), eps, rope_theta))
 
     @staticmethod
-    def _heads(q, k, head_dim, n):
-        out = []
-        for t in (q, k):
-            if t is not None and (t.shape[0] != n or t.shape[1] % head_dim):
-                raise ValueError("rows of %d values, %d of them: need %d of a multiple of %d" % (t.shape[1], t.shape[0], n, head_dim))
-            out.append(0 if t is None else t.shape[1] // head_dim)
-        return out
+    def _heads(q, k, head_dim):
+        if q is None and k is None:
+            raise ValueError("neither q nor k is given")
+        a = None if q is None else _matrix(q, "q")
+        b = (None, 0, a[2], 0) if k is None else _matrix(k, "k")
+        a = a or (None, 0, b[2], 0)
+        if a[2] != b[2] or a[3] % head_dim or b[3] % head_dim:
+            raise ValueError("%d rows of %d values, %d of %d: need as many rows, of multiples of %d" % (*a[2:], *b[2:], head_dim))
+        return a, b
 
-    def _packed(self, q, k, v, cu_q, cu_k, head_dim, scale, causal):
-        _same_shape("v", v, k)
-        a = AgzoPackedAttention()
-        (a.q, a.ldq), (a.k, a.ldk), (a.v, a.ldv) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
-        if q.shape[1] % head_dim or k.shape[1] % head_dim:
-            raise ValueError("rows of %d and %d values: need multiples of %d" % (q.shape[1], k.shape[1], head_dim))
-        a.n_q, a.n_k, a.n_seq = q.shape[0], k.shape[0], cu_q.numel() - 1
-        a.cu_q, a.cu_k = _flat(cu_q, "cu_q", torch.int32, a.n_seq + 1), _flat(cu_k, "cu_k", torch.int32, a.n_seq + 1)
-        a.n_heads, a.n_kv_heads, a.head_dim = q.shape[1] // head_dim, k.shape[1] // head_dim, head_dim
-        a.causal, a.scale = int(causal), head_dim ** -0.5 if scale is None else scale
-        return a
+    @staticmethod
+    def _packed(q, k, v, cu_q, cu_k, k_len, head_dim, scale, causal):
+        pq, lq, nq, wq = _matrix(q, "q")
+        pk, lk, nk, wk = _matrix(k, "k")
+        if wq % head_dim or wk % head_dim:
+            raise ValueError("rows of %d and %d values: need multiples of %d" % (wq, wk, head_dim))
+        pv, lv = _rows(v, "v", nk, wk)
+        n_seq, i32 = cu_q.numel() - 1, torch.int32
+        return AgzoPackedAttention(pq, pk, pv, lq, lk, lv, _flat(cu_q, "cu_q", i32, n_seq + 1), _flat(cu_k, "cu_k", i32, n_seq + 1), _flat(k_len, "k_len", i32, n_seq),
+                                   nq, nk, n_seq, wq // head_dim, wk // head_dim, head_dim, int(causal), head_dim ** -0.5 if scale is None else scale), nq, wq, nk, wk
 
     def glue_attention_packed(self, q, k, v, out, cu_q, cu_k, head_dim=128, scale=None, causal=True, lse=None, k_len=None):
         """q [n_q][heads * head_dim], k, v [n_k][key heads * head_dim] -> out like q; cu_q, cu_k: int32 offsets of the sequences
         (n_seq + 1 each); scale None: head_dim ** -0.5; lse: float32 [n_q][heads] or None; k_len: int32 [n_seq], how many keys each has
         of its room (a cache), or None: all."""
         self._same_device(q, k, v, out, cu_q, cu_k, lse, k_len)
-        a = self._packed(q, k, v, cu_q, cu_k, head_dim, scale, causal)
-        a.k_len = _flat(k_len, "k_len", torch.int32, a.n_seq)
-        _same_shape("out", out, q)
-        o, ldo = _rows(out, "out")
-        self._rc(self.lib.agzo_glue_attention_packed(self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, a.n_q * a.n_heads)))
+        a, nq, wq, _, _ = self._packed(q, k, v, cu_q, cu_k, k_len, head_dim, scale, causal)
+        o, ldo = _rows(out, "out", nq, wq)
+        self._rc(self.lib.agzo_glue_attention_packed(self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, nq * (wq // head_dim))))
 
     def glue_attention_packed_backward(self, q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, head_dim=128, scale=None, causal=True):
         """out, lse: of glue_attention_packed with the same arguments; dout: the gradient with respect to out -> dq, dk, dv."""
         self._same_device(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k)
-        a = self._packed(q, k, v, cu_q, cu_k, head_dim, scale, causal)
-        for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-            _same_shape(name, t, like)
-        (o, ldo), (do, lddo) = _rows(out, "out"), _rows(dout, "dout")
+        a, nq, wq, nk, wk = self._packed(q, k, v, cu_q, cu_k, None, head_dim, scale, causal)
         self._rc(self.lib.agzo_glue_attention_packed_backward(
-            self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, a.n_q * a.n_heads), do, lddo, *_rows(dq, "dq"), *_rows(dk, "dk"), *_rows(dv, "dv")))
+            self.h, ctypes.byref(a), *_rows(out, "out", nq, wq), _flat(lse, "lse", torch.float32, nq * (wq // head_dim)), *_rows(dout, "dout", nq, wq),
+            *_rows(dq, "dq", nq, wq), *_rows(dk, "dk", nk, wk), *_rows(dv, "dv", nk, wk)))
 
     def step_no_update(self, L, W, X, loss, K, eps, seed, flags, out_dev, B_out):
         self._rc(self.lib.agzo_step_no_update(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), K, eps,
