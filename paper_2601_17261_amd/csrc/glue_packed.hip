@@ -566,7 +566,7 @@ __global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float*
 
 // ---- backward --------------------------------------------------------------------------------------------------
 // Per row -lse / scale and -delta, delta = do . o, each as three bf16 (24 bits): what the scores and do v^T are to be corrected by, as further values
-// of the rows of q and do that are multiplied by ones.  (0 for rows that see nothing)
+// of the rows of q and do that are multiplied by ones.  (0 for rows that see nothing.)  The kernel of dq makes them for both
 __device__ __forceinline__ uint2 pk_split3(float f) {
     bf16_t h, m, l;
     split3_bf16(f, h, m, l);
@@ -575,31 +575,7 @@ __device__ __forceinline__ uint2 pk_split3(float f) {
 __device__ __forceinline__ float pk_join3(uint32_t a, uint32_t b) {
     return (__uint_as_float(a << 16) + __uint_as_float(a & 0xFFFF0000u)) + __uint_as_float(b << 16);
 }
-template <int HD>
-__global__ __launch_bounds__(256) void pk_delta_kernel(PackedArgs a, const bf16_t* __restrict__ o, int64_t ldo, const bf16_t* __restrict__ d, int64_t ldd,
-                                                       const float* __restrict__ lse, uint4* __restrict__ rowinfo) {
-    constexpr int LANES = HD / 8;
-    const int64_t rows = a.total_q * a.n_heads, row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-    if (row >= rows) return;
-    const int j = threadIdx.x % LANES;
-    const int64_t tok = row / a.n_heads, col = (row - tok * a.n_heads) * HD + 8 * j;
-    const uint4 x = *reinterpret_cast<const uint4*>(o + tok * ldo + col), y = *reinterpret_cast<const uint4*>(d + tok * ldd + col);
-    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        s = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), s);
-        s = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), s);
-    }
-#pragma unroll
-    for (int w = LANES / 2; w > 0; w >>= 1) s += __shfl_xor(s, w);
-    if (j != 0) return;
-    const float at = lse[row];
-    const uint2 u = pk_split3(at == -INFINITY ? 0.f : -at / a.scale), v = pk_split3(-s);
-    rowinfo[row] = make_uint4(u.x, u.y, v.x, v.y);
-}
-
-struct PkBackward { const bf16_t* dout; int64_t lddo; uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; float* part; };
+struct PkBackward { const bf16_t *out, *dout; int64_t ldo, lddo; const float* lse; uint4* rowinfo; bf16_t* dq; int64_t lddq; bf16_t* dk; int64_t lddk; bf16_t* dv; int64_t lddv; float* part; };
 
 // dq: the forward's shape, with do beside q in registers, and K read with and without transposition
 template <int HD, bool careful>
@@ -654,7 +630,27 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
             qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
             df[ks].u = *reinterpret_cast<const uint4*>(dsrc + 16 * ks);
         }
-        const uint4 parts = g.rowinfo[r.tok * a.n_heads + r.head];
+        uint4 parts, *const to = g.rowinfo + r.tok * a.n_heads + r.head;
+        if constexpr (careful) {
+            parts = *to;
+        } else {
+            const bf16_t* osrc = g.out + r.tok * g.ldo + (int64_t)r.head * HD + 8 * hi;
+            const float lse = g.lse[r.tok * a.n_heads + r.head];
+            PkFrag of[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) of[ks].u = *reinterpret_cast<const uint4*>(osrc + 16 * ks);
+            float s = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    s = fmaf(__uint_as_float(of[ks].w[w] << 16), __uint_as_float(df[ks].w[w] << 16), s);
+                    s = fmaf(__uint_as_float(of[ks].w[w] & 0xFFFF0000u), __uint_as_float(df[ks].w[w] & 0xFFFF0000u), s);
+                }
+            const uint2 l = pk_split3(lse == -INFINITY ? 0.f : -lse / a.scale), d = pk_split3(-pk_sum_halves(s));
+            parts = make_uint4(l.x, l.y, d.x, d.y);
+            if (r.mine && hi == 0) *to = parts;
+        }
         __builtin_amdgcn_s_waitcnt(0x0F70);
         info = make_float2(-sc * pk_join3(parts.x, parts.y), -pk_join3(parts.z, parts.w));
     };
@@ -1072,7 +1068,7 @@ int64_t pk_units(int64_t total, int n_seq, int n_kv) { return (total / PK_ROWS +
 // workgroup for each key head then, whatever its length) or where row tiles are fewer than the compute units: for about one share to each of two workgroups on a
 // compute unit, of 8 tiles and more (a share costs a workgroup's start, its sums and a launch that joins them), 128 of a sequence at most and 256 MB of sums.
 // Lengths are on the device: work is reckoned from their mean, and sequences of 16 tiles and more in the mean are taken to be uneven.  64 sequences of 200000
-// keys together, up to 16760: 361 us without, 190 so
+// keys together, up to 16760: 380 us without, 216 so
 int pk_chunk(const PackedArgs& a, int head_dim) {
     const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
     if (units < 1 || a.total_k < 1) return 0;
@@ -1084,7 +1080,7 @@ int pk_chunk(const PackedArgs& a, int head_dim) {
 int64_t pk_most_shares(const PackedArgs& a, int chunk) { return ((a.total_k + PK_T - 1) / PK_T + chunk - 1) / chunk; }
 
 // Shares of the rows that a tile of keys is multiplied with: few tiles of keys take several workgroups each, for about one to a compute unit, of four tiles of 64
-// rows and more in the mean.  1001 tokens of eight heads on one: 345 us without, 75 so
+// rows and more in the mean.  1001 tokens of eight heads on one: 301 us without, 37 so
 int pk_dkv_shares(const PackedArgs& a) {
     const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_k, a.n_seq, a.n_kv);
     if (units < 1) return 1;
@@ -1112,7 +1108,7 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
         part = static_cast<float*>(workspace);
         ml = reinterpret_cast<float2*>(part + shares * rows * HD);
         // (the row tiles and, for each share of a sequence more, as many as a sequence may have; numbers behind the last leave at once)
-        units = std::min<int64_t>(units + shares * (a.total_q * G / PK_ROWS + 1) * a.n_kv, 1 << 20);
+        units += shares * (a.total_q * G / PK_ROWS + 1) * a.n_kv;
     }
     if (units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, PkForwardOut{out, ldo, lse, part, ml, chunk});
@@ -1129,18 +1125,15 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
     if (attr_q != hipSuccess) return attr_q;
     if (attr_kv != hipSuccess) return attr_kv;
     const int64_t rows = a.total_q * a.n_heads, G = a.n_heads / a.n_kv;
-    const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv), blocks = (rows * (HD / 8) + 255) / 256;
-    if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv);
+    if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     uint4* info = static_cast<uint4*>(workspace);
     const int shares = pk_dkv_shares(a);
     const int64_t kv_rows = a.total_k * a.n_kv, kv_blocks = (kv_rows * (HD / 2) + 255) / 256;
     float* part = shares > 1 ? reinterpret_cast<float*>(info + rows) : nullptr;
-    const PkBackward b{g.dout, g.lddo, info, g.dq, g.lddq, g.dk, g.lddk, g.dv, g.lddv, part};
+    const PkBackward b{g.out, g.dout, g.ldo, g.lddo, g.lse, info, g.dq, g.lddq, g.dk, g.lddk, g.dv, g.lddv, part};
     hipError_t e = hipSuccess;
     if (rows > 0) {
-        hipLaunchKernelGGL(pk_delta_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, g.out, g.ldo, g.dout, g.lddo, g.lse, info);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
         hipLaunchKernelGGL(pk_dq_kernel<HD>, dim3((unsigned)dq_units), dim3(64 * PK_WAVES), SMEM, st, a, b);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
