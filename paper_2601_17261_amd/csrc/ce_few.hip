@@ -132,48 +132,64 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
     a.ms[tid * a.nch + blockIdx.x] = make_float2(mx, s);
 }
 
-// Loss and lse from the statistics, in one workgroup: a wave a token, sums in fp64
+// Loss and lse from the statistics, in one workgroup: 1, 2, 4, 8 or 16 waves a token, so that up to 16 tokens are looked at at once; sums in fp64
 __global__ __launch_bounds__(1024) void ce_few_finish_kernel(const float2* __restrict__ ms, const float* __restrict__ tl, const int32_t* __restrict__ ids, int M, int64_t V, int64_t nch,
                                                              float* __restrict__ lse, double* __restrict__ out) {
-    __shared__ double sum[16], count[16];
+    __shared__ float tops[16];
+    __shared__ double sums[16], logs[kCeFewTokens];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double loss = 0.0, n = 0.0;
-    for (int t = wave; t < M; t += 16) {
-        const float2* m = ms + t * nch;
-        double mx = -INFINITY, s = 0.0;
-        for (int64_t c0 = lane; c0 < nch; c0 += 64 * 8) {
-            float2 v[8];
+    // (the first wave's lanes: a token each)
+    const int id = threadIdx.x < M ? ids[threadIdx.x] : -1;
+    const bool counted = id >= 0 && id < V;
+    const float target = counted ? tl[threadIdx.x] : 0.f;
+    const int each = M > 8 ? 1 : M > 4 ? 2 : M > 2 ? 4 : M > 1 ? 8 : 16, stride = 64 * each, first = (wave % each) * 64 + lane;
+    for (int t0 = 0; t0 < M; t0 += 16 / each) {
+        const int t = t0 + wave / each;
+        float top = -INFINITY;
+        double s = 0.0;
+        if (t < M) {
+            const float2* m = ms + t * nch;
+            for (int64_t c0 = first; c0 < nch; c0 += stride * 8) {
+                float2 v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = m[min(c0 + 64 * u, nch - 1)];
-            float top = v[0].x;
+                for (int u = 0; u < 8; ++u) v[u] = m[min(c0 + stride * u, nch - 1)];
+                float now = top;
 #pragma unroll
-            for (int u = 1; u < 8; ++u) top = c0 + 64 * u < nch ? fmaxf(top, v[u].x) : top;
-            const double mn = fmax(mx, (double)top);
-            s = s > 0.0 ? s * exp(mx - mn) : s;
+                for (int u = 0; u < 8; ++u) now = fmaxf(now, v[u].x);              // (one that is there twice changes nothing)
+                const float base = now == -INFINITY ? 0.f : now;
+                s *= (double)__builtin_amdgcn_exp2f((top - base) * FEW_LOG2E);      // (0 to begin with)
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (c0 + 64 * u < nch && v[u].y != 0.f) s += (double)v[u].y * exp((double)v[u].x - mn);
-            mx = mn;
+                for (int u = 0; u < 8; ++u)
+                    if (c0 + stride * u < nch && v[u].y != 0.f) s += (double)(v[u].y * __builtin_amdgcn_exp2f((v[u].x - base) * FEW_LOG2E));
+                top = now;
+            }
+            float all = top;
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) all = fmaxf(all, __shfl_xor(all, off));
+            s = s == 0.0 ? 0.0 : s * (double)__builtin_amdgcn_exp2f((top - all) * FEW_LOG2E);
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+            top = all;
         }
-        double top = mx;
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) top = fmax(top, __shfl_xor(top, off));
-        s = s == 0.0 ? 0.0 : s * exp(mx - top);
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
-        const double l = log(s) + top;
-        const int id = ids[t];
-        if (lse && lane == 0) lse[t] = (float)l;
-        if (id >= 0 && id < V) {
-            loss += l - (double)tl[t];
-            n += 1.0;
+        if (lane == 0) { tops[wave] = top; sums[wave] = s; }
+        __syncthreads();
+        if (lane == 0 && wave % each == 0 && t < M) {
+            float all = top;
+            for (int w = 1; w < each; ++w) all = fmaxf(all, tops[wave + w]);
+            double sum = 0.0;
+            for (int w = 0; w < each; ++w) sum += sums[wave + w] == 0.0 ? 0.0 : sums[wave + w] * exp((double)tops[wave + w] - (double)all);
+            logs[t] = log(sum) + (double)all;
         }
+        __syncthreads();
     }
-    if (lane == 0) { sum[wave] = loss; count[wave] = n; }
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < 16; ++w) { loss += sum[w]; n += count[w]; }
-    *out = n > 0.0 ? loss / n : 0.0;
+    if (wave != 0) return;
+    const double l = lane < M ? logs[lane] : 0.0;
+    if (lse && lane < M) lse[lane] = (float)l;
+    double loss = counted ? l - (double)target : 0.0;
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(counted));
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) loss += __shfl_xor(loss, off);
+    if (lane == 0) *out = n > 0 ? loss / n : 0.0;
 }
 
 // A tile of 32 rows of 128 values, for a wave or a workgroup, which is read transposed: a lane gets four rows' values of a column with each read

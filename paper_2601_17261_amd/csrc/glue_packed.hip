@@ -550,11 +550,15 @@ __global__ __launch_bounds__(256) void pk_join_kernel(PackedArgs a, const float*
         const float f = s0 + j >= shares ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
         l += f == 0.f ? 0.f : f * m.y;
         const int n = min(LANES, shares - s0);
-#pragma unroll 4
-        for (int s = 0; s < n; ++s) {
-            const float w = __shfl(f, s, LANES);
-            const float4 v = *reinterpret_cast<const float4*>(part + ((int64_t)(s0 + s) * rows + row) * HD + 4 * j);
-            if (w != 0.f) { o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w); }
+        for (int s = 0; s < n; s += 4) {
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4*>(part + (min(s0 + s + u, shares - 1) * rows + row) * HD + 4 * j);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float w = __shfl(f, s + u, LANES);              // (0 from the last share on)
+                if (w != 0.f) { o.x = fmaf(w, v[u].x, o.x); o.y = fmaf(w, v[u].y, o.y); o.z = fmaf(w, v[u].z, o.z); o.w = fmaf(w, v[u].w, o.w); }
+            }
         }
     }
 #pragma unroll
@@ -1051,9 +1055,13 @@ __global__ __launch_bounds__(256) void pk_dkv_join_kernel(PackedArgs a, PkBackwa
     if (tok < a.cu_k[0] || tok >= a.cu_k[a.n_seq]) return;                    // a row of no sequence
     const int j = threadIdx.x % LANES;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < shares; ++i) {
-        const float4 v = *reinterpret_cast<const float4*>(g.part + (i * rows + row) * (2 * HD) + 4 * j);
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    for (int i = 0; i < shares; i += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const float4*>(g.part + (min(i + u, shares - 1) * rows + row) * (2 * HD) + 4 * j);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u < shares) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
     }
     const bool k = j < LANES / 2;
     const float f = k ? a.scale : 1.f;
@@ -1065,16 +1073,16 @@ __global__ __launch_bounds__(256) void pk_dkv_join_kernel(PackedArgs a, PkBackwa
 int64_t pk_units(int64_t total, int n_seq, int n_kv) { return (total / PK_ROWS + std::min<int64_t>(n_seq, total)) * n_kv; }
 
 // Tiles of 64 keys a share, 0: row tiles are not shared out.  They are where rows are few beside the keys (single new tokens: a sequence is a
-// workgroup for each key head then, whatever its length) or where row tiles are fewer than the compute units: for about one share to each of two workgroups on a
+// workgroup for each key head then, whatever its length) or where row tiles are fewer than the compute units: for about two shares to each of two workgroups on a
 // compute unit, of 8 tiles and more (a share costs a workgroup's start, its sums and a launch that joins them), 128 of a sequence at most and 256 MB of sums.
 // Lengths are on the device: work is reckoned from their mean, and sequences of 16 tiles and more in the mean are taken to be uneven.  64 sequences of 200000
-// keys together, up to 16760: 380 us without, 216 so
+// keys together, up to 16760: 380 us without, 206 so, 216 with one share to each
 int pk_chunk(const PackedArgs& a, int head_dim) {
     const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
     if (units < 1 || a.total_k < 1) return 0;
     const int64_t all = (a.total_k + PK_T - 1) / PK_T, mean = (a.total_k / std::max(1, a.n_seq) + PK_T - 1) / PK_T;
     if (mean < 16 || !(a.total_q * G * 8 <= a.total_k || units < 256)) return 0;
-    const int64_t chunk = std::max<int64_t>({8, (units * mean + 511) / 512, (all + 127) / 128, all * rows * head_dim * 4 / (1LL << 28)});
+    const int64_t chunk = std::max<int64_t>({8, (units * mean + 1023) / 1024, (all + 127) / 128, all * rows * head_dim * 4 / (1LL << 28)});
     return (int)std::min<int64_t>(chunk, 1 << 20);
 }
 int64_t pk_most_shares(const PackedArgs& a, int chunk) { return ((a.total_k + PK_T - 1) / PK_T + chunk - 1) / chunk; }
