@@ -13,41 +13,48 @@ namespace agzo {
 
 namespace {
 
-// *scale = g / max(count, 1), count of the rows whose id is an output; rowf: 1 for these, 0 for the others; one workgroup
-__global__ __launch_bounds__(1024) void ce_factor_kernel(const int32_t* __restrict__ ids, int64_t M, int64_t V, const double* __restrict__ g, float* __restrict__ rowf, float* __restrict__ scale) {
-    __shared__ int red[16];
+// What a piece's products need, in one launch (by itself each of these is a launch of some 5 us and next to no work): its blocks are
+//   one, for the first piece: *scale = g / max(count, 1), count of the rows whose id is an output; rowf: 1 for these, 0 for the others
+//   tiles of 64 x 64 of y [C][ldy] = x^T of x [R][ldx], for X (first piece) and for the piece of W; columns R .. ldy of y are zeros (rows C and on are not written), and
+//     with ids those of the rows that are not counted: D is 0 there, and a value that is not finite would make NaNs of it
+//   256 values each of the columns from .. to of rows of ld values <- 0, for D and D^T, whose products end before them
+struct CeFlip { const bf16_t* x; int64_t ldx, R, C; bf16_t* y; int64_t ldy; int64_t blocks; };
+struct CeZero { bf16_t* y; int64_t rows, ld, from, to; int64_t blocks; };
+struct CePrepare {
+    const int32_t* ids; int64_t M, V; const double* g; float *rowf, *scale; int64_t count_blocks;
+    CeFlip X, W;
+    CeZero D, Dt;
+};
+__device__ __forceinline__ void ce_count(const CePrepare& a) {
+    __shared__ int red[4];
     int n = 0;
-    for (int64_t t = threadIdx.x; t < M; t += 1024) n += ids[t] >= 0 && ids[t] < V;
+    for (int64_t t0 = threadIdx.x; t0 < a.M; t0 += 256 * 8) {
+        int32_t id[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) id[u] = a.ids[min(t0 + 256 * u, a.M - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (t0 + 256 * u < a.M) {
+                const bool counted = id[u] >= 0 && id[u] < a.V;
+                n += counted;
+                a.rowf[t0 + 256 * u] = counted ? 1.f : 0.f;
+            }
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
     __syncthreads();
-    n = 0;
-    for (int w = 0; w < 16; ++w) n += red[w];
-    if (threadIdx.x == 0) *scale = (float)((g ? *g : 1.0) / (double)max(n, 1));
-    for (int64_t t = threadIdx.x; t < M; t += 1024) rowf[t] = ids[t] >= 0 && ids[t] < V ? 1.f : 0.f;
+    if (threadIdx.x == 0) *a.scale = (float)((a.g ? *a.g : 1.0) / (double)max(red[0] + red[1] + red[2] + red[3], 1));
 }
-
-// columns from .. to of rows of ld values <- 0
-__global__ __launch_bounds__(256) void ce_zero_kernel(bf16_t* __restrict__ y, int64_t rows, int64_t ld, int64_t from, int64_t to) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, w = to - from;
-    if (i >= rows * w) return;
-    const int64_t row = i / w;
-    y[row * ld + from + (i - row * w)] = 0;
-}
-
-// y [C][ldy] = x^T of x [R][ldx] in 64 x 64 tiles; columns R .. ldy of y are zeros (rows C and on are not written), and with ids those of the rows
-// that are not counted: D is 0 there, and a value that is not finite would make NaNs of it
-__global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict__ x, int64_t ldx, int64_t R, int64_t C, bf16_t* __restrict__ y, int64_t ldy,
-                                                        const int32_t* __restrict__ ids, int64_t V) {
+__device__ __forceinline__ void ce_flip(const CeFlip& a, const int32_t* ids, int64_t V, int64_t block) {
     __shared__ bf16_t tile[64][66];
-    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    const int64_t across = (a.ldy + 63) / 64, r0 = block % across * 64, c0 = block / across * 64;
     const int t = threadIdx.x;
     for (int i = t; i < 64 * 8; i += 256) {
         const int r = i >> 3, c = (i & 7) * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
-        const bool counted = !ids || (r0 + r < R && ids[r0 + r] >= 0 && ids[r0 + r] < V);
-        if (counted && r0 + r < R && c0 + c < C) v = *reinterpret_cast<const uint4*>(x + (r0 + r) * ldx + c0 + c);      // (C is a multiple of 8)
+        const bool counted = !ids || (r0 + r < a.R && ids[r0 + r] >= 0 && ids[r0 + r] < V);
+        if (counted && r0 + r < a.R && c0 + c < a.C) v = *reinterpret_cast<const uint4*>(a.x + (r0 + r) * a.ldx + c0 + c);      // (C is a multiple of 8)
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) *reinterpret_cast<uint32_t*>(&tile[r][c + 2 * k]) = w[k];
@@ -55,12 +62,29 @@ __global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict
     __syncthreads();
     for (int i = t; i < 64 * 8; i += 256) {
         const int c = i >> 3, r = (i & 7) * 8;
-        if (c0 + c >= C || r0 + r >= ldy) continue;
+        if (c0 + c >= a.C || r0 + r >= a.ldy) continue;
         uint32_t w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[r + 2 * k][c] | (uint32_t)tile[r + 2 * k + 1][c] << 16;
-        *reinterpret_cast<uint4*>(y + (c0 + c) * ldy + r0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(a.y + (c0 + c) * a.ldy + r0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+__device__ __forceinline__ void ce_zero(const CeZero& a, int64_t block) {
+    const int64_t i = block * 256 + threadIdx.x, w = a.to - a.from;
+    if (i >= a.rows * w) return;
+    const int64_t row = i / w;
+    a.y[row * a.ld + a.from + (i - row * w)] = 0;
+}
+__global__ __launch_bounds__(256) void ce_prepare_kernel(const CePrepare a) {
+    int64_t b = blockIdx.x;
+    if (b < a.count_blocks) return ce_count(a);
+    b -= a.count_blocks;
+    if (b < a.X.blocks) return ce_flip(a.X, a.ids, a.V, b);
+    b -= a.X.blocks;
+    if (b < a.W.blocks) return ce_flip(a.W, nullptr, 0, b);
+    b -= a.W.blocks;
+    if (b < a.D.blocks) return ce_zero(a.D, b);
+    ce_zero(a.Dt, b - a.D.blocks);
 }
 
 // D and D^T of a piece, from its logits z [M][ldz]: outputs v0 .. v0 + n; D [M][ldd] zero from column n on, D^T [n][ldt] zero from column M on
@@ -174,14 +198,13 @@ CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) 
     return l;
 }
 
-hipError_t transpose(const bf16_t* x, int64_t ldx, int64_t R, int64_t C, bf16_t* y, int64_t ldy, const int32_t* ids, int64_t V, hipStream_t st) {
-    hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)((ldy + 63) / 64), (unsigned)((C + 63) / 64)), dim3(256), 0, st, x, ldx, R, C, y, ldy, ids, V);
-    return hipGetLastError();
-}
-
-hipError_t zero_columns(bf16_t* y, int64_t rows, int64_t ld, int64_t from, int64_t to, hipStream_t st) {
-    if (from >= to) return hipSuccess;
-    hipLaunchKernelGGL(ce_zero_kernel, dim3((unsigned)((rows * (to - from) + 255) / 256)), dim3(256), 0, st, y, rows, ld, from, to);
+CeFlip flip(const bf16_t* x, int64_t ldx, int64_t R, int64_t C, bf16_t* y, int64_t ldy) { return CeFlip{x, ldx, R, C, y, ldy, (ldy + 63) / 64 * ((C + 63) / 64)}; }
+CeZero zero_columns(bf16_t* y, int64_t rows, int64_t ld, int64_t from, int64_t to) { return CeZero{y, rows, ld, from, to, from < to ? (rows * (to - from) + 255) / 256 : 0}; }
+hipError_t prepare(const CePrepare& a, hipStream_t st) {
+    const int64_t blocks = a.count_blocks + a.X.blocks + a.W.blocks + a.D.blocks + a.Dt.blocks;
+    if (blocks == 0) return hipSuccess;
+    if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(ce_prepare_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
@@ -210,20 +233,23 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
     } while (0)
     if (l.few) {
         CE_TRY(launch_ce_few_d(a.X, a.ldx, a.W, a.ldw, a.M, a.V, a.d, a.ids, a.lse, a.g, scale, D, l.width, a.dW ? Dt : nullptr, st));
-    } else {
-        hipLaunchKernelGGL(ce_factor_kernel, dim3(1), dim3(1024), 0, st, a.ids, a.M, a.V, a.g, rowf, scale);
-        CE_TRY(hipGetLastError());
-        if (a.dW && !l.few_w) CE_TRY(transpose(a.X, a.ldx, a.M, a.d, Xt, l.kt, a.ids, a.V, st));
     }
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
         const int64_t n = std::min(l.piece, a.V - v0), width = ce_width(n, l.tiles_x ? l.shares : 1);
         const bf16_t* W = a.W + v0 * a.ldw;
+        const bool tiles_z = !l.few && gemm_bf16_grad_fits(a.M, n, a.d);
+        if (!l.few) {
+            CePrepare p{a.ids, a.M, a.V, a.g, rowf, scale, v0 == 0, {}, {}, {}, {}};
+            if (v0 == 0 && a.dW && !l.few_w) p.X = flip(a.X, a.ldx, a.M, a.d, Xt, l.kt);
+            if (a.dX && l.tiles_x) p.W = flip(W, a.ldw, n, a.d, Wt, width);
+            if (tiles_z && a.dX) p.D = zero_columns(D, a.M, width, n, width);
+            if (tiles_z && a.dW) p.Dt = zero_columns(Dt, n, l.kt, a.M, l.kt);
+            CE_TRY(prepare(p, st));
+        }
         if (l.few) {
             // (D is there)
-        } else if (gemm_bf16_grad_fits(a.M, n, a.d)) {
+        } else if (tiles_z) {
             CE_TRY(launch_gemm_bf16_softmax_grad(a.X, a.ldx, W, a.ldw, a.M, n, a.d, v0, a.ids, a.lse, rowf, D, width, Dt, l.kt, st));
-            if (a.dX) CE_TRY(zero_columns(D, a.M, width, n, width, st));
-            if (a.dW) CE_TRY(zero_columns(Dt, n, l.kt, a.M, l.kt, st));
         } else {
             CE_TRY(product(a.X, a.ldx, W, a.ldw, a.M, n, a.d, z, n, st));
             hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(width / 64), (unsigned)(l.kt / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.ids, a.lse, rowf, D, width, Dt, l.kt);
@@ -247,7 +273,6 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
             CE_TRY(launch_ce_few_dx(D, width, W, a.ldw, a.M, n, a.d, l.shares, v0 > 0, sum, st));
             continue;
         }
-        CE_TRY(transpose(W, a.ldw, n, a.d, Wt, width, nullptr, 0, st));
         CE_TRY(launch_gemm_bf16_sum(D, width, Wt, width, a.M, a.d, width / l.shares, l.shares, sum, v0 > 0, st));
     }
 #undef CE_TRY
