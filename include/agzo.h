@@ -329,10 +329,11 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
  *   ce_forward: *loss_dev = mean over the counted rows of lse_t - y_t[id] (0 if there are none) and, where wanted, lse [n_tokens] device fp32,
  *     lse_t = log sum exp of row t's logits, of every row.  bf16 and fp32 layers; the loss is agzo_layer_forward_sketch's, bit for
  *     bit for fp32 layers and from 33 tokens on (fewer have sums of their own order).
- *   ce_backward (bf16 layers): with D = (softmax(Y) - onehot(id)) g / count in the counted rows, 0 in the others, dX = D W [n_tokens][d_in]
- *     and dW = D^T X [d_out][d_in], bf16, overwritten; either may be NULL.  lse: of ce_forward with the same arguments; g = *g_dev (1 if NULL).  The
- *     logits are made again for a piece of the outputs at a time, D is rounded to bf16 for the products, sums are fp32, in an order that
- *     depends on the shape alone.  Workspace: three to five buffers of a piece, of 2^27 values at most unless n_tokens or d_in pass 2^17.
+ *   ce_backward: with D = (softmax(Y) - onehot(id)) g / count in the counted rows, 0 in the others, dX = D W [n_tokens][d_in]
+ *     and dW = D^T X [d_out][d_in], of the layer's type, overwritten; either may be NULL.  lse: of ce_forward with the same arguments; g = *g_dev (1 if NULL).  The
+ *     logits are made again for a piece of the outputs at a time; of bf16 layers D without g / count is rounded to bf16 for the products and sums are
+ *     fp32, of fp32 layers D is fp32 and sums are fp64, those over pieces fp32; their order depends on the shape alone.  Workspace: three to five buffers
+ *     of a piece, of 2^27 bf16 or 2^26 fp32 values at most unless n_tokens or d_in pass 2^17.
  * Device, workspace and captures as for the calls on packed batches.
  * Errors: AGZO_EINVAL for a bad layer or loss, NULL or misaligned tensors, outputs that overlap an input or each other, more than 2^21
  * tokens or inputs (backward). */

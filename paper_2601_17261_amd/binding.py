@@ -147,10 +147,10 @@ def _dt(t):
 
 
 # (the calls below take some microseconds, so what is asked of each tensor on the way to them is asked once)
-def _matrix(t, name):
-    """(pointer, leading dimension, rows, values of a row) of a bf16 matrix."""
-    if t.dtype is not torch.bfloat16:
-        raise TypeError("%s must be bfloat16, not %s" % (name, t.dtype))
+def _matrix(t, name, dtype=torch.bfloat16):
+    """(pointer, leading dimension, rows, values of a row) of a matrix, bf16 unless another type is asked for."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
     if t.dim() != 2:
         raise ValueError("%s must be a matrix with unit stride along its last axis" % name)
     (n, d), (ld, unit) = t.shape, t.stride()
@@ -160,11 +160,11 @@ def _matrix(t, name):
     return t.data_ptr(), ld if n > 1 else d, n, d
 
 
-def _rows(t, name, n=None, d=None):
-    """(pointer, leading dimension) of a bf16 matrix, of n x d if these are given; of None, nothing."""
+def _rows(t, name, n=None, d=None, dtype=torch.bfloat16):
+    """(pointer, leading dimension) of a matrix, of n x d if these are given; of None, nothing."""
     if t is None:
         return None, 0
-    p, ld, n_, d_ = _matrix(t, name)
+    p, ld, n_, d_ = _matrix(t, name, dtype)
     if n is not None and (n_ != n or d_ != d):
         raise ValueError("%s must have the shape %s" % (name, (n, d)))
     return p, ld
@@ -391,7 +391,7 @@ class Context:
         _same_shape("dX", dX, X)
         _same_shape("dW", dW, W)
         self._rc(self.lib.agzo_ce_backward(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), _flat(lse, "lse", torch.float32, L.n_tokens),
-                                           _flat(g_dev, "g_dev", torch.float64, 1), *_rows(dX, "dX"), *_rows(dW, "dW")))
+                                           _flat(g_dev, "g_dev", torch.float64, 1), *_rows(dX, "dX", dtype=X.dtype), *_rows(dW, "dW", dtype=X.dtype)))
 
     def glue_qk_norm_rope(self, q, k, positions, q_out, k_out, head_dim=128, q_gain=None, k_gain=None, eps=1e-6, rope_theta=1.0e6):
         """q [n][heads * head_dim], k [n][key heads * head_dim] -> q_out, k_out; either side may be None with its result."""

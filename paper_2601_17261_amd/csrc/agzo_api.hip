@@ -1371,7 +1371,7 @@ int check_device(agzo_ctx* ctx) {
 }
 
 struct Named { const char* name; Rows rows; };
-Named named(const char* name, const void* at, int64_t ld, int64_t n, int64_t d) { return Named{name, Rows{reinterpret_cast<uintptr_t>(at), 2 * ld, at ? n : 0, 2 * d}}; }
+Named named(const char* name, const void* at, int64_t ld, int64_t n, int64_t d, int64_t size = 2) { return Named{name, Rows{reinterpret_cast<uintptr_t>(at), size * ld, at ? n : 0, size * d}}; }
 // outputs that overlap each other or an input; in_place: inputs that an output may be (NULL: none), as pairs of indices
 int check_apart(agzo_ctx* ctx, std::initializer_list<Named> outs, std::initializer_list<Named> ins, std::initializer_list<std::pair<int, int>> in_place = {}) {
     int o = 0;
@@ -1460,14 +1460,27 @@ int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const vo
                      const double* g_dev, void* dX, int64_t lddx, void* dW, int64_t lddw) {
     agzo_layer c;
     TRY(check_ce(ctx, L, W, X, loss, c));
-    if (c.dtype != AGZO_BF16) return fail(ctx, AGZO_EINVAL, "gradients are made for bf16 layers");
     if (c.n_tokens > (1LL << 21) || c.d_in > (1LL << 21)) return fail(ctx, AGZO_EINVAL, "more than 2^21 tokens or inputs");
     if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3)) return fail(ctx, AGZO_EINVAL, "lse is NULL or misaligned");
     if (!dX && !dW) return fail(ctx, AGZO_EINVAL, "neither dX nor dW is wanted");
-    if (dX) TRY(check_glue(ctx, c.n_tokens, c.d_in, {dX}, {lddx}));
-    if (dW) TRY(check_glue(ctx, c.d_out, c.d_in, {dW}, {lddw}));
-    TRY(check_apart(ctx, {named("dX", dX, lddx, c.n_tokens, c.d_in), named("dW", dW, lddw, c.d_out, c.d_in)},
-                    {named("X", X, c.ldx, c.n_tokens, c.d_in), named("W", W, c.ldw, c.d_out, c.d_in)}));
+    const bool f32 = c.dtype == AGZO_F32;
+    if (f32) {
+        if ((dX && lddx < c.d_in) || (dW && lddw < c.d_in)) return fail(ctx, AGZO_EINVAL, "leading dimension below d_in");
+        if ((reinterpret_cast<uintptr_t>(dX) | reinterpret_cast<uintptr_t>(dW)) & 3) return fail(ctx, AGZO_EINVAL, "dX or dW is misaligned");
+    } else {
+        if (dX) TRY(check_glue(ctx, c.n_tokens, c.d_in, {dX}, {lddx}));
+        if (dW) TRY(check_glue(ctx, c.d_out, c.d_in, {dW}, {lddw}));
+    }
+    const int64_t size = f32 ? 4 : 2;
+    TRY(check_apart(ctx, {named("dX", dX, lddx, c.n_tokens, c.d_in, size), named("dW", dW, lddw, c.d_out, c.d_in, size)},
+                    {named("X", X, c.ldx, c.n_tokens, c.d_in, size), named("W", W, c.ldw, c.d_out, c.d_in, size)}));
+    if (f32) {
+        TRY(reserve(ctx, ce_grad_f32_workspace_bytes(c.n_tokens, c.d_out, c.d_in, dX != nullptr, dW != nullptr)));
+        const CeGradF32Args a{static_cast<const float*>(X), c.ldx, static_cast<const float*>(W), c.ldw, c.n_tokens, c.d_out, c.d_in,
+                              static_cast<const int32_t*>(loss->target), lse, g_dev, static_cast<float*>(dX), lddx, static_cast<float*>(dW), lddw};
+        HIPCHK(launch_ce_grad_f32(a, ctx->ws, ctx->stream));
+        return AGZO_OK;
+    }
     TRY(reserve(ctx, ce_grad_workspace_bytes(c.n_tokens, c.d_out, c.d_in, dX != nullptr, dW != nullptr)));
     const CeGradArgs a{static_cast<const bf16_t*>(X), c.ldx, static_cast<const bf16_t*>(W), c.ldw, c.n_tokens, c.d_out, c.d_in,
                        static_cast<const int32_t*>(loss->target), lse, g_dev, static_cast<bf16_t*>(dX), lddx, static_cast<bf16_t*>(dW), lddw};

@@ -367,6 +367,17 @@ struct CeGradArgs {
 };
 size_t ce_grad_workspace_bytes(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw);
 hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st);
+// ce_grad_f32.hip : the same of fp32 layers
+struct CeGradF32Args {
+    const float* X; int64_t ldx;
+    const float* W; int64_t ldw;
+    int64_t M, V, d;
+    const int32_t* ids; const float* lse; const double* g;
+    float* dX; int64_t lddx;
+    float* dW; int64_t lddw;
+};
+size_t ce_grad_f32_workspace_bytes(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw);
+hipError_t launch_ce_grad_f32(const CeGradF32Args& a, void* workspace, hipStream_t st);
 // out[b] = scale * sum(partials[b*n .. b*n+n)), b < nout
 hipError_t launch_finish_loss(const double* partials, int n, double scale, double* out, int nout, hipStream_t st);
 hipError_t launch_two_point(double* out4, float eps, int one_sided, hipStream_t st);

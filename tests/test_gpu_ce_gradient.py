@@ -77,6 +77,52 @@ def test_one_of_the_gradients_and_an_upstream_one():
         assert all(torch.equal(r[n], both[n]) for n in ("dx", "dw") if r[n] is not None)
 
 
+@pytest.mark.parametrize("n,d,v,pad", [(1, 1, 1, 0), (3, 5, 7, 2), (33, 65, 129, 1), (200, 100, 1001, 0), (700, 384, 5000, 4),
+                                       # several pieces of the outputs
+                                       (3, 40, 7000001, 0)])
+def test_layers_in_fp32(n, d, v, pad):
+    ctx = binding.Context()
+    w, x, ids = make(n + v, n, d, v, dtype=torch.float32, pad=pad)
+    ids[0] = v - 1
+    if n > 2:
+        ids[1] = v + 3
+    want, got = exact(w, x, ids), run(ctx, w, x, ids)
+    # steps of 2^-24: a logit's, lse's, their difference's and the exponential's to D, three of the results' and one a piece
+    u, W, X = 2.0 ** -24, w.double().abs(), x.double().abs()
+    y = x.double() @ w.double().T
+    p = torch.where(want["d"] != 0, (y - want["lse"][:, None]).exp(), 0.0)
+    count = max(1, int(((ids >= 0) & (ids < v)).sum()))
+    off = u * (p * (2 * y.abs() + 2 * want["lse"].abs()[:, None] + 8) / count + 2 * want["d"].abs())
+    assert abs(float(got["loss"]) - float(want["loss"])) <= 2e-6 * max(1.0, abs(float(want["loss"])))
+    for name, bound in (("dx", off @ W + 6 * u * (want["d"].abs() @ W)), ("dw", off.T @ X + 6 * u * (want["d"].abs().T @ X))):
+        bad = ~((got[name].double() - want[name]).abs() <= bound + 1e-37)
+        assert not bad.any(), (name, int(bad.sum()), float(((got[name].double() - want[name]).abs() - bound).max()))
+
+
+def test_fp32_rows_that_are_not_counted_one_gradient_and_refusals():
+    ctx = binding.Context()
+    w, x, ids = make(6, 50, 33, 90, dtype=torch.float32)
+    ids[7] = -1
+    both = run(ctx, w, x, ids)
+    assert (both["dx"][7] == 0).all()
+    y = x.clone()
+    y[7] = float("nan")
+    L, loss = binding.make_layer(w, y), binding.make_loss(ids, binding.LOSS_CE)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ctx.ce_backward(L, w, y, loss, both["lse"], dx, dw)
+    assert torch.equal(dw, both["dw"]) and torch.equal(dx, both["dx"])
+    for kw in (dict(dx=False), dict(dw=False)):
+        r = run(ctx, w, x, ids, **kw)
+        assert all(torch.equal(r[n], both[n]) for n in ("dx", "dw") if r[n] is not None)
+    L = binding.make_layer(w, x)
+    with pytest.raises(TypeError):
+        ctx.ce_backward(L, w, x, loss, both["lse"], dx.bfloat16(), dw)
+    with pytest.raises(binding.AgzoError):
+        ctx.ce_backward(L, w, x, loss, both["lse"], x, dw)
+    with pytest.raises(binding.AgzoError):
+        ctx.ce_backward(L, w, x, loss, both["lse"], dw[:50], dw)
+
+
 def test_no_row_counted():
     ctx = binding.Context()
     w, x, ids = make(5, 40, 64, 300)
