@@ -397,6 +397,8 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
 #pragma unroll
             for (int i = 0; i < 4; ++i) read_k(i);
             __builtin_amdgcn_sched_barrier(0);
+            // (of a SIMD's two waves the one that has matrix instructions to issue goes first, beside the other's maxima: 16001 tokens, 1074 -> 1047 us)
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 2 * KS; ++i) {
                 s[i & 1] = pk_mfma(f[i & 3], qf[i >> 1], i < 2 ? zero : s[i & 1]);
@@ -404,6 +406,7 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
                 else read_v(i + 4 - 2 * KS);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
             const bool mask = kb + PK_T - 1 > wfirst;                        // (wave-uniform)
             if (mask) {
                 const int rel = limit_of() - kb - 4 * hi;
@@ -447,6 +450,7 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
 #pragma unroll
             for (int e = 0; e < 8; e += 2) two(e);
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 4 * DB; ++i) {
                 acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
@@ -457,6 +461,7 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
     };
 #pragma unroll
     for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
