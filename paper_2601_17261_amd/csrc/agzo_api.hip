@@ -1408,8 +1408,10 @@ int packed_args(agzo_ctx* ctx, const agzo_packed_attention* a, PackedArgs& out) 
     if (!a) return fail(ctx, AGZO_EINVAL, "the attention's descriptor is NULL");
     if (a->n_heads < 1 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads || a->n_heads > 65535 || (a->head_dim != 64 && a->head_dim != 128) || a->n_seq < 0)
         return fail(ctx, AGZO_EINVAL, "bad attention shape: %d sequences, %d heads of %d values on %d key heads", a->n_seq, a->n_heads, a->head_dim, a->n_kv_heads);
-    if (a->n_q < 0 || a->n_k < 0 || a->n_k > 0x7FFFFFFFLL || a->n_q * (a->n_heads / a->n_kv_heads) > 0x7FFFFFFFLL || a->n_q > 0x7FFFFFFFLL)
-        return fail(ctx, AGZO_EINVAL, "%lld queries, %lld keys: too many", (long long)a->n_q, (long long)a->n_k);
+    // (rows and keys are counted in 32 bits, up to the end of the last tile.  A workgroup looks its sequence up, 64 of them at a time)
+    constexpr int64_t most = 0x7FFFFFFFLL - 1024;
+    if (a->n_q < 0 || a->n_k < 0 || a->n_k > most || a->n_q > most || a->n_q * (a->n_heads / a->n_kv_heads) > most || a->n_seq > 65536)
+        return fail(ctx, AGZO_EINVAL, "%d sequences, %lld queries, %lld keys: too many", a->n_seq, (long long)a->n_q, (long long)a->n_k);
     if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return fail(ctx, AGZO_EINVAL, "scale must be positive and finite");
     if (a->ldq >= (1LL << 22) || a->ldk >= (1LL << 22) || a->ldv >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "leading dimensions must be below 2^22");
     if (a->n_seq > 0 && (!a->cu_q || !a->cu_k || ((reinterpret_cast<uintptr_t>(a->cu_q) | reinterpret_cast<uintptr_t>(a->cu_k)) & 3)))

@@ -17,6 +17,7 @@
 // masked place's values, by 0, of which a value that is not finite makes a NaN.  Where a workgroup's results are not finite it goes over
 // its tiles once more with care: masked tiles then have such values taken out, and what the visible ones amount to is found by a product of two
 // indicators.
+#include <atomic>
 #include <type_traits>
 
 #include "agzo_internal.h"
@@ -1101,15 +1102,23 @@ int pk_dkv_shares(const PackedArgs& a) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(256 / units, rows / 4));
 }
 
+// so much LDS for a kernel, once on each device
 template <typename F>
-hipError_t pk_lds(F* f, int bytes) {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+hipError_t pk_lds(F* f, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (e != hipSuccess || (done.load(std::memory_order_relaxed) & bit)) return e;
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 template <int HD>
 hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
     constexpr int SMEM = 4 * PK_T * HD * 2;
-    static const hipError_t attr = pk_lds(pk_forward_kernel<HD>, SMEM);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t attr = pk_lds(pk_forward_kernel<HD>, SMEM, done);
     if (attr != hipSuccess) return attr;
     const int G = a.n_heads / a.n_kv, chunk = pk_chunk(a, HD);
     const int64_t rows = a.total_q * a.n_heads, blocks = (rows * (HD / 4) + 255) / 256;
@@ -1134,7 +1143,8 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
 template <int HD>
 hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* workspace, hipStream_t st) {
     constexpr int SMEM = 4 * PK_T * HD * 2, SMEM_KV = SMEM + 2 * PK_T * 20;
-    static const hipError_t attr_q = pk_lds(pk_dq_kernel<HD>, SMEM), attr_kv = pk_lds(pk_dkv_kernel<HD>, SMEM_KV);
+    static std::atomic<uint64_t> done_q{0}, done_kv{0};
+    const hipError_t attr_q = pk_lds(pk_dq_kernel<HD>, SMEM, done_q), attr_kv = pk_lds(pk_dkv_kernel<HD>, SMEM_KV, done_kv);
     if (attr_q != hipSuccess) return attr_q;
     if (attr_kv != hipSuccess) return attr_kv;
     const int64_t rows = a.total_q * a.n_heads, G = a.n_heads / a.n_kv;

@@ -278,6 +278,19 @@ def test_offsets_past_32_bits():
     assert torch.equal(dq, a["dq"]) and torch.equal(dk, a["dk"]) and torch.equal(dv, a["dv"])
 
 
+def test_many_sequences_and_too_many():
+    ctx = binding.Context()
+    klens = [3, 1, 2, 5] * 2048
+    q, k, v, d, cq, ck = make(31, [1] * len(klens), klens, 2, 1, 64)
+    check(run(ctx, q, k, v, None, cq, ck, 64), ref.attention(q, k, v, cq.tolist(), ck.tolist(), 64), cq, ck)
+    qlens = [2, 0, 70, 1, 3] * 20
+    q, k, v, d, cq, ck = make(32, qlens, qlens, 4, 2, 128)
+    check(run(ctx, q, k, v, d, cq, ck, 128), ref.attention(q, k, v, cq.tolist(), ck.tolist(), 128, dout=d), cq, ck)
+    cu = torch.zeros(65538, dtype=torch.int32, device="cuda")
+    with pytest.raises(binding.AgzoError):
+        ctx.glue_attention_packed(q, k, v, torch.empty_like(q), cu, cu, 128)
+
+
 def test_refusals():
     ctx = binding.Context()
     q, k, v, d, cq, ck = make(19, [8], [8], 4, 2, 64)
