@@ -307,8 +307,9 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  *   backward: out, lse of the forward call with the same arguments and the gradient dout -> dq, dk, dv (all three written, for all rows of
  *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
  * Inputs are only read; outputs may not overlap inputs or each other.
- * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, more than 2^16 sequences, keys or queries times heads of a key head from 2^31 - 1024 on, leading
- * dimensions from 2^22 on), scale not positive and finite, overlapping outputs, lengths in the backward call. */
+ * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, more than 2^16 sequences; n_k, or n_q times
+ * the heads of a key head, from 2^31 - 1024 on; leading dimensions from 2^22 on), scale not positive and finite, overlapping outputs, k_len in the
+ * backward call. */
 typedef struct {
     const void *q, *k, *v;       /* [n_q][n_heads head_dim], [n_k][n_kv_heads head_dim] twice */
     int64_t ldq, ldk, ldv;
