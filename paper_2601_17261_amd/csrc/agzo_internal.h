@@ -352,9 +352,13 @@ hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t 
 hipError_t launch_ce_few_d(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, const float* lse, const double* g,
                            float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st);
 int ce_few_dx_shares(int64_t M, int64_t n, int64_t d);
-hipError_t launch_ce_few_dx(const bf16_t* D, int64_t ldd, const bf16_t* W, int64_t ldw, int64_t M, int64_t n, int64_t d, int shares, bool add, float* sums, hipStream_t st);
-hipError_t launch_ce_few_dw(const bf16_t* Dt, int64_t ldt, const bf16_t* X, int64_t ldx, int64_t M, int64_t n, int64_t d, const int32_t* ids, int64_t V, const float* scale,
-                            bf16_t* dW, int64_t lddw, hipStream_t st);
+// of n outputs: dX's sums (sums NULL: not wanted) and dW (NULL: not wanted), in one launch
+struct CeFewGrad {
+    int64_t M, n, d;
+    const bf16_t* D; int64_t ldd; const bf16_t* W; int64_t ldw; int shares; bool add; float* sums;
+    const bf16_t* Dt; int64_t ldt; const bf16_t* X; int64_t ldx; const int32_t* ids; int64_t V; const float* scale; bf16_t* dW; int64_t lddw;
+};
+hipError_t launch_ce_few_grad(const CeFewGrad& a, hipStream_t st);
 
 // ce_grad.hip : gradient of that loss: dX [M][d], dW [V][d] bf16 (either may be NULL), g: device scalar (NULL: 1), lse: of every row
 struct CeGradArgs {

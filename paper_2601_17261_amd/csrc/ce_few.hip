@@ -229,13 +229,18 @@ __device__ __forceinline__ FewFrag few_order(const bf16_t* row, int s) {
 // turn.  Rows of W go through LDS, a wave's own 8 KB, so that no wave waits for another and no transposed copy of W is made; D's values straight from memory.
 // sums [shares][M][d], added to if this is not the first piece of the outputs.  7 tokens, 2048 <- 32000: 22 us (5.9 TB/s: W lies in the last cache by then);
 // a transposed copy and a product of it 51 and 340.  200 tokens, four blocks that read W each: 102, and 51 and 347
+struct FewDx { const bf16_t* D; int64_t ldd; const bf16_t* W; int64_t ldw; int64_t M, n, d; bool add; float* sums; int slices, shares; };
+constexpr int FEW_LDS = 4 * 32 * 256 + 4 * 32 * 33 * 4;
 template <int TB>
-__global__ __launch_bounds__(256) void ce_few_dx_kernel(const bf16_t* __restrict__ D, int64_t ldd, const bf16_t* __restrict__ W, int64_t ldw, int64_t M, int64_t n, int64_t d, bool add,
-                                                        float* __restrict__ sums) {
-    __shared__ __align__(1024) char stage[4][32 * 256];
-    __shared__ float red[4][32][33];
+__device__ __forceinline__ void ce_few_dx(const FewDx& a, char* lds, int64_t block) {
+    char (*stage)[32 * 256] = reinterpret_cast<char (*)[32 * 256]>(lds);
+    float (*red)[32][33] = reinterpret_cast<float (*)[32][33]>(lds + 4 * 32 * 256);
+    const bf16_t *const D = a.D, *const W = a.W;
+    const int64_t ldd = a.ldd, ldw = a.ldw, M = a.M, n = a.n, d = a.d;
+    // (a slice of dims, a share of the outputs, some tokens)
+    const int64_t slice = block % a.slices, share = block / a.slices % a.shares;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
-    const int64_t d0 = (int64_t)blockIdx.x * 128, m0 = (int64_t)blockIdx.z * (32 * TB);
+    const int64_t d0 = slice * 128, m0 = block / a.slices / a.shares * (32 * TB);
     const int64_t blocks = (n + 31) / 32;
     char* own = stage[wave];
     const FewTrans trans(lane);
@@ -254,7 +259,7 @@ __global__ __launch_bounds__(256) void ce_few_dx_kernel(const bf16_t* __restrict
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb) drow[tb] = D + min(m0 + 32 * tb + r, M - 1) * ldd + 4 * hi;
     floatx16 acc[TB][4] = {};
-    const int64_t first = (int64_t)blockIdx.y * 4 + wave, step = (int64_t)gridDim.y * 4;
+    const int64_t first = share * 4 + wave, step = (int64_t)a.shares * 4;
     if (first < blocks) load(first);
     for (int64_t b = first; b < blocks; b += step) {
 #pragma unroll
@@ -290,9 +295,9 @@ __global__ __launch_bounds__(256) void ce_few_dx_kernel(const bf16_t* __restrict
                     const int c = (tid >> 5) + 8 * u;
                     const int64_t tok = m0 + 32 * tb + c;
                     if (tok >= M) continue;
-                    float* to = sums + (blockIdx.y * M + tok) * d + d0 + 32 * db + dim;
+                    float* to = a.sums + (share * M + tok) * d + d0 + 32 * db + dim;
                     const float s = (red[0][dim][c] + red[1][dim][c]) + (red[2][dim][c] + red[3][dim][c]);
-                    *to = add ? *to + s : s;
+                    *to = a.add ? *to + s : s;
                 }
         }
 }
@@ -300,13 +305,18 @@ __global__ __launch_bounds__(256) void ce_few_dx_kernel(const bf16_t* __restrict
 // dW = *scale D^T X for up to 32 KB tokens, as many as D^T [n][32 KB] has columns: a workgroup has 128 dims, whose X lies in LDS (rows that are not counted as
 // zeros: D is 0 there, and a value that is not finite would make NaNs of it) and in registers from there, and its waves take 32 outputs in turn.
 // Bound by what it writes.  7 tokens, 2048 x 32000: 27 us (4.8 TB/s), a product of X transposed 72
+struct FewDw { const bf16_t* Dt; const bf16_t* X; int64_t ldx; int M; int64_t n, d; const int32_t* ids; int64_t V; const float* scale; bf16_t* dW; int64_t lddw; int slices, groups; };
 template <int KB>
-__global__ __launch_bounds__(256) void ce_few_dw_kernel(const bf16_t* __restrict__ Dt, const bf16_t* __restrict__ X, int64_t ldx, int M, int64_t n, int64_t d, const int32_t* __restrict__ ids,
-                                                        int64_t V, const float* __restrict__ scale, bf16_t* __restrict__ dW, int64_t lddw) {
-    __shared__ __align__(1024) char xs[KB][32 * 256];
+__device__ __forceinline__ void ce_few_dw(const FewDw& a, char* lds, int64_t block) {
+    char (*xs)[32 * 256] = reinterpret_cast<char (*)[32 * 256]>(lds);
+    const bf16_t *const Dt = a.Dt, *const X = a.X;
+    const int32_t* const ids = a.ids;
+    bf16_t* const dW = a.dW;
+    const int64_t ldx = a.ldx, n = a.n, d = a.d, V = a.V, lddw = a.lddw, group = block / a.slices;
+    const int M = a.M;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
-    const int64_t d0 = (int64_t)blockIdx.x * 128, blocks = (n + 31) / 32;
-    const float f = *scale;
+    const int64_t d0 = block % a.slices * 128, blocks = (n + 31) / 32;
+    const float f = *a.scale;
     for (int i = tid; i < 32 * KB * 16; i += 256) {
         const int row = i >> 4, c = i & 15, id = row < M ? ids[row] : -1;
         uint4 v = make_uint4(0, 0, 0, 0);
@@ -320,7 +330,7 @@ __global__ __launch_bounds__(256) void ce_few_dw_kernel(const bf16_t* __restrict
     for (int s = 0; s < 2 * KB; ++s)
 #pragma unroll
         for (int db = 0; db < 4; ++db) x[s][db] = trans.read(xs[s >> 1], s & 1, db);
-    for (int64_t b = (int64_t)blockIdx.y * 4 + wave; b < blocks; b += (int64_t)gridDim.y * 4) {
+    for (int64_t b = group * 4 + wave; b < blocks; b += (int64_t)a.groups * 4) {
         const int64_t out = b * 32 + r;
         const bf16_t* row = Dt + min(out, n - 1) * (32 * KB) + 4 * hi;
         FewFrag t[2 * KB];
@@ -342,6 +352,25 @@ __global__ __launch_bounds__(256) void ce_few_dw_kernel(const bf16_t* __restrict
             }
         }
     }
+}
+
+// Both beside each other, dX's workgroups first: what reads W out of the last cache leaves what writes dW the memory.  7 tokens, 2048 x 32000: 46 us for 22 and 27.  (With
+// four blocks of tokens the registers leave one wave a SIMD: 100 tokens, 1024 -> 50000: a gradient of 182 us, two launches 162)
+template <int TB, int KB>
+__global__ __launch_bounds__(256) void ce_few_grad_kernel(const FewDx x, const FewDw w, int64_t x_blocks) {
+    __shared__ __align__(1024) char lds[FEW_LDS];
+    if (blockIdx.x < x_blocks) ce_few_dx<TB>(x, lds, blockIdx.x);
+    else ce_few_dw<KB>(w, lds, blockIdx.x - x_blocks);
+}
+template <int TB>
+__global__ __launch_bounds__(256) void ce_few_dx_kernel(const FewDx x) {
+    __shared__ __align__(1024) char lds[FEW_LDS];
+    ce_few_dx<TB>(x, lds, blockIdx.x);
+}
+template <int KB>
+__global__ __launch_bounds__(256) void ce_few_dw_kernel(const FewDw w) {
+    __shared__ __align__(1024) char lds[KB * 32 * 256];
+    ce_few_dw<KB>(w, lds, blockIdx.x);
 }
 
 FewArgs few_args(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids) {
@@ -382,23 +411,32 @@ int ce_few_dx_shares(int64_t M, int64_t n, int64_t d) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, blocks / 32, 64}));
 }
 
-hipError_t launch_ce_few_dx(const bf16_t* D, int64_t ldd, const bf16_t* W, int64_t ldw, int64_t M, int64_t n, int64_t d, int shares, bool add, float* sums, hipStream_t st) {
-    if (M < 1 || shares < 1 || ldd < (n + 31) / 32 * 32 || ldd % 4) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((d + 127) / 128), (unsigned)shares, (unsigned)((M + 63) / 64));
-    if (M <= 32) hipLaunchKernelGGL(ce_few_dx_kernel<1>, grid, dim3(256), 0, st, D, ldd, W, ldw, M, n, d, add, sums);
-    else hipLaunchKernelGGL(ce_few_dx_kernel<2>, grid, dim3(256), 0, st, D, ldd, W, ldw, M, n, d, add, sums);
-    return hipGetLastError();
-}
-
-hipError_t launch_ce_few_dw(const bf16_t* Dt, int64_t ldt, const bf16_t* X, int64_t ldx, int64_t M, int64_t n, int64_t d, const int32_t* ids, int64_t V, const float* scale,
-                            bf16_t* dW, int64_t lddw, hipStream_t st) {
-    if (M < 1 || M > ldt || (ldt != 32 && ldt != 64 && ldt != 128)) return hipErrorInvalidValue;
-    const int64_t slices = (d + 127) / 128, groups = (n + 127) / 128;
-    // eight workgroups to a compute unit, no more: each has to read X first
-    const dim3 grid((unsigned)slices, (unsigned)std::max<int64_t>(1, std::min(groups, 2048 / slices)));
-    if (ldt == 32) hipLaunchKernelGGL(ce_few_dw_kernel<1>, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, n, d, ids, V, scale, dW, lddw);
-    else if (ldt == 64) hipLaunchKernelGGL(ce_few_dw_kernel<2>, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, n, d, ids, V, scale, dW, lddw);
-    else hipLaunchKernelGGL(ce_few_dw_kernel<4>, grid, dim3(256), 0, st, Dt, X, ldx, (int)M, n, d, ids, V, scale, dW, lddw);
+hipError_t launch_ce_few_grad(const CeFewGrad& a, hipStream_t st) {
+    const int64_t M = a.M, n = a.n, d = a.d, slices = (d + 127) / 128;
+    const bool dx = a.sums != nullptr, dw = a.dW != nullptr;
+    if (M < 1 || (dx && (a.shares < 1 || a.ldd < (n + 31) / 32 * 32 || a.ldd % 4)) || (dw && (M > a.ldt || (a.ldt != 32 && a.ldt != 64 && a.ldt != 128)))) return hipErrorInvalidValue;
+    const FewDx x{a.D, a.ldd, a.W, a.ldw, M, n, d, a.add, a.sums, (int)slices, a.shares};
+    // dW: eight workgroups to a compute unit, no more: each has to read X first
+    const FewDw w{a.Dt, a.X, a.ldx, (int)M, n, d, a.ids, a.V, a.scale, a.dW, a.lddw, (int)slices, (int)std::max<int64_t>(1, std::min((n + 127) / 128, 2048 / slices))};
+    const bool one = M <= 32;
+    const int64_t xb = dx ? slices * a.shares * ((M + (one ? 31 : 63)) / (one ? 32 : 64)) : 0, wb = dw ? slices * w.groups : 0;
+    if (xb + wb == 0) return hipSuccess;
+    if (xb + wb > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    const dim3 wg(256);
+    if (dx && dw && a.ldt != 128) {
+        if (one) hipLaunchKernelGGL((ce_few_grad_kernel<1, 1>), dim3((unsigned)(xb + wb)), wg, 0, st, x, w, xb);
+        else hipLaunchKernelGGL((ce_few_grad_kernel<2, 2>), dim3((unsigned)(xb + wb)), wg, 0, st, x, w, xb);
+        return hipGetLastError();
+    }
+    if (dx) {
+        if (one) hipLaunchKernelGGL(ce_few_dx_kernel<1>, dim3((unsigned)xb), wg, 0, st, x);
+        else hipLaunchKernelGGL(ce_few_dx_kernel<2>, dim3((unsigned)xb), wg, 0, st, x);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || !dw) return e;
+    }
+    if (a.ldt == 32) hipLaunchKernelGGL(ce_few_dw_kernel<1>, dim3((unsigned)wb), wg, 0, st, w);
+    else if (a.ldt == 64) hipLaunchKernelGGL(ce_few_dw_kernel<2>, dim3((unsigned)wb), wg, 0, st, w);
+    else hipLaunchKernelGGL(ce_few_dw_kernel<4>, dim3((unsigned)wb), wg, 0, st, w);
     return hipGetLastError();
 }
 

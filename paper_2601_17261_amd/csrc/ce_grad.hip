@@ -255,11 +255,13 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
             hipLaunchKernelGGL(ce_softmax_grad_kernel, dim3((unsigned)(width / 64), (unsigned)(l.kt / 64)), dim3(256), 0, st, z, n, a.M, v0, n, a.ids, a.lse, rowf, D, width, Dt, l.kt);
             CE_TRY(hipGetLastError());
         }
-        if (a.dW) {
-            bf16_t* dW = a.dW + v0 * a.lddw;
-            if (l.few_w) {
-                CE_TRY(launch_ce_few_dw(Dt, l.kt, a.X, a.ldx, a.M, n, a.d, a.ids, a.V, scale, dW, a.lddw, st));
-            } else if (ce_dw_stored(l, n, a.d)) {
+        bf16_t* dW = a.dW ? a.dW + v0 * a.lddw : nullptr;
+        const bool few_x = a.dX && !l.tiles_x, few_w = a.dW && l.few_w;
+        if (few_x || few_w)
+            CE_TRY(launch_ce_few_grad(CeFewGrad{a.M, n, a.d, D, width, W, a.ldw, l.shares, v0 > 0, few_x ? sum : nullptr,
+                                                Dt, l.kt, a.X, a.ldx, a.ids, a.V, scale, few_w ? dW : nullptr, a.lddw}, st));
+        if (a.dW && !l.few_w) {
+            if (ce_dw_stored(l, n, a.d)) {
                 CE_TRY(launch_gemm_bf16_scaled(Dt, l.kt, Xt, l.kt, n, a.d, l.kt, scale, dW, a.lddw, st));
             } else {
                 const bool fits = gemm_bf16_grad_fits(n, a.d, l.kt / l.shares_w);
@@ -268,11 +270,7 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
                 CE_TRY(join(wsum, fits ? l.shares_w : 1, n, a.d, scale, dW, a.lddw, st));
             }
         }
-        if (!a.dX) continue;
-        if (!l.tiles_x) {
-            CE_TRY(launch_ce_few_dx(D, width, W, a.ldw, a.M, n, a.d, l.shares, v0 > 0, sum, st));
-            continue;
-        }
+        if (!a.dX || !l.tiles_x) continue;
         CE_TRY(launch_gemm_bf16_sum(D, width, Wt, width, a.M, a.d, width / l.shares, l.shares, sum, v0 > 0, st));
     }
 #undef CE_TRY
