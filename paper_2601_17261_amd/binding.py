@@ -146,36 +146,43 @@ def _dt(t):
     raise TypeError("unsupported dtype %s" % t.dtype)
 
 
-# (the calls below take some microseconds, so what is asked of each tensor on the way to them is asked once)
-def _matrix(t, name, dtype=torch.bfloat16):
+# (the calls on packed batches take some microseconds, so what is asked of each tensor on the way to them is asked once.  device: an index; None: any)
+def _elsewhere(t, device):
+    raise ValueError("a tensor on %s, and the context is of cuda:%d" % (t.device, device))
+
+
+def _matrix(t, name, device=None, dtype=torch.bfloat16):
     """(pointer, leading dimension, rows, values of a row) of a matrix, bf16 unless another type is asked for."""
     if t.dtype is not dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if t.dim() != 2:
+    if device is not None and t.get_device() != device:
+        _elsewhere(t, device)
+    shape, strides = t.shape, t.stride()
+    if len(strides) != 2 or (strides[1] != 1 and shape[1] > 1 and shape[0]):
         raise ValueError("%s must be a matrix with unit stride along its last axis" % name)
-    (n, d), (ld, unit) = t.shape, t.stride()
-    if unit != 1 and d > 1 and n:
-        raise ValueError("%s must be a matrix with unit stride along its last axis" % name)
+    n, d = shape
     # (the stride of a single row says nothing)
-    return t.data_ptr(), ld if n > 1 else d, n, d
+    return t.data_ptr(), strides[0] if n > 1 else d, n, d
 
 
-def _rows(t, name, n=None, d=None, dtype=torch.bfloat16):
+def _rows(t, name, n=None, d=None, device=None, dtype=torch.bfloat16):
     """(pointer, leading dimension) of a matrix, of n x d if these are given; of None, nothing."""
     if t is None:
         return None, 0
-    p, ld, n_, d_ = _matrix(t, name, dtype)
+    p, ld, n_, d_ = _matrix(t, name, device, dtype)
     if n is not None and (n_ != n or d_ != d):
         raise ValueError("%s must have the shape %s" % (name, (n, d)))
     return p, ld
 
 
-def _flat(t, name, dtype, numel):
+def _flat(t, name, dtype, numel, device=None):
     """Pointer of a contiguous tensor of so many values; None stays None."""
     if t is None:
         return None
     if t.dtype is not dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if device is not None and t.get_device() != device:
+        _elsewhere(t, device)
     if t.numel() != numel or not t.is_contiguous():
         raise ValueError("%s must be %d contiguous values" % (name, numel))
     return t.data_ptr()
@@ -395,63 +402,61 @@ class Context:
 
     def glue_qk_norm_rope(self, q, k, positions, q_out, k_out, head_dim=128, q_gain=None, k_gain=None, eps=1e-6, rope_theta=1.0e6):
         """q [n][heads * head_dim], k [n][key heads * head_dim] -> q_out, k_out; either side may be None with its result."""
-        self._same_device(q, k, positions, q_out, k_out, q_gain, k_gain)
         (pq, lq, _, wq), (pk, lk, n, wk) = self._heads(q, k, head_dim)
-        f32 = torch.float32
+        f32, at = torch.float32, self.device
+        oq, loq = _rows(q_out, "q_out", n, wq, at)
+        ok, lok = _rows(k_out, "k_out", n, wk, at)
         self._rc(self.lib.agzo_glue_qk_norm_rope(
-            self.h, pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n), *_rows(q_out, "q_out", n, wq), *_rows(k_out, "k_out", n, wk), n,
-            wq // head_dim, wk // head_dim, head_dim, _flat(q_gain, "q_gain", f32, head_dim), _flat(k_gain, "k_gain", f32, head_dim), eps, rope_theta))
+            self.h, pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n, at), oq, loq, ok, lok, n, wq // head_dim, wk // head_dim, head_dim,
+            _flat(q_gain, "q_gain", f32, head_dim, at), _flat(k_gain, "k_gain", f32, head_dim, at), eps, rope_theta))
 
     def glue_qk_norm_rope_backward(self, q, k, positions, dq_out, dk_out, dq, dk, head_dim=128, q_gain=None, k_gain=None, dq_gain=None, dk_gain=None,
                                    eps=1e-6, rope_theta=1.0e6):
         """q, k: the inputs of glue_qk_norm_rope; dq_out, dk_out: the gradients with respect to its results -> dq, dk and, where given, dq_gain and
         dk_gain (float32 [head_dim])."""
-        self._same_device(q, k, positions, dq_out, dk_out, dq, dk, q_gain, k_gain, dq_gain, dk_gain)
         (pq, lq, _, wq), (pk, lk, n, wk) = self._heads(q, k, head_dim)
-        f32 = torch.float32
+        f32, at = torch.float32, self.device
         self._rc(self.lib.agzo_glue_qk_norm_rope_backward(
-            self.h, pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n), *_rows(dq_out, "dq_out", n, wq), *_rows(dk_out, "dk_out", n, wk),
-            *_rows(dq, "dq", n, wq), *_rows(dk, "dk", n, wk), n, wq // head_dim, wk // head_dim, head_dim, _flat(q_gain, "q_gain", f32, head_dim),
-            _flat(k_gain, "k_gain", f32, head_dim), _flat(dq_gain, "dq_gain", f32, head_dim), _flat(dk_gain, "dk_gain", f32, head_dim), eps, rope_theta))
+            self.h, pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n, at), *_rows(dq_out, "dq_out", n, wq, at), *_rows(dk_out, "dk_out", n, wk, at),
+            *_rows(dq, "dq", n, wq, at), *_rows(dk, "dk", n, wk, at), n, wq // head_dim, wk // head_dim, head_dim, _flat(q_gain, "q_gain", f32, head_dim, at),
+            _flat(k_gain, "k_gain", f32, head_dim, at), _flat(dq_gain, "dq_gain", f32, head_dim, at), _flat(dk_gain, "dk_gain", f32, head_dim, at), eps, rope_theta))
 
-    @staticmethod
-    def _heads(q, k, head_dim):
+    def _heads(self, q, k, head_dim):
         if q is None and k is None:
             raise ValueError("neither q nor k is given")
-        a = None if q is None else _matrix(q, "q")
-        b = (None, 0, a[2], 0) if k is None else _matrix(k, "k")
+        a = None if q is None else _matrix(q, "q", self.device)
+        b = (None, 0, a[2], 0) if k is None else _matrix(k, "k", self.device)
         a = a or (None, 0, b[2], 0)
         if a[2] != b[2] or a[3] % head_dim or b[3] % head_dim:
             raise ValueError("%d rows of %d values, %d of %d: need as many rows, of multiples of %d" % (*a[2:], *b[2:], head_dim))
         return a, b
 
-    @staticmethod
-    def _packed(q, k, v, cu_q, cu_k, k_len, head_dim, scale, causal):
-        pq, lq, nq, wq = _matrix(q, "q")
-        pk, lk, nk, wk = _matrix(k, "k")
+    def _packed(self, q, k, v, cu_q, cu_k, k_len, head_dim, scale, causal):
+        at = self.device
+        pq, lq, nq, wq = _matrix(q, "q", at)
+        pk, lk, nk, wk = _matrix(k, "k", at)
         if wq % head_dim or wk % head_dim:
             raise ValueError("rows of %d and %d values: need multiples of %d" % (wq, wk, head_dim))
-        pv, lv = _rows(v, "v", nk, wk)
+        pv, lv = _rows(v, "v", nk, wk, at)
         n_seq, i32 = cu_q.numel() - 1, torch.int32
-        return AgzoPackedAttention(pq, pk, pv, lq, lk, lv, _flat(cu_q, "cu_q", i32, n_seq + 1), _flat(cu_k, "cu_k", i32, n_seq + 1), _flat(k_len, "k_len", i32, n_seq),
-                                   nq, nk, n_seq, wq // head_dim, wk // head_dim, head_dim, int(causal), head_dim ** -0.5 if scale is None else scale), nq, wq, nk, wk
+        return AgzoPackedAttention(pq, pk, pv, lq, lk, lv, _flat(cu_q, "cu_q", i32, n_seq + 1, at), _flat(cu_k, "cu_k", i32, n_seq + 1, at), _flat(k_len, "k_len", i32, n_seq, at),
+                                   nq, nk, n_seq, wq // head_dim, wk // head_dim, head_dim, causal, head_dim ** -0.5 if scale is None else scale), nq, wq, nk, wk
 
     def glue_attention_packed(self, q, k, v, out, cu_q, cu_k, head_dim=128, scale=None, causal=True, lse=None, k_len=None):
         """q [n_q][heads * head_dim], k, v [n_k][key heads * head_dim] -> out like q; cu_q, cu_k: int32 offsets of the sequences
         (n_seq + 1 each); scale None: head_dim ** -0.5; lse: float32 [n_q][heads] or None; k_len: int32 [n_seq], how many keys each has
         of its room (a cache), or None: all."""
-        self._same_device(q, k, v, out, cu_q, cu_k, lse, k_len)
         a, nq, wq, _, _ = self._packed(q, k, v, cu_q, cu_k, k_len, head_dim, scale, causal)
-        o, ldo = _rows(out, "out", nq, wq)
-        self._rc(self.lib.agzo_glue_attention_packed(self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, nq * (wq // head_dim))))
+        o, ldo = _rows(out, "out", nq, wq, self.device)
+        self._rc(self.lib.agzo_glue_attention_packed(self.h, ctypes.byref(a), o, ldo, _flat(lse, "lse", torch.float32, nq * (wq // head_dim), self.device)))
 
     def glue_attention_packed_backward(self, q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, head_dim=128, scale=None, causal=True):
         """out, lse: of glue_attention_packed with the same arguments; dout: the gradient with respect to out -> dq, dk, dv."""
-        self._same_device(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k)
         a, nq, wq, nk, wk = self._packed(q, k, v, cu_q, cu_k, None, head_dim, scale, causal)
+        at = self.device
         self._rc(self.lib.agzo_glue_attention_packed_backward(
-            self.h, ctypes.byref(a), *_rows(out, "out", nq, wq), _flat(lse, "lse", torch.float32, nq * (wq // head_dim)), *_rows(dout, "dout", nq, wq),
-            *_rows(dq, "dq", nq, wq), *_rows(dk, "dk", nk, wk), *_rows(dv, "dv", nk, wk)))
+            self.h, ctypes.byref(a), *_rows(out, "out", nq, wq, at), _flat(lse, "lse", torch.float32, nq * (wq // head_dim), at), *_rows(dout, "dout", nq, wq, at),
+            *_rows(dq, "dq", nq, wq, at), *_rows(dk, "dk", nk, wk, at), *_rows(dv, "dv", nk, wk, at)))
 
     def step_no_update(self, L, W, X, loss, K, eps, seed, flags, out_dev, B_out):
         self._rc(self.lib.agzo_step_no_update(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), K, eps,
