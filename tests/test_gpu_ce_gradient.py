@@ -221,6 +221,54 @@ def test_repeated_captured_and_on_another_stream():
             assert all(torch.equal(got[n], want[n]) for n in want)
 
 
+@pytest.mark.parametrize("n,d,v,dtype", [(1, 64, 500, torch.bfloat16), (29, 264, 3001, torch.bfloat16), (50, 128, 900, torch.bfloat16), (127, 512, 2000, torch.bfloat16),
+                                         (600, 200, 700, torch.bfloat16), (60, 50, 333, torch.float32)])
+def test_every_way_is_captured_and_repeats(n, d, v, dtype):
+    st = torch.cuda.Stream()
+    w, x, ids = make(n, n, d, v, dtype=dtype)
+    w2, x2, ids2 = make(n + 1, n, d, v, dtype=dtype)
+    plain = binding.Context()
+    first, second = run(plain, w, x, ids), run(plain, w2, x2, ids2)
+    assert all(torch.equal(first[k], t) for k, t in run(plain, w, x, ids).items())
+    torch.cuda.synchronize()
+    ctx = binding.Context(st)
+    wc, xc, idc = w.clone(), x.clone(), ids.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        r = run(ctx, wc, xc, idc)
+        L, loss = binding.make_layer(wc, xc), binding.make_loss(idc, binding.LOSS_CE)
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            ctx.ce_forward(L, wc, xc, loss, r["loss"], r["lse"])
+            ctx.ce_backward(L, wc, xc, loss, r["lse"], r["dx"], r["dw"])
+    for data, want in (((w2, x2, ids2), second), ((w, x, ids), first), ((w2, x2, ids2), second)):
+        for a, b in zip((wc, xc, idc), data):
+            a.copy_(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(r[k], want[k]) for k in want)
+        run(plain, w, x, ids)
+
+
+def test_two_contexts_on_two_streams_at_once():
+    sets = [make(50 + i, 7 + 200 * i, 1024, 9000) for i in range(2)]
+    want = [run(binding.Context(), *s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    contexts = [binding.Context(s) for s in streams]
+    outs = [[], []]
+    for _ in range(4):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(run(contexts[i], *sets[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for got in outs[i]:
+            assert all(torch.equal(got[k], want[i][k]) for k in got)
+
+
 def test_refusals():
     ctx = binding.Context()
     w, x, ids = make(11, 32, 64, 100)
