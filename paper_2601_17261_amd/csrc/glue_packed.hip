@@ -317,7 +317,7 @@ constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
 
 // ---- forward ---------------------------------------------------------------------------------------------------
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
-// waits.  A tile is 64 matrix instructions a wave (HD = 128, 2048 cycles) beside some 1500 cycles of exponentials and 32 KB of LDS reads.
+// waits.  A tile is 32 matrix instructions a wave (HD = 128, 1024 cycles) beside some 1200 cycles of other vector instructions and 32 KB of LDS reads.
 // chunk > 0: a row tile's keys are dealt out, `chunk` tiles of them a share, and workgroups take shares until there are none left, whose sums, maximum and
 // sum of exponentials they leave for pk_join_kernel
 struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; int chunk; };
@@ -387,8 +387,7 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
             const int kb = j * PK_T;
             if (kb > wlast) return;                                          // (wave-uniform)
             const char* kt = pk_smem + (j & 1) * (2 * TILE);
-            // (operands are read four instructions ahead, the exponentials of 16 keys run beside the second product of the 16 before them: left to
-            // itself the compiler reads right before each instruction)
+            // (operands are read four instructions ahead: left to itself the compiler reads right before each instruction)
             const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
             PkFrag f[4];
             auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = o.row(i & 1, i >> 1); };
@@ -398,7 +397,8 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
 #pragma unroll
             for (int i = 0; i < 4; ++i) read_k(i);
             __builtin_amdgcn_sched_barrier(0);
-            // (of a SIMD's two waves the one that has matrix instructions to issue goes first, beside the other's maxima: 16001 tokens, 1074 -> 1047 us)
+            // (of a SIMD's two waves the one that has matrix instructions to issue goes first, beside the other's maxima and exponentials.  16001 tokens: 1029 us, 1074
+            // without; 1047 with the exponentials among the second product's instructions)
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 2 * KS; ++i) {
@@ -449,17 +449,13 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
                 return;
             }
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) two(e);
+            for (int e = 0; e < 32; e += 2) two(e);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 4 * DB; ++i) {
                 acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
                 if (i + 4 < 4 * DB) read_v(i + 4);
-                if (i < 3 * DB) {
-#pragma unroll
-                    for (int e = 0; e < 8 / DB; e += 2) two(8 + i * (8 / DB) + e);
-                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             __builtin_amdgcn_s_setprio(0);
