@@ -329,7 +329,7 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
  * the logits ever being stored.  loss: kind AGZO_LOSS_CE, target ids [n_tokens]; rows whose id is not in [0, d_out) are not counted.
  *   ce_forward: *loss_dev = mean over the counted rows of lse_t - y_t[id] (0 if there are none) and, where wanted, lse [n_tokens] device fp32,
  *     lse_t = log sum exp of row t's logits, of every row.  bf16 and fp32 layers; the loss is agzo_layer_forward_sketch's, bit for
- *     bit for fp32 layers and from 33 tokens on (fewer have sums of their own order).
+ *     bit for fp32 layers and from 256 tokens on (fewer may have sums of their own order).
  *   ce_backward: with D = (softmax(Y) - onehot(id)) g / count in the counted rows, 0 in the others, dX = D W [n_tokens][d_in]
  *     and dW = D^T X [d_out][d_in], of the layer's type, overwritten; either may be NULL.  lse: of ce_forward with the same arguments; g = *g_dev (1 if NULL).  The
  *     logits are made again for a piece of the outputs at a time; of bf16 layers D without g / count is rounded to bf16 for the products and sums are

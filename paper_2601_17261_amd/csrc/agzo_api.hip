@@ -1447,7 +1447,7 @@ int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const voi
     TRY(check_ce(ctx, L, W, X, loss, c));
     if (!loss_dev) return fail(ctx, AGZO_EINVAL, "loss_dev is NULL");
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
-    if (c.dtype == AGZO_BF16 && c.n_tokens <= kCeFewTokens) {
+    if (c.dtype == AGZO_BF16 && ce_few_fits(c.n_tokens, c.d_out)) {
         TRY(reserve(ctx, ce_few_workspace_bytes(c.n_tokens, c.d_out)));
         HIPCHK(launch_ce_few(static_cast<const bf16_t*>(X), c.ldx, static_cast<const bf16_t*>(W), c.ldw, c.n_tokens, c.d_out, c.d_in,
                              static_cast<const int32_t*>(loss->target), lse, loss_dev, ctx->ws, ctx->stream));

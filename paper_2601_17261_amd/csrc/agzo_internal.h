@@ -343,14 +343,18 @@ hipError_t launch_ce_combine(const void* ms, const float* tl, const int32_t* tar
 hipError_t launch_ce_rows_f32(const float* Y, int64_t ldy, int64_t M, int64_t N, const int32_t* target, double* scratch,
                               double* out, hipStream_t st, float* lse = nullptr);
 
+// the last of its launches: out = sum / count over nblk {sum, count} pairs
+hipError_t launch_ce_finish(const double* scratch, int nblk, double* out, hipStream_t st);
+
 // ce_few.hip : the same loss and its gradient for few tokens, bf16.  D = exp(y - lse) - onehot, 0 in rows that are not counted, [M][ldd] (ldd: outputs rounded up to 32
-// at least), where wanted D^T [V][32], zero from column M on, and g / count as *scale; dX's sums without that factor, over shares of the outputs, [shares][M][d] fp32, for
+// at least), where wanted D^T [V][ldt], zero from column M on, and g / count as *scale; dX's sums without that factor, over shares of the outputs, [shares][M][d] fp32, for
 // any number of tokens; dW = *scale D^T X for up to ldt = 32, 64 or 128 of them
-constexpr int64_t kCeFewTokens = 32;
+constexpr int64_t kCeFewTokens = 255;
+bool ce_few_fits(int64_t M, int64_t V);
 size_t ce_few_workspace_bytes(int64_t M, int64_t V);
 hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, float* lse, double* out, void* workspace, hipStream_t st);
 hipError_t launch_ce_few_d(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, const float* lse, const double* g,
-                           float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st);
+                           float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, int64_t ldt, hipStream_t st);
 int ce_few_dx_shares(int64_t M, int64_t n, int64_t d);
 // of n outputs: dX's sums (sums NULL: not wanted) and dW (NULL: not wanted), in one launch
 struct CeFewGrad {

@@ -1,10 +1,10 @@
-// Token cross-entropy of a layer's outputs, and its gradient, for few tokens (answers that are scored, a short sentence): what counts is that W is read, and dW
+// Token cross-entropy of a layer's outputs, and its gradient, for few tokens (answers that are scored, a short sentence; see ce_few_fits): what counts is that W is read, and dW
 // written, at the rate of memory.  Products are v_mfma_f32_32x32x16_bf16 with W's rows or dims as the instruction's rows and the tokens as its columns.
 //
-// Logits, up to 32 tokens: a workgroup has 32 outputs, its four waves every fourth 256 bytes of their rows, requested a round ahead straight into registers in the
+// Logits, 32 tokens at a time: a workgroup has 32 outputs, its four waves every fourth 256 bytes of their rows, requested a round ahead straight into registers in the
 // layout of the instruction: whole lines, 8 KB a wave, and nothing that a wave waits for another with until the four sums meet in LDS.
-// 7 tokens, 2048 -> 32000 (131 MB): 30 us, and the 256 x 256 tiles of gemm_bf16_aligned.hip 54.  Two blocks of tokens leave room for one wave a SIMD:
-// 40 tokens, 1024 -> 50000: 52 us, the tiles 38; so more tokens go to the tiles.
+// 7 tokens, 2048 -> 32000 (131 MB): 30 us, and the 256 x 256 tiles of gemm_bf16_aligned.hip 54.  (Two blocks of tokens to a wave
+// leave room for one wave a SIMD: 40 tokens, 1024 -> 50000: 52 us, the tiles 38.)
 #include "gemm_bf16_common.h"
 
 namespace agzo {
@@ -31,7 +31,8 @@ struct FewArgs {
     // statistics of 32 outputs each, [token][outputs / 32], and the targets' logits
     float2* ms; float* tl; int64_t nch;
     // gradient: D [M][ldd], D^T [V][32]
-    const float* lse; const double* g; bf16_t* D; int64_t ldd; bf16_t* Dt; float* scale;
+    const float* lse; const double* g; bf16_t* D; int64_t ldd; bf16_t* Dt; int64_t ldt; float* scale;
+    int blocks;                     // of 32 tokens
 };
 
 template <bool GRAD>
@@ -40,11 +41,14 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
     __shared__ float2 part[8][32];
     __shared__ __align__(16) bf16_t tile[GRAD ? FEW_OUT : 1][32];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hi = lane >> 5;
-    const int64_t out0 = (int64_t)blockIdx.x * FEW_OUT;
+    // workgroups of the same outputs follow each other on one XCD (ids are dealt round-robin over the eight), so that W comes out of its L2 for all but the first
+    const int at = blockIdx.x >> 3, m0 = at % a.blocks * 32, M = min(32, a.M - m0);
+    const int64_t chunk = (int64_t)(at / a.blocks) * 8 + (blockIdx.x & 7), out0 = chunk * FEW_OUT;
+    if (out0 >= a.V) return;
     const int left = (int)min((int64_t)FEW_OUT, a.V - out0);
-    const auto rw = few_rsrc(a.W + out0 * a.ldw), rx = few_rsrc(a.X);
+    const auto rw = few_rsrc(a.W + out0 * a.ldw), rx = few_rsrc(a.X + (M > 0 ? (int64_t)m0 * a.ldx : 0));        // (M <= 0: only zeros of D^T are wanted)
     // (outputs and tokens past the end repeat the last ones, uncounted)
-    const int woff = min(r, left - 1) * (int)(2 * a.ldw) + 16 * hi, xoff = min(r, a.M - 1) * (int)(2 * a.ldx) + 16 * hi;
+    const int woff = min(r, left - 1) * (int)(2 * a.ldw) + 16 * hi, xoff = min(r, max(M, 1) - 1) * (int)(2 * a.ldx) + 16 * hi;
     const int nchunk = (int)((a.d + FEW_K - 1) / FEW_K);
     FewFrag w0[8], x0[8], w1[8], x1[8];
     auto load = [&](int c, FewFrag (&w)[8], FewFrag (&x)[8]) __attribute__((always_inline)) {
@@ -74,9 +78,14 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
     for (int e = 0; e < 16; ++e) red[wave][8 * (e >> 2) + 4 * hi + (e & 3)][r] = acc[e];
     if (GRAD) {
         if (tid < FEW_OUT * 4) reinterpret_cast<uint4*>(&tile[0][0])[tid] = make_uint4(0, 0, 0, 0);
-        const int id = lane < a.M ? a.ids[lane] : -1;
-        const int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(id >= 0 && id < a.V));
-        if (blockIdx.x == 0 && tid == 0) *a.scale = (float)((a.g ? *a.g : 1.0) / (double)max(count, 1));
+        if (blockIdx.x == 0 && wave == 0) {
+            int count = 0;
+            for (int t = 0; t < a.M; t += 64) {
+                const int id = t + lane < a.M ? a.ids[t + lane] : -1;
+                count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(id >= 0 && id < a.V));
+            }
+            if (lane == 0) *a.scale = (float)((a.g ? *a.g : 1.0) / (double)max(count, 1));
+        }
     }
     __syncthreads();
     // four outputs of a token a thread
@@ -84,14 +93,14 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
     float y[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) y[u] = (red[0][4 * grp + u][tok] + red[1][4 * grp + u][tok]) + (red[2][4 * grp + u][tok] + red[3][4 * grp + u][tok]);
-    const int64_t id = tok < a.M ? a.ids[tok] : -1;
+    const int64_t id = tok < M ? a.ids[m0 + tok] : -1;
     if (!GRAD) {
         float mx = -INFINITY, s = 0.f;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (4 * grp + u < left) {
                 mx = fmaxf(mx, y[u]);
-                if (out0 + 4 * grp + u == id) a.tl[tok] = y[u];
+                if (out0 + 4 * grp + u == id) a.tl[m0 + tok] = y[u];
             }
         // (a NaN among them stays in the sum)
         const float m0 = mx == -INFINITY ? 0.f : mx;
@@ -101,7 +110,7 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
         part[grp][tok] = make_float2(mx, s);
     } else {
         const bool counted = id >= 0 && id < a.V;
-        const float l = tok < a.M ? a.lse[tok] : 0.f;
+        const float l = tok < M ? a.lse[m0 + tok] : 0.f;
         float v[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -109,18 +118,18 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
             v[u] = counted && 4 * grp + u < left ? (out0 + 4 * grp + u == id ? p - 1.f : p) : 0.f;
         }
         const uint2 two = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-        if (tok < a.M) {
-            *reinterpret_cast<uint2*>(a.D + tok * a.ldd + out0 + 4 * grp) = two;
+        if (tok < M) {
+            *reinterpret_cast<uint2*>(a.D + (int64_t)(m0 + tok) * a.ldd + out0 + 4 * grp) = two;
             tile[4 * grp][tok] = (bf16_t)two.x; tile[4 * grp + 1][tok] = (bf16_t)(two.x >> 16);
             tile[4 * grp + 2][tok] = (bf16_t)two.y; tile[4 * grp + 3][tok] = (bf16_t)(two.y >> 16);
         }
     }
     __syncthreads();
     if (GRAD) {
-        if (a.Dt && tid < 4 * left) *reinterpret_cast<uint4*>(a.Dt + out0 * 32 + tid * 8) = reinterpret_cast<const uint4*>(&tile[0][0])[tid];
+        if (a.Dt && tid < 4 * left) *reinterpret_cast<uint4*>(a.Dt + (out0 + (tid >> 2)) * a.ldt + m0 + (tid & 3) * 8) = reinterpret_cast<const uint4*>(&tile[0][0])[tid];
         return;
     }
-    if (tid >= a.M) return;
+    if (tid >= M) return;
     float mx = -INFINITY, s = 0.f;
 #pragma unroll
     for (int g8 = 0; g8 < 8; ++g8) mx = fmaxf(mx, part[g8][tid].x);
@@ -129,14 +138,20 @@ __global__ __launch_bounds__(256) void ce_few_kernel(const FewArgs a) {
         const float2 p = part[g8][tid];
         s += p.y == 0.f ? 0.f : p.y * __builtin_amdgcn_exp2f((p.x - (mx == -INFINITY ? 0.f : mx)) * FEW_LOG2E);
     }
-    a.ms[tid * a.nch + blockIdx.x] = make_float2(mx, s);
+    a.ms[(m0 + tid) * a.nch + chunk] = make_float2(mx, s);
 }
 
-// Loss and lse from the statistics, in one workgroup: 1, 2, 4, 8 or 16 waves a token, so that up to 16 tokens are looked at at once; sums in fp64
+// Loss and lse from the statistics: a workgroup has up to 32 tokens, 1, 2, 4, 8 or 16 waves to each, so that up to 16 are looked at at once; sums in fp64.  One
+// workgroup: the loss; several: {sum, count} of each, which loss.hip's last launch adds
 __global__ __launch_bounds__(1024) void ce_few_finish_kernel(const float2* __restrict__ ms, const float* __restrict__ tl, const int32_t* __restrict__ ids, int M, int64_t V, int64_t nch,
-                                                             float* __restrict__ lse, double* __restrict__ out) {
+                                                             float* __restrict__ lse, double* __restrict__ scratch, double* __restrict__ out) {
+    const int m0 = blockIdx.x * 32;
+    ms += m0 * nch;
+    tl += m0;
+    ids += m0;
+    M = min(32, M - m0);
     __shared__ float tops[16];
-    __shared__ double sums[16], logs[kCeFewTokens];
+    __shared__ double sums[16], logs[32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // (the first wave's lanes: a token each)
     const int id = threadIdx.x < M ? ids[threadIdx.x] : -1;
@@ -184,12 +199,15 @@ __global__ __launch_bounds__(1024) void ce_few_finish_kernel(const float2* __res
     }
     if (wave != 0) return;
     const double l = lane < M ? logs[lane] : 0.0;
-    if (lse && lane < M) lse[lane] = (float)l;
+    if (lse && lane < M) lse[m0 + lane] = (float)l;
     double loss = counted ? l - (double)target : 0.0;
     const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(counted));
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) loss += __shfl_xor(loss, off);
-    if (lane == 0) *out = n > 0 ? loss / n : 0.0;
+    if (lane != 0) return;
+    if (gridDim.x == 1) { *out = n > 0 ? loss / n : 0.0; return; }
+    scratch[2 * blockIdx.x] = loss;
+    scratch[2 * blockIdx.x + 1] = n;
 }
 
 // A tile of 32 rows of 128 values, for a wave or a workgroup, which is read transposed: a lane gets four rows' values of a column with each read
@@ -375,14 +393,19 @@ __global__ __launch_bounds__(256) void ce_few_dw_kernel(const FewDw w) {
 
 FewArgs few_args(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids) {
     FewArgs a{};
-    a.X = X; a.ldx = ldx; a.W = W; a.ldw = ldw; a.M = (int)M; a.V = V; a.d = d; a.ids = ids;
+    a.X = X; a.ldx = ldx; a.W = W; a.ldw = ldw; a.M = (int)M; a.V = V; a.d = d; a.ids = ids; a.blocks = (int)((M + 31) / 32);
     return a;
 }
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 
-size_t ce_few_workspace_bytes(int64_t M, int64_t V) { return up256((size_t)((V + FEW_OUT - 1) / FEW_OUT) * M * sizeof(float2)) + up256((size_t)M * 4); }
+// Up to 32 tokens, and more (in blocks of 32, W out of the XCD's L2 for all but the first) while that is at most seven workgroups to a compute unit: beyond, the tiles
+// of the layers' forward, bound by how deep d is, are faster.  60 tokens, 1000 -> 10000: loss in 27 us, tiles 44; 146, 2488 -> 4588: 41 and 91; 120, 2000 -> 10000:
+// 48 and 70; 240, 1000 -> 10000 (ten workgroups): 51 and 48; 40, 1024 -> 50000 (twelve): 73 and 51
+bool ce_few_fits(int64_t M, int64_t V) { return M <= 32 || (M <= kCeFewTokens && (M + 31) / 32 * ((V + FEW_OUT - 1) / FEW_OUT) <= 7 * 256); }
+
+size_t ce_few_workspace_bytes(int64_t M, int64_t V) { return up256((size_t)((V + FEW_OUT - 1) / FEW_OUT) * M * sizeof(float2)) + up256((size_t)M * 4) + up256(8 * 2 * 8); }
 
 hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, float* lse, double* out, void* workspace, hipStream_t st) {
     if (M < 1 || M > kCeFewTokens) return hipErrorInvalidValue;
@@ -391,24 +414,28 @@ hipError_t launch_ce_few(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t 
     char* ws = static_cast<char*>(workspace);
     a.ms = reinterpret_cast<float2*>(ws);
     a.tl = reinterpret_cast<float*>(ws + up256((size_t)a.nch * M * sizeof(float2)));
-    hipLaunchKernelGGL(ce_few_kernel<false>, dim3((unsigned)a.nch), dim3(256), 0, st, a);
-    hipLaunchKernelGGL(ce_few_finish_kernel, dim3(1), dim3(1024), 0, st, a.ms, a.tl, ids, (int)M, V, a.nch, lse, out);
-    return hipGetLastError();
+    double* scratch = reinterpret_cast<double*>(reinterpret_cast<char*>(a.tl) + up256((size_t)M * 4));
+    hipLaunchKernelGGL(ce_few_kernel<false>, dim3((unsigned)((a.nch + 7) / 8 * 8 * a.blocks)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(ce_few_finish_kernel, dim3(a.blocks), dim3(1024), 0, st, a.ms, a.tl, ids, (int)M, V, a.nch, lse, scratch, out);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.blocks == 1 ? e : launch_ce_finish(scratch, a.blocks, out, st);
 }
 
 hipError_t launch_ce_few_d(const bf16_t* X, int64_t ldx, const bf16_t* W, int64_t ldw, int64_t M, int64_t V, int64_t d, const int32_t* ids, const float* lse, const double* g,
-                           float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, hipStream_t st) {
-    if (M < 1 || M > kCeFewTokens || ldd < (V + 31) / 32 * 32 || ldd % 4) return hipErrorInvalidValue;
+                           float* scale, bf16_t* D, int64_t ldd, bf16_t* Dt, int64_t ldt, hipStream_t st) {
+    if (M < 1 || M > kCeFewTokens || ldd < (V + 31) / 32 * 32 || ldd % 4 || (Dt && (ldt % 32 || ldt < M))) return hipErrorInvalidValue;
     FewArgs a = few_args(X, ldx, W, ldw, M, V, d, ids);
-    a.lse = lse; a.g = g; a.scale = scale; a.D = D; a.ldd = ldd; a.Dt = Dt;
-    hipLaunchKernelGGL(ce_few_kernel<true>, dim3((unsigned)((V + FEW_OUT - 1) / FEW_OUT)), dim3(256), 0, st, a);
+    a.lse = lse; a.g = g; a.scale = scale; a.D = D; a.ldd = ldd; a.Dt = Dt; a.ldt = ldt;
+    // (the columns of D^T behind the tokens too)
+    if (Dt) a.blocks = (int)(ldt / 32);
+    hipLaunchKernelGGL(ce_few_kernel<true>, dim3((unsigned)(((V + FEW_OUT - 1) / FEW_OUT + 7) / 8 * 8 * a.blocks)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
-// for two workgroups to a compute unit, of eight blocks of 32 outputs to a wave at least
+// for two workgroups to a compute unit, of four blocks of 32 outputs to a wave at least
 int ce_few_dx_shares(int64_t M, int64_t n, int64_t d) {
     const int64_t tiles = (d + 127) / 128 * ((M + 63) / 64), blocks = (n + 31) / 32;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, blocks / 32, 64}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, blocks / 16, 64}));
 }
 
 hipError_t launch_ce_few_grad(const CeFewGrad& a, hipStream_t st) {

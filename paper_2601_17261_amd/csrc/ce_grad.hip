@@ -172,7 +172,7 @@ bool ce_dw_stored(const CeLayout& l, int64_t n, int64_t d) { return gemm_bf16_gr
 
 CeLayout ce_layout(int64_t M, int64_t V, int64_t d, bool want_dx, bool want_dw) {
     CeLayout l;
-    l.few = M <= kCeFewTokens;
+    l.few = ce_few_fits(M, V);
     l.few_w = M <= 128;
     l.piece = l.few ? V : std::min(ce_piece(M, V, d), V);
     l.tiles_z = gemm_bf16_grad_fits(M, l.piece, d);
@@ -232,14 +232,14 @@ hipError_t launch_ce_grad(const CeGradArgs& a, void* workspace, hipStream_t st) 
         if (e__ != hipSuccess) return e__;      \
     } while (0)
     if (l.few) {
-        CE_TRY(launch_ce_few_d(a.X, a.ldx, a.W, a.ldw, a.M, a.V, a.d, a.ids, a.lse, a.g, scale, D, l.width, a.dW ? Dt : nullptr, st));
+        CE_TRY(launch_ce_few_d(a.X, a.ldx, a.W, a.ldw, a.M, a.V, a.d, a.ids, a.lse, a.g, scale, D, l.width, a.dW ? Dt : nullptr, l.kt, st));
     }
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
         const int64_t n = std::min(l.piece, a.V - v0), width = ce_width(n, l.tiles_x ? l.shares : 1);
         const bf16_t* W = a.W + v0 * a.ldw;
         const bool tiles_z = !l.few && gemm_bf16_grad_fits(a.M, n, a.d);
-        if (!l.few) {
-            CePrepare p{a.ids, a.M, a.V, a.g, rowf, scale, v0 == 0, {}, {}, {}, {}};
+        if (!l.few || (a.dW && !l.few_w)) {
+            CePrepare p{a.ids, a.M, a.V, a.g, rowf, scale, !l.few && v0 == 0, {}, {}, {}, {}};
             if (v0 == 0 && a.dW && !l.few_w) p.X = flip(a.X, a.ldx, a.M, a.d, Xt, l.kt);
             if (a.dX && l.tiles_x) p.W = flip(W, a.ldw, n, a.d, Wt, width);
             if (tiles_z && a.dX) p.D = zero_columns(D, a.M, width, n, width);

@@ -169,6 +169,11 @@ hipError_t launch_ce_combine(const void* ms, const float* tl, const int32_t* tar
     return hipGetLastError();
 }
 
+hipError_t launch_ce_finish(const double* scratch, int nblk, double* out, hipStream_t st) {
+    hipLaunchKernelGGL(ce_finish_kernel, dim3(1), dim3(256), 0, st, scratch, nblk, out);
+    return hipGetLastError();
+}
+
 // fp32-storage path: one workgroup per token row of stored logits, fp64 statistics
 __global__ __launch_bounds__(256) void ce_rows_f32_kernel(const float* __restrict__ Y, int64_t ldy, int64_t M, int64_t N,
                                                           const int32_t* __restrict__ target, double* __restrict__ scratch, float* __restrict__ lse) {

@@ -55,6 +55,8 @@ def check(got, want):
 @pytest.mark.parametrize("n,d,v,pad", [
     (1, 8, 1, 0), (1, 64, 2, 0), (3, 40, 7, 8), (7, 2048, 999, 0), (63, 72, 64, 0), (64, 64, 65, 16), (65, 136, 257, 0), (200, 256, 1000, 0),
     (256, 128, 256, 0), (257, 264, 4097, 8), (256, 256, 512, 0), (512, 128, 768, 0), (300, 512, 12345, 0), (1000, 1024, 5000, 0), (5, 16, 140000, 0), (70, 8, 300001, 0),
+    # blocks of 32 tokens, the last outputs and tokens alone
+    (33, 72, 1000, 0), (96, 264, 1025, 8), (129, 512, 2000, 0), (255, 1000, 7000, 0), (255, 128, 7300, 0), (161, 2488, 4588, 0),
     # several pieces of the outputs
     (2049, 64, 70001, 0), (40, 8192, 33000, 0)])
 def test_loss_and_gradients(n, d, v, pad):
@@ -221,7 +223,7 @@ def test_repeated_captured_and_on_another_stream():
             assert all(torch.equal(got[n], want[n]) for n in want)
 
 
-@pytest.mark.parametrize("n,d,v,dtype", [(1, 64, 500, torch.bfloat16), (29, 264, 3001, torch.bfloat16), (50, 128, 900, torch.bfloat16), (127, 512, 2000, torch.bfloat16),
+@pytest.mark.parametrize("n,d,v,dtype", [(1, 64, 500, torch.bfloat16), (29, 264, 3001, torch.bfloat16), (50, 128, 900, torch.bfloat16), (200, 256, 5000, torch.bfloat16), (70, 256, 30000, torch.bfloat16), (127, 512, 2000, torch.bfloat16),
                                          (600, 200, 700, torch.bfloat16), (60, 50, 333, torch.float32)])
 def test_every_way_is_captured_and_repeats(n, d, v, dtype):
     st = torch.cuda.Stream()
