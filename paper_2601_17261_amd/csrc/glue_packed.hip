@@ -448,14 +448,21 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
                 pk_second_careful<HD, true>(kt + TILE, pf, seen, acc);
                 return;
             }
+            // (heads of 64, whose tiles are half the matrix instructions beside as many exponentials: those of 16 keys beside the second product of the 16 before
+            // them; 8192 tokens forward and back 214 us, 219 like heads of 128)
+            constexpr bool beside = HD == 64;
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) two(e);
+            for (int e = 0; e < (beside ? 8 : 32); e += 2) two(e);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 4 * DB; ++i) {
                 acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
                 if (i + 4 < 4 * DB) read_v(i + 4);
+                if (beside && i < 3 * DB) {
+#pragma unroll
+                    for (int e = 0; e < 8 / DB; e += 2) two(8 + i * (8 / DB) + e);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             __builtin_amdgcn_s_setprio(0);
