@@ -111,10 +111,10 @@ __device__ __forceinline__ void pk_second(const PkOffsets<HD>& o, int at, const 
 }
 
 // The same with care: values that are not finite are taken out, and with INF, where `seen` (fragments of ones and zeros) has a one for them, the
-// sum becomes what they make of it: a product of seen with 1 for inf, 2^12 for -inf and 2^23 for NaN has at most 64 of each.  LOW: p's second part
-// in its place
-template <int HD, bool INF, bool LOW = false>
-__device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag (&p)[4], const PkFrag (&seen)[4], pk_floatx16 (&acc)[HD / 32]) {
+// sum becomes what they make of it: a product of seen with 1 for inf, 2^12 for -inf and 2^23 for NaN has at most 64 of each.  LOW: p has a
+// second part
+template <int HD, bool INF, bool LOW>
+__device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag (&p)[4], const PkFrag (&low)[4], const PkFrag (&seen)[4], pk_floatx16 (&acc)[HD / 32]) {
     const int lane = threadIdx.x & 63, hi = lane >> 5;
 #pragma unroll
     for (int db = 0; db < HD / 32; ++db) {
@@ -139,7 +139,7 @@ __device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag
                 k.w[w] = kw;
             }
             acc[db] = pk_mfma(f, p[s], acc[db]);       // (in the order of pk_second: the same bits)
-            if (LOW) acc[db] = pk_mfma(f, seen[s], acc[db]);
+            if (LOW) acc[db] = pk_mfma(f, low[s], acc[db]);
             if (INF) c = pk_mfma(k, seen[s], c);
         }
         if (INF) {
@@ -320,10 +320,13 @@ constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
 // waits.  A tile is 32 matrix instructions a wave (HD = 128, 1024 cycles) beside some 1200 cycles of other vector instructions and 32 KB of LDS reads.
 // chunk > 0: a row tile's keys are dealt out, `chunk` tiles of them a share, and workgroups take shares until there are none left, whose sums, maximum and
 // sum of exponentials they leave for pk_join_kernel
+// fine: the probabilities go into the second product in two bf16 parts.  For few rows beside the keys, whose time is the keys' reading: their sums are of few large
+// probabilities often, whose roundings no others' balance (single rows were off by 0.0021 to 0.0028 of their norm, and are by the 0.0017 of
+// the result's own rounding; 64 on 200000 keys: 206 us for 202)
 struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; int chunk; };
 // again: stored nothing, the tiles have to be gone over with care
 enum class PkDone { stored, again, none };
-template <int HD, bool careful>
+template <int HD, bool fine, bool careful>
 __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwardOut& to_, int unit, pk_lchar lds) {
     char* pk_smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
@@ -433,19 +436,21 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
                 top = grown;
                 topsc = to;
             }
-            PkFrag pf[4];
+            PkFrag pf[4], pl[4];
             // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that)
             auto two = [&](int e) __attribute__((always_inline)) {              // probabilities e and e + 1 of the lane's 32
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][(e & 15) + 1], sc, -topsc));
                 l += p0 + p1;
-                pf[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
+                const uint32_t w = pack_bf16x2(p0, p1);
+                pf[e >> 3].w[(e & 7) >> 1] = w;
+                if (fine) pl[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
             };
             if (careful && mask) {
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) two(e);
                 PkFrag seen[4];
                 pk_seen(kb, limit_of(), seen);
-                pk_second_careful<HD, true>(kt + TILE, pf, seen, acc);
+                pk_second_careful<HD, true, fine>(kt + TILE, pf, pl, seen, acc);
                 return;
             }
             // (heads of 64, whose tiles are half the matrix instructions beside as many exponentials: those of 16 keys beside the second product of the 16 before
@@ -458,6 +463,7 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
 #pragma unroll
             for (int i = 0; i < 4 * DB; ++i) {
                 acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
+                if (fine) acc[i % DB] = pk_mfma(f[i & 3], pl[i / DB], acc[i % DB]);
                 if (i + 4 < 4 * DB) read_v(i + 4);
                 if (beside && i < 3 * DB) {
 #pragma unroll
@@ -500,14 +506,14 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
     return PkDone::stored;
 }
 // (a function that is called: its registers are not the kernel's)
-template <int HD>
-__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, int unit, pk_lchar lds) { (void)pk_forward<HD, true>(a, to, unit, lds); }
-template <int HD>
+template <int HD, bool fine>
+__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, int unit, pk_lchar lds) { (void)pk_forward<HD, fine, true>(a, to, unit, lds); }
+template <int HD, bool fine>
 __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_forward_kernel(PackedArgs a, PkForwardOut to) {
     extern __shared__ __align__(1024) char pk_dynamic[];
     for (int unit = (int)blockIdx.x;; unit += (int)gridDim.x) {
-        const PkDone done = pk_forward<HD, false>(a, to, unit, (pk_lchar)pk_dynamic);
-        if (done == PkDone::again) pk_forward_again<HD>(a, to, unit, (pk_lchar)pk_dynamic);
+        const PkDone done = pk_forward<HD, fine, false>(a, to, unit, (pk_lchar)pk_dynamic);
+        if (done == PkDone::again) pk_forward_again<HD, fine>(a, to, unit, (pk_lchar)pk_dynamic);
         if (done == PkDone::none || to.chunk == 0) return;
     }
 }
@@ -727,7 +733,7 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
             }
             if constexpr (careful) {
                 if (mask) {
-                    pk_second_careful<HD, false, true>(kt, pf, pl, acc);
+                    pk_second_careful<HD, false, true>(kt, pf, pl, pl, acc);
                     return;
                 }
                 read_trans(0);
@@ -991,8 +997,8 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
                     const int at = 16 * s4 + (w >> 1) * 8 + (w & 1) * 2;
                     seen[s4].w[w] = (wkey + (lane & 31) <= limit[at] ? 0x3F80u : 0u) | (wkey + (lane & 31) <= limit[at + 1] ? 0x3F800000u : 0u);
                 }
-            pk_second_careful<HD, true>(qt + TILE, pf, seen, av);
-            pk_second_careful<HD, false>(qt, df, df, ak);
+            pk_second_careful<HD, true, false>(qt + TILE, pf, pf, seen, av);
+            pk_second_careful<HD, false, false>(qt, df, df, df, ak);
             return;
         }
 #pragma unroll
@@ -1086,11 +1092,12 @@ int64_t pk_units(int64_t total, int n_seq, int n_kv) { return (total / PK_ROWS +
 // compute unit, of 8 tiles and more (a share costs a workgroup's start, its sums and a launch that joins them), 128 of a sequence at most and 256 MB of sums.
 // Lengths are on the device: work is reckoned from their mean, and sequences of 16 tiles and more in the mean are taken to be uneven.  64 sequences of 200000
 // keys together, up to 16760: 380 us without, 206 so, 216 with one share to each
+bool pk_few_rows(const PackedArgs& a) { return a.total_q * (a.n_heads / a.n_kv) * 8 <= a.total_k; }
 int pk_chunk(const PackedArgs& a, int head_dim) {
     const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
     if (units < 1 || a.total_k < 1) return 0;
     const int64_t all = (a.total_k + PK_T - 1) / PK_T, mean = (a.total_k / std::max(1, a.n_seq) + PK_T - 1) / PK_T;
-    if (mean < 16 || !(a.total_q * G * 8 <= a.total_k || units < 256)) return 0;
+    if (mean < 16 || !(pk_few_rows(a) || units < 256)) return 0;
     const int64_t chunk = std::max<int64_t>({8, (units * mean + 1023) / 1024, (all + 127) / 128, all * rows * head_dim * 4 / (1LL << 28)});
     return (int)std::min<int64_t>(chunk, 1 << 20);
 }
@@ -1120,8 +1127,9 @@ hipError_t pk_lds(F* f, int bytes, std::atomic<uint64_t>& done) {
 template <int HD>
 hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
     constexpr int SMEM = 4 * PK_T * HD * 2;
-    static std::atomic<uint64_t> done{0};
-    const hipError_t attr = pk_lds(pk_forward_kernel<HD>, SMEM, done);
+    static std::atomic<uint64_t> done{0}, done_fine{0};
+    const bool fine = a.total_q <= a.n_seq || pk_few_rows(a);      // (single rows, of however few keys)
+    const hipError_t attr = fine ? pk_lds(pk_forward_kernel<HD, true>, SMEM, done_fine) : pk_lds(pk_forward_kernel<HD, false>, SMEM, done);
     if (attr != hipSuccess) return attr;
     const int G = a.n_heads / a.n_kv, chunk = pk_chunk(a, HD);
     const int64_t rows = a.total_q * a.n_heads, blocks = (rows * (HD / 4) + 255) / 256;
@@ -1136,7 +1144,9 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
         units += shares * (a.total_q * G / PK_ROWS + 1) * a.n_kv;
     }
     if (units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(pk_forward_kernel<HD>, dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, PkForwardOut{out, ldo, lse, part, ml, chunk});
+    const PkForwardOut to{out, ldo, lse, part, ml, chunk};
+    if (fine) hipLaunchKernelGGL((pk_forward_kernel<HD, true>), dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, to);
+    else hipLaunchKernelGGL((pk_forward_kernel<HD, false>), dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, to);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunk == 0) return e;
     hipLaunchKernelGGL(pk_join_kernel<HD>, dim3((unsigned)blocks), dim3(256), 0, st, a, part, ml, chunk, out, ldo, lse);
