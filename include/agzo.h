@@ -298,9 +298,9 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  * cu_k[s + 1] - 1 (device int32 [n_seq + 1], not decreasing, within 0 .. n_q and 0 .. n_k: offsets outside are taken as the nearest inside);
  * its queries are its last positions: with causal != 0 query i of Lq sees the keys 0 .. i + Lk - Lq of Lk, else all Lk.  Lq = Lk is a prompt,
  * Lq = 1 a new token behind the keys that are there.  out = softmax(scale q k^T) v for each head (head h reads key head h / (n_heads / n_kv_heads)); the
- * probabilities are rounded to bf16 for the second product (in two parts for single queries), sums are fp32.  A query that sees no key (Lk < Lq, or no keys at all) gets 0
- * and takes part in no gradient.  Values of keys that a query does not see have no part in its result, whatever they are (NaN and
- * infinities too).  Rows of no sequence are neither read nor written.
+ * probabilities are rounded to bf16 for the second product (to two bf16 parts where queries are single ones or few beside the keys), sums are fp32.  A query
+ * that sees no key (Lk < Lq, or no keys at all) gets 0 and takes part in no gradient.  Values of keys that a query does not see have no part in its result,
+ * whatever they are (NaN and infinities too).  Rows of no sequence are neither read nor written.
  *   k_len (nullable; forward call only): how many of its keys sequence s has, the first k_len[s] (0 .. cu_k[s + 1] - cu_k[s]: a length outside is taken as
  *     the nearest of these): a cache with room for each sequence, of which the rest is not read
  *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key
