@@ -214,6 +214,7 @@ def make_loss(target=None, kind=LOSS_MSE):
         return s
     s.kind = kind
     s.target = target.data_ptr()
+    s._target = target      # (as long as the address is in use; what ce_forward and ce_backward look at)
     if kind == LOSS_CE and target.dtype != torch.int32:
         raise TypeError("cross-entropy targets must be int32 ids")
     if kind == LOSS_MSE:
@@ -386,18 +387,35 @@ class Context:
             if t is not None and t.get_device() != device:
                 raise ValueError("a tensor on %s, and the context is of %s" % (t.device, self.stream.device))
 
+    def _ce_operands(self, L, W, X, loss):
+        """Pointers of W and X, which have to be those that L describes, and the ids as many as its tokens."""
+        dtype, at = torch.bfloat16 if L.dtype == BF16 else torch.float32, self.device
+        pointers = []
+        for t, name, n, ld in ((W, "W", L.d_out, L.ldw), (X, "X", L.n_tokens, L.ldx)):
+            p, ld_, n_, d_ = (None, ld, n, L.d_in) if t is None else _matrix(t, name, at, dtype)
+            if n_ != n or d_ != L.d_in or (n > 1 and ld_ != ld):
+                raise ValueError("%s is %d x %d with rows %d apart, the layer's %d x %d, %d apart" % (name, n_, d_, ld_, n, L.d_in, ld))
+            pointers.append(p)
+        if loss.kind == LOSS_CE:
+            ids = getattr(loss, "_target", None)
+            if ids is None or (_flat(ids, "ids", torch.int32, L.n_tokens, at) or None) != loss.target:
+                raise ValueError("the loss must be make_loss(ids, LOSS_CE)")
+        return pointers
+
     def ce_forward(self, L, W, X, loss, loss_dev, lse=None):
-        """loss: make_loss(ids, LOSS_CE); loss_dev: one float64 on the device; lse: float32 [n_tokens] or None."""
-        self._same_device(W, X, loss_dev, lse)
-        self._rc(self.lib.agzo_ce_forward(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), _flat(loss_dev, "loss_dev", torch.float64, 1),
+        """L: make_layer(W, X); loss: make_loss(ids, LOSS_CE), ids int32 [n_tokens]; loss_dev: one float64 on the device; lse: float32 [n_tokens] or None."""
+        w, x = self._ce_operands(L, W, X, loss)
+        self._same_device(loss_dev, lse)
+        self._rc(self.lib.agzo_ce_forward(self.h, ctypes.byref(L), w, x, ctypes.byref(loss), _flat(loss_dev, "loss_dev", torch.float64, 1),
                                           _flat(lse, "lse", torch.float32, L.n_tokens)))
 
     def ce_backward(self, L, W, X, loss, lse, dX, dW, g_dev=None):
-        """lse: of ce_forward; dX like X, dW like W (either may be None); g_dev: one float64 on the device or None (1)."""
-        self._same_device(W, X, lse, dX, dW, g_dev)
+        """L, loss: as for ce_forward, and lse of it; dX like X, dW like W (either may be None); g_dev: one float64 on the device or None (1)."""
+        w, x = self._ce_operands(L, W, X, loss)
+        self._same_device(lse, dX, dW, g_dev)
         _same_shape("dX", dX, X)
         _same_shape("dW", dW, W)
-        self._rc(self.lib.agzo_ce_backward(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), _flat(lse, "lse", torch.float32, L.n_tokens),
+        self._rc(self.lib.agzo_ce_backward(self.h, ctypes.byref(L), w, x, ctypes.byref(loss), _flat(lse, "lse", torch.float32, L.n_tokens),
                                            _flat(g_dev, "g_dev", torch.float64, 1), *_rows(dX, "dX", dtype=X.dtype), *_rows(dW, "dW", dtype=X.dtype)))
 
     def glue_qk_norm_rope(self, q, k, positions, q_out, k_out, head_dim=128, q_gain=None, k_gain=None, eps=1e-6, rope_theta=1.0e6):
