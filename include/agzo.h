@@ -285,7 +285,8 @@ int agzo_glue_add(agzo_ctx* ctx, void* h, int64_t ldh, const void* delta, int64_
  *   any tensor otherwise.  positions: device int32 [n].
  * qk_norm_rope_backward: from the gradients dq_out, dk_out with respect to its results, those with respect to q, k (dq, dk) and, where wanted
  *   (not NULL), to the gains (fp32 [D], sums over tokens and heads in a fixed order, overwritten).  q and k are the inputs of the forward
- *   call.  dq may be dq_out or q (and dk dk_out or k), and may not overlap any tensor otherwise. */
+ *   call.  dq may be dq_out or q (and dk dk_out or k), dq_gain may be q_gain and dk_gain k_gain; no result may overlap any tensor otherwise.
+ * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape, eps negative, rope_theta not above 1, either not finite, overlaps. */
 int agzo_glue_qk_norm_rope(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out,
                            int64_t ldqo, void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                            const float* q_gain, const float* k_gain, float eps, float rope_theta);
@@ -306,7 +307,7 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key
  *   backward: out, lse of the forward call with the same arguments and the gradient dout -> dq, dk, dv (all three written, for all rows of
  *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
- * Inputs are only read; outputs may not overlap inputs or each other.
+ * Inputs are only read; outputs (lse of the forward call too) may not overlap inputs (offsets and lengths too) or each other.
  * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, more than 2^16 sequences; n_k, or n_q times
  * the heads of a key head, from 2^31 - 1024 on; leading dimensions from 2^22 on), scale not positive and finite, overlapping outputs, k_len in the
  * backward call. */
@@ -336,8 +337,8 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
  *     fp32, of fp32 layers D is fp32 and sums are fp64, those over pieces fp32; their order depends on the shape alone.  Workspace: three to five buffers
  *     of a piece, of 2^27 bf16 or 2^26 fp32 values at most unless n_tokens or d_in pass 2^17.
  * Device, workspace and captures as for the calls on packed batches.
- * Errors: AGZO_EINVAL for a bad layer or loss, NULL or misaligned tensors, outputs that overlap an input or each other, more than 2^21
- * tokens or inputs (backward). */
+ * Errors: AGZO_EINVAL for a bad layer or loss, NULL or misaligned tensors, outputs (loss_dev and lse too) that overlap an input (ids, lse and g_dev
+ * too) or each other, more than 2^21 tokens or inputs (backward). */
 int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, double* loss_dev, float* lse);
 int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, const float* lse,
                      const double* g_dev, void* dX, int64_t lddx, void* dW, int64_t lddw);

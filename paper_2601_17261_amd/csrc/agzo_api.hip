@@ -1372,6 +1372,8 @@ int check_device(agzo_ctx* ctx) {
 
 struct Named { const char* name; Rows rows; };
 Named named(const char* name, const void* at, int64_t ld, int64_t n, int64_t d, int64_t size = 2) { return Named{name, Rows{reinterpret_cast<uintptr_t>(at), size * ld, at ? n : 0, size * d}}; }
+// (a list of `count` values of `size` bytes)
+Named listed(const char* name, const void* at, int64_t count, int64_t size = 4) { return named(name, at, count, 1, count, size); }
 // outputs that overlap each other or an input; in_place: inputs that an output may be (NULL: none), as pairs of indices
 int check_apart(agzo_ctx* ctx, std::initializer_list<Named> outs, std::initializer_list<Named> ins, std::initializer_list<std::pair<int, int>> in_place = {}) {
     int o = 0;
@@ -1391,13 +1393,16 @@ int check_apart(agzo_ctx* ctx, std::initializer_list<Named> outs, std::initializ
     return 0;
 }
 
-int check_norm_rope(agzo_ctx* ctx, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions, float eps, float rope_theta) {
+int check_norm_rope(agzo_ctx* ctx, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions, std::initializer_list<const float*> gains, float eps,
+                    float rope_theta) {
     if (!ctx) return AGZO_EINVAL;
     if (n_heads < 0 || n_kv_heads < 0 || n_heads > 65535 || n_kv_heads > 65535 || (head_dim != 64 && head_dim != 128))
         return fail(ctx, AGZO_EINVAL, "%d heads, %d key heads of %d values", n_heads, n_kv_heads, head_dim);
     if (n < 0 || n > 0x7FFFFFFFLL) return fail(ctx, AGZO_EINVAL, "%lld tokens", (long long)n);
     if (n > 0 && !positions) return fail(ctx, AGZO_EINVAL, "positions is NULL");
     if (reinterpret_cast<uintptr_t>(positions) & 3) return fail(ctx, AGZO_EINVAL, "positions is misaligned");
+    for (const float* g : gains)
+        if (reinterpret_cast<uintptr_t>(g) & 3) return fail(ctx, AGZO_EINVAL, "a gain or its gradient is misaligned");
     if (!(eps >= 0.f) || !(eps < INFINITY)) return fail(ctx, AGZO_EINVAL, "eps must be finite and not negative");
     if (!(rope_theta > 1.f) || !(rope_theta < INFINITY)) return fail(ctx, AGZO_EINVAL, "rope_theta must be finite and exceed 1");
     return check_device(ctx);
@@ -1445,8 +1450,11 @@ int check_ce(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, c
 int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, double* loss_dev, float* lse) {
     agzo_layer c;
     TRY(check_ce(ctx, L, W, X, loss, c));
-    if (!loss_dev) return fail(ctx, AGZO_EINVAL, "loss_dev is NULL");
+    if (!loss_dev || (reinterpret_cast<uintptr_t>(loss_dev) & 7)) return fail(ctx, AGZO_EINVAL, "loss_dev is NULL or misaligned");
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
+    const int64_t size = c.dtype == AGZO_F32 ? 4 : 2;
+    TRY(check_apart(ctx, {listed("loss_dev", loss_dev, 1, 8), listed("lse", lse, c.n_tokens)},
+                    {named("X", X, c.ldx, c.n_tokens, c.d_in, size), named("W", W, c.ldw, c.d_out, c.d_in, size), listed("the target ids", loss->target, c.n_tokens)}));
     if (c.dtype == AGZO_BF16 && ce_few_fits(c.n_tokens, c.d_out)) {
         TRY(reserve(ctx, ce_few_workspace_bytes(c.n_tokens, c.d_out)));
         HIPCHK(launch_ce_few(static_cast<const bf16_t*>(X), c.ldx, static_cast<const bf16_t*>(W), c.ldw, c.n_tokens, c.d_out, c.d_in,
@@ -1464,6 +1472,7 @@ int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const vo
     TRY(check_ce(ctx, L, W, X, loss, c));
     if (c.n_tokens > (1LL << 21) || c.d_in > (1LL << 21)) return fail(ctx, AGZO_EINVAL, "more than 2^21 tokens or inputs");
     if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3)) return fail(ctx, AGZO_EINVAL, "lse is NULL or misaligned");
+    if (reinterpret_cast<uintptr_t>(g_dev) & 7) return fail(ctx, AGZO_EINVAL, "g_dev is misaligned");
     if (!dX && !dW) return fail(ctx, AGZO_EINVAL, "neither dX nor dW is wanted");
     const bool f32 = c.dtype == AGZO_F32;
     if (f32) {
@@ -1475,7 +1484,8 @@ int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const vo
     }
     const int64_t size = f32 ? 4 : 2;
     TRY(check_apart(ctx, {named("dX", dX, lddx, c.n_tokens, c.d_in, size), named("dW", dW, lddw, c.d_out, c.d_in, size)},
-                    {named("X", X, c.ldx, c.n_tokens, c.d_in, size), named("W", W, c.ldw, c.d_out, c.d_in, size)}));
+                    {named("X", X, c.ldx, c.n_tokens, c.d_in, size), named("W", W, c.ldw, c.d_out, c.d_in, size), listed("the target ids", loss->target, c.n_tokens),
+                     listed("lse", lse, c.n_tokens), listed("g_dev", g_dev, 1, 8)}));
     if (f32) {
         TRY(reserve(ctx, ce_grad_f32_workspace_bytes(c.n_tokens, c.d_out, c.d_in, dX != nullptr, dW != nullptr)));
         const CeGradF32Args a{static_cast<const float*>(X), c.ldx, static_cast<const float*>(W), c.ldw, c.n_tokens, c.d_out, c.d_in,
@@ -1493,11 +1503,13 @@ int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const vo
 int agzo_glue_qk_norm_rope(agzo_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out,
                            int64_t ldqo, void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                            const float* q_gain, const float* k_gain, float eps, float rope_theta) {
-    TRY(check_norm_rope(ctx, n, n_heads, n_kv_heads, head_dim, positions, eps, rope_theta));
+    TRY(check_norm_rope(ctx, n, n_heads, n_kv_heads, head_dim, positions, {q_gain, k_gain}, eps, rope_theta));
     const int64_t dq = (int64_t)n_heads * head_dim, dk = (int64_t)n_kv_heads * head_dim;
     TRY(check_glue(ctx, n, dq, {q, q_out}, {ldq, ldqo}));
     TRY(check_glue(ctx, n, dk, {k, k_out}, {ldk, ldko}));
-    TRY(check_apart(ctx, {named("q_out", q_out, ldqo, n, dq), named("k_out", k_out, ldko, n, dk)}, {named("q", q, ldq, n, dq), named("k", k, ldk, n, dk)}, {{0, 0}, {1, 1}}));
+    TRY(check_apart(ctx, {named("q_out", q_out, ldqo, n, dq), named("k_out", k_out, ldko, n, dk)},
+                    {named("q", q, ldq, n, dq), named("k", k, ldk, n, dk), listed("positions", positions, n), listed("q_gain", q_gain, head_dim), listed("k_gain", k_gain, head_dim)},
+                    {{0, 0}, {1, 1}}));
     HIPCHK(launch_norm_rope(NormRopeSide{static_cast<const bf16_t*>(q), ldq, static_cast<bf16_t*>(q_out), ldqo, q_gain, n_heads},
                             NormRopeSide{static_cast<const bf16_t*>(k), ldk, static_cast<bf16_t*>(k_out), ldko, k_gain, n_kv_heads}, positions, n, head_dim, eps,
                             rope_theta, ctx->stream));
@@ -1508,14 +1520,15 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
                                     const void* dq_out, int64_t lddqo, const void* dk_out, int64_t lddko, void* dq, int64_t lddq,
                                     void* dk, int64_t lddk, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                     const float* q_gain, const float* k_gain, float* dq_gain, float* dk_gain, float eps, float rope_theta) {
-    TRY(check_norm_rope(ctx, n, n_heads, n_kv_heads, head_dim, positions, eps, rope_theta));
+    TRY(check_norm_rope(ctx, n, n_heads, n_kv_heads, head_dim, positions, {q_gain, k_gain, dq_gain, dk_gain}, eps, rope_theta));
     const int64_t wq = (int64_t)n_heads * head_dim, wk = (int64_t)n_kv_heads * head_dim;
     TRY(check_glue(ctx, n, wq, {q, dq_out, dq}, {ldq, lddqo, lddq}));
     TRY(check_glue(ctx, n, wk, {k, dk_out, dk}, {ldk, lddko, lddk}));
-    TRY(check_apart(ctx, {named("dq", dq, lddq, n, wq), named("dk", dk, lddk, n, wk)},
-                    {named("q", q, ldq, n, wq), named("dq_out", dq_out, lddqo, n, wq), named("k", k, ldk, n, wk), named("dk_out", dk_out, lddko, n, wk)},
-                    {{0, 0}, {0, 1}, {1, 2}, {1, 3}}));
-    if (dq_gain && dq_gain == dk_gain) return fail(ctx, AGZO_EINVAL, "dq_gain and dk_gain overlap");
+    // (the gains have been read when their gradients are written)
+    TRY(check_apart(ctx, {named("dq", dq, lddq, n, wq), named("dk", dk, lddk, n, wk), listed("dq_gain", dq_gain, head_dim), listed("dk_gain", dk_gain, head_dim)},
+                    {named("q", q, ldq, n, wq), named("dq_out", dq_out, lddqo, n, wq), named("k", k, ldk, n, wk), named("dk_out", dk_out, lddko, n, wk),
+                     listed("positions", positions, n), listed("q_gain", q_gain, head_dim), listed("k_gain", k_gain, head_dim)},
+                    {{0, 0}, {0, 1}, {1, 2}, {1, 3}, {2, 5}, {3, 6}}));
     if (dq_gain || dk_gain) TRY(reserve(ctx, norm_rope_workspace_bytes(n, head_dim)));
     HIPCHK(launch_norm_rope_grad(NormRopeSide{static_cast<const bf16_t*>(q), ldq, static_cast<bf16_t*>(dq), lddq, q_gain, n_heads, static_cast<const bf16_t*>(dq_out), lddqo},
                                  NormRopeSide{static_cast<const bf16_t*>(k), ldk, static_cast<bf16_t*>(dk), lddk, k_gain, n_kv_heads, static_cast<const bf16_t*>(dk_out), lddko},
@@ -1529,7 +1542,9 @@ int agzo_glue_attention_packed(agzo_ctx* ctx, const agzo_packed_attention* a, vo
     const int64_t dq = (int64_t)a->n_heads * a->head_dim, dkv = (int64_t)a->n_kv_heads * a->head_dim;
     TRY(check_glue(ctx, a->n_q, dq, {out}, {ldo}));
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
-    TRY(check_apart(ctx, {named("out", out, ldo, a->n_q, dq)}, {named("q", a->q, a->ldq, a->n_q, dq), named("k", a->k, a->ldk, a->n_k, dkv), named("v", a->v, a->ldv, a->n_k, dkv)}));
+    TRY(check_apart(ctx, {named("out", out, ldo, a->n_q, dq), listed("lse", lse, a->n_q * a->n_heads)},
+                    {named("q", a->q, a->ldq, a->n_q, dq), named("k", a->k, a->ldk, a->n_k, dkv), named("v", a->v, a->ldv, a->n_k, dkv), listed("cu_q", a->cu_q, a->n_seq + 1LL),
+                     listed("cu_k", a->cu_k, a->n_seq + 1LL), listed("k_len", a->k_len, a->n_seq)}));
     TRY(reserve(ctx, packed_forward_workspace_bytes(p, a->head_dim)));
     HIPCHK(launch_packed_forward(p, a->head_dim, static_cast<bf16_t*>(out), ldo, lse, ctx->ws, ctx->stream));
     return AGZO_OK;
@@ -1548,7 +1563,8 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
     if (a->n_q > 0 && (!lse || (reinterpret_cast<uintptr_t>(lse) & 3))) return fail(ctx, AGZO_EINVAL, "lse is NULL or misaligned");
     TRY(check_apart(ctx, {named("dq", dq, lddq, a->n_q, wq), named("dk", dk, lddk, a->n_k, wk), named("dv", dv, lddv, a->n_k, wk)},
                     {named("q", a->q, a->ldq, a->n_q, wq), named("k", a->k, a->ldk, a->n_k, wk), named("v", a->v, a->ldv, a->n_k, wk),
-                     named("out", out, ldo, a->n_q, wq), named("dout", dout, lddo, a->n_q, wq)}));
+                     named("out", out, ldo, a->n_q, wq), named("dout", dout, lddo, a->n_q, wq), listed("lse", lse, a->n_q * a->n_heads),
+                     listed("cu_q", a->cu_q, a->n_seq + 1LL), listed("cu_k", a->cu_k, a->n_seq + 1LL)}));
     TRY(reserve(ctx, packed_backward_workspace_bytes(p, a->head_dim)));
     const PackedGrad g{static_cast<const bf16_t*>(out), static_cast<const bf16_t*>(dout), ldo, lddo, lse, static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk),
                        static_cast<bf16_t*>(dv), lddq, lddk, lddv};
