@@ -176,6 +176,7 @@ __global__ __launch_bounds__(1024) void norm_rope_dgain_kernel(const float* __re
 // (few tokens: a workgroup each, for it is latency that counts; more share a workgroup and with it the first loads' latency)
 int norm_rope_tokens_per_wg(int64_t n) { return n >= 2048 ? 4 : 1; }
 constexpr int kNormRopeGradBlocks = 1024;      // four workgroups to a compute unit
+constexpr int64_t kNormRopeTokens = 1 << 25;   // of a launch: one of 2^32 threads and more is cut off without a word
 
 int norm_rope_grad_blocks(int64_t n) {
     const int per = norm_rope_tokens_per_wg(n);
@@ -189,14 +190,19 @@ size_t norm_rope_workspace_bytes(int64_t n, int head_dim) { return (size_t)norm_
 hipError_t launch_norm_rope(const NormRopeSide& q, const NormRopeSide& k, const int32_t* positions, int64_t n, int head_dim, float eps, float theta, hipStream_t st) {
     if (n == 0) return hipSuccess;
     const int per = norm_rope_tokens_per_wg(n);
-    const int64_t blocks = (n + per - 1) / per;
-    if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     const size_t smem = (size_t)per * head_dim / 2 * sizeof(float2);
     const double l2 = log2((double)theta);
-    if (head_dim == 128) hipLaunchKernelGGL(norm_rope_kernel<128>, dim3((unsigned)blocks), dim3(NR_WG), smem, st, q, k, positions, n, per, eps, l2);
-    else if (head_dim == 64) hipLaunchKernelGGL(norm_rope_kernel<64>, dim3((unsigned)blocks), dim3(NR_WG), smem, st, q, k, positions, n, per, eps, l2);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    auto from = [](NormRopeSide a, int64_t t) { a.x += t * a.ldx; a.y += t * a.ldy; return a; };
+    for (int64_t t = 0; t < n; t += kNormRopeTokens) {
+        const int64_t some = std::min(n - t, kNormRopeTokens);
+        const dim3 blocks((unsigned)((some + per - 1) / per));
+        if (head_dim == 128) hipLaunchKernelGGL(norm_rope_kernel<128>, blocks, dim3(NR_WG), smem, st, from(q, t), from(k, t), positions + t, some, per, eps, l2);
+        else if (head_dim == 64) hipLaunchKernelGGL(norm_rope_kernel<64>, blocks, dim3(NR_WG), smem, st, from(q, t), from(k, t), positions + t, some, per, eps, l2);
+        else return hipErrorInvalidValue;
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_norm_rope_grad(const NormRopeSide& q, const NormRopeSide& k, const int32_t* positions, int64_t n, int head_dim, float eps, float theta,
