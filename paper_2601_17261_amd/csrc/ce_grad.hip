@@ -125,24 +125,26 @@ __global__ __launch_bounds__(256) void ce_softmax_grad_kernel(const float* __res
 
 // dX or dW: the shares' sums [shares][M][d] added in order, times *scale, as bf16
 __global__ __launch_bounds__(256) void ce_join_kernel(const float* __restrict__ sums, int shares, int64_t M, int64_t d, const float* __restrict__ scale, bf16_t* __restrict__ out, int64_t ldo) {
-    const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
-    if (i >= M * d) return;
-    float4 s = *reinterpret_cast<const float4*>(sums + i);
-    for (int k = 1; k < shares; k += 8) {
-        float4 o[8];
+    for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < M * d; i += (int64_t)gridDim.x * blockDim.x * 4) {
+        float4 s = *reinterpret_cast<const float4*>(sums + i);
+        for (int k = 1; k < shares; k += 8) {
+            float4 o[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) o[u] = *reinterpret_cast<const float4*>(sums + min(k + u, shares - 1) * M * d + i);
+            for (int u = 0; u < 8; ++u) o[u] = *reinterpret_cast<const float4*>(sums + min(k + u, shares - 1) * M * d + i);
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (k + u < shares) { s.x += o[u].x; s.y += o[u].y; s.z += o[u].z; s.w += o[u].w; }
+            for (int u = 0; u < 8; ++u)
+                if (k + u < shares) { s.x += o[u].x; s.y += o[u].y; s.z += o[u].z; s.w += o[u].w; }
+        }
+        const int64_t row = i / d;
+        const float f = *scale;
+        *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
     }
-    const int64_t row = i / d;
-    const float f = *scale;
-    *reinterpret_cast<uint2*>(out + row * ldo + (i - row * d)) = make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
 }
 hipError_t join(const float* sums, int shares, int64_t M, int64_t d, const float* scale, bf16_t* out, int64_t ldo, hipStream_t st) {
     const int wide = M * d <= 1 << 18 ? 64 : 256;      // (few values: a wave a workgroup, for the sake of their number)
-    hipLaunchKernelGGL(ce_join_kernel, dim3((unsigned)((M * d / 4 + wide - 1) / wide)), dim3(wide), 0, st, sums, shares, M, d, scale, out, ldo);
+    // (a launch of 2^32 threads and more is cut off without a word: from 2^33 values on workgroups go round)
+    const int64_t blocks = std::min<int64_t>((M * d / 4 + wide - 1) / wide, 1 << 23);
+    hipLaunchKernelGGL(ce_join_kernel, dim3((unsigned)blocks), dim3(wide), 0, st, sums, shares, M, d, scale, out, ldo);
     return hipGetLastError();
 }
 

@@ -54,16 +54,15 @@ __global__ __launch_bounds__(256) void ce32_d_kernel(float* __restrict__ z, int6
 }
 
 __global__ __launch_bounds__(256) void ce32_add_kernel(const float* __restrict__ part, float* __restrict__ sum, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) sum[i] += part[i];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) sum[i] += part[i];
 }
 
 // out [rows][ldo] = *scale in [rows][ldi]; in may be out
 __global__ __launch_bounds__(256) void ce32_out_kernel(const float* in, int64_t ldi, int64_t rows, int64_t d, const double* __restrict__ scale, float* out, int64_t ldo) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * d) return;
-    const int64_t row = i / d, c = i - row * d;
-    out[row * ldo + c] = (float)(*scale * (double)in[row * ldi + c]);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * d; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / d, c = i - row * d;
+        out[row * ldo + c] = (float)(*scale * (double)in[row * ldi + c]);
+    }
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -99,8 +98,10 @@ hipError_t product(const float* x, int64_t ldx, const float* w, int64_t ldw, int
     a.X = x; a.ldx = ldx; a.W = w; a.ldw = ldw; a.M = M; a.N = N; a.K = K; a.Y = y; a.ldy = ldy; a.r = 1;
     return launch_forward_f32_many(&a, 1, st);
 }
+// workgroups for so many values.  (A launch of 2^32 threads and more is cut off without a word: from 2^31 values on they go round)
+unsigned ce32_blocks(int64_t values) { return (unsigned)std::min<int64_t>((values + 255) / 256, 1 << 23); }
 hipError_t store(const float* in, int64_t ldi, int64_t rows, int64_t d, const double* scale, float* out, int64_t ldo, hipStream_t st) {
-    hipLaunchKernelGGL(ce32_out_kernel, dim3((unsigned)((rows * d + 255) / 256)), dim3(256), 0, st, in, ldi, rows, d, scale, out, ldo);
+    hipLaunchKernelGGL(ce32_out_kernel, dim3(ce32_blocks(rows * d)), dim3(256), 0, st, in, ldi, rows, d, scale, out, ldo);
     return hipGetLastError();
 }
 
@@ -137,7 +138,7 @@ hipError_t launch_ce_grad_f32(const CeGradF32Args& a, void* workspace, hipStream
         CE_TRY(flip(W, a.ldw, n, a.d, wt, nullptr, 0, st));
         CE_TRY(product(z, n, wt, n, a.M, a.d, n, v0 ? part : sum, a.d, st));
         if (v0) {
-            hipLaunchKernelGGL(ce32_add_kernel, dim3((unsigned)((a.M * a.d + 255) / 256)), dim3(256), 0, st, part, sum, a.M * a.d);
+            hipLaunchKernelGGL(ce32_add_kernel, dim3(ce32_blocks(a.M * a.d)), dim3(256), 0, st, part, sum, a.M * a.d);
             CE_TRY(hipGetLastError());
         }
     }

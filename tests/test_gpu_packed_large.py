@@ -22,3 +22,34 @@ def test_norms_with_rotation_of_2_26_tokens():
         k[a:b] = x[:b - a]
     ctx.glue_qk_norm_rope(None, k, pos.repeat(65)[:n].contiguous(), None, k, 64)
     assert all(torch.equal(k[a:b], want[:b - a]) for a, b in parts)
+
+
+def test_gradient_of_inputs_of_more_than_2_32_values():
+    """(69 GB) an fp32 layer in two pieces of its outputs.  Few rows are counted; the others' gradients are zeros"""
+    ctx = binding.Context()
+    n, d, v = 1 << 21, 2049, 300
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x, dx = torch.zeros(n, d, device="cuda"), torch.empty(n, d, device="cuda")
+    w = torch.randn(v, d, device="cuda", generator=gen) / d ** 0.5
+    ids, lse = torch.full((n,), -1, device="cuda", dtype=I32), torch.zeros(n, device="cuda")
+    rows = torch.tensor([0, 1, 70000, n // 2, n - 1030, n - 2, n - 1], device="cuda")
+    x[rows] = torch.randn(len(rows), d, device="cuda", generator=gen)
+    ids[rows] = torch.arange(len(rows), device="cuda", dtype=I32) * 49
+    y = x[rows].double() @ w.double().T
+    lse[rows] = y.logsumexp(1).float()
+    for part in (dx[:4096], dx[n // 2:n // 2 + 4096], dx[-4096:]):
+        part.fill_(7.0)
+    ctx.ce_backward(binding.make_layer(w, x), w, x, binding.make_loss(ids, binding.LOSS_CE), lse, dx, None)
+    p = (y - y.logsumexp(1, keepdim=True)).exp()
+    D = p.clone()
+    D[torch.arange(len(rows)), ids[rows].long()] -= 1.0
+    want = D @ w.double() / len(rows)
+    # steps of 2^-24: a logit's, lse's, their difference's and the exponential's to D, and six of the sums and the result
+    off = 2.0 ** -24 * ((p * (2 * y.abs() + 2 * y.logsumexp(1, keepdim=True).abs() + 8) + 8 * D.abs()) @ w.double().abs()) / len(rows)
+    assert ((dx[rows].double() - want).abs() <= off).all()
+    other = torch.ones(n, device="cuda", dtype=torch.bool)
+    other[rows] = False
+    for a in (0, n // 2, n - 4096):
+        assert not dx[a:a + 4096][other[a:a + 4096]].any()
+    del x, dx, ctx
+    torch.cuda.empty_cache()
