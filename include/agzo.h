@@ -309,8 +309,8 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
  * Inputs are only read; outputs (lse of the forward call too) may not overlap inputs (offsets and lengths too) or each other.
  * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, more than 2^16 sequences; n_k, or n_q times
- * the heads of a key head, from 2^31 - 1024 on; leading dimensions from 2^22 on), scale not positive and finite, overlapping outputs, k_len in the
- * backward call. */
+ * the heads of a key head, from 2^31 - 1024 on; 2^24 tiles of 128 rows or keys and more, reckoned as one more than fit for each sequence and key head; leading
+ * dimensions from 2^22 on), scale not positive and finite, overlapping outputs, k_len in the backward call. */
 typedef struct {
     const void *q, *k, *v;       /* [n_q][n_heads head_dim], [n_k][n_kv_heads head_dim] twice */
     int64_t ldq, ldk, ldv;
@@ -338,7 +338,7 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
  *     of a piece, of 2^27 bf16 or 2^26 fp32 values at most unless n_tokens or d_in pass 2^17.
  * Device, workspace and captures as for the calls on packed batches.
  * Errors: AGZO_EINVAL for a bad layer or loss, NULL or misaligned tensors, outputs (loss_dev and lse too) that overlap an input (ids, lse and g_dev
- * too) or each other, more than 2^21 tokens or inputs (backward). */
+ * too) or each other, more than 2^21 tokens or inputs (backward), 2^24 tokens of an fp32 layer. */
 int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, double* loss_dev, float* lse);
 int agzo_ce_backward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const void* X, const agzo_loss_spec* loss, const float* lse,
                      const double* g_dev, void* dX, int64_t lddx, void* dW, int64_t lddw);

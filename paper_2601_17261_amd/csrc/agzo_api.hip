@@ -1427,6 +1427,8 @@ int packed_args(agzo_ctx* ctx, const agzo_packed_attention* a, PackedArgs& out) 
     TRY(check_glue(ctx, a->n_k, dkv, {a->k, a->v}, {a->ldk, a->ldv}));
     out = PackedArgs{static_cast<const bf16_t*>(a->q), static_cast<const bf16_t*>(a->k), static_cast<const bf16_t*>(a->v), a->ldq, a->ldk, a->ldv,
                      a->cu_q, a->cu_k, a->n_seq ? a->k_len : nullptr, a->n_q, a->n_k, a->n_seq, a->n_heads, a->n_kv_heads, a->causal != 0, a->scale};
+    if (packed_units(out) >= kPackedUnits)
+        return fail(ctx, AGZO_EINVAL, "%d sequences of %d key heads, %lld queries, %lld keys: too many tiles", a->n_seq, a->n_kv_heads, (long long)a->n_q, (long long)a->n_k);
     return check_device(ctx);
 }
 }  // namespace
@@ -1452,6 +1454,7 @@ int agzo_ce_forward(agzo_ctx* ctx, const agzo_layer* L, const void* W, const voi
     TRY(check_ce(ctx, L, W, X, loss, c));
     if (!loss_dev || (reinterpret_cast<uintptr_t>(loss_dev) & 7)) return fail(ctx, AGZO_EINVAL, "loss_dev is NULL or misaligned");
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
+    if (c.dtype == AGZO_F32 && c.n_tokens >= (1LL << 24)) return fail(ctx, AGZO_EINVAL, "2^24 tokens and more of an fp32 layer");
     const int64_t size = c.dtype == AGZO_F32 ? 4 : 2;
     TRY(check_apart(ctx, {listed("loss_dev", loss_dev, 1, 8), listed("lse", lse, c.n_tokens)},
                     {named("X", X, c.ldx, c.n_tokens, c.d_in, size), named("W", W, c.ldw, c.d_out, c.d_in, size), listed("the target ids", loss->target, c.n_tokens)}));

@@ -440,6 +440,9 @@ struct PackedGrad {
     const bf16_t *out, *dout; int64_t ldo, lddo; const float* lse;
     bf16_t *dq, *dk, *dv; int64_t lddq, lddk, lddv;
 };
+// workgroups of a launch, at most (but for shares of the keys); below kPackedUnits: a launch of 2^32 threads and more is cut off without a word
+constexpr int64_t kPackedUnits = 1 << 24;
+int64_t packed_units(const PackedArgs& a);
 size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim);
 hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out, int64_t ldo, float* lse, void* workspace, hipStream_t st);
 size_t packed_backward_workspace_bytes(const PackedArgs& a, int head_dim);

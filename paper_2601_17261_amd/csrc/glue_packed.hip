@@ -1150,7 +1150,7 @@ hipError_t pk_launch_forward(const PackedArgs& a, bf16_t* out, int64_t ldo, floa
         // (the row tiles and, for each share of a sequence more, as many as a sequence may have; numbers behind the last leave at once)
         units += shares * (a.total_q * G / PK_ROWS + 1) * a.n_kv;
     }
-    if (units > 0x7FFFFFFFLL || blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    if (units >= kPackedUnits || (chunk > 0 && blocks >= kPackedUnits)) return hipErrorInvalidValue;
     const PkForwardOut to{out, ldo, lse, part, ml, chunk};
     if (fine) hipLaunchKernelGGL((pk_forward_kernel<HD, true>), dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, to);
     else hipLaunchKernelGGL((pk_forward_kernel<HD, false>), dim3((unsigned)units), dim3(64 * PK_WAVES), SMEM, st, a, to);
@@ -1169,7 +1169,7 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
     if (attr_kv != hipSuccess) return attr_kv;
     const int64_t rows = a.total_q * a.n_heads, G = a.n_heads / a.n_kv;
     const int64_t dq_units = pk_units(a.total_q * G, a.n_seq, a.n_kv), kv_units = pk_units(a.total_k, a.n_seq, a.n_kv);
-    if (dq_units > 0x7FFFFFFFLL || kv_units > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    if (dq_units >= kPackedUnits || kv_units >= kPackedUnits) return hipErrorInvalidValue;
     uint4* info = static_cast<uint4*>(workspace);
     const int shares = pk_dkv_shares(a);
     const int64_t kv_rows = a.total_k * a.n_kv, kv_blocks = (kv_rows * (HD / 2) + 255) / 256;
@@ -1193,6 +1193,7 @@ hipError_t pk_launch_backward(const PackedArgs& a, const PackedGrad& g, void* wo
 
 }  // namespace
 
+int64_t packed_units(const PackedArgs& a) { return std::max(pk_units(a.total_q * (a.n_heads / a.n_kv), a.n_seq, a.n_kv), pk_units(a.total_k, a.n_seq, a.n_kv)); }
 size_t packed_forward_workspace_bytes(const PackedArgs& a, int head_dim) {
     const int chunk = pk_chunk(a, head_dim);
     return chunk == 0 ? 0 : (size_t)pk_most_shares(a, chunk) * a.total_q * a.n_heads * (head_dim * sizeof(float) + sizeof(float2));

@@ -214,6 +214,7 @@ __global__ __launch_bounds__(256) void ce_rows_f32_kernel(const float* __restric
 
 hipError_t launch_ce_rows_f32(const float* Y, int64_t ldy, int64_t M, int64_t N, const int32_t* target, double* scratch,
                               double* out, hipStream_t st, float* lse) {
+    if (M >= (1LL << 24)) return hipErrorInvalidValue;        // (of 2^32 threads the low 32 bits are started)
     hipLaunchKernelGGL(ce_rows_f32_kernel, dim3((unsigned)M), dim3(256), 0, st, Y, ldy, M, N, target, scratch, lse);
     hipLaunchKernelGGL(ce_finish_kernel, dim3(1), dim3(256), 0, st, scratch, (int)M, out);
     return hipGetLastError();

@@ -53,3 +53,31 @@ def test_gradient_of_inputs_of_more_than_2_32_values():
         assert not dx[a:a + 4096][other[a:a + 4096]].any()
     del x, dx, ctx
     torch.cuda.empty_cache()
+
+
+def test_more_tiles_than_a_launch_takes_are_refused():
+    """65536 sequences of one token with 256 heads: (65536 + 512) 256 workgroups, 2^32 threads and more"""
+    ctx = binding.Context()
+    n, width = 65536, 256 * 64
+    q, k, v, out = (torch.empty(n, width, device="cuda", dtype=BF) for _ in range(4))
+    cu = torch.arange(n + 1, device="cuda", dtype=I32)
+    out[::1024] = 7.0
+    with pytest.raises(binding.AgzoError) as e:
+        ctx.glue_attention_packed(q, k, v, out, cu, cu, 64)
+    assert e.value.code == binding.EINVAL
+    lse = torch.zeros(n, 256, device="cuda")
+    with pytest.raises(binding.AgzoError) as e:
+        ctx.glue_attention_packed_backward(q, k, v, q, lse, k, out, torch.empty_like(k), torch.empty_like(v), cu, cu, 64)
+    assert e.value.code == binding.EINVAL and (out[::1024] == 7.0).all()
+
+
+def test_an_fp32_loss_of_2_24_tokens_is_refused():
+    ctx = binding.Context()
+    n = 1 << 24
+    w, x, ids = torch.ones(1, 1, device="cuda"), torch.ones(n, 1, device="cuda"), torch.zeros(n, device="cuda", dtype=I32)
+    out = torch.full((1,), 7.0, device="cuda", dtype=torch.float64)
+    with pytest.raises(binding.AgzoError) as e:
+        ctx.ce_forward(binding.make_layer(w, x), w, x, binding.make_loss(ids, binding.LOSS_CE), out)
+    assert e.value.code == binding.EINVAL and float(out) == 7.0
+    ctx.ce_forward(binding.make_layer(w, x[1:]), w, x[1:], binding.make_loss(ids[1:], binding.LOSS_CE), out)
+    assert float(out) == 0.0
