@@ -304,13 +304,14 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  * whatever they are (NaN and infinities too).  Rows of no sequence are neither read nor written.
  *   k_len (nullable; forward call only): how many of its keys sequence s has, the first k_len[s] (0 .. cu_k[s + 1] - cu_k[s]: a length outside is taken as
  *     the nearest of these): a cache with room for each sequence, of which the rest is not read
- *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key
+ *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key.  Scores are fp32
+ *     and so is lse: probabilities are off by 2^-22 of a row's largest score, and rows with scaled scores beyond 2^30 may be NaN
  *   backward: out, lse of the forward call with the same arguments and the gradient dout -> dq, dk, dv (all three written, for all rows of
  *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
  * Inputs are only read; outputs (lse of the forward call too) may not overlap inputs (offsets and lengths too) or each other.
  * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, more than 2^16 sequences; n_k, or n_q times
  * the heads of a key head, from 2^31 - 1024 on; 2^24 tiles of 128 rows or keys and more, reckoned as one more than fit for each sequence and key head; leading
- * dimensions from 2^22 on), scale not positive and finite, overlapping outputs, k_len in the backward call. */
+ * dimensions from 2^22 on), scale not finite or below 2^-100, overlapping outputs, k_len in the backward call. */
 typedef struct {
     const void *q, *k, *v;       /* [n_q][n_heads head_dim], [n_k][n_kv_heads head_dim] twice */
     int64_t ldq, ldk, ldv;

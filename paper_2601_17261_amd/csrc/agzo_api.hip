@@ -1417,7 +1417,8 @@ int packed_args(agzo_ctx* ctx, const agzo_packed_attention* a, PackedArgs& out) 
     constexpr int64_t most = 0x7FFFFFFFLL - 1024;
     if (a->n_q < 0 || a->n_k < 0 || a->n_k > most || a->n_q > most || a->n_q * (a->n_heads / a->n_kv_heads) > most || a->n_seq > 65536)
         return fail(ctx, AGZO_EINVAL, "%d sequences, %lld queries, %lld keys: too many", a->n_seq, (long long)a->n_q, (long long)a->n_k);
-    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return fail(ctx, AGZO_EINVAL, "scale must be positive and finite");
+    // (the gradient divides lse by it)
+    if (!(a->scale >= 0x1p-100f) || !(a->scale < INFINITY)) return fail(ctx, AGZO_EINVAL, "scale must be finite and 2^-100 at least");
     if (a->ldq >= (1LL << 22) || a->ldk >= (1LL << 22) || a->ldv >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "leading dimensions must be below 2^22");
     if (a->n_seq > 0 && (!a->cu_q || !a->cu_k || ((reinterpret_cast<uintptr_t>(a->cu_q) | reinterpret_cast<uintptr_t>(a->cu_k)) & 3)))
         return fail(ctx, AGZO_EINVAL, "cu_q or cu_k is NULL or misaligned");
