@@ -325,25 +325,23 @@ constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
 // ---- forward ---------------------------------------------------------------------------------------------------
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits.  A tile is 32 matrix instructions a wave (HD = 128, 1024 cycles) beside some 1200 cycles of other vector instructions and 32 KB of LDS reads.
-// chunk > 0: a row tile's keys are dealt out, `chunk` tiles of them a share, and workgroups take shares until there are none left, whose sums, maximum and
-// sum of exponentials they leave for pk_join_kernel
+// chunk > 0: a row tile's keys are dealt out, `chunk` tiles of them a share to a workgroup, which leaves its sums, maximum and sum of exponentials for pk_join_kernel
 // fine: the probabilities go into the second product in two bf16 parts.  For few rows beside the keys, whose time is the keys' reading: their sums are of few large
 // probabilities often, whose roundings no others' balance (single rows were off by 0.0021 to 0.0028 of their norm, and are by the 0.0017 of
 // the result's own rounding; 64 on 200000 keys: 206 us for 202)
 struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; int chunk; };
-// again: stored nothing, the tiles have to be gone over with care
-enum class PkDone { stored, again, none };
+// true: stored nothing, the tiles have to be gone over with care
 template <int HD, bool fine, bool careful>
-__device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwardOut& to_, int unit, pk_lchar lds) {
+__device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardOut& to_, pk_lchar lds) {
     char* pk_smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
     constexpr int TILE = PK_T * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
     // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
-    const int G = PkDiv(a.n_kv)(a.n_heads), at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
+    const int G = PkDiv(a.n_kv)(a.n_heads), unit = (int)blockIdx.x, at = PkDiv(a.n_kv)(unit), kvh = unit - at * a.n_kv;
     PkTile t;
-    if (!pk_find<PK_ROWS, false>(a, at, G, to_.chunk, t)) return PkDone::none;
+    if (!pk_find<PK_ROWS, false>(a, at, G, to_.chunk, t)) return false;
     const PkDiv by_group(G);
     const int R = t.nq * G, row0 = t.tile * PK_ROWS + wave * 32, shift = t.nk - t.nq;
     // The lane's row: its query, its head, the last key that it sees.  (Worked out where they are needed, from a lane number that the compiler does not know
@@ -363,7 +361,7 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
     const int tiles = last < 0 ? 0 : last / PK_T + 1;
     const int j0 = to_.chunk > 0 ? t.share * to_.chunk : 0, j1 = to_.chunk > 0 ? min(tiles, j0 + to_.chunk) : tiles;
     // (a share that none of the row tile sees.  The first one is there for rows that see nothing at all)
-    if (j0 >= j1 && t.share > 0) return PkDone::stored;
+    if (j0 >= j1 && t.share > 0) return false;
     const bf16_t* Kh = a.k + (int64_t)t.k0 * a.ldk + kvh * HD;
     const bf16_t* Vh = a.v + (int64_t)t.k0 * a.ldv + kvh * HD;
     PkLoader<HD> lk, lv;
@@ -491,12 +489,11 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
         one_tile(j);
         if (j + 1 < j1) arrive(j + 1);
     }
-    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return PkDone::again;
-    if (careful) __syncthreads();
+    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return true;
     l = pk_sum_halves(l);
     const Row r = row_of_lane();
     if (to_.part) {
-        if (!r.mine) return PkDone::stored;
+        if (!r.mine) return false;
         const int64_t at = (int64_t)t.share * a.total_q * a.n_heads + r.tok * a.n_heads + r.head;
         float* to = to_.part + at * HD + 4 * hi;
 #pragma unroll
@@ -505,24 +502,20 @@ __device__ __forceinline__ PkDone pk_forward(const PackedArgs& a, const PkForwar
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<float4*>(to + 32 * db + 8 * g) = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
         if (hi == 0) to_.part_ml[at] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
-        return PkDone::stored;
+        return false;
     }
     const bool empty = r.limit < 0;
     pk_store<HD>(acc, empty ? 0.f : 1.f / l, to_.out + r.tok * to_.ldo + (int64_t)r.head * HD, r.mine);
     if (to_.lse && r.mine && hi == 0) to_.lse[r.tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
-    return PkDone::stored;
+    return false;
 }
 // (a function that is called: its registers are not the kernel's)
 template <int HD, bool fine>
-__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, int unit, pk_lchar lds) { (void)pk_forward<HD, fine, true>(a, to, unit, lds); }
+__device__ __noinline__ void pk_forward_again(PackedArgs a, PkForwardOut to, pk_lchar lds) { (void)pk_forward<HD, fine, true>(a, to, lds); }
 template <int HD, bool fine>
 __global__ __launch_bounds__(64 * PK_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void pk_forward_kernel(PackedArgs a, PkForwardOut to) {
     extern __shared__ __align__(1024) char pk_dynamic[];
-    for (int unit = (int)blockIdx.x;; unit += (int)gridDim.x) {
-        const PkDone done = pk_forward<HD, fine, false>(a, to, unit, (pk_lchar)pk_dynamic);
-        if (done == PkDone::again) pk_forward_again<HD, fine>(a, to, unit, (pk_lchar)pk_dynamic);
-        if (done == PkDone::none || to.chunk == 0) return;
-    }
+    if (pk_forward<HD, fine, false>(a, to, (pk_lchar)pk_dynamic)) pk_forward_again<HD, fine>(a, to, (pk_lchar)pk_dynamic);
 }
 
 // Shares of the keys joined: HD / 4 lanes a row.  Rows of no sequence are left alone: their partial sums are what the workspace held
