@@ -22,3 +22,16 @@ def test_inputs_gradients_of_several_pieces_in_ragged_tiles(n, d, v):
     check(got, exact(w, x, ids))
     one = run(binding.Context(), w, x, ids, dw=False)
     assert torch.equal(one["dx"], got["dx"])
+
+
+@pytest.mark.parametrize("n,d,v", [(7, 64, 500), (31, 264, 3001), (50, 128, 900), (120, 512, 2000), (200, 256, 5000), (70, 256, 30000), (600, 200, 700), (1500, 264, 4001)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_rows_that_are_not_counted_have_no_part_on_any_way(n, d, v, value):
+    ctx = binding.Context()
+    w, x, ids = make(n, n, d, v)
+    ids[2], ids[n - 1] = -1, v
+    clean = run(ctx, w, x, ids)
+    y = x.clone()
+    y[2], y[n - 1] = value, value
+    got = run(ctx, w, y, ids)
+    assert not got["dx"][2].any() and not got["dx"][n - 1].any() and all(torch.equal(got[name], clean[name]) for name in ("dx", "dw", "loss"))

@@ -6,7 +6,7 @@ import torch
 
 import packed_reference as ref
 from paper_2601_17261_amd import binding
-from test_gpu_packed_attention import check, make, run
+from test_gpu_packed_attention import MARK, check, make, run
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +128,15 @@ def test_the_queries_gradient_of_one_tile_of_keys_has_two_parts_and_its_own_delt
     got = run(binding.Context(), q, k, v, d, cq, ck, dim)
     want, off = fp32_bounds(q, k, v, cq.tolist(), ck.tolist(), dim, d)["dq"]
     within(got["dq"], want, off, "dq")
+
+
+@pytest.mark.parametrize("qlens,klens", [([], []), ([0], [0]), ([0, 0], [70, 3]), ([3, 200], [0, 0]), ([0, 5, 0], [0, 0, 9])])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_no_queries_or_no_keys(qlens, klens, dim):
+    """Of rows that see nothing 0 and -inf, and of keys that nothing sees gradients of 0; where there are no sequences nothing is written"""
+    ctx = binding.Context()
+    for behind in (0, 4):
+        q, k, v, d, cq, ck = make(7, qlens, klens, 4, 2, dim, behind=behind)
+        for name, t in run(ctx, q, k, v, d, cq, ck, dim).items():
+            n = sum(klens if name in ("dk", "dv") else qlens)
+            assert (t[:n] == (-float("inf") if name == "lse" else 0.0)).all() and (t[n:] == MARK).all(), name
