@@ -275,7 +275,7 @@ int agzo_glue_add(agzo_ctx* ctx, void* h, int64_t ldh, const void* delta, int64_
  * These calls need the device that is current to be the context's.  They use the context's workspace, which cannot grow while the
  * stream is captured: a call that would have to make it larger then is refused with AGZO_ENOMEM and enqueues nothing (make the call once
  * before the capture).  A workspace that a captured call uses stays allocated until agzo_destroy, also where the context's grows
- * later; graphs captured from one context share it and must not run at the same time.
+ * later; graphs captured from one context share it and must not run at the same time, nor beside the context's other calls.
  *
  * qk_norm_rope: norms of queries and keys for each head with the rotation by the token's position in one pass.  For the head_dim = D
  *   values x of a head, n = gain x / sqrt(mean(x^2) + eps) (gain: device fp32 [D], the same for all heads, NULL = 1), then the pair
@@ -299,15 +299,17 @@ int agzo_glue_qk_norm_rope_backward(agzo_ctx* ctx, const void* q, int64_t ldq, c
  * cu_k[s + 1] - 1 (device int32 [n_seq + 1], not decreasing, within 0 .. n_q and 0 .. n_k: offsets outside are taken as the nearest inside);
  * its queries are its last positions: with causal != 0 query i of Lq sees the keys 0 .. i + Lk - Lq of Lk, else all Lk.  Lq = Lk is a prompt,
  * Lq = 1 a new token behind the keys that are there.  out = softmax(scale q k^T) v for each head (head h reads key head h / (n_heads / n_kv_heads)); the
- * probabilities are rounded to bf16 for the second product (to two bf16 parts where queries are single ones or few beside the keys), sums are fp32.  A query
- * that sees no key (Lk < Lq, or no keys at all) gets 0 and takes part in no gradient.  Values of keys that a query does not see have no part in its result,
- * whatever they are (NaN and infinities too).  Rows of no sequence are neither read nor written.
+ * probabilities are rounded to bf16 for the second product (to two bf16 parts where n_q is n_seq at most, or n_q times the heads of a key head an eighth of n_k),
+ * sums are fp32.  A query that sees no key (Lk < Lq, or no keys at all) gets 0 and takes part in no gradient.  Values of keys that a query does not see have no
+ * part in its result, whatever they are (NaN and infinities too).  Rows of no sequence are neither read nor written.
  *   k_len (nullable; forward call only): how many of its keys sequence s has, the first k_len[s] (0 .. cu_k[s + 1] - cu_k[s]: a length outside is taken as
  *     the nearest of these): a cache with room for each sequence, of which the rest is not read
  *   lse (nullable in the forward call): device fp32 [n_q][n_heads], log sum exp of a row's scaled scores, -inf for a query that sees no key.  Scores are fp32
- *     and so is lse: probabilities are off by 2^-22 of a row's largest score, and rows with scaled scores beyond 2^30 may be NaN
+ *     and so is lse: probabilities are off by up to 2^-22 (of themselves) times a row's largest score, and rows with scaled scores beyond 2^30 may be NaN
  *   backward: out, lse of the forward call with the same arguments and the gradient dout -> dq, dk, dv (all three written, for all rows of
- *     sequences).  The sums over the heads of a group and over queries are fp32, in an order that depends on the lengths alone.
+ *     sequences).  The sums over the heads of a group and over queries are fp32.  Probabilities and dS = P (dP - rowsum(dout out)) are rounded to bf16 for dk and
+ *     dv, dS to two bf16 parts for dq; rowsum(dout out) is that of out as it is given (in sequences of up to 64 keys: of the probabilities themselves).
+ * Results repeat bit for bit.  Forms and orders of sums go by the tensors' sizes and the lengths of all sequences, so that a sequence can have other last bits beside others.
  * Inputs are only read; outputs (lse of the forward call too) may not overlap inputs (offsets and lengths too) or each other.
  * Errors: AGZO_EINVAL for NULL or misaligned tensors, a bad shape (heads no multiple of key heads, head_dim, more than 2^16 sequences; n_k, or n_q times
  * the heads of a key head, from 2^31 - 1024 on; 2^24 tiles of 128 rows or keys and more, reckoned as one more than fit for each sequence and key head; leading
@@ -327,16 +329,19 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
                                         const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
                                         int64_t lddv);
 
-/* Token cross-entropy of a layer's outputs and its gradient (an LM head: d_out outputs; the layer's r, y_dtype and ldy are not used), without
- * the logits ever being stored.  loss: kind AGZO_LOSS_CE, target ids [n_tokens]; rows whose id is not in [0, d_out) are not counted.
+/* Token cross-entropy of a layer's outputs and its gradient (an LM head: d_out outputs; the layer's r, y_dtype and ldy are not used).  The logits of bf16
+ * layers are never stored whole; the forward call of an fp32 layer keeps n_tokens d_out fp32 of them in the workspace.
+ * loss: kind AGZO_LOSS_CE, target ids [n_tokens]; rows whose id is not in [0, d_out) are not counted.
  *   ce_forward: *loss_dev = mean over the counted rows of lse_t - y_t[id] (0 if there are none) and, where wanted, lse [n_tokens] device fp32,
  *     lse_t = log sum exp of row t's logits, of every row.  bf16 and fp32 layers; the loss is agzo_layer_forward_sketch's, bit for
  *     bit for fp32 layers and from 256 tokens on (fewer may have sums of their own order).
  *   ce_backward: with D = (softmax(Y) - onehot(id)) g / count in the counted rows, 0 in the others, dX = D W [n_tokens][d_in]
  *     and dW = D^T X [d_out][d_in], of the layer's type, overwritten; either may be NULL.  lse: of ce_forward with the same arguments; g = *g_dev (1 if NULL).  The
  *     logits are made again for a piece of the outputs at a time; of bf16 layers D without g / count is rounded to bf16 for the products and sums are
- *     fp32, of fp32 layers D is fp32 and sums are fp64, those over pieces fp32; their order depends on the shape alone.  Workspace: three to five buffers
- *     of a piece, of 2^27 bf16 or 2^26 fp32 values at most unless n_tokens or d_in pass 2^17.
+ *     fp32, of fp32 layers D is fp32 and sums are fp64, those over pieces fp32; their order depends on the shape alone.  Workspace, for a piece of n
+ *     outputs: D and D^T (n n_tokens values each), W transposed (n d_in, where dX is wanted), of at most 2^27 bf16 or 2^26 fp32 values each unless n_tokens or
+ *     d_in pass 2^17; X transposed (n_tokens d_in, where dW is wanted); fp32 sums of dX (n_tokens d_in) and of a piece of dW (n d_in), up to 16 times (64 times below
+ *     256 tokens or inputs) where they are made in shares; fp32 logits of a piece where no 256 x 256 tile fits.  Up to 32 tokens of a bf16 layer, and up to 255 where outputs are few, n is all outputs.
  * Device, workspace and captures as for the calls on packed batches.
  * Errors: AGZO_EINVAL for a bad layer or loss, NULL or misaligned tensors, outputs (loss_dev and lse too) that overlap an input (ids, lse and g_dev
  * too) or each other, more than 2^21 tokens or inputs (backward), 2^24 tokens of an fp32 layer. */

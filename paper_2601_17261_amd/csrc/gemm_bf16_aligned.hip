@@ -768,7 +768,8 @@ __device__ __forceinline__ void aligned_tiles(const AlignedArgs<PHASES, CAP>& tb
             if (!more) break;
         } else if constexpr (OUT == 3) {
             // As above with fp32 values: a token block of the wave, 16 tokens of 128 outputs, at a time, stored two whole rows to an instruction.
-            // What the tile before this one stores is left to it, for sums that are added to may be added to once
+            // What the tile before this one stores is left to it, for sums that are added to may be added to once.  (Some 40 registers are spilled, addresses that a
+            // tile's end and beginning read back; none in the loop over slices)
             settle();
             char* stg = smem + W_BASE + ((wst == 0) ? 2 : wst - 1) * TILE_BYTES + wave * 8192;
             const int rs = RAGGED ? (int)(tm * BT - m0) - wb * 128 : 0, cs = RAGGED ? (int)(tn * BT - n0) - wa * 128 : 0;

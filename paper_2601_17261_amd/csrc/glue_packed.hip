@@ -219,7 +219,8 @@ __device__ __forceinline__ int pk_total(int x) {
 // Tile number t of all sequences' tiles, UNIT rows (BY_KEYS: keys) each; with chunk > 0 a row tile is one for every `chunk` tiles of 64 keys that its sequence has.
 // The tiles that see most (BY_KEYS: that are seen most) of up to 64 sequences come first: a sequence's last row tile (its first tile of keys) is as many
 // levels high as it has tiles, the next one a level less, and tiles are numbered level by level.  (Sequence by sequence a long one may start
-// last: 8192 tokens in eight of up to 1923 took dk, dv 260 us, so 170.)  Offsets are taken as far as they lie inside the tensors and grow
+// last: a training pass of 8192 tokens in eight of up to 1923 took 444 us, so 338.  From 65 sequences on, and with chunk > 0, it is sequence by sequence all the
+// same.)  Offsets are taken as far as they lie inside the tensors and grow
 template <int UNIT, bool BY_KEYS>
 __device__ __forceinline__ bool pk_find(const PackedArgs& a, int t, int G, int chunk, PkTile& out) {
     const int lane = threadIdx.x & 63, total_q = (int)a.total_q, total_k = (int)a.total_k;
@@ -328,7 +329,7 @@ constexpr int PK_WAVES = 4, PK_ROWS = 32 * PK_WAVES;
 // chunk > 0: a row tile's keys are dealt out, `chunk` tiles of them a share to a workgroup, which leaves its sums, maximum and sum of exponentials for pk_join_kernel
 // fine: the probabilities go into the second product in two bf16 parts.  For few rows beside the keys, whose time is the keys' reading: their sums are of few large
 // probabilities often, whose roundings no others' balance (single rows were off by 0.0021 to 0.0028 of their norm, and are by the 0.0017 of
-// the result's own rounding; 64 on 200000 keys: 206 us for 202)
+// the result's own rounding; 64 on 200000 keys: 175 us for 171)
 struct PkForwardOut { bf16_t* out; int64_t ldo; float* lse; float* part; float2* part_ml; int chunk; };
 // true: stored nothing, the tiles have to be gone over with care
 template <int HD, bool fine, bool careful>
@@ -405,8 +406,8 @@ __device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardO
 #pragma unroll
             for (int i = 0; i < 4; ++i) read_k(i);
             __builtin_amdgcn_sched_barrier(0);
-            // (of a SIMD's two waves the one that has matrix instructions to issue goes first, beside the other's maxima and exponentials.  16001 tokens: 1029 us, 1074
-            // without; 1047 with the exponentials among the second product's instructions)
+            // (of a SIMD's two waves the one that has matrix instructions to issue goes first, beside the other's maxima and exponentials.  16001 tokens: 1022 us, 1079
+            // without; 1038 with the exponentials among the second product's instructions)
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 2 * KS; ++i) {
@@ -459,7 +460,7 @@ __device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardO
                 return;
             }
             // (heads of 64, whose tiles are half the matrix instructions beside as many exponentials: those of 16 keys beside the second product of the 16 before
-            // them; 8192 tokens forward and back 214 us, 219 like heads of 128)
+            // them; 8192 tokens forward and back 213 us, 222 like heads of 128)
             constexpr bool beside = HD == 64;
 #pragma unroll
             for (int e = 0; e < (beside ? 8 : 32); e += 2) two(e);
@@ -639,7 +640,9 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
     PkFrag qf[KS], df[KS];
     const float sc = a.scale * PK_LOG2E;
     float2 info;                                                              // lse log2 e, delta
-    auto begin = [&]() __attribute__((always_inline)) {                       // (as in the forward)
+    // (as in the forward.  Heads of 128 are out of registers all the same: an LDS offset is reloaded in every tile behind the request of the next one, whose loads
+    // the wait for it is for too)
+    auto begin = [&]() __attribute__((always_inline)) {
         if (tiles > 0) request(0);
         const Row r = row_of_lane();
         const bf16_t* qsrc = a.q + r.tok * a.ldq + (int64_t)r.head * HD + 8 * hi;
@@ -681,7 +684,7 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
             const bool mask = kb + PK_T - 1 > wfirst;
             // (operands two pairs of instructions ahead; see the forward)
             // dS in two bf16 parts (16 bits): the keys of a head share directions, dS of a row sums to 0, so that its roundings are large beside what is left of
-            // the sum: in one part dq was off by 0.0028 of its norm, and is by 0.0020 (0.0017 is out's own rounding).  8192 tokens: 131 us for 105
+            // the sum: in one part dq was off by 0.0028 of its norm, and is by 0.0020 (0.0017 is its own rounding).  8192 tokens forward and back: 338 us, 320 in one
             PkFrag fk[2], fv[2], ft[2], pf[4], pl[4];
             const PkOffsets<HD> o(off, lds_at + (j & 1) * (2 * TILE));
             auto read_rows = [&](int i) __attribute__((always_inline)) {
@@ -949,6 +952,8 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
                 // (the only key that a row sees has the probability 1 whatever its score)
                 d_[e & 1] = seen && l > 0 ? d_[e & 1] : 0.f;
             }
+            // (in one bf16 part each: dk and dv are off by 0.0024 and 0.0023 of their norms, of which 0.0017 is their own rounding.  Second parts would be half as many
+            // matrix instructions again, and registers that there are none of)
             if (e & 1) {
                 pf[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(p_[0], p_[1]);
                 df[2 * h + (e >> 3)].w[(e & 7) >> 1] = pack_bf16x2(d_[0], d_[1]);
@@ -1090,8 +1095,9 @@ int64_t pk_units(int64_t total, int n_seq, int n_kv) { return (total / PK_ROWS +
 // Tiles of 64 keys a share, 0: row tiles are not shared out.  They are where rows are few beside the keys (single new tokens: a sequence is a
 // workgroup for each key head then, whatever its length) or where row tiles are fewer than the compute units: for about two shares to each of two workgroups on a
 // compute unit, of 8 tiles and more (a share costs a workgroup's start, its sums and a launch that joins them), 128 of a sequence at most and 256 MB of sums.
-// Lengths are on the device: work is reckoned from their mean, and sequences of 16 tiles and more in the mean are taken to be uneven.  64 sequences of 200000
-// keys together, up to 16760: 380 us without, 206 so, 216 with one share to each
+// Lengths are on the device: work is reckoned from their mean, and sequences of 16 tiles and more in the mean are taken to be uneven.  (Where a
+// cache's rooms are mostly empty, or one long sequence is among many short ones, shares are too few for it.)  64 sequences of 200000
+// keys together, up to 16760: 426 us without, 175 so, 186 with one share to each
 bool pk_few_rows(const PackedArgs& a) { return a.total_q * (a.n_heads / a.n_kv) * 8 <= a.total_k; }
 int pk_chunk(const PackedArgs& a, int head_dim) {
     const int64_t G = a.n_heads / a.n_kv, units = pk_units(a.total_q * G, a.n_seq, a.n_kv), rows = a.total_q * a.n_heads;
