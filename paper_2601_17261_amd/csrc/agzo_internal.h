@@ -43,6 +43,13 @@ __device__ __forceinline__ void split3_bf16(float f, bf16_t& hi, bf16_t& mid, bf
     lo = f32_to_bf16(r2);
 }
 
+// A barrier in a loop, behind which waves read what others have written to LDS.  The wait stands by itself: where a loop's ways meet the compiler drops, in some
+// kernels, the one that __syncthreads() stands for
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0)
+    __syncthreads();
+}
+
 // ---------------------------------------------------------------------------
 // Philox4x32-10 (Salmon et al., SC'11) and the Box-Muller map used for every
 // Gaussian matrix of the method (Alg. 2: generated from a seed, never stored).

@@ -294,13 +294,6 @@ struct PkLoader {
     }
 };
 
-// The barrier of a loop over tiles, behind which waves read what others have written to LDS.  (The wait by itself: where a loop's ways meet, the compiler has
-// dropped the one that __syncthreads() stands for, in the loop of dk, dv)
-__device__ __forceinline__ void pk_tile_barrier() {
-    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0)
-    __syncthreads();
-}
-
 __device__ __forceinline__ void pk_zero(pk_floatx16& x) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
@@ -485,7 +478,7 @@ __device__ __forceinline__ bool pk_forward(const PackedArgs& a, const PkForwardO
     begin();
     if (j0 < j1) arrive(j0);
     for (int j = j0; j < j1; ++j) {
-        pk_tile_barrier();
+        lds_barrier();
         if (j + 1 < j1) request(j + 1);
         one_tile(j);
         if (j + 1 < j1) arrive(j + 1);
@@ -789,7 +782,7 @@ __device__ __forceinline__ bool pk_dq(const PackedArgs& a, const PkBackward& g, 
         }
     }
     for (int j = 0; j < tiles; ++j) {
-        pk_tile_barrier();
+        lds_barrier();
         if (j + 1 < tiles) request(j + 1);
         one_tile(j);
         if (j + 1 < tiles) arrive(j + 1);
@@ -1031,7 +1024,7 @@ __device__ __forceinline__ bool pk_dkv(const PackedArgs& a, const PkBackward& g,
     begin();
     if (tiles > 0) arrive(0);
     for (int j = 0; j < tiles; ++j) {
-        pk_tile_barrier();
+        lds_barrier();
         if (j + 1 < tiles) request(j + 1);
         one_tile(j);
         // (the sums stay in accumulation registers: where the ways through a tile meet, the compiler takes them to ordinary ones and back, 256 instructions)

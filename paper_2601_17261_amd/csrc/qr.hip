@@ -168,19 +168,19 @@ __device__ int factor_inverse(double* G, double* Rinv, int r) {
     const doublex4 zero = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 1
     for (int p = 0; p < Q::NB; ++p) {
-        __syncthreads();
+        lds_barrier();
         if (wave == 0) {
             const int bad = factor16(G + Q::pair(p, p) * QR_BLK, Rinv + Q::pair(p, p) * QR_BLK, min(16, r - 16 * p));
             if (bad && tid == 0) bad_s = 1;
         }
-        __syncthreads();
+        lds_barrier();
         if (p + 1 < Q::NB) {
             const int q = p + 1 + wave;                          // panel: R_pq = R_pp^-T G_pq
             if (q < Q::NB) {
                 double* blk = G + Q::pair(p, q) * QR_BLK;
                 put_block(blk, mul_tn(Rinv + Q::pair(p, p) * QR_BLK, blk, zero, false));
             }
-            __syncthreads();
+            lds_barrier();
             int job = 0;                                         // trailing blocks: G_ab -= R_pa^T R_pb
             for (int a = p + 1; a < Q::NB; ++a)
                 for (int b = a; b < Q::NB; ++b, ++job) {
@@ -200,7 +200,7 @@ __device__ int factor_inverse(double* G, double* Rinv, int r) {
             put_block(blk, t);
             put_block(blk, mul_nn(Rinv + Q::pair(p, p) * QR_BLK, blk, zero, true));
         }
-        __syncthreads();
+        lds_barrier();
     }
     return bad_s;
 }
