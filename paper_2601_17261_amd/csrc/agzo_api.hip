@@ -748,6 +748,10 @@ int agzo_create(agzo_ctx** out, void* hip_stream) {
 
 void agzo_destroy(agzo_ctx* ctx) {
     if (!ctx) return;
+    // (Callers' languages let go of contexts at times of their own, also while this thread captures another stream: in the other modes the waits and frees below
+    // would end that capture.  What is waited for and freed here is none of it)
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool exchanged = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
     (void)hipStreamSynchronize(ctx->stream);
     if (ctx->side) {
         (void)hipStreamSynchronize(ctx->side);    // (joined to the above, unless joining failed)
@@ -764,6 +768,7 @@ void agzo_destroy(agzo_ctx* ctx) {
         for (hipEvent_t e : pc.stop) (void)hipEventDestroy(e);
     }
     delete ctx;
+    if (exchanged) (void)hipThreadExchangeStreamCaptureMode(&mode);
 }
 
 const char* agzo_last_error(const agzo_ctx* ctx) { return ctx ? ctx->err : "null context"; }
