@@ -329,6 +329,89 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
                                         const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
                                         int64_t lddv);
 
+/* Serving from a cache of keys and values in pages, with tokens drafted ahead (bf16 device tensors as above, head_dim 64 or 128; device, workspace and captures as for the
+ * calls on packed batches).  One step of a program: cache_append (the new tokens' queries turned, their keys and values into the cache), attention_paged, the layer's rest, and behind the last layer
+ * verify_drafts and, for trees, cache_keep in each layer.
+ *
+ * The cache: place p of sequence s lies in page id = table[s ld_table + p / page_size], slot i = p % page_size; its key of key head h are the head_dim values from k + id k_page + i k_row +
+ * h k_head on (in values; v likewise), so that heads may lie inside tokens or tokens inside heads, and k and v in one tensor.  Strides of axes of more than one index are multiples of 8, do not make
+ * rows overlap, and k_row, v_row are below 2^22; k and v are 16-byte aligned.  Pages may be shared by sequences that only read them.
+ * New tokens: sequence s has the rows cu_q[s] .. cu_q[s + 1] - 1 of a call (device int32 [n_seq + 1], as in packed batches), which are its last places: k_len[s] counts them too, so that row i
+ * of m has the place k_len[s] - m + i.  A length outside 0 .. max_pages page_size is taken as the nearest of these.  Rows of no sequence are neither read nor written.
+ * Errors of all calls: AGZO_EINVAL for NULL or misaligned tensors, a bad shape or layout (more than 1024 key heads, 2^16 sequences, 2^26 new tokens, or 2^31 - 1024 places of a sequence), outputs that
+ * overlap inputs or each other (the cache counted from its first to its last value). */
+typedef struct {
+    void *k, *v;
+    int64_t k_page, k_row, k_head, v_page, v_row, v_head;   /* in values */
+    int64_t n_pages;
+    const int32_t* table;        /* device int32 [n_seq][ld_table]: ids of pages, max_pages a sequence */
+    int64_t ld_table;
+    const int32_t* k_len;        /* device int32 [n_seq] */
+    int32_t page_size, max_pages, n_seq, n_kv_heads, head_dim;
+} agzo_paged_cache;
+
+/* Rotation by position.  Of a head's values x the first rot_dim (a multiple of 16) are turned in pairs (a, b) = (p, p + rot_dim/2), or (2p, 2p + 1) if interleaved != 0, by the angle
+ * t f'_p, t the position:  y_a = magnitude (x_a cos - x_b sin),  y_b = magnitude (x_b cos + x_a sin);  the rest stays.  With f_p = theta^(-2p/rot_dim), what a pair keeps of it in a context
+ * longer than the trained one is f'_p = f_p (m + (1 - m) / factor):
+ *   PLAIN: m = 1;   LINEAR: m = 0;
+ *   TURNS: m goes from 0 to 1 as the turns that the pair makes in `original` positions, original f_p / (2 pi), go from low to high;
+ *   DIMS: m goes from 1 to 0 as p goes from the pair that makes `high` turns in them (rounded down, 0 at least) to the one that makes `low` (rounded up, rot_dim - 1 at most).
+ * Angles are reduced in fp64 (any int32 position), products are fp32, one rounding. */
+enum { AGZO_ROPE_PLAIN = 0, AGZO_ROPE_LINEAR = 1, AGZO_ROPE_TURNS = 2, AGZO_ROPE_DIMS = 3 };
+typedef struct {
+    int32_t rot_dim, interleaved;
+    float theta;
+    int32_t scaling;
+    float factor, low, high, original;   /* of the scalings that use them */
+    float magnitude;
+} agzo_rope;
+
+/* rope: q [n][n_heads head_dim] -> q_out, k [n][n_kv_heads head_dim] -> k_out, of dtype AGZO_BF16 or AGZO_F32, head_dim a multiple of 16 up to 256; either side may be left out with 0
+ * heads.  An output may be its own input (same pointer and leading dimension).  positions: device int32 [n].  Norms with it, for the whole head in halves: qk_norm_rope.
+ * rope_backward: from the gradients with respect to its results those with respect to q and k (in place too): the turn by the opposite angle, times magnitude.
+ * Errors: AGZO_EINVAL for NULL or misaligned tensors (leading dimensions are multiples of 8), a bad shape, a rotation that is none, overlaps. */
+int agzo_glue_rope(agzo_ctx* ctx, const agzo_rope* rope, int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out, int64_t ldqo,
+                   void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+int agzo_glue_rope_backward(agzo_ctx* ctx, const agzo_rope* rope, int32_t dtype, const void* dq_out, int64_t lddqo, const void* dk_out, int64_t lddko, const int32_t* positions, void* dq,
+                            int64_t lddq, void* dk, int64_t lddk, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+
+/* cache_append: k and v of the new tokens ([n][n_kv_heads head_dim]) to their places in the cache, q ([n][n_heads head_dim]; n_heads 0: none) to q_out, which may be q.  Queries and keys are, with
+ * norm != 0, divided by sqrt(mean(x^2) + eps) of their head and multiplied with a gain (device fp32 [head_dim], NULL = 1), then turned as `rope` says (NULL: not at all) by positions[t] (device
+ * int32 [n]; NULL: by the token's place), in fp32 with one rounding.  What has no place (k_len[s] below the number of new tokens, an id in the table that is no page's) is not stored; its
+ * query is turned all the same.  Two new tokens of one call may not have the same place (sequences that share the page): one of them is stored, or parts of both. */
+int agzo_glue_cache_append(agzo_ctx* ctx, const agzo_paged_cache* cache, const agzo_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           const int32_t* cu_q, int64_t n, int32_t n_heads, const int32_t* positions, void* q_out, int64_t ldqo, int32_t norm, const float* q_gain, const float* k_gain,
+                           float eps);
+
+/* attention_paged: out = softmax(scale q k^T) v for each head over the cache; q, out [n][n_heads head_dim], n_heads a multiple of n_kv_heads.  New token i of m sees its sequence's places
+ * 0 .. k_len[s] - m + i; or, with tree (device int32 [n][ld_tree], tree_words of a row used, the lowest bit first), all places in front of the new ones and, of those, the ones j whose bit j is set in
+ * its row (bits behind the words are not set; a token that sees itself has its own bit set).  A token that sees no place gets 0.  Keys and values that a token does not see have
+ * no part in its result, whatever they are; what a page holds behind a sequence's last place is not read.  Ids in the table that are no page's are taken as the nearest.
+ * lse (nullable): device fp32 [n][n_heads], log sum exp of a row's scaled scores, -inf where it sees none.  Precisions as for attention over packed sequences, the probabilities in two bf16 parts up
+ * to 512 rows (n times the heads of a key head) a sequence in the mean.  Results repeat bit for bit; orders of sums go by the lengths of all sequences.
+ * Errors also: scale not finite or below 2^-100, n times the heads of a key head from 2^31 - 1024 on, 2^24 tiles of rows and more, q's leading dimension from 2^22 on. */
+int agzo_glue_attention_paged(agzo_ctx* ctx, const agzo_paged_cache* cache, const void* q, int64_t ldq, const int32_t* cu_q, int64_t n, int32_t n_heads, float scale, const int32_t* tree,
+                              int64_t ld_tree, int32_t tree_words, void* out, int64_t ldo, float* lse);
+
+/* cache_keep: accepted tokens of a tree together.  Of sequence s's m new places the ones rows[cu_q[s]], rows[cu_q[s] + 1], .. (n_kept[s] of them, device int32; each behind the one before) are
+ * moved to its new places 1, 2, ..: entry j comes from new place rows[cu_q[s] + j] to new place j + 1.  An entry that is not in j + 1 .. m - 1, or has no page, stays where it is.  k_len is left
+ * alone: the sequence then has k_len[s] - m + 1 + n_kept[s] places.  rows and n_kept are verify_drafts's out_rows and n_accepted.  Errors also: 2^24 sequences times key heads. */
+int agzo_glue_cache_keep(agzo_ctx* ctx, const agzo_paged_cache* cache, const int32_t* cu_q, int64_t n, const int32_t* rows, const int32_t* n_kept);
+
+/* verify_drafts: which drafted tokens the target accepts, and the token behind them.  Sequence s has the rows cu[s] .. cu[s + 1] - 1: row 0 is the token that is there already, the rows behind it
+ * are drafted tokens; parents (device int32 [n], NULL: a chain): the row, counted in its sequence, that a row's token follows, in front of it (else the row is not looked at); row 0's is not read.
+ * p [n][vocab]: the target's probabilities behind each row (dtype AGZO_F32 or AGZO_BF16, rows ldp apart); q (nullable, chains only; likewise): the probabilities that each row's token was
+ * drawn from by the draft, row 0's are not read; NULL: tokens are proposed for certain.  uniforms (device fp32 [n]): random numbers of [0, 1), row 0's for the last draw.
+ * From row 0 on, the rows that follow the row reached are tried in order.  Row i's token x is accepted, and its row reached, if p(x) > 0, behind the row that it follows, and
+ *     u_i q_i(x) < p(x),   without q:  u_i (1 - sum of p over the tokens refused here before) < p(x)   (a token refused here before has p(x) = 0).
+ * The token that follows is the first x with  sum_{y <= x} w(y) > u_0 sum_y w(y),  w = max(p - q_i, 0) where row i was refused last, without q p but 0 for the tokens refused here; the last one with
+ * w > 0 if there is no such, w = p if no w is positive, -1 if no p is.  Negative probabilities and NaN count as 0, and so does a token outside the vocabulary.
+ *   out_tokens, out_rows [n]: a sequence's accepted tokens and their rows, then (out_tokens) the token that follows, then -1;  n_accepted [n_seq]: how many (device int32).
+ * Products, differences and sums are fp64.  Rows of no sequence are neither read nor written.  Device, workspace and captures as for the calls on packed batches.
+ * Errors: AGZO_EINVAL for NULL or misaligned tensors, q with parents, leading dimensions below vocab, more than 65535 sequences, 2^26 rows or 2^24 probabilities a row, overlapping outputs. */
+int agzo_verify_drafts(agzo_ctx* ctx, int32_t dtype, const void* p, int64_t ldp, const void* q, int64_t ldq, const int32_t* tokens, const int32_t* parents, const float* uniforms,
+                       const int32_t* cu, int64_t n, int32_t n_seq, int64_t vocab, int32_t* out_tokens, int32_t* out_rows, int32_t* n_accepted);
+
 /* Token cross-entropy of a layer's outputs and its gradient (an LM head: d_out outputs; the layer's r, y_dtype and ldy are not used).  The logits of bf16
  * layers are never stored whole; the forward call of an fp32 layer keeps n_tokens d_out fp32 of them in the workspace.
  * loss: kind AGZO_LOSS_CE, target ids [n_tokens]; rows whose id is not in [0, d_out) are not counted.

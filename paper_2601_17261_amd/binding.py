@@ -18,6 +18,7 @@ LOSS_NONE, LOSS_MSE, LOSS_CE = 0, 1, 2
 SKETCH_NONE, SKETCH_RANGE, SKETCH_POWER, SKETCH_RANGE_FUSED = 0, 1, 2, 3
 TAG_G, TAG_OMEGA, TAG_Q0, TAG_DENSE = 0, 1, 2, 3
 ONE_SIDED, NAIVE_INPLACE, INIT_FEATURE, SHARED_FORWARD = 1, 2, 4, 8
+ROPE_PLAIN, ROPE_LINEAR, ROPE_TURNS, ROPE_DIMS = 0, 1, 2, 3
 OK, EINVAL, ENOMEM, ENUMERIC, EHIP = 0, -1, -2, -3, -4
 
 TILING_AUTO, TILING_LARGE = 0, 1
@@ -30,6 +31,7 @@ EXPORTS = ["agzo_create", "agzo_destroy", "agzo_last_error", "agzo_check", "agzo
            "agzo_update_many", "agzo_step", "agzo_step_no_update", "agzo_basis_many", "agzo_step_many",
            "agzo_glue_rmsnorm", "agzo_glue_swiglu", "agzo_glue_add", "agzo_glue_attention",
            "agzo_glue_qk_norm_rope", "agzo_glue_qk_norm_rope_backward", "agzo_glue_attention_packed", "agzo_glue_attention_packed_backward",
+           "agzo_glue_rope", "agzo_glue_rope_backward", "agzo_glue_cache_append", "agzo_glue_attention_paged", "agzo_glue_cache_keep", "agzo_verify_drafts",
            "agzo_ce_forward", "agzo_ce_backward"]
 
 
@@ -68,6 +70,18 @@ class AgzoPackedAttention(ctypes.Structure):
                 ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p), ("k_len", ctypes.c_void_p), ("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64),
                 ("n_seq", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("causal", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class AgzoPagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_page", ctypes.c_int64), ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("v_page", ctypes.c_int64), ("v_row", ctypes.c_int64), ("v_head", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("k_len", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_seq", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class AgzoRope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("theta", ctypes.c_float), ("scaling", ctypes.c_int32), ("factor", ctypes.c_float),
+                ("low", ctypes.c_float), ("high", ctypes.c_float), ("original", ctypes.c_float), ("magnitude", ctypes.c_float)]
 
 
 class AgzoError(RuntimeError):
@@ -123,6 +137,13 @@ def load():
     lib.agzo_glue_qk_norm_rope_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, f32, f32]
     lib.agzo_glue_attention_packed.argtypes = [vp, pp, vp, i64, vp]
     lib.agzo_glue_attention_packed_backward.argtypes = [vp, pp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64]
+    rp, cp = ctypes.POINTER(AgzoRope), ctypes.POINTER(AgzoPagedCache)
+    lib.agzo_glue_rope.argtypes = [vp, rp, i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32]
+    lib.agzo_glue_rope_backward.argtypes = [vp, rp, i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32]
+    lib.agzo_glue_cache_append.argtypes = [vp, cp, rp, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i64, i32, vp, vp, f32]
+    lib.agzo_glue_attention_paged.argtypes = [vp, cp, vp, i64, vp, i64, i32, f32, vp, i64, i32, vp, i64, vp]
+    lib.agzo_glue_cache_keep.argtypes = [vp, cp, vp, i64, vp, vp]
+    lib.agzo_verify_drafts.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, i64, vp, vp, vp]
     lib.agzo_ce_forward.argtypes = [vp, lp, vp, vp, sp, vp, vp]
     lib.agzo_ce_backward.argtypes = [vp, lp, vp, vp, sp, vp, vp, vp, i64, vp, i64]
     lib.agzo_step.argtypes = [vp, lp, vp, vp, sp, i32, f32, f32, u64, i32, vp]
@@ -221,6 +242,36 @@ def make_loss(target=None, kind=LOSS_MSE):
         s.target_dtype = _dt(target)
         s.ldt = target.stride(0)
     return s
+
+
+def make_rope(rot_dim, theta=1.0e6, interleaved=False, scaling=ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, original=0.0, magnitude=1.0):
+    """How queries and keys are turned by their positions: the first rot_dim values of a head, in pairs half of these apart or side by side (interleaved).  scaling:
+    ROPE_LINEAR (factor), ROPE_TURNS and ROPE_DIMS (factor, low, high, original)."""
+    return AgzoRope(rot_dim, interleaved, theta, scaling, factor, low, high, original, magnitude)
+
+
+def make_cache(k, v, table, k_len):
+    """A cache in pages.  k, v: bf16 [n_pages][page_size][key heads][head_dim] of any strides, unit along the last axis; table: int32 [n_seq][pages a sequence may have], ids
+    of pages; k_len: int32 [n_seq], keys that each sequence has, the new tokens of a call among them.  The tensors stay the caller's, and what they hold may change
+    between calls."""
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        raise TypeError("k and v must be torch.bfloat16, not %s and %s" % (k.dtype, v.dtype))
+    shape, ks, vs = k.shape, k.stride(), v.stride()
+    if len(shape) != 4 or v.shape != shape or ((ks[3] != 1 or vs[3] != 1) and shape[3] > 1):
+        raise ValueError("k and v must be [n_pages][page_size][key heads][head_dim] alike, with unit stride along the last axis")
+    if table.dtype is not torch.int32 or k_len.dtype is not torch.int32:
+        raise TypeError("table and k_len must be torch.int32")
+    if table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1) or k_len.shape != (table.shape[0],) or not k_len.is_contiguous():
+        raise ValueError("table must be [n_seq][pages], with unit stride along the last axis, and k_len contiguous, of n_seq")
+    device = k.get_device()
+    if v.get_device() != device or table.get_device() != device or k_len.get_device() != device:
+        raise ValueError("k, v, table and k_len must be on one device")
+    n_seq, pages = table.shape
+    c = AgzoPagedCache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], table.data_ptr(), table.stride(0) if n_seq > 1 else pages, k_len.data_ptr(),
+                       shape[1], pages, n_seq, shape[2], shape[3])
+    c._held = (k, v, table, k_len)      # (as long as the addresses are in use)
+    c._device = device
+    return c
 
 
 class Context:
@@ -475,6 +526,82 @@ class Context:
         self._rc(self.lib.agzo_glue_attention_packed_backward(
             self.h, ctypes.byref(a), *_rows(out, "out", nq, wq, at), _flat(lse, "lse", torch.float32, nq * (wq // head_dim), at), *_rows(dout, "dout", nq, wq, at),
             *_rows(dq, "dq", nq, wq, at), *_rows(dk, "dk", nk, wk, at), *_rows(dv, "dv", nk, wk, at)))
+
+    def glue_rope(self, rope, q, k, positions, q_out, k_out, head_dim=128):
+        """rope: make_rope(); q [n][heads * head_dim], k [n][key heads * head_dim] of bf16 or float32 -> q_out, k_out; either side may be None with its result."""
+        self._rope(self.lib.agzo_glue_rope, rope, q, k, positions, q_out, k_out, head_dim)
+
+    def glue_rope_backward(self, rope, dq_out, dk_out, positions, dq, dk, head_dim=128):
+        """The gradients with respect to glue_rope's results -> those with respect to its inputs."""
+        self._rope(self.lib.agzo_glue_rope_backward, rope, dq_out, dk_out, positions, dq, dk, head_dim)
+
+    def _rope(self, call, rope, q, k, positions, q_out, k_out, head_dim):
+        if q is None and k is None:
+            raise ValueError("neither q nor k is given")
+        at, dtype = self.device, (k if q is None else q).dtype
+        pq, lq, nq, wq = (None, 0, k.shape[0], 0) if q is None else _matrix(q, "q", at, dtype)
+        pk, lk, n, wk = (None, 0, nq, 0) if k is None else _matrix(k, "k", at, dtype)
+        if nq != n or wq % head_dim or wk % head_dim:
+            raise ValueError("%d rows of %d values, %d of %d: need as many rows, of multiples of %d" % (nq, wq, n, wk, head_dim))
+        oq, loq = _rows(q_out, "q_out", n, wq, at, dtype)
+        ok, lok = _rows(k_out, "k_out", n, wk, at, dtype)
+        self._rc(call(self.h, ctypes.byref(rope), _dt(k if q is None else q), pq, lq, pk, lk, _flat(positions, "positions", torch.int32, n, at), oq, loq, ok, lok, n, wq // head_dim,
+                      wk // head_dim, head_dim))
+
+    def _cache(self, cache, cu_q):
+        if cache._device != self.device:
+            raise ValueError("a cache on device %d, and the context is of %s" % (cache._device, self.stream.device))
+        return ctypes.byref(cache), _flat(cu_q, "cu_q", torch.int32, cache.n_seq + 1, self.device)
+
+    def glue_cache_append(self, cache, rope, q, k, v, q_out, cu_q, positions=None, q_gain=None, k_gain=None, eps=None):
+        """k, v [n][key heads * head_dim] to their places in the cache (make_cache()), q [n][heads * head_dim] -> q_out (both may be None); rope: make_rope() or None; cu_q: int32 offsets of
+        the sequences' new tokens; positions: int32 [n] or None (the places); eps: norms of q and k come first (gains: float32 [head_dim] or None), or None: no norms."""
+        at, d, f32 = self.device, cache.head_dim, torch.float32
+        c, cu = self._cache(cache, cu_q)
+        pk, lk, n, wk = _matrix(k, "k", at)
+        pv, lv = _rows(v, "v", n, wk, at)
+        pq, lq, nq, wq = (None, 0, n, 0) if q is None else _matrix(q, "q", at)
+        if nq != n or wq % d or wk != cache.n_kv_heads * d:
+            raise ValueError("%d rows of %d values, %d of %d: need as many rows, of multiples of %d and of %d" % (nq, wq, n, wk, d, cache.n_kv_heads * d))
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        oq, loq = _rows(q_out, "q_out", n, wq, at)
+        self._rc(self.lib.agzo_glue_cache_append(self.h, c, None if rope is None else ctypes.byref(rope), pq, lq, pk, lk, pv, lv, cu, n, wq // d, _flat(positions, "positions", torch.int32, n, at),
+                                                 oq, loq, eps is not None, _flat(q_gain, "q_gain", f32, d, at), _flat(k_gain, "k_gain", f32, d, at), 0.0 if eps is None else eps))
+
+    def glue_attention_paged(self, cache, q, out, cu_q, scale=None, tree=None, lse=None):
+        """q [n][heads * head_dim] -> out like q, over the cache (make_cache()); cu_q: int32 offsets of the sequences' new tokens, their last places; scale None: head_dim ** -0.5; tree: int32
+        [n][words], for each new token a bit for each one of its sequence that it sees, or None: those up to itself; lse: float32 [n][heads] or None."""
+        at, d = self.device, cache.head_dim
+        c, cu = self._cache(cache, cu_q)
+        pq, lq, n, wq = _matrix(q, "q", at)
+        if wq % d:
+            raise ValueError("rows of %d values: need multiples of %d" % (wq, d))
+        o, ldo = _rows(out, "out", n, wq, at)
+        pt, lt, nt, words = (None, 0, n, 0) if tree is None else _matrix(tree, "tree", at, torch.int32)
+        if nt != n:
+            raise ValueError("a tree of %d rows for %d tokens" % (nt, n))
+        if tree is not None and words == 0:
+            pt = cu      # (an empty tensor has no address, and none would be no tree)
+        self._rc(self.lib.agzo_glue_attention_paged(self.h, c, pq, lq, cu, n, wq // d, d ** -0.5 if scale is None else scale, pt, lt, words, o, ldo,
+                                                    _flat(lse, "lse", torch.float32, n * (wq // d), at)))
+
+    def glue_cache_keep(self, cache, cu_q, rows, n_kept):
+        """Accepted tokens of trees together in the cache: rows, n_kept are out_rows, n_accepted of verify_drafts."""
+        c, cu = self._cache(cache, cu_q)
+        n = rows.numel()
+        self._rc(self.lib.agzo_glue_cache_keep(self.h, c, cu, n, _flat(rows, "rows", torch.int32, n, self.device), _flat(n_kept, "n_kept", torch.int32, cache.n_seq, self.device)))
+
+    def verify_drafts(self, p, q, tokens, uniforms, cu, out_tokens, out_rows, n_accepted, parents=None):
+        """p [n][vocab]: the target's probabilities behind each row (bf16 or float32); q: like p, what each row's token was drawn from, or None (proposed for certain); tokens, parents (None:
+        chains), out_tokens, out_rows: int32 [n]; uniforms: float32 [n]; cu: int32 offsets of the sequences' rows; n_accepted: int32 [n_seq]."""
+        at, i32, dtype = self.device, torch.int32, p.dtype
+        pp, lp, n, vocab = _matrix(p, "p", at, dtype)
+        pq, lq = _rows(q, "q", n, vocab, at, dtype)
+        n_seq = cu.numel() - 1
+        self._rc(self.lib.agzo_verify_drafts(self.h, _dt(p), pp, lp, pq, lq, _flat(tokens, "tokens", i32, n, at), _flat(parents, "parents", i32, n, at),
+                                             _flat(uniforms, "uniforms", torch.float32, n, at), _flat(cu, "cu", i32, n_seq + 1, at), n, n_seq, vocab,
+                                             _flat(out_tokens, "out_tokens", i32, n, at), _flat(out_rows, "out_rows", i32, n, at), _flat(n_accepted, "n_accepted", i32, n_seq, at)))
 
     def step_no_update(self, L, W, X, loss, K, eps, seed, flags, out_dev, B_out):
         self._rc(self.lib.agzo_step_no_update(self.h, ctypes.byref(L), _ptr(W), _ptr(X), ctypes.byref(loss), K, eps,

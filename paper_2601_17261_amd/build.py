@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libagzo.so")
 SOURCES = ["philox.hip", "gemm_f32.hip", "gemm_bf16.hip", "gemm_bf16_aligned.hip", "gemm_bf16_small.hip", "gemm_bf16_mid.hip", "gemm_bf16_few.hip",
-           "skinny.hip", "qr.hip", "update.hip", "loss.hip", "ce_grad.hip", "ce_grad_f32.hip", "ce_few.hip", "glue.hip", "glue_norm_rope.hip", "glue_packed.hip", "probe.hip", "agzo_api.hip"]
+           "skinny.hip", "qr.hip", "update.hip", "loss.hip", "ce_grad.hip", "ce_grad_f32.hip", "ce_few.hip", "glue.hip", "glue_norm_rope.hip", "glue_packed.hip", "glue_cache.hip", "glue_paged.hip", "verify.hip", "probe.hip", "agzo_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 VALU forms are switched off for every device compile (some forms have misbehaved
 # on the test machines); the host pass does not know the feature and says so, harmlessly.
@@ -22,7 +22,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wno-unused-com
 def _compile(src, force):
     obj = os.path.join(OBJ, src.replace(".hip", ".o"))
     srcp = os.path.join(CSRC, src)
-    deps = [srcp, os.path.join(CSRC, "agzo_internal.h"), os.path.join(CSRC, "gemm_bf16_common.h"), os.path.join(CSRC, "ext_prep.h"), os.path.join(CSRC, "fork.h"), os.path.join(CSRC, "overlap.h"), os.path.join(CSRC, "grow.h"), os.path.join(CSRC, "slots.h"),
+    deps = [srcp, os.path.join(CSRC, "agzo_internal.h"), os.path.join(CSRC, "gemm_bf16_common.h"), os.path.join(CSRC, "ext_prep.h"), os.path.join(CSRC, "fork.h"), os.path.join(CSRC, "overlap.h"), os.path.join(CSRC, "grow.h"), os.path.join(CSRC, "slots.h"), os.path.join(CSRC, "packed_tiles.h"), os.path.join(CSRC, "paged.h"),
             os.path.join(ROOT, "include", "agzo.h")]
     if not force and os.path.exists(obj) and all(os.path.getmtime(obj) > os.path.getmtime(d) for d in deps):
         return obj, ""

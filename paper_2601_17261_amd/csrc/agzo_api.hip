@@ -1,6 +1,7 @@
 // C ABI of libagzo: argument checks, workspace carving and the stream-ordered sequence of kernel
 // launches that makes up one AGZO step (Alg. 2) for a linear layer.  No arithmetic lives here.
 #include <stdarg.h>
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -1578,6 +1579,222 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
     const PackedGrad g{static_cast<const bf16_t*>(out), static_cast<const bf16_t*>(dout), ldo, lddo, lse, static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk),
                        static_cast<bf16_t*>(dv), lddq, lddk, lddv};
     HIPCHK(launch_packed_backward(p, a->head_dim, g, ctx->ws, ctx->stream));
+    return AGZO_OK;
+}
+
+// ---- a cache in pages ------------------------------------------------------------------------------------------------
+namespace {
+// How one of a cache's tensors lies in memory: its axes of more than one index from the closest on, and what each covers (in values).  extent[0]: a head's values
+struct CacheLayout { int64_t stride[3], size[3], extent[4]; int axes; };
+
+int check_cache_tensor(agzo_ctx* ctx, const agzo_paged_cache* c, const char* name, const void* at, int64_t page, int64_t row, int64_t head, CacheLayout& out) {
+    if ((!at && c->n_pages > 0) || (reinterpret_cast<uintptr_t>(at) & 15)) return fail(ctx, AGZO_EINVAL, "the cache's %s is NULL or misaligned", name);
+    if (c->page_size > 1 && row >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "rows of the cache's %s must be less than 2^22 values apart", name);
+    out = CacheLayout{};
+    out.extent[0] = c->head_dim;
+    const int64_t axes[3][2] = {{page, c->n_pages}, {row, c->page_size}, {head, c->n_kv_heads}};
+    for (const auto& x : axes) {
+        if (x[1] <= 1) continue;
+        if (x[0] % 8 || x[0] < c->head_dim || x[0] >= (1LL << 40)) return fail(ctx, AGZO_EINVAL, "a stride of %lld in the cache's %s", (long long)x[0], name);
+        int i = out.axes++;
+        for (; i > 0 && out.stride[i - 1] > x[0]; --i) { out.stride[i] = out.stride[i - 1]; out.size[i] = out.size[i - 1]; }
+        out.stride[i] = x[0];
+        out.size[i] = x[1];
+    }
+    for (int i = 0; i < out.axes; ++i) {
+        if (out.stride[i] < out.extent[i]) return fail(ctx, AGZO_EINVAL, "rows or pages of the cache's %s overlap each other", name);
+        const __int128 more = (__int128)(out.size[i] - 1) * out.stride[i] + out.extent[i];
+        if (more >= (__int128)1 << 60) return fail(ctx, AGZO_EINVAL, "the cache's %s is too large", name);
+        out.extent[i + 1] = (int64_t)more;
+    }
+    return 0;
+}
+
+Named cache_range(const char* name, const void* at, const CacheLayout& l, int64_t n_pages) {
+    const int64_t all = l.extent[l.axes];
+    return named(name, n_pages > 0 ? at : nullptr, all, 1, all);
+}
+
+// whether keys and values share no memory: apart as a whole, or one in the gaps that the other leaves at some level
+bool caches_apart(const agzo_paged_cache* c, const CacheLayout& k, const CacheLayout& v) {
+    if (!rows_overlap(cache_range("", c->k, k, c->n_pages).rows, cache_range("", c->v, v, c->n_pages).rows)) return true;
+    if (k.axes != v.axes) return false;
+    for (int i = 0; i < k.axes; ++i)
+        if (k.stride[i] != v.stride[i] || k.size[i] != v.size[i]) return false;
+    const int64_t d = static_cast<const char*>(c->v) - static_cast<const char*>(c->k), between = (d < 0 ? -d : d) / 2;
+    for (int i = 0; i < k.axes; ++i)
+        if (k.extent[i] <= between && between + k.extent[i] <= k.stride[i]) return true;
+    return false;
+}
+
+// kr, vr: where its tensors lie.  written: by the call
+int check_cache(agzo_ctx* ctx, const agzo_paged_cache* c, int64_t n, const int32_t* cu_q, bool written, PagedCache& out, Named& kr, Named& vr) {
+    if (!ctx) return AGZO_EINVAL;
+    if (!c) return fail(ctx, AGZO_EINVAL, "the cache's descriptor is NULL");
+    if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || (c->head_dim != 64 && c->head_dim != 128) || c->n_seq < 0 || c->n_seq > 65536 || c->n_pages < 0 || c->n_pages > 0x7FFFFFFFLL ||
+        c->page_size < 1 || c->max_pages < 0)
+        return fail(ctx, AGZO_EINVAL, "bad cache: %lld pages of %d tokens, %d key heads of %d values, %d sequences of up to %d pages", (long long)c->n_pages, c->page_size, c->n_kv_heads,
+                    c->head_dim, c->n_seq, c->max_pages);
+    constexpr int64_t most = 0x7FFFFFFFLL - 1024;
+    if ((int64_t)c->max_pages * c->page_size > most) return fail(ctx, AGZO_EINVAL, "%d pages of %d tokens for a sequence: too many", c->max_pages, c->page_size);
+    if (c->n_seq > 0 && c->max_pages > 0 && (c->n_pages < 1 || !c->table || c->ld_table < c->max_pages)) return fail(ctx, AGZO_EINVAL, "no pages, or the table is NULL or has rows of fewer than %d", c->max_pages);
+    if (c->n_seq > 0 && (!c->k_len || !cu_q)) return fail(ctx, AGZO_EINVAL, "k_len or cu_q is NULL");
+    if ((reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->k_len) | reinterpret_cast<uintptr_t>(cu_q)) & 3)
+        return fail(ctx, AGZO_EINVAL, "the table, k_len or cu_q is misaligned");
+    if (n < 0 || n > (1LL << 26)) return fail(ctx, AGZO_EINVAL, "%lld new tokens", (long long)n);
+    CacheLayout k, v;
+    TRY(check_cache_tensor(ctx, c, "k", c->k, c->k_page, c->k_row, c->k_head, k));
+    TRY(check_cache_tensor(ctx, c, "v", c->v, c->v_page, c->v_row, c->v_head, v));
+    if (written && !caches_apart(c, k, v)) return fail(ctx, AGZO_EINVAL, "the cache's k and v overlap");
+    kr = cache_range("the cache's k", c->k, k, c->n_pages);
+    vr = cache_range("the cache's v", c->v, v, c->n_pages);
+    out = PagedCache{static_cast<bf16_t*>(c->k), static_cast<bf16_t*>(c->v), c->k_page, c->k_row, c->k_head, c->v_page, c->v_row, c->v_head, c->n_pages, c->table, c->ld_table, c->k_len,
+                     c->page_size, c->max_pages, c->n_seq, c->n_kv_heads};
+    return check_device(ctx);
+}
+Named table_of(const agzo_paged_cache* c) { return named("the table", c->max_pages ? c->table : nullptr, c->ld_table, c->n_seq, c->max_pages, 4); }
+
+int rope_args(agzo_ctx* ctx, const agzo_rope* r, int32_t head_dim, RopeArgs& out) {
+    if (!r) return fail(ctx, AGZO_EINVAL, "the rotation's descriptor is NULL");
+    if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > head_dim) return fail(ctx, AGZO_EINVAL, "%d of a head's %d values to rotate: need a multiple of 16", r->rot_dim, head_dim);
+    if (!(r->theta > 1.f) || !(r->theta < INFINITY)) return fail(ctx, AGZO_EINVAL, "theta must be finite and exceed 1");
+    if (!(r->magnitude > -INFINITY) || !(r->magnitude < INFINITY)) return fail(ctx, AGZO_EINVAL, "the magnitude must be finite");
+    out = RopeArgs{r->rot_dim, r->interleaved != 0, 0, r->magnitude, log2((double)r->theta), 1.0, 0.0, 1.0};
+    if (r->scaling == AGZO_ROPE_PLAIN) return 0;
+    if (!(r->factor > 0.f) || !(r->factor < INFINITY)) return fail(ctx, AGZO_EINVAL, "the factor must be finite and positive");
+    out.inv_factor = 1.0 / r->factor;
+    out.keep_from = 0.0;
+    if (r->scaling == AGZO_ROPE_LINEAR) return 0;
+    if (r->scaling != AGZO_ROPE_TURNS && r->scaling != AGZO_ROPE_DIMS) return fail(ctx, AGZO_EINVAL, "scaling %d", r->scaling);
+    if (!(r->original > 0.f) || !(r->original < INFINITY) || !(r->low > 0.f) || !(r->high > r->low) || !(r->high < INFINITY))
+        return fail(ctx, AGZO_EINVAL, "original, low and high must be finite and positive, and high exceed low");
+    constexpr double circle = 6.283185307179586477;
+    if (r->scaling == AGZO_ROPE_TURNS) {
+        out.by_turns = 1;
+        out.keep_by = r->original / circle / ((double)r->high - r->low);
+        out.keep_from = -(double)r->low / ((double)r->high - r->low);
+        return 0;
+    }
+    auto pair_of = [&](double turns) { return r->rot_dim * log(r->original / (circle * turns)) / (2.0 * log((double)r->theta)); };
+    const double first = std::max(floor(pair_of(r->high)), 0.0), last = std::min(ceil(pair_of(r->low)), r->rot_dim - 1.0), wide = std::max(last - first, 0.001);
+    out.keep_by = -1.0 / wide;
+    out.keep_from = 1.0 + first / wide;
+    return 0;
+}
+
+int rope_call(agzo_ctx* ctx, const agzo_rope* r, int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out, int64_t ldqo, void* k_out,
+              int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, bool back) {
+    if (!ctx) return AGZO_EINVAL;
+    if (n_heads < 0 || n_kv_heads < 0 || n_heads > 65535 || n_kv_heads > 65535 || head_dim < 16 || head_dim % 16 || head_dim > 256)
+        return fail(ctx, AGZO_EINVAL, "%d heads, %d key heads of %d values", n_heads, n_kv_heads, head_dim);
+    if (dtype != AGZO_F32 && dtype != AGZO_BF16) return fail(ctx, AGZO_EINVAL, "dtype %d", dtype);
+    RopeArgs args;
+    TRY(rope_args(ctx, r, head_dim, args));
+    if (n < 0 || n > 0x7FFFFFFFLL) return fail(ctx, AGZO_EINVAL, "%lld tokens", (long long)n);
+    if ((n > 0 && !positions) || (reinterpret_cast<uintptr_t>(positions) & 3)) return fail(ctx, AGZO_EINVAL, "positions is NULL or misaligned");
+    const int64_t wq = (int64_t)n_heads * head_dim, wk = (int64_t)n_kv_heads * head_dim, size = dtype == AGZO_F32 ? 4 : 2;
+    TRY(check_glue(ctx, n, wq, {q, q_out}, {ldq, ldqo}));
+    TRY(check_glue(ctx, n, wk, {k, k_out}, {ldk, ldko}));
+    TRY(check_apart(ctx, {named("q_out", q_out, ldqo, n, wq, size), named("k_out", k_out, ldko, n, wk, size)},
+                    {named("q", q, ldq, n, wq, size), named("k", k, ldk, n, wk, size), listed("positions", positions, n)}, {{0, 0}, {1, 1}}));
+    TRY(check_device(ctx));
+    HIPCHK(launch_rope(args, dtype == AGZO_F32, RopeTensor{q, ldq, q_out, ldqo, n_heads}, RopeTensor{k, ldk, k_out, ldko, n_kv_heads}, positions, n, head_dim, back, ctx->stream));
+    return AGZO_OK;
+}
+}  // namespace
+
+int agzo_glue_rope(agzo_ctx* ctx, const agzo_rope* rope, int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const int32_t* positions, void* q_out, int64_t ldqo,
+                   void* k_out, int64_t ldko, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+    return rope_call(ctx, rope, dtype, q, ldq, k, ldk, positions, q_out, ldqo, k_out, ldko, n, n_heads, n_kv_heads, head_dim, false);
+}
+int agzo_glue_rope_backward(agzo_ctx* ctx, const agzo_rope* rope, int32_t dtype, const void* dq_out, int64_t lddqo, const void* dk_out, int64_t lddko, const int32_t* positions, void* dq,
+                            int64_t lddq, void* dk, int64_t lddk, int64_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+    return rope_call(ctx, rope, dtype, dq_out, lddqo, dk_out, lddko, positions, dq, lddq, dk, lddk, n, n_heads, n_kv_heads, head_dim, true);
+}
+
+int agzo_glue_cache_append(agzo_ctx* ctx, const agzo_paged_cache* cache, const agzo_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           const int32_t* cu_q, int64_t n, int32_t n_heads, const int32_t* positions, void* q_out, int64_t ldqo, int32_t norm, const float* q_gain, const float* k_gain,
+                           float eps) {
+    PagedCache c;
+    Named kr, vr;
+    TRY(check_cache(ctx, cache, n, cu_q, true, c, kr, vr));
+    if (n_heads < 0 || n_heads > 65535) return fail(ctx, AGZO_EINVAL, "%d heads", n_heads);
+    const int64_t wq = (int64_t)n_heads * cache->head_dim, wk = (int64_t)cache->n_kv_heads * cache->head_dim;
+    TRY(check_glue(ctx, n, wq, {q, q_out}, {ldq, ldqo}));
+    TRY(check_glue(ctx, n, wk, {k, v}, {ldk, ldv}));
+    if ((reinterpret_cast<uintptr_t>(positions) | reinterpret_cast<uintptr_t>(q_gain) | reinterpret_cast<uintptr_t>(k_gain)) & 3) return fail(ctx, AGZO_EINVAL, "positions or a gain is misaligned");
+    if (norm ? !(eps >= 0.f) || !(eps < INFINITY) : q_gain || k_gain) return fail(ctx, AGZO_EINVAL, "eps must be finite and not negative, and gains are for norms");
+    RopeArgs r{};
+    if (rope) TRY(rope_args(ctx, rope, cache->head_dim, r));
+    const int64_t d = norm ? cache->head_dim : 0;
+    TRY(check_apart(ctx, {named("q_out", q_out, ldqo, n, wq)},
+                    {named("q", q, ldq, n, wq), kr, vr, named("k", k, ldk, n, wk), named("v", v, ldv, n, wk), listed("cu_q", cu_q, c.n_seq + 1LL), listed("positions", positions, n),
+                     listed("q_gain", q_gain, d), listed("k_gain", k_gain, d), table_of(cache), listed("k_len", c.k_len, c.n_seq)}, {{0, 0}}));
+    // (k and v of the cache have been held against each other)
+    for (const Named& of : {kr, vr})
+        TRY(check_apart(ctx, {of}, {named("q", q, ldq, n, wq), named("k", k, ldk, n, wk), named("v", v, ldv, n, wk), listed("cu_q", cu_q, c.n_seq + 1LL), listed("positions", positions, n),
+                                    listed("q_gain", q_gain, d), listed("k_gain", k_gain, d), table_of(cache), listed("k_len", c.k_len, c.n_seq)}));
+    HIPCHK(launch_cache_append(c, cache->head_dim, r, CacheAppend{static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v), ldq, ldk, ldv,
+                               static_cast<bf16_t*>(q_out), ldqo, cu_q, positions, n, n_heads, q_gain, k_gain, norm != 0, eps}, ctx->stream));
+    return AGZO_OK;
+}
+
+int agzo_glue_cache_keep(agzo_ctx* ctx, const agzo_paged_cache* cache, const int32_t* cu_q, int64_t n, const int32_t* rows, const int32_t* n_kept) {
+    PagedCache c;
+    Named kr, vr;
+    TRY(check_cache(ctx, cache, n, cu_q, true, c, kr, vr));
+    if ((n > 0 && (!rows || (c.n_seq > 0 && !n_kept))) || ((reinterpret_cast<uintptr_t>(rows) | reinterpret_cast<uintptr_t>(n_kept)) & 3)) return fail(ctx, AGZO_EINVAL, "rows or n_kept is NULL or misaligned");
+    if ((int64_t)c.n_seq * c.n_kv >= (1LL << 24)) return fail(ctx, AGZO_EINVAL, "%d sequences of %d key heads: too many", c.n_seq, c.n_kv);
+    for (const Named& of : {kr, vr})
+        TRY(check_apart(ctx, {of}, {listed("cu_q", cu_q, c.n_seq + 1LL), listed("rows", rows, n), listed("n_kept", n_kept, c.n_seq), table_of(cache), listed("k_len", c.k_len, c.n_seq)}));
+    HIPCHK(launch_cache_keep(c, cache->head_dim, cu_q, n, rows, n_kept, ctx->stream));
+    return AGZO_OK;
+}
+
+int agzo_glue_attention_paged(agzo_ctx* ctx, const agzo_paged_cache* cache, const void* q, int64_t ldq, const int32_t* cu_q, int64_t n, int32_t n_heads, float scale, const int32_t* tree,
+                              int64_t ld_tree, int32_t tree_words, void* out, int64_t ldo, float* lse) {
+    PagedCache c;
+    Named kr, vr;
+    TRY(check_cache(ctx, cache, n, cu_q, false, c, kr, vr));
+    if (n_heads < 1 || n_heads > 65535 || n_heads % c.n_kv) return fail(ctx, AGZO_EINVAL, "%d heads on %d key heads", n_heads, c.n_kv);
+    constexpr int64_t most = 0x7FFFFFFFLL - 1024;
+    if (n * (n_heads / c.n_kv) > most) return fail(ctx, AGZO_EINVAL, "%lld new tokens of %d heads: too many", (long long)n, n_heads);
+    if (!(scale >= 0x1p-100f) || !(scale < INFINITY)) return fail(ctx, AGZO_EINVAL, "scale must be finite and 2^-100 at least");
+    if (ldq >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "leading dimensions must be below 2^22");
+    const int64_t wq = (int64_t)n_heads * cache->head_dim;
+    TRY(check_glue(ctx, n, wq, {q, out}, {ldq, ldo}));
+    if (tree && (tree_words < 0 || ld_tree < tree_words || (reinterpret_cast<uintptr_t>(tree) & 3))) return fail(ctx, AGZO_EINVAL, "a tree of %d words in rows of %lld, or misaligned", tree_words, (long long)ld_tree);
+    if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(ctx, AGZO_EINVAL, "lse is misaligned");
+    TRY(check_apart(ctx, {named("out", out, ldo, n, wq), listed("lse", lse, n * n_heads)},
+                    {named("q", q, ldq, n, wq), kr, vr, listed("cu_q", cu_q, c.n_seq + 1LL), table_of(cache), listed("k_len", c.k_len, c.n_seq),
+                     named("the tree", tree_words > 0 ? tree : nullptr, ld_tree, n, tree_words, 4)}));
+    const PagedAttention a{static_cast<const bf16_t*>(q), ldq, cu_q, n, n_heads, scale, reinterpret_cast<const uint32_t*>(tree), ld_tree, tree_words, static_cast<bf16_t*>(out), ldo, lse};
+    if (paged_units(c, a) >= kPackedUnits) return fail(ctx, AGZO_EINVAL, "%d sequences of %d key heads, %lld new tokens: too many tiles", c.n_seq, c.n_kv, (long long)n);
+    TRY(reserve(ctx, paged_workspace_bytes(c, a, cache->head_dim)));
+    HIPCHK(launch_paged_attention(c, a, cache->head_dim, ctx->ws, ctx->stream));
+    return AGZO_OK;
+}
+
+int agzo_verify_drafts(agzo_ctx* ctx, int32_t dtype, const void* p, int64_t ldp, const void* q, int64_t ldq, const int32_t* tokens, const int32_t* parents, const float* uniforms,
+                       const int32_t* cu, int64_t n, int32_t n_seq, int64_t vocab, int32_t* out_tokens, int32_t* out_rows, int32_t* n_accepted) {
+    if (!ctx) return AGZO_EINVAL;
+    if (dtype != AGZO_F32 && dtype != AGZO_BF16) return fail(ctx, AGZO_EINVAL, "dtype %d", dtype);
+    if (n_seq < 0 || n_seq > 65535 || n < 0 || n > (1LL << 26) || vocab < 1 || vocab > (1LL << 24)) return fail(ctx, AGZO_EINVAL, "%d sequences, %lld rows of %lld probabilities", n_seq, (long long)n, (long long)vocab);
+    if (q && parents) return fail(ctx, AGZO_EINVAL, "the draft's probabilities are for chains, a tree's tokens are proposed for certain");
+    const int64_t size = dtype == AGZO_F32 ? 4 : 2;
+    if (n > 0 && (!p || !tokens || !uniforms || !out_tokens || !out_rows)) return fail(ctx, AGZO_EINVAL, "p, tokens, uniforms, out_tokens or out_rows is NULL");
+    if (n_seq > 0 && (!cu || !n_accepted)) return fail(ctx, AGZO_EINVAL, "cu or n_accepted is NULL");
+    if (ldp < vocab || (q && ldq < vocab)) return fail(ctx, AGZO_EINVAL, "leading dimension below the row length");
+    if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & (size - 1)) || ((reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(uniforms) |
+        reinterpret_cast<uintptr_t>(cu) | reinterpret_cast<uintptr_t>(out_tokens) | reinterpret_cast<uintptr_t>(out_rows) | reinterpret_cast<uintptr_t>(n_accepted)) & 3))
+        return fail(ctx, AGZO_EINVAL, "misaligned tensor");
+    TRY(check_apart(ctx, {listed("out_tokens", out_tokens, n), listed("out_rows", out_rows, n), listed("n_accepted", n_accepted, n_seq)},
+                    {named("p", p, ldp, n, vocab, size), named("q", q, ldq, n, vocab, size), listed("tokens", tokens, n), listed("parents", parents, n), listed("uniforms", uniforms, n),
+                     listed("cu", cu, n_seq + 1LL)}));
+    TRY(check_device(ctx));
+    if (n == 0 || n_seq == 0) return AGZO_OK;
+    TRY(reserve(ctx, verify_workspace_bytes(n_seq, vocab)));
+    HIPCHK(launch_verify(VerifyArgs{p, q, ldp, ldq, tokens, parents, uniforms, cu, n, n_seq, vocab, out_tokens, out_rows, n_accepted}, dtype == AGZO_F32, ctx->ws, ctx->stream));
     return AGZO_OK;
 }
 

@@ -455,6 +455,54 @@ hipError_t launch_packed_forward(const PackedArgs& a, int head_dim, bf16_t* out,
 size_t packed_backward_workspace_bytes(const PackedArgs& a, int head_dim);
 hipError_t launch_packed_backward(const PackedArgs& a, int head_dim, const PackedGrad& g, void* workspace, hipStream_t st);
 
+// A cache of keys and values in pages of page_size tokens: place p of sequence s lies in page table[s ld_table + p / page_size], slot p % page_size, values
+// page * k_page + slot * k_row + key head * k_head + .. of k.  k_len: the sequences' keys, the new tokens of a call among them
+struct PagedCache {
+    bf16_t *k, *v;
+    int64_t k_page, k_row, k_head, v_page, v_row, v_head, n_pages;
+    const int32_t* table; int64_t ld_table;
+    const int32_t* k_len;
+    int page_size, max_pages, n_seq, n_kv;
+};
+// glue_cache.hip : rotation by positions [n] of rows [n][heads head_dim] (bf16 or fp32), y may be x; into the cache; a tree's accepted tokens together in it
+struct RopeArgs {
+    int rot, interleaved, by_turns; float magnitude;
+    double log2_theta, keep_from, keep_by, inv_factor;      // kept: keep_from + keep_by * (frequency if by_turns, else number of the pair), within 0 .. 1
+};
+struct RopeTensor { const void* x; int64_t ldx; void* y; int64_t ldy; int heads; };
+hipError_t launch_rope(const RopeArgs& r, bool f32, const RopeTensor& q, const RopeTensor& k, const int32_t* positions, int64_t n, int head_dim, bool back, hipStream_t st);
+struct CacheAppend {
+    const bf16_t *q, *k, *v; int64_t ldq, ldk, ldv;
+    bf16_t* q_out; int64_t ldqo;
+    const int32_t *cu_q, *positions;       // positions: nullable
+    int64_t n; int n_heads;
+    const float *q_gain, *k_gain; bool norm; float eps;
+};
+hipError_t launch_cache_append(const PagedCache& c, int head_dim, const RopeArgs& r, const CacheAppend& a, hipStream_t st);
+hipError_t launch_cache_keep(const PagedCache& c, int head_dim, const int32_t* cu_q, int64_t n, const int32_t* rows, const int32_t* n_kept, hipStream_t st);
+
+// glue_paged.hip : attention of new tokens over such a cache, causal or with the bits of `tree` among the new ones
+struct PagedAttention {
+    const bf16_t* q; int64_t ldq;
+    const int32_t* cu_q; int64_t total_q;  // total_q n_heads / n_kv below 2^31
+    int n_heads; float scale;
+    const uint32_t* tree; int64_t ld_tree; int words;      // nullable; words of a row
+    bf16_t* out; int64_t ldo; float* lse;
+};
+int64_t paged_units(const PagedCache& c, const PagedAttention& a);
+size_t paged_workspace_bytes(const PagedCache& c, const PagedAttention& a, int head_dim);
+hipError_t launch_paged_attention(const PagedCache& c, const PagedAttention& a, int head_dim, void* workspace, hipStream_t st);
+
+// verify.hip : drafted tokens against rows of probabilities (bf16 or fp32)
+struct VerifyArgs {
+    const void *p, *q; int64_t ldp, ldq;   // q: nullable
+    const int32_t *tokens, *parents; const float* uniforms;      // parents: nullable
+    const int32_t* cu; int64_t n; int n_seq; int64_t vocab;
+    int32_t *out_tokens, *out_rows, *n_accepted;
+};
+size_t verify_workspace_bytes(int n_seq, int64_t vocab);
+hipError_t launch_verify(const VerifyArgs& a, bool f32, void* workspace, hipStream_t st);
+
 // probe.hip : register-only MFMA loop for measuring the sustained matrix rate and shader clock of the device;
 // clk4: four 64-bit words for the counters plus 1 KiB that the kernel may (never does) write behind them
 hipError_t launch_probe_mfma(const void* operands, int duty, int iters, unsigned long long* clk4, hipStream_t st);

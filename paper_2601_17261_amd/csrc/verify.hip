@@ -1,0 +1,321 @@
+// Drafted tokens verified against the target's probabilities with given random numbers, and the token that follows them.  Row 0 of a sequence is the token
+// that is there already, the rows behind it are its drafted tokens, a chain or a tree (a row's parent is in front of it).  From the root on, the children of the node
+// that has been reached are tried in order: with the node's probabilities p, child x with the random number u is accepted where
+//     u q(x) < p(x)         in a chain whose tokens were drawn from the probabilities q,
+//     u (1 - sum of p over the node's children refused so far) < p(x)     where tokens are proposed for certain,
+// and the token that follows the last one accepted is drawn, by the root's random number, from the weights
+//     w = max(p - q, 0)  or  p without the refused children,
+// as the first x whose sum of w up to it exceeds u times all of them.  Each accepted token then has the target's distribution: what a refusal leaves out of it, the
+// last draw makes up for.
+//
+// Products, differences and sums are fp64: differences of fp32 values are exact there, and a draw's border is off by 2^-50 of the sum, so that the choice is that
+// of the exact sums but for one draw in 10^13 or so.
+//
+// One row (two in a chain) of each sequence is read whole, which is what bounds it; the walk before that is a chain of three loads, and every workgroup makes it again
+// by itself: a launch of its own would take longer.
+#include "agzo_internal.h"
+
+namespace agzo {
+
+namespace {
+
+constexpr int VF_WG = 256, VF_LEAST = 2048, VF_MOST_SEGMENTS = 256;
+
+__device__ __forceinline__ float vf_get(const float* p, int64_t i) { return p[i]; }
+__device__ __forceinline__ float vf_get(const bf16_t* p, int64_t i) { return bf16_to_f32(p[i]); }
+// (negative values and NaN count as 0)
+__device__ __forceinline__ double vf_mass(float x) { return x > 0.f ? (double)x : 0.0; }
+
+__device__ __forceinline__ double vf_readlane(double x, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
+}
+
+// Where a sequence's walk ends: at a row, a chain's row refused there (0: none), how many rows accepted
+struct VfEnd { int at, refused, count; };
+
+// By one wave, 64 rows at a time, which is right since a node's children stand behind it.  write: the accepted rows are stored too
+template <typename T>
+__device__ __forceinline__ VfEnd vf_walk(const VerifyArgs& a, int64_t r0, int rows, bool write) {
+    const T *p = static_cast<const T*>(a.p), *q = static_cast<const T*>(a.q);
+    const int lane = threadIdx.x & 63;
+    VfEnd e{0, 0, 0};
+    double left = 1.0;
+    for (int b = 0; b < rows; b += 64) {
+        const int row = b + lane;
+        const bool there = row > 0 && row < rows;
+        const int tok = there ? a.tokens[r0 + row] : -1;
+        const int up = !there ? -1 : a.parents ? a.parents[r0 + row] : row - 1;
+        const int parent = up >= 0 && up < row ? up : -1;
+        const bool known = parent >= 0 && tok >= 0 && tok < a.vocab;
+        const double target = known ? vf_mass(vf_get(p, (r0 + parent) * a.ldp + tok)) : 0.0;
+        const double draft = known && q ? vf_mass(vf_get(q, (r0 + row) * a.ldq + tok)) : 0.0;
+        const double u = there ? (double)a.uniforms[r0 + row] : 0.0;
+        int tried = b - 1;
+        while (true) {
+            const uint64_t next = __builtin_amdgcn_ballot_w64(parent == e.at && row > max(tried, e.at));
+            if (!next) break;
+            const int i = __builtin_ctzll(next), x = __builtin_amdgcn_readlane(tok, i);
+            double mass = vf_readlane(target, i);
+            tried = b + i;
+            if (!q) {
+                // a token that a sibling before has been refused with has nothing left
+                bool again = __builtin_amdgcn_ballot_w64(parent == e.at && row < tried && tok == x) != 0;
+                for (int c = 0; c < b && !again; c += 64) {
+                    const bool sibling = c + lane > e.at && a.parents && a.parents[r0 + c + lane] == e.at && a.tokens[r0 + c + lane] == x;
+                    again = __builtin_amdgcn_ballot_w64(sibling) != 0;
+                }
+                if (again) mass = 0.0;
+            }
+            const double of = q ? vf_readlane(draft, i) : left;
+            if (mass > 0.0 && vf_readlane(u, i) * of < mass) {
+                if (write && lane == 0) {
+                    a.out_tokens[r0 + e.count] = x;
+                    a.out_rows[r0 + e.count] = tried;
+                }
+                e.at = tried;
+                e.refused = 0;
+                ++e.count;
+                left = 1.0;
+            } else {
+                left -= mass;
+                e.refused = tried;
+            }
+        }
+    }
+    return e;
+}
+
+// bits of the tokens first .. first + n that children of `at` have: all of them were refused
+__device__ __forceinline__ void vf_refused(const VerifyArgs& a, int64_t r0, int rows, int at, int64_t first, int n, uint32_t* bits) {
+    for (int row = at + 1 + (int)threadIdx.x; row < rows; row += VF_WG) {
+        const int up = a.parents ? a.parents[r0 + row] : row - 1;
+        const int64_t x = (int64_t)a.tokens[r0 + row] - first;
+        if (up == at && x >= 0 && x < n) atomicOr(&bits[x >> 5], 1u << (x & 31));
+    }
+}
+
+// eight values of a row from i on (0 behind its end)
+__device__ __forceinline__ void vf_eight(const float* p, int64_t i, int64_t end, float (&f)[8]) {
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+    if (i + 8 <= end) {
+        const vec x = *reinterpret_cast<const vec*>(p + i), y = *reinterpret_cast<const vec*>(p + i + 4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { f[u] = x[u]; f[4 + u] = y[u]; }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) f[u] = i + u < end ? p[i + u] : 0.f;
+    }
+}
+__device__ __forceinline__ void vf_eight(const bf16_t* p, int64_t i, int64_t end, float (&f)[8]) {
+    typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+    if (i + 8 <= end) {
+        const vec x = *reinterpret_cast<const vec*>(p + i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { f[2 * u] = __uint_as_float(x[u] << 16); f[2 * u + 1] = __uint_as_float(x[u] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) f[u] = i + u < end ? bf16_to_f32(p[i + u]) : 0.f;
+    }
+}
+
+// weights of eight tokens, the first one `in` of its segment
+__device__ __forceinline__ void vf_weights(const float (&p)[8], const float (&q)[8], uint32_t gone, double (&w)[8]) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const double d = vf_mass(p[u]) - vf_mass(q[u]);
+        w[u] = d > 0.0 && !((gone >> u) & 1) ? d : 0.0;
+    }
+}
+
+struct VfState { double2* sums; int4* ends; };      // [n_seq][segments]: of the weights and of p; [n_seq]
+__device__ __forceinline__ void vf_rows(const VerifyArgs& a, int seq, int64_t& r0, int& rows) {
+    r0 = min(max((int64_t)a.cu[seq], (int64_t)0), a.n);
+    rows = (int)(min(max((int64_t)a.cu[seq + 1], r0), a.n) - r0);
+}
+
+template <typename T>
+__global__ __launch_bounds__(VF_WG) void verify_sums_kernel(VerifyArgs a, VfState s, int segment) {
+    extern __shared__ uint32_t vf_bits[];
+    __shared__ double2 part[VF_WG / 64];
+    const int seq = blockIdx.y, seg = blockIdx.x;
+    int64_t r0;
+    int rows;
+    vf_rows(a, seq, r0, rows);
+    if (rows == 0) {
+        if (seg == 0 && threadIdx.x == 0) {
+            a.n_accepted[seq] = 0;
+            s.ends[seq] = make_int4(0, 0, 0, 0);
+        }
+        return;
+    }
+    const VfEnd e = vf_walk<T>(a, r0, rows, seg == 0 && threadIdx.x < 64);
+    if (seg == 0) {
+        if (threadIdx.x == 0) {
+            a.n_accepted[seq] = e.count;
+            s.ends[seq] = make_int4(e.at, e.refused, e.count, 0);
+        }
+        // (the entry behind the accepted ones is the draw's)
+        for (int i = e.count + (int)threadIdx.x; i < rows; i += VF_WG) {
+            if (i > e.count) a.out_tokens[r0 + i] = -1;
+            a.out_rows[r0 + i] = -1;
+        }
+    }
+    const T *p = static_cast<const T*>(a.p) + (r0 + e.at) * a.ldp, *q = a.q && e.refused ? static_cast<const T*>(a.q) + (r0 + e.refused) * a.ldq : nullptr;
+    const int64_t first = (int64_t)seg * segment, end = min(first + segment, a.vocab);
+    const bool marked = !a.q && e.refused;
+    if (marked) {
+        for (int i = threadIdx.x; i < segment / 32; i += VF_WG) vf_bits[i] = 0;
+        __syncthreads();
+        vf_refused(a, r0, rows, e.at, first, segment, vf_bits);
+        lds_barrier();
+    }
+    double sum = 0.0, all = 0.0;
+    for (int64_t i = first + 8 * threadIdx.x; i < end; i += 8 * VF_WG) {
+        float f[8], g[8] = {};
+        vf_eight(p, i, end, f);
+        if (q) vf_eight(q, i, end, g);
+        double w[8];
+        vf_weights(f, g, marked ? vf_bits[(i - first) >> 5] >> ((i - first) & 31) : 0, w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { sum += w[u]; all += vf_mass(f[u]); }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { sum += __shfl_xor(sum, o); all += __shfl_xor(all, o); }
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = make_double2(sum, all);
+    lds_barrier();
+    if (threadIdx.x == 0) {
+        double2 t = part[0];
+        for (int i = 1; i < VF_WG / 64; ++i) { t.x += part[i].x; t.y += part[i].y; }
+        s.sums[(int64_t)seq * gridDim.x + seg] = t;
+    }
+}
+
+// sums of the threads up to each, this one among them
+__device__ __forceinline__ double vf_scan(double x, double* red) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 63) red[wave] = x;
+    lds_barrier();
+    for (int i = 0; i < wave; ++i) x += red[i];
+    return x;
+}
+
+// The draw: the segment that the border lies in, then the token in it.  A thread has `segment / 256` tokens, 8 and more
+template <typename T>
+__global__ __launch_bounds__(VF_WG) void verify_draw_kernel(VerifyArgs a, VfState s, int segment, int segments) {
+    extern __shared__ uint32_t vf_bits[];
+    __shared__ double red[2][VF_WG / 64];
+    __shared__ double before;
+    __shared__ int found, last;
+    const int seq = blockIdx.x, t = threadIdx.x;
+    int64_t r0;
+    int rows;
+    vf_rows(a, seq, r0, rows);
+    if (rows == 0) return;
+    const int4 e = s.ends[seq];
+    const double2 mine = t < segments ? s.sums[(int64_t)seq * segments + t] : make_double2(0.0, 0.0);
+    // (nothing left, as where the probabilities do not add up to 1: the target's own)
+    const bool own = !__syncthreads_or(mine.x > 0.0);
+    const double sum = own ? mine.y : mine.x;
+    if (t == 0) { found = 1 << 30; last = -1; }
+    const double upto = vf_scan(sum, red[0]);
+    __shared__ double total;
+    if (t == VF_WG - 1) total = upto;
+    lds_barrier();
+    const double border = (double)a.uniforms[r0] * total;
+    if (sum > 0.0) {
+        atomicMax(&last, t);
+        if (upto > border) atomicMin(&found, t);
+    }
+    lds_barrier();
+    if (last < 0) {                       // no token has any probability
+        if (t == 0) a.out_tokens[r0 + e.z] = -1;
+        return;
+    }
+    // (a border at the end or behind it: the last token that has any weight)
+    const bool behind = found == 1 << 30;
+    const int seg = behind ? last : found;
+    if (t == seg) before = upto - sum;
+    const T *p = static_cast<const T*>(a.p) + (r0 + e.x) * a.ldp, *q = a.q && e.y && !own ? static_cast<const T*>(a.q) + (r0 + e.y) * a.ldq : nullptr;
+    const int64_t first = (int64_t)seg * segment, end = min(first + segment, a.vocab);
+    const bool marked = !a.q && e.y && !own;
+    if (marked) {
+        for (int i = t; i < segment / 32; i += VF_WG) vf_bits[i] = 0;
+        lds_barrier();
+        vf_refused(a, r0, rows, e.x, first, segment, vf_bits);
+    }
+    lds_barrier();
+    if (t == 0) { found = 1 << 30; last = -1; }
+    const int per = segment / VF_WG;
+    const int64_t from = first + (int64_t)t * per;
+    auto weights = [&](int64_t i, double (&w)[8]) __attribute__((always_inline)) {
+        float f[8], g[8] = {};
+        vf_eight(p, i, end, f);
+        if (q) vf_eight(q, i, end, g);
+        vf_weights(f, g, marked ? vf_bits[(i - first) >> 5] >> ((i - first) & 31) : 0, w);
+    };
+    double x = 0.0, w[8];
+    for (int64_t i = from; i < min(from + per, end); i += 8) {
+        weights(i, w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x += w[u];
+    }
+    const double run = before + vf_scan(x, red[1]);
+    if (x > 0.0) {
+        atomicMax(&last, t);
+        if (!behind && run > border) atomicMin(&found, t);
+    }
+    lds_barrier();
+    // (sums in another order than the segment's: a border within 2^-50 of its end may be behind all of them)
+    const bool at_end = found == 1 << 30;
+    if (t != (at_end ? last : found)) return;
+    double so_far = run - x;
+    int64_t pick = -1;
+    for (int64_t i = from; i < min(from + per, end); i += 8) {
+        weights(i, w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const double prior = so_far;
+            so_far += w[u];
+            if (w[u] > 0.0 && (at_end || pick < 0 || !(prior > border))) pick = i + u;
+        }
+    }
+    a.out_tokens[r0 + e.z] = (int)pick;
+}
+
+int verify_segment(int n_seq, int64_t vocab) {
+    // enough workgroups to keep every compute unit's loads in flight, of no fewer tokens than a workgroup takes at a time
+    int64_t size = VF_LEAST;
+    while ((vocab + size - 1) / size > VF_MOST_SEGMENTS || (n_seq * ((vocab + size - 1) / size) > 1024 && size < 16 * VF_LEAST)) size *= 2;
+    return (int)size;
+}
+
+template <typename T>
+hipError_t launch_verify_typed(const VerifyArgs& a, void* workspace, hipStream_t st) {
+    const int segment = verify_segment(a.n_seq, a.vocab), segments = (int)((a.vocab + segment - 1) / segment);
+    const VfState s{static_cast<double2*>(workspace), reinterpret_cast<int4*>(static_cast<double2*>(workspace) + (int64_t)a.n_seq * segments)};
+    const size_t smem = a.q ? 0 : segment / 8;
+    hipLaunchKernelGGL(verify_sums_kernel<T>, dim3(segments, a.n_seq), dim3(VF_WG), smem, st, a, s, segment);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(a.n_seq), dim3(VF_WG), smem, st, a, s, segment, segments);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t verify_workspace_bytes(int n_seq, int64_t vocab) {
+    const int segment = verify_segment(n_seq, vocab);
+    return (size_t)n_seq * ((vocab + segment - 1) / segment) * sizeof(double2) + (size_t)n_seq * sizeof(int4);
+}
+
+hipError_t launch_verify(const VerifyArgs& a, bool f32, void* workspace, hipStream_t st) {
+    if (a.n == 0 || a.n_seq == 0) return hipSuccess;
+    return f32 ? launch_verify_typed<float>(a, workspace, st) : launch_verify_typed<bf16_t>(a, workspace, st);
+}
+
+}  // namespace agzo
