@@ -8,12 +8,11 @@
 // from LDS with a transposition.  Keys and values reach LDS through registers, 16 rows to a group, so that where a page's size is a multiple of 16 (WHOLE) a
 // group has one page, found by a scalar load; else every lane looks its rows' pages up.  Pages are looked up a tile ahead of the loads that they lead to.
 //
-// Lengths are on the device, so how the work is shared out is worked out there too, by every workgroup alike: all row tiles' key tiles together over the workgroups
-// that are wanted is a share, and what has more keys than that is made in equal shares of them, joined by a second launch.  However uneven the
-// lengths are, no workgroup has more than a share, and few rows on many keys (single tokens, trees) fill the device.
+// Lengths are on the device, so how the work is shared out is worked out there too, by every workgroup alike, and however uneven they are no workgroup has more than
+// its share: few rows on many keys (single tokens, trees) fill the device.  What several workgroups have of a row tile a second launch joins.
 //
 // What a masked place holds takes part in nothing: scores there are replaced, and where a workgroup's results are not finite it goes over its tiles once more with
-// care, with such values taken out, and what the visible ones amount to found by a product of two indicators.
+// care, with such values taken out of the products and added where they are seen.
 #include <atomic>
 
 #include "packed_tiles.h"
@@ -23,69 +22,176 @@ namespace agzo {
 
 namespace {
 
-constexpr int PG_WAVES = 4, PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgroup, keys of a tile
+constexpr int PG_WAVES = 4;
 
-struct PgOut { float* part; float2* part_ml; int slots, target, least; QuickDiv by_kv, by_group, by_page; };
+// What a launch is told: the workgroups of each key head that work may be shared out to, and the keys of a row tile that a share has at least (it costs its start, its
+// sums, and a part in the launch that joins them)
+struct PgOut { float* part; float2* part_ml; int shares, least; QuickDiv by_kv, by_group, by_page; };
 
-// One workgroup's work: a tile of rows of a sequence, and the tiles [from, to) of its keys that it goes over, had every row seen all.  slot: where its sums go, -1: it
-// is not shared out
-struct PgUnit { PagedSeq s; int seq, tile, share, per, slot; };
+// ---- who does what -----------------------------------------------------------------------------------------------
+// A row tile's work is about the keys that its rows see: first + t step of row tile t of a sequence, so that the work in front of one is a whole number that every
+// workgroup finds alike.  Row tiles are one workgroup's each where that leaves none of them much longer than the others' work, else the work of all of them in a row
+// is cut into equal pieces: a workgroup then has the end of one row tile, perhaps whole ones, and the beginning of another.  (A share each to 64 sequences' row tiles
+// and 512 places for them: 219 us of keys that took 175 so)
+struct PgWork { int tiles; int64_t first, step; };      // of a sequence: its row tiles, their work
 
-__device__ __forceinline__ float pg_total(float x) {
+template <int ROWS>
+__device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there) {
+    PgWork w;
+    w.tiles = there ? (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
+    w.step = a.tree ? 0 : (ROWS + G - 1) / G;
+    w.first = max((a.tree ? s.nk : s.nk - s.nq) + (int)w.step, 1);
+    return w;
+}
+__device__ __forceinline__ int64_t pg_before(const PgWork& w, int t) { return w.first * t + w.step * ((int64_t)t * (t - 1) / 2); }
+
+__device__ __forceinline__ int64_t pg_lane(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
+}
+// sums over the lanes up to each
+__device__ __forceinline__ int64_t pg_scan(int64_t x) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
     return x;
 }
+__device__ __forceinline__ int pg_max(int x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
+    return __builtin_amdgcn_readfirstlane(x);
+}
 
-// Tiles of keys of a share: those of all row tiles over the workgroups of a key head that are wanted, `least` at least.  (In fp32: the same in every workgroup, which is
-// all that is asked of it)
-template <int ROWS, int KEYS>
-__device__ __forceinline__ int pg_share(const PagedCache& c, const PagedAttention& a, const PgOut& o, int G) {
-    float work = 0.f;
+// the sequences 64 at a time, one to a lane; `first`: those of the first 64
+struct PgSeqs {
+    PagedSeq first;
+    __device__ __forceinline__ PgSeqs(const PagedCache& c, const PagedAttention& a) : first(load(c, a, 0)) {}
+    static __device__ __forceinline__ PagedSeq load(const PagedCache& c, const PagedAttention& a, int b) {
+        return paged_seq(c, a.cu_q, (int)a.total_q, min(b + (int)(threadIdx.x & 63), c.n_seq - 1));
+    }
+    __device__ __forceinline__ PagedSeq at(const PagedCache& c, const PagedAttention& a, int b) const { return b == 0 ? first : load(c, a, b); }
+};
+
+template <int ROWS>
+__device__ __forceinline__ void pg_share_out(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgSeqs& seqs, int G, int64_t& total, int& shares) {
+    const int lane = threadIdx.x & 63;
+    int64_t tiles = 0;
+    int longest = 0;
+    total = 0;
     for (int b = 0; b < c.n_seq; b += 64) {
+        const PagedSeq s = seqs.at(c, a, b);
+        const PgWork w = pg_work<ROWS>(a, s, G, b + lane < c.n_seq);
+        total += pg_lane(pg_scan(pg_before(w, w.tiles)), 63);
+        tiles += pg_lane(pg_scan(w.tiles), 63);
+        longest = max(longest, pg_max(w.tiles ? s.nk : 0));
+    }
+    const int64_t wanted = min((int64_t)o.shares, (total + o.least - 1) / o.least), each = total / max(o.shares, 1) + o.least;
+    // (2^52: what a piece's number times all work still fits)
+    const bool whole = longest <= o.least || (tiles <= o.shares ? longest <= each : longest <= each / 4) || total >= (1LL << 52);
+    shares = whole ? 0 : (int)wanted;
+}
+
+// Where a piece of the work lies: a row tile, the part [from, to) of its work `all`; slot: where its sums go, -1: it is the whole row tile
+struct PgUnit { PagedSeq s; int seq, tile; int64_t from, to, all; int slot; };
+__device__ __forceinline__ int pg_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t pg_uniform(int64_t x) { return (int64_t)((uint64_t)(uint32_t)pg_uniform((int)(x >> 32)) << 32 | (uint32_t)pg_uniform((int)x)); }
+// (the same in all lanes, and known to be)
+__device__ __forceinline__ PgUnit pg_uniform(const PgUnit& u) {
+    return PgUnit{PagedSeq{pg_uniform(u.s.q0), pg_uniform(u.s.nq), pg_uniform(u.s.nk)}, pg_uniform(u.seq), pg_uniform(u.tile), pg_uniform(u.from), pg_uniform(u.to), pg_uniform(u.all),
+                  pg_uniform(u.slot)};
+}
+
+// A workgroup's pieces of work, one after the other
+template <int ROWS>
+struct PgWalk {
+    int64_t pos, end, start;      // work in front of what is left, and behind it; start: in front of sequence seq's row tile `tile`
+    int seq, tile, index;
+    bool whole, first;
+    PagedSeq s;
+    PgWork w;
+
+    // its place: workgroup `index` of a key head's.  false: there is nothing for it
+    __device__ __forceinline__ bool begin(const PagedCache& c, const PagedAttention& a, const PgOut& o, int index_, int G) {
         const int lane = threadIdx.x & 63;
-        const PagedSeq s = paged_seq(c, a.cu_q, (int)a.total_q, min(b + lane, c.n_seq - 1));
-        const int rows = (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS), keys = (s.nk + KEYS - 1) / KEYS;
-        work += pg_total(b + lane < c.n_seq ? (float)rows * (float)keys : 0.f);
-    }
-    return (int)fminf(1073741824.f, fmaxf((float)o.least, ceilf(work / (float)o.target)));
-}
-
-// shares of a sequence with so many tiles of keys, and tiles of each
-__device__ __forceinline__ int pg_shares(int keys, int chunk, int& per) {
-    const int shares = max(1, (keys + chunk - 1) / chunk);
-    per = max(1, (keys + shares - 1) / shares);
-    return shares;
-}
-
-// Unit number t of all sequences' units
-template <int ROWS, int KEYS>
-__device__ __forceinline__ bool pg_find(const PagedCache& c, const PagedAttention& a, const PgOut& o, int t, int G, PgUnit& u) {
-    const int lane = threadIdx.x & 63, chunk = pg_share<ROWS, KEYS>(c, a, o, G);
-    int slots = 0;
-    for (int b = 0; b < c.n_seq; b += 64) {
-        const PagedSeq s = paged_seq(c, a.cu_q, (int)a.total_q, min(b + lane, c.n_seq - 1));
-        const int rows = b + lane < c.n_seq ? (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
-        int per;
-        const int shares = pg_shares((s.nk + KEYS - 1) / KEYS, chunk, per), count = rows * shares, split = shares > 1 ? count : 0;
-        const int sum = pk_scan(count), splits = pk_scan(split), total = __builtin_amdgcn_readlane(sum, 63);
-        if (t < total) {
-            const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > t));
-            const int in = t - __builtin_amdgcn_readlane(sum - count, src), tiles = __builtin_amdgcn_readlane(rows, src);
-            u.seq = b + src;
-            u.s = PagedSeq{__builtin_amdgcn_readlane(s.q0, src), __builtin_amdgcn_readlane(s.nq, src), __builtin_amdgcn_readlane(s.nk, src)};
-            u.per = __builtin_amdgcn_readlane(per, src);
-            u.share = in / tiles;
-            // (a prompt's last rows see most: they come first)
-            u.tile = tiles - 1 - (in - u.share * tiles);
-            u.slot = __builtin_amdgcn_readlane(split, src) > 0 ? slots + __builtin_amdgcn_readlane(splits - split, src) + u.share * tiles + u.tile : -1;
-            return true;
+        const PgSeqs seqs(c, a);
+        int64_t total;
+        int shares;
+        pg_share_out<ROWS>(c, a, o, seqs, G, total, shares);
+        index = index_;
+        whole = shares == 0;
+        first = true;
+        if (whole) {
+            pos = index;
+            end = pos + 1;
+        } else {
+            if (index >= shares) return false;
+            pos = index * total / shares;
+            end = (index + 1) * total / shares;
+            if (pos >= end) return false;
         }
-        t -= total;
-        slots += __builtin_amdgcn_readlane(splits, 63);
+        int64_t before = 0;
+        for (int b = 0; b < c.n_seq; b += 64) {
+            const PagedSeq its = seqs.at(c, a, b);
+            const PgWork work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq);
+            const int64_t own = whole ? work.tiles : pg_before(work, work.tiles), sum = pg_scan(own) + before;
+            const uint64_t m = __builtin_amdgcn_ballot_w64(sum > pos);
+            if (m) {
+                const int src = __builtin_ctzll(m);
+                seq = b + src;
+                s = PagedSeq{__builtin_amdgcn_readlane(its.q0, src), __builtin_amdgcn_readlane(its.nq, src), __builtin_amdgcn_readlane(its.nk, src)};
+                w = pg_work<ROWS>(a, s, G, true);
+                const int64_t in = pos - (pg_lane(sum, src) - pg_lane(own, src));
+                if (whole) {
+                    tile = w.tiles - 1 - (int)in;      // (a prompt's last rows see most: they come first)
+                    return true;
+                }
+                // the last row tile that begins at or in front of it
+                int low = 0, high = w.tiles - 1;
+                while (low < high) {
+                    const int mid = (low + high + 1) >> 1;
+                    if (pg_before(w, mid) <= in) low = mid;
+                    else high = mid - 1;
+                }
+                tile = low;
+                start = pos - (in - pg_before(w, low));
+                return true;
+            }
+            before = pg_lane(sum, 63);
+        }
+        return false;
     }
-    return false;
-}
+    __device__ __forceinline__ PgUnit unit() const {
+        PgUnit u;
+        u.s = s;
+        u.seq = seq;
+        u.tile = tile;
+        u.all = w.first + w.step * tile;
+        u.from = whole ? 0 : pos - start;
+        u.to = whole ? u.all : min(u.all, end - start);
+        u.slot = u.from == 0 && u.to == u.all ? -1 : 2 * index + (first ? 0 : 1);
+        return u;
+    }
+    // on to the next one
+    __device__ __forceinline__ bool next(const PagedCache& c, const PagedAttention& a, int G) {
+        if (whole) return false;
+        start += w.first + w.step * tile;
+        pos = start;
+        first = false;
+        if (pos >= end) return false;
+        if (++tile < w.tiles) return true;
+        tile = 0;
+        while (++seq < c.n_seq) {
+            s = paged_seq(c, a.cu_q, (int)a.total_q, __builtin_amdgcn_readfirstlane(seq));
+            w = pg_work<ROWS>(a, s, G, true);
+            if (w.tiles > 0) return true;
+        }
+        return false;
+    }
+};
+// of a row tile's `tiles` tiles of keys those that a piece of its work has
+__device__ __forceinline__ int pg_cut(int tiles, int64_t part, int64_t all) { return part >= all ? tiles : (int)((tiles * part + all - 1) / all); }
 
 // The 32 keys from kb on that new token q of a sequence sees, a bit for each
 __device__ __forceinline__ uint32_t pg_seen(const PagedAttention& a, const PagedSeq& s, int q, int kb) {
@@ -123,7 +229,9 @@ struct PgGroup {
     static __device__ __forceinline__ Pages pages(const PagedCache& c, const QuickDiv& by_page, const int32_t* table, int kg, int nk) {
         Pages p;
         if (WHOLE) {
-            p.id[0] = table[by_page(min(kg, nk - 1))];
+            // (a scalar load: a vector one's wait would be one for the tile's loads in front of it too)
+            typedef const __attribute__((address_space(4))) int32_t* scalar;
+            p.id[0] = ((scalar)(uintptr_t)table)[by_page(min(kg, nk - 1))];
         } else {
             const int r = row_of_lane();
 #pragma unroll
@@ -148,7 +256,9 @@ struct PgGroup {
                 const int key = min(kg + r + ROWS * i, nk - 1), slot = key - by_page(key) * c.page_size;
                 const int64_t page = min(max(p.id[WHOLE ? 0 : i], 0), most);
                 const char* at = reinterpret_cast<const char*>(base + page * page_ld + slot * row_ld) + (chunk ^ (pk_swz<HD>(ROWS * i) << 4));
-                data[i] = *reinterpret_cast<const uint4*>(at);
+                typedef uint32_t vec __attribute__((ext_vector_type(4)));
+                const vec v = *reinterpret_cast<const vec*>(at);
+                data[i] = make_uint4(v[0], v[1], v[2], v[3]);
             }
         }
     }
@@ -159,37 +269,83 @@ struct PgGroup {
     }
 };
 
-// ones and zeros of 32 bits of keys, as a lane's fragments of two times 16 positions
-__device__ __forceinline__ void pg_fragments(uint32_t seen, PkFrag* f) {
-    const uint32_t m = seen >> (4 * ((threadIdx.x >> 5) & 1));
+// ---- with care ---------------------------------------------------------------------------------------------------
+// Values that are not finite, in a tile of KEYS values in LDS: in which keys there are any
+template <int HD, int KEYS>
+__device__ __forceinline__ uint64_t pg_bad_keys(const char* tile) {
+    constexpr int LANES = HD / 8, ROWS = 64 / LANES;
+    uint64_t keys = 0;
+#pragma unroll 1
+    for (int i = 0; i < KEYS / ROWS; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(tile + i * 1024 + (threadIdx.x & 63) * 16);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        bool bad = false;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+        for (int x = 0; x < 4; ++x) bad = bad || (w[x] & 0x7F80u) == 0x7F80u || (w[x] & 0x7F800000u) == 0x7F800000u;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(bad);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int at = 16 * s + (w >> 1) * 8 + (w & 1) * 2;
-            f[s].w[w] = ((m >> at) & 1 ? 0x3F80u : 0u) | ((m >> (at + 1)) & 1 ? 0x3F800000u : 0u);
+        for (int r = 0; r < ROWS; ++r) keys |= (uint64_t)((m >> (r * LANES)) & ((1ull << LANES) - 1) ? 1 : 0) << (i * ROWS + r);
+    }
+    return keys;
+}
+// ... added to the sums of the rows that see them: infinities and NaN as they are, whatever their probability
+template <int HD>
+__device__ __forceinline__ void pg_add_bad(const char* tile, uint64_t keys, uint64_t seen, pk_floatx16 (&acc)[HD / 32]) {
+    const int hi = (threadIdx.x >> 5) & 1;
+#pragma unroll 1
+    for (; keys; keys &= keys - 1) {
+        const int r = __builtin_ctzll(keys);
+        const bool sees = (seen >> r) & 1;
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint2 v = *reinterpret_cast<const uint2*>(tile + r * (HD * 2) + (((4 * db + g) ^ pk_swz<HD>(r)) << 4) + 8 * hi);
+                const uint32_t x[4] = {v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (sees && (x[i] & 0x7F800000u) == 0x7F800000u) acc[db][4 * g + i] += __uint_as_float(x[i]);
+            }
+    }
+}
+__device__ __forceinline__ void pg_clean(PkFrag& f) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if ((f.w[w] & 0x7F80u) == 0x7F80u) f.w[w] &= 0xFFFF0000u;
+        if ((f.w[w] & 0x7F800000u) == 0x7F800000u) f.w[w] &= 0xFFFFu;
+    }
+}
+// the second product with them taken out, its fragments of 16 positions `at` on
+template <int HD, bool LOW, int N>
+__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[N], const PkFrag (&low)[N], pk_floatx16 (&acc)[HD / 32]) {
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db) {
+            PkFrag f;
+            pk_read_trans<HD>(o, at + s * 16 * HD * 2, db, f);
+            pg_clean(f);
+            acc[db] = pk_mfma(f, p[s], acc[db]);
+            if (LOW) acc[db] = pk_mfma(f, low[s], acc[db]);
         }
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------
+constexpr int PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgroup, keys of a tile
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits: the shape of attention over packed sequences, for the same reasons.
 // fine: the probabilities go into the second product in two bf16 parts (16 bits).  For few rows on many keys, whose time is the keys' reading: their sums are of few large
 // probabilities often, whose roundings no others' balance.
 // true: stored nothing, the tiles have to be gone over with care
 template <int HD, bool WHOLE, bool fine, bool careful>
-__device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAttention& a, const PgOut& o, pk_lchar lds) {
+__device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
     char* smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
     constexpr int TILE = PG_KEYS * HD * 2, KS = HD / 16, DB = HD / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
-    // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
-    const int G = (int)o.by_group.d, unit = (int)blockIdx.x, at = o.by_kv(unit), kvh = unit - at * c.n_kv;
-    PgUnit u;
-    if (!pg_find<PG_ROWS, PG_KEYS>(c, a, o, at, G, u)) return false;
+    const int G = (int)o.by_group.d;
     const PagedSeq s_ = u.s;
-    if (u.slot >= o.slots) return false;      // (offsets that do not grow: more of it than there is room for)
     const int R = s_.nq * G, row0 = u.tile * PG_ROWS + wave * 32, shift = s_.nk - s_.nq;
     // The lane's row: its query, its head.  (Worked out where they are needed, from a lane number that the compiler does not know again: kept through the loop they
     // are spilled)
@@ -205,9 +361,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     const int wlast = row0 >= R ? -1 : a.tree ? s_.nk - 1 : o.by_group(min(row0 + 31, R - 1)) + shift;
     const int last = a.tree ? s_.nk - 1 : o.by_group(min((u.tile + 1) * PG_ROWS - 1, R - 1)) + shift;
     const int tiles = last < 0 ? 0 : last / PG_KEYS + 1;
-    const int j0 = u.share * u.per, j1 = min(tiles, j0 + u.per);
-    // (a share that none of the row tile sees.  The first one is there for rows that see nothing at all)
-    if (j0 >= j1 && u.share > 0) return false;
+    const int j0 = pg_cut(tiles, u.from, u.all), j1 = pg_cut(tiles, u.to, u.all);
     const bf16_t* Kh = c.k + kvh * c.k_head;
     const bf16_t* Vh = c.v + kvh * c.v_head;
     const int32_t* table = c.table + (int64_t)u.seq * c.ld_table;
@@ -302,10 +456,9 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         }
         if (careful) {
             const int q = row_of_lane().q;
-            PkFrag seen[4];
-            pg_fragments(pg_seen(a, s_, q, kb), seen);
-            pg_fragments(pg_seen(a, s_, q, kb + 32), seen + 2);
-            pk_second_careful<HD, true, fine>(kt + TILE, pf, pl, seen, acc);
+            const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
+            pg_second_clean<HD, fine, 4>(of, TILE, pf, pl, acc);
+            pg_add_bad<HD>(kt + TILE, pg_bad_keys<HD, PG_KEYS>(kt + TILE), seen, acc);
             return;
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -323,6 +476,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
     top = -INFINITY; topsc = 0.f; l = 0.f;
     begin();
+    lds_barrier();                       // (of the piece before)
     if (j0 < j1) arrive(j0);
     for (int j = j0; j < j1; ++j) {
         lds_barrier();
@@ -333,7 +487,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         one_tile(j);
         if (j + 1 < j1) arrive(j + 1);
     }
-    if (!careful && __syncthreads_or(row_of_lane().mine && pk_not_finite(acc))) return true;
+    if (!careful && __builtin_amdgcn_readfirstlane(__syncthreads_or(row_of_lane().mine && pk_not_finite(acc)))) return true;
     l = pk_sum_halves(l);
     const Row r = row_of_lane();
     if (u.slot >= 0) {
@@ -354,78 +508,362 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     if (a.lse && r.mine && hi == 0) a.lse[tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
     return false;
 }
-// (a function that is called: its registers are not the kernel's)
-template <int HD, bool WHOLE, bool fine>
-__device__ __noinline__ void pg_forward_again(PagedCache c, PagedAttention a, PgOut o, pk_lchar lds) { (void)pg_forward<HD, WHOLE, fine, true>(c, a, o, lds); }
 template <int HD, bool WHOLE, bool fine>
 __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_kernel(PagedCache c, PagedAttention a, PgOut o) {
     extern __shared__ __align__(1024) char pg_dynamic[];
-    if (pg_forward<HD, WHOLE, fine, false>(c, a, o, (pk_lchar)pg_dynamic)) pg_forward_again<HD, WHOLE, fine>(c, a, o, (pk_lchar)pg_dynamic);
+    // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
+    const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
+    PgWalk<PG_ROWS> walk;
+    if (!walk.begin(c, a, o, at, G)) return;
+    do {
+        const PgUnit u = pg_uniform(walk.unit());
+        if (pg_forward<HD, WHOLE, fine, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_forward<HD, WHOLE, fine, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+    } while (walk.next(c, a, G));
 }
 
-// ---- shares joined -----------------------------------------------------------------------------------------------
-// HD / 4 lanes a row, 256 / (HD / 4) rows of one unit's: a workgroup for every row tile's rows, of sequences that are not shared out none
-template <int HD, int ROWS, int KEYS>
+// ---- few rows ----------------------------------------------------------------------------------------------------
+// 32 rows and less (a single token's heads of a group, small trees): the time is the keys' reading.  Four waves that each go over tiles of 32 keys of their own, every
+// fourth of a workgroup's, without a barrier: a tile waits in registers (HD = 128: 16 KB a wave, 128 KB a compute unit in flight from two workgroups, where 32 KB keep
+// memory busy), goes through the wave's own LDS, and the next one is asked for before its products.  The waves' sums are joined at the end.
+// BLOCKS times 16 rows, in instructions of 16 x 16 x 32: lane n + 16 g has row n's scores of the keys 4 g + i and 16 + 4 g + i, and of its sums the dims 16 db + 4 g + i.
+// (32 x 32 x 16 for 16 rows too are 96 registers more, and what is then spilled into the loop makes it wait for the next tile's loads.)  The probabilities go into the second
+// product in two bf16 parts (16 bits): a row's sums are of few large probabilities often, whose roundings no others' balance
+constexpr int PG_FEW_KEYS = 32;
+typedef float pg_floatx4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ pg_floatx4 pg_mfma16(const PkFrag& a, const PkFrag& b, const pg_floatx4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }
+// over the lanes of a row
+__device__ __forceinline__ float pg_max_row(float x) { x = pk_max_halves(x); return fmaxf(x, __shfl_xor(x, 16)); }
+__device__ __forceinline__ float pg_sum_row(float x) { x = pk_sum_halves(x); return x + __shfl_xor(x, 16); }
+
+// true: stored nothing, the tiles have to be gone over with care
+template <int HD, bool WHOLE, int BLOCKS, bool careful>
+__device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
+    constexpr int ROWS = 16 * BLOCKS, TILE = PG_FEW_KEYS * HD * 2, KS = HD / 32, DB = HD / 16, PITCH = HD + 4;
+    static_assert(2 * ROWS * (PITCH + 2) * 4 <= PG_WAVES * 2 * TILE, "two waves' sums in LDS");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, n16 = lane & 15;
+    char* smem = (char*)lds + wave * (2 * TILE);
+    const int lds_at = (int)(uint32_t)(uintptr_t)lds + wave * (2 * TILE);
+    const int G = (int)o.by_group.d;
+    const PagedSeq s_ = u.s;
+    const int R = s_.nq * G, row0 = u.tile * ROWS, shift = s_.nk - s_.nq;
+    struct Row { int q, head; bool mine; };
+    auto row_of_lane = [&](int b) __attribute__((always_inline)) {
+        int lane_ = (int)threadIdx.x & 15;
+        asm volatile("" : "+v"(lane_));
+        const int row = min(row0 + 16 * b + lane_, R - 1), q = o.by_group(row);
+        return Row{q, kvh * G + row - q * G, row0 + 16 * b + lane_ < R};
+    };
+    // the last key that all rows see, and the last that one of them may
+    const int all_see = a.tree ? shift - 1 : o.by_group(row0) + shift;
+    const int last = a.tree ? s_.nk - 1 : o.by_group(min(row0 + ROWS - 1, R - 1)) + shift;
+    const int tiles = last < 0 ? 0 : last / PG_FEW_KEYS + 1;
+    const int j0 = pg_cut(tiles, u.from, u.all) + wave, j1 = pg_cut(tiles, u.to, u.all);
+    const bf16_t* Kh = c.k + kvh * c.k_head;
+    const bf16_t* Vh = c.v + kvh * c.v_head;
+    const int32_t* table = c.table + (int64_t)u.seq * c.ld_table;
+    typedef PgGroup<HD, WHOLE> Group;
+    Group lk[2], lv[2];
+    typename Group::Pages next[2];
+    auto find = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) next[h] = Group::pages(c, o.by_page, table, j * PG_FEW_KEYS + 16 * h, s_.nk);
+    };
+    auto request = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lk[h].load(c, o.by_page, Kh, c.k_page, c.k_row, next[h], j * PG_FEW_KEYS + 16 * h, s_.nk);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lv[h].load(c, o.by_page, Vh, c.v_page, c.v_row, next[h], j * PG_FEW_KEYS + 16 * h, s_.nk);
+    };
+    // byte offsets in a tile of what a lane reads: chunk g of row n16 (chunk 4 ks + g: ^ ks << 6; rows 16 further on: + 16 rows' bytes), and with transposition the
+    // four rows 4 g .., dims 0 .. 16 (16 db ..: ^ db << 5)
+    const int vrow = 4 * g + (n16 >> 2);
+    int at_k = lds_at + n16 * (HD * 2) + ((g ^ pk_swz<HD>(n16)) << 4), at_v = lds_at + TILE + vrow * (HD * 2) + ((((n16 & 3) >> 1) ^ pk_swz<HD>(vrow)) << 4) + (n16 & 1) * 8;
+    auto read_k = [&](int h, int ks) __attribute__((always_inline)) {
+        typedef const __attribute__((address_space(3))) pk_bf16x8* ptr;
+        PkFrag f;
+        f.v = *(ptr)(uintptr_t)(uint32_t)((at_k ^ (ks << 6)) + h * 16 * HD * 2);
+        return f;
+    };
+    auto read_v = [&](int db) __attribute__((always_inline)) {
+        union { pk_bf16x4 v; uint2 u; } lo, hi;
+        lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(uintptr_t)(uint32_t)(at_v ^ (db << 5)));
+        hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((pk_trptr)(uintptr_t)(uint32_t)((at_v ^ (db << 5)) + 16 * HD * 2));
+        PkFrag f;
+        f.u = make_uint4(lo.u.x, lo.u.y, hi.u.x, hi.u.y);
+        return f;
+    };
+    PkFrag qf[BLOCKS][KS];
+    const float sc = a.scale * PK_LOG2E, slack = 8.f / sc;
+    pg_floatx4 acc[BLOCKS][DB];
+    float top[BLOCKS], topsc[BLOCKS], l[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[b][d] = pg_floatx4{0.f, 0.f, 0.f, 0.f};
+        top[b] = -INFINITY; topsc[b] = 0.f; l[b] = 0.f;
+    }
+    if (j0 < j1) {
+        find(j0);
+        request(j0);
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            const Row r = row_of_lane(b);
+            const bf16_t* qsrc = a.q + (int64_t)(s_.q0 + r.q) * a.ldq + (int64_t)r.head * HD + 8 * g;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[b][ks].u = *reinterpret_cast<const uint4*>(qsrc + 32 * ks);
+        }
+        find(min(j0 + PG_WAVES, j1 - 1));
+    }
+    lds_barrier();                       // (the sums of the piece before)
+    for (int j = j0; j < j1; j += PG_WAVES) {
+        const int kb = j * PG_FEW_KEYS;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lk[h].store(smem, h);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lv[h].store(smem + TILE, h);
+        if (j + PG_WAVES < j1) {
+            request(j + PG_WAVES);
+            find(min(j + 2 * PG_WAVES, j1 - 1));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // (a wave's own accesses to LDS are in order)
+        asm volatile("" : "+v"(at_k), "+v"(at_v));
+        pg_floatx4 s[BLOCKS][2];
+        PkFrag fk[4] = {read_k(0, 0), read_k(1, 0), read_k(0, 1), read_k(1, 1)};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+            const int ks = i >> 1, h = i & 1;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) s[b][h] = pg_mfma16(fk[i & 3], qf[b][ks], ks == 0 ? pg_floatx4{0.f, 0.f, 0.f, 0.f} : s[b][h]);
+            if (i + 4 < 2 * KS) fk[i & 3] = read_k(h, ks + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        PkFrag pf[BLOCKS], pl[BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            if (kb + PG_FEW_KEYS - 1 > all_see) {                    // (wave-uniform)
+                const uint32_t m = pg_seen(a, s_, row_of_lane(b).q, kb) >> (4 * g);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][h][e] = m & (1u << (16 * h + e)) ? s[b][h][e] : -INFINITY;
+            }
+            float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])), fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
+            mx = pg_max_row(mx);
+            // sums are rescaled when a maximum has grown by more than 2^8 times: what they and the probabilities are relative to need not be the maximum itself
+            if (__any(mx > top[b] + slack)) {
+                const float grown = fmaxf(top[b], mx), to = grown == -INFINITY ? 0.f : grown * sc;
+                const float alpha = top[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(topsc[b] - to);
+                l[b] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[b][d] *= alpha;
+                top[b] = grown;
+                topsc[b] = to;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][e >> 2][e & 3], sc, -topsc[b])), p1 = __builtin_amdgcn_exp2f(fmaf(s[b][e >> 2][(e & 3) + 1], sc, -topsc[b]));
+                l[b] += p0 + p1;
+                const uint32_t w = pack_bf16x2(p0, p1);
+                pf[b].w[e >> 1] = w;
+                pl[b].w[e >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
+            }
+        }
+        // (read two ahead: left to itself the compiler reads all first, into registers that are not there)
+        auto second = [&](bool clean) __attribute__((always_inline)) {
+            PkFrag f[2] = {read_v(0), read_v(1)};
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                if (clean) pg_clean(f[db & 1]);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    acc[b][db] = pg_mfma16(f[db & 1], pf[b], acc[b][db]);
+                    acc[b][db] = pg_mfma16(f[db & 1], pl[b], acc[b][db]);
+                }
+                if (db + 2 < DB) f[db & 1] = read_v(db + 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        if (!careful) {
+            second(false);
+        } else {
+            second(true);
+            const char* tile = smem + TILE;
+#pragma unroll 1
+            for (uint64_t keys = pg_bad_keys<HD, PG_FEW_KEYS>(tile); keys; keys &= keys - 1) {
+                const int r = __builtin_ctzll(keys);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    const bool sees = (pg_seen(a, s_, row_of_lane(b).q, kb) >> r) & 1;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(tile + r * (HD * 2) + (((2 * db + (g >> 1)) ^ pk_swz<HD>(r)) << 4) + 8 * (g & 1));
+                        const uint32_t x[4] = {v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (sees && (x[i] & 0x7F800000u) == 0x7F800000u) acc[b][db][i] += __uint_as_float(x[i]);
+                    }
+                }
+            }
+        }
+    }
+    float z = 0.f;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        float zb = 0.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) zb = fmaf(acc[b][d][e], 0.f, zb);
+        z += row_of_lane(b).mine ? zb : 0.f;
+    }
+    if (!careful && __builtin_amdgcn_readfirstlane(__syncthreads_or(!(z == 0.f)))) return true;
+    // The waves' sums, the second two to the first two and the second to the first: what they are relative to, -inf: no part, their exponentials' sum, the sums
+    float* const sums = (float*)(char*)lds;
+    float* const rel = sums + 2 * ROWS * PITCH;
+    float base[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        l[b] = pg_sum_row(l[b]);
+        base[b] = top[b] == -INFINITY && l[b] == 0.f ? -INFINITY : topsc[b];
+    }
+#pragma unroll
+    for (int half = 2; half > 0; half >>= 1) {
+        lds_barrier();
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const int row = (wave - half) * ROWS + 16 * b + n16;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) *reinterpret_cast<pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g) = acc[b][db];
+                if (g == 0) {
+                    rel[row * 2] = base[b];
+                    rel[row * 2 + 1] = l[b];
+                }
+            }
+        }
+        lds_barrier();
+        if (wave < half) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const int row = wave * ROWS + 16 * b + n16;
+                const float other = rel[row * 2], other_l = rel[row * 2 + 1], both = fmaxf(base[b], other);
+                const float f = base[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base[b] - both), g_ = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - both);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const pg_floatx4 x = *reinterpret_cast<const pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[b][db][i] = fmaf(acc[b][db][i], f, x[i] * g_);
+                }
+                l[b] = fmaf(l[b], f, other_l * g_);
+                base[b] = both;
+            }
+        }
+    }
+    if (wave != 0) return false;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        const Row r = row_of_lane(b);
+        if (!r.mine) continue;
+        if (u.slot >= 0) {
+            const int64_t to = ((int64_t)u.slot * c.n_kv + kvh) * ROWS + 16 * b + n16;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<pg_floatx4*>(o.part + to * HD + 16 * db + 4 * g) = acc[b][db];
+            if (g == 0) o.part_ml[to] = make_float2(base[b], l[b]);
+            continue;
+        }
+        const bool empty = pg_empty(a, s_, r.q);
+        const int64_t tok = s_.q0 + r.q;
+        const float f = empty ? 0.f : 1.f / l[b];
+        bf16_t* to = a.out + tok * a.ldo + (int64_t)r.head * HD + 4 * g;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            *reinterpret_cast<uint2*>(to + 16 * db) = make_uint2(pack_bf16x2(acc[b][db][0] * f, acc[b][db][1] * f), pack_bf16x2(acc[b][db][2] * f, acc[b][db][3] * f));
+        if (a.lse && g == 0) a.lse[tok * a.n_heads + r.head] = empty ? -INFINITY : (base[b] + log2f(l[b])) * PK_LN2;
+    }
+    return false;
+}
+template <int HD, bool WHOLE, int BLOCKS>
+__global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_few_kernel(PagedCache c, PagedAttention a, PgOut o) {
+    extern __shared__ __align__(1024) char pg_dynamic[];
+    const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
+    PgWalk<16 * BLOCKS> walk;
+    if (!walk.begin(c, a, o, at, G)) return;
+    do {
+        const PgUnit u = pg_uniform(walk.unit());
+        if (pg_few<HD, WHOLE, BLOCKS, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_few<HD, WHOLE, BLOCKS, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+    } while (walk.next(c, a, G));
+}
+
+// ---- pieces joined -----------------------------------------------------------------------------------------------
+// HD / 4 lanes a row.  Rows of a row tile that one workgroup has had whole are there already
+template <int HD, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAttention a, PgOut o) {
     constexpr int LANES = HD / 4;
-    const int G = (int)o.by_group.d;
-    const int64_t rows = a.total_q * a.n_heads, at_row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-    // (the lanes of a wave have one token's heads or two tokens': the sequence is looked for by all of them)
-    const int64_t row = min(at_row, rows - 1);
+    const int G = (int)o.by_group.d, lane = threadIdx.x & 63;
+    const int64_t rows = a.total_q * a.n_heads, at_row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES, row = min(at_row, rows - 1);
     const int tok = (int)(row / a.n_heads), head = (int)(row - (int64_t)tok * a.n_heads), j = threadIdx.x % LANES;
-    const int chunk = pg_share<ROWS, KEYS>(c, a, o, G);
+    const PgSeqs seqs(c, a);
+    int64_t total;
+    int shares;
+    pg_share_out<ROWS>(c, a, o, seqs, G, total, shares);
+    if (shares == 0) return;
+    // the token's sequence and the work in front of it, by all lanes for each of the wave's rows
     PagedSeq s{};
-    int seq = -1, slot = 0, per = 1, shares = 1;
-    int before = 0;
+    int64_t start = 0, before = 0;
+    bool found = false;
     for (int b = 0; b < c.n_seq; b += 64) {
-        const int lane = threadIdx.x & 63;
-        const PagedSeq mine = paged_seq(c, a.cu_q, (int)a.total_q, min(b + lane, c.n_seq - 1));
-        const int n_rows = b + lane < c.n_seq ? (int)(((uint32_t)mine.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
-        int its_per;
-        const int its_shares = pg_shares((mine.nk + KEYS - 1) / KEYS, chunk, its_per), split = its_shares > 1 ? n_rows * its_shares : 0;
-        const int splits = pk_scan(split);
+        const PagedSeq its = seqs.at(c, a, b);
+        const PgWork work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq);
+        const int64_t own = pg_before(work, work.tiles), sum = pg_scan(own) + before;
 #pragma unroll
         for (int w = 0; w < 64 / LANES; ++w) {
             const int t = __builtin_amdgcn_readlane(tok, w * LANES);
-            const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(b + lane < c.n_seq && mine.q0 <= t));
+            const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(b + lane < c.n_seq && its.q0 <= t));
             if (n == 0) continue;
-            const int q0 = __builtin_amdgcn_readlane(mine.q0, n - 1), nq = __builtin_amdgcn_readlane(mine.nq, n - 1), nk = __builtin_amdgcn_readlane(mine.nk, n - 1);
-            const int at = before + __builtin_amdgcn_readlane(splits - split, n - 1), p = __builtin_amdgcn_readlane(its_per, n - 1), sh = __builtin_amdgcn_readlane(its_shares, n - 1);
-            if (lane / LANES == w) { s = PagedSeq{q0, nq, nk}; seq = b + n - 1; slot = at; per = p; shares = sh; }
+            const int64_t at = pg_lane(sum - own, n - 1);
+            const int q0 = __builtin_amdgcn_readlane(its.q0, n - 1), nq = __builtin_amdgcn_readlane(its.nq, n - 1), nk = __builtin_amdgcn_readlane(its.nk, n - 1);
+            if (lane / LANES == w) { s = PagedSeq{q0, nq, nk}; start = at; found = true; }
         }
-        before += __builtin_amdgcn_readlane(splits, 63);
+        before = pg_lane(sum, 63);
     }
-    if (at_row >= rows || seq < 0 || tok - s.q0 >= s.nq || shares == 1) return;
-    const int kvh = o.by_group(head), q = tok - s.q0, R = s.nq * G, in = q * G + head - kvh * G, tile = in / ROWS, tiles = (R + ROWS - 1) / ROWS;
-    // the shares that its row tile sees something of
-    const int last = a.tree ? s.nk - 1 : o.by_group(min((tile + 1) * ROWS - 1, R - 1)) + s.nk - s.nq;
-    const int used = last < 0 ? 1 : (last / KEYS + per) / per;
-    if (slot + (used - 1) * tiles + tile >= o.slots) return;
-    auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(slot + i * tiles + tile) * c.n_kv + kvh) * ROWS + in - tile * ROWS; };
-    // maxima and sums by share in the lanes of the row; a share that the row sees nothing of has no part
+    if (at_row >= rows || !found || tok - s.q0 >= s.nq) return;
+    const int kvh = o.by_group(head), q = tok - s.q0, in = q * G + head - kvh * G, tile = in / ROWS;
+    const PgWork w = pg_work<ROWS>(a, s, G, true);
+    start += pg_before(w, tile);
+    // the pieces that its row tile lies in: the last one that begins at or in front of its first and of its last bit of work
+    auto piece = [&](int64_t x) { return (int)(((x + 1) * shares - 1) / total); };
+    const int p0 = piece(start), parts = min(piece(start + w.first + w.step * tile - 1), shares - 1) - p0 + 1;
+    if (parts <= 1) return;
+    // (all but the first begin in it)
+    const int first_slot = 2 * p0 + (p0 * total / shares >= start ? 0 : 1);
+    auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + in - tile * ROWS; };
+    // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none
     float top = -INFINITY, l = 0.f;
-    for (int s0 = 0; s0 < used; s0 += LANES) top = fmaxf(top, s0 + j < used ? o.part_ml[at(s0 + j)].x : -INFINITY);
+    for (int s0 = 0; s0 < parts; s0 += LANES) top = fmaxf(top, s0 + j < parts ? o.part_ml[at(s0 + j)].x : -INFINITY);
 #pragma unroll
-    for (int w = LANES / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    for (int x = LANES / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < used; s0 += LANES) {
-        const float2 m = o.part_ml[at(min(s0 + j, used - 1))];
-        const float f = s0 + j >= used ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
+    for (int s0 = 0; s0 < parts; s0 += LANES) {
+        const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
+        const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
         l += f == 0.f ? 0.f : f * m.y;
-        const int n = min(LANES, used - s0);
+        const int n = min(LANES, parts - s0);
         for (int i = 0; i < n; i += 4) {
             float4 v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, used - 1)) * HD + 4 * j);
+            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float w = __shfl(f, i + k, LANES);              // (0 from the last share on)
-                if (w != 0.f) { x.x = fmaf(w, v[k].x, x.x); x.y = fmaf(w, v[k].y, x.y); x.z = fmaf(w, v[k].z, x.z); x.w = fmaf(w, v[k].w, x.w); }
+                const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
+                if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
             }
         }
     }
 #pragma unroll
-    for (int w = LANES / 2; w > 0; w >>= 1) l += __shfl_xor(l, w);
+    for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
     const bool empty = pg_empty(a, s, q);
     const float inv = empty ? 0.f : 1.f / l;
     *reinterpret_cast<uint2*>(a.out + (int64_t)tok * a.ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
@@ -433,19 +871,21 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAtte
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
-// Workgroups wanted for each key head, and the fewest tiles of keys that a share has (it costs a workgroup's start, its sums and a launch that joins them)
-constexpr int PG_WANTED = 512, PG_LEAST = 8;
+// two workgroups to each of 256 compute units
+constexpr int PG_PLACES = 512, PG_LEAST = 256;
 
-struct PgPlan { int64_t units, row_tiles; int target, slots; };
-PgPlan pg_plan(const PagedCache& c, const PagedAttention& a, int rows, int keys, int wanted, int least) {
-    PgPlan p{};
-    const int64_t G = a.n_heads / c.n_kv, most_keys = ((int64_t)c.max_pages * c.page_size + keys - 1) / keys;
-    p.row_tiles = a.total_q * G / rows + std::min<int64_t>(c.n_seq, a.total_q);
-    p.target = std::max(1, (wanted + c.n_kv - 1) / c.n_kv);
-    // What is shared out has more tiles of keys than a share, so at most twice as many units as tiles / share; a share is all tiles / target at least
-    // (the 64 more are for sums in fp32).  And no sequence has more than its room
-    p.slots = most_keys <= least ? 0 : (int)std::min<int64_t>(2 * p.target + 64, p.row_tiles * ((most_keys + least - 1) / least));
-    p.units = (p.row_tiles + p.slots) * c.n_kv;
+struct PgLaunch { int rows; int64_t units, slots; int shares; };
+PgLaunch pg_launch_of(const PagedCache& c, const PagedAttention& a) {
+    PgLaunch p{};
+    const int64_t G = a.n_heads / c.n_kv;
+    // up to 16 and 32 rows of a sequence in the mean
+    const int64_t mean = (a.total_q * G + c.n_seq - 1) / std::max(1, c.n_seq);
+    p.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : PG_ROWS;
+    const int64_t tiles = a.total_q * G / p.rows + std::min<int64_t>(c.n_seq, a.total_q);
+    // (no sequence has more keys than its room: nothing is shared out then)
+    p.shares = (int64_t)c.max_pages * c.page_size <= PG_LEAST ? 0 : std::max(1, (PG_PLACES + c.n_kv - 1) / c.n_kv);
+    p.slots = 2LL * p.shares * c.n_kv;
+    p.units = std::max<int64_t>(tiles, p.shares) * c.n_kv;
     return p;
 }
 
@@ -470,32 +910,42 @@ hipError_t pg_launch(const PagedCache& c, const PagedAttention& a, const PgOut& 
     hipLaunchKernelGGL((paged_kernel<HD, WHOLE, fine>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
     return hipGetLastError();
 }
+template <int HD, bool WHOLE, int BLOCKS>
+hipError_t pg_launch_few(const PagedCache& c, const PagedAttention& a, const PgOut& o, int64_t units, hipStream_t st) {
+    constexpr int SMEM = PG_WAVES * 2 * PG_FEW_KEYS * HD * 2;
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = pg_lds((paged_few_kernel<HD, WHOLE, BLOCKS>), SMEM, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((paged_few_kernel<HD, WHOLE, BLOCKS>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
+    return hipGetLastError();
+}
 
 template <int HD>
 hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void* workspace, hipStream_t st) {
-    const PgPlan p = pg_plan(c, a, PG_ROWS, PG_KEYS, PG_WANTED, PG_LEAST);
-    const int64_t G = a.n_heads / c.n_kv, part_rows = (int64_t)p.slots * c.n_kv * PG_ROWS;
+    const PgLaunch p = pg_launch_of(c, a);
+    const int64_t G = a.n_heads / c.n_kv;
     float* part = static_cast<float*>(workspace);
-    const PgOut o{part, reinterpret_cast<float2*>(part + part_rows * HD), p.slots, p.target, p.slots > 0 ? PG_LEAST : 1 << 30, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
+    const PgOut o{part, reinterpret_cast<float2*>(part + p.slots * p.rows * HD), p.shares, p.shares ? PG_LEAST : 0x7FFFFFFF, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
     const int64_t blocks = (a.total_q * a.n_heads * (HD / 4) + 255) / 256;
     if (p.units >= kPackedUnits || blocks >= kPackedUnits) return hipErrorInvalidValue;
     const bool whole = c.page_size % 16 == 0, fine = a.total_q * G <= 512 * (int64_t)c.n_seq;
-    const hipError_t e = whole ? (fine ? pg_launch<HD, true, true>(c, a, o, p.units, st) : pg_launch<HD, true, false>(c, a, o, p.units, st))
+    const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true, 1>(c, a, o, p.units, st) : pg_launch_few<HD, false, 1>(c, a, o, p.units, st))
+                       : p.rows == 32 ? (whole ? pg_launch_few<HD, true, 2>(c, a, o, p.units, st) : pg_launch_few<HD, false, 2>(c, a, o, p.units, st))
+                       : whole ? (fine ? pg_launch<HD, true, true>(c, a, o, p.units, st) : pg_launch<HD, true, false>(c, a, o, p.units, st))
                                : (fine ? pg_launch<HD, false, true>(c, a, o, p.units, st) : pg_launch<HD, false, false>(c, a, o, p.units, st));
-    if (e != hipSuccess || p.slots == 0) return e;
-    hipLaunchKernelGGL((paged_join_kernel<HD, PG_ROWS, PG_KEYS>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
+    if (e != hipSuccess || p.shares == 0) return e;
+    if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
+    else if (p.rows == 32) hipLaunchKernelGGL((paged_join_kernel<HD, 32>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
+    else hipLaunchKernelGGL((paged_join_kernel<HD, PG_ROWS>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t paged_units(const PagedCache& c, const PagedAttention& a) {
-    const PgPlan p = pg_plan(c, a, PG_ROWS, PG_KEYS, PG_WANTED, PG_LEAST);
-    return std::max(p.units, (a.total_q * a.n_heads * 32 + 255) / 256);
-}
+int64_t paged_units(const PagedCache& c, const PagedAttention& a) { return std::max(pg_launch_of(c, a).units, (a.total_q * a.n_heads * 32 + 255) / 256); }
 size_t paged_workspace_bytes(const PagedCache& c, const PagedAttention& a, int head_dim) {
-    const PgPlan p = pg_plan(c, a, PG_ROWS, PG_KEYS, PG_WANTED, PG_LEAST);
-    return (size_t)p.slots * c.n_kv * PG_ROWS * (head_dim * sizeof(float) + sizeof(float2));
+    const PgLaunch p = pg_launch_of(c, a);
+    return (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_paged_attention(const PagedCache& c, const PagedAttention& a, int head_dim, void* workspace, hipStream_t st) {
