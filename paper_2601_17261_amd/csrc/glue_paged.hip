@@ -24,79 +24,57 @@ namespace {
 
 constexpr int PG_WAVES = 4;
 
-// What a launch is told: the workgroups of each key head that work may be shared out to, and the keys of a row tile that a share has at least (it costs its start, its
-// sums, and a part in the launch that joins them)
-struct PgOut { float* part; float2* part_ml; int shares, least; QuickDiv by_kv, by_group, by_page; };
+// What a launch is told: the workgroups of each key head that there are places for at once, the keys of a row tile that a piece has at least, and the keys that go over in
+// the time that sharing out costs (a piece's start, its sums, the launch that joins them)
+struct PgOut { float* part; float2* part_ml; int places, least, cost; QuickDiv by_kv, by_group, by_page; };
 
 // ---- who does what -----------------------------------------------------------------------------------------------
 // A row tile's work is about the keys that its rows see: first + t step of row tile t of a sequence, so that the work in front of one is a whole number that every
-// workgroup finds alike.  Row tiles are one workgroup's each where that leaves none of them much longer than the others' work, else the work of all of them in a row
-// is cut into equal pieces: a workgroup then has the end of one row tile, perhaps whole ones, and the beginning of another.  (A share each to 64 sequences' row tiles
-// and 512 places for them: 219 us of keys that took 175 so)
-struct PgWork { int tiles; int64_t first, step; };      // of a sequence: its row tiles, their work
+// workgroup finds alike.  Row tiles are one workgroup's each where that is about as soon done, else the work of all of them in a row is cut into equal pieces, one to
+// each place: a workgroup then has the end of one row tile, perhaps whole ones, and the beginning of another.  (64 single tokens on 200000 keys: 219 us with shares of each
+// sequence for its own, 193 so.  Sums over the lanes by __shfl_up were most of a workgroup's start, 6 us)
+struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles, the first one's work, and what each has more than the one before
 
 template <int ROWS>
 __device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there) {
     PgWork w;
     w.tiles = there ? (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
     w.step = a.tree ? 0 : (ROWS + G - 1) / G;
-    w.first = max((a.tree ? s.nk : s.nk - s.nq) + (int)w.step, 1);
+    w.first = max((a.tree ? s.nk : s.nk - s.nq + w.step), 1);
     return w;
 }
-__device__ __forceinline__ int64_t pg_before(const PgWork& w, int t) { return w.first * t + w.step * ((int64_t)t * (t - 1) / 2); }
+__device__ __forceinline__ int64_t pg_before(const PgWork& w, int t) { return (int64_t)w.first * t + (int64_t)w.step * ((int64_t)t * (t - 1) / 2); }
+__device__ __forceinline__ int pg_of(const PgWork& w, int t) { return w.first + w.step * t; }
 
 __device__ __forceinline__ int64_t pg_lane(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
 }
-// sums over the lanes up to each
+template <int CTRL>
+__device__ __forceinline__ int64_t pg_dpp(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, 0xF, 0xF, true) << 32 | (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true));
+}
+// sums over the lanes up to each (row_shr 1, 2, 4, 8 within 16 lanes; what comes from outside them is 0)
 __device__ __forceinline__ int64_t pg_scan(int64_t x) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    return x;
+    x += pg_dpp<0x111>(x);
+    x += pg_dpp<0x112>(x);
+    x += pg_dpp<0x114>(x);
+    x += pg_dpp<0x118>(x);
+    const int64_t a = pg_lane(x, 15), b = a + pg_lane(x, 31), c = b + pg_lane(x, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return x + (row == 0 ? 0 : row == 1 ? a : row == 2 ? b : c);
 }
+// the largest of the lanes' (none below 0)
 __device__ __forceinline__ int pg_max(int x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-    return __builtin_amdgcn_readfirstlane(x);
-}
-
-// the sequences 64 at a time, one to a lane; `first`: those of the first 64
-struct PgSeqs {
-    PagedSeq first;
-    __device__ __forceinline__ PgSeqs(const PagedCache& c, const PagedAttention& a) : first(load(c, a, 0)) {}
-    static __device__ __forceinline__ PagedSeq load(const PagedCache& c, const PagedAttention& a, int b) {
-        return paged_seq(c, a.cu_q, (int)a.total_q, min(b + (int)(threadIdx.x & 63), c.n_seq - 1));
-    }
-    __device__ __forceinline__ PagedSeq at(const PagedCache& c, const PagedAttention& a, int b) const { return b == 0 ? first : load(c, a, b); }
-};
-
-template <int ROWS>
-__device__ __forceinline__ void pg_share_out(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgSeqs& seqs, int G, int64_t& total, int& shares) {
-    const int lane = threadIdx.x & 63;
-    int64_t tiles = 0;
-    int longest = 0;
-    total = 0;
-    for (int b = 0; b < c.n_seq; b += 64) {
-        const PagedSeq s = seqs.at(c, a, b);
-        const PgWork w = pg_work<ROWS>(a, s, G, b + lane < c.n_seq);
-        total += pg_lane(pg_scan(pg_before(w, w.tiles)), 63);
-        tiles += pg_lane(pg_scan(w.tiles), 63);
-        longest = max(longest, pg_max(w.tiles ? s.nk : 0));
-    }
-    const int64_t wanted = min((int64_t)o.shares, (total + o.least - 1) / o.least), each = total / max(o.shares, 1) + o.least;
-    // (2^52: what a piece's number times all work still fits)
-    const bool whole = longest <= o.least || (tiles <= o.shares ? longest <= each : longest <= each / 4) || total >= (1LL << 52);
-    shares = whole ? 0 : (int)wanted;
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true));
+    return max(max(__builtin_amdgcn_readlane(x, 15), __builtin_amdgcn_readlane(x, 31)), max(__builtin_amdgcn_readlane(x, 47), __builtin_amdgcn_readlane(x, 63)));
 }
 
 // Where a piece of the work lies: a row tile, the part [from, to) of its work `all`; slot: where its sums go, -1: it is the whole row tile
-struct PgUnit { PagedSeq s; int seq, tile; int64_t from, to, all; int slot; };
+struct PgUnit { PagedSeq s; int seq, tile, from, to, all, slot; };
 __device__ __forceinline__ int pg_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t pg_uniform(int64_t x) { return (int64_t)((uint64_t)(uint32_t)pg_uniform((int)(x >> 32)) << 32 | (uint32_t)pg_uniform((int)x)); }
 // (the same in all lanes, and known to be)
 __device__ __forceinline__ PgUnit pg_uniform(const PgUnit& u) {
     return PgUnit{PagedSeq{pg_uniform(u.s.q0), pg_uniform(u.s.nq), pg_uniform(u.s.nk)}, pg_uniform(u.seq), pg_uniform(u.tile), pg_uniform(u.from), pg_uniform(u.to), pg_uniform(u.all),
@@ -107,44 +85,81 @@ __device__ __forceinline__ PgUnit pg_uniform(const PgUnit& u) {
 template <int ROWS>
 struct PgWalk {
     int64_t pos, end, start;      // work in front of what is left, and behind it; start: in front of sequence seq's row tile `tile`
-    int seq, tile, index;
+    int64_t total, each;          // of all sequences; of a piece
+    int seq, tile, index, pieces;
     bool whole, first;
     PagedSeq s;
     PgWork w;
 
+    // work in front of a piece
+    __device__ __forceinline__ int64_t begin_of(int i) const { return min(i * each, total); }
     // its place: workgroup `index` of a key head's.  false: there is nothing for it
     __device__ __forceinline__ bool begin(const PagedCache& c, const PagedAttention& a, const PgOut& o, int index_, int G) {
         const int lane = threadIdx.x & 63;
-        const PgSeqs seqs(c, a);
-        int64_t total;
-        int shares;
-        pg_share_out<ROWS>(c, a, o, seqs, G, total, shares);
+        auto load = [&](int b, PagedSeq& its, PgWork& work) __attribute__((always_inline)) {
+            its = paged_seq(c, a.cu_q, (int)a.total_q, min(b + lane, c.n_seq - 1));
+            work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq);
+        };
+        PagedSeq its;
+        PgWork work;
+        int64_t sum = 0;          // of the first 64, which need no second look
+        int tiles = 0, longest = 0, shortest = 0x7FFFFFFF;
+        total = 0;
+        for (int b = 0; b < c.n_seq; b += 64) {
+            load(b, its, work);
+            sum = pg_scan(pg_before(work, work.tiles));
+            total += pg_lane(sum, 63);
+            tiles += pk_total(work.tiles);
+            longest = max(longest, pg_max(work.tiles ? pg_of(work, work.tiles - 1) : 0));
+            shortest = min(shortest, 0x7FFFFFFF - pg_max(work.tiles ? 0x7FFFFFFF - work.first : 0));
+        }
         index = index_;
-        whole = shares == 0;
         first = true;
+        // How long row tiles take one workgroup each: the longest, or the rounds that they go in, whose last one is short where row tiles are unlike (the heavy ones come
+        // first).  2^52: what is worked out in fp64 is exact
+        pieces = (int)min((int64_t)o.places, total / max(o.least, 1) + 1);
+        const float share = (float)total / (float)pieces, rounds = (float)tiles / (float)o.places;
+        const float alike = (float)shortest / (float)longest, alone = (float)total / (float)o.places * (1.f + alike * (ceilf(rounds) / rounds - 1.f));
+        whole = fmaxf((float)longest, tiles > o.places ? alone : 0.f) <= share + (float)o.cost || o.places < 2 || total >= (1LL << 52);
+        each = (int64_t)((double)total / pieces) + 1;
         if (whole) {
+            if (index >= tiles) return false;
             pos = index;
             end = pos + 1;
         } else {
-            if (index >= shares) return false;
-            pos = index * total / shares;
-            end = (index + 1) * total / shares;
-            if (pos >= end) return false;
+            pos = begin_of(index);
+            end = begin_of(index + 1);
+            if (index >= pieces || pos >= end) return false;
+        }
+        if (whole && tiles > o.places && c.n_seq <= 64) {
+            // level by level: a sequence's last row tile, which sees most, is as many levels high as it has row tiles, the next one a level less
+            const int own = work.tiles, t = index;
+            int low = 0, high = pg_max(own);
+            while (low < high) {
+                const int mid = (low + high) >> 1;
+                if (pk_total(max(own - mid, 0)) <= t) high = mid;
+                else low = mid + 1;
+            }
+            const int place = t - pk_total(max(own - low, 0));
+            const uint64_t m = __builtin_amdgcn_ballot_w64(own >= low);
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+            take(its, __builtin_ctzll(__builtin_amdgcn_ballot_w64(own >= low && before == place)), 0, a, G);
+            tile = low - 1;
+            return true;
         }
         int64_t before = 0;
         for (int b = 0; b < c.n_seq; b += 64) {
-            const PagedSeq its = seqs.at(c, a, b);
-            const PgWork work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq);
-            const int64_t own = whole ? work.tiles : pg_before(work, work.tiles), sum = pg_scan(own) + before;
-            const uint64_t m = __builtin_amdgcn_ballot_w64(sum > pos);
+            if (c.n_seq > 64) load(b, its, work);
+            const int64_t own = whole ? (int64_t)work.tiles : pg_before(work, work.tiles);
+            if (whole) sum = pk_scan(work.tiles);
+            else if (c.n_seq > 64) sum = pg_scan(own);
+            const uint64_t m = __builtin_amdgcn_ballot_w64(before + sum > pos);
             if (m) {
                 const int src = __builtin_ctzll(m);
-                seq = b + src;
-                s = PagedSeq{__builtin_amdgcn_readlane(its.q0, src), __builtin_amdgcn_readlane(its.nq, src), __builtin_amdgcn_readlane(its.nk, src)};
-                w = pg_work<ROWS>(a, s, G, true);
-                const int64_t in = pos - (pg_lane(sum, src) - pg_lane(own, src));
+                take(its, src, b, a, G);
+                const int64_t in = pos - before - (pg_lane(sum, src) - pg_lane(own, src));
                 if (whole) {
-                    tile = w.tiles - 1 - (int)in;      // (a prompt's last rows see most: they come first)
+                    tile = w.tiles - 1 - (int)in;
                     return true;
                 }
                 // the last row tile that begins at or in front of it
@@ -158,25 +173,30 @@ struct PgWalk {
                 start = pos - (in - pg_before(w, low));
                 return true;
             }
-            before = pg_lane(sum, 63);
+            before += pg_lane(sum, 63);
         }
         return false;
+    }
+    __device__ __forceinline__ void take(const PagedSeq& its, int src, int b, const PagedAttention& a, int G) {
+        seq = b + src;
+        s = PagedSeq{__builtin_amdgcn_readlane(its.q0, src), __builtin_amdgcn_readlane(its.nq, src), __builtin_amdgcn_readlane(its.nk, src)};
+        w = pg_work<ROWS>(a, s, G, true);
     }
     __device__ __forceinline__ PgUnit unit() const {
         PgUnit u;
         u.s = s;
         u.seq = seq;
         u.tile = tile;
-        u.all = w.first + w.step * tile;
-        u.from = whole ? 0 : pos - start;
-        u.to = whole ? u.all : min(u.all, end - start);
+        u.all = pg_of(w, tile);
+        u.from = whole ? 0 : (int)(pos - start);
+        u.to = whole ? u.all : (int)min((int64_t)u.all, end - start);
         u.slot = u.from == 0 && u.to == u.all ? -1 : 2 * index + (first ? 0 : 1);
         return u;
     }
     // on to the next one
     __device__ __forceinline__ bool next(const PagedCache& c, const PagedAttention& a, int G) {
         if (whole) return false;
-        start += w.first + w.step * tile;
+        start += pg_of(w, tile);
         pos = start;
         first = false;
         if (pos >= end) return false;
@@ -191,7 +211,9 @@ struct PgWalk {
     }
 };
 // of a row tile's `tiles` tiles of keys those that a piece of its work has
-__device__ __forceinline__ int pg_cut(int tiles, int64_t part, int64_t all) { return part >= all ? tiles : (int)((tiles * part + all - 1) / all); }
+__device__ __forceinline__ int pg_cut(int tiles, int part, int all) {
+    return part >= all ? tiles : part <= 0 ? 0 : min(tiles, (int)ceil((double)tiles * part / all));
+}
 
 // The 32 keys from kb on that new token q of a sequence sees, a bit for each
 __device__ __forceinline__ uint32_t pg_seen(const PagedAttention& a, const PagedSeq& s, int q, int kb) {
@@ -342,6 +364,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     char* smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
     constexpr int TILE = PG_KEYS * HD * 2, KS = HD / 16, DB = HD / 32;
+    static_assert(PG_KEYS == 16 * PG_WAVES, "16 keys are a wave's to load");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hi = lane >> 5;
     const int G = (int)o.by_group.d;
@@ -398,8 +421,8 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     auto one_tile = [&](int j) __attribute__((always_inline)) {
         const int kb = j * PG_KEYS;
         if (kb > wlast) return;                                          // (wave-uniform)
-        const char* kt = smem + (j & 1) * (2 * TILE);
-        const PkOffsets<HD> of(off, lds_at + (j & 1) * (2 * TILE));
+        const int tile_at = (j & 1) * (2 * TILE);
+        const PkOffsets<HD> of(off, lds_at + tile_at);
         PkFrag f[4];
         auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = of.row(i & 1, i >> 1); };
         auto read_v = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(of, TILE + (i / DB) * 16 * HD * 2, i % DB, f[i & 3]); };
@@ -458,7 +481,8 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
             const int q = row_of_lane().q;
             const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
             pg_second_clean<HD, fine, 4>(of, TILE, pf, pl, acc);
-            pg_add_bad<HD>(kt + TILE, pg_bad_keys<HD, PG_KEYS>(kt + TILE), seen, acc);
+            const char* values = smem + tile_at + TILE;
+            pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
             return;
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -798,94 +822,78 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
 }
 
 // ---- pieces joined -----------------------------------------------------------------------------------------------
-// HD / 4 lanes a row.  Rows of a row tile that one workgroup has had whole are there already
+// For every border between two pieces the row tile that it lies in, if it is the first one there: the parts that the pieces have of it, joined by HD / 4 lanes a row,
+// 16 rows a workgroup
 template <int HD, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAttention a, PgOut o) {
     constexpr int LANES = HD / 4;
-    const int G = (int)o.by_group.d, lane = threadIdx.x & 63;
-    const int64_t rows = a.total_q * a.n_heads, at_row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES, row = min(at_row, rows - 1);
-    const int tok = (int)(row / a.n_heads), head = (int)(row - (int64_t)tok * a.n_heads), j = threadIdx.x % LANES;
-    const PgSeqs seqs(c, a);
-    int64_t total;
-    int shares;
-    pg_share_out<ROWS>(c, a, o, seqs, G, total, shares);
-    if (shares == 0) return;
-    // the token's sequence and the work in front of it, by all lanes for each of the wave's rows
-    PagedSeq s{};
-    int64_t start = 0, before = 0;
-    bool found = false;
-    for (int b = 0; b < c.n_seq; b += 64) {
-        const PagedSeq its = seqs.at(c, a, b);
-        const PgWork work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq);
-        const int64_t own = pg_before(work, work.tiles), sum = pg_scan(own) + before;
+    const int border = 1 + o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - (border - 1) * c.n_kv, G = (int)o.by_group.d;
+    PgWalk<ROWS> walk;
+    if (!walk.begin(c, a, o, border, G) || walk.whole) return;
+    const int64_t start = walk.start, past = start + pg_of(walk.w, walk.tile);
+    const int p0 = border - 1;
+    if (walk.pos == start || walk.begin_of(p0) > start) return;
+    // how many pieces begin in front of its end
+    int parts = 2;
+    while (p0 + parts < walk.pieces && walk.begin_of(p0 + parts) < past) ++parts;
+    // (all parts but the first begin in it)
+    const int first_slot = 2 * p0 + (walk.begin_of(p0) >= start ? 0 : 1);
+    const PagedSeq s = walk.s;
+    const int R = s.nq * G, j = threadIdx.x % LANES;
+    for (int r = blockIdx.y * 16 + threadIdx.x / LANES; r < (int)blockIdx.y * 16 + 16; r += 256 / LANES) {
+        const int in = walk.tile * ROWS + r;
+        if (in >= R) return;
+        const int q = o.by_group(in), head = kvh * G + in - q * G;
+        auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + r; };
+        // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none
+        float top = -INFINITY, l = 0.f;
+        for (int s0 = 0; s0 < parts; s0 += LANES) top = fmaxf(top, s0 + j < parts ? o.part_ml[at(s0 + j)].x : -INFINITY);
 #pragma unroll
-        for (int w = 0; w < 64 / LANES; ++w) {
-            const int t = __builtin_amdgcn_readlane(tok, w * LANES);
-            const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(b + lane < c.n_seq && its.q0 <= t));
-            if (n == 0) continue;
-            const int64_t at = pg_lane(sum - own, n - 1);
-            const int q0 = __builtin_amdgcn_readlane(its.q0, n - 1), nq = __builtin_amdgcn_readlane(its.nq, n - 1), nk = __builtin_amdgcn_readlane(its.nk, n - 1);
-            if (lane / LANES == w) { s = PagedSeq{q0, nq, nk}; start = at; found = true; }
-        }
-        before = pg_lane(sum, 63);
-    }
-    if (at_row >= rows || !found || tok - s.q0 >= s.nq) return;
-    const int kvh = o.by_group(head), q = tok - s.q0, in = q * G + head - kvh * G, tile = in / ROWS;
-    const PgWork w = pg_work<ROWS>(a, s, G, true);
-    start += pg_before(w, tile);
-    // the pieces that its row tile lies in: the last one that begins at or in front of its first and of its last bit of work
-    auto piece = [&](int64_t x) { return (int)(((x + 1) * shares - 1) / total); };
-    const int p0 = piece(start), parts = min(piece(start + w.first + w.step * tile - 1), shares - 1) - p0 + 1;
-    if (parts <= 1) return;
-    // (all but the first begin in it)
-    const int first_slot = 2 * p0 + (p0 * total / shares >= start ? 0 : 1);
-    auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + in - tile * ROWS; };
-    // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none
-    float top = -INFINITY, l = 0.f;
-    for (int s0 = 0; s0 < parts; s0 += LANES) top = fmaxf(top, s0 + j < parts ? o.part_ml[at(s0 + j)].x : -INFINITY);
+        for (int x = LANES / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = 0; s0 < parts; s0 += LANES) {
+            const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
+            const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
+            l += f == 0.f ? 0.f : f * m.y;
+            const int n = min(LANES, parts - s0);
+            for (int i = 0; i < n; i += 4) {
+                float4 v[4];
 #pragma unroll
-    for (int x = LANES / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < parts; s0 += LANES) {
-        const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
-        const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
-        l += f == 0.f ? 0.f : f * m.y;
-        const int n = min(LANES, parts - s0);
-        for (int i = 0; i < n; i += 4) {
-            float4 v[4];
+                for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
-                if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
+                for (int k = 0; k < 4; ++k) {
+                    const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
+                    if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
+                }
             }
         }
-    }
 #pragma unroll
-    for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
-    const bool empty = pg_empty(a, s, q);
-    const float inv = empty ? 0.f : 1.f / l;
-    *reinterpret_cast<uint2*>(a.out + (int64_t)tok * a.ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
-    if (a.lse && j == 0) a.lse[row] = empty ? -INFINITY : (top + log2f(l)) * PK_LN2;
+        for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
+        const bool empty = pg_empty(a, s, q);
+        const float inv = empty ? 0.f : 1.f / l;
+        const int64_t tok = s.q0 + q;
+        *reinterpret_cast<uint2*>(a.out + tok * a.ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
+        if (a.lse && j == 0) a.lse[tok * a.n_heads + head] = empty ? -INFINITY : (top + log2f(l)) * PK_LN2;
+    }
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
 // two workgroups to each of 256 compute units
 constexpr int PG_PLACES = 512, PG_LEAST = 256;
 
-struct PgLaunch { int rows; int64_t units, slots; int shares; };
+struct PgLaunch { int rows; int64_t units, slots; int places, cost; };
 PgLaunch pg_launch_of(const PagedCache& c, const PagedAttention& a) {
     PgLaunch p{};
     const int64_t G = a.n_heads / c.n_kv;
-    // up to 16 and 32 rows of a sequence in the mean
+    // by the rows of a sequence in the mean
     const int64_t mean = (a.total_q * G + c.n_seq - 1) / std::max(1, c.n_seq);
-    p.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : PG_ROWS;
+    p.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
     const int64_t tiles = a.total_q * G / p.rows + std::min<int64_t>(c.n_seq, a.total_q);
     // (no sequence has more keys than its room: nothing is shared out then)
-    p.shares = (int64_t)c.max_pages * c.page_size <= PG_LEAST ? 0 : std::max(1, (PG_PLACES + c.n_kv - 1) / c.n_kv);
-    p.slots = 2LL * p.shares * c.n_kv;
-    p.units = std::max<int64_t>(tiles, p.shares) * c.n_kv;
+    p.cost = p.rows >= 128 ? 384 : 256;
+    p.places = (int64_t)c.max_pages * c.page_size <= p.cost ? 1 : std::max(1, (PG_PLACES + c.n_kv - 1) / c.n_kv);
+    p.slots = p.places < 2 ? 0 : 2LL * p.places * c.n_kv;
+    p.units = std::max<int64_t>(tiles, p.places) * c.n_kv;
     return p;
 }
 
@@ -925,24 +933,24 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
     const PgLaunch p = pg_launch_of(c, a);
     const int64_t G = a.n_heads / c.n_kv;
     float* part = static_cast<float*>(workspace);
-    const PgOut o{part, reinterpret_cast<float2*>(part + p.slots * p.rows * HD), p.shares, p.shares ? PG_LEAST : 0x7FFFFFFF, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
-    const int64_t blocks = (a.total_q * a.n_heads * (HD / 4) + 255) / 256;
-    if (p.units >= kPackedUnits || blocks >= kPackedUnits) return hipErrorInvalidValue;
+    const PgOut o{part, reinterpret_cast<float2*>(part + p.slots * p.rows * HD), p.places, PG_LEAST, p.cost, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
+    if (p.units >= kPackedUnits) return hipErrorInvalidValue;
     const bool whole = c.page_size % 16 == 0, fine = a.total_q * G <= 512 * (int64_t)c.n_seq;
     const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true, 1>(c, a, o, p.units, st) : pg_launch_few<HD, false, 1>(c, a, o, p.units, st))
                        : p.rows == 32 ? (whole ? pg_launch_few<HD, true, 2>(c, a, o, p.units, st) : pg_launch_few<HD, false, 2>(c, a, o, p.units, st))
                        : whole ? (fine ? pg_launch<HD, true, true>(c, a, o, p.units, st) : pg_launch<HD, true, false>(c, a, o, p.units, st))
                                : (fine ? pg_launch<HD, false, true>(c, a, o, p.units, st) : pg_launch<HD, false, false>(c, a, o, p.units, st));
-    if (e != hipSuccess || p.shares == 0) return e;
-    if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
-    else if (p.rows == 32) hipLaunchKernelGGL((paged_join_kernel<HD, 32>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
-    else hipLaunchKernelGGL((paged_join_kernel<HD, PG_ROWS>), dim3((unsigned)blocks), dim3(256), 0, st, c, a, o);
+    if (e != hipSuccess || p.places < 2) return e;
+    const dim3 borders((unsigned)((p.places - 1) * c.n_kv), p.rows / 16);
+    if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), borders, dim3(256), 0, st, c, a, o);
+    else if (p.rows == 32) hipLaunchKernelGGL((paged_join_kernel<HD, 32>), borders, dim3(256), 0, st, c, a, o);
+    else hipLaunchKernelGGL((paged_join_kernel<HD, 128>), borders, dim3(256), 0, st, c, a, o);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t paged_units(const PagedCache& c, const PagedAttention& a) { return std::max(pg_launch_of(c, a).units, (a.total_q * a.n_heads * 32 + 255) / 256); }
+int64_t paged_units(const PagedCache& c, const PagedAttention& a) { return pg_launch_of(c, a).units; }
 size_t paged_workspace_bytes(const PagedCache& c, const PagedAttention& a, int head_dim) {
     const PgLaunch p = pg_launch_of(c, a);
     return (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2));
