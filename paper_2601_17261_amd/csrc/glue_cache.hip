@@ -211,7 +211,8 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
 // writes.  Entry j goes to place j + 1 and comes from a place behind that one or from it, so that no thread writes a piece that it has yet to read
 __global__ __launch_bounds__(RC_WG) void cache_keep_kernel(PagedCache c, const int32_t* __restrict__ cu_q, int64_t n, const int32_t* __restrict__ rows,
                                                            const int32_t* __restrict__ n_kept, int head_dim, QuickDiv by_page, QuickDiv by_pieces) {
-    __shared__ int64_t k_from[64], k_to[64], v_from[64], v_to[64];      // k_from: -1: stays
+    __shared__ int64_t k_from[64], k_to[64], v_from[64], v_to[64];
+    __shared__ int moves;
     const int seq = blockIdx.x;
     const PagedSeq s = paged_seq(c, cu_q, (int)n, seq);
     const int kept = min(n_kept[seq], s.nq - 1), base = s.nk - s.nq, pieces = (int)by_pieces.d;
@@ -222,7 +223,6 @@ __global__ __launch_bounds__(RC_WG) void cache_keep_kernel(PagedCache c, const i
     const int64_t* from = is_k ? k_from : v_from;
     const int64_t* to = is_k ? k_to : v_to;
     for (int j0 = 0; j0 < kept; j0 += 64) {
-        const int some = min(64, kept - j0);
         if (threadIdx.x < 64) {
             const int j = j0 + (int)threadIdx.x;
             int64_t p0 = 0, p1 = 0;
@@ -232,22 +232,28 @@ __global__ __launch_bounds__(RC_WG) void cache_keep_kernel(PagedCache c, const i
                 const int row = rows[s.q0 + j];
                 moved = row > j + 1 && row < s.nq && paged_slot(c, by_page, seq, base + row, p0, s0) && paged_slot(c, by_page, seq, base + j + 1, p1, s1);
             }
-            k_from[threadIdx.x] = moved ? p0 * c.k_page + s0 * c.k_row : -1;
-            v_from[threadIdx.x] = moved ? p0 * c.v_page + s0 * c.v_row : -1;
-            k_to[threadIdx.x] = p1 * c.k_page + s1 * c.k_row;
-            v_to[threadIdx.x] = p1 * c.v_page + s1 * c.v_row;
+            // (one behind the other: those that stay would be branches around each load, and a wait for it)
+            const uint64_t m = __builtin_amdgcn_ballot_w64(moved);
+            const int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+            if (moved) {
+                k_from[at] = p0 * c.k_page + s0 * c.k_row;
+                v_from[at] = p0 * c.v_page + s0 * c.v_row;
+                k_to[at] = p1 * c.k_page + s1 * c.k_row;
+                v_to[at] = p1 * c.v_page + s1 * c.v_row;
+            }
+            if (threadIdx.x == 0) moves = __builtin_popcountll(m);
         }
         lds_barrier();
-        if (there)
-            for (int i = 0; i < some; i += 4) {
-                uint4 v[4];
+        const int some = there ? moves : 0;
+        typedef uint32_t vec __attribute__((ext_vector_type(4)));
+        for (int i = 0; i < some; i += 4) {
+            vec v[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (i + u < some && from[i + u] >= 0) v[u] = *reinterpret_cast<const uint4*>(x + from[i + u]);
+            for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const vec*>(x + from[min(i + u, some - 1)]);
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (i + u < some && from[i + u] >= 0) *reinterpret_cast<uint4*>(x + to[i + u]) = v[u];
-            }
+            for (int u = 0; u < 4; ++u)
+                if (i + u < some) *reinterpret_cast<vec*>(x + to[i + u]) = v[u];
+        }
         lds_barrier();
     }
 }

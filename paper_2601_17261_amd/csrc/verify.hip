@@ -19,7 +19,7 @@ namespace agzo {
 
 namespace {
 
-constexpr int VF_WG = 256, VF_LEAST = 2048, VF_MOST_SEGMENTS = 256;
+constexpr int VF_WG = 256, VF_PIECE = 512, VF_LEAST = 8 * VF_WG, VF_MOST_SEGMENTS = 256;      // VF_PIECE: tokens that a wave takes at a time, each with a sum of its own
 
 __device__ __forceinline__ float vf_get(const float* p, int64_t i) { return p[i]; }
 __device__ __forceinline__ float vf_get(const bf16_t* p, int64_t i) { return bf16_to_f32(p[i]); }
@@ -127,7 +127,25 @@ __device__ __forceinline__ void vf_weights(const float (&p)[8], const float (&q)
     }
 }
 
-struct VfState { double2* sums; int4* ends; };      // [n_seq][segments]: of the weights and of p; [n_seq]
+template <int CTRL>
+__device__ __forceinline__ double vf_dpp(double x) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, 0xF, 0xF, true), __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, 0xF, 0xF, true));
+}
+// sums over the lanes up to each (row_shr 1, 2, 4, 8 within 16 lanes; what comes from outside them is 0)
+__device__ __forceinline__ double vf_upto(double x) {
+    x += vf_dpp<0x111>(x);
+    x += vf_dpp<0x112>(x);
+    x += vf_dpp<0x114>(x);
+    x += vf_dpp<0x118>(x);
+    const double a = vf_readlane(x, 15), b = a + vf_readlane(x, 31), c = b + vf_readlane(x, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return x + (row == 0 ? 0.0 : row == 1 ? a : row == 2 ? b : c);
+}
+__device__ __forceinline__ double vf_total(double x) { return vf_readlane(vf_upto(x), 63); }
+
+// What the walk leaves for the draw (in one place: a load that waits for another one is a microsecond)
+struct VfReached { int at, refused, count, rows; int64_t r0; float u; int unused; };
+struct VfState { double* sums; VfReached* reached; int pieces; };      // [n_seq][pieces]: sums of the weights; [n_seq]
 __device__ __forceinline__ void vf_rows(const VerifyArgs& a, int seq, int64_t& r0, int& rows) {
     r0 = min(max((int64_t)a.cu[seq], (int64_t)0), a.n);
     rows = (int)(min(max((int64_t)a.cu[seq + 1], r0), a.n) - r0);
@@ -136,7 +154,6 @@ __device__ __forceinline__ void vf_rows(const VerifyArgs& a, int seq, int64_t& r
 template <typename T>
 __global__ __launch_bounds__(VF_WG) void verify_sums_kernel(VerifyArgs a, VfState s, int segment) {
     extern __shared__ uint32_t vf_bits[];
-    __shared__ double2 part[VF_WG / 64];
     const int seq = blockIdx.y, seg = blockIdx.x;
     int64_t r0;
     int rows;
@@ -144,7 +161,7 @@ __global__ __launch_bounds__(VF_WG) void verify_sums_kernel(VerifyArgs a, VfStat
     if (rows == 0) {
         if (seg == 0 && threadIdx.x == 0) {
             a.n_accepted[seq] = 0;
-            s.ends[seq] = make_int4(0, 0, 0, 0);
+            s.reached[seq] = VfReached{0, 0, 0, 0, 0, 0.f, 0};
         }
         return;
     }
@@ -152,7 +169,7 @@ __global__ __launch_bounds__(VF_WG) void verify_sums_kernel(VerifyArgs a, VfStat
     if (seg == 0) {
         if (threadIdx.x == 0) {
             a.n_accepted[seq] = e.count;
-            s.ends[seq] = make_int4(e.at, e.refused, e.count, 0);
+            s.reached[seq] = VfReached{e.at, e.refused, e.count, rows, r0, a.uniforms[r0], 0};
         }
         // (the entry behind the accepted ones is the draw's)
         for (int i = e.count + (int)threadIdx.x; i < rows; i += VF_WG) {
@@ -169,122 +186,115 @@ __global__ __launch_bounds__(VF_WG) void verify_sums_kernel(VerifyArgs a, VfStat
         vf_refused(a, r0, rows, e.at, first, segment, vf_bits);
         lds_barrier();
     }
-    double sum = 0.0, all = 0.0;
-    for (int64_t i = first + 8 * threadIdx.x; i < end; i += 8 * VF_WG) {
+    for (int64_t i = first + 8 * threadIdx.x; i - 8 * (threadIdx.x & 63) < end; i += 8 * VF_WG) {      // (a wave's lanes together)
         float f[8], g[8] = {};
         vf_eight(p, i, end, f);
         if (q) vf_eight(q, i, end, g);
         double w[8];
         vf_weights(f, g, marked ? vf_bits[(i - first) >> 5] >> ((i - first) & 31) : 0, w);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) { sum += w[u]; all += vf_mass(f[u]); }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { sum += __shfl_xor(sum, o); all += __shfl_xor(all, o); }
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = make_double2(sum, all);
-    lds_barrier();
-    if (threadIdx.x == 0) {
-        double2 t = part[0];
-        for (int i = 1; i < VF_WG / 64; ++i) { t.x += part[i].x; t.y += part[i].y; }
-        s.sums[(int64_t)seq * gridDim.x + seg] = t;
+        const double sum = vf_total(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])));
+        if ((threadIdx.x & 63) == 0) s.sums[(int64_t)seq * s.pieces + i / VF_PIECE] = sum;
     }
 }
 
-// sums of the threads up to each, this one among them
-__device__ __forceinline__ double vf_scan(double x, double* red) {
+// Sums of the threads up to each, this one among them, and of all
+__device__ __forceinline__ double vf_scan(double x, double* red, double& all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
+    x = vf_upto(x);
     if (lane == 63) red[wave] = x;
     lds_barrier();
     for (int i = 0; i < wave; ++i) x += red[i];
+    all = ((red[3] + red[0]) + red[1]) + red[2];      // (as the last thread has it)
     return x;
 }
+// The first thread with `first`, VF_WG if none has, and the last one with `last`, -1 if none.  (By ballots: atomics of 256 threads on one place in LDS were 7 of the draw's 11 us)
+__device__ __forceinline__ void vf_ends(bool first, bool last, int2* red, int& from, int& to) {
+    const uint64_t f = __builtin_amdgcn_ballot_w64(first), l = __builtin_amdgcn_ballot_w64(last);
+    const int wave = threadIdx.x / 64;
+    if ((threadIdx.x & 63) == 0) red[wave] = make_int2(f ? 64 * wave + __builtin_ctzll(f) : VF_WG, l ? 64 * wave + 63 - __builtin_clzll(l) : -1);
+    lds_barrier();
+    from = min(min(red[0].x, red[1].x), min(red[2].x, red[3].x));
+    to = max(max(red[0].y, red[1].y), max(red[2].y, red[3].y));
+}
 
-// The draw: the segment that the border lies in, then the token in it.  A thread has `segment / 256` tokens, 8 and more
+// The draw: the piece that the border lies in, then the token in it, two to a thread
 template <typename T>
-__global__ __launch_bounds__(VF_WG) void verify_draw_kernel(VerifyArgs a, VfState s, int segment, int segments) {
-    extern __shared__ uint32_t vf_bits[];
-    __shared__ double red[2][VF_WG / 64];
+__global__ __launch_bounds__(VF_WG) void verify_draw_kernel(VerifyArgs a, VfState s) {
+    static_assert(VF_WG == 256 && VF_PIECE == 2 * VF_WG, "four waves, two tokens a thread");
+    __shared__ double red[3][VF_WG / 64];
+    __shared__ int2 ends[3][VF_WG / 64];
     __shared__ double before;
-    __shared__ int found, last;
+    __shared__ int piece;
+    __shared__ uint32_t bits[VF_PIECE / 32];
     const int seq = blockIdx.x, t = threadIdx.x;
-    int64_t r0;
-    int rows;
-    vf_rows(a, seq, r0, rows);
-    if (rows == 0) return;
-    const int4 e = s.ends[seq];
-    const double2 mine = t < segments ? s.sums[(int64_t)seq * segments + t] : make_double2(0.0, 0.0);
-    // (nothing left, as where the probabilities do not add up to 1: the target's own)
-    const bool own = !__syncthreads_or(mine.x > 0.0);
-    const double sum = own ? mine.y : mine.x;
-    if (t == 0) { found = 1 << 30; last = -1; }
-    const double upto = vf_scan(sum, red[0]);
-    __shared__ double total;
-    if (t == VF_WG - 1) total = upto;
-    lds_barrier();
-    const double border = (double)a.uniforms[r0] * total;
-    if (sum > 0.0) {
-        atomicMax(&last, t);
-        if (upto > border) atomicMin(&found, t);
-    }
-    lds_barrier();
-    if (last < 0) {                       // no token has any probability
-        if (t == 0) a.out_tokens[r0 + e.z] = -1;
-        return;
-    }
-    // (a border at the end or behind it: the last token that has any weight)
-    const bool behind = found == 1 << 30;
-    const int seg = behind ? last : found;
-    if (t == seg) before = upto - sum;
-    const T *p = static_cast<const T*>(a.p) + (r0 + e.x) * a.ldp, *q = a.q && e.y && !own ? static_cast<const T*>(a.q) + (r0 + e.y) * a.ldq : nullptr;
-    const int64_t first = (int64_t)seg * segment, end = min(first + segment, a.vocab);
-    const bool marked = !a.q && e.y && !own;
-    if (marked) {
-        for (int i = t; i < segment / 32; i += VF_WG) vf_bits[i] = 0;
-        lds_barrier();
-        vf_refused(a, r0, rows, e.x, first, segment, vf_bits);
-    }
-    lds_barrier();
-    if (t == 0) { found = 1 << 30; last = -1; }
-    const int per = segment / VF_WG;
-    const int64_t from = first + (int64_t)t * per;
-    auto weights = [&](int64_t i, double (&w)[8]) __attribute__((always_inline)) {
-        float f[8], g[8] = {};
-        vf_eight(p, i, end, f);
-        if (q) vf_eight(q, i, end, g);
-        vf_weights(f, g, marked ? vf_bits[(i - first) >> 5] >> ((i - first) & 31) : 0, w);
+    const VfReached e = s.reached[seq];
+    // a thread's run of pieces
+    const int per = (s.pieces + VF_WG - 1) / VF_WG, from = min(t * per, s.pieces), to = min(from + per, s.pieces);
+    const double* sums = s.sums + (int64_t)seq * s.pieces;
+    double mine = 0.0;
+    for (int i = from; i < to; ++i) mine += sums[i];
+    if (e.rows == 0) return;
+    const int64_t r0 = e.r0;
+    const T* p = static_cast<const T*>(a.p) + (r0 + e.at) * a.ldp;
+    if (t < VF_PIECE / 32) bits[t] = 0;
+    double all;
+    double upto = vf_scan(mine, red[0], all), border = (double)e.u * all;
+    int found, last;
+    vf_ends(mine > 0.0 && upto > border, mine > 0.0, ends[0], found, last);
+    // (nothing left, as where the probabilities do not add up to 1: the target's own, whose sums nobody has made)
+    const bool own = last < 0;
+    auto own_sum = [&](int i) {
+        double x = 0.0;
+        for (int64_t j = (int64_t)i * VF_PIECE; j < min((int64_t)(i + 1) * VF_PIECE, a.vocab); ++j) x += vf_mass(vf_get(p, j));
+        return x;
     };
-    double x = 0.0, w[8];
-    for (int64_t i = from; i < min(from + per, end); i += 8) {
-        weights(i, w);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x += w[u];
-    }
-    const double run = before + vf_scan(x, red[1]);
-    if (x > 0.0) {
-        atomicMax(&last, t);
-        if (!behind && run > border) atomicMin(&found, t);
-    }
-    lds_barrier();
-    // (sums in another order than the segment's: a border within 2^-50 of its end may be behind all of them)
-    const bool at_end = found == 1 << 30;
-    if (t != (at_end ? last : found)) return;
-    double so_far = run - x;
-    int64_t pick = -1;
-    for (int64_t i = from; i < min(from + per, end); i += 8) {
-        weights(i, w);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const double prior = so_far;
-            so_far += w[u];
-            if (w[u] > 0.0 && (at_end || pick < 0 || !(prior > border))) pick = i + u;
+    if (own) {
+        mine = 0.0;
+        for (int i = from; i < to; ++i) mine += own_sum(i);
+        upto = vf_scan(mine, red[1], all);
+        border = (double)e.u * all;
+        vf_ends(mine > 0.0 && upto > border, mine > 0.0, ends[1], found, last);
+        if (last < 0) {                       // no token has any probability
+            if (t == 0) a.out_tokens[r0 + e.count] = -1;
+            return;
         }
     }
-    a.out_tokens[r0 + e.z] = (int)pick;
+    // (a border at the end or behind it: the last token that has any weight)
+    const bool behind = found == VF_WG;
+    if (t == (behind ? last : found)) {
+        double so_far = upto - mine;
+        int pick = -1;
+        for (int i = from; i < to; ++i) {
+            const double x = own ? own_sum(i) : per == 1 ? mine : sums[i];
+            if (x > 0.0 && (behind || pick < 0 || !(so_far > border))) { pick = i; before = so_far; }
+            so_far += x;
+        }
+        piece = pick;
+    }
+    lds_barrier();
+    const T* q = a.q && e.refused && !own ? static_cast<const T*>(a.q) + (r0 + e.refused) * a.ldq : nullptr;
+    const int64_t first = (int64_t)piece * VF_PIECE, at = first + 2 * t;
+    double w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool there = at + i < a.vocab;
+        const double d = there ? vf_mass(vf_get(p, at + i)) - (q ? vf_mass(vf_get(q, at + i)) : 0.0) : 0.0;
+        w[i] = d > 0.0 ? d : 0.0;
+    }
+    if (!a.q && e.refused && !own) {
+        vf_refused(a, r0, e.rows, e.at, first, VF_PIECE, bits);
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if ((bits[(2 * t + i) >> 5] >> ((2 * t + i) & 31)) & 1) w[i] = 0.0;
+    }
+    const double x = w[0] + w[1], run = before + vf_scan(x, red[2], all);
+    vf_ends(!behind && x > 0.0 && run > border, x > 0.0, ends[2], found, last);
+    // (sums in another order than the piece's: a border within 2^-50 of its end may be behind all of them)
+    const bool at_end = found == VF_WG;
+    if (t != (at_end ? last : found)) return;
+    const bool second = w[0] > 0.0 && w[1] > 0.0 ? at_end || !(run - w[1] > border) : w[1] > 0.0;
+    a.out_tokens[r0 + e.count] = (int)(at + second);
 }
 
 int verify_segment(int n_seq, int64_t vocab) {
@@ -296,22 +306,19 @@ int verify_segment(int n_seq, int64_t vocab) {
 
 template <typename T>
 hipError_t launch_verify_typed(const VerifyArgs& a, void* workspace, hipStream_t st) {
-    const int segment = verify_segment(a.n_seq, a.vocab), segments = (int)((a.vocab + segment - 1) / segment);
-    const VfState s{static_cast<double2*>(workspace), reinterpret_cast<int4*>(static_cast<double2*>(workspace) + (int64_t)a.n_seq * segments)};
+    const int segment = verify_segment(a.n_seq, a.vocab), segments = (int)((a.vocab + segment - 1) / segment), pieces = (int)((a.vocab + VF_PIECE - 1) / VF_PIECE);
+    const VfState s{reinterpret_cast<double*>(static_cast<VfReached*>(workspace) + a.n_seq), static_cast<VfReached*>(workspace), pieces};
     const size_t smem = a.q ? 0 : segment / 8;
     hipLaunchKernelGGL(verify_sums_kernel<T>, dim3(segments, a.n_seq), dim3(VF_WG), smem, st, a, s, segment);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(a.n_seq), dim3(VF_WG), smem, st, a, s, segment, segments);
+    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(a.n_seq), dim3(VF_WG), 0, st, a, s);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t verify_workspace_bytes(int n_seq, int64_t vocab) {
-    const int segment = verify_segment(n_seq, vocab);
-    return (size_t)n_seq * ((vocab + segment - 1) / segment) * sizeof(double2) + (size_t)n_seq * sizeof(int4);
-}
+size_t verify_workspace_bytes(int n_seq, int64_t vocab) { return (size_t)n_seq * ((vocab + VF_PIECE - 1) / VF_PIECE * sizeof(double) + sizeof(VfReached)); }
 
 hipError_t launch_verify(const VerifyArgs& a, bool f32, void* workspace, hipStream_t st) {
     if (a.n == 0 || a.n_seq == 0) return hipSuccess;
