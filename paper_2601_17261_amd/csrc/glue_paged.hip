@@ -34,13 +34,16 @@ struct PgOut { float* part; float2* part_ml; int places, least, cost; QuickDiv b
 // each place: a workgroup then has the end of one row tile, perhaps whole ones, and the beginning of another.  (64 single tokens on 200000 keys: 219 us with shares of each
 // sequence for its own, 193 so.  Sums over the lanes by __shfl_up were most of a workgroup's start, 6 us)
 struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles, the first one's work, and what each has more than the one before
+// keys that go over in the time that a row tile's start and end take.  (Without them 15 of a prompt's short first row tiles went to one workgroup, and 2500 tokens of
+// three prompts took 352 us for 300)
+constexpr int pg_start(int rows) { return rows >= 128 ? 128 : 64; }
 
 template <int ROWS>
 __device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there) {
     PgWork w;
     w.tiles = there ? (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
     w.step = a.tree ? 0 : (ROWS + G - 1) / G;
-    w.first = max((a.tree ? s.nk : s.nk - s.nq + w.step), 1);
+    w.first = max((a.tree ? s.nk : s.nk - s.nq + w.step), 0) + pg_start(ROWS);
     return w;
 }
 __device__ __forceinline__ int64_t pg_before(const PgWork& w, int t) { return (int64_t)w.first * t + (int64_t)w.step * ((int64_t)t * (t - 1) / 2); }
@@ -291,6 +294,14 @@ struct PgGroup {
     }
 };
 
+// whether any of a workgroup's lanes has it; a barrier, before which LDS has been read.  (Not __syncthreads_or(), which counts in LDS)
+__device__ __forceinline__ bool pg_any(bool x, int* flags) {
+    const uint64_t m = __builtin_amdgcn_ballot_w64(x);
+    if ((threadIdx.x & 63) == 0) flags[threadIdx.x >> 6] = m != 0;
+    lds_barrier();
+    return __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+}
+
 // ---- with care ---------------------------------------------------------------------------------------------------
 // Values that are not finite, in a tile of KEYS values in LDS: in which keys there are any
 template <int HD, int KEYS>
@@ -511,7 +522,8 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         one_tile(j);
         if (j + 1 < j1) arrive(j + 1);
     }
-    if (!careful && __builtin_amdgcn_readfirstlane(__syncthreads_or(row_of_lane().mine && pk_not_finite(acc)))) return true;
+    __shared__ int flags[PG_WAVES];
+    if (!careful && pg_any(row_of_lane().mine && pk_not_finite(acc), flags)) return true;
     l = pk_sum_halves(l);
     const Row r = row_of_lane();
     if (u.slot >= 0) {
@@ -743,7 +755,8 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
             for (int e = 0; e < 4; ++e) zb = fmaf(acc[b][d][e], 0.f, zb);
         z += row_of_lane(b).mine ? zb : 0.f;
     }
-    if (!careful && __builtin_amdgcn_readfirstlane(__syncthreads_or(!(z == 0.f)))) return true;
+    __shared__ int flags[PG_WAVES];
+    if (!careful && pg_any(!(z == 0.f), flags)) return true;
     // The waves' sums, the second two to the first two and the second to the first: what they are relative to, -inf: no part, their exponentials' sum, the sums
     float* const sums = (float*)(char*)lds;
     float* const rel = sums + 2 * ROWS * PITCH;
