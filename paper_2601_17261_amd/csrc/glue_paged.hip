@@ -26,7 +26,8 @@ constexpr int PG_WAVES = 4;
 
 // What a launch is told: the workgroups of each key head that there are places for at once, the keys of a row tile that a piece has at least, and the keys that go over in
 // the time that sharing out costs (a piece's start, its sums, the launch that joins them)
-struct PgOut { float* part; float2* part_ml; int places, least, cost; QuickDiv by_kv, by_group, by_page; };
+struct PgCut { PagedSeq s; int tile, parts, slot, unused[2]; };      // a row tile that several workgroups have parts of, and the first one's slot; parts < 2: none
+struct PgOut { float* part; float2* part_ml; PgCut* cuts; int places, least, cost; QuickDiv by_kv, by_group, by_page; };
 
 // ---- who does what -----------------------------------------------------------------------------------------------
 // A row tile's work is about the keys that its rows see: first + t step of row tile t of a sequence, so that the work in front of one is a whole number that every
@@ -35,8 +36,8 @@ struct PgOut { float* part; float2* part_ml; int places, least, cost; QuickDiv b
 // sequence for its own, 193 so.  Sums over the lanes by __shfl_up were most of a workgroup's start, 6 us)
 struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles, the first one's work, and what each has more than the one before
 // keys that go over in the time that a row tile's start and end take.  (Without them 15 of a prompt's short first row tiles went to one workgroup, and 2500 tokens of
-// three prompts took 352 us for 300)
-constexpr int pg_start(int rows) { return rows >= 128 ? 128 : 64; }
+// three prompts took 356 us for 293)
+constexpr int pg_start(int rows) { return rows >= 128 ? 256 : 64; }
 
 template <int ROWS>
 __device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there) {
@@ -198,11 +199,10 @@ struct PgWalk {
     }
     // on to the next one
     __device__ __forceinline__ bool next(const PagedCache& c, const PagedAttention& a, int G) {
-        if (whole) return false;
+        if (whole || start + pg_of(w, tile) >= end) return false;
         start += pg_of(w, tile);
         pos = start;
         first = false;
-        if (pos >= end) return false;
         if (++tile < w.tiles) return true;
         tile = 0;
         while (++seq < c.n_seq) {
@@ -213,6 +213,21 @@ struct PgWalk {
         return false;
     }
 };
+// A workgroup's entry for the launch that joins: the row tile that it has the beginning of and not the end, its last one.  (Worked out once more there it is 3 us)
+template <int ROWS>
+__device__ __forceinline__ void pg_leave(const PgOut& o, const PgWalk<ROWS>* walk, const PgUnit* u, int index, int kvh) {
+    if (kvh != 0 || threadIdx.x != 0 || index >= o.places || o.places < 2) return;
+    PgCut cut{};
+    if (u && u->from == 0 && u->to < u->all) {
+        cut.s = u->s;
+        cut.tile = u->tile;
+        cut.slot = u->slot;
+        cut.parts = 1;
+        const int64_t past = walk->start + u->all;
+        while (index + cut.parts < walk->pieces && walk->begin_of(index + cut.parts) < past) ++cut.parts;
+    }
+    o.cuts[index] = cut;
+}
 // of a row tile's `tiles` tiles of keys those that a piece of its work has
 __device__ __forceinline__ int pg_cut(int tiles, int part, int all) {
     return part >= all ? tiles : part <= 0 ? 0 : min(tiles, (int)ceil((double)tiles * part / all));
@@ -550,11 +565,17 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
     // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
     const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
     PgWalk<PG_ROWS> walk;
-    if (!walk.begin(c, a, o, at, G)) return;
-    do {
+    if (!walk.begin(c, a, o, at, G)) {
+        pg_leave<PG_ROWS>(o, nullptr, nullptr, at, kvh);
+        return;
+    }
+    while (true) {
         const PgUnit u = pg_uniform(walk.unit());
         if (pg_forward<HD, WHOLE, fine, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_forward<HD, WHOLE, fine, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
-    } while (walk.next(c, a, G));
+        if (walk.next(c, a, G)) continue;
+        pg_leave<PG_ROWS>(o, &walk, &u, at, kvh);
+        return;
+    }
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------
@@ -827,34 +848,32 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
     extern __shared__ __align__(1024) char pg_dynamic[];
     const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
     PgWalk<16 * BLOCKS> walk;
-    if (!walk.begin(c, a, o, at, G)) return;
-    do {
+    if (!walk.begin(c, a, o, at, G)) {
+        pg_leave<16 * BLOCKS>(o, nullptr, nullptr, at, kvh);
+        return;
+    }
+    while (true) {
         const PgUnit u = pg_uniform(walk.unit());
         if (pg_few<HD, WHOLE, BLOCKS, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_few<HD, WHOLE, BLOCKS, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
-    } while (walk.next(c, a, G));
+        if (walk.next(c, a, G)) continue;
+        pg_leave<16 * BLOCKS>(o, &walk, &u, at, kvh);
+        return;
+    }
 }
 
 // ---- pieces joined -----------------------------------------------------------------------------------------------
-// For every border between two pieces the row tile that it lies in, if it is the first one there: the parts that the pieces have of it, joined by HD / 4 lanes a row,
-// 16 rows a workgroup
+// What workgroups have left of row tiles that others go on with: the parts joined by HD / 4 lanes a row, 16 rows a workgroup
 template <int HD, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAttention a, PgOut o) {
     constexpr int LANES = HD / 4;
-    const int border = 1 + o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - (border - 1) * c.n_kv, G = (int)o.by_group.d;
-    PgWalk<ROWS> walk;
-    if (!walk.begin(c, a, o, border, G) || walk.whole) return;
-    const int64_t start = walk.start, past = start + pg_of(walk.w, walk.tile);
-    const int p0 = border - 1;
-    if (walk.pos == start || walk.begin_of(p0) > start) return;
-    // how many pieces begin in front of its end
-    int parts = 2;
-    while (p0 + parts < walk.pieces && walk.begin_of(p0 + parts) < past) ++parts;
-    // (all parts but the first begin in it)
-    const int first_slot = 2 * p0 + (walk.begin_of(p0) >= start ? 0 : 1);
-    const PagedSeq s = walk.s;
+    const int p0 = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - p0 * c.n_kv, G = (int)o.by_group.d;
+    const PgCut cut = o.cuts[p0];
+    const int parts = cut.parts, first_slot = cut.slot;
+    if (parts < 2) return;
+    const PagedSeq s = cut.s;
     const int R = s.nq * G, j = threadIdx.x % LANES;
     for (int r = blockIdx.y * 16 + threadIdx.x / LANES; r < (int)blockIdx.y * 16 + 16; r += 256 / LANES) {
-        const int in = walk.tile * ROWS + r;
+        const int in = cut.tile * ROWS + r;
         if (in >= R) return;
         const int q = o.by_group(in), head = kvh * G + in - q * G;
         auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + r; };
@@ -946,7 +965,8 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
     const PgLaunch p = pg_launch_of(c, a);
     const int64_t G = a.n_heads / c.n_kv;
     float* part = static_cast<float*>(workspace);
-    const PgOut o{part, reinterpret_cast<float2*>(part + p.slots * p.rows * HD), p.places, PG_LEAST, p.cost, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
+    float2* part_ml = reinterpret_cast<float2*>(part + p.slots * p.rows * HD);
+    const PgOut o{part, part_ml, reinterpret_cast<PgCut*>(part_ml + p.slots * p.rows), p.places, PG_LEAST, p.cost, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
     if (p.units >= kPackedUnits) return hipErrorInvalidValue;
     const bool whole = c.page_size % 16 == 0, fine = a.total_q * G <= 512 * (int64_t)c.n_seq;
     const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true, 1>(c, a, o, p.units, st) : pg_launch_few<HD, false, 1>(c, a, o, p.units, st))
@@ -966,7 +986,7 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
 int64_t paged_units(const PagedCache& c, const PagedAttention& a) { return pg_launch_of(c, a).units; }
 size_t paged_workspace_bytes(const PagedCache& c, const PagedAttention& a, int head_dim) {
     const PgLaunch p = pg_launch_of(c, a);
-    return (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2));
+    return p.slots == 0 ? 0 : (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2)) + p.places * sizeof(PgCut);
 }
 
 hipError_t launch_paged_attention(const PagedCache& c, const PagedAttention& a, int head_dim, void* workspace, hipStream_t st) {
