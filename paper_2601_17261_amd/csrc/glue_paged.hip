@@ -364,8 +364,8 @@ __device__ __forceinline__ void pg_clean(PkFrag& f) {
     }
 }
 // the second product with them taken out, its fragments of 16 positions `at` on
-template <int HD, bool LOW, int N>
-__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[N], const PkFrag (&low)[N], pk_floatx16 (&acc)[HD / 32]) {
+template <int HD, int N>
+__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[N], pk_floatx16 (&acc)[HD / 32]) {
 #pragma unroll
     for (int s = 0; s < N; ++s)
 #pragma unroll
@@ -374,7 +374,6 @@ __device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, 
             pk_read_trans<HD>(o, at + s * 16 * HD * 2, db, f);
             pg_clean(f);
             acc[db] = pk_mfma(f, p[s], acc[db]);
-            if (LOW) acc[db] = pk_mfma(f, low[s], acc[db]);
         }
 }
 
@@ -382,10 +381,10 @@ __device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, 
 constexpr int PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgroup, keys of a tile
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits: the shape of attention over packed sequences, for the same reasons.
-// fine: the probabilities go into the second product in two bf16 parts (16 bits).  For few rows on many keys, whose time is the keys' reading: their sums are of few large
-// probabilities often, whose roundings no others' balance.
+// The probabilities are rounded to bf16 for the second product: in two parts, as for few rows, a result is off by 0.0017 of its norm and not 0.0023, and trees on 60000 keys
+// take 126 us and not 99
 // true: stored nothing, the tiles have to be gone over with care
-template <int HD, bool WHOLE, bool fine, bool careful>
+template <int HD, bool WHOLE, bool careful>
 __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
     char* smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
@@ -395,7 +394,10 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     const int hi = lane >> 5;
     const int G = (int)o.by_group.d;
     const PagedSeq s_ = u.s;
-    const int R = s_.nq * G, row0 = u.tile * PG_ROWS + wave * 32, shift = s_.nk - s_.nq;
+    // (which of the 32 rows are a wave's: the other way round in the second 256 workgroups, of which a compute unit has one beside one of the first, so that tiles with few
+    // rows keep all four SIMDs busy together)
+    const int block = (blockIdx.x >> 8) & 1 ? PG_WAVES - 1 - wave : wave;
+    const int R = s_.nq * G, row0 = u.tile * PG_ROWS + block * 32, shift = s_.nk - s_.nq;
     // The lane's row: its query, its head.  (Worked out where they are needed, from a lane number that the compiler does not know again: kept through the loop they
     // are spilled)
     struct Row { int q, head; bool mine; };
@@ -493,20 +495,18 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
             top = grown;
             topsc = to;
         }
-        PkFrag pf[4], pl[4];
+        PkFrag pf[4];
         // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that)
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][(e & 15) + 1], sc, -topsc));
             l += p0 + p1;
-            const uint32_t w = pack_bf16x2(p0, p1);
-            pf[e >> 3].w[(e & 7) >> 1] = w;
-            if (fine) pl[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
+            pf[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
         }
         if (careful) {
             const int q = row_of_lane().q;
             const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
-            pg_second_clean<HD, fine, 4>(of, TILE, pf, pl, acc);
+            pg_second_clean<HD, 4>(of, TILE, pf, acc);
             const char* values = smem + tile_at + TILE;
             pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
             return;
@@ -516,7 +516,6 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
 #pragma unroll
         for (int i = 0; i < 4 * DB; ++i) {
             acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
-            if (fine) acc[i % DB] = pk_mfma(f[i & 3], pl[i / DB], acc[i % DB]);
             if (i + 4 < 4 * DB) read_v(i + 4);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -543,7 +542,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     const Row r = row_of_lane();
     if (u.slot >= 0) {
         if (!r.mine) return false;
-        const int64_t to = ((int64_t)u.slot * c.n_kv + kvh) * PG_ROWS + wave * 32 + (lane & 31);
+        const int64_t to = ((int64_t)u.slot * c.n_kv + kvh) * PG_ROWS + block * 32 + (lane & 31);
         float* part = o.part + to * HD + 4 * hi;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -559,7 +558,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     if (a.lse && r.mine && hi == 0) a.lse[tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
     return false;
 }
-template <int HD, bool WHOLE, bool fine>
+template <int HD, bool WHOLE>
 __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_kernel(PagedCache c, PagedAttention a, PgOut o) {
     extern __shared__ __align__(1024) char pg_dynamic[];
     // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
@@ -571,7 +570,7 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
     }
     while (true) {
         const PgUnit u = pg_uniform(walk.unit());
-        if (pg_forward<HD, WHOLE, fine, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_forward<HD, WHOLE, fine, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        if (pg_forward<HD, WHOLE, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_forward<HD, WHOLE, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
         if (walk.next(c, a, G)) continue;
         pg_leave<PG_ROWS>(o, &walk, &u, at, kvh);
         return;
@@ -727,19 +726,29 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
                 pl[b].w[e >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
             }
         }
-        // (read two ahead: left to itself the compiler reads all first, into registers that are not there)
+        // (Read ahead so far: left to itself the compiler reads all first, into registers that are not there.  Two sums at a time: an instruction whose sum the one
+        // before makes waits for it)
         auto second = [&](bool clean) __attribute__((always_inline)) {
-            PkFrag f[2] = {read_v(0), read_v(1)};
+            PkFrag f[4] = {read_v(0), read_v(1), read_v(2), read_v(3)};
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                if (clean) pg_clean(f[db & 1]);
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    acc[b][db] = pg_mfma16(f[db & 1], pf[b], acc[b][db]);
-                    acc[b][db] = pg_mfma16(f[db & 1], pl[b], acc[b][db]);
+            for (int db = 0; db < DB; db += 2) {
+                PkFrag &f0 = f[db & 3], &f1 = f[(db + 1) & 3];
+                if (clean) {
+                    pg_clean(f0);
+                    pg_clean(f1);
                 }
-                if (db + 2 < DB) f[db & 1] = read_v(db + 2);
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b) {
+                        acc[b][db] = pg_mfma16(f0, part ? pl[b] : pf[b], acc[b][db]);
+                        acc[b][db + 1] = pg_mfma16(f1, part ? pl[b] : pf[b], acc[b][db + 1]);
+                    }
+                if (db + 4 < DB) {
+                    f0 = read_v(db + 4);
+                    f1 = read_v(db + 5);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -941,13 +950,13 @@ hipError_t pg_lds(F* f, int bytes, std::atomic<uint64_t>& done) {
     return e;
 }
 
-template <int HD, bool WHOLE, bool fine>
+template <int HD, bool WHOLE>
 hipError_t pg_launch(const PagedCache& c, const PagedAttention& a, const PgOut& o, int64_t units, hipStream_t st) {
     constexpr int SMEM = 4 * PG_KEYS * HD * 2;
     static std::atomic<uint64_t> done{0};
-    const hipError_t e = pg_lds(paged_kernel<HD, WHOLE, fine>, SMEM, done);
+    const hipError_t e = pg_lds(paged_kernel<HD, WHOLE>, SMEM, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_kernel<HD, WHOLE, fine>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
+    hipLaunchKernelGGL((paged_kernel<HD, WHOLE>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
     return hipGetLastError();
 }
 template <int HD, bool WHOLE, int BLOCKS>
@@ -968,11 +977,10 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
     float2* part_ml = reinterpret_cast<float2*>(part + p.slots * p.rows * HD);
     const PgOut o{part, part_ml, reinterpret_cast<PgCut*>(part_ml + p.slots * p.rows), p.places, PG_LEAST, p.cost, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
     if (p.units >= kPackedUnits) return hipErrorInvalidValue;
-    const bool whole = c.page_size % 16 == 0, fine = a.total_q * G <= 512 * (int64_t)c.n_seq;
+    const bool whole = c.page_size % 16 == 0;
     const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true, 1>(c, a, o, p.units, st) : pg_launch_few<HD, false, 1>(c, a, o, p.units, st))
                        : p.rows == 32 ? (whole ? pg_launch_few<HD, true, 2>(c, a, o, p.units, st) : pg_launch_few<HD, false, 2>(c, a, o, p.units, st))
-                       : whole ? (fine ? pg_launch<HD, true, true>(c, a, o, p.units, st) : pg_launch<HD, true, false>(c, a, o, p.units, st))
-                               : (fine ? pg_launch<HD, false, true>(c, a, o, p.units, st) : pg_launch<HD, false, false>(c, a, o, p.units, st));
+                       : whole ? pg_launch<HD, true>(c, a, o, p.units, st) : pg_launch<HD, false>(c, a, o, p.units, st);
     if (e != hipSuccess || p.places < 2) return e;
     const dim3 borders((unsigned)((p.places - 1) * c.n_kv), p.rows / 16);
     if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), borders, dim3(256), 0, st, c, a, o);
