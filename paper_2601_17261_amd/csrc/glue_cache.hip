@@ -136,6 +136,7 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
     extern __shared__ float2 rc_cs[];
     __shared__ int64_t k_at[RC_MOST], v_at[RC_MOST];
     __shared__ int pos[RC_MOST];
+    __shared__ __align__(16) float gain[2][HD];      // of queries and keys.  (In registers, 32 of them, three workgroups fewer fit on a compute unit)
     const int64_t tok0 = (int64_t)blockIdx.x * per_wg;
     const int count = (int)min((int64_t)per_wg, a.n - tok0);
     for (int t = threadIdx.x / 64; t < count; t += RC_WG / 64) {
@@ -153,23 +154,18 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
             pos[t] = a.positions ? a.positions[tok] : place;
         }
     }
-    __syncthreads();
+    if (NORM)
+        for (int i = threadIdx.x; i < 2 * HD; i += RC_WG) {
+            const float* of = i < HD ? a.q_gain : a.k_gain;
+            gain[i / HD][i % HD] = of ? of[i % HD] : 1.f;
+        }
+    lds_barrier();
     if (r.rot > 0) rc_angles(rc_cs, r, pos, count, 1.f);
-    __syncthreads();
+    lds_barrier();
     const int j = threadIdx.x % LANES, heads = a.n_heads + 2 * c.n_kv;
     int ia, ib;
     rc_at(j, r.rot, r.interleaved, ia, ib);
     const bool turned = j < r.rot / 16;
-    float qa[8], qb[8], ka[8], kb[8];                     // gains
-    if (NORM) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            qa[i] = a.q_gain ? a.q_gain[ia + i] : 1.f;
-            qb[i] = a.q_gain ? a.q_gain[ib + i] : 1.f;
-            ka[i] = a.k_gain ? a.k_gain[ia + i] : 1.f;
-            kb[i] = a.k_gain ? a.k_gain[ib + i] : 1.f;
-        }
-    }
     for (int th = threadIdx.x / LANES; th < count * heads; th += RC_WG / LANES) {
         const int t = by_heads(th), h = th - t * heads;
         const int64_t at = k_at[t], tok = tok0 + t;
@@ -194,10 +190,13 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
 #pragma unroll
             for (int off = LANES / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
             const float scale = rsqrtf(ss * (1.f / HD) + a.eps);
+            float ga[8], gb[8];
+            rc_load(gain[is_q ? 0 : 1] + ia, ga);
+            rc_load(gain[is_q ? 0 : 1] + ib, gb);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                f[i] *= scale * (is_q ? qa[i] : ka[i]);
-                g[i] *= scale * (is_q ? qb[i] : kb[i]);
+                f[i] *= scale * ga[i];
+                g[i] *= scale * gb[i];
             }
         }
         if (turned) rc_turn(f, g, rc_cs + t * (r.rot / 2) + 8 * j, r.interleaved);
