@@ -1641,7 +1641,8 @@ int check_cache(agzo_ctx* ctx, const agzo_paged_cache* c, int64_t n, const int32
     if (c->n_seq > 0 && (!c->k_len || !cu_q)) return fail(ctx, AGZO_EINVAL, "k_len or cu_q is NULL");
     if ((reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->k_len) | reinterpret_cast<uintptr_t>(cu_q)) & 3)
         return fail(ctx, AGZO_EINVAL, "the table, k_len or cu_q is misaligned");
-    if (n < 0 || n > (1LL << 26)) return fail(ctx, AGZO_EINVAL, "%lld new tokens", (long long)n);
+    // (launches of fewer than 2^32 threads)
+    if (n < 0 || n > (1LL << 24)) return fail(ctx, AGZO_EINVAL, "%lld new tokens", (long long)n);
     CacheLayout k, v;
     TRY(check_cache_tensor(ctx, c, "k", c->k, c->k_page, c->k_row, c->k_head, k));
     TRY(check_cache_tensor(ctx, c, "v", c->v, c->v_page, c->v_row, c->v_head, v));

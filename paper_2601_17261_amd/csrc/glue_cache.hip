@@ -80,19 +80,19 @@ __device__ __forceinline__ void rc_turn(float (&a)[8], float (&b)[8], const floa
 template <typename T>
 struct RopeSide { const T* x; int64_t ldx; T* y; int64_t ldy; int heads; };
 
+// A token a workgroup: 16384 tokens of 40 heads of 128 in 60 us, 5.5 TB/s, and in 63, 65, 69 with two, four and eight
 template <typename T>
-__global__ __launch_bounds__(RC_WG) void rope_kernel(RopeSide<T> q, RopeSide<T> k, const int32_t* __restrict__ positions, int64_t n, int per_wg, RopeArgs r, float sign,
-                                                     int head_dim, QuickDiv by_heads, QuickDiv by_lanes) {
+__global__ __launch_bounds__(RC_WG) void rope_kernel(RopeSide<T> q, RopeSide<T> k, const int32_t* __restrict__ positions, RopeArgs r, float sign, int head_dim, QuickDiv by_lanes) {
     extern __shared__ float2 rc_cs[];
-    const int64_t tok0 = (int64_t)blockIdx.x * per_wg;
-    const int count = (int)min((int64_t)per_wg, n - tok0), lanes = (int)by_lanes.d, heads = q.heads + k.heads;
-    rc_angles(rc_cs, r, positions + tok0, count, sign);
-    __syncthreads();
-    for (int item = threadIdx.x; item < count * heads * lanes; item += RC_WG) {
-        const int th = by_lanes(item), j = item - th * lanes, t = by_heads(th), h = th - t * heads;
+    const int64_t t = blockIdx.x;
+    const int lanes = (int)by_lanes.d, heads = q.heads + k.heads;
+    rc_angles(rc_cs, r, positions + t, 1, sign);
+    lds_barrier();
+    for (int item = threadIdx.x; item < heads * lanes; item += RC_WG) {
+        const int h = by_lanes(item), j = item - h * lanes;
         const bool is_q = h < q.heads;
-        const T* x = (is_q ? q.x + (tok0 + t) * q.ldx + (int64_t)h * head_dim : k.x + (tok0 + t) * k.ldx + (int64_t)(h - q.heads) * head_dim);
-        T* y = (is_q ? q.y + (tok0 + t) * q.ldy + (int64_t)h * head_dim : k.y + (tok0 + t) * k.ldy + (int64_t)(h - q.heads) * head_dim);
+        const T* x = is_q ? q.x + t * q.ldx + (int64_t)h * head_dim : k.x + t * k.ldx + (int64_t)(h - q.heads) * head_dim;
+        T* y = is_q ? q.y + t * q.ldy + (int64_t)h * head_dim : k.y + t * k.ldy + (int64_t)(h - q.heads) * head_dim;
         const bool turned = j < r.rot / 16;
         if (!turned && x == y) continue;                  // (in place)
         int ia, ib;
@@ -100,26 +100,21 @@ __global__ __launch_bounds__(RC_WG) void rope_kernel(RopeSide<T> q, RopeSide<T> 
         float a[8], b[8];
         rc_load(x + ia, a);
         rc_load(x + ib, b);
-        if (turned) rc_turn(a, b, rc_cs + t * (r.rot / 2) + 8 * j, r.interleaved);
+        if (turned) rc_turn(a, b, rc_cs + 8 * j, r.interleaved);
         rc_store(y + ia, a);
         rc_store(y + ib, b);
     }
 }
 
-// (few tokens: a workgroup each; more share a workgroup, and with it its angles' frequencies)
-int rc_tokens_per_wg(int64_t n) { return n >= 4096 ? 8 : n >= 1024 ? 2 : 1; }
-constexpr int64_t kRopeTokens = 1 << 24;      // of a launch: one of 2^32 threads and more is cut off without a word
+constexpr int64_t kRopeTokens = 1 << 23;      // of a launch: one of 2^32 threads and more is cut off without a word
 
 template <typename T>
 hipError_t launch_rope_typed(const RopeArgs& r, const RopeTensor& q, const RopeTensor& k, const int32_t* positions, int64_t n, int head_dim, bool back, hipStream_t st) {
-    const int heads = q.heads + k.heads;
-    if (n == 0 || heads == 0) return hipSuccess;
-    const int per = rc_tokens_per_wg(n);
+    if (n == 0 || q.heads + k.heads == 0) return hipSuccess;
     auto from = [](const RopeTensor& a, int64_t t) { return RopeSide<T>{static_cast<const T*>(a.x) + t * a.ldx, a.ldx, static_cast<T*>(a.y) + t * a.ldy, a.ldy, a.heads}; };
     for (int64_t t = 0; t < n; t += kRopeTokens) {
-        const int64_t some = std::min(n - t, kRopeTokens);
-        hipLaunchKernelGGL(rope_kernel<T>, dim3((unsigned)((some + per - 1) / per)), dim3(RC_WG), (size_t)per * (r.rot / 2) * sizeof(float2), st, from(q, t), from(k, t),
-                           positions + t, some, per, r, back ? -1.f : 1.f, head_dim, QuickDiv(heads), QuickDiv(head_dim / 16));
+        hipLaunchKernelGGL(rope_kernel<T>, dim3((unsigned)std::min(n - t, kRopeTokens)), dim3(RC_WG), r.rot / 2 * sizeof(float2), st, from(q, t), from(k, t), positions + t, r, back ? -1.f : 1.f,
+                           head_dim, QuickDiv(head_dim / 16));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -127,7 +122,7 @@ hipError_t launch_rope_typed(const RopeArgs& r, const RopeTensor& q, const RopeT
 }
 
 // ---- into the cache --------------------------------------------------------------------------------------------
-constexpr int RC_MOST = 8;      // tokens of a workgroup
+constexpr int RC_MOST = 2;      // tokens of a workgroup, where they are many.  (16384 tokens: 83, 81, 81 and 88 us with one, two, four and eight)
 
 // HD / 16 lanes a head; queries to their rows, keys and values to their pages
 template <int HD, bool NORM>
@@ -265,7 +260,7 @@ hipError_t launch_rope(const RopeArgs& r, bool f32, const RopeTensor& q, const R
 
 hipError_t launch_cache_append(const PagedCache& c, int head_dim, const RopeArgs& r, const CacheAppend& a, hipStream_t st) {
     if (a.n == 0 || c.n_seq == 0) return hipSuccess;
-    const int per = rc_tokens_per_wg(a.n);
+    const int per = a.n >= 1024 ? RC_MOST : 1;
     const dim3 blocks((unsigned)((a.n + per - 1) / per));
     const size_t smem = (size_t)per * (r.rot / 2) * sizeof(float2);
     const QuickDiv by_page(c.page_size), by_heads(a.n_heads + 2 * c.n_kv);
