@@ -254,21 +254,26 @@ def make_cache(k, v, table, k_len):
     """A cache in pages.  k, v: bf16 [n_pages][page_size][key heads][head_dim] of any strides, unit along the last axis; table: int32 [n_seq][pages a sequence may have], ids
     of pages; k_len: int32 [n_seq], keys that each sequence has, the new tokens of a call among them.  The tensors stay the caller's, and what they hold may change
     between calls."""
-    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+    # (a serving step makes one for each layer: what is asked of a tensor is asked once)
+    bf16, i32, shape, ks, vs = torch.bfloat16, torch.int32, k.shape, k.stride(), v.stride()
+    if k.dtype is not bf16 or v.dtype is not bf16:
         raise TypeError("k and v must be torch.bfloat16, not %s and %s" % (k.dtype, v.dtype))
-    shape, ks, vs = k.shape, k.stride(), v.stride()
-    if len(shape) != 4 or v.shape != shape or ((ks[3] != 1 or vs[3] != 1) and shape[3] > 1):
-        raise ValueError("k and v must be [n_pages][page_size][key heads][head_dim] alike, with unit stride along the last axis")
-    if table.dtype is not torch.int32 or k_len.dtype is not torch.int32:
+    if table.dtype is not i32 or k_len.dtype is not i32:
         raise TypeError("table and k_len must be torch.int32")
-    if table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1) or k_len.shape != (table.shape[0],) or not k_len.is_contiguous():
-        raise ValueError("table must be [n_seq][pages], with unit stride along the last axis, and k_len contiguous, of n_seq")
+    if v.shape != shape or len(ks) != 4 or ((ks[3] != 1 or vs[3] != 1) and shape[3] > 1):
+        raise ValueError("k and v must be [n_pages][page_size][key heads][head_dim] alike, with unit stride along the last axis")
+    n_pages, page, heads, dim = shape
+    ts = table.stride()
+    if len(ts) != 2 or k_len.dim() != 1:
+        raise ValueError("table must be [n_seq][pages], k_len [n_seq]")
+    n_seq, pages = table.shape
+    if (ts[1] != 1 and pages > 1) or k_len.shape[0] != n_seq or not k_len.is_contiguous():
+        raise ValueError("table must have unit stride along its last axis, and k_len be contiguous, of n_seq")
     device = k.get_device()
     if v.get_device() != device or table.get_device() != device or k_len.get_device() != device:
         raise ValueError("k, v, table and k_len must be on one device")
-    n_seq, pages = table.shape
-    c = AgzoPagedCache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], table.data_ptr(), table.stride(0) if n_seq > 1 else pages, k_len.data_ptr(),
-                       shape[1], pages, n_seq, shape[2], shape[3])
+    c = AgzoPagedCache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], n_pages, table.data_ptr(), ts[0] if n_seq > 1 else pages, k_len.data_ptr(),
+                       page, pages, n_seq, heads, dim)
     c._held = (k, v, table, k_len)      # (as long as the addresses are in use)
     c._device = device
     return c
