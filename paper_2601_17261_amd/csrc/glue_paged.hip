@@ -382,7 +382,7 @@ constexpr int PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgro
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits: the shape of attention over packed sequences, for the same reasons.
 // The probabilities are rounded to bf16 for the second product: in two parts, as for few rows, a result is off by 0.0017 of its norm and not 0.0023, and trees on 60000 keys
-// take 126 us and not 99
+// take 109 us and not 87
 // true: stored nothing, the tiles have to be gone over with care
 template <int HD, bool WHOLE, bool careful>
 __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
@@ -395,7 +395,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     const int G = (int)o.by_group.d;
     const PagedSeq s_ = u.s;
     // (which of the 32 rows are a wave's: the other way round in the second 256 workgroups, of which a compute unit has one beside one of the first, so that tiles with few
-    // rows keep all four SIMDs busy together)
+    // rows keep all four SIMDs busy together: trees of 48 tokens, 192 rows in tiles of 128 and 64, 102.6 -> 97.3 us)
     const int block = (blockIdx.x >> 8) & 1 ? PG_WAVES - 1 - wave : wave;
     const int R = s_.nq * G, row0 = u.tile * PG_ROWS + block * 32, shift = s_.nk - s_.nq;
     // The lane's row: its query, its head.  (Worked out where they are needed, from a lane number that the compiler does not know again: kept through the loop they
@@ -871,7 +871,10 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
 }
 
 // ---- pieces joined -----------------------------------------------------------------------------------------------
-// What workgroups have left of row tiles that others go on with: the parts joined by HD / 4 lanes a row, 16 rows a workgroup
+// What workgroups have left of row tiles that others go on with: the parts joined by HD / 4 lanes a row, a row to each, and four parts on their way at a time.  It reads what the first launch
+// has just written, fp32 sums: 32 MB where all 512 places are cut and have 128 rows.  (16 rows of 128 a workgroup, one after the other: trees on 60000 keys 93.5 us in both launches
+// and not 91; eight parts at a time: as soon)
+constexpr int pg_join_rows(int head_dim) { return 1024 / head_dim; }
 template <int HD, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAttention a, PgOut o) {
     constexpr int LANES = HD / 4;
@@ -881,41 +884,40 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAtte
     if (parts < 2) return;
     const PagedSeq s = cut.s;
     const int R = s.nq * G, j = threadIdx.x % LANES;
-    for (int r = blockIdx.y * 16 + threadIdx.x / LANES; r < (int)blockIdx.y * 16 + 16; r += 256 / LANES) {
-        const int in = cut.tile * ROWS + r;
-        if (in >= R) return;
-        const int q = o.by_group(in), head = kvh * G + in - q * G;
-        auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + r; };
-        // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none
-        float top = -INFINITY, l = 0.f;
-        for (int s0 = 0; s0 < parts; s0 += LANES) top = fmaxf(top, s0 + j < parts ? o.part_ml[at(s0 + j)].x : -INFINITY);
+    const int r = blockIdx.y * pg_join_rows(HD) + threadIdx.x / LANES;
+    const int in = cut.tile * ROWS + r;
+    if (in >= R) return;
+    const int q = o.by_group(in), head = kvh * G + in - q * G;
+    auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + r; };
+    // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none
+    float top = -INFINITY, l = 0.f;
+    for (int s0 = 0; s0 < parts; s0 += LANES) top = fmaxf(top, s0 + j < parts ? o.part_ml[at(s0 + j)].x : -INFINITY);
 #pragma unroll
-        for (int x = LANES / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s0 = 0; s0 < parts; s0 += LANES) {
-            const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
-            const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
-            l += f == 0.f ? 0.f : f * m.y;
-            const int n = min(LANES, parts - s0);
-            for (int i = 0; i < n; i += 4) {
-                float4 v[4];
+    for (int x = LANES / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < parts; s0 += LANES) {
+        const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
+        const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
+        l += f == 0.f ? 0.f : f * m.y;
+        const int n = min(LANES, parts - s0);
+        for (int i = 0; i < n; i += 4) {
+            float4 v[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
+            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
-                    if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
-                }
+            for (int k = 0; k < 4; ++k) {
+                const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
+                if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
             }
         }
-#pragma unroll
-        for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
-        const bool empty = pg_empty(a, s, q);
-        const float inv = empty ? 0.f : 1.f / l;
-        const int64_t tok = s.q0 + q;
-        *reinterpret_cast<uint2*>(a.out + tok * a.ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
-        if (a.lse && j == 0) a.lse[tok * a.n_heads + head] = empty ? -INFINITY : (top + log2f(l)) * PK_LN2;
     }
+#pragma unroll
+    for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
+    const bool empty = pg_empty(a, s, q);
+    const float inv = empty ? 0.f : 1.f / l;
+    const int64_t tok = s.q0 + q;
+    *reinterpret_cast<uint2*>(a.out + tok * a.ldo + (int64_t)head * HD + 4 * j) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
+    if (a.lse && j == 0) a.lse[tok * a.n_heads + head] = empty ? -INFINITY : (top + log2f(l)) * PK_LN2;
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
@@ -982,7 +984,7 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
                        : p.rows == 32 ? (whole ? pg_launch_few<HD, true, 2>(c, a, o, p.units, st) : pg_launch_few<HD, false, 2>(c, a, o, p.units, st))
                        : whole ? pg_launch<HD, true>(c, a, o, p.units, st) : pg_launch<HD, false>(c, a, o, p.units, st);
     if (e != hipSuccess || p.places < 2) return e;
-    const dim3 borders((unsigned)((p.places - 1) * c.n_kv), p.rows / 16);
+    const dim3 borders((unsigned)((p.places - 1) * c.n_kv), p.rows / pg_join_rows(HD));
     if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), borders, dim3(256), 0, st, c, a, o);
     else if (p.rows == 32) hipLaunchKernelGGL((paged_join_kernel<HD, 32>), borders, dim3(256), 0, st, c, a, o);
     else hipLaunchKernelGGL((paged_join_kernel<HD, 128>), borders, dim3(256), 0, st, c, a, o);
