@@ -388,7 +388,7 @@ int agzo_glue_cache_append(agzo_ctx* ctx, const agzo_paged_cache* cache, const a
  * its row (bits behind the words are not set; a token that sees itself has its own bit set).  A token that sees no place gets 0.  Keys and values that a token does not see have
  * no part in its result, whatever they are; what a page holds behind a sequence's last place is not read.  Ids in the table that are no page's are taken as the nearest.
  * lse (nullable): device fp32 [n][n_heads], log sum exp of a row's scaled scores, -inf where it sees none.  Precisions as for attention over packed sequences, the probabilities in two bf16 parts up
- * to 32 rows (n times the heads of a key head) a sequence in the mean.  Results repeat bit for bit; orders of sums go by the lengths of all sequences.
+ * to 16 rows (n times the heads of a key head) a sequence in the mean.  Results repeat bit for bit; orders of sums go by the lengths of all sequences.
  * Errors also: scale not finite or below 2^-100, n times the heads of a key head from 2^31 - 1024 on, 2^24 tiles of rows and more, q's leading dimension from 2^22 on. */
 int agzo_glue_attention_paged(agzo_ctx* ctx, const agzo_paged_cache* cache, const void* q, int64_t ldq, const int32_t* cu_q, int64_t n, int32_t n_heads, float scale, const int32_t* tree,
                               int64_t ld_tree, int32_t tree_words, void* out, int64_t ldo, float* lse);

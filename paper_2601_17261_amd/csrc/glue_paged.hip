@@ -14,6 +14,7 @@
 // What a masked place holds takes part in nothing: scores there are replaced, and where a workgroup's results are not finite it goes over its tiles once more with
 // care, with such values taken out of the products and added where they are seen.
 #include <atomic>
+#include <type_traits>
 
 #include "packed_tiles.h"
 #include "paged.h"
@@ -36,15 +37,17 @@ struct PgOut { float* part; float2* part_ml; PgCut* cuts; int places, least, cos
 // sequence for its own, 193 so.  Sums over the lanes by __shfl_up were most of a workgroup's start, 6 us)
 struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles, the first one's work, and what each has more than the one before
 // keys that go over in the time that a row tile's start and end take.  (Without them 15 of a prompt's short first row tiles went to one workgroup, and 2500 tokens of
-// three prompts took 356 us for 293)
-constexpr int pg_start(int rows) { return rows >= 128 ? 256 : 64; }
+// three prompts took 356 us for 293.)  Fewer where memory is busy: with few rows a piece's start is 4 to 5 us, in which a workgroup goes over 350 keys by itself and 80 among
+// 512 that share the memory's rate.  (256 throughout: 64 single tokens on 200000 keys 159 us for 156; 64 throughout: trees on 5600 keys 19.1 us for 16.8)
+constexpr int pg_start(int rows, bool busy) { return rows < 128 && busy ? 64 : 256; }
+constexpr int PG_BUSY = 1024;      // ... from so many keys a workgroup on
 
 template <int ROWS>
-__device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there) {
+__device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there, int start) {
     PgWork w;
     w.tiles = there ? (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
     w.step = a.tree ? 0 : (ROWS + G - 1) / G;
-    w.first = max((a.tree ? s.nk : s.nk - s.nq + w.step), 0) + pg_start(ROWS);
+    w.first = max((a.tree ? s.nk : s.nk - s.nq + w.step), 0) + start;
     return w;
 }
 __device__ __forceinline__ int64_t pg_before(const PgWork& w, int t) { return (int64_t)w.first * t + (int64_t)w.step * ((int64_t)t * (t - 1) / 2); }
@@ -90,7 +93,7 @@ template <int ROWS>
 struct PgWalk {
     int64_t pos, end, start;      // work in front of what is left, and behind it; start: in front of sequence seq's row tile `tile`
     int64_t total, each;          // of all sequences; of a piece
-    int seq, tile, index, pieces;
+    int seq, tile, index, pieces, start_cost;
     bool whole, first;
     PagedSeq s;
     PgWork w;
@@ -100,9 +103,10 @@ struct PgWalk {
     // its place: workgroup `index` of a key head's.  false: there is nothing for it
     __device__ __forceinline__ bool begin(const PagedCache& c, const PagedAttention& a, const PgOut& o, int index_, int G) {
         const int lane = threadIdx.x & 63;
+        start_cost = 0;          // (not known yet)
         auto load = [&](int b, PagedSeq& its, PgWork& work) __attribute__((always_inline)) {
             its = paged_seq(c, a.cu_q, (int)a.total_q, min(b + lane, c.n_seq - 1));
-            work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq);
+            work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq, start_cost);
         };
         PagedSeq its;
         PgWork work;
@@ -117,6 +121,12 @@ struct PgWalk {
             longest = max(longest, pg_max(work.tiles ? pg_of(work, work.tiles - 1) : 0));
             shortest = min(shortest, 0x7FFFFFFF - pg_max(work.tiles ? 0x7FFFFFFF - work.first : 0));
         }
+        start_cost = pg_start(ROWS, total >= (int64_t)o.places * PG_BUSY);
+        total += (int64_t)start_cost * tiles;
+        longest += start_cost;
+        shortest += start_cost;
+        sum += (int64_t)start_cost * pk_scan(work.tiles);
+        work.first += start_cost;
         index = index_;
         first = true;
         // How long row tiles take one workgroup each: the longest, or the rounds that they go in, whose last one is short where row tiles are unlike (the heavy ones come
@@ -184,7 +194,7 @@ struct PgWalk {
     __device__ __forceinline__ void take(const PagedSeq& its, int src, int b, const PagedAttention& a, int G) {
         seq = b + src;
         s = PagedSeq{__builtin_amdgcn_readlane(its.q0, src), __builtin_amdgcn_readlane(its.nq, src), __builtin_amdgcn_readlane(its.nk, src)};
-        w = pg_work<ROWS>(a, s, G, true);
+        w = pg_work<ROWS>(a, s, G, true, start_cost);
     }
     __device__ __forceinline__ PgUnit unit() const {
         PgUnit u;
@@ -207,7 +217,7 @@ struct PgWalk {
         tile = 0;
         while (++seq < c.n_seq) {
             s = paged_seq(c, a.cu_q, (int)a.total_q, __builtin_amdgcn_readfirstlane(seq));
-            w = pg_work<ROWS>(a, s, G, true);
+            w = pg_work<ROWS>(a, s, G, true, start_cost);
             if (w.tiles > 0) return true;
         }
         return false;
@@ -578,10 +588,10 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------
-// 32 rows and less (a single token's heads of a group, small trees): the time is the keys' reading.  Four waves that each go over tiles of 32 keys of their own, every
+// 16 rows and less (a single token's heads of a group, small trees): the time is the keys' reading.  Four waves that each go over tiles of 32 keys of their own, every
 // fourth of a workgroup's, without a barrier: a tile waits in registers (HD = 128: 16 KB a wave, 128 KB a compute unit in flight from two workgroups, where 32 KB keep
 // memory busy), goes through the wave's own LDS, and the next one is asked for before its products.  The waves' sums are joined at the end.
-// BLOCKS times 16 rows, in instructions of 16 x 16 x 32: lane n + 16 g has row n's scores of the keys 4 g + i and 16 + 4 g + i, and of its sums the dims 16 db + 4 g + i.
+// 16 rows, in instructions of 16 x 16 x 32: lane n + 16 g has row n's scores of the keys 4 g + i and 16 + 4 g + i, and of its sums the dims 16 db + 4 g + i.
 // (32 x 32 x 16 for 16 rows too are 96 registers more, and what is then spilled into the loop makes it wait for the next tile's loads.)  The probabilities go into the second
 // product in two bf16 parts (16 bits): a row's sums are of few large probabilities often, whose roundings no others' balance
 constexpr int PG_FEW_KEYS = 32;
@@ -592,9 +602,9 @@ __device__ __forceinline__ float pg_max_row(float x) { x = pk_max_halves(x); ret
 __device__ __forceinline__ float pg_sum_row(float x) { x = pk_sum_halves(x); return x + __shfl_xor(x, 16); }
 
 // true: stored nothing, the tiles have to be gone over with care
-template <int HD, bool WHOLE, int BLOCKS, bool careful>
+template <int HD, bool WHOLE, bool careful>
 __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
-    constexpr int ROWS = 16 * BLOCKS, TILE = PG_FEW_KEYS * HD * 2, KS = HD / 32, DB = HD / 16, PITCH = HD + 4;
+    constexpr int ROWS = 16, TILE = PG_FEW_KEYS * HD * 2, KS = HD / 32, DB = HD / 16, PITCH = HD + 4;
     static_assert(2 * ROWS * (PITCH + 2) * 4 <= PG_WAVES * 2 * TILE, "two waves' sums in LDS");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, n16 = lane & 15;
     char* smem = (char*)lds + wave * (2 * TILE);
@@ -603,11 +613,11 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
     const PagedSeq s_ = u.s;
     const int R = s_.nq * G, row0 = u.tile * ROWS, shift = s_.nk - s_.nq;
     struct Row { int q, head; bool mine; };
-    auto row_of_lane = [&](int b) __attribute__((always_inline)) {
+    auto row_of_lane = [&]() __attribute__((always_inline)) {
         int lane_ = (int)threadIdx.x & 15;
         asm volatile("" : "+v"(lane_));
-        const int row = min(row0 + 16 * b + lane_, R - 1), q = o.by_group(row);
-        return Row{q, kvh * G + row - q * G, row0 + 16 * b + lane_ < R};
+        const int row = min(row0 + lane_, R - 1), q = o.by_group(row);
+        return Row{q, kvh * G + row - q * G, row0 + lane_ < R};
     };
     // the last key that all rows see, and the last that one of them may
     const int all_see = a.tree ? shift - 1 : o.by_group(row0) + shift;
@@ -648,26 +658,20 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
         f.u = make_uint4(lo.u.x, lo.u.y, hi.u.x, hi.u.y);
         return f;
     };
-    PkFrag qf[BLOCKS][KS];
+    PkFrag qf[KS];
     const float sc = a.scale * PK_LOG2E, slack = 8.f / sc;
-    pg_floatx4 acc[BLOCKS][DB];
-    float top[BLOCKS], topsc[BLOCKS], l[BLOCKS];
+    pg_floatx4 acc[DB];
+    float top, topsc, l;
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[b][d] = pg_floatx4{0.f, 0.f, 0.f, 0.f};
-        top[b] = -INFINITY; topsc[b] = 0.f; l[b] = 0.f;
-    }
+    for (int d = 0; d < DB; ++d) acc[d] = pg_floatx4{0.f, 0.f, 0.f, 0.f};
+    top = -INFINITY; topsc = 0.f; l = 0.f;
     if (j0 < j1) {
         find(j0);
         request(j0);
+        const Row r = row_of_lane();
+        const bf16_t* qsrc = a.q + (int64_t)(s_.q0 + r.q) * a.ldq + (int64_t)r.head * HD + 8 * g;
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            const Row r = row_of_lane(b);
-            const bf16_t* qsrc = a.q + (int64_t)(s_.q0 + r.q) * a.ldq + (int64_t)r.head * HD + 8 * g;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[b][ks].u = *reinterpret_cast<const uint4*>(qsrc + 32 * ks);
-        }
+        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 32 * ks);
         find(min(j0 + PG_WAVES, j1 - 1));
     }
     lds_barrier();                       // (the sums of the piece before)
@@ -684,47 +688,43 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
         __builtin_amdgcn_sched_barrier(0);
         // (a wave's own accesses to LDS are in order)
         asm volatile("" : "+v"(at_k), "+v"(at_v));
-        pg_floatx4 s[BLOCKS][2];
+        pg_floatx4 s[2];
         PkFrag fk[4] = {read_k(0, 0), read_k(1, 0), read_k(0, 1), read_k(1, 1)};
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
             const int ks = i >> 1, h = i & 1;
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) s[b][h] = pg_mfma16(fk[i & 3], qf[b][ks], ks == 0 ? pg_floatx4{0.f, 0.f, 0.f, 0.f} : s[b][h]);
+            s[h] = pg_mfma16(fk[i & 3], qf[ks], ks == 0 ? pg_floatx4{0.f, 0.f, 0.f, 0.f} : s[h]);
             if (i + 4 < 2 * KS) fk[i & 3] = read_k(h, ks + 2);
             __builtin_amdgcn_sched_barrier(0);
         }
-        PkFrag pf[BLOCKS], pl[BLOCKS];
+        PkFrag pf, pl;
+        if (kb + PG_FEW_KEYS - 1 > all_see) {                    // (wave-uniform)
+            const uint32_t m = pg_seen(a, s_, row_of_lane().q, kb) >> (4 * g);
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            if (kb + PG_FEW_KEYS - 1 > all_see) {                    // (wave-uniform)
-                const uint32_t m = pg_seen(a, s_, row_of_lane(b).q, kb) >> (4 * g);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int e = 0; e < 4; ++e) s[h][e] = m & (1u << (16 * h + e)) ? s[h][e] : -INFINITY;
+        }
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        mx = pg_max_row(mx);
+        // sums are rescaled when a maximum has grown by more than 2^8 times: what they and the probabilities are relative to need not be the maximum itself
+        if (__any(mx > top + slack)) {
+            const float grown = fmaxf(top, mx), to = grown == -INFINITY ? 0.f : grown * sc;
+            const float alpha = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(topsc - to);
+            l *= alpha;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][h][e] = m & (1u << (16 * h + e)) ? s[b][h][e] : -INFINITY;
-            }
-            float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])), fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
-            mx = pg_max_row(mx);
-            // sums are rescaled when a maximum has grown by more than 2^8 times: what they and the probabilities are relative to need not be the maximum itself
-            if (__any(mx > top[b] + slack)) {
-                const float grown = fmaxf(top[b], mx), to = grown == -INFINITY ? 0.f : grown * sc;
-                const float alpha = top[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(topsc[b] - to);
-                l[b] *= alpha;
+            for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+            top = grown;
+            topsc = to;
+        }
 #pragma unroll
-                for (int d = 0; d < DB; ++d) acc[b][d] *= alpha;
-                top[b] = grown;
-                topsc[b] = to;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][e >> 2][e & 3], sc, -topsc[b])), p1 = __builtin_amdgcn_exp2f(fmaf(s[b][e >> 2][(e & 3) + 1], sc, -topsc[b]));
-                l[b] += p0 + p1;
-                const uint32_t w = pack_bf16x2(p0, p1);
-                pf[b].w[e >> 1] = w;
-                pl[b].w[e >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
-            }
+        for (int e = 0; e < 8; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][(e & 3) + 1], sc, -topsc));
+            l += p0 + p1;
+            const uint32_t w = pack_bf16x2(p0, p1);
+            pf.w[e >> 1] = w;
+            pl.w[e >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
         }
         // (Read ahead so far: left to itself the compiler reads all first, into registers that are not there.  Two sums at a time: an instruction whose sum the one
         // before makes waits for it)
@@ -739,12 +739,10 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
                     pg_clean(f1);
                 }
 #pragma unroll
-                for (int part = 0; part < 2; ++part)
-#pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) {
-                        acc[b][db] = pg_mfma16(f0, part ? pl[b] : pf[b], acc[b][db]);
-                        acc[b][db + 1] = pg_mfma16(f1, part ? pl[b] : pf[b], acc[b][db + 1]);
-                    }
+                for (int part = 0; part < 2; ++part) {
+                    acc[db] = pg_mfma16(f0, part ? pl : pf, acc[db]);
+                    acc[db + 1] = pg_mfma16(f1, part ? pl : pf, acc[db + 1]);
+                }
                 if (db + 4 < DB) {
                     f0 = read_v(db + 4);
                     f1 = read_v(db + 5);
@@ -760,120 +758,99 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
 #pragma unroll 1
             for (uint64_t keys = pg_bad_keys<HD, PG_FEW_KEYS>(tile); keys; keys &= keys - 1) {
                 const int r = __builtin_ctzll(keys);
+                const bool sees = (pg_seen(a, s_, row_of_lane().q, kb) >> r) & 1;
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    const bool sees = (pg_seen(a, s_, row_of_lane(b).q, kb) >> r) & 1;
+                for (int db = 0; db < DB; ++db) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(tile + r * (HD * 2) + (((2 * db + (g >> 1)) ^ pk_swz<HD>(r)) << 4) + 8 * (g & 1));
+                    const uint32_t x[4] = {v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u};
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        const uint2 v = *reinterpret_cast<const uint2*>(tile + r * (HD * 2) + (((2 * db + (g >> 1)) ^ pk_swz<HD>(r)) << 4) + 8 * (g & 1));
-                        const uint32_t x[4] = {v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (sees && (x[i] & 0x7F800000u) == 0x7F800000u) acc[b][db][i] += __uint_as_float(x[i]);
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        if (sees && (x[i] & 0x7F800000u) == 0x7F800000u) acc[db][i] += __uint_as_float(x[i]);
                 }
             }
         }
     }
     float z = 0.f;
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-        float zb = 0.f;
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) zb = fmaf(acc[b][d][e], 0.f, zb);
-        z += row_of_lane(b).mine ? zb : 0.f;
-    }
+        for (int e = 0; e < 4; ++e) z = fmaf(acc[d][e], 0.f, z);
     __shared__ int flags[PG_WAVES];
-    if (!careful && pg_any(!(z == 0.f), flags)) return true;
+    if (!careful && pg_any(row_of_lane().mine && !(z == 0.f), flags)) return true;
     // The waves' sums, the second two to the first two and the second to the first: what they are relative to, -inf: no part, their exponentials' sum, the sums
     float* const sums = (float*)(char*)lds;
     float* const rel = sums + 2 * ROWS * PITCH;
-    float base[BLOCKS];
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-        l[b] = pg_sum_row(l[b]);
-        base[b] = top[b] == -INFINITY && l[b] == 0.f ? -INFINITY : topsc[b];
-    }
+    l = pg_sum_row(l);
+    float base = top == -INFINITY && l == 0.f ? -INFINITY : topsc;
 #pragma unroll
     for (int half = 2; half > 0; half >>= 1) {
         lds_barrier();
         if (wave >= half && wave < 2 * half) {
+            const int row = (wave - half) * ROWS + n16;
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                const int row = (wave - half) * ROWS + 16 * b + n16;
-#pragma unroll
-                for (int db = 0; db < DB; ++db) *reinterpret_cast<pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g) = acc[b][db];
-                if (g == 0) {
-                    rel[row * 2] = base[b];
-                    rel[row * 2 + 1] = l[b];
-                }
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g) = acc[db];
+            if (g == 0) {
+                rel[row * 2] = base;
+                rel[row * 2 + 1] = l;
             }
         }
         lds_barrier();
         if (wave < half) {
+            const int row = wave * ROWS + n16;
+            const float other = rel[row * 2], other_l = rel[row * 2 + 1], both = fmaxf(base, other);
+            const float f = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - both), g_ = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - both);
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                const int row = wave * ROWS + 16 * b + n16;
-                const float other = rel[row * 2], other_l = rel[row * 2 + 1], both = fmaxf(base[b], other);
-                const float f = base[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base[b] - both), g_ = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - both);
+            for (int db = 0; db < DB; ++db) {
+                const pg_floatx4 x = *reinterpret_cast<const pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    const pg_floatx4 x = *reinterpret_cast<const pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[b][db][i] = fmaf(acc[b][db][i], f, x[i] * g_);
-                }
-                l[b] = fmaf(l[b], f, other_l * g_);
-                base[b] = both;
+                for (int i = 0; i < 4; ++i) acc[db][i] = fmaf(acc[db][i], f, x[i] * g_);
             }
+            l = fmaf(l, f, other_l * g_);
+            base = both;
         }
     }
     if (wave != 0) return false;
+    const Row r = row_of_lane();
+    if (!r.mine) return false;
+    if (u.slot >= 0) {
+        const int64_t to = ((int64_t)u.slot * c.n_kv + kvh) * ROWS + n16;
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-        const Row r = row_of_lane(b);
-        if (!r.mine) continue;
-        if (u.slot >= 0) {
-            const int64_t to = ((int64_t)u.slot * c.n_kv + kvh) * ROWS + 16 * b + n16;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) *reinterpret_cast<pg_floatx4*>(o.part + to * HD + 16 * db + 4 * g) = acc[b][db];
-            if (g == 0) o.part_ml[to] = make_float2(base[b], l[b]);
-            continue;
-        }
-        const bool empty = pg_empty(a, s_, r.q);
-        const int64_t tok = s_.q0 + r.q;
-        const float f = empty ? 0.f : 1.f / l[b];
-        bf16_t* to = a.out + tok * a.ldo + (int64_t)r.head * HD + 4 * g;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-            *reinterpret_cast<uint2*>(to + 16 * db) = make_uint2(pack_bf16x2(acc[b][db][0] * f, acc[b][db][1] * f), pack_bf16x2(acc[b][db][2] * f, acc[b][db][3] * f));
-        if (a.lse && g == 0) a.lse[tok * a.n_heads + r.head] = empty ? -INFINITY : (base[b] + log2f(l[b])) * PK_LN2;
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<pg_floatx4*>(o.part + to * HD + 16 * db + 4 * g) = acc[db];
+        if (g == 0) o.part_ml[to] = make_float2(base, l);
+        return false;
     }
+    const bool empty = pg_empty(a, s_, r.q);
+    const int64_t tok = s_.q0 + r.q;
+    const float f = empty ? 0.f : 1.f / l;
+    bf16_t* to = a.out + tok * a.ldo + (int64_t)r.head * HD + 4 * g;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        *reinterpret_cast<uint2*>(to + 16 * db) = make_uint2(pack_bf16x2(acc[db][0] * f, acc[db][1] * f), pack_bf16x2(acc[db][2] * f, acc[db][3] * f));
+    if (a.lse && g == 0) a.lse[tok * a.n_heads + r.head] = empty ? -INFINITY : (base + log2f(l)) * PK_LN2;
     return false;
 }
-template <int HD, bool WHOLE, int BLOCKS>
+template <int HD, bool WHOLE>
 __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_few_kernel(PagedCache c, PagedAttention a, PgOut o) {
     extern __shared__ __align__(1024) char pg_dynamic[];
     const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
-    PgWalk<16 * BLOCKS> walk;
+    PgWalk<16> walk;
     if (!walk.begin(c, a, o, at, G)) {
-        pg_leave<16 * BLOCKS>(o, nullptr, nullptr, at, kvh);
+        pg_leave<16>(o, nullptr, nullptr, at, kvh);
         return;
     }
     while (true) {
         const PgUnit u = pg_uniform(walk.unit());
-        if (pg_few<HD, WHOLE, BLOCKS, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_few<HD, WHOLE, BLOCKS, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        if (pg_few<HD, WHOLE, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_few<HD, WHOLE, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
         if (walk.next(c, a, G)) continue;
-        pg_leave<16 * BLOCKS>(o, &walk, &u, at, kvh);
+        pg_leave<16>(o, &walk, &u, at, kvh);
         return;
     }
 }
 
 // ---- pieces joined -----------------------------------------------------------------------------------------------
-// What workgroups have left of row tiles that others go on with: the parts joined by HD / 4 lanes a row, a row to each, and four parts on their way at a time.  It reads what the first launch
-// has just written, fp32 sums: 32 MB where all 512 places are cut and have 128 rows.  (16 rows of 128 a workgroup, one after the other: trees on 60000 keys 93.5 us in both launches
-// and not 91; eight parts at a time: as soon)
+// What workgroups have left of row tiles that others go on with: the parts joined by HD / 4 lanes a row, a row to each, and four parts on their way at a time, or eight.  It reads what the first
+// launch has just written, fp32 sums: 64 MB where all 512 places have a beginning and an end of 128 rows.  (16 rows of 128 a workgroup, one after the other: trees on 60000 keys
+// 93.5 us in both launches and not 91; four parts at a time throughout: 48 heads on two key heads, single tokens on 100000 keys 39.5 and not 38.6; eight: a prompt's piece 285 and not 283)
 constexpr int pg_join_rows(int head_dim) { return 1024 / head_dim; }
 template <int HD, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAttention a, PgOut o) {
@@ -900,16 +877,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAtte
         const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
         l += f == 0.f ? 0.f : f * m.y;
         const int n = min(LANES, parts - s0);
-        for (int i = 0; i < n; i += 4) {
-            float4 v[4];
+        auto add = [&](int i, auto count) __attribute__((always_inline)) {
+            constexpr int N = decltype(count)::value;
+            float4 v[N];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
+            for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < N; ++k) {
                 const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
                 if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
             }
-        }
+        };
+        if (parts <= 4) add(0, std::integral_constant<int, 4>());
+        else
+            for (int i = 0; i < n; i += 8) add(i, std::integral_constant<int, 8>());
     }
 #pragma unroll
     for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
@@ -928,12 +909,15 @@ struct PgLaunch { int rows; int64_t units, slots; int places, cost; };
 PgLaunch pg_launch_of(const PagedCache& c, const PagedAttention& a) {
     PgLaunch p{};
     const int64_t G = a.n_heads / c.n_kv;
-    // by the rows of a sequence in the mean
+    // By the rows of a sequence in the mean.  (The kernel of few rows with two blocks of 16, for up to 32: single tokens with 32 heads on one key head, 200000 keys, 56 us and 44 with
+    // the other, trees of 6 tokens with 4 heads on a key head 192 and 176; with 16 rows in the mean 90 in the one of few and 98 in the other, with 4 rows 156 and 170)
     const int64_t mean = (a.total_q * G + c.n_seq - 1) / std::max(1, c.n_seq);
-    p.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
+    p.rows = mean <= 16 ? 16 : 128;
     const int64_t tiles = a.total_q * G / p.rows + std::min<int64_t>(c.n_seq, a.total_q);
-    // (no sequence has more keys than its room: nothing is shared out then)
-    p.cost = p.rows >= 128 ? 384 : 256;
+    // What sharing out costs is a second piece's start, storing sums and the launch that joins them: 8 to 10 us in all.  (384 and 256 keys: 15 prompts' pieces on 3100 keys 38 us for
+    // 19, trees of 44 tokens on 1400 keys 18.7 for 14.9, the first tokens of four conversations 11.5 for 10.0; 1536 and 1024: two prompts' on 1700 keys 31 for 23.)  No sequence has
+    // more keys than its room: with less than that nothing is shared out
+    p.cost = p.rows >= 128 ? 1024 : 768;
     p.places = (int64_t)c.max_pages * c.page_size <= p.cost ? 1 : std::max(1, (PG_PLACES + c.n_kv - 1) / c.n_kv);
     p.slots = p.places < 2 ? 0 : 2LL * p.places * c.n_kv;
     p.units = std::max<int64_t>(tiles, p.places) * c.n_kv;
@@ -961,13 +945,13 @@ hipError_t pg_launch(const PagedCache& c, const PagedAttention& a, const PgOut& 
     hipLaunchKernelGGL((paged_kernel<HD, WHOLE>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
     return hipGetLastError();
 }
-template <int HD, bool WHOLE, int BLOCKS>
+template <int HD, bool WHOLE>
 hipError_t pg_launch_few(const PagedCache& c, const PagedAttention& a, const PgOut& o, int64_t units, hipStream_t st) {
     constexpr int SMEM = PG_WAVES * 2 * PG_FEW_KEYS * HD * 2;
     static std::atomic<uint64_t> done{0};
-    const hipError_t e = pg_lds((paged_few_kernel<HD, WHOLE, BLOCKS>), SMEM, done);
+    const hipError_t e = pg_lds((paged_few_kernel<HD, WHOLE>), SMEM, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_few_kernel<HD, WHOLE, BLOCKS>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
+    hipLaunchKernelGGL((paged_few_kernel<HD, WHOLE>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
     return hipGetLastError();
 }
 
@@ -980,13 +964,11 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
     const PgOut o{part, part_ml, reinterpret_cast<PgCut*>(part_ml + p.slots * p.rows), p.places, PG_LEAST, p.cost, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
     if (p.units >= kPackedUnits) return hipErrorInvalidValue;
     const bool whole = c.page_size % 16 == 0;
-    const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true, 1>(c, a, o, p.units, st) : pg_launch_few<HD, false, 1>(c, a, o, p.units, st))
-                       : p.rows == 32 ? (whole ? pg_launch_few<HD, true, 2>(c, a, o, p.units, st) : pg_launch_few<HD, false, 2>(c, a, o, p.units, st))
-                       : whole ? pg_launch<HD, true>(c, a, o, p.units, st) : pg_launch<HD, false>(c, a, o, p.units, st);
+    const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true>(c, a, o, p.units, st) : pg_launch_few<HD, false>(c, a, o, p.units, st))
+                                      : whole ? pg_launch<HD, true>(c, a, o, p.units, st) : pg_launch<HD, false>(c, a, o, p.units, st);
     if (e != hipSuccess || p.places < 2) return e;
     const dim3 borders((unsigned)((p.places - 1) * c.n_kv), p.rows / pg_join_rows(HD));
     if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), borders, dim3(256), 0, st, c, a, o);
-    else if (p.rows == 32) hipLaunchKernelGGL((paged_join_kernel<HD, 32>), borders, dim3(256), 0, st, c, a, o);
     else hipLaunchKernelGGL((paged_join_kernel<HD, 128>), borders, dim3(256), 0, st, c, a, o);
     return hipGetLastError();
 }
