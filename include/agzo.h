@@ -337,7 +337,7 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
  * h k_head on (in values; v likewise), so that heads may lie inside tokens or tokens inside heads, and k and v in one tensor.  Strides of axes of more than one index are multiples of 8, do not make
  * rows overlap, and k_row, v_row are below 2^22; k and v are 16-byte aligned.  Pages may be shared by sequences that only read them.
  * New tokens: sequence s has the rows cu_q[s] .. cu_q[s + 1] - 1 of a call (device int32 [n_seq + 1], as in packed batches), which are its last places: k_len[s] counts them too, so that row i
- * of m has the place k_len[s] - m + i.  A length outside 0 .. max_pages page_size is taken as the nearest of these.  Rows of no sequence are neither read nor written.
+ * of m has the place k_len[s] - m + i.  A length outside 0 .. max_pages page_size is taken as the nearest of these.  Rows of no sequence have no part in anything and are not written.
  * Errors of all calls: AGZO_EINVAL for NULL or misaligned tensors, a bad shape or layout (more than 1024 key heads, 2^16 sequences, 2^24 new tokens, or 2^31 - 1024 places of a sequence), outputs that
  * overlap inputs or each other (the cache counted from its first to its last value). */
 typedef struct {

@@ -12,8 +12,7 @@ namespace {
 
 constexpr int RC_WG = 256;
 
-__device__ __forceinline__ void rc_load(const bf16_t* p, float (&f)[8]) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ void rc_widen(const uint4& v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -21,6 +20,7 @@ __device__ __forceinline__ void rc_load(const bf16_t* p, float (&f)[8]) {
         f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
+__device__ __forceinline__ void rc_load(const bf16_t* p, float (&f)[8]) { rc_widen(*reinterpret_cast<const uint4*>(p), f); }
 __device__ __forceinline__ void rc_load(const float* p, float (&f)[8]) {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
@@ -122,7 +122,8 @@ hipError_t launch_rope_typed(const RopeArgs& r, const RopeTensor& q, const RopeT
 }
 
 // ---- into the cache --------------------------------------------------------------------------------------------
-constexpr int RC_MOST = 2;      // tokens of a workgroup, where they are many.  (16384 tokens: 83, 81, 81 and 88 us with one, two, four and eight)
+constexpr int RC_MOST = 2;      // tokens of a workgroup, where they are many.  (16384 tokens, 403 MB: 80, 79 and 81 us with one, two and four, 5.1 TB/s; 81 where
+// an item's values are only asked for when its turn has come)
 
 // HD / 16 lanes a head; queries to their rows, keys and values to their pages
 template <int HD, bool NORM>
@@ -133,7 +134,21 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
     __shared__ int pos[RC_MOST];
     __shared__ __align__(16) float gain[2][HD];      // of queries and keys.  (In registers, 32 of them, three workgroups fewer fit on a compute unit)
     const int64_t tok0 = (int64_t)blockIdx.x * per_wg;
-    const int count = (int)min((int64_t)per_wg, a.n - tok0);
+    const int count = (int)min((int64_t)per_wg, a.n - tok0), heads = a.n_heads + 2 * c.n_kv, items = count * heads;
+    const int j = threadIdx.x % LANES;
+    int ia, ib;
+    rc_at(j, r.rot, r.interleaved, ia, ib);
+    // A head's values, eight from ia and eight from ib on, of an item, which is a token's head: asked for while the item before is worked on, the first one's before the look-ups
+    struct Data { uint4 a, b; };
+    auto load = [&](int th) __attribute__((always_inline)) {
+        const int t = by_heads(th), h = th - t * heads;
+        const int64_t tok = tok0 + t;
+        const bf16_t* x = h < a.n_heads ? a.q + tok * a.ldq + (int64_t)h * HD
+                        : h < a.n_heads + c.n_kv ? a.k + tok * a.ldk + (int64_t)(h - a.n_heads) * HD : a.v + tok * a.ldv + (int64_t)(h - a.n_heads - c.n_kv) * HD;
+        return Data{*reinterpret_cast<const uint4*>(x + ia), *reinterpret_cast<const uint4*>(x + ib)};
+    };
+    int th = threadIdx.x / LANES;
+    Data next = load(min(th, items - 1));
     for (int t = threadIdx.x / 64; t < count; t += RC_WG / 64) {
         const int tok = (int)tok0 + t;
         PagedSeq s{};
@@ -157,27 +172,24 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
     lds_barrier();
     if (r.rot > 0) rc_angles(rc_cs, r, pos, count, 1.f);
     lds_barrier();
-    const int j = threadIdx.x % LANES, heads = a.n_heads + 2 * c.n_kv;
-    int ia, ib;
-    rc_at(j, r.rot, r.interleaved, ia, ib);
     const bool turned = j < r.rot / 16;
-    for (int th = threadIdx.x / LANES; th < count * heads; th += RC_WG / LANES) {
+    for (; th < items; th += RC_WG / LANES) {
+        const Data x = next;
+        next = load(min(th + RC_WG / LANES, items - 1));
         const int t = by_heads(th), h = th - t * heads;
         const int64_t at = k_at[t], tok = tok0 + t;
         const bool is_q = h < a.n_heads, is_k = !is_q && h < a.n_heads + c.n_kv;
         if (at == -2 || (at == -1 && !is_q)) continue;
         const int kh = is_k ? h - a.n_heads : h - a.n_heads - c.n_kv;
-        const bf16_t* x = is_q ? a.q + tok * a.ldq + (int64_t)h * HD : is_k ? a.k + tok * a.ldk + (int64_t)kh * HD : a.v + tok * a.ldv + (int64_t)kh * HD;
         bf16_t* y = is_q ? a.q_out + tok * a.ldqo + (int64_t)h * HD : is_k ? c.k + at + kh * c.k_head : c.v + v_at[t] + kh * c.v_head;
         if (!is_q && !is_k) {                             // values: as they are
-            const uint4 v0 = *reinterpret_cast<const uint4*>(x + 16 * j), v1 = *reinterpret_cast<const uint4*>(x + 16 * j + 8);
-            *reinterpret_cast<uint4*>(y + 16 * j) = v0;
-            *reinterpret_cast<uint4*>(y + 16 * j + 8) = v1;
+            *reinterpret_cast<uint4*>(y + ia) = x.a;
+            *reinterpret_cast<uint4*>(y + ib) = x.b;
             continue;
         }
         float f[8], g[8];
-        rc_load(x + ia, f);
-        rc_load(x + ib, g);
+        rc_widen(x.a, f);
+        rc_widen(x.b, g);
         if (NORM) {
             float ss = 0.f;
 #pragma unroll
