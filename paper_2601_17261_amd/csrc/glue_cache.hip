@@ -214,7 +214,8 @@ __global__ __launch_bounds__(RC_WG) void cache_append_kernel(PagedCache c, RopeA
 
 // ---- accepted tokens together ------------------------------------------------------------------------------------
 // A workgroup has one sequence and 256 of its rows' 16-byte pieces, each thread one piece of every row: a thread reads four rows ahead of what it
-// writes.  Entry j goes to place j + 1 and comes from a place behind that one or from it, so that no thread writes a piece that it has yet to read
+// writes.  Entry j goes to place j + 1 and comes from a place behind that one or from it, so that no thread writes a piece that it has yet to read.  One tree's take 2.2 us, 256 trees' 3.9:
+// the chain of loads from an entry to its row
 __global__ __launch_bounds__(RC_WG) void cache_keep_kernel(PagedCache c, const int32_t* __restrict__ cu_q, int64_t n, const int32_t* __restrict__ rows,
                                                            const int32_t* __restrict__ n_kept, int head_dim, QuickDiv by_page, QuickDiv by_pieces) {
     __shared__ int64_t k_from[64], k_to[64], v_from[64], v_to[64];

