@@ -39,7 +39,8 @@ struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles,
 // keys that go over in the time that a row tile's start and end take.  (Without them 15 of a prompt's short first row tiles went to one workgroup, and 2500 tokens of
 // three prompts took 356 us for 293.)  Fewer where memory is busy: with few rows a piece's start is 4 to 5 us, in which a workgroup goes over 350 keys by itself and 80 among
 // 512 that share the memory's rate.  (256 throughout: 64 single tokens on 200000 keys 159 us for 156; 64 throughout: trees on 5600 keys 19.1 us for 16.8)
-constexpr int pg_start(int rows, bool busy) { return rows < 128 && busy ? 64 : 256; }
+// (256 rows: 2500 tokens of three prompts 275 us with 256, 250 with 448, 255 with 640)
+constexpr int pg_start(int rows, bool busy) { return rows < 128 && busy ? 64 : rows > 128 ? 448 : 256; }
 constexpr int PG_BUSY = 1024;      // ... from so many keys a workgroup on
 
 template <int ROWS>
@@ -312,6 +313,20 @@ struct PgGroup {
             }
         }
     }
+    // ... straight to LDS, at byte `to` on
+    static __device__ __forceinline__ void direct(const PagedCache& c, const QuickDiv& by_page, const bf16_t* base, int64_t page_ld, int64_t row_ld, const Pages& p, int kg, int nk, int to) {
+        static_assert(WHOLE, "one page");
+        const int r = row_of_lane(), most = (int)c.n_pages - 1;
+        const int chunk = ((int)(threadIdx.x % (HD / 8)) ^ pk_swz<HD>(r)) << 4;
+        const int first = min(kg, nk - 1), slot = first - by_page(first) * c.page_size, left = nk - 1 - first;
+        const int64_t page = min(max(p.id[0], 0), most);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base + page * page_ld + slot * row_ld), 0, (int)0xFFFFFFFFu, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = (int)(__umul24((uint32_t)min(r + ROWS * i, left), (uint32_t)(2 * row_ld)) + (uint32_t)(chunk ^ (pk_swz<HD>(ROWS * i) << 4)));
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + i * 1024), "v"(at), "s"(rsrc) : "memory", "m0");
+        }
+    }
     // to rows 16 g .. of a tile
     __device__ __forceinline__ void store(char* tile, int g) const {
 #pragma unroll
@@ -319,12 +334,19 @@ struct PgGroup {
     }
 };
 
+// (the same in all lanes: a scalar register's)
+__device__ __forceinline__ float pg_uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
 // whether any of a workgroup's lanes has it; a barrier, before which LDS has been read.  (Not __syncthreads_or(), which counts in LDS)
+template <int WAVES>
 __device__ __forceinline__ bool pg_any(bool x, int* flags) {
     const uint64_t m = __builtin_amdgcn_ballot_w64(x);
     if ((threadIdx.x & 63) == 0) flags[threadIdx.x >> 6] = m != 0;
     lds_barrier();
-    return __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+    int of = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) of |= flags[i];
+    return __builtin_amdgcn_readfirstlane(of) != 0;
 }
 
 // ---- with care ---------------------------------------------------------------------------------------------------
@@ -390,10 +412,9 @@ __device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, 
 // ---- many rows ---------------------------------------------------------------------------------------------------
 constexpr int PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgroup, keys of a tile
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
-// waits: the shape of attention over packed sequences, for the same reasons.  2500 tokens with 4 heads on each of 8 key heads, behind and among 20001 keys, 235 GFLOP, take 265 us,
-// 890 TFLOP/s: matrix cores busy 49 % of the time, vector instructions 51 %, mostly in turn; 12 trees of 48 on 60000 keys, 253 MB, 76.
-// (Products of 16 x 16 x 32: 319 us for 283 with the join.  Eight waves of 256 rows, one half's products beside the other's exponentials by barriers: 288 for 286, trees of 64
-// tokens 145 for 159, 8000 tokens of 16 prompts 332 for 300.  A second 256 workgroups with less work, or with priority: no gain, or a loss)
+// waits: the shape of attention over packed sequences, for the same reasons.  16 trees of 30 tokens with 4 heads on each of 8 key heads, 100000 keys, 415 MB, take 110 us in both
+// launches, 3.7 TB/s; 2500 tokens behind and among 20001 keys, 235 GFLOP, 265 in this one, matrix cores busy 49 % of the time, vector instructions 51 %, mostly in turn.
+// (Products of 16 x 16 x 32: 319 us for 283 with the join.  A second 256 workgroups with less work, or with priority: no gain, or a loss)
 // The probabilities are rounded to bf16 for the second product: in two parts, as for few rows, a result is off by 0.0017 of its norm and not 0.0023, and trees on 60000 keys
 // take 109 us and not 87
 // true: stored nothing, the tiles have to be gone over with care
@@ -550,7 +571,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         if (j + 1 < j1) arrive(j + 1);
     }
     __shared__ int flags[PG_WAVES];
-    if (!careful && pg_any(row_of_lane().mine && pk_not_finite(acc), flags)) return true;
+    if (!careful && pg_any<PG_WAVES>(row_of_lane().mine && pk_not_finite(acc), flags)) return true;
     l = pk_sum_halves(l);
     const Row r = row_of_lane();
     if (u.slot >= 0) {
@@ -586,6 +607,225 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
         if (pg_forward<HD, WHOLE, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_forward<HD, WHOLE, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
         if (walk.next(c, a, G)) continue;
         pg_leave<PG_ROWS>(o, &walk, &u, at, kvh);
+        return;
+    }
+}
+
+// ---- more rows on long caches --------------------------------------------------------------------------------------
+// Eight waves of 32 rows against tiles of 64 keys, one workgroup to a compute unit.  Of a SIMD's two waves one makes products, a tile's second and the next tile's first, while the other
+// has its exponentials: the second four waves are half a tile behind, and a barrier ends each half.  Tiles go straight from memory to LDS, K's asked for by the first four waves and V's by the
+// others, three tiles ahead in rings of four (HD = 128: 96 KB on their way; a tile's place is free again before its next one is asked for, since both halves have read it a barrier
+// before).  How far loads are is waited for by their number: the compiler does not see them, and would wait for all of them in front of each read of LDS.
+// Against 128 rows with tiles through registers: 2500 tokens behind and among 20001 keys 278 -> 250 us in both launches, 940 TFLOP/s, 4096 tokens of one prompt 182 -> 168, trees of 48 tokens on 60000
+// keys 92 -> 87, of 64 on 100000 158 -> 135: keys are read by half as many row tiles.  One tile by itself takes 1.7 us and not 1.4, so that short caches are not for it (20 trees on 4200
+// keys 28 -> 33 us, two prompts' pieces on 1700 keys 23 -> 31)
+constexpr int PG_WIDE = 8;
+template <int HD, bool careful>
+__device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
+    char* smem = (char*)lds;
+    const int lds_at = (int)(uint32_t)(uintptr_t)lds;
+    constexpr int ROWS = 32 * PG_WIDE, TILE = PG_KEYS * HD * 2, KS = HD / 16, DB = HD / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hi = lane >> 5, late = wave >> 2, part16 = wave & 3;
+    const int G = (int)o.by_group.d;
+    const PagedSeq s_ = u.s;
+    const int R = s_.nq * G, row0 = u.tile * ROWS + wave * 32, shift = s_.nk - s_.nq;
+    struct Row { int q, head; bool mine; };
+    auto row_of_lane = [&]() __attribute__((always_inline)) {
+        int lane_ = (int)threadIdx.x & 31;
+        asm volatile("" : "+v"(lane_));
+        const int row = min(row0 + lane_, R - 1), q = o.by_group(row);
+        return Row{q, kvh * G + row - q * G, row0 + lane_ < R};
+    };
+    const int wfirst = a.tree ? shift - 1 : o.by_group(min(row0, R - 1)) + shift;
+    const int wlast = row0 >= R ? -1 : a.tree ? s_.nk - 1 : o.by_group(min(row0 + 31, R - 1)) + shift;
+    const int last = a.tree ? s_.nk - 1 : o.by_group(min((u.tile + 1) * ROWS - 1, R - 1)) + shift;
+    const int tiles = last < 0 ? 0 : last / PG_KEYS + 1;
+    const int j0 = pg_cut(tiles, u.from, u.all), j1 = pg_cut(tiles, u.to, u.all);
+    const bf16_t* base = late ? c.v + kvh * c.v_head : c.k + kvh * c.k_head;
+    const int64_t page_ld = late ? c.v_page : c.k_page, row_ld = late ? c.v_row : c.k_row;
+    const int32_t* table = c.table + (int64_t)u.seq * c.ld_table;
+    typedef PgGroup<HD, true> Group;
+    typename Group::Pages next;
+    constexpr int N = Group::N;
+    auto find = [&](int j) __attribute__((always_inline)) { next = Group::pages(c, o.by_page, table, j * PG_KEYS + 16 * part16, s_.nk); };
+    // tile j asked for, into its place of four
+    auto request = [&](int j, const typename Group::Pages& p) __attribute__((always_inline)) {
+        Group::direct(c, o.by_page, base, page_ld, row_ld, p, j * PG_KEYS + 16 * part16, s_.nk, lds_at + (4 * late + (j & 3)) * TILE + part16 * (N * 1024));
+    };
+    const PkOffsets<HD> off;
+    PkFrag qf[KS];
+    lds_barrier();                       // (of the piece before)
+    if (j0 < j1) {
+        // (the first pages' numbers together: each is a load that the next step waits for)
+        typename Group::Pages first[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            find(min(j0 + i, j1 - 1));
+            first[i] = next;
+        }
+        find(min(j0 + 3, j1 - 1));
+        const Row r = row_of_lane();
+        const bf16_t* qsrc = a.q + (int64_t)(s_.q0 + r.q) * a.ldq + (int64_t)r.head * HD + 8 * hi;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(qsrc + 16 * ks);
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (j0 + i < j1) request(j0 + i, first[i]);
+    }
+    const float sc = pg_uniform(a.scale * PK_LOG2E), slack = pg_uniform(8.f / sc);
+    pk_floatx16 acc[DB], s[2];
+    PkFrag pf[4];
+    float top = -INFINITY, topsc = 0.f, l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
+    PkFrag f[4];
+    // both products: the second of tile j - 1, the first of tile j
+    auto matrix = [&](int j) __attribute__((always_inline)) {
+        const bool second = j > j0 && (j - 1) * PG_KEYS <= wlast, first = j < j1 && j * PG_KEYS <= wlast;
+        if (second) {
+            const PkOffsets<HD> of(off, lds_at + (4 + ((j - 1) & 3)) * TILE);
+            auto read_v = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(of, (i / DB) * 16 * HD * 2, i % DB, f[i & 3]); };
+            if (careful) {
+                const int q = row_of_lane().q, kb = (j - 1) * PG_KEYS;
+                const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
+                pg_second_clean<HD, 4>(of, 0, pf, acc);
+                const char* values = smem + (4 + ((j - 1) & 3)) * TILE;
+                pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) read_v(i);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int i = 0; i < 4 * DB; ++i) {
+                    acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
+                    if (i + 4 < 4 * DB) read_v(i + 4);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+            }
+        }
+        if (first) {
+            const PkOffsets<HD> of(off, lds_at + (j & 3) * TILE);
+            auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = of.row(i & 1, i >> 1); };
+            const pk_floatx16 zero = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) read_k(i);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i) {
+                s[i & 1] = pk_mfma(f[i & 3], qf[i >> 1], i < 2 ? zero : s[i & 1]);
+                if (i + 4 < 2 * KS) read_k(i + 4);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+        } else {
+            pk_zero(s[0]);
+            pk_zero(s[1]);
+        }
+    };
+    auto softmax = [&](int j) __attribute__((always_inline)) {
+        const int kb = j * PG_KEYS;
+        if (kb > wlast) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pf[i].u = make_uint4(0, 0, 0, 0);
+            return;
+        }
+        if (kb + PG_KEYS - 1 > wfirst) {                     // (wave-uniform)
+            const int q = row_of_lane().q;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t m = pg_seen(a, s_, q, kb + 32 * h) >> (4 * hi);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[h][e] = m & (1u << pk_pos(e)) ? s[h][e] : -INFINITY;
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[h][e]);
+        mx = pk_max_halves(mx);
+        if (__any(mx > top + slack)) {
+            const float grown = fmaxf(top, mx), to = grown == -INFINITY ? 0.f : grown * sc;
+            const float alpha = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(topsc - to);
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+            top = grown;
+            topsc = to;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][(e & 15) + 1], sc, -topsc));
+            l += p0 + p1;
+            pf[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
+        }
+    };
+    // tile j has: up to two behind it, of N loads, may still be on their way
+    auto landed = [&](int j) __attribute__((always_inline)) {
+        if (j + 2 < j1) __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * N));
+        else if (j + 1 < j1) __builtin_amdgcn_s_waitcnt(0x0F70 | N);
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+    };
+    landed(j0);
+    if (late) lds_barrier();
+    for (int j = j0; j < j1; ++j) {
+        lds_barrier();
+        matrix(j);
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        if (j + 3 < j1) {
+            request(j + 3, next);
+            find(min(j + 4, j1 - 1));
+        }
+        softmax(j);
+        __builtin_amdgcn_sched_barrier(0);
+        landed(j + 1);
+    }
+    lds_barrier();
+    matrix(j1);
+    if (!late) lds_barrier();
+    __shared__ int flags[PG_WIDE];
+    if (!careful && pg_any<PG_WIDE>(row_of_lane().mine && pk_not_finite(acc), flags)) return true;
+    l = pk_sum_halves(l);
+    const Row r = row_of_lane();
+    if (u.slot >= 0) {
+        if (!r.mine) return false;
+        const int64_t to = ((int64_t)u.slot * c.n_kv + kvh) * ROWS + wave * 32 + (lane & 31);
+        float* part = o.part + to * HD + 4 * hi;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4*>(part + 32 * db + 8 * g) = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
+        if (hi == 0) o.part_ml[to] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : topsc, l);
+        return false;
+    }
+    const bool empty = pg_empty(a, s_, r.q);
+    const int64_t tok = s_.q0 + r.q;
+    pk_store<HD>(acc, empty ? 0.f : 1.f / l, a.out + tok * a.ldo + (int64_t)r.head * HD, r.mine);
+    if (a.lse && r.mine && hi == 0) a.lse[tok * a.n_heads + r.head] = empty ? -INFINITY : (topsc + log2f(l)) * PK_LN2;
+    return false;
+}
+template <int HD>
+__global__ __launch_bounds__(64 * PG_WIDE) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_wide_kernel(PagedCache c, PagedAttention a, PgOut o) {
+    extern __shared__ __align__(1024) char pg_dynamic[];
+    const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
+    PgWalk<32 * PG_WIDE> walk;
+    if (!walk.begin(c, a, o, at, G)) {
+        pg_leave<32 * PG_WIDE>(o, nullptr, nullptr, at, kvh);
+        return;
+    }
+    while (true) {
+        const PgUnit u = pg_uniform(walk.unit());
+        if (pg_wide<HD, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_wide<HD, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        if (walk.next(c, a, G)) continue;
+        pg_leave<32 * PG_WIDE>(o, &walk, &u, at, kvh);
         return;
     }
 }
@@ -780,7 +1020,7 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
 #pragma unroll
         for (int e = 0; e < 4; ++e) z = fmaf(acc[d][e], 0.f, z);
     __shared__ int flags[PG_WAVES];
-    if (!careful && pg_any(row_of_lane().mine && !(z == 0.f), flags)) return true;
+    if (!careful && pg_any<PG_WAVES>(row_of_lane().mine && !(z == 0.f), flags)) return true;
     // The waves' sums, the second two to the first two and the second to the first: what they are relative to, -inf: no part, their exponentials' sum, the sums
     float* const sums = (float*)(char*)lds;
     float* const rel = sums + 2 * ROWS * PITCH;
@@ -906,8 +1146,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAtte
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
-// two workgroups to each of 256 compute units
-constexpr int PG_PLACES = 512, PG_LEAST = 256;
+// two workgroups to each of 256 compute units, or one of twice the waves
+constexpr int PG_PLACES = 512, PG_LEAST = 256, PG_LONG = 2048;      // PG_LONG: room of a sequence from which on 256 rows are taken together
 
 struct PgLaunch { int rows; int64_t units, slots; int places, cost; };
 PgLaunch pg_launch_of(const PagedCache& c, const PagedAttention& a) {
@@ -916,13 +1156,13 @@ PgLaunch pg_launch_of(const PagedCache& c, const PagedAttention& a) {
     // By the rows of a sequence in the mean.  (The kernel of few rows with two blocks of 16, for up to 32: single tokens with 32 heads on one key head, 200000 keys, 56 us and 44 with
     // the other, trees of 6 tokens with 4 heads on a key head 192 and 176; with 16 rows in the mean 90 in the one of few and 98 in the other, with 4 rows 156 and 170)
     const int64_t mean = (a.total_q * G + c.n_seq - 1) / std::max(1, c.n_seq);
-    p.rows = mean <= 16 ? 16 : 128;
+    p.rows = mean <= 16 ? 16 : mean <= 128 || c.page_size % 16 || (int64_t)c.max_pages * c.page_size < PG_LONG ? 128 : 256;
     const int64_t tiles = a.total_q * G / p.rows + std::min<int64_t>(c.n_seq, a.total_q);
     // What sharing out costs is a second piece's start, storing sums and the launch that joins them: 8 to 10 us in all.  (384 and 256 keys: 15 prompts' pieces on 3100 keys 38 us for
     // 19, trees of 44 tokens on 1400 keys 18.7 for 14.9, the first tokens of four conversations 11.5 for 10.0; 1536 and 1024: two prompts' on 1700 keys 31 for 23.)  No sequence has
     // more keys than its room: with less than that nothing is shared out
     p.cost = p.rows >= 128 ? 1024 : 768;
-    p.places = (int64_t)c.max_pages * c.page_size <= p.cost ? 1 : std::max(1, (PG_PLACES + c.n_kv - 1) / c.n_kv);
+    p.places = (int64_t)c.max_pages * c.page_size <= p.cost ? 1 : std::max(1, (PG_PLACES / (p.rows > 128 ? 2 : 1) + c.n_kv - 1) / c.n_kv);
     p.slots = p.places < 2 ? 0 : 2LL * p.places * c.n_kv;
     p.units = std::max<int64_t>(tiles, p.places) * c.n_kv;
     return p;
@@ -949,6 +1189,15 @@ hipError_t pg_launch(const PagedCache& c, const PagedAttention& a, const PgOut& 
     hipLaunchKernelGGL((paged_kernel<HD, WHOLE>), dim3((unsigned)units), dim3(64 * PG_WAVES), SMEM, st, c, a, o);
     return hipGetLastError();
 }
+template <int HD>
+hipError_t pg_launch_wide(const PagedCache& c, const PagedAttention& a, const PgOut& o, int64_t units, hipStream_t st) {
+    constexpr int SMEM = 8 * PG_KEYS * HD * 2;
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = pg_lds(paged_wide_kernel<HD>, SMEM, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_wide_kernel<HD>, dim3((unsigned)units), dim3(64 * PG_WIDE), SMEM, st, c, a, o);
+    return hipGetLastError();
+}
 template <int HD, bool WHOLE>
 hipError_t pg_launch_few(const PagedCache& c, const PagedAttention& a, const PgOut& o, int64_t units, hipStream_t st) {
     constexpr int SMEM = PG_WAVES * 2 * PG_FEW_KEYS * HD * 2;
@@ -966,20 +1215,25 @@ hipError_t pg_launch_forward(const PagedCache& c, const PagedAttention& a, void*
     float* part = static_cast<float*>(workspace);
     float2* part_ml = reinterpret_cast<float2*>(part + p.slots * p.rows * HD);
     const PgOut o{part, part_ml, reinterpret_cast<PgCut*>(part_ml + p.slots * p.rows), p.places, PG_LEAST, p.cost, QuickDiv(c.n_kv), QuickDiv((int)G), QuickDiv(c.page_size)};
-    if (p.units >= kPackedUnits) return hipErrorInvalidValue;
+    if (paged_units(c, a) >= kPackedUnits) return hipErrorInvalidValue;
     const bool whole = c.page_size % 16 == 0;
     const hipError_t e = p.rows == 16 ? (whole ? pg_launch_few<HD, true>(c, a, o, p.units, st) : pg_launch_few<HD, false>(c, a, o, p.units, st))
+                                      : p.rows == 256 ? pg_launch_wide<HD>(c, a, o, p.units, st)
                                       : whole ? pg_launch<HD, true>(c, a, o, p.units, st) : pg_launch<HD, false>(c, a, o, p.units, st);
     if (e != hipSuccess || p.places < 2) return e;
     const dim3 borders((unsigned)((p.places - 1) * c.n_kv), p.rows / pg_join_rows(HD));
     if (p.rows == 16) hipLaunchKernelGGL((paged_join_kernel<HD, 16>), borders, dim3(256), 0, st, c, a, o);
+    else if (p.rows == 256) hipLaunchKernelGGL((paged_join_kernel<HD, 256>), borders, dim3(256), 0, st, c, a, o);
     else hipLaunchKernelGGL((paged_join_kernel<HD, 128>), borders, dim3(256), 0, st, c, a, o);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t paged_units(const PagedCache& c, const PagedAttention& a) { return pg_launch_of(c, a).units; }
+int64_t paged_units(const PagedCache& c, const PagedAttention& a) {
+    const PgLaunch p = pg_launch_of(c, a);
+    return p.rows > 128 ? 2 * p.units : p.units;      // (of 256 threads)
+}
 size_t paged_workspace_bytes(const PagedCache& c, const PagedAttention& a, int head_dim) {
     const PgLaunch p = pg_launch_of(c, a);
     return p.slots == 0 ? 0 : (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2)) + p.places * sizeof(PgCut);
