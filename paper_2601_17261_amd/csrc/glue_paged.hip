@@ -313,7 +313,8 @@ struct PgGroup {
             }
         }
     }
-    // ... straight to LDS, at byte `to` on
+    // ... straight to LDS, at byte `to` on.  (Written out, for what the compiler does not see it does not wait for; so the wait states are written out too: five from a scalar register that
+    // a vector instruction writes, a spilled one's reload say, to a load that reads it, one from m0)
     static __device__ __forceinline__ void direct(const PagedCache& c, const QuickDiv& by_page, const bf16_t* base, int64_t page_ld, int64_t row_ld, const Pages& p, int kg, int nk, int to) {
         static_assert(WHOLE, "one page");
         const int r = row_of_lane(), most = (int)c.n_pages - 1;
@@ -324,7 +325,7 @@ struct PgGroup {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = (int)(__umul24((uint32_t)min(r + ROWS * i, left), (uint32_t)(2 * row_ld)) + (uint32_t)(chunk ^ (pk_swz<HD>(ROWS * i) << 4)));
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + i * 1024), "v"(at), "s"(rsrc) : "memory", "m0");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + i * 1024), "v"(at), "s"(rsrc) : "memory", "m0");
         }
     }
     // to rows 16 g .. of a tile

@@ -57,3 +57,15 @@ def test_the_loops_over_keys_reload_only_for_masked_tiles(kernels):
         found += 1
         assert sum(ins.op.startswith("scratch") for ins in body[t:i + 1]) <= 1, name
     assert found == 10
+
+
+def test_loads_to_lds_that_are_written_out_have_their_wait_states(kernels):
+    """five between a scalar register that a vector instruction writes and a load that reads it, one between m0 and a load to LDS: the compiler keeps them only where it knows of the load"""
+    found = 0
+    for name, (body, _) in kernels["glue_paged.hip"].items():
+        for i, ins in enumerate(body):
+            if ins.op.startswith("buffer_load") and ins.text.split()[-1] == "lds":
+                found += 1
+                assert ins.in_asm and "wide" in name
+                assert body[i - 1].text.split()[:2] == ["s_nop", "4"] and body[i - 2].text.startswith("s_mov_b32 m0")
+    assert found > 0
