@@ -32,7 +32,7 @@ struct PgOut { float* part; float2* part_ml; PgCut* cuts; int places, least, cos
 
 // ---- who does what -----------------------------------------------------------------------------------------------
 // A row tile's work is about the keys that its rows see: first + t step of row tile t of a sequence, so that the work in front of one is a whole number that every
-// workgroup finds alike.  Row tiles are one workgroup's each where that is about as soon done, else the work of all of them in a row is cut into equal pieces, one to
+// workgroup finds alike.  Row tiles are one workgroup's each where that is about as soon done, or equal parts of each are, else the work of all of them in a row is cut into equal pieces, one to
 // each place: a workgroup then has the end of one row tile, perhaps whole ones, and the beginning of another.  (64 single tokens on 200000 keys: 219 us with shares of each
 // sequence for its own, 193 so.  Sums over the lanes by __shfl_up were most of a workgroup's start, 6 us)
 struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles, the first one's work, and what each has more than the one before
@@ -95,6 +95,7 @@ struct PgWalk {
     int64_t pos, end, start;      // work in front of what is left, and behind it; start: in front of sequence seq's row tile `tile`
     int64_t total, each;          // of all sequences; of a piece
     int seq, tile, index, pieces, start_cost;
+    int parts, part;              // where each workgroup has one part of a row tile: of how many, which.  parts = 0: it is not so
     bool whole, first;
     PagedSeq s;
     PgWork w;
@@ -123,6 +124,7 @@ struct PgWalk {
             shortest = min(shortest, 0x7FFFFFFF - pg_max(work.tiles ? 0x7FFFFFFF - work.first : 0));
         }
         start_cost = pg_start(ROWS, total >= (int64_t)o.places * PG_BUSY);
+        const int64_t keys = total;
         total += (int64_t)start_cost * tiles;
         longest += start_cost;
         shortest += start_cost;
@@ -137,29 +139,56 @@ struct PgWalk {
         const float alike = (float)shortest / (float)longest, alone = (float)total / (float)o.places * (1.f + alike * (ceilf(rounds) / rounds - 1.f));
         whole = fmaxf((float)longest, tiles > o.places ? alone : 0.f) <= share + (float)o.cost || o.places < 2 || total >= (1LL << 52);
         each = (int64_t)((double)total / pieces) + 1;
+        parts = 0;
+        int src = -1;
         if (whole) {
             if (index >= tiles) return false;
             pos = index;
             end = pos + 1;
-        } else {
+        } else if (c.n_seq <= 64 && tiles < o.places) {
+            // Every row tile in equal parts, so many that all of them have places, where such a part is little more than an even share: no workgroup then has a second piece to start.  (16 trees
+            // of 6 tokens on 100000 keys in both launches 44.6 us and 39.8 so, 20 trees on 4200 keys 32.6 and 29, two prompts' pieces on 1700 keys 23.3 and 20.2)
+            const int most = work.tiles ? pg_of(work, work.tiles - 1) - start_cost : 0;      // keys of a sequence's longest
+            const float even = (float)keys / (float)pieces;
+            float size = fmaxf(even, (float)o.least);
+            int k = 1, all = 0;
+            for (int i = 0; i < 12; ++i, size *= 1.1f) {
+                k = max((int)ceilf((float)most / size), 1);
+                all = pk_total(work.tiles * k);
+                if (all <= o.places) break;
+            }
+            if (all <= o.places && (float)pg_max((int)((float)most / (float)k)) <= even + (float)start_cost) {
+                if (index >= all) return false;
+                const int upto = pk_scan(work.tiles * k);
+                src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > index));
+                parts = __builtin_amdgcn_readlane(k, src);
+                const int in = index - __builtin_amdgcn_readlane(upto - work.tiles * k, src);
+                tile = (int)(((float)in + 0.5f) / (float)parts);
+                part = in - tile * parts;
+            }
+        }
+        if (!whole && parts == 0) {
             pos = begin_of(index);
             end = begin_of(index + 1);
             if (index >= pieces || pos >= end) return false;
         }
         if (whole && tiles > o.places && c.n_seq <= 64) {
             // level by level: a sequence's last row tile, which sees most, is as many levels high as it has row tiles, the next one a level less
-            const int own = work.tiles, t = index;
+            const int own = work.tiles;
             int low = 0, high = pg_max(own);
             while (low < high) {
                 const int mid = (low + high) >> 1;
-                if (pk_total(max(own - mid, 0)) <= t) high = mid;
+                if (pk_total(max(own - mid, 0)) <= index) high = mid;
                 else low = mid + 1;
             }
-            const int place = t - pk_total(max(own - low, 0));
+            const int place = index - pk_total(max(own - low, 0));
             const uint64_t m = __builtin_amdgcn_ballot_w64(own >= low);
             const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-            take(its, __builtin_ctzll(__builtin_amdgcn_ballot_w64(own >= low && before == place)), 0, a, G);
+            src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(own >= low && before == place));
             tile = low - 1;
+        }
+        if (src >= 0) {
+            take(its, src, 0, a, G);
             return true;
         }
         int64_t before = 0;
@@ -203,6 +232,13 @@ struct PgWalk {
         u.seq = seq;
         u.tile = tile;
         u.all = pg_of(w, tile);
+        if (parts) {
+            const int size = (int)((float)u.all / (float)parts) + (u.all >> 22) + 1;      // (fp32: parts times it are all)
+            u.from = (int)min((int64_t)u.all, (int64_t)part * size);
+            u.to = (int)min((int64_t)u.all, (int64_t)u.from + size);
+            u.slot = parts == 1 ? -1 : 2 * index;
+            return u;
+        }
         u.from = whole ? 0 : (int)(pos - start);
         u.to = whole ? u.all : (int)min((int64_t)u.all, end - start);
         u.slot = u.from == 0 && u.to == u.all ? -1 : 2 * index + (first ? 0 : 1);
@@ -210,7 +246,7 @@ struct PgWalk {
     }
     // on to the next one
     __device__ __forceinline__ bool next(const PagedCache& c, const PagedAttention& a, int G) {
-        if (whole || start + pg_of(w, tile) >= end) return false;
+        if (whole || parts || start + pg_of(w, tile) >= end) return false;
         start += pg_of(w, tile);
         pos = start;
         first = false;
@@ -224,6 +260,22 @@ struct PgWalk {
         return false;
     }
 };
+// What a wave knows of the walk, in LDS while it goes over a piece: some forty scalar registers, which would be spilled otherwise.  (111 reloads in the kernel of 128 rows, 60 so; a piece's
+// end waits for them: four trees on 600 keys 13.8 us and 13.1)
+template <int ROWS>
+__device__ __forceinline__ void pg_put(const PgWalk<ROWS>& w, uint32_t* at) {
+    union { PgWalk<ROWS> walk; uint32_t word[sizeof(PgWalk<ROWS>) / 4]; } u;
+    u.walk = w;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(PgWalk<ROWS>) / 4); ++i) at[i] = u.word[i];
+}
+template <int ROWS>
+__device__ __forceinline__ void pg_get(PgWalk<ROWS>& w, const uint32_t* at) {
+    union { PgWalk<ROWS> walk; uint32_t word[sizeof(PgWalk<ROWS>) / 4]; } u;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(PgWalk<ROWS>) / 4); ++i) u.word[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)at[i]);
+    w = u.walk;
+}
 // A workgroup's entry for the launch that joins: the row tile that it has the beginning of and not the end, its last one.  (Worked out once more there it is 3 us)
 template <int ROWS>
 __device__ __forceinline__ void pg_leave(const PgOut& o, const PgWalk<ROWS>* walk, const PgUnit* u, int index, int kvh) {
@@ -233,9 +285,9 @@ __device__ __forceinline__ void pg_leave(const PgOut& o, const PgWalk<ROWS>* wal
         cut.s = u->s;
         cut.tile = u->tile;
         cut.slot = u->slot;
-        cut.parts = 1;
+        cut.parts = max(walk->parts, 1);
         const int64_t past = walk->start + u->all;
-        while (index + cut.parts < walk->pieces && walk->begin_of(index + cut.parts) < past) ++cut.parts;
+        while (walk->parts == 0 && index + cut.parts < walk->pieces && walk->begin_of(index + cut.parts) < past) ++cut.parts;
     }
     o.cuts[index] = cut;
 }
@@ -598,6 +650,8 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
     extern __shared__ __align__(1024) char pg_dynamic[];
     // the key heads side by side: an XCD (workgroup number mod 8) then has few of them
     const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
+    __shared__ uint32_t walks[PG_WAVES][sizeof(PgWalk<PG_ROWS>) / 4];
+    uint32_t* const saved = walks[threadIdx.x >> 6];
     PgWalk<PG_ROWS> walk;
     if (!walk.begin(c, a, o, at, G)) {
         pg_leave<PG_ROWS>(o, nullptr, nullptr, at, kvh);
@@ -605,7 +659,9 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
     }
     while (true) {
         const PgUnit u = pg_uniform(walk.unit());
+        pg_put(walk, saved);
         if (pg_forward<HD, WHOLE, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_forward<HD, WHOLE, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        pg_get(walk, saved);
         if (walk.next(c, a, G)) continue;
         pg_leave<PG_ROWS>(o, &walk, &u, at, kvh);
         return;
@@ -817,6 +873,8 @@ template <int HD>
 __global__ __launch_bounds__(64 * PG_WIDE) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_wide_kernel(PagedCache c, PagedAttention a, PgOut o) {
     extern __shared__ __align__(1024) char pg_dynamic[];
     const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
+    __shared__ uint32_t walks[PG_WIDE][sizeof(PgWalk<32 * PG_WIDE>) / 4];
+    uint32_t* const saved = walks[threadIdx.x >> 6];
     PgWalk<32 * PG_WIDE> walk;
     if (!walk.begin(c, a, o, at, G)) {
         pg_leave<32 * PG_WIDE>(o, nullptr, nullptr, at, kvh);
@@ -824,7 +882,9 @@ __global__ __launch_bounds__(64 * PG_WIDE) __attribute__((amdgpu_waves_per_eu(2,
     }
     while (true) {
         const PgUnit u = pg_uniform(walk.unit());
+        pg_put(walk, saved);
         if (pg_wide<HD, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_wide<HD, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        pg_get(walk, saved);
         if (walk.next(c, a, G)) continue;
         pg_leave<32 * PG_WIDE>(o, &walk, &u, at, kvh);
         return;
@@ -1078,6 +1138,8 @@ template <int HD, bool WHOLE>
 __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_few_kernel(PagedCache c, PagedAttention a, PgOut o) {
     extern __shared__ __align__(1024) char pg_dynamic[];
     const int at = o.by_kv((int)blockIdx.x), kvh = (int)blockIdx.x - at * c.n_kv, G = (int)o.by_group.d;
+    __shared__ uint32_t walks[PG_WAVES][sizeof(PgWalk<16>) / 4];
+    uint32_t* const saved = walks[threadIdx.x >> 6];
     PgWalk<16> walk;
     if (!walk.begin(c, a, o, at, G)) {
         pg_leave<16>(o, nullptr, nullptr, at, kvh);
@@ -1085,7 +1147,9 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
     }
     while (true) {
         const PgUnit u = pg_uniform(walk.unit());
+        pg_put(walk, saved);
         if (pg_few<HD, WHOLE, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_few<HD, WHOLE, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        pg_get(walk, saved);
         if (walk.next(c, a, G)) continue;
         pg_leave<16>(o, &walk, &u, at, kvh);
         return;
