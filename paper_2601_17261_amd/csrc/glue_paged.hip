@@ -146,8 +146,9 @@ struct PgWalk {
             pos = index;
             end = pos + 1;
         } else if (c.n_seq <= 64 && tiles < o.places) {
-            // Every row tile in equal parts, so many that all of them have places, where such a part is little more than an even share: no workgroup then has a second piece to start.  (16 trees
-            // of 6 tokens on 100000 keys in both launches 44.6 us and 39.8 so, 20 trees on 4200 keys 32.6 and 29, two prompts' pieces on 1700 keys 23.3 and 20.2)
+            // Every row tile in equal parts, so many that all of them have places, where such a part is little more than an even share: no workgroup then has a second piece to start.  (32
+            // single tokens with 32 heads on one key head, 200000 keys, in both launches 44.6 us and 39.8 so, four trees of 17 tokens on 42000 keys 32.6 and 28.9, two prompts' pieces on 1700 keys
+            // 23.3 and 20.4; what the choice costs where row tiles stay whole: 0.3 us for single tokens, 0.8 for more rows)
             const int most = work.tiles ? pg_of(work, work.tiles - 1) - start_cost : 0;      // keys of a sequence's longest
             const float even = (float)keys / (float)pieces;
             float size = fmaxf(even, (float)o.least);
