@@ -675,7 +675,7 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
 // others, three tiles ahead in rings of four (HD = 128: 96 KB on their way; a tile's place is free again before its next one is asked for, since both halves have read it a barrier
 // before).  How far loads are is waited for by their number: the compiler does not see them, and would wait for all of them in front of each read of LDS.
 // Against 128 rows with tiles through registers: 2500 tokens behind and among 20001 keys 278 -> 250 us in both launches, 940 TFLOP/s, 4096 tokens of one prompt 182 -> 168, trees of 48 tokens on 60000
-// keys 92 -> 87, of 64 on 100000 158 -> 135: keys are read by half as many row tiles.  One tile by itself takes 1.7 us and not 1.4, so that short caches are not for it (20 trees on 4200
+// keys 92 -> 85, of 64 on 100000 158 -> 135: keys are read by half as many row tiles.  One tile by itself takes 1.7 us and not 1.4, so that short caches are not for it (20 trees on 4200
 // keys 28 -> 33 us, two prompts' pieces on 1700 keys 23 -> 31)
 constexpr int PG_WIDE = 8;
 template <int HD, bool careful>
