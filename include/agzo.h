@@ -406,7 +406,7 @@ int agzo_glue_cache_keep(agzo_ctx* ctx, const agzo_paged_cache* cache, const int
  *     u_i q_i(x) < p(x),   without q:  u_i (1 - sum of p over the tokens refused here before) < p(x)   (a token refused here before has p(x) = 0).
  * The token that follows is the first x with  sum_{y <= x} w(y) > u_0 sum_y w(y),  w = max(p - q_i, 0) where row i was refused last, without q p but 0 for the tokens refused here; the last one with
  * w > 0 if there is no such, w = p if no w is positive, -1 if no p is.  Negative probabilities and NaN count as 0, and so does a token outside the vocabulary.
- *   out_tokens, out_rows [n]: a sequence's accepted tokens and their rows, then (out_tokens) the token that follows, then -1;  n_accepted [n_seq]: how many (device int32).
+ *   out_tokens, out_rows [n]: a sequence's accepted tokens and their rows, then (out_tokens) the token that follows, then -1;  n_accepted [n_seq]: how many (device int32), 0 for a sequence without rows.
  * Products, differences and sums are fp64.  Rows of no sequence are neither read nor written.  Device, workspace and captures as for the calls on packed batches.
  * Errors: AGZO_EINVAL for NULL or misaligned tensors, q with parents, leading dimensions below vocab, more than 65535 sequences, 2^26 rows or 2^24 probabilities a row, overlapping outputs. */
 int agzo_verify_drafts(agzo_ctx* ctx, int32_t dtype, const void* p, int64_t ldp, const void* q, int64_t ldq, const int32_t* tokens, const int32_t* parents, const float* uniforms,

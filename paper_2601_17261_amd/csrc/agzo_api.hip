@@ -1793,8 +1793,8 @@ int agzo_verify_drafts(agzo_ctx* ctx, int32_t dtype, const void* p, int64_t ldp,
                     {named("p", p, ldp, n, vocab, size), named("q", q, ldq, n, vocab, size), listed("tokens", tokens, n), listed("parents", parents, n), listed("uniforms", uniforms, n),
                      listed("cu", cu, n_seq + 1LL)}));
     TRY(check_device(ctx));
-    if (n == 0 || n_seq == 0) return AGZO_OK;
-    TRY(reserve(ctx, verify_workspace_bytes(n_seq, vocab)));
+    if (n_seq == 0) return AGZO_OK;
+    if (n > 0) TRY(reserve(ctx, verify_workspace_bytes(n_seq, vocab)));
     HIPCHK(launch_verify(VerifyArgs{p, q, ldp, ldq, tokens, parents, uniforms, cu, n, n_seq, vocab, out_tokens, out_rows, n_accepted}, dtype == AGZO_F32, ctx->ws, ctx->stream));
     return AGZO_OK;
 }

@@ -298,6 +298,12 @@ __global__ __launch_bounds__(VF_WG) void verify_draw_kernel(VerifyArgs a, VfStat
     a.out_tokens[r0 + e.count] = (int)(at + second);
 }
 
+// no sequence has a row: none is accepted
+__global__ __launch_bounds__(VF_WG) void verify_none_kernel(int32_t* n_accepted, int n_seq) {
+    const int i = blockIdx.x * VF_WG + threadIdx.x;
+    if (i < n_seq) n_accepted[i] = 0;
+}
+
 int verify_segment(int n_seq, int64_t vocab) {
     // enough workgroups to keep every compute unit's loads in flight, of no fewer tokens than a workgroup takes at a time
     int64_t size = VF_LEAST;
@@ -322,7 +328,11 @@ hipError_t launch_verify_typed(const VerifyArgs& a, void* workspace, hipStream_t
 size_t verify_workspace_bytes(int n_seq, int64_t vocab) { return (size_t)n_seq * ((vocab + VF_PIECE - 1) / VF_PIECE * sizeof(double) + sizeof(VfReached)); }
 
 hipError_t launch_verify(const VerifyArgs& a, bool f32, void* workspace, hipStream_t st) {
-    if (a.n == 0 || a.n_seq == 0) return hipSuccess;
+    if (a.n_seq == 0) return hipSuccess;
+    if (a.n == 0) {
+        hipLaunchKernelGGL(verify_none_kernel, dim3((a.n_seq + VF_WG - 1) / VF_WG), dim3(VF_WG), 0, st, a.n_accepted, a.n_seq);
+        return hipGetLastError();
+    }
     return f32 ? launch_verify_typed<float>(a, workspace, st) : launch_verify_typed<bf16_t>(a, workspace, st);
 }
 
