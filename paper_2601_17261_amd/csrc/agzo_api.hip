@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "agzo_internal.h"
+#include "cache_layout.h"
 #include "fork.h"
 #include "grow.h"
 #include "overlap.h"
@@ -1584,30 +1585,17 @@ int agzo_glue_attention_packed_backward(agzo_ctx* ctx, const agzo_packed_attenti
 
 // ---- a cache in pages ------------------------------------------------------------------------------------------------
 namespace {
-// How one of a cache's tensors lies in memory: its axes of more than one index from the closest on, and what each covers (in values).  extent[0]: a head's values
-struct CacheLayout { int64_t stride[3], size[3], extent[4]; int axes; };
-
 int check_cache_tensor(agzo_ctx* ctx, const agzo_paged_cache* c, const char* name, const void* at, int64_t page, int64_t row, int64_t head, CacheLayout& out) {
     if ((!at && c->n_pages > 0) || (reinterpret_cast<uintptr_t>(at) & 15)) return fail(ctx, AGZO_EINVAL, "the cache's %s is NULL or misaligned", name);
     if (c->page_size > 1 && row >= (1LL << 22)) return fail(ctx, AGZO_EINVAL, "rows of the cache's %s must be less than 2^22 values apart", name);
-    out = CacheLayout{};
-    out.extent[0] = c->head_dim;
-    const int64_t axes[3][2] = {{page, c->n_pages}, {row, c->page_size}, {head, c->n_kv_heads}};
-    for (const auto& x : axes) {
-        if (x[1] <= 1) continue;
-        if (x[0] % 8 || x[0] < c->head_dim || x[0] >= (1LL << 40)) return fail(ctx, AGZO_EINVAL, "a stride of %lld in the cache's %s", (long long)x[0], name);
-        int i = out.axes++;
-        for (; i > 0 && out.stride[i - 1] > x[0]; --i) { out.stride[i] = out.stride[i - 1]; out.size[i] = out.size[i - 1]; }
-        out.stride[i] = x[0];
-        out.size[i] = x[1];
+    int64_t bad = 0;
+    switch (cache_layout(c->head_dim, {{page, c->n_pages}, {row, c->page_size}, {head, c->n_kv_heads}}, out, bad)) {
+        case CacheFault::none: return 0;
+        case CacheFault::stride: return fail(ctx, AGZO_EINVAL, "a stride of %lld in the cache's %s", (long long)bad, name);
+        case CacheFault::overlap: return fail(ctx, AGZO_EINVAL, "rows or pages of the cache's %s overlap each other", name);
+        case CacheFault::large: break;
     }
-    for (int i = 0; i < out.axes; ++i) {
-        if (out.stride[i] < out.extent[i]) return fail(ctx, AGZO_EINVAL, "rows or pages of the cache's %s overlap each other", name);
-        const __int128 more = (__int128)(out.size[i] - 1) * out.stride[i] + out.extent[i];
-        if (more >= (__int128)1 << 60) return fail(ctx, AGZO_EINVAL, "the cache's %s is too large", name);
-        out.extent[i + 1] = (int64_t)more;
-    }
-    return 0;
+    return fail(ctx, AGZO_EINVAL, "the cache's %s is too large", name);
 }
 
 Named cache_range(const char* name, const void* at, const CacheLayout& l, int64_t n_pages) {
@@ -1615,16 +1603,11 @@ Named cache_range(const char* name, const void* at, const CacheLayout& l, int64_
     return named(name, n_pages > 0 ? at : nullptr, all, 1, all);
 }
 
-// whether keys and values share no memory: apart as a whole, or one in the gaps that the other leaves at some level
+// whether keys and values share no memory
 bool caches_apart(const agzo_paged_cache* c, const CacheLayout& k, const CacheLayout& v) {
     if (!rows_overlap(cache_range("", c->k, k, c->n_pages).rows, cache_range("", c->v, v, c->n_pages).rows)) return true;
-    if (k.axes != v.axes) return false;
-    for (int i = 0; i < k.axes; ++i)
-        if (k.stride[i] != v.stride[i] || k.size[i] != v.size[i]) return false;
-    const int64_t d = static_cast<const char*>(c->v) - static_cast<const char*>(c->k), between = (d < 0 ? -d : d) / 2;
-    for (int i = 0; i < k.axes; ++i)
-        if (k.extent[i] <= between && between + k.extent[i] <= k.stride[i]) return true;
-    return false;
+    const int64_t d = static_cast<const char*>(c->v) - static_cast<const char*>(c->k);
+    return layouts_apart(k, v, (d < 0 ? -d : d) / 2);
 }
 
 // kr, vr: where its tensors lie.  written: by the call
