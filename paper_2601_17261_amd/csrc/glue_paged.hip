@@ -451,7 +451,7 @@ __device__ __forceinline__ void pg_clean(PkFrag& f) {
 }
 // the second product with them taken out, its fragments of 16 positions `at` on
 template <int HD, int N>
-__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[N], pk_floatx16 (&acc)[HD / 32]) {
+__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[N], const PkFrag (&low)[N], pk_floatx16 (&acc)[HD / 32]) {
 #pragma unroll
     for (int s = 0; s < N; ++s)
 #pragma unroll
@@ -460,17 +460,24 @@ __device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, 
             pk_read_trans<HD>(o, at + s * 16 * HD * 2, db, f);
             pg_clean(f);
             acc[db] = pk_mfma(f, p[s], acc[db]);
+            acc[db] = pk_mfma(f, low[s], acc[db]);
         }
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------
+// Whether a sequence's probabilities go into the second product in two bf16 parts (16 bits) and not in one: a single token's, which are few large ones often, and those of as few rows as
+// the kernel of few rows is for.  By the sequence's own rows, so that what it is beside does not change its bits' number
+__device__ __forceinline__ bool pg_two_parts(const PagedSeq& s, int G) { return s.nq <= 1 || s.nq * G <= 16; }
+
 constexpr int PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgroup, keys of a tile
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
 // waits: the shape of attention over packed sequences, for the same reasons.  16 trees of 30 tokens with 4 heads on each of 8 key heads, 100000 keys, 415 MB, take 110 us in both
 // launches, 3.7 TB/s; 2500 tokens behind and among 20001 keys, 235 GFLOP, 265 in this one, matrix cores busy 49 % of the time, vector instructions 51 %, mostly in turn.
 // (Products of 16 x 16 x 32: 319 us for 283 with the join.  A second 256 workgroups with less work, or with priority: no gain, or a loss)
-// The probabilities are rounded to bf16 for the second product: in two parts, as for few rows, a result is off by 0.0017 of its norm and not 0.0023, and trees on 60000 keys
-// take 109 us and not 87
+// The probabilities are rounded to bf16 for the second product, but for pg_two_parts.  In two parts throughout a result is off by 0.0017 of its norm and not 0.0023; 2500 tokens on 20001 keys in
+// pages of 20 then take 453 us and not 360, 900 on 1700 keys 35 and not 30, 48 single tokens' heads on two key heads, which have them, 36 and not 33.  The second part's products are a
+// pass over the values of their own: beside the first part's, a branch at each, tiles without them take 3 % longer, and in a copy of the whole pass registers are reloaded in its
+// loop (16 trees of 30 tokens 156 us and not 110)
 // true: stored nothing, the tiles have to be gone over with care
 template <int HD, bool WHOLE, bool careful>
 __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
@@ -482,6 +489,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
     const int hi = lane >> 5;
     const int G = (int)o.by_group.d;
     const PagedSeq s_ = u.s;
+    const bool fine = careful || pg_two_parts(s_, G);
     // (which of the 32 rows are a wave's: the other way round in the second 256 workgroups, of which a compute unit has one beside one of the first, so that tiles with few
     // rows keep all four SIMDs busy together: trees of 48 tokens, 192 rows in tiles of 128 and 64, 102.6 -> 97.3 us)
     const int block = (blockIdx.x >> 8) & 1 ? PG_WAVES - 1 - wave : wave;
@@ -538,7 +546,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         const int kb = j * PG_KEYS;
         if (kb > wlast) return;                                          // (wave-uniform)
         const int tile_at = (j & 1) * (2 * TILE);
-        const PkOffsets<HD> of(off, lds_at + tile_at);
+        const PkOffsets<HD> of(off.rows, off.trans[0], lds_at + tile_at);
         PkFrag f[4];
         auto read_k = [&](int i) __attribute__((always_inline)) { f[i & 3].v = of.row(i & 1, i >> 1); };
         auto read_v = [&](int i) __attribute__((always_inline)) { pk_read_trans<HD>(of, TILE + (i / DB) * 16 * HD * 2, i % DB, f[i & 3]); };
@@ -559,9 +567,12 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         const bool mask = kb + PG_KEYS - 1 > wfirst;                     // (wave-uniform)
         if (mask) {
             const int q = row_of_lane().q;
+            int lane_ = (int)threadIdx.x;                                // (as for rows)
+            asm volatile("" : "+v"(lane_));
+            const int hi_ = (lane_ >> 5) & 1;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t m = pg_seen(a, s_, q, kb + 32 * h) >> (4 * hi);
+                const uint32_t m = pg_seen(a, s_, q, kb + 32 * h) >> (4 * hi_);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[h][e] = m & (1u << pk_pos(e)) ? s[h][e] : -INFINITY;
             }
@@ -583,18 +594,26 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
             top = grown;
             topsc = to;
         }
-        PkFrag pf[4];
-        // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that)
+        PkFrag pf[4], pl[4];
+        // (rounded to bf16 for the second product, whose sums are fp32; their sum is taken before that.  What that leaves is the second part)
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][(e & 15) + 1], sc, -topsc));
             l += p0 + p1;
             pf[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
+            s[e >> 4][e & 15] = p0;
+            s[e >> 4][(e & 15) + 1] = p1;
         }
+        if (fine)
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+                const uint32_t w = pf[e >> 3].w[(e & 7) >> 1];
+                pl[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(s[e >> 4][e & 15] - __uint_as_float(w << 16), s[e >> 4][(e & 15) + 1] - __uint_as_float(w & 0xFFFF0000u));
+            }
         if (careful) {
             const int q = row_of_lane().q;
             const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
-            pg_second_clean<HD, 4>(of, TILE, pf, acc);
+            pg_second_clean<HD, 4>(of, TILE, pf, pl, acc);
             const char* values = smem + tile_at + TILE;
             pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
             return;
@@ -606,6 +625,17 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
             acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
             if (i + 4 < 4 * DB) read_v(i + 4);
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if (fine) {                                                      // (workgroup-uniform)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) read_v(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4 * DB; ++i) {
+                acc[i % DB] = pk_mfma(f[i & 3], pl[i / DB], acc[i % DB]);
+                if (i + 4 < 4 * DB) read_v(i + 4);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
     };
@@ -678,7 +708,7 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
 // keys 92 -> 85, of 64 on 100000 158 -> 135: keys are read by half as many row tiles.  One tile by itself takes 1.7 us and not 1.4, so that short caches are not for it (20 trees on 4200
 // keys 28 -> 33 us, two prompts' pieces on 1700 keys 23 -> 31)
 constexpr int PG_WIDE = 8;
-template <int HD, bool careful>
+template <int HD, bool fine, bool careful>
 __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
     char* smem = (char*)lds;
     const int lds_at = (int)(uint32_t)(uintptr_t)lds;
@@ -733,7 +763,7 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
     }
     const float sc = pg_uniform(a.scale * PK_LOG2E), slack = pg_uniform(8.f / sc);
     pk_floatx16 acc[DB], s[2];
-    PkFrag pf[4];
+    PkFrag pf[4], pl[4];
     float top = -INFINITY, topsc = 0.f, l = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d) pk_zero(acc[d]);
@@ -747,7 +777,7 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
             if (careful) {
                 const int q = row_of_lane().q, kb = (j - 1) * PG_KEYS;
                 const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
-                pg_second_clean<HD, 4>(of, 0, pf, acc);
+                pg_second_clean<HD, 4>(of, 0, pf, pl, acc);
                 const char* values = smem + (4 + ((j - 1) & 3)) * TILE;
                 pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
             } else {
@@ -758,6 +788,7 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
 #pragma unroll
                 for (int i = 0; i < 4 * DB; ++i) {
                     acc[i % DB] = pk_mfma(f[i & 3], pf[i / DB], acc[i % DB]);
+                    if (fine) acc[i % DB] = pk_mfma(f[i & 3], pl[i / DB], acc[i % DB]);
                     if (i + 4 < 4 * DB) read_v(i + 4);
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -788,7 +819,7 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
         const int kb = j * PG_KEYS;
         if (kb > wlast) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pf[i].u = make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < 4; ++i) pf[i].u = pl[i].u = make_uint4(0, 0, 0, 0);
             return;
         }
         if (kb + PG_KEYS - 1 > wfirst) {                     // (wave-uniform)
@@ -821,7 +852,9 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
         for (int e = 0; e < 32; e += 2) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], sc, -topsc)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][(e & 15) + 1], sc, -topsc));
             l += p0 + p1;
-            pf[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0, p1);
+            const uint32_t w = pack_bf16x2(p0, p1);
+            pf[e >> 3].w[(e & 7) >> 1] = w;
+            if (fine) pl[e >> 3].w[(e & 7) >> 1] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xFFFF0000u));
         }
     };
     // tile j has: up to two behind it, of N loads, may still be on their way
@@ -884,7 +917,9 @@ __global__ __launch_bounds__(64 * PG_WIDE) __attribute__((amdgpu_waves_per_eu(2,
     while (true) {
         const PgUnit u = pg_uniform(walk.unit());
         pg_put(walk, saved);
-        if (pg_wide<HD, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic)) (void)pg_wide<HD, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        // (trees of 48 tokens on 60000 keys with two parts throughout: 88 us and not 75)
+        const bool again = pg_two_parts(u.s, G) ? pg_wide<HD, true, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic) : pg_wide<HD, false, false>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
+        if (again) (void)pg_wide<HD, true, true>(c, a, o, u, kvh, (pk_lchar)pg_dynamic);
         pg_get(walk, saved);
         if (walk.next(c, a, G)) continue;
         pg_leave<32 * PG_WIDE>(o, &walk, &u, at, kvh);

@@ -60,6 +60,10 @@ struct PkOffsets {
     __device__ __forceinline__ PkOffsets(const PkOffsets& of, int at) : rows(of.rows + at), trans{of.trans[0] + at, of.trans[1] + at} {
         asm volatile("" : "+v"(rows), "+v"(trans[0]), "+v"(trans[1]));
     }
+    // ... from two offsets kept: the second eight positions are 8 rows on, and their chunks ^ 2
+    __device__ __forceinline__ PkOffsets(int rows_, int trans_, int at) : rows(rows_ + at), trans{trans_ + at, ((trans_ + at) ^ 32) + 8 * HD * 2} {
+        asm volatile("" : "+v"(rows), "+v"(trans[0]), "+v"(trans[1]));
+    }
     // chunk 2 ks + lane / 32 of row 32 h + lane % 32
     __device__ __forceinline__ pk_bf16x8 row(int h, int ks, int more = 0) const {
         typedef const __attribute__((address_space(3))) pk_bf16x8* ptr;
