@@ -18,6 +18,7 @@
 
 #include "packed_tiles.h"
 #include "paged.h"
+#include "paged_work.h"
 
 namespace agzo {
 
@@ -31,11 +32,9 @@ struct PgCut { PagedSeq s; int tile, parts, slot, unused[2]; };      // a row ti
 struct PgOut { float* part; float2* part_ml; PgCut* cuts; int places, least, cost; QuickDiv by_kv, by_group, by_page; };
 
 // ---- who does what -----------------------------------------------------------------------------------------------
-// A row tile's work is about the keys that its rows see: first + t step of row tile t of a sequence, so that the work in front of one is a whole number that every
-// workgroup finds alike.  Row tiles are one workgroup's each where that is about as soon done, or equal parts of each are, else the work of all of them in a row is cut into equal pieces, one to
+// Row tiles are one workgroup's each where that is about as soon done, or equal parts of each are, else the work of all of them in a row is cut into equal pieces, one to
 // each place: a workgroup then has the end of one row tile, perhaps whole ones, and the beginning of another.  (64 single tokens on 200000 keys: 219 us with shares of each
 // sequence for its own, 193 so.  Sums over the lanes by __shfl_up were most of a workgroup's start, 6 us)
-struct PgWork { int tiles, first, step; };      // of a sequence: its row tiles, the first one's work, and what each has more than the one before
 // keys that go over in the time that a row tile's start and end take.  (Without them 15 of a prompt's short first row tiles went to one workgroup, and 2500 tokens of
 // three prompts took 356 us for 293.)  Fewer where memory is busy: with few rows a piece's start is 4 to 5 us, in which a workgroup goes over 350 keys by itself and 80 among
 // 512 that share the memory's rate.  (256 throughout: 64 single tokens on 200000 keys 159 us for 156; 64 throughout: trees on 5600 keys 19.1 us for 16.8)
@@ -44,15 +43,7 @@ constexpr int pg_start(int rows, bool busy) { return rows < 128 && busy ? 64 : r
 constexpr int PG_BUSY = 1024;      // ... from so many keys a workgroup on
 
 template <int ROWS>
-__device__ __forceinline__ PgWork pg_work(const PagedAttention& a, const PagedSeq& s, int G, bool there, int start) {
-    PgWork w;
-    w.tiles = there ? (int)(((uint32_t)s.nq * (uint32_t)G + (ROWS - 1)) / ROWS) : 0;
-    w.step = a.tree ? 0 : (ROWS + G - 1) / G;
-    w.first = max((a.tree ? s.nk : s.nk - s.nq + w.step), 0) + start;
-    return w;
-}
-__device__ __forceinline__ int64_t pg_before(const PgWork& w, int t) { return (int64_t)w.first * t + (int64_t)w.step * ((int64_t)t * (t - 1) / 2); }
-__device__ __forceinline__ int pg_of(const PgWork& w, int t) { return w.first + w.step * t; }
+__device__ __forceinline__ PgWork pg_work_of(const PagedAttention& a, const PagedSeq& s, int G, bool there, int start) { return pg_work(there ? s.nq : 0, s.nk, G, ROWS, a.tree != nullptr, start); }
 
 __device__ __forceinline__ int64_t pg_lane(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
@@ -108,7 +99,7 @@ struct PgWalk {
         start_cost = 0;          // (not known yet)
         auto load = [&](int b, PagedSeq& its, PgWork& work) __attribute__((always_inline)) {
             its = paged_seq(c, a.cu_q, (int)a.total_q, min(b + lane, c.n_seq - 1));
-            work = pg_work<ROWS>(a, its, G, b + lane < c.n_seq, start_cost);
+            work = pg_work_of<ROWS>(a, its, G, b + lane < c.n_seq, start_cost);
         };
         PagedSeq its;
         PgWork work;
@@ -225,7 +216,7 @@ struct PgWalk {
     __device__ __forceinline__ void take(const PagedSeq& its, int src, int b, const PagedAttention& a, int G) {
         seq = b + src;
         s = PagedSeq{__builtin_amdgcn_readlane(its.q0, src), __builtin_amdgcn_readlane(its.nq, src), __builtin_amdgcn_readlane(its.nk, src)};
-        w = pg_work<ROWS>(a, s, G, true, start_cost);
+        w = pg_work_of<ROWS>(a, s, G, true, start_cost);
     }
     __device__ __forceinline__ PgUnit unit() const {
         PgUnit u;
@@ -255,7 +246,7 @@ struct PgWalk {
         tile = 0;
         while (++seq < c.n_seq) {
             s = paged_seq(c, a.cu_q, (int)a.total_q, __builtin_amdgcn_readfirstlane(seq));
-            w = pg_work<ROWS>(a, s, G, true, start_cost);
+            w = pg_work_of<ROWS>(a, s, G, true, start_cost);
             if (w.tiles > 0) return true;
         }
         return false;
