@@ -386,7 +386,7 @@ int agzo_glue_cache_append(agzo_ctx* ctx, const agzo_paged_cache* cache, const a
 /* attention_paged: out = softmax(scale q k^T) v for each head over the cache; q, out [n][n_heads head_dim], n_heads a multiple of n_kv_heads.  New token i of m sees its sequence's places
  * 0 .. k_len[s] - m + i; or, with tree (device int32 [n][ld_tree], tree_words of a row used, the lowest bit first), all places in front of the new ones and, of those, the ones j whose bit j is set in
  * its row (bits behind the words are not set; a token that sees itself has its own bit set).  A token that sees no place gets 0.  Keys and values that a token does not see have
- * no part in its result, whatever they are; what a page holds behind a sequence's last place is not read.  Ids in the table that are no page's are taken as the nearest.
+ * no part in its result, whatever they are, and values that it sees and that are not finite do, however small their probability; what a page holds behind a sequence's last place is not read.  Ids in the table that are no page's are taken as the nearest.
  * lse (nullable): device fp32 [n][n_heads], log sum exp of a row's scaled scores, -inf where it sees none.  Precisions as for attention over packed sequences, but for which
  *   probabilities go into the second product in two bf16 parts: those of a sequence of one new token or of up to 16 rows (its new tokens times the heads of a key head), whatever is beside it, and
  *   all of a call whose sequences have 16 rows in the mean at most.  Others are rounded to bf16 once (trees and pieces of prompts, on long caches too). Results repeat bit for bit; orders of sums go by the lengths of all sequences.

@@ -395,6 +395,14 @@ __device__ __forceinline__ bool pg_any(bool x, int* flags) {
 }
 
 // ---- with care ---------------------------------------------------------------------------------------------------
+// f x: what is not finite is so however small its weight, also where that is less than fp32 has
+__device__ __forceinline__ bool pg_finite(float x) { return fabsf(x) <= __FLT_MAX__; }
+__device__ __forceinline__ float pg_weighed(float f, float x) { return f == 0.f && !pg_finite(x) ? x : f * x; }
+// y + f x
+__device__ __forceinline__ float pg_weighed(float f, float x, float y) {
+    const float r = fmaf(f, x, y);
+    return pg_finite(r) ? r : y + pg_weighed(f, x);
+}
 // Values that are not finite, in a tile of KEYS values in LDS: in which keys there are any
 template <int HD, int KEYS>
 __device__ __forceinline__ uint64_t pg_bad_keys(const char* tile) {
@@ -581,7 +589,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+                for (int e = 0; e < 16; ++e) acc[d][e] = careful ? pg_weighed(alpha, acc[d][e]) : acc[d][e] * alpha;
             top = grown;
             topsc = to;
         }
@@ -835,7 +843,7 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+                for (int e = 0; e < 16; ++e) acc[d][e] = careful ? pg_weighed(alpha, acc[d][e]) : acc[d][e] * alpha;
             top = grown;
             topsc = to;
         }
@@ -1046,7 +1054,9 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
             const float alpha = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(topsc - to);
             l *= alpha;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[d][e] = careful ? pg_weighed(alpha, acc[d][e]) : acc[d][e] * alpha;
             top = grown;
             topsc = to;
         }
@@ -1135,7 +1145,7 @@ __device__ __forceinline__ bool pg_few(const PagedCache& c, const PagedAttention
             for (int db = 0; db < DB; ++db) {
                 const pg_floatx4 x = *reinterpret_cast<const pg_floatx4*>(sums + row * PITCH + 16 * db + 4 * g);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[db][i] = fmaf(acc[db][i], f, x[i] * g_);
+                for (int i = 0; i < 4; ++i) acc[db][i] = careful ? pg_weighed(f, acc[db][i], pg_weighed(g_, x[i])) : fmaf(acc[db][i], f, x[i] * g_);
             }
             l = fmaf(l, f, other_l * g_);
             base = both;
@@ -1202,32 +1212,41 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedCache c, PagedAtte
     if (in >= R) return;
     const int q = o.by_group(in), head = kvh * G + in - q * G;
     auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)(i == 0 ? first_slot : 2 * (p0 + i)) * c.n_kv + kvh) * ROWS + r; };
-    // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none
-    float top = -INFINITY, l = 0.f;
+    // maxima and sums by part in the lanes of the row; a part that the row sees nothing of has none, its weight is -1 here
+    float top = -INFINITY, l;
     for (int s0 = 0; s0 < parts; s0 += LANES) top = fmaxf(top, s0 + j < parts ? o.part_ml[at(s0 + j)].x : -INFINITY);
 #pragma unroll
     for (int x = LANES / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < parts; s0 += LANES) {
-        const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
-        const float f = s0 + j >= parts ? 0.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : 0.f;
-        l += f == 0.f ? 0.f : f * m.y;
-        const int n = min(LANES, parts - s0);
-        auto add = [&](int i, auto count) __attribute__((always_inline)) {
-            constexpr int N = decltype(count)::value;
-            float4 v[N];
+    float4 x;
+    auto join = [&](auto careful) __attribute__((always_inline)) {
+        x = make_float4(0.f, 0.f, 0.f, 0.f);
+        l = 0.f;
+        for (int s0 = 0; s0 < parts; s0 += LANES) {
+            const float2 m = o.part_ml[at(min(s0 + j, parts - 1))];
+            const float f = s0 + j >= parts ? -1.f : m.y != m.y ? NAN : m.x != -INFINITY ? __builtin_amdgcn_exp2f(m.x - top) : -1.f;
+            l += f <= 0.f ? 0.f : f * m.y;
+            const int n = min(LANES, parts - s0);
+            auto add = [&](int i, auto count) __attribute__((always_inline)) {
+                constexpr int N = decltype(count)::value;
+                float4 v[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
+                for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const float4*>(o.part + at(min(s0 + i + k, parts - 1)) * HD + 4 * j);
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float f_ = __shfl(f, i + k, LANES);              // (0 from the last part on)
-                if (f_ != 0.f) { x.x = fmaf(f_, v[k].x, x.x); x.y = fmaf(f_, v[k].y, x.y); x.z = fmaf(f_, v[k].z, x.z); x.w = fmaf(f_, v[k].w, x.w); }
-            }
-        };
-        if (parts <= 4) add(0, std::integral_constant<int, 4>());
-        else
-            for (int i = 0; i < n; i += 8) add(i, std::integral_constant<int, 8>());
-    }
+                for (int k = 0; k < N; ++k) {
+                    const float f_ = __shfl(f, i + k, LANES);              // (-1 from the last part on)
+                    if (f_ < 0.f) continue;
+                    if (decltype(careful)::value) x = make_float4(pg_weighed(f_, v[k].x, x.x), pg_weighed(f_, v[k].y, x.y), pg_weighed(f_, v[k].z, x.z), pg_weighed(f_, v[k].w, x.w));
+                    else x = make_float4(fmaf(f_, v[k].x, x.x), fmaf(f_, v[k].y, x.y), fmaf(f_, v[k].z, x.z), fmaf(f_, v[k].w, x.w));
+                }
+            };
+            if (parts <= 4) add(0, std::integral_constant<int, 4>());
+            else
+                for (int i = 0; i < n; i += 8) add(i, std::integral_constant<int, 8>());
+        }
+    };
+    join(std::false_type());
+    // (by the lanes of a row together: they read its maxima and sums from each other)
+    if (__builtin_amdgcn_ballot_w64(!(pg_finite(x.x) && pg_finite(x.y) && pg_finite(x.z) && pg_finite(x.w)))) join(std::true_type());
 #pragma unroll
     for (int y = LANES / 2; y > 0; y >>= 1) l += __shfl_xor(l, y);
     const bool empty = pg_empty(a, s, q);
