@@ -3,10 +3,11 @@
 // j over the keys in front of the new tokens, and of those the ones up to i, or the ones that i's bits of a tree name.
 //
 // A row is a (query, head) pair, row r of a sequence and key head being head r mod G of query r / G (G heads to a key head), so that a tile of rows is full whether it
-// holds many queries or one with its group's heads.  Products are v_mfma_f32_32x32x16_bf16, made transposed: a lane holds for one row the scores of the
-// positions 8 (e / 4) + 4 (lane / 32) + e % 4 of a block of 32 keys, and its probabilities go into the second product as they are, whose other operand is read
-// from LDS with a transposition.  Keys and values reach LDS through registers, 16 rows to a group, so that where a page's size is a multiple of 16 (WHOLE) a
-// group has one page, found by a scalar load; else every lane looks its rows' pages up.  Pages are looked up a tile ahead of the loads that they lead to.
+// holds many queries or one with its group's heads.  Products are made transposed: a lane's scores are one row's, and its probabilities go into the second product as
+// they are, whose other operand is read from LDS with a transposition.  Where 128 or 256 rows are taken together they are v_mfma_f32_32x32x16_bf16, and a lane has the positions
+// 8 (e / 4) + 4 (lane / 32) + e % 4 of a block of 32 keys; of 16 rows they are v_mfma_f32_16x16x32_bf16.  Keys and values reach LDS through registers, for 256 rows straight from
+// memory, 16 rows to a group, so that where a page's size is a multiple of 16 (WHOLE) a group has one page, found by a scalar load; else every lane looks its rows' pages up.  Pages are
+// looked up a tile ahead of the loads that they lead to.
 //
 // Lengths are on the device, so how the work is shared out is worked out there too, by every workgroup alike, and however uneven they are no workgroup has more than
 // its share: few rows on many keys (single tokens, trees) fill the device.  What several workgroups have of a row tile a second launch joins.
@@ -449,10 +450,10 @@ __device__ __forceinline__ void pg_clean(PkFrag& f) {
     }
 }
 // the second product with them taken out, its fragments of 16 positions `at` on
-template <int HD, int N>
-__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[N], const PkFrag (&low)[N], pk_floatx16 (&acc)[HD / 32]) {
+template <int HD>
+__device__ __forceinline__ void pg_second_clean(const PkOffsets<HD>& o, int at, const PkFrag (&p)[4], const PkFrag (&low)[4], pk_floatx16 (&acc)[HD / 32]) {
 #pragma unroll
-    for (int s = 0; s < N; ++s)
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int db = 0; db < HD / 32; ++db) {
             PkFrag f;
@@ -470,13 +471,13 @@ __device__ __forceinline__ bool pg_two_parts(const PagedSeq& s, int G) { return 
 
 constexpr int PG_ROWS = 32 * PG_WAVES, PG_KEYS = PK_T;      // rows of a workgroup, keys of a tile
 // Four waves of 32 rows against tiles of 64 keys that they share, two tiles of K and V in LDS, two workgroups to a compute unit, which fill each other's
-// waits: the shape of attention over packed sequences, for the same reasons.  16 trees of 30 tokens with 4 heads on each of 8 key heads, 100000 keys, 415 MB, take 110 us in both
-// launches, 3.7 TB/s; 2500 tokens behind and among 20001 keys, 235 GFLOP, 265 in this one, matrix cores busy 49 % of the time, vector instructions 51 %, mostly in turn.
+// waits: the shape of attention over packed sequences, for the same reasons.  16 trees of 30 tokens with 4 heads on each of 8 key heads, 100000 keys, 415 MB, take 109 us in both
+// launches, 3.8 TB/s; 2500 tokens behind and among 20001 keys, 235 GFLOP, 300 in this one, matrix cores busy 46 % of the time, vector instructions 49 %, mostly in turn.
 // (Products of 16 x 16 x 32: 319 us for 283 with the join.  A second 256 workgroups with less work, or with priority: no gain, or a loss)
 // The probabilities are rounded to bf16 for the second product, but for pg_two_parts.  In two parts throughout a result is off by 0.0017 of its norm and not 0.0023; 2500 tokens on 20001 keys in
-// pages of 20 then take 453 us and not 360, 900 on 1700 keys 35 and not 30, 48 single tokens' heads on two key heads, which have them, 36 and not 33.  The second part's products are a
-// pass over the values of their own: beside the first part's, a branch at each, tiles without them take 3 % longer, and in a copy of the whole pass registers are reloaded in its
-// loop (16 trees of 30 tokens 156 us and not 110)
+// pages of 20 then take 480 us and not 368, 900 on 1700 keys 34 and not 29, trees of 17 on 42000 keys 47.5 and not 42.  (32 single tokens with 96 heads on two key heads, which have
+// them: 35.6 and not 33.)  The second part's products are a pass over the values of their own: beside the first part's, a branch at each, tiles without them take 3 % longer, and with a
+// copy of the whole pass for them registers are reloaded in the loop (16 trees of 30 tokens 156 us and not 109)
 // true: stored nothing, the tiles have to be gone over with care
 template <int HD, bool WHOLE, bool careful>
 __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
@@ -612,7 +613,7 @@ __device__ __forceinline__ bool pg_forward(const PagedCache& c, const PagedAtten
         if (careful) {
             const int q = row_of_lane().q;
             const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
-            pg_second_clean<HD, 4>(of, TILE, pf, pl, acc);
+            pg_second_clean<HD>(of, TILE, pf, pl, acc);
             const char* values = smem + tile_at + TILE;
             pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
             return;
@@ -703,9 +704,10 @@ __global__ __launch_bounds__(64 * PG_WAVES) __attribute__((amdgpu_waves_per_eu(2
 // has its exponentials: the second four waves are half a tile behind, and a barrier ends each half.  Tiles go straight from memory to LDS, K's asked for by the first four waves and V's by the
 // others, three tiles ahead in rings of four (HD = 128: 96 KB on their way; a tile's place is free again before its next one is asked for, since both halves have read it a barrier
 // before).  How far loads are is waited for by their number: the compiler does not see them, and would wait for all of them in front of each read of LDS.
-// Against 128 rows with tiles through registers: 2500 tokens behind and among 20001 keys 278 -> 250 us in both launches, 940 TFLOP/s, 4096 tokens of one prompt 182 -> 168, trees of 48 tokens on 60000
-// keys 92 -> 85, of 64 on 100000 158 -> 135: keys are read by half as many row tiles.  One tile by itself takes 1.7 us and not 1.4, so that short caches are not for it (20 trees on 4200
-// keys 28 -> 33 us, two prompts' pieces on 1700 keys 23 -> 31)
+// Against 128 rows with tiles through registers: 2500 tokens behind and among 20001 keys 312 -> 277 us in both launches (260 to 285 by card), 850 TFLOP/s, 4096 tokens of one prompt
+// 161 -> 148, trees of 48 tokens on 60000 keys 88 -> 75, of 64 on 100000 155 -> 129: keys are read by half as many row tiles.  One tile by itself takes 1.7 us and not 1.4, so that short
+// caches are not for it (15 prompts' pieces on 3100 keys 17.6 -> 20.6 us, two on 1700 keys 29 -> 33).  Matrix cores are busy 51 % of the time and vector instructions 51 %: the two halves
+// do not fill each other, waves wait 28 % of theirs for loads, LDS and barriers and 29 % to issue.  With heads of 64 trees lose by it, 52 -> 59
 constexpr int PG_WIDE = 8;
 template <int HD, bool fine, bool careful>
 __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttention& a, const PgOut& o, const PgUnit& u, int kvh, pk_lchar lds) {
@@ -776,7 +778,7 @@ __device__ __forceinline__ bool pg_wide(const PagedCache& c, const PagedAttentio
             if (careful) {
                 const int q = row_of_lane().q, kb = (j - 1) * PG_KEYS;
                 const uint64_t seen = (uint64_t)pg_seen(a, s_, q, kb + 32) << 32 | pg_seen(a, s_, q, kb);
-                pg_second_clean<HD, 4>(of, 0, pf, pl, acc);
+                pg_second_clean<HD>(of, 0, pf, pl, acc);
                 const char* values = smem + (4 + ((j - 1) & 3)) * TILE;
                 pg_add_bad<HD>(values, pg_bad_keys<HD, PG_KEYS>(values), seen, acc);
             } else {
@@ -933,7 +935,7 @@ __global__ __launch_bounds__(64 * PG_WIDE) __attribute__((amdgpu_waves_per_eu(2,
 // 16 rows, in instructions of 16 x 16 x 32: lane n + 16 g has row n's scores of the keys 4 g + i and 16 + 4 g + i, and of its sums the dims 16 db + 4 g + i.
 // (32 x 32 x 16 for 16 rows too are 96 registers more, and what is then spilled into the loop makes it wait for the next tile's loads.)  The probabilities go into the second
 // product in two bf16 parts (16 bits): a row's sums are of few large probabilities often, whose roundings no others' balance.
-// 64 single tokens on 200000 keys, 820 MB: 147 us, 5.6 TB/s, where a kernel that only reads such pages gets 6.2
+// 64 single tokens on 200000 keys, 820 MB: 147 to 151 us, 5.4 to 5.6 TB/s, where a kernel that only reads such pages gets 6.2
 constexpr int PG_FEW_KEYS = 32;
 typedef float pg_floatx4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ pg_floatx4 pg_mfma16(const PkFrag& a, const PkFrag& b, const pg_floatx4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }

@@ -97,16 +97,16 @@ __device__ __forceinline__ void pk_second(const PkOffsets<HD>& o, int at, const 
 
 // The same with care: values that are not finite are taken out, and with INF, where `seen` (fragments of ones and zeros) has a one for them, the
 // sum becomes what they make of it: a product of seen with 1 for inf, 2^12 for -inf and 2^23 for NaN has at most 64 of each.  LOW: p has a
-// second part.  (16 N positions)
-template <int HD, bool INF, bool LOW, int N = 4>
-__device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag (&p)[N], const PkFrag (&low)[N], const PkFrag (&seen)[N], pk_floatx16 (&acc)[HD / 32]) {
+// second part
+template <int HD, bool INF, bool LOW>
+__device__ __forceinline__ void pk_second_careful(const char* tile, const PkFrag (&p)[4], const PkFrag (&low)[4], const PkFrag (&seen)[4], pk_floatx16 (&acc)[HD / 32]) {
     const int lane = threadIdx.x & 63, hi = lane >> 5;
 #pragma unroll
     for (int db = 0; db < HD / 32; ++db) {
         const int dim = 32 * db + (lane & 31);
         pk_floatx16 c = {};
 #pragma unroll
-        for (int s = 0; s < N; ++s) {
+        for (int s = 0; s < 4; ++s) {
             PkFrag f, k;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {

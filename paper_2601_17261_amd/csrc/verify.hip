@@ -8,12 +8,13 @@
 // as the first x whose sum of w up to it exceeds u times all of them.  Each accepted token then has the target's distribution: what a refusal leaves out of it, the
 // last draw makes up for.
 //
-// Products, differences and sums are fp64: differences of fp32 values are exact there, and a draw's border is off by 2^-50 of the sum, so that the choice is that
-// of the exact sums but for one draw in 10^13 or so.
+// Products, differences and sums are fp64: a difference is rounded to 2^-53 of itself, and with 131072 tokens a sum has passed fewer than 40 roundings, so that a border and the sum that is
+// held against it are off by less than 2^-47 of all.  The choice then is that of the exact sums but where a border is that near a token's, two draws in 10^9 at most.
 //
 // One row (two in a chain) of each sequence is read whole, which is what bounds it; the walk before that is a chain of three loads, and every workgroup makes it again
-// by itself: a launch of its own would take longer.  64 chains of eight drafted tokens, 131072 fp32 probabilities a row, 67 MB: 12.3 us for the sums, 5.5 TB/s, 3.4 for the draw,
-// which is three rounds of dependent loads; 12 trees of 48 with 32011: 5.1 and 3.5, the walk's and the draw's chains.
+// by itself: a launch of its own would take longer.  64 chains of eight drafted tokens, 131072 fp32 probabilities a row, 67 MB: 13 to 14.5 us for the sums, 4.6 to 5.1 TB/s, 3 to 4 for the
+// draw, which is three rounds of dependent loads; 12 trees of 48 with 32011: 5.2 and 3 to 4, the walk's and the draw's chains.  But where no weight is left, which takes probabilities that do
+// not add up to 1, a draw's threads sum pieces of the target's row by themselves: a call then takes 90 us with 32011 tokens, 111 with 131072, 12.5 ms with 2^24.
 #include "agzo_internal.h"
 
 namespace agzo {
