@@ -389,7 +389,7 @@ int agzo_glue_cache_append(agzo_ctx* ctx, const agzo_paged_cache* cache, const a
  * no part in its result, whatever they are, and values that it sees and that are not finite do, however small their probability; what a page holds behind a sequence's last place is not read.  Ids in the table that are no page's are taken as the nearest.
  * lse (nullable): device fp32 [n][n_heads], log sum exp of a row's scaled scores, -inf where it sees none.  Precisions as for attention over packed sequences, but for which
  *   probabilities go into the second product in two bf16 parts: those of a sequence of one new token or of up to 16 rows (its new tokens times the heads of a key head), whatever is beside it, and
- *   all of a call whose sequences have 16 rows in the mean at most.  Others are rounded to bf16 once (trees and pieces of prompts, on long caches too). Results repeat bit for bit; orders of sums go by the lengths of all sequences.
+ *   all of a call of 16 n_seq rows at most.  Others are rounded to bf16 once (trees and pieces of prompts, on long caches too). Results repeat bit for bit; orders of sums go by the lengths of all sequences.
  * Errors also: scale not finite or below 2^-100, n times the heads of a key head from 2^31 - 1024 on, 2^24 tiles of rows and more, q's leading dimension from 2^22 on. */
 int agzo_glue_attention_paged(agzo_ctx* ctx, const agzo_paged_cache* cache, const void* q, int64_t ldq, const int32_t* cu_q, int64_t n, int32_t n_heads, float scale, const int32_t* tree,
                               int64_t ld_tree, int32_t tree_words, void* out, int64_t ldo, float* lse);
